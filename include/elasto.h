@@ -434,6 +434,151 @@ elasto_status_t elasto_op_conv2d(const void* x, int32_t batch, int32_t H, int32_
                                  const void* w, int64_t ldw, int64_t wseg, const float* bias,
                                  void* y, int64_t ldy, int32_t n, int32_t relu, void* hip_stream);
 
+/* ------------------------------------------- operators on token sequences */
+/* A [batch][tokens][heads][head_dim] tensor in device memory: the features of
+ * a head are contiguous, the other axes have strides in elements of any
+ * order (so q, k and v may lie head by head in one buffer, as the q/k/v
+ * projection writes them: head_stride 3 * head_dim, token_stride qkv_stride;
+ * or in a cache of [batch][kv_heads][capacity][head_dim]).  data and every
+ * stride are multiples of 16 bytes.  Strides of tensors that are written are
+ * at least head_dim along axes longer than 1; rows of one tensor must not
+ * overlap, nor written tensors others unless stated. */
+typedef struct {
+  void* data;
+  int64_t batch_stride, token_stride, head_stride;
+} elasto_heads_t;
+
+/* Norms of queries and keys for each head, with the position rotation in the
+ * same pass, as transformers put them between the q/k/v projection and the
+ * attention.  For every head vector x of q and of k:
+ *   u = x / sqrt(mean(x^2) + eps),  y = gamma (.) u (gamma NULL: y = u),
+ *   out = y with the first rot_dim features turned in pairs (a, b) to
+ *   (a c - b s, b c + a s), where c and s are row `position` of cos and sin:
+ *   pair f is features (f, f + rot_dim / 2), or, interleaved, (2f, 2f + 1).
+ * Tables of a grid's coordinates give a two-dimensional rotation; rot_dim = 0
+ * leaves the norm alone.  The position of token t of sequence b is
+ * positions[b * tokens + t], or t where positions is NULL; a position outside
+ * [0, table_rows) makes the rotated features NaN.  lens (or NULL): tokens t >=
+ * lens[b] are neither read nor written and add nothing to the gradients.
+ * BF16: q and k in bf16, everything between load and store in fp32, rounded
+ * once; FP32: fp32 throughout.
+ * Needs head_dim a multiple of 16 in [16, 256], rot_dim a multiple of 16 in
+ * [0, head_dim], eps > 0, batch, tokens, q_heads and kv_heads >= 0 with at
+ * least one head (a side of no heads takes NULL tensors). */
+typedef struct {
+  int32_t dtype, batch, tokens, q_heads, kv_heads, head_dim;
+  int32_t rot_dim, interleaved, table_rows;
+  float eps;
+  const int32_t* positions; /* device [batch][tokens] or NULL                  */
+  const int32_t* lens;      /* device [batch] or NULL                          */
+  const float *cos, *sin;   /* device [table_rows][rot_dim / 2]                */
+  const float *q_gamma, *k_gamma; /* device [head_dim] or NULL                 */
+} elasto_qk_norm_t;
+
+/* q_out and k_out may be q and k themselves (same pointer and strides). */
+elasto_status_t elasto_op_qk_norm_rotate(const elasto_qk_norm_t* desc, const elasto_heads_t* q,
+                                         const elasto_heads_t* k, const elasto_heads_t* q_out,
+                                         const elasto_heads_t* k_out, void* hip_stream);
+
+/* The gradients: dq and dk of q and k from those of the results, dq_out and
+ * dk_out, and, where the pointers are given, the weights' (fp32 [head_dim],
+ * summed over tokens and heads in a fixed order).  q and k are the forward's
+ * inputs.  dq and dk may be dq_out and dk_out themselves.  The workspace
+ * (elasto_qk_norm_rotate_workspace, 16-byte aligned) is needed where a weight
+ * gradient is asked for; it is free again when the call's work is done. */
+elasto_status_t elasto_op_qk_norm_rotate_bwd(const elasto_qk_norm_t* desc, const elasto_heads_t* q,
+                                             const elasto_heads_t* k, const elasto_heads_t* dq_out,
+                                             const elasto_heads_t* dk_out, const elasto_heads_t* dq,
+                                             const elasto_heads_t* dk, float* dq_gamma,
+                                             float* dk_gamma, void* workspace,
+                                             int64_t workspace_bytes, void* hip_stream);
+elasto_status_t elasto_qk_norm_rotate_workspace(const elasto_qk_norm_t* desc, int64_t* bytes);
+
+/* Attention in a sliding window, with a few first tokens (sinks) that stay
+ * visible, for sequences of any length.  Sequence b has k_lens[b] keys and
+ * q_lens[b] queries (NULL: k_tokens and q_tokens; lengths are clamped to
+ * those); its queries are the last of its positions: query i stands at
+ * p = i + k_lens[b] - q_lens[b], key j at j.  p sees key j if
+ *   |p - j| < window or j < sinks, and, where causal is set, j <= p,
+ * so one new token against a cache is q_tokens = 1 with the cache's lengths,
+ * and a window of at least k_tokens is plain attention.  With that mask
+ *   o_i = sum_j softmax_j(scale q_i . k_j) v_j,
+ *   lse_i = log sum_j exp(scale q_i . k_j)   (fp32 [batch][heads][q_tokens]).
+ * A query that sees no key gets o = 0 and lse = -infinity.  Query head h reads
+ * key head h / (heads / kv_heads).  What lies behind a sequence's lengths is
+ * neither used (it may be anything, NaN included) nor written.
+ * BF16: products of bf16 with fp32 sums, softmax statistics in fp32, the
+ * probabilities (backward: also the gradients of the scores) rounded to bf16
+ * for the products that sum them.  FP32: fp32 throughout.  Results are the
+ * same bits every time.
+ * Needs head_dim 64 or 128, heads a multiple of kv_heads, window >= 1,
+ * 0 <= sinks <= 64, scale > 0; k_tokens, q_tokens * heads / kv_heads and
+ * batch * heads at most 2^29. */
+typedef struct {
+  int32_t dtype, batch, q_tokens, k_tokens, heads, kv_heads, head_dim;
+  int32_t causal, window, sinks;
+  float scale;
+  const int32_t *q_lens, *k_lens; /* device [batch] or NULL */
+} elasto_window_t;
+
+/* lse may be NULL.  The workspace (256-byte aligned; 0 bytes for launches that
+ * fill the GPU by themselves) is free again when the call's work is done:
+ * calls that may overlap need one each. */
+elasto_status_t elasto_op_window_attention(const elasto_window_t* desc, const elasto_heads_t* q,
+                                           const elasto_heads_t* k, const elasto_heads_t* v,
+                                           const elasto_heads_t* o, float* lse, void* workspace,
+                                           int64_t workspace_bytes, void* hip_stream);
+
+/* The gradients of q, k and v (of a shared key head: summed over its query
+ * heads) from dout, with the forward's o and lse.  Keys that no query sees get
+ * zeros. */
+elasto_status_t elasto_op_window_attention_bwd(const elasto_window_t* desc, const elasto_heads_t* q,
+                                               const elasto_heads_t* k, const elasto_heads_t* v,
+                                               const elasto_heads_t* o, const float* lse,
+                                               const elasto_heads_t* dout, const elasto_heads_t* dq,
+                                               const elasto_heads_t* dk, const elasto_heads_t* dv,
+                                               void* workspace, int64_t workspace_bytes,
+                                               void* hip_stream);
+/* Bytes of workspace of either call: of the shapes alone, not of the lengths. */
+elasto_status_t elasto_window_attention_workspace(const elasto_window_t* desc, int32_t backward,
+                                                  int64_t* bytes);
+
+/* The `top` largest logits of each row, largest first, the lower class first
+ * among equal ones (NaN counts as larger than any number, -0 equals 0): what
+ * a teacher's answer is reduced to for elasto_op_distill.  logits row r starts
+ * at logits + r * ld (any ld >= classes, any alignment of the type); values
+ * fp32 and indices int32, [rows][top] contiguous.  1 <= top <= min(256,
+ * classes), classes <= 2^30. */
+elasto_status_t elasto_op_top_logits(int32_t dtype, const void* logits, int64_t ld, int64_t rows,
+                                     int32_t classes, int32_t top, float* values, int32_t* indices,
+                                     void* hip_stream);
+
+/* Distillation from a teacher's largest logits, mixed with the cross-entropy
+ * of labels.  Row r's teacher entries are teacher_values[r * top + i] (fp32) at
+ * classes teacher_indices[r * top + i]; with p = softmax(values / temperature)
+ * over the row's entries and z the row of student logits,
+ *   loss[r] = alpha * temperature^2 * sum_i p_i (log p_i
+ *               - log softmax(z / temperature)[index_i])
+ *             + (1 - alpha) * (log sum exp(z) - z[label]),
+ * and, where dlogits is given, its gradient with respect to z times
+ * scale * row_weight[r] (row_weight NULL: 1) in dlogits row r, row stride ldg,
+ * of type grad_dtype.  An index of -1 is an entry that is not there; a class
+ * may come more than once.  A row without entries (or whose values are all
+ * -infinity) has no teacher part.  Another index outside [0, classes), or such
+ * a label, makes the row's loss NaN (it adds nothing to the gradient).  A row
+ * of weight 0 is not read: its loss and gradient are 0.
+ * labels may be NULL with alpha = 1; with alpha = 0 top may be 0 and the call
+ * is the cross-entropy.  dlogits may be logits itself (same type and stride).
+ * fp32 between load and store, sums in fp32 in a fixed order.  Needs top <=
+ * 256, temperature > 0, alpha in [0, 1], scale finite, classes <= 2^30. */
+elasto_status_t elasto_op_distill(int32_t dtype, const void* logits, int64_t ld, int64_t rows,
+                                  int32_t classes, const float* teacher_values,
+                                  const int32_t* teacher_indices, int32_t top,
+                                  const int32_t* labels, const float* row_weight,
+                                  float temperature, float alpha, float scale, float* loss,
+                                  int32_t grad_dtype, void* dlogits, int64_t ldg,
+                                  void* hip_stream);
+
 /* ================================================ growth step (Section 4.2) */
 /* Growing DN mode k re-introduces the weights mode k holds and the next
  * smaller mode k + 1 (the previous level) lacks; mode k + 1's weights are
@@ -470,6 +615,19 @@ elasto_status_t elasto_growth_destroy(elasto_growth_t g);
 elasto_status_t elasto_growth_step(elasto_growth_t g, int32_t mode, const void* images,
                                    const int32_t* labels, int32_t batch, float lr,
                                    float clip_norm, float* stats, void* hip_stream);
+
+/* elasto_growth_step with the loss of elasto_op_distill in the place of the
+ * cross-entropy: DN mode k learns from a wider one (or any other teacher).
+ * teacher_values and teacher_indices are device [batch][top], as
+ * elasto_op_top_logits leaves them from the teacher's logits (elasto_set_mode
+ * to the teacher, elasto_forward, elasto_op_top_logits); labels may be NULL
+ * with alpha = 1.  The step's loss (stats[0]) is the mean over the batch.
+ * Everything else as for elasto_growth_step. */
+elasto_status_t elasto_growth_step_distill(elasto_growth_t g, int32_t mode, const void* images,
+                                           const int32_t* labels, const float* teacher_values,
+                                           const int32_t* teacher_indices, int32_t top,
+                                           float temperature, float alpha, int32_t batch, float lr,
+                                           float clip_norm, float* stats, void* hip_stream);
 
 /* Synchronous copy to host memory: which = 0 the handle's packed weights
  * (elasto_packed_bytes long), which = 1 the fp32 masters (one float per

@@ -1,0 +1,341 @@
+// Distillation from a teacher's largest logits, mixed with the cross-entropy of
+// labels: the row losses and, in the same call, the gradient of the student's
+// logits z.  With the teacher's values t_i at classes c_i, i < top, temperature
+// tau and p = softmax(t / tau) over the entries given:
+//   loss = alpha tau^2 sum_i p_i (log p_i - log softmax(z / tau)[c_i])
+//          + (1 - alpha) (lse(z) - z_label),
+//   dz_j = w (alpha tau (softmax(z / tau)_j - sum of p_i with c_i = j)
+//          + (1 - alpha) (softmax(z)_j - [j = label])),
+// w the row's weight.  The full softmax enters the gradient of every class, the
+// teacher and the label only top + 1 of them.
+//
+// One workgroup a row.  A first walk takes the maximum and the sums of both
+// temperatures together, a second one writes the gradient; the row comes from
+// memory once, the second time from the caches behind L2.  The top + 1 special
+// classes are then written again by the threads that hold them, from their
+// logits gathered before: each sums what all entries of its class take off (a
+// class may come twice), so no order of atomics enters.
+//
+// Bound by memory: the logits once, the gradient once.
+#include <math.h>
+
+#include "distill.h"
+#include "growth_step.h"
+#include "heads.h"
+#include "logits.h"
+
+namespace elasto {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+template <typename T, typename G>
+struct DistillP {
+  const T* logits;
+  int64_t ld;
+  const float* teacher;
+  const int32_t* index;
+  const int32_t* labels;
+  const float* weight;
+  float* loss;
+  G* grad;  // NULL: the loss alone
+  int64_t ldg;
+  int C, top;
+  float alpha, beta;  // of the teacher's and of the labels' part
+  float tau, scale;
+};
+
+// A running maximum of x and sums of 2^(c (x - max)) for two factors c.
+struct Sums {
+  float m, a, b;
+};
+__device__ __forceinline__ void merge(Sums& s, float m, float a, float b, float ca, float cb) {
+  const float t = fmaxf(s.m, m), base = t == -INFINITY ? 0.0f : t;
+  const float fs = s.m - base, fo = m - base;
+  s.a = s.a * __builtin_amdgcn_exp2f(fs * ca) + a * __builtin_amdgcn_exp2f(fo * ca);
+  s.b = s.b * __builtin_amdgcn_exp2f(fs * cb) + b * __builtin_amdgcn_exp2f(fo * cb);
+  s.m = t;
+}
+
+// TWO: the sums of both temperatures are needed and differ.
+template <typename T, typename G, int N, bool TWO>
+__global__ __launch_bounds__(N) void distill_kernel(DistillP<T, G> p) {
+  constexpr int W = N / 64;
+  __shared__ float red[W][4];
+  __shared__ float amount[kMaxTop + 1];  // what entry i takes off its class
+  __shared__ int where[kMaxTop + 1];     // its class, -1: none
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t r = blockIdx.x;
+  const T* z = p.logits + r * p.ld;
+  const int C = p.C;
+  const float weight = (p.weight ? p.weight[r] : 1.0f);
+  G* g = p.grad ? p.grad + r * p.ldg : nullptr;
+  if (weight == 0.0f) {  // a row left out: its logits are not read
+    if (g)
+      for (int i = tid; i < C; i += N) store1(g + i, 0.0f);
+    if (tid == 0) p.loss[r] = 0.0f;
+    return;
+  }
+  const float w = weight * p.scale;
+  const float ct = kLog2e / p.tau;
+  const RowSpan<T> span(z, C);
+
+  // The special classes: teacher entries, then the label.
+  int cls = -1;
+  bool bad = false;
+  float tv = -INFINITY, zs = 0.0f;
+  if (tid < p.top) {
+    const int c = p.index[r * p.top + tid];
+    bad = c < -1 || c >= C;
+    if (c >= 0 && c < C) {
+      cls = c;
+      tv = p.teacher[r * p.top + tid] / p.tau;
+      bad = tv != tv;
+    }
+  } else if (tid == p.top && p.labels) {
+    const int c = p.labels[r];
+    bad = c < 0 || c >= C;
+    if (!bad) cls = c;
+  }
+  if (cls >= 0) zs = load1(z + cls);
+
+  // One walk: maximum and sums.
+  Sums s = {-INFINITY, 0.0f, 0.0f};
+  auto add = [&](float x, float base) {
+    s.a += __builtin_amdgcn_exp2f((x - base) * ct);
+    if constexpr (TWO) s.b += __builtin_amdgcn_exp2f((x - base) * kLog2e);
+  };
+  auto raise = [&](float t) {
+    if (t > s.m) {
+      const float d = s.m - t;
+      s.a *= __builtin_amdgcn_exp2f(d * ct);
+      if constexpr (TWO) s.b *= __builtin_amdgcn_exp2f(d * kLog2e);
+      s.m = t;
+    }
+    return s.m == -INFINITY ? 0.0f : s.m;
+  };
+  walk_row<N>(z, span, tid,
+              [&](int, const float* v) {
+                float t = v[0];
+#pragma unroll
+                for (int e = 1; e < 8; ++e) t = fmaxf(t, v[e]);
+                const float base = raise(t);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) add(v[e], base);
+              },
+              [&](int, float v) { add(v, raise(v)); });
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1)
+    merge(s, __shfl_xor(s.m, o, 64), __shfl_xor(s.a, o, 64), __shfl_xor(s.b, o, 64), ct, kLog2e);
+  // The teacher's maximum goes along.
+  const float tw = wave_max(tv);
+  if (lane == 0) {
+    red[wave][0] = s.m;
+    red[wave][1] = s.a;
+    red[wave][2] = s.b;
+    red[wave][3] = tw;
+  }
+  const bool any_bad = __syncthreads_or(bad);
+  s = Sums{red[0][0], red[0][1], red[0][2]};
+  float tm = red[0][3];
+#pragma unroll
+  for (int i = 1; i < W; ++i) {
+    merge(s, red[i][0], red[i][1], red[i][2], ct, kLog2e);
+    tm = fmaxf(tm, red[i][3]);
+  }
+  __syncthreads();
+  if constexpr (!TWO) s.b = s.a;  // tau 1, or one of the two not needed
+
+  // Teacher probabilities and the row's loss.
+  const float te = tid < p.top && tm > -INFINITY ? __builtin_amdgcn_exp2f((tv - tm) * kLog2e) : 0.0f;
+  const float ts = wave_sum(te);
+  if (lane == 0) red[wave][0] = ts;
+  __syncthreads();
+  float tsum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < W; ++i) tsum += red[i][0];
+  __syncthreads();
+  const bool taught = p.alpha > 0.0f && tm > -INFINITY;  // the teacher gives the row something
+  const float prob = taught ? te / tsum : 0.0f;
+  const float la = log2f(s.a) * kLn2, lb = log2f(s.b) * kLn2;  // of the sums about the maximum
+  float part = 0.0f;
+  if (tid < p.top) {
+    // log p - log q, each from differences to its own maximum.
+    if (prob > 0.0f || prob != prob)
+      part = p.alpha * p.tau * p.tau * prob *
+             ((tv - tm) - log2f(tsum) * kLn2 - ((zs - s.m) / p.tau - la));
+  } else if (tid == p.top && p.beta > 0.0f) {
+    part = p.beta * (lb - (zs - s.m));
+  }
+  const float total = wave_sum(part);
+  if (lane == 0) red[wave][0] = total;
+  if (tid <= p.top) {
+    where[tid] = cls;
+    amount[tid] = tid < p.top ? p.alpha * p.tau * prob : p.beta;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    float sum = 0.0f;
+    for (int i = 0; i < W; ++i) sum += red[i][0];
+    p.loss[r] = any_bad ? NAN : sum;
+  }
+  if (!g) return;
+
+  // The gradient: fa 2^((z - m) ct) + fb 2^((z - m) log2 e), factors of both sums.
+  const float fa = taught ? p.alpha * p.tau / s.a : 0.0f;
+  const float fb = p.labels ? p.beta / s.b : 0.0f;
+  const float m = s.m;
+  auto value = [&](float x) {
+    if constexpr (TWO)
+      return fmaf(fa, __builtin_amdgcn_exp2f((x - m) * ct), fb * __builtin_amdgcn_exp2f((x - m) * kLog2e));
+    else
+      return (fa + fb) * __builtin_amdgcn_exp2f((x - m) * ct);
+  };
+  const bool wide = (reinterpret_cast<uintptr_t>(g + span.head) & 15) == 0;
+  walk_row<N>(z, span, tid,
+              [&](int i, const float* v) {
+                float o[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = value(v[e]) * w;
+                if (wide) {
+                  store8(g + i, o);
+                } else {
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) store1(g + i + e, o[e]);
+                }
+              },
+              [&](int i, float v) { store1(g + i, value(v) * w); });
+  __syncthreads();  // the special classes' values go over those
+  if (tid <= p.top && cls >= 0) {
+    float off = 0.0f;
+    bool first = true;
+    for (int i = 0; i <= p.top; ++i)
+      if (where[i] == cls) {
+        if (i < tid) first = false;
+        off += amount[i];
+      }
+    if (first) store1(g + cls, (value(zs) - off) * w);
+  }
+}
+
+template <typename T, typename G, int N>
+hipError_t launch(const DistillArgs& a, hipStream_t s) {
+  DistillP<T, G> p;
+  p.logits = static_cast<const T*>(a.logits);
+  p.ld = a.ld;
+  p.teacher = a.values;
+  p.index = a.indices;
+  p.labels = a.labels;
+  p.weight = a.row_weight;
+  p.loss = a.loss;
+  p.grad = static_cast<G*>(a.dlogits);
+  p.ldg = a.ldg;
+  p.C = a.classes;
+  p.top = a.top;
+  p.alpha = a.alpha;
+  p.beta = a.labels ? 1.0f - a.alpha : 0.0f;
+  p.tau = a.temperature;
+  p.scale = a.scale;
+  // With no labels, or none of the teacher, one sum does: at the temperature
+  // that is needed.
+  if (a.alpha == 0.0f) p.tau = 1.0f;
+  const bool two = a.labels && a.alpha > 0.0f && a.alpha < 1.0f && p.tau != 1.0f;
+  if (two)
+    hipLaunchKernelGGL((distill_kernel<T, G, N, true>), dim3((unsigned)a.rows), dim3(N), 0, s, p);
+  else
+    hipLaunchKernelGGL((distill_kernel<T, G, N, false>), dim3((unsigned)a.rows), dim3(N), 0, s, p);
+  return hipGetLastError();
+}
+
+template <typename T, typename G>
+hipError_t launch_threads(const DistillArgs& a, hipStream_t s) {
+  return a.classes >= 8192 ? launch<T, G, 1024>(a, s) : launch<T, G, 512>(a, s);
+}
+
+}  // namespace
+
+bool check_distill(const DistillArgs& a) {
+  const int es = a.dtype == ELASTO_BF16 ? 2 : 4, gs = a.grad_dtype == ELASTO_BF16 ? 2 : 4;
+  if ((a.dtype != ELASTO_BF16 && a.dtype != ELASTO_FP32) ||
+      (a.grad_dtype != ELASTO_BF16 && a.grad_dtype != ELASTO_FP32))
+    return fail(ELASTO_ERR_INVALID_ARG, "distill: bad dtype %d or %d", a.dtype, a.grad_dtype), false;
+  if (a.rows < 0 || a.rows > 0x7fffffff || a.classes < 1 || a.classes > (1 << 30) || a.ld < a.classes ||
+      (a.dlogits && a.ldg < a.classes))
+    return fail(ELASTO_ERR_INVALID_ARG, "distill: bad rows, classes or row strides"), false;
+  if (a.top < 0 || a.top > kMaxTop)
+    return fail(ELASTO_ERR_INVALID_ARG, "distill: top %d outside [0, %d]", a.top, kMaxTop), false;
+  if (!(a.temperature > 0.0f) || !(a.temperature < INFINITY) || !(a.alpha >= 0.0f) || !(a.alpha <= 1.0f) ||
+      !(fabsf(a.scale) < INFINITY))
+    return fail(ELASTO_ERR_INVALID_ARG, "distill: needs temperature > 0, alpha in [0, 1] and a finite scale"), false;
+  if (a.alpha > 0.0f && a.top == 0)
+    return fail(ELASTO_ERR_INVALID_ARG, "distill: alpha > 0 needs teacher entries"), false;
+  if (a.rows == 0) return true;
+  if (!a.logits || !a.loss || (a.top > 0 && (!a.values || !a.indices)))
+    return fail(ELASTO_ERR_INVALID_ARG, "distill: NULL pointer"), false;
+  if (a.alpha < 1.0f && !a.labels) return fail(ELASTO_ERR_INVALID_ARG, "distill: alpha < 1 needs labels"), false;
+  if (!aligned(a.logits, es) || !aligned(a.dlogits, gs) || !aligned(a.loss, 4) || !aligned(a.values, 4) ||
+      !aligned(a.indices, 4) || !aligned(a.labels, 4) || !aligned(a.row_weight, 4))
+    return fail(ELASTO_ERR_INVALID_ARG, "distill: misaligned pointer"), false;
+  if (a.dlogits == a.logits && (a.dtype != a.grad_dtype || a.ld != a.ldg))
+    return fail(ELASTO_ERR_INVALID_ARG, "distill: dlogits over logits needs the same type and row stride"), false;
+  return true;
+}
+
+hipError_t launch_distill(const DistillArgs& a, hipStream_t s) {
+  if (a.rows == 0) return hipSuccess;
+  if (a.dtype == ELASTO_BF16)
+    return a.grad_dtype == ELASTO_BF16 ? launch_threads<uint16_t, uint16_t>(a, s)
+                                       : launch_threads<uint16_t, float>(a, s);
+  return a.grad_dtype == ELASTO_BF16 ? launch_threads<float, uint16_t>(a, s)
+                                     : launch_threads<float, float>(a, s);
+}
+
+}  // namespace elasto
+
+using namespace elasto;
+
+extern "C" elasto_status_t elasto_op_distill(int32_t dtype, const void* logits, int64_t ld, int64_t rows,
+                                             int32_t classes, const float* teacher_values,
+                                             const int32_t* teacher_indices, int32_t top,
+                                             const int32_t* labels, const float* row_weight,
+                                             float temperature, float alpha, float scale, float* loss,
+                                             int32_t grad_dtype, void* dlogits, int64_t ldg,
+                                             void* hip_stream) {
+  DistillArgs a;
+  a.dtype = dtype; a.logits = logits; a.ld = ld; a.rows = rows; a.classes = classes;
+  a.values = teacher_values; a.indices = teacher_indices; a.top = top; a.labels = labels;
+  a.row_weight = row_weight; a.temperature = temperature; a.alpha = alpha; a.scale = scale;
+  a.loss = loss; a.grad_dtype = grad_dtype; a.dlogits = dlogits; a.ldg = ldg;
+  if (!check_distill(a)) return ELASTO_ERR_INVALID_ARG;
+  const hipError_t e = launch_distill(a, static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return fail(ELASTO_ERR_HIP, "distill: %s", hipGetErrorString(e));
+  return ELASTO_OK;
+}
+
+extern "C" elasto_status_t elasto_growth_step_distill(elasto_growth_t g, int32_t mode, const void* images,
+                                                      const int32_t* labels, const float* teacher_values,
+                                                      const int32_t* teacher_indices, int32_t top,
+                                                      float temperature, float alpha, int32_t batch,
+                                                      float lr, float clip_norm, float* stats,
+                                                      void* hip_stream) {
+  if (!g) return fail(ELASTO_ERR_INVALID_ARG, "context is NULL");
+  DistillArgs a;
+  a.dtype = ELASTO_FP32; a.grad_dtype = ELASTO_BF16;
+  a.values = teacher_values; a.indices = teacher_indices; a.top = top; a.labels = labels;
+  a.temperature = temperature; a.alpha = alpha;
+  // What the step itself fills in is checked there; here the caller's part.
+  a.logits = a.loss = reinterpret_cast<float*>(256);
+  a.rows = a.classes = a.ld = 1;
+  if (!check_distill(a)) return ELASTO_ERR_INVALID_ARG;
+  const GrowthLoss loss = {"distillation loss",
+                           [](const void* args, const GrowthLogits& z, hipStream_t s) {
+                             DistillArgs d = *static_cast<const DistillArgs*>(args);
+                             d.logits = z.logits; d.ld = z.ld; d.rows = z.batch; d.classes = z.classes;
+                             d.loss = z.rowloss; d.dlogits = z.dlogits; d.ldg = z.ldg;
+                             d.scale = 1.0f / (float)z.batch;
+                             return launch_distill(d, s);
+                           },
+                           &a};
+  return growth_step(g, mode, images, batch, lr, clip_norm, stats, hip_stream, loss);
+}

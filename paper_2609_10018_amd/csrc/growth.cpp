@@ -7,7 +7,7 @@
 //   u1 / u2, qkv, the attention output o, the mid-block stream Xm_l, and the
 //   fc1 pre-activation and GELU output; the residual stream is bf16 in all
 //   rows (class rows included);
-//   cross-entropy -> dlogits; head backward -> d(class LN output);
+//   the loss (cross-entropy, or a given one) -> dlogits; head backward -> d(class LN output);
 //   final LN backward into the fp32 stream gradient dX (class rows);
 //   per layer, last to first:
 //     fc2:  dh = (dX W2[:, :m]) * GELU'(pre)     (GEMM, GELU' epilogue)
@@ -34,6 +34,7 @@
 #include <new>
 #include <vector>
 
+#include "growth_step.h"
 #include "handle.h"
 #include "kernels.h"
 #include "layout.h"
@@ -322,8 +323,28 @@ elasto_status_t elasto_growth_step(elasto_growth_t g, int32_t mode, const void* 
                                    const int32_t* labels, int32_t batch, float lr,
                                    float clip_norm, float* stats, void* hip_stream) {
   if (!g) return fail(ELASTO_ERR_INVALID_ARG, "context is NULL");
-  elasto_handle_s* h = g->h;
   if (!images || !labels) return fail(ELASTO_ERR_INVALID_ARG, "images / labels is NULL");
+  if (!aligned(labels, 4)) return fail(ELASTO_ERR_INVALID_ARG, "misaligned pointer");
+  const GrowthLoss loss = {"cross-entropy",
+                           [](const void* y, const GrowthLogits& z, hipStream_t s) {
+                             return launch_cross_entropy(z.logits, z.ld, static_cast<const int32_t*>(y),
+                                                         z.classes, z.batch, z.dlogits, z.ldg,
+                                                         z.rowloss, s);
+                           },
+                           labels};
+  return growth_step(g, mode, images, batch, lr, clip_norm, stats, hip_stream, loss);
+}
+
+}  // extern "C"
+
+namespace elasto {
+
+elasto_status_t growth_step(elasto_growth_t g, int32_t mode, const void* images, int32_t batch,
+                            float lr, float clip_norm, float* stats, void* hip_stream,
+                            const GrowthLoss& loss) {
+  if (!g) return fail(ELASTO_ERR_INVALID_ARG, "context is NULL");
+  elasto_handle_s* h = g->h;
+  if (!images) return fail(ELASTO_ERR_INVALID_ARG, "images is NULL");
   if (batch < 1 || batch > g->max_batch)
     return fail(ELASTO_ERR_BATCH_RANGE, "batch %d outside [1, %d]", batch, g->max_batch);
   if (mode < 0 || mode + 1 >= h->num_modes)
@@ -331,7 +352,7 @@ elasto_status_t elasto_growth_step(elasto_growth_t g, int32_t mode, const void* 
   const char* why = nullptr;
   if (!growable(h, mode, &why)) return fail(ELASTO_ERR_BAD_TABLE, "%s", why);
   if (!isfinite(lr) || !(clip_norm > 0.0f)) return fail(ELASTO_ERR_INVALID_ARG, "lr must be finite, clip_norm > 0");
-  if (!aligned(images, 16) || !aligned(labels, 4) || (stats && !aligned(stats, 4)))
+  if (!aligned(images, 16) || (stats && !aligned(stats, 4)))
     return fail(ELASTO_ERR_INVALID_ARG, "misaligned pointer");
   int cur = -1;
   if (hipGetDevice(&cur) != hipSuccess || cur != h->device) {
@@ -405,8 +426,10 @@ elasto_status_t elasto_growth_step(elasto_growth_t g, int32_t mode, const void* 
         "head");
 
   // ------------------------------------------------------------ backward
-  G_TRY(launch_cross_entropy(g->logits, g->ldlogits, labels, C, batch, g->dlog, g->ldlog,
-                             g->rowloss, s), "cross-entropy");
+  {
+    const GrowthLogits z = {g->logits, g->ldlogits, g->dlog, g->ldlog, g->rowloss, C, batch};
+    G_TRY(loss.launch(loss.args, z, s), "%s", loss.name);
+  }
   G_TRY(launch_transposes_bf16(plan.jobs, plan.njobs, plan.job_tiles, h->dw, g->WT, s),
         "weight transposes");
   G_TRY(launch_gemm_bf16(Epi::Bias, gemm(Epi::Bias, g->dlog, g->ldlog, g->WT + g->wt_head, g->ldlog,
@@ -473,4 +496,4 @@ elasto_status_t elasto_growth_step(elasto_growth_t g, int32_t mode, const void* 
   return ELASTO_OK;
 }
 
-}  // extern "C"
+}  // namespace elasto

@@ -1,0 +1,188 @@
+// The largest logits of each row, largest first, the lower index first among
+// equal ones: what a teacher's answer is reduced to for distillation.
+//
+// Values and indices are ordered together: key = (order of the value, ~index),
+// so keys differ and ties need no care.  One workgroup a row:
+//  1. every thread finds the largest key of its share.  Each of the W waves
+//     sorts its 64 and gives the ceil(top / W)-th: at least `top` keys of the
+//     row are no smaller than the least of those;
+//  2. the keys from that bound on, hardly more than `top` of them, are
+//     collected in LDS.  Where they are too many to hold (the largest ones lie
+//     in few threads' shares), the top-th of those held is the next bound: each
+//     round drops all but `top` of what it held, so the rounds end;
+//  3. the collected keys are sorted and the first `top` written.
+// The order of collecting does not matter to the result.
+//
+// Bound by memory: the second reading finds the row in the caches behind L2.
+#include "layout.h"
+#include "logits.h"
+
+namespace elasto {
+namespace {
+
+constexpr int kHold = 2048;  // keys held in LDS
+
+// Order of floats as unsigned integers, -0 as 0, NaN above all.
+__device__ __forceinline__ uint32_t order_of(float x) {
+  const uint32_t u = __float_as_uint(x + 0.0f);
+  const uint32_t o = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+  return x == x ? o : 0xffffffffu;
+}
+__device__ __forceinline__ uint64_t key_of(uint32_t order, int i) {
+  return (uint64_t)order << 32 | (uint32_t)~i;
+}
+
+// The wave's 64 keys, largest in lane 0.
+__device__ __forceinline__ uint64_t wave_sort(uint64_t k, int lane) {
+#pragma unroll
+  for (int size = 2; size <= 64; size *= 2)
+#pragma unroll
+    for (int step = size / 2; step >= 1; step /= 2) {
+      const uint64_t o = (uint64_t)(uint32_t)__shfl_xor((int)(k >> 32), step, 64) << 32 |
+                         (uint32_t)__shfl_xor((int)(uint32_t)k, step, 64);
+      const bool down = (lane & size) == 0, low = (lane & step) == 0;
+      k = (low == down) == (k > o) ? k : o;
+    }
+  return k;
+}
+
+// keys[0, n) largest first; n a power of two.
+template <int N>
+__device__ __forceinline__ void block_sort(uint64_t* keys, int n, int tid) {
+  for (int size = 2; size <= n; size *= 2)
+    for (int step = size / 2; step >= 1; step /= 2) {
+      for (int t = tid; t < n / 2; t += N) {
+        const int i = 2 * t - (t & (step - 1)), j = i + step;
+        const uint64_t a = keys[i], b = keys[j];
+        if ((a < b) == ((i & size) == 0)) {
+          keys[i] = b;
+          keys[j] = a;
+        }
+      }
+      __syncthreads();
+    }
+}
+
+template <typename T, int N>
+__global__ __launch_bounds__(N) void top_logits_kernel(const T* logits, int64_t ld, int C, int top,
+                                                       float* values, int32_t* indices) {
+  __shared__ uint64_t held[kHold];
+  __shared__ uint64_t bounds[N / 64];
+  __shared__ int count;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const T* z = logits + (int64_t)blockIdx.x * ld;
+  const RowSpan<T> span(z, C);
+
+  uint32_t bo = 0;
+  int bi = 0;
+  uint64_t best = 0;  // less than any key
+  walk_row<N>(z, span, tid,
+              [&](int i, const float* v) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                  const uint32_t o = order_of(v[e]);
+                  bi = o > bo ? i + e : bi;
+                  bo = o > bo ? o : bo;
+                }
+              },
+              [&](int i, float v) {
+                const uint64_t k = key_of(order_of(v), i);
+                best = k > best ? k : best;
+              });
+  if (bo) {
+    const uint64_t k = key_of(bo, bi);
+    best = k > best ? k : best;
+  }
+  constexpr int W = N / 64;
+  const uint64_t sorted = wave_sort(best, lane);
+  if (lane == (top + W - 1) / W - 1) bounds[tid >> 6] = sorted;
+  __syncthreads();
+  uint64_t bound = bounds[0];
+#pragma unroll
+  for (int w = 1; w < W; ++w) bound = bounds[w] < bound ? bounds[w] : bound;
+
+  int n;
+  while (true) {
+    if (tid == 0) count = 0;
+    __syncthreads();
+    auto keep = [&](uint64_t k) {
+      const int at = atomicAdd(&count, 1);
+      if (at < kHold) held[at] = k;
+    };
+    const uint32_t bh = (uint32_t)(bound >> 32);
+    walk_row<N>(z, span, tid,
+                [&](int i, const float* v) {
+                  uint32_t o[8], m = 0;
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) {
+                    o[e] = order_of(v[e]);
+                    m = o[e] > m ? o[e] : m;
+                  }
+                  if (m < bh) return;
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) {
+                    const uint64_t k = key_of(o[e], i + e);
+                    if (k >= bound) keep(k);
+                  }
+                },
+                [&](int i, float v) {
+                  const uint64_t k = key_of(order_of(v), i);
+                  if (k >= bound) keep(k);
+                });
+    __syncthreads();
+    n = count;
+    const int got = n < kHold ? n : kHold;
+    int p2 = 1;
+    while (p2 < got) p2 *= 2;
+    for (int t = got + tid; t < p2; t += N) held[t] = 0;
+    __syncthreads();
+    block_sort<N>(held, p2, tid);
+    if (n <= kHold) break;
+    bound = held[top - 1];
+    __syncthreads();
+  }
+  for (int t = tid; t < top; t += N) {
+    const int i = (int)~(uint32_t)held[t];
+    values[(int64_t)blockIdx.x * top + t] = load1(z + i);
+    indices[(int64_t)blockIdx.x * top + t] = i;
+  }
+}
+
+template <typename T>
+hipError_t launch(const void* logits, int64_t ld, int64_t rows, int C, int top, float* values,
+                  int32_t* indices, hipStream_t s) {
+  const T* z = static_cast<const T*>(logits);
+  if (C >= 8192)
+    hipLaunchKernelGGL((top_logits_kernel<T, 1024>), dim3((unsigned)rows), dim3(1024), 0, s, z, ld, C,
+                       top, values, indices);
+  else
+    hipLaunchKernelGGL((top_logits_kernel<T, 256>), dim3((unsigned)rows), dim3(256), 0, s, z, ld, C,
+                       top, values, indices);
+  return hipGetLastError();
+}
+
+}  // namespace
+}  // namespace elasto
+
+using namespace elasto;
+
+extern "C" elasto_status_t elasto_op_top_logits(int32_t dtype, const void* logits, int64_t ld,
+                                                int64_t rows, int32_t classes, int32_t top,
+                                                float* values, int32_t* indices, void* hip_stream) {
+  if (dtype != ELASTO_BF16 && dtype != ELASTO_FP32) return fail(ELASTO_ERR_INVALID_ARG, "bad dtype %d", dtype);
+  if (rows < 0 || rows > 0x7fffffff || classes < 1 || classes > (1 << 30) || ld < classes)
+    return fail(ELASTO_ERR_INVALID_ARG, "top_logits: bad rows, classes or row stride");
+  if (top < 1 || top > 256 || top > classes)
+    return fail(ELASTO_ERR_INVALID_ARG, "top_logits: top %d outside [1, min(256, classes)]", top);
+  if (rows == 0) return ELASTO_OK;
+  if (!logits || !values || !indices) return fail(ELASTO_ERR_INVALID_ARG, "NULL pointer");
+  if (reinterpret_cast<uintptr_t>(logits) % (dtype == ELASTO_BF16 ? 2 : 4) ||
+      reinterpret_cast<uintptr_t>(values) % 4 || reinterpret_cast<uintptr_t>(indices) % 4)
+    return fail(ELASTO_ERR_INVALID_ARG, "top_logits: misaligned pointer");
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const hipError_t e = dtype == ELASTO_BF16
+                           ? launch<uint16_t>(logits, ld, rows, classes, top, values, indices, s)
+                           : launch<float>(logits, ld, rows, classes, top, values, indices, s);
+  if (e != hipSuccess) return fail(ELASTO_ERR_HIP, "top_logits: %s", hipGetErrorString(e));
+  return ELASTO_OK;
+}

@@ -1,0 +1,435 @@
+// Attention in a sliding window with first tokens that stay visible (sinks):
+//   o_i = sum_j softmax_j(scale q_i . k_j) v_j over the keys that query i sees,
+//   lse_i = log sum_j exp(scale q_i . k_j)
+// (the mask and the packed rows: window.h).  One pass over the visible tiles of
+// keys with the running maximum and sum of each row; tiles that no row of the
+// workgroup sees are not read, so the cost goes with tokens x window.
+//
+// Scores are taken transposed, S^T = K Q^T: a lane holds one row's scores, so
+// the softmax needs one exchange between the half-waves a tile, and the
+// probabilities (rounded to bf16 on the bf16 path, after the sum has been taken
+// in fp32) are the operand of O^T = V^T P^T without moving.
+//
+// Two shapes of a workgroup of four waves:
+// * rows: 128 rows, 32 a wave, which share each tile of keys;
+// * keys: 32 rows, the tiles shared out over the waves, joined in LDS at the
+//   end: single tokens, and launches that would leave CUs idle.
+// Where the workgroups are still few, each row block's tiles are split over
+// several, whose unnormalised results a second kernel joins (the running
+// maximum and sum of each part go with it).
+#include <algorithm>
+
+#include "layout.h"
+#include "window.h"
+#include "window_args.h"
+
+namespace elasto {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+
+struct FwdP {
+  View q, k, v, o;
+  float* lse;              // [batch][heads][q_tokens] or NULL
+  const int32_t *q_lens, *k_lens;
+  int q_tokens, k_tokens, heads, kv_heads, group;
+  Mask mask;
+  float c2;                // scale * log2(e)
+  int row_blocks, splits;
+  int64_t blocks;
+  float *part_o, *part_ml;  // splits > 1: [batch * kv_heads][split][row][HD], [...][2]
+};
+
+template <typename T, int HD, bool KEYS>
+struct Shape {
+  static constexpr int kSub = !KEYS && sizeof(T) == 2 ? 2 : 1;  // 32-key blocks of a tile
+  static constexpr int kKeys = 32 * kSub;
+  static constexpr int kTile = kKeys * Tile<T, HD>::kRow;       // bytes of K (and of V)
+  static constexpr int kPrivate = KEYS ? kWaves : 1;            // tiles held at once
+  static constexpr int kBuffers = kPrivate * kTile * 4 <= 128 * 1024 ? 2 : 1;
+  static constexpr int kOs = HD + 4;  // floats of a row of the join
+  static constexpr int kJoin = KEYS ? kWaves * 32 * kOs * 4 + kWaves * 64 * 4 : 0;
+  static constexpr int kLds = std::max(kPrivate * kBuffers * 2 * kTile, kJoin);
+  static constexpr int kRows = KEYS ? 32 : 32 * kWaves;
+};
+
+// The running state of 32 rows: a lane's row is column l % 32 of S^T.
+template <typename T, int HD>
+struct State {
+  f32x16 o[HD / 32];
+  float m, l;  // running maximum (of raw scores), this half-wave's part of the sum
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int n = 0; n < HD / 32; ++n) zero(o[n]);
+    m = -INFINITY;
+    l = 0.0f;
+  }
+
+  // One tile of SUB * 32 keys from j0 on.
+  template <int SUB>
+  __device__ __forceinline__ void tile(const char* kt, const char* vt, int j0, const Frag<T>* q,
+                                       float c2, bool inside, const Keys& ks, int lane) {
+    const int r = lane & 31, h = lane >> 5;
+    f32x16 s[SUB];
+#pragma unroll
+    for (int b = 0; b < SUB; ++b) {
+      zero(s[b]);
+#pragma unroll
+      for (int kk = 0; kk < HD / 16; ++kk) {
+        Frag<T> a;
+        Tile<T, HD>::operand(kt, b * 32 + r, kk, h, a);
+        s[b] = mma(a, q[kk], s[b]);
+      }
+    }
+    if (!inside) {
+      const unsigned len = (unsigned)max(ks.hi - ks.lo + 1, 0);
+#pragma unroll
+      for (int b = 0; b < SUB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = j0 + b * 32 + 8 * (i >> 2) + 4 * h + (i & 3);
+          const bool sees = j <= ks.hs || (unsigned)(j - ks.lo) < len;
+          s[b][i] = sees ? s[b][i] : -INFINITY;
+        }
+    }
+    float t = s[0][0];
+#pragma unroll
+    for (int b = 0; b < SUB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) t = fmaxf(t, s[b][i]);
+    t = fmaxf(m, half_max(t));
+    // Rows whose maximum rises bring their sums to the new one.
+    if (__any(t > m)) {
+      const float f = t > m ? __builtin_amdgcn_exp2f((m - t) * c2) : 1.0f;
+      l *= f;
+#pragma unroll
+      for (int n = 0; n < HD / 32; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[n][i] *= f;
+      m = t;
+    }
+    const float off = m == -INFINITY ? 0.0f : -m * c2;  // nothing seen so far: all terms are 0
+#pragma unroll
+    for (int b = 0; b < SUB; ++b) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c2, off));
+        l += s[b][i];
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        Frag<T> pf;
+        as_operand(s[b], u, pf);
+#pragma unroll
+        for (int n = 0; n < HD / 32; ++n) {
+          Frag<T> a;
+          Tile<T, HD>::transposed(vt, b * 32 + u * 16, n, lane, a);
+          o[n] = mma(a, pf, o[n]);
+        }
+      }
+    }
+  }
+};
+
+template <typename T, int HD, bool KEYS>
+__global__ __launch_bounds__(kThreads) void window_fwd_kernel(FwdP p) {
+  using S = Shape<T, HD, KEYS>;
+  using Tl = Tile<T, HD>;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t id = xcd_order(blockIdx.x, p.blocks);
+  const int z = (int)(id % p.splits);
+  const int64_t rest = id / p.splits;
+  const int rb = (int)(rest % p.row_blocks);
+  const int64_t bk = rest / p.row_blocks;
+  const int b = (int)(bk / p.kv_heads), hk = (int)(bk - (int64_t)b * p.kv_heads);
+  const int ql = clamp_len(p.q_lens, b, p.q_tokens), kl = clamp_len(p.k_lens, b, p.k_tokens);
+  const int G = p.group, rows = ql * G;
+  const int first = rb * S::kRows;
+  if (first >= rows) return;
+
+  // This lane's row, this wave's and the workgroup's positions.
+  const int wfirst = first + (KEYS ? 0 : 32 * wave);
+  const int row = wfirst + (lane & 31), rc = min(row, rows - 1);
+  const int i = rc / G, g = rc - i * G, shift = kl - ql;
+  const Keys mine = keys_of(p.mask, i + shift, kl);
+  const Keys a0 = keys_of(p.mask, first / G + shift, kl);
+  const Keys a1 = keys_of(p.mask, (min(first + S::kRows, rows) - 1) / G + shift, kl);
+  const int wl = min(wfirst, rows - 1);
+  const Keys w0 = keys_of(p.mask, wl / G + shift, kl);
+  const Keys w1 = keys_of(p.mask, (min(wl + 32, rows) - 1) / G + shift, kl);
+  const bool idle = wfirst >= rows;
+
+  // Tiles: those of the sinks, then those of the window.
+  const int sink_tiles = a1.hs >= 0 ? a1.hs / S::kKeys + 1 : 0;
+  const int t0 = max(a0.lo / S::kKeys, sink_tiles);
+  const int tiles = sink_tiles + (a1.hi >= a0.lo ? max(a1.hi / S::kKeys + 1 - t0, 0) : 0);
+  const int zs = (int)((int64_t)tiles * z / p.splits), ze = (int)((int64_t)tiles * (z + 1) / p.splits);
+  auto key0 = [&](int n) { return (n < sink_tiles ? n : t0 + n - sink_tiles) * S::kKeys; };
+
+  const char* kp = p.k.p + b * p.k.sb + hk * p.k.sh;
+  const char* vp = p.v.p + b * p.v.sb + hk * p.v.sh;
+  auto stage = [&](int n, char* dst) {
+    const int j0 = key0(n);
+    const int w = KEYS ? 0 : wave;
+    constexpr int W = KEYS ? 1 : kWaves;
+    // Keys past the last one are that one again: they are masked, and what the
+    // memory holds there is not read.
+    Tl::template stage<S::kKeys, W>(dst, w, lane, [&](int r) { return kp + (int64_t)min(j0 + r, kl - 1) * p.k.st; });
+    Tl::template stage<S::kKeys, W>(dst + S::kTile, w, lane, [&](int r) { return vp + (int64_t)min(j0 + r, kl - 1) * p.v.st; });
+  };
+
+  State<T, HD> st;
+  st.clear();
+  Frag<T> q[HD / 16];
+  const char* qrow = p.q.p + b * p.q.sb + (int64_t)i * p.q.st + (int64_t)(hk * G + g) * p.q.sh;
+#pragma unroll
+  for (int kk = 0; kk < HD / 16; ++kk) load_operand(qrow, kk, h, q[kk]);
+
+  auto compute = [&](int n, const char* buf) {
+    const int j0 = key0(n), j1 = j0 + S::kKeys - 1;
+    // Nothing of the tile is seen by this wave's rows.
+    if (idle || (j0 > w1.hs && (j1 < w0.lo || j0 > w1.hi))) return;
+    const bool inside = j0 >= w1.lo && j1 <= w0.hi;
+    st.template tile<S::kSub>(buf, buf + S::kTile, j0, q, p.c2, inside, mine, lane);
+  };
+  constexpr int kLoads = 2 * Tl::template loads<S::kKeys, KEYS ? 1 : kWaves>();
+  char* mem = smem + (KEYS ? wave * S::kBuffers * 2 * S::kTile : 0);
+  const int step = KEYS ? kWaves : 1;
+  int n = zs + (KEYS ? wave : 0);
+  if constexpr (S::kBuffers == 2) {
+    if (n < ze) stage(n, mem);
+    int cur = 0;
+    for (; n < ze; n += step) {
+      char* buf = mem + cur * 2 * S::kTile;
+      const bool more = n + step < ze;
+      if (more) stage(n + step, mem + (cur ^ 1) * 2 * S::kTile);
+      asm volatile("" ::: "memory");
+      if (more) wait_vm_lds<kLoads>();
+      else wait_vm_lds<0>();
+      if (!KEYS) __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      compute(n, buf);
+      // Every read of this tile is done before the next but one overwrites it.
+      asm volatile("" ::: "memory");
+      wait_lds();
+      if (!KEYS) __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      cur ^= 1;
+    }
+  } else {
+    for (; n < ze; n += step) {
+      stage(n, mem);
+      asm volatile("" ::: "memory");
+      wait_vm_lds<0>();
+      if (!KEYS) __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      compute(n, mem);
+      asm volatile("" ::: "memory");
+      wait_lds();
+      if (!KEYS) __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    }
+  }
+  st.l = half_sum(st.l);
+
+  const int head = hk * G + g;
+  const int64_t prow = (bk * p.splits + z) * ((int64_t)p.q_tokens * G) + row;
+  if constexpr (!KEYS) {
+    if (row >= rows) return;
+    if (p.splits > 1) {
+      float* po = p.part_o + prow * HD;
+#pragma unroll
+      for (int n = 0; n < HD / 32; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          store4(po + n * 32 + 8 * e + 4 * h, st.o[n][4 * e], st.o[n][4 * e + 1], st.o[n][4 * e + 2], st.o[n][4 * e + 3]);
+      if (h == 0) {
+        p.part_ml[prow * 2] = st.m;
+        p.part_ml[prow * 2 + 1] = st.l;
+      }
+      return;
+    }
+    const float inv = st.l > 0.0f ? 1.0f / st.l : st.l == 0.0f ? 0.0f : NAN;
+    T* orow = reinterpret_cast<T*>(p.o.p + b * p.o.sb + (int64_t)i * p.o.st + (int64_t)head * p.o.sh);
+#pragma unroll
+    for (int n = 0; n < HD / 32; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        store4(orow + n * 32 + 8 * e + 4 * h, st.o[n][4 * e] * inv, st.o[n][4 * e + 1] * inv,
+               st.o[n][4 * e + 2] * inv, st.o[n][4 * e + 3] * inv);
+    if (p.lse && h == 0)
+      p.lse[((int64_t)b * p.heads + head) * p.q_tokens + i] =
+          st.l == 0.0f ? -INFINITY : fmaf(st.m, p.c2, log2f(st.l)) * kLn2;
+  } else {
+    // Join the waves: their maxima and sums first, then their rows at the
+    // common maximum.
+    float* ml = reinterpret_cast<float*>(smem + kWaves * 32 * S::kOs * 4);
+    float* jo = reinterpret_cast<float*>(smem);
+    __syncthreads();  // every wave is done with its tiles
+    if (h == 0) {
+      ml[wave * 64 + lane] = st.m;
+      ml[wave * 64 + 32 + lane] = st.l;
+    }
+    __syncthreads();
+    float M = -INFINITY, L = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, ml[w * 64 + (lane & 31)]);
+    const float base = M == -INFINITY ? 0.0f : M;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+      L += ml[w * 64 + 32 + (lane & 31)] * __builtin_amdgcn_exp2f((ml[w * 64 + (lane & 31)] - base) * p.c2);
+    const float f = __builtin_amdgcn_exp2f((st.m - base) * p.c2);
+    float* jr = jo + (wave * 32 + (lane & 31)) * S::kOs;
+#pragma unroll
+    for (int n = 0; n < HD / 32; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        store4(jr + n * 32 + 8 * e + 4 * h, st.o[n][4 * e] * f, st.o[n][4 * e + 1] * f,
+               st.o[n][4 * e + 2] * f, st.o[n][4 * e + 3] * f);
+    // The joined maximum and sum of row r, for the threads that write it.
+    __syncthreads();
+    if (wave == 0 && h == 0) {
+      ml[lane] = M;
+      ml[32 + lane] = L;
+    }
+    __syncthreads();
+    for (int u = threadIdx.x; u < 32 * (HD / 4); u += kThreads) {
+      const int r = u / (HD / 4), c = (u - r * (HD / 4)) * 4, gr = first + r;
+      if (gr >= rows) break;
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(jo + (w * 32 + r) * S::kOs + c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += x[e];
+      }
+      const float Lr = ml[32 + r];
+      if (p.splits > 1) {
+        const int64_t pr = (bk * p.splits + z) * ((int64_t)p.q_tokens * G) + gr;
+        store4(p.part_o + pr * HD + c, v[0], v[1], v[2], v[3]);
+        if (c == 0) {
+          p.part_ml[pr * 2] = ml[r];
+          p.part_ml[pr * 2 + 1] = Lr;
+        }
+      } else {
+        const float inv = Lr > 0.0f ? 1.0f / Lr : Lr == 0.0f ? 0.0f : NAN;
+        const int qi = gr / G, hd = hk * G + gr - qi * G;
+        T* orow = reinterpret_cast<T*>(p.o.p + b * p.o.sb + (int64_t)qi * p.o.st + (int64_t)hd * p.o.sh);
+        store4(orow + c, v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+        if (p.lse && c == 0)
+          p.lse[((int64_t)b * p.heads + hd) * p.q_tokens + qi] =
+              Lr == 0.0f ? -INFINITY : fmaf(ml[r], p.c2, log2f(Lr)) * kLn2;
+      }
+    }
+  }
+}
+
+// Joins the splits of a row: HD / 4 threads a row.
+template <typename T, int HD>
+__global__ __launch_bounds__(kThreads) void window_join_kernel(FwdP p) {
+  constexpr int kPer = HD / 4;
+  const int64_t at = (int64_t)blockIdx.x * (kThreads / kPer) + threadIdx.x / kPer;
+  const int c = (threadIdx.x % kPer) * 4;
+  const int64_t rmax = (int64_t)p.q_tokens * p.group, bk = at / rmax;
+  const int row = (int)(at - bk * rmax);
+  const int b = (int)(bk / p.kv_heads), hk = (int)(bk - (int64_t)b * p.kv_heads);
+  const int64_t total = p.blocks / p.splits / p.row_blocks * rmax;
+  if (at >= total || row >= clamp_len(p.q_lens, b, p.q_tokens) * p.group) return;
+  float M = -INFINITY, L = 0.0f, v[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int z = 0; z < p.splits; ++z) M = fmaxf(M, p.part_ml[((bk * p.splits + z) * rmax + row) * 2]);
+  const float base = M == -INFINITY ? 0.0f : M;
+  for (int z = 0; z < p.splits; ++z) {
+    const int64_t pr = (bk * p.splits + z) * rmax + row;
+    const float f = __builtin_amdgcn_exp2f((p.part_ml[pr * 2] - base) * p.c2);
+    const f32x4 x = *reinterpret_cast<const f32x4*>(p.part_o + pr * HD + c);
+    L = fmaf(p.part_ml[pr * 2 + 1], f, L);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = fmaf(x[e], f, v[e]);
+  }
+  const float inv = L > 0.0f ? 1.0f / L : L == 0.0f ? 0.0f : NAN;
+  const int i = row / p.group, head = hk * p.group + row - i * p.group;
+  T* orow = reinterpret_cast<T*>(p.o.p + b * p.o.sb + (int64_t)i * p.o.st + (int64_t)head * p.o.sh);
+  store4(orow + c, v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+  if (p.lse && c == 0)
+    p.lse[((int64_t)b * p.heads + head) * p.q_tokens + i] =
+        L == 0.0f ? -INFINITY : fmaf(M, p.c2, log2f(L)) * kLn2;
+}
+
+// How a launch is cut: workgroup shape, row blocks, splits.
+struct Cut {
+  bool keys;
+  int row_blocks, splits;
+};
+Cut cut_of(const elasto_window_t& a) {
+  constexpr int kCUs = 256;
+  const int64_t pairs = (int64_t)a.batch * a.kv_heads, rows = (int64_t)a.q_tokens * (a.heads / a.kv_heads);
+  Cut c;
+  c.keys = rows <= 32;
+  const int per = c.keys ? 32 : 128;
+  c.row_blocks = (int)((rows + per - 1) / per);
+  const int64_t blocks = pairs * c.row_blocks;
+  // Keys that a row block can see, in shares of at least 256 a workgroup.
+  const int64_t reach = (a.causal ? (int64_t)a.window : 2 * (int64_t)a.window - 1) + per / (a.heads / a.kv_heads);
+  const int64_t keys = std::min<int64_t>(a.k_tokens, reach + a.sinks);
+  const int64_t want = (2 * kCUs + blocks - 1) / std::max<int64_t>(blocks, 1);
+  c.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, keys / 256, 64}));
+  return c;
+}
+
+template <typename T, int HD, bool KEYS>
+hipError_t launch(const FwdP& p, hipStream_t s) {
+  constexpr int lds = Shape<T, HD, KEYS>::kLds;
+  static_assert(lds <= 160 * 1024, "LDS");
+  hipLaunchKernelGGL((window_fwd_kernel<T, HD, KEYS>), dim3((unsigned)p.blocks), dim3(kThreads), lds, s, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  const int64_t rows = p.blocks / p.splits / p.row_blocks * p.q_tokens * p.group;
+  constexpr int kRows = kThreads / (HD / 4);
+  hipLaunchKernelGGL((window_join_kernel<T, HD>), dim3((unsigned)((rows + kRows - 1) / kRows)),
+                     dim3(kThreads), 0, s, p);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_dim(const FwdP& p, int dim, bool keys, hipStream_t s) {
+  if (dim == 64) return keys ? launch<T, 64, true>(p, s) : launch<T, 64, false>(p, s);
+  return keys ? launch<T, 128, true>(p, s) : launch<T, 128, false>(p, s);
+}
+
+int64_t split_floats(const elasto_window_t& a, const Cut& c) {
+  return c.splits == 1 ? 0 : (int64_t)a.batch * a.heads * a.q_tokens * c.splits * (a.head_dim + 2);
+}
+
+}  // namespace
+
+int64_t window_fwd_workspace(const elasto_window_t& a) { return split_floats(a, cut_of(a)) * 4; }
+
+hipError_t launch_window_fwd(const elasto_window_t& a, const WindowTensors& t, void* ws, hipStream_t s) {
+  const Cut c = cut_of(a);
+  FwdP p = {};
+  p.q = t.q; p.k = t.k; p.v = t.v; p.o = t.o;
+  p.lse = t.lse;
+  p.q_lens = a.q_lens;
+  p.k_lens = a.k_lens;
+  p.q_tokens = a.q_tokens;
+  p.k_tokens = a.k_tokens;
+  p.heads = a.heads;
+  p.kv_heads = a.kv_heads;
+  p.group = a.heads / a.kv_heads;
+  p.mask = Mask{a.causal, a.window, a.sinks};
+  p.c2 = a.scale * kLog2e;
+  p.row_blocks = c.row_blocks;
+  p.splits = c.splits;
+  p.blocks = (int64_t)a.batch * a.kv_heads * c.row_blocks * c.splits;
+  p.part_o = static_cast<float*>(ws);
+  p.part_ml = p.part_o + (int64_t)a.batch * a.heads * a.q_tokens * c.splits * a.head_dim;
+  if (p.blocks > 0x7fffffff) return hipErrorInvalidValue;
+  return a.dtype == ELASTO_BF16 ? launch_dim<uint16_t>(p, a.head_dim, c.keys, s)
+                                : launch_dim<float>(p, a.head_dim, c.keys, s);
+}
+
+}  // namespace elasto

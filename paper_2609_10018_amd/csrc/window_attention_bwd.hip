@@ -1,0 +1,446 @@
+// Backward of the windowed attention (window_attention.hip).  With
+// P = exp(scale S - lse) inside the mask, 0 outside, and D_i = do_i . o_i:
+//   dv_j = sum_i P_ij do_i,  dS = P (.) (do v^T - D),
+//   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i.
+// The scores are formed again from q, k and lse rather than kept.  Two kernels,
+// each of which sums in one order in registers, so there are no atomics and the
+// gradients are the same bits every time:
+// * rows: 32 packed rows a wave, over the tiles of keys that they see: dq, and
+//   the row's lse (base 2) and D for the second kernel;
+// * keys: 32 keys a wave, over the tiles of packed rows that see them: dk and
+//   dv, summed over the heads of the group.
+// Seven products of the size of S where five would do: what the two extra ones
+// cost is less than adding dq up in memory would.
+//
+// P and dS are rounded to bf16 (bf16 path) as operands of the products that
+// sum them; all sums are fp32.
+//
+// A key among the sinks is seen by every later row, so the first tile of keys
+// has far more rows than the others: its rows are cut into parts of about an
+// ordinary tile's, each a workgroup, whose fp32 sums a third kernel adds up.
+#include <algorithm>
+
+#include "layout.h"
+#include "window.h"
+#include "window_args.h"
+
+namespace elasto {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kKeys = 32 * kWaves;  // keys of a workgroup of the key kernel
+static_assert(kMaxSinks <= kKeys, "the sinks lie in the first tile of keys");
+
+struct BwdP {
+  View q, k, v, o, dout, dq, dk, dv;
+  const float* lse;
+  const int32_t *q_lens, *k_lens;
+  int q_tokens, k_tokens, heads, kv_heads, group;
+  Mask mask;
+  float scale, c2;
+  int64_t blocks;
+  int row_blocks;          // row kernel
+  int key_tiles, parts;    // key kernel: tiles of keys, parts of the first tile's rows
+  float2* stat;            // [batch * kv_heads][row]: lse in base 2, D
+  float* part;             // parts > 1: [batch * kv_heads][part][2][kKeys][HD]
+};
+
+template <typename T, int HD>
+struct Shape {
+  static constexpr int kSub = sizeof(T) == 2 ? 2 : 1;
+  static constexpr int kRows = 32 * kSub;                    // of a staged tile
+  static constexpr int kTile = kRows * Tile<T, HD>::kRow;
+  static constexpr int kStat = 64 * 8 * 2;                   // a tile's lse and D, and a spare
+  static constexpr int kLdsRow = 2 * 2 * kTile;
+  static constexpr int kLdsKey = 2 * (2 * kTile + kStat);
+};
+
+template <typename T, int HD>
+__global__ __launch_bounds__(kThreads) void window_dq_kernel(BwdP p) {
+  using S = Shape<T, HD>;
+  using Tl = Tile<T, HD>;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t id = xcd_order(blockIdx.x, p.blocks);
+  const int rb = (int)(id % p.row_blocks);
+  const int64_t bk = id / p.row_blocks;
+  const int b = (int)(bk / p.kv_heads), hk = (int)(bk - (int64_t)b * p.kv_heads);
+  const int ql = clamp_len(p.q_lens, b, p.q_tokens), kl = clamp_len(p.k_lens, b, p.k_tokens);
+  const int G = p.group, rows = ql * G, shift = kl - ql;
+  const int first = rb * 32 * kWaves;
+  if (first >= rows) return;
+  const int wfirst = first + 32 * wave;
+  const int row = wfirst + l32, rc = min(row, rows - 1);
+  const int i = rc / G, head = hk * G + rc - i * G;
+  const Keys mine = keys_of(p.mask, i + shift, kl);
+  const Keys a0 = keys_of(p.mask, first / G + shift, kl);
+  const Keys a1 = keys_of(p.mask, (min(first + 32 * kWaves, rows) - 1) / G + shift, kl);
+  const int wl = min(wfirst, rows - 1);
+  const Keys w0 = keys_of(p.mask, wl / G + shift, kl);
+  const Keys w1 = keys_of(p.mask, (min(wl + 32, rows) - 1) / G + shift, kl);
+  const bool idle = wfirst >= rows;
+  const int sink_tiles = a1.hs >= 0 ? a1.hs / S::kRows + 1 : 0;
+  const int t0 = max(a0.lo / S::kRows, sink_tiles);
+  const int tiles = sink_tiles + (a1.hi >= a0.lo ? max(a1.hi / S::kRows + 1 - t0, 0) : 0);
+  auto key0 = [&](int n) { return (n < sink_tiles ? n : t0 + n - sink_tiles) * S::kRows; };
+  const char* kp = p.k.p + b * p.k.sb + hk * p.k.sh;
+  const char* vp = p.v.p + b * p.v.sb + hk * p.v.sh;
+  auto stage = [&](int n, char* dst) {
+    const int j0 = key0(n);
+    Tl::template stage<S::kRows, kWaves>(dst, wave, lane, [&](int r) { return kp + (int64_t)min(j0 + r, kl - 1) * p.k.st; });
+    Tl::template stage<S::kRows, kWaves>(dst + S::kTile, wave, lane, [&](int r) { return vp + (int64_t)min(j0 + r, kl - 1) * p.v.st; });
+  };
+
+  Frag<T> q[HD / 16], d[HD / 16];
+  const char* qrow = p.q.p + b * p.q.sb + (int64_t)i * p.q.st + (int64_t)head * p.q.sh;
+  const char* drow = p.dout.p + b * p.dout.sb + (int64_t)i * p.dout.st + (int64_t)head * p.dout.sh;
+  const char* orow = p.o.p + b * p.o.sb + (int64_t)i * p.o.st + (int64_t)head * p.o.sh;
+  float D = 0.0f;
+#pragma unroll
+  for (int kk = 0; kk < HD / 16; ++kk) {
+    Frag<T> of;
+    load_operand(qrow, kk, h, q[kk]);
+    load_operand(drow, kk, h, d[kk]);
+    load_operand(orow, kk, h, of);
+    D = dot(d[kk], of, D);
+  }
+  D = half_sum(D);
+  float l2 = p.lse[((int64_t)b * p.heads + head) * p.q_tokens + i] * kLog2e;
+  if (l2 == -INFINITY) l2 = 0.0f;  // a row that sees nothing: every term is masked
+  if (h == 0 && row < rows) p.stat[bk * ((int64_t)p.q_tokens * G) + row] = make_float2(l2, D);
+
+  f32x16 dq[HD / 32];
+#pragma unroll
+  for (int n = 0; n < HD / 32; ++n) zero(dq[n]);
+  constexpr int kLoads = 2 * Tl::template loads<S::kRows, kWaves>();
+  if (tiles > 0) stage(0, smem);
+  for (int n = 0; n < tiles; ++n) {
+    const char* kt = smem + (n & 1) * 2 * S::kTile;
+    const char* vt = kt + S::kTile;
+    if (n + 1 < tiles) {
+      stage(n + 1, smem + ((n + 1) & 1) * 2 * S::kTile);
+      wait_and_meet<kLoads>();
+    } else {
+      wait_and_meet<0>();
+    }
+    const int j0 = key0(n), j1 = j0 + S::kRows - 1;
+    const bool skip = idle || (j0 > w1.hs && (j1 < w0.lo || j0 > w1.hi));
+    if (!skip) {
+      const bool inside = j0 >= w1.lo && j1 <= w0.hi;
+      const unsigned len = (unsigned)max(mine.hi - mine.lo + 1, 0);
+#pragma unroll
+      for (int s = 0; s < S::kSub; ++s) {
+        f32x16 sc, dp;
+        zero(sc);
+        zero(dp);
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk) {
+          Frag<T> a;
+          Tl::operand(kt, s * 32 + l32, kk, h, a);
+          sc = mma(a, q[kk], sc);
+          Tl::operand(vt, s * 32 + l32, kk, h, a);
+          dp = mma(a, d[kk], dp);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          float pr = __builtin_amdgcn_exp2f(fmaf(sc[e], p.c2, -l2));
+          if (!inside) {
+            const int j = j0 + s * 32 + 8 * (e >> 2) + 4 * h + (e & 3);
+            pr = j <= mine.hs || (unsigned)(j - mine.lo) < len ? pr : 0.0f;
+          }
+          sc[e] = pr * (dp[e] - D);
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          Frag<T> df;
+          as_operand(sc, u, df);
+#pragma unroll
+          for (int f = 0; f < HD / 32; ++f) {
+            Frag<T> a;
+            Tl::transposed(kt, s * 32 + u * 16, f, lane, a);
+            dq[f] = mma(a, df, dq[f]);
+          }
+        }
+      }
+    }
+    asm volatile("" ::: "memory");
+    wait_lds();  // every read of this tile is done before the next but one overwrites it
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  }
+  if (row >= rows) return;
+  T* out = reinterpret_cast<T*>(p.dq.p + b * p.dq.sb + (int64_t)i * p.dq.st + (int64_t)head * p.dq.sh);
+#pragma unroll
+  for (int n = 0; n < HD / 32; ++n)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      store4(out + n * 32 + 8 * e + 4 * h, dq[n][4 * e] * p.scale, dq[n][4 * e + 1] * p.scale,
+             dq[n][4 * e + 2] * p.scale, dq[n][4 * e + 3] * p.scale);
+}
+
+// Packed rows that see key j: [lo, hi]; sink: as one of the sinks, if it is one.
+struct Rows {
+  int lo, hi;
+};
+__device__ __forceinline__ Rows rows_of(const Mask& m, int j, int shift, int rows, int G, bool sink) {
+  const int plo = m.causal ? j : sink && j < m.sinks ? 0 : j - m.window + 1;
+  const int64_t phi = sink && j < m.sinks ? (int64_t)1 << 31 : (int64_t)j + m.window - 1;
+  Rows r;
+  r.lo = (int)min((int64_t)rows, max((int64_t)0, (int64_t)(plo - shift) * G));
+  if (!m.causal && sink && j < m.sinks) r.lo = 0;
+  r.hi = (int)min((int64_t)rows - 1, max((int64_t)-1, (phi - shift + 1) * G - 1));
+  return r;
+}
+
+template <typename T, int HD>
+__global__ __launch_bounds__(kThreads) void window_dkv_kernel(BwdP p) {
+  using S = Shape<T, HD>;
+  using Tl = Tile<T, HD>;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t id = xcd_order(blockIdx.x, p.blocks);
+  const int per = p.key_tiles + p.parts - 1;
+  const int64_t bk = id / per;
+  const int item = (int)(id - bk * per);
+  const int tile = max(item - (p.parts - 1), 0), part = min(item, p.parts - 1);
+  const int b = (int)(bk / p.kv_heads), hk = (int)(bk - (int64_t)b * p.kv_heads);
+  const int ql = clamp_len(p.q_lens, b, p.q_tokens), kl = clamp_len(p.k_lens, b, p.k_tokens);
+  const int G = p.group, rows = ql * G, shift = kl - ql;
+  const int first = tile * kKeys;
+  if (first >= kl) return;
+  const int wfirst = first + 32 * wave, key = wfirst + l32, kc = min(key, kl - 1);
+  // Rows of the workgroup, of this wave, of this lane's key.
+  const int wlast = min(wfirst + 31, kl - 1);
+  Rows mine = rows_of(p.mask, kc, shift, rows, G, true);
+  if (key >= kl) mine = Rows{0, -1};
+  // The earliest row is that of the first key, the last that of the last key
+  // or, with a sink among the keys, of the first.
+  const Rows w0 = rows_of(p.mask, wfirst, shift, rows, G, true);
+  const Rows w1 = rows_of(p.mask, wlast, shift, rows, G, true);
+  const Rows n0 = rows_of(p.mask, first, shift, rows, G, true);
+  const Rows n1 = rows_of(p.mask, min(first + kKeys, kl) - 1, shift, rows, G, true);
+  int lo = n0.lo, hi = max(n0.hi, n1.hi);
+  const bool idle = wfirst >= kl;
+  const int wlo = w0.lo, whi = max(w0.hi, w1.hi);
+  // Rows that every key of the wave is seen by: up to the last of the first
+  // key's window (a sink's rows go on, those of the keys after it do not).
+  const int ilo = w1.lo, ihi = rows_of(p.mask, wfirst, shift, rows, G, false).hi;
+  const bool whole = wfirst + 31 < kl;
+  const int t_lo = lo / S::kRows, t_all = hi >= lo ? hi / S::kRows + 1 - t_lo : 0;
+  const bool split = p.parts > 1 && tile == 0;
+  const int ts = split ? (int)((int64_t)t_all * part / p.parts) : 0;
+  const int te = split ? (int)((int64_t)t_all * (part + 1) / p.parts) : t_all;
+
+  const char* qp = p.q.p + b * p.q.sb + (int64_t)hk * G * p.q.sh;
+  const char* dp_ = p.dout.p + b * p.dout.sb + (int64_t)hk * G * p.dout.sh;
+  const float2* stat = p.stat + bk * ((int64_t)p.q_tokens * G);
+  auto stage = [&](int n, char* dst) {
+    const int r0 = (t_lo + n) * S::kRows;
+    auto at = [&](const char* base, const View& t, int r) {
+      const int rr = min(r0 + r, rows - 1), i = rr / G, g = rr - i * G;
+      return base + (int64_t)i * t.st + (int64_t)g * t.sh;
+    };
+    Tl::template stage<S::kRows, kWaves>(dst, wave, lane, [&](int r) { return at(qp, p.q, r); });
+    Tl::template stage<S::kRows, kWaves>(dst + S::kTile, wave, lane, [&](int r) { return at(dp_, p.dout, r); });
+    // 64 rows' lse and D, 4 bytes a lane: two loads for the 512 bytes; every
+    // wave issues one, so that all count the same (waves 2 and 3 to the spare).
+    const int w = wave & 1, r = w * 32 + (lane >> 1);
+    const char* src = reinterpret_cast<const char*>(stat + min(r0 + r, rows - 1)) + (lane & 1) * 4;
+    __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)src,
+                                     (lds_void*)(dst + 2 * S::kTile + wave * 256), 4, 0, 0);
+  };
+
+  Frag<T> k[HD / 16], v[HD / 16];
+  const char* krow = p.k.p + b * p.k.sb + (int64_t)kc * p.k.st + hk * p.k.sh;
+  const char* vrow = p.v.p + b * p.v.sb + (int64_t)kc * p.v.st + hk * p.v.sh;
+#pragma unroll
+  for (int kk = 0; kk < HD / 16; ++kk) {
+    load_operand(krow, kk, h, k[kk]);
+    load_operand(vrow, kk, h, v[kk]);
+  }
+  f32x16 dk[HD / 32], dv[HD / 32];
+#pragma unroll
+  for (int n = 0; n < HD / 32; ++n) {
+    zero(dk[n]);
+    zero(dv[n]);
+  }
+  constexpr int kLoads = 2 * Tl::template loads<S::kRows, kWaves>() + 1;
+  constexpr int kBuf = 2 * S::kTile + S::kStat;
+  const unsigned len = (unsigned)max(mine.hi - mine.lo + 1, 0);
+  if (ts < te) stage(ts, smem);
+  for (int n = ts; n < te; ++n) {
+    const char* qt = smem + ((n - ts) & 1) * kBuf;
+    const char* dt = qt + S::kTile;
+    const f32x4* st = reinterpret_cast<const f32x4*>(qt + 2 * S::kTile);  // two rows each
+    if (n + 1 < te) {
+      stage(n + 1, smem + ((n + 1 - ts) & 1) * kBuf);
+      wait_and_meet<kLoads>();
+    } else {
+      wait_and_meet<0>();
+    }
+    const int r0 = (t_lo + n) * S::kRows, r1 = r0 + S::kRows - 1;
+    if (!idle && r1 >= wlo && r0 <= whi) {
+      const bool inside = whole && r0 >= ilo && r1 <= ihi;
+#pragma unroll
+      for (int s = 0; s < S::kSub; ++s) {
+        f32x16 sc, dp;
+        zero(sc);
+        zero(dp);
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk) {
+          Frag<T> a;
+          Tl::operand(qt, s * 32 + l32, kk, h, a);
+          sc = mma(a, k[kk], sc);
+          Tl::operand(dt, s * 32 + l32, kk, h, a);
+          dp = mma(a, v[kk], dp);
+        }
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          const int rr = s * 32 + 8 * (e >> 2) + 4 * h + (e & 3);
+          const f32x4 ld = st[rr >> 1];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            float pr = __builtin_amdgcn_exp2f(fmaf(sc[e + x], p.c2, -ld[2 * x]));
+            if (!inside) pr = (unsigned)(r0 + rr + x - mine.lo) < len ? pr : 0.0f;
+            sc[e + x] = pr;
+            dp[e + x] = pr * (dp[e + x] - ld[2 * x + 1]);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          Frag<T> pf, df;
+          as_operand(sc, u, pf);
+          as_operand(dp, u, df);
+#pragma unroll
+          for (int f = 0; f < HD / 32; ++f) {
+            Frag<T> a;
+            Tl::transposed(dt, s * 32 + u * 16, f, lane, a);
+            dv[f] = mma(a, pf, dv[f]);
+            Tl::transposed(qt, s * 32 + u * 16, f, lane, a);
+            dk[f] = mma(a, df, dk[f]);
+          }
+        }
+      }
+    }
+    asm volatile("" ::: "memory");
+    wait_lds();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  }
+  if (split) {
+    float* out = p.part + ((bk * p.parts + part) * 2 * kKeys + wave * 32 + l32) * (int64_t)HD;
+#pragma unroll
+    for (int n = 0; n < HD / 32; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int c = n * 32 + 8 * e + 4 * h;
+        store4(out + c, dk[n][4 * e], dk[n][4 * e + 1], dk[n][4 * e + 2], dk[n][4 * e + 3]);
+        store4(out + kKeys * HD + c, dv[n][4 * e], dv[n][4 * e + 1], dv[n][4 * e + 2], dv[n][4 * e + 3]);
+      }
+    return;
+  }
+  if (key >= kl) return;
+  T* ok = reinterpret_cast<T*>(p.dk.p + b * p.dk.sb + (int64_t)key * p.dk.st + hk * p.dk.sh);
+  T* ov = reinterpret_cast<T*>(p.dv.p + b * p.dv.sb + (int64_t)key * p.dv.st + hk * p.dv.sh);
+#pragma unroll
+  for (int n = 0; n < HD / 32; ++n)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int c = n * 32 + 8 * e + 4 * h;
+      store4(ok + c, dk[n][4 * e] * p.scale, dk[n][4 * e + 1] * p.scale, dk[n][4 * e + 2] * p.scale,
+             dk[n][4 * e + 3] * p.scale);
+      store4(ov + c, dv[n][4 * e], dv[n][4 * e + 1], dv[n][4 * e + 2], dv[n][4 * e + 3]);
+    }
+}
+
+// The first tile's keys: the parts' sums added up in order, four features a
+// thread, one workgroup a 1024 / HD keys.
+template <typename T, int HD>
+__global__ __launch_bounds__(kThreads) void window_sink_kernel(BwdP p) {
+  constexpr int kPer = HD / 4, kBlockKeys = kThreads / kPer;
+  const int64_t bk = blockIdx.x / (kKeys / kBlockKeys);
+  const int key = (int)(blockIdx.x % (kKeys / kBlockKeys)) * kBlockKeys + threadIdx.x / kPer;
+  const int c = (threadIdx.x % kPer) * 4;
+  const int b = (int)(bk / p.kv_heads), hk = (int)(bk - (int64_t)b * p.kv_heads);
+  if (key >= clamp_len(p.k_lens, b, p.k_tokens)) return;
+  f32x4 dk = {0.f, 0.f, 0.f, 0.f}, dv = dk;
+  for (int i = 0; i < p.parts; ++i) {
+    const float* in = p.part + ((bk * p.parts + i) * 2 * kKeys + key) * (int64_t)HD + c;
+    dk += *reinterpret_cast<const f32x4*>(in);
+    dv += *reinterpret_cast<const f32x4*>(in + kKeys * HD);
+  }
+  T* ok = reinterpret_cast<T*>(p.dk.p + b * p.dk.sb + (int64_t)key * p.dk.st + hk * p.dk.sh);
+  T* ov = reinterpret_cast<T*>(p.dv.p + b * p.dv.sb + (int64_t)key * p.dv.st + hk * p.dv.sh);
+  store4(ok + c, dk[0] * p.scale, dk[1] * p.scale, dk[2] * p.scale, dk[3] * p.scale);
+  store4(ov + c, dv[0], dv[1], dv[2], dv[3]);
+}
+
+// Parts of the first tile's rows: an ordinary tile has the rows of its own
+// positions and its window's, the first tile all that follow.
+int parts_of(const elasto_window_t& a) {
+  const int64_t G = a.heads / a.kv_heads, rows = (int64_t)a.q_tokens * G;
+  const int64_t near = (kKeys + (a.causal ? (int64_t)a.window : 2 * (int64_t)a.window)) * G;
+  if (a.sinks == 0) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(64, rows / std::max<int64_t>(near, 1024)));
+}
+
+int64_t stat_bytes(const elasto_window_t& a) { return (int64_t)a.batch * a.heads * a.q_tokens * 8; }
+
+template <typename T, int HD>
+hipError_t launch(BwdP p, int64_t pairs, hipStream_t s) {
+  hipError_t e = hipSuccess;
+  if (p.row_blocks > 0) {
+    p.blocks = pairs * p.row_blocks;
+    hipLaunchKernelGGL((window_dq_kernel<T, HD>), dim3((unsigned)p.blocks), dim3(kThreads),
+                       (Shape<T, HD>::kLdsRow), s, p);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess || p.key_tiles == 0) return e;
+  p.blocks = pairs * (p.key_tiles + p.parts - 1);
+  hipLaunchKernelGGL((window_dkv_kernel<T, HD>), dim3((unsigned)p.blocks), dim3(kThreads),
+                     (Shape<T, HD>::kLdsKey), s, p);
+  e = hipGetLastError();
+  if (e != hipSuccess || p.parts == 1) return e;
+  hipLaunchKernelGGL((window_sink_kernel<T, HD>), dim3((unsigned)(pairs * (kKeys * HD / 1024))),
+                     dim3(kThreads), 0, s, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t window_bwd_workspace(const elasto_window_t& a) {
+  const int parts = parts_of(a);
+  return (stat_bytes(a) + 255) / 256 * 256 +
+         (parts > 1 ? (int64_t)a.batch * a.kv_heads * parts * 2 * kKeys * a.head_dim * 4 : 0);
+}
+
+hipError_t launch_window_bwd(const elasto_window_t& a, const WindowTensors& t, void* ws, hipStream_t s) {
+  BwdP p = {};
+  p.q = t.q; p.k = t.k; p.v = t.v; p.o = t.o; p.dout = t.dout; p.dq = t.dq; p.dk = t.dk; p.dv = t.dv;
+  p.lse = t.lse;
+  p.q_lens = a.q_lens;
+  p.k_lens = a.k_lens;
+  p.q_tokens = a.q_tokens;
+  p.k_tokens = a.k_tokens;
+  p.heads = a.heads;
+  p.kv_heads = a.kv_heads;
+  p.group = a.heads / a.kv_heads;
+  p.mask = Mask{a.causal, a.window, a.sinks};
+  p.scale = a.scale;
+  p.c2 = a.scale * kLog2e;
+  const int64_t pairs = (int64_t)a.batch * a.kv_heads;
+  p.row_blocks = (int)(((int64_t)a.q_tokens * p.group + 32 * kWaves - 1) / (32 * kWaves));
+  p.key_tiles = (a.k_tokens + kKeys - 1) / kKeys;
+  p.parts = parts_of(a);
+  p.stat = static_cast<float2*>(ws);
+  p.part = reinterpret_cast<float*>(static_cast<char*>(ws) + (stat_bytes(a) + 255) / 256 * 256);
+  if (pairs * std::max(p.row_blocks, p.key_tiles + p.parts) > 0x7fffffff) return hipErrorInvalidValue;
+  if (a.dtype == ELASTO_BF16)
+    return a.head_dim == 64 ? launch<uint16_t, 64>(p, pairs, s) : launch<uint16_t, 128>(p, pairs, s);
+  return a.head_dim == 64 ? launch<float, 64>(p, pairs, s) : launch<float, 128>(p, pairs, s);
+}
+
+}  // namespace elasto

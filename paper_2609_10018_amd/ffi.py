@@ -81,6 +81,24 @@ class CNNTableC(ctypes.Structure):
                 ("order1", c_vp), ("order2", c_vp)]
 
 
+class Heads(ctypes.Structure):
+    _fields_ = [("data", c_vp), ("batch_stride", c_i64), ("token_stride", c_i64),
+                ("head_stride", c_i64)]
+
+
+class QkNorm(ctypes.Structure):
+    _fields_ = [(n, c_i32) for n in ("dtype", "batch", "tokens", "q_heads", "kv_heads", "head_dim",
+                                     "rot_dim", "interleaved", "table_rows")] + \
+               [("eps", c_f32)] + \
+               [(n, c_vp) for n in ("positions", "lens", "cos", "sin", "q_gamma", "k_gamma")]
+
+
+class Window(ctypes.Structure):
+    _fields_ = [(n, c_i32) for n in ("dtype", "batch", "q_tokens", "k_tokens", "heads", "kv_heads",
+                                     "head_dim", "causal", "window", "sinks")] + \
+               [("scale", c_f32), ("q_lens", c_vp), ("k_lens", c_vp)]
+
+
 _lib: Optional[ctypes.CDLL] = None
 
 
@@ -119,10 +137,22 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
                                 c_f32, c_vp],
         "elasto_op_conv2d": [c_vp, c_i32, c_i32, c_i32, c_i32, c_i32, c_i32, c_i32, c_i32, c_i32,
                              c_vp, c_i64, c_i64, c_vp, c_vp, c_i64, c_i32, c_i32, c_vp],
+        "elasto_op_qk_norm_rotate": [P(QkNorm)] + [P(Heads)] * 4 + [c_vp],
+        "elasto_op_qk_norm_rotate_bwd": [P(QkNorm)] + [P(Heads)] * 6 + [c_vp, c_vp, c_vp, c_i64, c_vp],
+        "elasto_qk_norm_rotate_workspace": [P(QkNorm), P(c_i64)],
+        "elasto_op_window_attention": [P(Window)] + [P(Heads)] * 4 + [c_vp, c_vp, c_i64, c_vp],
+        "elasto_op_window_attention_bwd": [P(Window)] + [P(Heads)] * 4 + [c_vp] + [P(Heads)] * 4 +
+                                          [c_vp, c_i64, c_vp],
+        "elasto_window_attention_workspace": [P(Window), c_i32, P(c_i64)],
+        "elasto_op_top_logits": [c_i32, c_vp, c_i64, c_i64, c_i32, c_i32, c_vp, c_vp, c_vp],
+        "elasto_op_distill": [c_i32, c_vp, c_i64, c_i64, c_i32, c_vp, c_vp, c_i32, c_vp, c_vp, c_f32,
+                              c_f32, c_f32, c_vp, c_i32, c_vp, c_i64, c_vp],
         "elasto_select_mode": [P(DNLut), c_f64, c_f64, c_f64, c_f64, P(c_i32)],
         "elasto_growth_create": [c_vp, c_i32, P(c_vp)],
         "elasto_growth_destroy": [c_vp],
         "elasto_growth_step": [c_vp, c_i32, c_vp, c_vp, c_i32, c_f32, c_f32, c_vp, c_vp],
+        "elasto_growth_step_distill": [c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, c_i32, c_f32, c_f32,
+                                       c_i32, c_f32, c_f32, c_vp, c_vp],
         "elasto_growth_read": [c_vp, c_i32, c_vp, c_i64],
         "elasto_profile_modes": [c_vp, c_vp, c_i32, c_vp, c_i32, c_i32, c_vp, P(c_f64), P(c_f64),
                                  P(c_f64)],
@@ -350,6 +380,231 @@ def op_attention(dtype: int, qkv, qkv_stride: int, o, o_stride: int, batch: int,
                                              _stream_ptr(stream)))
 
 
+def _same_device(*tensors) -> None:
+    """Refuse tensors that do not all lie on the current device: the kernels run there."""
+    import torch
+    d = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != d:
+            raise ValueError(f"a tensor lies on {t.device}, the current device is cuda:{d}")
+
+
+def _dtype(t) -> int:
+    name = str(t.dtype)
+    if name == "torch.bfloat16":
+        return BF16
+    if name == "torch.float32":
+        return FP32
+    raise ValueError(f"{name} is not supported: bfloat16 or float32")
+
+
+def _typed(want: str, **tensors) -> None:
+    """Contiguous device tensors of one element type (None passes)."""
+    for name, t in tensors.items():
+        if t is not None and (str(t.dtype) != want or not t.is_contiguous()):
+            raise ValueError(f"{name} must be contiguous and {want}")
+
+
+def _heads(t, shape, dtype, name: str):
+    """A [batch, tokens, heads, head_dim] tensor as the C ABI takes it (None: no heads)."""
+    if t is None:
+        return None
+    if tuple(t.shape) != shape or t.dtype != dtype:
+        raise ValueError(f"{name} is {tuple(t.shape)} {t.dtype}, not {shape} {dtype}")
+    s = t.stride()
+    if s[3] != 1 and shape[3] > 1:
+        raise ValueError(f"the features of {name} must be contiguous")
+    # The stride of an axis of one element means nothing; torch may give any.
+    n = shape[3]
+    return Heads(t.data_ptr(), *(s[i] if shape[i] > 1 else n for i in range(3)))
+
+
+def _qk_desc(q, k, cos, sin, q_gamma, k_gamma, positions, lens, eps, interleaved):
+    x = q if q is not None else k
+    b, t, _, d = x.shape
+    rot = 0 if cos is None else 2 * int(cos.shape[1])
+    if (cos is None) != (sin is None) or (cos is not None and cos.shape != sin.shape):
+        raise ValueError("cos and sin must be given together, of one shape")
+    _typed("torch.float32", cos=cos, sin=sin, q_gamma=q_gamma, k_gamma=k_gamma)
+    _typed("torch.int32", positions=positions, lens=lens)
+    for name, g in (("q_gamma", q_gamma), ("k_gamma", k_gamma)):
+        if g is not None and g.numel() != d:
+            raise ValueError(f"{name} has {g.numel()} elements, not {d}")
+    if positions is not None and tuple(positions.shape) != (b, t):
+        raise ValueError(f"positions is {tuple(positions.shape)}, not {(b, t)}")
+    if lens is not None and lens.numel() != b:
+        raise ValueError(f"lens has {lens.numel()} elements, not {b}")
+    _same_device(q, k, cos, sin, q_gamma, k_gamma, positions, lens)
+    return QkNorm(_dtype(x), b, t, 0 if q is None else int(q.shape[2]),
+                  0 if k is None else int(k.shape[2]), d, rot, int(bool(interleaved)),
+                  0 if cos is None else int(cos.shape[0]), eps, _ptr(positions), _ptr(lens),
+                  _ptr(cos), _ptr(sin), _ptr(q_gamma), _ptr(k_gamma))
+
+
+def qk_norm_rotate_workspace(q, k) -> int:
+    """Workspace bytes of op_qk_norm_rotate_bwd for these q and k."""
+    n = c_i64()
+    a = _qk_desc(q, k, None, None, None, None, None, None, 1.0, False)
+    check(load_library().elasto_qk_norm_rotate_workspace(ctypes.byref(a), ctypes.byref(n)))
+    return n.value
+
+
+def op_qk_norm_rotate(q, k, q_out, k_out, cos=None, sin=None, q_gamma=None, k_gamma=None,
+                      positions=None, lens=None, eps: float = 1e-6, interleaved: bool = False,
+                      stream=None) -> None:
+    """q, q_out: [batch, tokens, heads, head_dim] device tensors of any strides (the features
+    contiguous); k, k_out likewise with their own heads; either pair may be None.  cos, sin: fp32
+    [rows, rot_dim / 2] (None: no rotation).  positions: int32 [batch, tokens]; lens: int32
+    [batch]."""
+    a = _qk_desc(q, k, cos, sin, q_gamma, k_gamma, positions, lens, eps, interleaved)
+    _same_device(q_out, k_out)
+    h = [_heads(t, (a.batch, a.tokens, n, a.head_dim), (q if q is not None else k).dtype, name)
+         for t, n, name in ((q, a.q_heads, "q"), (k, a.kv_heads, "k"), (q_out, a.q_heads, "q_out"),
+                            (k_out, a.kv_heads, "k_out"))]
+    check(load_library().elasto_op_qk_norm_rotate(a, *h, _stream_ptr(stream)))
+
+
+def op_qk_norm_rotate_bwd(q, k, dq_out, dk_out, dq, dk, dq_gamma=None, dk_gamma=None,
+                          workspace=None, cos=None, sin=None, q_gamma=None, k_gamma=None,
+                          positions=None, lens=None, eps: float = 1e-6, interleaved: bool = False,
+                          stream=None) -> None:
+    """dq_out, dk_out: the gradients of op_qk_norm_rotate's results; dq, dk: those of q and k;
+    dq_gamma, dk_gamma: fp32 [head_dim] or None.  workspace: a uint8 device tensor of
+    qk_norm_rotate_workspace() bytes where a weight gradient is asked for."""
+    a = _qk_desc(q, k, cos, sin, q_gamma, k_gamma, positions, lens, eps, interleaved)
+    _typed("torch.float32", dq_gamma=dq_gamma, dk_gamma=dk_gamma)
+    _typed("torch.uint8", workspace=workspace)
+    for name, g in (("dq_gamma", dq_gamma), ("dk_gamma", dk_gamma)):
+        if g is not None and g.numel() != a.head_dim:
+            raise ValueError(f"{name} has {g.numel()} elements, not {a.head_dim}")
+    _same_device(dq_out, dk_out, dq, dk, dq_gamma, dk_gamma, workspace)
+    h = [_heads(t, (a.batch, a.tokens, n, a.head_dim), (q if q is not None else k).dtype, name)
+         for t, n, name in ((q, a.q_heads, "q"), (k, a.kv_heads, "k"),
+                            (dq_out, a.q_heads, "dq_out"), (dk_out, a.kv_heads, "dk_out"),
+                            (dq, a.q_heads, "dq"), (dk, a.kv_heads, "dk"))]
+    check(load_library().elasto_op_qk_norm_rotate_bwd(
+        a, *h, _ptr(dq_gamma), _ptr(dk_gamma), _ptr(workspace),
+        0 if workspace is None else workspace.numel(), _stream_ptr(stream)))
+
+
+def _window_desc(q, k, window, sinks, causal, scale, q_lens, k_lens):
+    if q.dim() != 4 or k.dim() != 4 or q.shape[0] != k.shape[0] or q.shape[3] != k.shape[3]:
+        raise ValueError(f"q {tuple(q.shape)} and k {tuple(k.shape)} do not go together")
+    b, tq, h, d = q.shape
+    _typed("torch.int32", q_lens=q_lens, k_lens=k_lens)
+    for name, n in (("q_lens", q_lens), ("k_lens", k_lens)):
+        if n is not None and n.numel() != b:
+            raise ValueError(f"{name} has {n.numel()} elements, not {b}")
+    return Window(_dtype(q), b, tq, int(k.shape[1]), h, int(k.shape[2]), d, int(bool(causal)),
+                  min(int(window), 2 ** 31 - 1), int(sinks),
+                  1.0 / math.sqrt(d) if scale is None else scale, _ptr(q_lens), _ptr(k_lens))
+
+
+def window_attention_workspace(q, k, window: int, sinks: int = 0, causal: bool = True,
+                               backward: bool = False) -> int:
+    """Workspace bytes of op_window_attention (backward: op_window_attention_bwd) for tensors of
+    these shapes."""
+    n = c_i64()
+    a = _window_desc(q, k, window, sinks, causal, None, None, None)
+    check(load_library().elasto_window_attention_workspace(a, int(bool(backward)), ctypes.byref(n)))
+    return n.value
+
+
+def op_window_attention(q, k, v, o, window: int, sinks: int = 0, causal: bool = True,
+                        scale: Optional[float] = None, lse=None, q_lens=None, k_lens=None,
+                        workspace=None, stream=None) -> None:
+    """q, o: [batch, q_tokens, heads, head_dim] device tensors of any strides (the features
+    contiguous); k, v: [batch, k_tokens, kv_heads, head_dim].  lse: fp32 [batch, heads, q_tokens]
+    or None.  q_lens, k_lens: int32 [batch] or None.  scale: None for 1 / sqrt(head_dim).
+    workspace: a uint8 device tensor of window_attention_workspace() bytes."""
+    a = _window_desc(q, k, window, sinks, causal, scale, q_lens, k_lens)
+    _same_device(q, k, v, o, lse, q_lens, k_lens, workspace)
+    _typed("torch.float32", lse=lse)
+    _typed("torch.uint8", workspace=workspace)
+    if lse is not None and lse.numel() != a.batch * a.heads * a.q_tokens:
+        raise ValueError(f"lse has {lse.numel()} elements")
+    sq, sk = tuple(q.shape), tuple(k.shape)
+    check(load_library().elasto_op_window_attention(
+        a, _heads(q, sq, q.dtype, "q"), _heads(k, sk, q.dtype, "k"), _heads(v, sk, q.dtype, "v"),
+        _heads(o, sq, q.dtype, "o"), _ptr(lse), _ptr(workspace),
+        0 if workspace is None else workspace.numel(), _stream_ptr(stream)))
+
+
+def op_window_attention_bwd(q, k, v, o, lse, dout, dq, dk, dv, window: int, sinks: int = 0,
+                            causal: bool = True, scale: Optional[float] = None, q_lens=None,
+                            k_lens=None, workspace=None, stream=None) -> None:
+    """The gradients dq, dk, dv (shaped like q, k, v) from dout (like o), with op_window_attention's
+    o and lse."""
+    a = _window_desc(q, k, window, sinks, causal, scale, q_lens, k_lens)
+    _same_device(q, k, v, o, lse, dout, dq, dk, dv, q_lens, k_lens, workspace)
+    _typed("torch.float32", lse=lse)
+    _typed("torch.uint8", workspace=workspace)
+    if lse.numel() != a.batch * a.heads * a.q_tokens:
+        raise ValueError(f"lse has {lse.numel()} elements")
+    sq, sk, dt = tuple(q.shape), tuple(k.shape), q.dtype
+    h = {n: _heads(t, s, dt, n) for n, t, s in (
+        ("q", q, sq), ("k", k, sk), ("v", v, sk), ("o", o, sq), ("dout", dout, sq), ("dq", dq, sq),
+        ("dk", dk, sk), ("dv", dv, sk))}
+    check(load_library().elasto_op_window_attention_bwd(
+        a, h["q"], h["k"], h["v"], h["o"], _ptr(lse), h["dout"], h["dq"], h["dk"], h["dv"],
+        _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream)))
+
+
+def _rows(t, name: str):
+    """A [rows, classes] tensor with contiguous rows: (rows, classes, row stride)."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"{name} must be [rows, classes] with contiguous rows")
+    r, c = t.shape
+    return r, c, t.stride(0) if r > 1 else c
+
+
+def op_top_logits(logits, values, indices, stream=None) -> None:
+    """logits: bf16 or fp32 [rows, classes] device tensor (any row stride); values: fp32 and
+    indices: int32, [rows, top]."""
+    r, c, ld = _rows(logits, "logits")
+    _typed("torch.float32", values=values)
+    _typed("torch.int32", indices=indices)
+    if values.dim() != 2 or values.shape != indices.shape or values.shape[0] != r:
+        raise ValueError(f"values {tuple(values.shape)} and indices {tuple(indices.shape)} must be "
+                         f"[{r}, top]")
+    _same_device(logits, values, indices)
+    check(load_library().elasto_op_top_logits(_dtype(logits), logits.data_ptr(), ld, r, c,
+                                              int(values.shape[1]), values.data_ptr(),
+                                              indices.data_ptr(), _stream_ptr(stream)))
+
+
+def op_distill(logits, teacher_values, teacher_indices, loss, dlogits=None, labels=None,
+               temperature: float = 1.0, alpha: float = 1.0, row_weight=None, scale: float = 1.0,
+               stream=None) -> None:
+    """logits: bf16 or fp32 [rows, classes] device tensor (any row stride); teacher_values: fp32
+    and teacher_indices: int32, [rows, top] (None with alpha 0); loss: fp32 [rows]; dlogits: bf16
+    or fp32 [rows, classes] or None; labels: int32 [rows] or None; row_weight: fp32 [rows] or
+    None."""
+    r, c, ld = _rows(logits, "logits")
+    _typed("torch.float32", teacher_values=teacher_values, loss=loss, row_weight=row_weight)
+    _typed("torch.int32", teacher_indices=teacher_indices, labels=labels)
+    top = 0
+    if teacher_values is not None:
+        if (teacher_indices is None or teacher_values.dim() != 2 or teacher_values.shape[0] != r
+                or teacher_values.shape != teacher_indices.shape):
+            raise ValueError(f"teacher values and indices must both be [{r}, top]")
+        top = int(teacher_values.shape[1])
+    for name, t in (("loss", loss), ("labels", labels), ("row_weight", row_weight)):
+        if t is not None and t.numel() != r:
+            raise ValueError(f"{name} has {t.numel()} elements, not {r}")
+    gd, ldg = _dtype(logits), ld
+    if dlogits is not None:
+        rg, cg, ldg = _rows(dlogits, "dlogits")
+        if (rg, cg) != (r, c):
+            raise ValueError(f"dlogits is {(rg, cg)}, not {(r, c)}")
+        gd = _dtype(dlogits)
+    _same_device(logits, teacher_values, teacher_indices, loss, dlogits, labels, row_weight)
+    check(load_library().elasto_op_distill(
+        _dtype(logits), logits.data_ptr(), ld, r, c, _ptr(teacher_values), _ptr(teacher_indices),
+        top, _ptr(labels), _ptr(row_weight), float(temperature), float(alpha), float(scale),
+        loss.data_ptr(), gd, _ptr(dlogits), ldg, _stream_ptr(stream)))
+
+
 class GrowthContext:
     """Growth-step state of a bf16 ElasticViT handle (fp32 masters, saved
     activations, gradients) for batches of up to max_batch images."""
@@ -370,6 +625,24 @@ class GrowthContext:
         check(self.lib.elasto_growth_step(self.g, int(mode), images.data_ptr(), labels.data_ptr(),
                                           int(images.shape[0]), float(lr), float(clip),
                                           _ptr(stats), _stream_ptr(stream)))
+
+    def step_distill(self, mode: int, images, labels, teacher_values, teacher_indices, lr: float,
+                     clip: float, temperature: float = 1.0, alpha: float = 1.0, stats=None,
+                     stream=None) -> None:
+        """The growth step with op_distill's loss: teacher_values (fp32) and teacher_indices
+        (int32) are [batch, top] device tensors; labels may be None with alpha 1."""
+        if not images.is_contiguous() or (labels is not None and not labels.is_contiguous()):
+            raise ValueError("images and labels must be contiguous")
+        _typed("torch.float32", teacher_values=teacher_values)
+        _typed("torch.int32", teacher_indices=teacher_indices, labels=labels)
+        n = int(images.shape[0])
+        if teacher_values.dim() != 2 or teacher_values.shape != teacher_indices.shape or \
+                teacher_values.shape[0] != n or (labels is not None and labels.numel() != n):
+            raise ValueError(f"teacher values and indices must be [{n}, top], labels [{n}]")
+        check(self.lib.elasto_growth_step_distill(
+            self.g, int(mode), images.data_ptr(), _ptr(labels), teacher_values.data_ptr(),
+            teacher_indices.data_ptr(), int(teacher_values.shape[1]), float(temperature),
+            float(alpha), n, float(lr), float(clip), _ptr(stats), _stream_ptr(stream)))
 
     def read(self, which: int) -> np.ndarray:
         """which 0: packed weights (uint8); 1: fp32 masters (float32, one per bf16 element)."""
@@ -496,4 +769,7 @@ def select_mode(flops, latency_ms, memory_bytes, accuracy=None, power_w=None,
 
 __all__ = ["ElasticViT", "ElasticResNet", "cnn_validate", "select_mode", "ElastoError", "load_library", "validate", "packed_bytes",
            "packed_layout", "pack_weights", "op_layernorm", "op_linear", "op_linear_ln", "op_attention",
+           "op_qk_norm_rotate", "op_qk_norm_rotate_bwd", "qk_norm_rotate_workspace",
+           "op_window_attention", "op_window_attention_bwd", "window_attention_workspace",
+           "op_top_logits", "op_distill",
            "KERNELS", "FP32", "BF16"]
