@@ -134,7 +134,7 @@ struct State {
 };
 
 template <typename T, int HD, bool KEYS>
-__global__ __launch_bounds__(kThreads) void window_fwd_kernel(FwdP p) {
+__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) void window_fwd_kernel(FwdP p) {
   using S = Shape<T, HD, KEYS>;
   using Tl = Tile<T, HD>;
   extern __shared__ __attribute__((aligned(16))) char smem[];

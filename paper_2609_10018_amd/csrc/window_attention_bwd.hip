@@ -57,7 +57,7 @@ struct Shape {
 };
 
 template <typename T, int HD>
-__global__ __launch_bounds__(kThreads) void window_dq_kernel(BwdP p) {
+__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) void window_dq_kernel(BwdP p) {
   using S = Shape<T, HD>;
   using Tl = Tile<T, HD>;
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -195,7 +195,7 @@ __device__ __forceinline__ Rows rows_of(const Mask& m, int j, int shift, int row
 }
 
 template <typename T, int HD>
-__global__ __launch_bounds__(kThreads) void window_dkv_kernel(BwdP p) {
+__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) void window_dkv_kernel(BwdP p) {
   using S = Shape<T, HD>;
   using Tl = Tile<T, HD>;
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -284,7 +284,7 @@ __global__ __launch_bounds__(kThreads) void window_dkv_kernel(BwdP p) {
     const int r0 = (t_lo + n) * S::kRows, r1 = r0 + S::kRows - 1;
     if (!idle && r1 >= wlo && r0 <= whi) {
       const bool inside = whole && r0 >= ilo && r1 <= ihi;
-#pragma unroll
+#pragma unroll 1
       for (int s = 0; s < S::kSub; ++s) {
         f32x16 sc, dp;
         zero(sc);
