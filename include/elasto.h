@@ -440,7 +440,7 @@ elasto_status_t elasto_op_conv2d(const void* x, int32_t batch, int32_t H, int32_
  * order (so q, k and v may lie head by head in one buffer, as the q/k/v
  * projection writes them: head_stride 3 * head_dim, token_stride qkv_stride;
  * or in a cache of [batch][kv_heads][capacity][head_dim]).  data and every
- * stride are multiples of 16 bytes.  Strides of tensors that are written are
+ * stride are multiples of 16 bytes, no stride is negative.  Strides of tensors that are written are
  * at least head_dim along axes longer than 1; rows of one tensor must not
  * overlap, nor written tensors others unless stated. */
 typedef struct {
@@ -513,7 +513,9 @@ elasto_status_t elasto_qk_norm_rotate_workspace(const elasto_qk_norm_t* desc, in
  * same bits every time.
  * Needs head_dim 64 or 128, heads a multiple of kv_heads, window >= 1,
  * 0 <= sinks <= 64, scale > 0; k_tokens, q_tokens * heads / kv_heads and
- * batch * heads at most 2^29. */
+ * batch * heads at most 2^29; 64 tokens of a head of k and of v (backward: of
+ * the heads / kv_heads heads of q and of dout that share a key head) within
+ * 4 GiB. */
 typedef struct {
   int32_t dtype, batch, q_tokens, k_tokens, heads, kv_heads, head_dim;
   int32_t causal, window, sinks;

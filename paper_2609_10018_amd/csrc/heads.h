@@ -24,6 +24,8 @@ inline bool take_view(const char* op, const char* name, const elasto_heads_t* t,
   if (!aligned(t->data, 16) || t->batch_stride * es % 16 || t->token_stride * es % 16 ||
       t->head_stride * es % 16)
     return fail(ELASTO_ERR_INVALID_ARG, "%s: %s and its strides must be multiples of 16 bytes", op, name), false;
+  if (t->batch_stride < 0 || t->token_stride < 0 || t->head_stride < 0)
+    return fail(ELASTO_ERR_INVALID_ARG, "%s: %s has a negative stride", op, name), false;
   if (written && ((batch > 1 && t->batch_stride < dim) || (tokens > 1 && t->token_stride < dim) ||
                   (heads > 1 && t->head_stride < dim)))
     return fail(ELASTO_ERR_INVALID_ARG, "%s: rows of %s overlap", op, name), false;

@@ -148,26 +148,35 @@ struct Tile {
     return r * kRow + ((piece ^ (r & kXor)) << 4);
   }
 
-  // Loads rows [0, ROWS) straight to LDS, the blocks of 1 KB shared out over
-  // WAVES waves; addr(r) is where row r lies in memory.  ROWS * kRow / 1024 /
-  // WAVES loads a wave.
-  template <int ROWS, int WAVES, typename F>
-  static __device__ __forceinline__ void stage(char* tile, int wave, int lane, F&& addr) {
-    constexpr int kBlocks = ROWS / kBlockRows;
-    static_assert(kBlocks % WAVES == 0, "every wave loads the same number of blocks");
-#pragma unroll
-    for (int i = 0; i < kBlocks / WAVES; ++i) {
-      const int blk = wave + WAVES * i;
-      const int r = blk * kBlockRows + lane / kPieces;
-      const int c = (lane % kPieces) ^ (r & kXor);
-      __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)(addr(r) + c * 16),
-                                       (lds_void*)(tile + blk * 1024), 16, 0, 0);
-    }
-  }
+  // Loads of ROWS rows straight to LDS, the blocks of 1 KB shared out over
+  // WAVES waves: kLoads a wave, each lane 16 bytes at a constant offset from
+  // the tile's first row.
   template <int ROWS, int WAVES>
-  static constexpr int loads() {
-    return ROWS / kBlockRows / WAVES;
-  }
+  struct Loads {
+    static constexpr int kLoads = ROWS / kBlockRows / WAVES;
+    static_assert(ROWS % (kBlockRows * WAVES) == 0, "every wave loads the same number of blocks");
+    uint32_t off[kLoads];
+
+    // offset(r): where row r lies after the first.
+    template <typename F>
+    __device__ __forceinline__ void set(int wave, int lane, F&& offset) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int r = (wave + WAVES * i) * kBlockRows + lane / kPieces;
+        off[i] = offset(r) + (((lane % kPieces) ^ (r & kXor)) << 4);
+      }
+    }
+    // From `bytes` bytes at base; what lies past them arrives as zeros.
+    __device__ __forceinline__ void issue(char* tile, int wave, const char* base, int64_t bytes) const {
+      const __amdgpu_buffer_rsrc_t src = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<char*>(base), (short)0, (int)(uint32_t)(bytes < 0xffffffffll ? bytes : 0xffffffffll),
+          kRsrcWord3);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(tile + (wave + WAVES * i) * 1024), 16,
+                                                 (int)off[i], 0, 0, 0);
+    }
+  };
 
   // Row r, features 16kk + 8h + 0..7.
   static __device__ __forceinline__ void operand(const char* tile, int r, int kk, int h, Frag<T>& f) {

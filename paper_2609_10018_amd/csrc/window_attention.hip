@@ -7,8 +7,9 @@
 //
 // Scores are taken transposed, S^T = K Q^T: a lane holds one row's scores, so
 // the softmax needs one exchange between the half-waves a tile, and the
-// probabilities (rounded to bf16 on the bf16 path, after the sum has been taken
-// in fp32) are the operand of O^T = V^T P^T without moving.
+// probabilities (rounded to bf16 on the bf16 path; their sum is taken before, in
+// fp32, since lse is an fp32 result) are the operand of O^T = V^T P^T without
+// moving.
 //
 // Two shapes of a workgroup of four waves:
 // * rows: 128 rows, 32 a wave, which share each tile of keys;
@@ -172,14 +173,17 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
 
   const char* kp = p.k.p + b * p.k.sb + hk * p.k.sh;
   const char* vp = p.v.p + b * p.v.sb + hk * p.v.sh;
+  // Keys past the last one arrive as zeros: they are masked, and what the
+  // memory holds there is not read.
+  using Ld = typename Tl::template Loads<S::kKeys, KEYS ? 1 : kWaves>;
+  Ld lk, lv;
+  const int lw = KEYS ? 0 : wave;
+  lk.set(lw, lane, [&](int r) { return (uint32_t)r * (uint32_t)p.k.st; });
+  lv.set(lw, lane, [&](int r) { return (uint32_t)r * (uint32_t)p.v.st; });
   auto stage = [&](int n, char* dst) {
     const int j0 = key0(n);
-    const int w = KEYS ? 0 : wave;
-    constexpr int W = KEYS ? 1 : kWaves;
-    // Keys past the last one are that one again: they are masked, and what the
-    // memory holds there is not read.
-    Tl::template stage<S::kKeys, W>(dst, w, lane, [&](int r) { return kp + (int64_t)min(j0 + r, kl - 1) * p.k.st; });
-    Tl::template stage<S::kKeys, W>(dst + S::kTile, w, lane, [&](int r) { return vp + (int64_t)min(j0 + r, kl - 1) * p.v.st; });
+    lk.issue(dst, lw, kp + j0 * p.k.st, (kl - 1 - j0) * p.k.st + Tl::kRow);
+    lv.issue(dst + S::kTile, lw, vp + j0 * p.v.st, (kl - 1 - j0) * p.v.st + Tl::kRow);
   };
 
   State<T, HD> st;
@@ -196,7 +200,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
     const bool inside = j0 >= w1.lo && j1 <= w0.hi;
     st.template tile<S::kSub>(buf, buf + S::kTile, j0, q, p.c2, inside, mine, lane);
   };
-  constexpr int kLoads = 2 * Tl::template loads<S::kKeys, KEYS ? 1 : kWaves>();
+  constexpr int kLoads = 2 * Ld::kLoads;
   char* mem = smem + (KEYS ? wave * S::kBuffers * 2 * S::kTile : 0);
   const int step = KEYS ? kWaves : 1;
   int n = zs + (KEYS ? wave : 0);

@@ -87,10 +87,14 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   auto key0 = [&](int n) { return (n < sink_tiles ? n : t0 + n - sink_tiles) * S::kRows; };
   const char* kp = p.k.p + b * p.k.sb + hk * p.k.sh;
   const char* vp = p.v.p + b * p.v.sb + hk * p.v.sh;
+  using Ld = typename Tl::template Loads<S::kRows, kWaves>;
+  Ld lk, lv;
+  lk.set(wave, lane, [&](int r) { return (uint32_t)r * (uint32_t)p.k.st; });
+  lv.set(wave, lane, [&](int r) { return (uint32_t)r * (uint32_t)p.v.st; });
   auto stage = [&](int n, char* dst) {
     const int j0 = key0(n);
-    Tl::template stage<S::kRows, kWaves>(dst, wave, lane, [&](int r) { return kp + (int64_t)min(j0 + r, kl - 1) * p.k.st; });
-    Tl::template stage<S::kRows, kWaves>(dst + S::kTile, wave, lane, [&](int r) { return vp + (int64_t)min(j0 + r, kl - 1) * p.v.st; });
+    lk.issue(dst, wave, kp + j0 * p.k.st, (kl - 1 - j0) * p.k.st + Tl::kRow);
+    lv.issue(dst + S::kTile, wave, vp + j0 * p.v.st, (kl - 1 - j0) * p.v.st + Tl::kRow);
   };
 
   Frag<T> q[HD / 16], d[HD / 16];
@@ -114,7 +118,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   f32x16 dq[HD / 32];
 #pragma unroll
   for (int n = 0; n < HD / 32; ++n) zero(dq[n]);
-  constexpr int kLoads = 2 * Tl::template loads<S::kRows, kWaves>();
+  constexpr int kLoads = 2 * Ld::kLoads;
   if (tiles > 0) stage(0, smem);
   for (int n = 0; n < tiles; ++n) {
     const char* kt = smem + (n & 1) * 2 * S::kTile;
@@ -143,15 +147,17 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
           Tl::operand(vt, s * 32 + l32, kk, h, a);
           dp = mma(a, d[kk], dp);
         }
+        if (!inside) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          float pr = __builtin_amdgcn_exp2f(fmaf(sc[e], p.c2, -l2));
-          if (!inside) {
+          for (int e = 0; e < 16; ++e) {
             const int j = j0 + s * 32 + 8 * (e >> 2) + 4 * h + (e & 3);
-            pr = j <= mine.hs || (unsigned)(j - mine.lo) < len ? pr : 0.0f;
+            const bool sees = j <= mine.hs || (unsigned)(j - mine.lo) < len;
+            sc[e] = sees ? sc[e] : -INFINITY;
           }
-          sc[e] = pr * (dp[e] - D);
         }
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          sc[e] = __builtin_amdgcn_exp2f(fmaf(sc[e], p.c2, -l2)) * (dp[e] - D);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           Frag<T> df;
@@ -229,7 +235,12 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   // key's window (a sink's rows go on, those of the keys after it do not).
   const int ilo = w1.lo, ihi = rows_of(p.mask, wfirst, shift, rows, G, false).hi;
   const bool whole = wfirst + 31 < kl;
-  const int t_lo = lo / S::kRows, t_all = hi >= lo ? hi / S::kRows + 1 - t_lo : 0;
+  // A tile holds whole queries, so that a row's place in it is the same in every
+  // tile: the most of them whose rows it can take (groups larger than a tile:
+  // rows as they come, placed row by row).
+  const bool whole_queries = G <= S::kRows;
+  const int step = whole_queries ? S::kRows / G * G : S::kRows;
+  const int t_lo = lo / step, t_all = hi >= lo ? hi / step + 1 - t_lo : 0;
   const bool split = p.parts > 1 && tile == 0;
   const int ts = split ? (int)((int64_t)t_all * part / p.parts) : 0;
   const int te = split ? (int)((int64_t)t_all * (part + 1) / p.parts) : t_all;
@@ -237,17 +248,34 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   const char* qp = p.q.p + b * p.q.sb + (int64_t)hk * G * p.q.sh;
   const char* dp_ = p.dout.p + b * p.dout.sb + (int64_t)hk * G * p.dout.sh;
   const float2* stat = p.stat + bk * ((int64_t)p.q_tokens * G);
+  using Ld = typename Tl::template Loads<S::kRows, kWaves>;
+  Ld lq, ld;
+  // Offsets from the tile's first query i0; rows past the last are that one again.
+  auto set = [&](Ld& l, const View& t, int r0, int i0, int last) {
+    l.set(wave, lane, [&](int r) {
+      const int rr = min(r0 + r, last), i = rr / G;
+      return (uint32_t)(i - i0) * (uint32_t)t.st + (uint32_t)(rr - i * G) * (uint32_t)t.sh;
+    });
+  };
+  set(lq, p.q, 0, 0, step - 1);
+  set(ld, p.dout, 0, 0, step - 1);
   auto stage = [&](int n, char* dst) {
-    const int r0 = (t_lo + n) * S::kRows;
-    auto at = [&](const char* base, const View& t, int r) {
-      const int rr = min(r0 + r, rows - 1), i = rr / G, g = rr - i * G;
-      return base + (int64_t)i * t.st + (int64_t)g * t.sh;
-    };
-    Tl::template stage<S::kRows, kWaves>(dst, wave, lane, [&](int r) { return at(qp, p.q, r); });
-    Tl::template stage<S::kRows, kWaves>(dst + S::kTile, wave, lane, [&](int r) { return at(dp_, p.dout, r); });
+    const int r0 = (t_lo + n) * step, i0 = r0 / G;
+    const char* qb = qp + i0 * p.q.st;
+    const char* db = dp_ + i0 * p.dout.st;
+    if (whole_queries && r0 + step <= rows) {
+      lq.issue(dst, wave, qb, 0xffffffffll);
+      ld.issue(dst + S::kTile, wave, db, 0xffffffffll);
+    } else {
+      Ld l;
+      set(l, p.q, r0, i0, rows - 1);
+      l.issue(dst, wave, qb, 0xffffffffll);
+      set(l, p.dout, r0, i0, rows - 1);
+      l.issue(dst + S::kTile, wave, db, 0xffffffffll);
+    }
     // 64 rows' lse and D, 4 bytes a lane: two loads for the 512 bytes; every
     // wave issues one, so that all count the same (waves 2 and 3 to the spare).
-    const int w = wave & 1, r = w * 32 + (lane >> 1);
+    const int r = (wave & 1) * 32 + (lane >> 1);
     const char* src = reinterpret_cast<const char*>(stat + min(r0 + r, rows - 1)) + (lane & 1) * 4;
     __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)src,
                                      (lds_void*)(dst + 2 * S::kTile + wave * 256), 4, 0, 0);
@@ -267,9 +295,8 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
     zero(dk[n]);
     zero(dv[n]);
   }
-  constexpr int kLoads = 2 * Tl::template loads<S::kRows, kWaves>() + 1;
+  constexpr int kLoads = 2 * Ld::kLoads + 1;
   constexpr int kBuf = 2 * S::kTile + S::kStat;
-  const unsigned len = (unsigned)max(mine.hi - mine.lo + 1, 0);
   if (ts < te) stage(ts, smem);
   for (int n = ts; n < te; ++n) {
     const char* qt = smem + ((n - ts) & 1) * kBuf;
@@ -281,9 +308,10 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
     } else {
       wait_and_meet<0>();
     }
-    const int r0 = (t_lo + n) * S::kRows, r1 = r0 + S::kRows - 1;
+    const int r0 = (t_lo + n) * step, r1 = r0 + step - 1;
     if (!idle && r1 >= wlo && r0 <= whi) {
-      const bool inside = whole && r0 >= ilo && r1 <= ihi;
+      const bool inside = whole && step == S::kRows && r0 >= ilo && r1 <= ihi;
+      const unsigned len = (unsigned)max(min(mine.hi, r1) - mine.lo + 1, 0);
 #pragma unroll 1
       for (int s = 0; s < S::kSub; ++s) {
         f32x16 sc, dp;
@@ -297,17 +325,20 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
           Tl::operand(dt, s * 32 + l32, kk, h, a);
           dp = mma(a, v[kk], dp);
         }
+        if (!inside) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int r = r0 + s * 32 + 8 * (e >> 2) + 4 * h + (e & 3);
+            sc[e] = (unsigned)(r - mine.lo) < len ? sc[e] : -INFINITY;
+          }
+        }
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
-          const int rr = s * 32 + 8 * (e >> 2) + 4 * h + (e & 3);
-          const f32x4 ld = st[rr >> 1];
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            float pr = __builtin_amdgcn_exp2f(fmaf(sc[e + x], p.c2, -ld[2 * x]));
-            if (!inside) pr = (unsigned)(r0 + rr + x - mine.lo) < len ? pr : 0.0f;
-            sc[e + x] = pr;
-            dp[e + x] = pr * (dp[e + x] - ld[2 * x + 1]);
-          }
+          const f32x4 x = st[(s * 32 + 8 * (e >> 2) + 4 * h + (e & 3)) >> 1];
+          sc[e] = __builtin_amdgcn_exp2f(fmaf(sc[e], p.c2, -x[0]));
+          sc[e + 1] = __builtin_amdgcn_exp2f(fmaf(sc[e + 1], p.c2, -x[2]));
+          dp[e] = sc[e] * (dp[e] - x[1]);
+          dp[e + 1] = sc[e + 1] * (dp[e + 1] - x[3]);
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {

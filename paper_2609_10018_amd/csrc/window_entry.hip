@@ -40,6 +40,15 @@ bool set_view(const char* name, const elasto_window_t& a, const elasto_heads_t* 
                    a.dtype == ELASTO_BF16 ? 2 : 4, written, v);
 }
 
+// Tiles of up to 64 tokens (of `heads` heads together) are loaded at 32-bit
+// offsets from their first row.
+bool check_reach(const char* name, const View& v, int heads) {
+  const int64_t limit = (int64_t)1 << 32;
+  if (v.st > limit || v.sh > limit || 64 * v.st + (heads - 1) * v.sh + 512 >= limit)
+    return fail(ELASTO_ERR_INVALID_ARG, "window attention: 64 tokens of %s span 4 GiB or more", name), false;
+  return true;
+}
+
 bool check_ws(const void* ws, int64_t have, int64_t need) {
   if (need == 0) return true;
   if (!ws || have < need)
@@ -73,7 +82,8 @@ elasto_status_t elasto_op_window_attention(const elasto_window_t* desc, const el
   if (!set_view("q", a, q, a.q_tokens, a.heads, false, &t.q) ||
       !set_view("k", a, k, a.k_tokens, a.kv_heads, false, &t.k) ||
       !set_view("v", a, v, a.k_tokens, a.kv_heads, false, &t.v) ||
-      !set_view("o", a, o, a.q_tokens, a.heads, true, &t.o))
+      !set_view("o", a, o, a.q_tokens, a.heads, true, &t.o) || !check_reach("k", t.k, 1) ||
+      !check_reach("v", t.v, 1))
     return ELASTO_ERR_INVALID_ARG;
   if (!aligned(lse, 4)) return fail(ELASTO_ERR_INVALID_ARG, "window attention: misaligned lse");
   if (!check_ws(workspace, workspace_bytes, window_fwd_workspace(a))) return ELASTO_ERR_INVALID_ARG;
@@ -101,7 +111,9 @@ elasto_status_t elasto_op_window_attention_bwd(const elasto_window_t* desc, cons
       !set_view("dout", a, dout, a.q_tokens, a.heads, false, &t.dout) ||
       !set_view("dq", a, dq, a.q_tokens, a.heads, true, &t.dq) ||
       !set_view("dk", a, dk, a.k_tokens, a.kv_heads, true, &t.dk) ||
-      !set_view("dv", a, dv, a.k_tokens, a.kv_heads, true, &t.dv))
+      !set_view("dv", a, dv, a.k_tokens, a.kv_heads, true, &t.dv) || !check_reach("k", t.k, 1) ||
+      !check_reach("v", t.v, 1) || !check_reach("q", t.q, a.heads / a.kv_heads) ||
+      !check_reach("dout", t.dout, a.heads / a.kv_heads))
     return ELASTO_ERR_INVALID_ARG;
   if (a.q_tokens > 0 && (!lse || !aligned(lse, 4)))
     return fail(ELASTO_ERR_INVALID_ARG, "window attention: lse is NULL or misaligned");

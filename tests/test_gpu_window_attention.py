@@ -384,14 +384,23 @@ def test_captured_training_step():
 
 
 def test_cache_offsets_beyond_four_gigabytes():
-    """A cache whose last tokens lie past 2^32 bytes: [tokens] of a 17 GB stride apart in total."""
-    tk, d = 40, 64
-    stride = (1 << 32) // 2 // 16                         # elements between tokens: 256 MB each
+    """A cache whose last tokens lie past 2^32 bytes, 16 MiB from token to token."""
+    tk, d = 300, 64
+    stride = (1 << 24) // 2
     buf = torch.zeros(stride * (tk - 1) + d, dtype=BF, device="cuda")
     k = torch.as_strided(buf, (1, tk, 1, d), (buf.numel(), stride, d, 1))
-    c = Case(b=1, tq=1, tk=tk, h=2, kv=1, window=100, sinks=0)
+    c = Case(b=1, tq=1, tk=tk, h=2, kv=1, window=1000, sinks=0)
     k.copy_(c.k)
     want, l1 = c.forward()
     o, lse = c.like(c.q), torch.zeros(1, 2, 1, device="cuda")
     ffi.op_window_attention(c.q, k, c.v, o, c.window, lse=lse, workspace=c.workspace(), **c.kw)
     assert torch.equal(o, want) and torch.equal(lse, l1)
+
+
+def test_gradients_of_large_and_odd_groups():
+    """Groups that do not divide a tile of rows, and one larger than it."""
+    for h, kv, dtype in ((7, 1, BF), (33, 1, F32), (40, 1, BF), (71, 1, BF), (130, 2, F32)):
+        c = Case(dtype=dtype, b=1, tq=37, h=h, kv=kv, window=11, sinks=2)
+        o, lse = c.exact_forward()
+        c.check_backward(o, *c.backward(o, lse))
+        c.check_forward(*c.forward())

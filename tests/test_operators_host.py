@@ -142,6 +142,22 @@ def test_window_attention_backward_refuses_bad_gradients(lib, side):
     assert attn_bwd(lib, lse=None) == INVALID
 
 
+def test_window_attention_refuses_tiles_wider_than_four_gigabytes(lib):
+    far = heads(t=1 << 25)                           # bf16: 64 tokens are 4 GiB apart
+    for side in "kv":
+        assert attn(lib, **{side: far}) == INVALID
+        assert attn_bwd(lib, **{side: far}) == INVALID
+    for side in ("q", "dout"):
+        assert attn_bwd(lib, **{side: far}) == INVALID
+        assert attn_bwd(lib, **{side: heads(h=1 << 30)}) == INVALID
+
+
+def test_negative_strides_are_refused(lib):
+    for bad in (heads(b=-64), heads(t=-64), heads(h=-64)):
+        assert attn(lib, q=bad) == INVALID
+        assert qk(lib, k=bad) == INVALID
+
+
 def test_window_attention_refuses_a_short_workspace(lib):
     n = ctypes.c_int64()
     one = dict(q_tokens=1, k_tokens=8192, window=4096)
