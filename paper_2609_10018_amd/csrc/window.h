@@ -47,6 +47,26 @@ __device__ __forceinline__ Keys keys_of(const Mask& m, int pos, int kl) {
   return k;
 }
 
+// What a block of scores starts from where the mask hides some of them: 0, or
+// -infinity, so that the branch over it leaves the scores where they are.  x[i]
+// is for key (or row) `from` + 8 * (i / 4) + i % 4 of a range of len; with
+// sinks, for key j + 8 * (i / 4) + i % 4.
+__device__ __forceinline__ f32x16 hidden(int from, unsigned len) {
+  f32x16 x;
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    x[i] = (unsigned)(from + 8 * (i >> 2) + (i & 3)) < len ? 0.0f : -INFINITY;
+  return x;
+}
+__device__ __forceinline__ f32x16 hidden(int j, const Keys& k, bool sinks) {
+  f32x16 x = hidden(j - k.lo, (unsigned)max(k.hi - k.lo + 1, 0));
+  const int sink = k.hs - j;
+  if (sinks)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = sink >= 8 * (i >> 2) + (i & 3) ? 0.0f : x[i];
+  return x;
+}
+
 __device__ __forceinline__ int clamp_len(const int32_t* lens, int b, int longest) {
   return lens ? min(max(lens[b], 0), longest) : longest;
 }
@@ -57,6 +77,14 @@ __device__ __forceinline__ int clamp_len(const int32_t* lens, int b, int longest
 __device__ __forceinline__ int64_t xcd_order(int64_t id, int64_t n) {
   const int64_t x = id & 7, q = n >> 3, rem = n & 7;
   return x * q + (x < rem ? x : rem) + (id >> 3);
+}
+
+// Keeps an accumulator where it is across a branch: without this the compiler
+// moves whole accumulators (16 instructions each) at the join.  Kernels whose
+// accumulators also live in the other register file do without.
+template <bool ON>
+__device__ __forceinline__ void stay(f32x16& x) {
+  if constexpr (ON) asm volatile("" : "+v"(x));
 }
 
 // The other half-wave's value.
@@ -134,90 +162,132 @@ __device__ __forceinline__ void store4(float* p, float a, float b, float c, floa
   *reinterpret_cast<f32x4*>(p) = f32x4{a, b, c, d};
 }
 
-// A tile of rows of HD features in LDS, in the order of memory but for the
-// 16-byte pieces of a row, which are XORed with the row number: the 32 rows (or
-// 4 x 4 pieces) that one read takes then lie in different banks.
+// A tile of rows of HD features in LDS: blocks of 1 KB, which one load of a wave
+// fills (16 bytes a lane, in the lanes' order), 64 bytes apart.  Row r lies in
+// block r % 4 of each four, (r / 4) % kBlockRows rows down, its 16-byte pieces
+// XORed in their low two bits with (r / 4) % 4.  The LDS is 256 bytes wide:
+// the 16 rows whose same piece one step of a row read takes, and the four rows
+// x 32 bytes of a group of a transposed read, then lie side by side in it.  All
+// of a lane's reads are at constant offsets from four addresses (Reader).
 template <typename T, int HD>
 struct Tile {
   static constexpr int kRow = HD * (int)sizeof(T);  // bytes of a row
   static constexpr int kPieces = kRow / 16;
-  static constexpr int kXor = (kPieces < 16 ? kPieces : 16) - 1;
-  static constexpr int kBlockRows = 64 / kPieces;  // rows of the 1 KB that a wave loads at once
-
-  static __device__ __forceinline__ int at(int r, int piece) {
-    return r * kRow + ((piece ^ (r & kXor)) << 4);
+  static constexpr int kBlockRows = 64 / kPieces;
+  static constexpr int kBlock = 1024 + 64;
+  template <int ROWS>
+  static constexpr int bytes() {
+    return ROWS / kBlockRows * kBlock;
+  }
+  // Where row r, a multiple of 4, starts.
+  static __host__ __device__ constexpr int row_at(int r) {
+    return (r >> 2) / kBlockRows * 4 * kBlock + (r >> 2) % kBlockRows * kRow;
   }
 
-  // Loads of ROWS rows straight to LDS, the blocks of 1 KB shared out over
-  // WAVES waves: kLoads a wave, each lane 16 bytes at a constant offset from
-  // the tile's first row.
+  // Loads of ROWS rows straight to LDS, the blocks shared out over WAVES waves.
   template <int ROWS, int WAVES>
   struct Loads {
     static constexpr int kLoads = ROWS / kBlockRows / WAVES;
-    static_assert(ROWS % (kBlockRows * WAVES) == 0, "every wave loads the same number of blocks");
-    uint32_t off[kLoads];
-
-    // offset(r): where row r lies after the first.
-    template <typename F>
-    __device__ __forceinline__ void set(int wave, int lane, F&& offset) {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const int r = (wave + WAVES * i) * kBlockRows + lane / kPieces;
-        off[i] = offset(r) + (((lane % kPieces) ^ (r & kXor)) << 4);
-      }
+    static_assert(ROWS % (kBlockRows * WAVES) == 0 && (WAVES == 1 || WAVES == 4), "whole blocks a wave");
+    // Row of the tile that a lane loads from at load i, and its piece there.
+    static __device__ __forceinline__ int row(int i, int wave, int lane) {
+      const int blk = wave + WAVES * i;
+      return (blk & 3) + 4 * (lane / kPieces + kBlockRows * (blk >> 2));
     }
-    // From `bytes` bytes at base; what lies past them arrives as zeros.
-    __device__ __forceinline__ void issue(char* tile, int wave, const char* base, int64_t bytes) const {
+    static __device__ __forceinline__ int piece(int i, int wave, int lane) {
+      return (lane % kPieces) ^ ((row(i, wave, lane) >> 2) & 3);
+    }
+    // offset(i): where the lane's row of load i lies after base; what lies past
+    // `bytes` bytes arrives as zeros.
+    template <typename F>
+    static __device__ __forceinline__ void issue(char* tile, int wave, int lane, const char* base,
+                                                 int64_t bytes, F&& offset) {
       const __amdgpu_buffer_rsrc_t src = __builtin_amdgcn_make_buffer_rsrc(
           const_cast<char*>(base), (short)0, (int)(uint32_t)(bytes < 0xffffffffll ? bytes : 0xffffffffll),
           kRsrcWord3);
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(tile + (wave + WAVES * i) * 1024), 16,
-                                                 (int)off[i], 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(tile + (wave + WAVES * i) * kBlock), 16,
+                                                 (int)(offset(i) + piece(i, wave, lane) * 16), 0, 0, 0);
+    }
+    // Rows st bytes apart.
+    static __device__ __forceinline__ void issue(char* tile, int wave, int lane, const char* base,
+                                                 int64_t bytes, uint32_t st) {
+      const uint32_t first = (uint32_t)row(0, wave, lane) * st;
+      issue(tile, wave, lane, base, bytes, [&](int i) {
+        // The rows of two loads are the same number apart in every lane.
+        return first + (uint32_t)(row(i, 0, 0) - row(0, 0, 0)) * st;
+      });
     }
   };
 
-  // Row r, features 16kk + 8h + 0..7.
-  static __device__ __forceinline__ void operand(const char* tile, int r, int kk, int h, Frag<T>& f) {
-    if constexpr (sizeof(T) == 2) {
-      f.v = *reinterpret_cast<const bf16x8*>(tile + at(r, 2 * kk + h));
-    } else {
-      const f32x4 a = *reinterpret_cast<const f32x4*>(tile + at(r, 4 * kk + 2 * h));
-      const f32x4 b = *reinterpret_cast<const f32x4*>(tile + at(r, 4 * kk + 2 * h + 1));
-#pragma unroll
-      for (int e = 0; e < 4; ++e) f.v[e] = a[e], f.v[4 + e] = b[e];
-    }
-  }
-
-  // Feature 32n + l % 32 of rows r0 + 4h + 0..3 and r0 + 8 + 4h + 0..3.
-  // bf16: the transposing LDS read.  In each group of 16 lanes, lane i addresses
-  // columns 4 (i % 4) .. + 3 of row i / 4 and receives column i of the four rows.
-  static __device__ __forceinline__ void transposed(const char* tile, int r0, int n, int lane,
-                                                    Frag<T>& f) {
-    const int h = lane >> 5;
-    if constexpr (sizeof(T) == 2) {
-      typedef short i16x4 __attribute__((ext_vector_type(4)));
-      typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-      const int r = r0 + 4 * h + ((lane & 15) >> 2);
-      const int col = n * 32 + (lane & 16) + 4 * (lane & 3);
-      const int sub = (col & 4) * 2;
-      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (lds_i16x4*)(tile + at(r, col >> 3) + sub)));
-      const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (lds_i16x4*)(tile + at(r + 8, col >> 3) + sub)));
-      const u32x4 w = {lo[0], lo[1], hi[0], hi[1]};
-      f.v = __builtin_bit_cast(bf16x8, w);
-    } else {
-      const int col = n * 32 + (lane & 31);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int r = r0 + 4 * h + (e & 3) + (e & 4) * 2;
-        f.v[e] = *reinterpret_cast<const float*>(tile + at(r, col >> 2) + (col & 3) * 4);
+  // A lane's addresses in a tile.
+  struct Reader {
+    int even, odd;  // of row l % 32: pieces 2kk + h of even and odd kk (fp32: pieces 2h and 2h + 1)
+    int lo, hi;     // transposed: rows 4h .., 8 + 4h ..
+    __device__ __forceinline__ explicit Reader(int lane) {
+      const int r = lane & 31, h = lane >> 5, x = (r >> 2) & 3;
+      const int at = (r & 3) * kBlock + row_at(r & ~3);
+      if constexpr (sizeof(T) == 2) {
+        even = at + ((h ^ x) << 4);
+        odd = at + (((h + 2) ^ x) << 4);
+        const int c = ((lane & 16) >> 3) | ((lane & 2) >> 1), sub = (lane & 1) * 8;
+        const int from = ((lane & 15) >> 2) * kBlock + h * kRow + sub;
+        lo = from + ((c ^ h) << 4);
+        hi = from + row_at(8) + ((c ^ h ^ 2) << 4);
+      } else {
+        even = at + (((2 * h) ^ x) << 4);
+        odd = at + (((2 * h + 1) ^ x) << 4);
+        const int c = (r >> 2) & 3, from = h * kRow + (r >> 4) * 64 + (lane & 3) * 4;
+        lo = from + ((c ^ h) << 4);
+        hi = from + row_at(8) + ((c ^ h ^ 2) << 4);
       }
     }
-  }
+
+    // Row r0 + l % 32 (r0 a multiple of 32), features 16kk + 8h + 0..7.
+    __device__ __forceinline__ void operand(const char* tile, int r0, int kk, Frag<T>& f) const {
+      if constexpr (sizeof(T) == 2) {
+        f.v = *reinterpret_cast<const bf16x8*>(tile + ((kk & 1) ? odd : even) + (kk >> 1) * 64 + row_at(r0));
+      } else {
+        const f32x4 a = *reinterpret_cast<const f32x4*>(tile + even + kk * 64 + row_at(r0));
+        const f32x4 b = *reinterpret_cast<const f32x4*>(tile + odd + kk * 64 + row_at(r0));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f.v[e] = a[e], f.v[4 + e] = b[e];
+      }
+    }
+
+    // Feature 32n + l % 32 of rows r0 + 4h + 0..3 and r0 + 8 + 4h + 0..3 (r0 a
+    // multiple of 16).  bf16: the transposing LDS read; in each group of 16
+    // lanes, lane i addresses columns 4 (i % 4) .. + 3 of row i / 4 and receives
+    // column i of the four rows.
+    __device__ __forceinline__ void transposed(const char* tile, int r0, int n, Frag<T>& f) const {
+      if constexpr (sizeof(T) == 2) {
+        typedef short i16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+        const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_i16x4*)(tile + lo + row_at(r0) + n * 64)));
+        const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_i16x4*)(tile + hi + row_at(r0) + n * 64)));
+        const u32x4 w = {a[0], a[1], b[0], b[1]};
+        f.v = __builtin_bit_cast(bf16x8, w);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          f.v[e] = *reinterpret_cast<const float*>(tile + lo + row_at(r0) + n * 128 + e * kBlock);
+          f.v[4 + e] = *reinterpret_cast<const float*>(tile + hi + row_at(r0) + n * 128 + e * kBlock);
+        }
+      }
+    }
+  };
 };
+
+// Waits for all of this wave's loads: ahead of a loop over tiles, so that inside
+// it nothing waits for the operands loaded before it, and with them for tiles.
+__device__ __forceinline__ void settle() {
+  asm volatile("" ::: "memory");
+  wait_vm_lds<0>();
+  asm volatile("" ::: "memory");
+}
 
 // Waits until at most N of this wave's loads are in flight and its LDS reads
 // are done, then for the workgroup's waves.

@@ -46,9 +46,9 @@ template <typename T, int HD, bool KEYS>
 struct Shape {
   static constexpr int kSub = !KEYS && sizeof(T) == 2 ? 2 : 1;  // 32-key blocks of a tile
   static constexpr int kKeys = 32 * kSub;
-  static constexpr int kTile = kKeys * Tile<T, HD>::kRow;       // bytes of K (and of V)
+  static constexpr int kTile = Tile<T, HD>::template bytes<kKeys>();  // of K (and of V)
   static constexpr int kPrivate = KEYS ? kWaves : 1;            // tiles held at once
-  static constexpr int kBuffers = kPrivate * kTile * 4 <= 128 * 1024 ? 2 : 1;
+  static constexpr int kBuffers = kPrivate * kTile * 4 <= 140 * 1024 ? 2 : 1;
   static constexpr int kOs = HD + 4;  // floats of a row of the join
   static constexpr int kJoin = KEYS ? kWaves * 32 * kOs * 4 + kWaves * 64 * 4 : 0;
   static constexpr int kLds = std::max(kPrivate * kBuffers * 2 * kTile, kJoin);
@@ -68,33 +68,36 @@ struct State {
     l = 0.0f;
   }
 
-  // One tile of SUB * 32 keys from j0 on.
+  __device__ __forceinline__ void hold() {
+#pragma unroll
+    for (int n = 0; n < HD / 32; ++n) stay<sizeof(T) == 2 || HD == 64>(o[n]);
+  }
+
+  // One tile of SUB * 32 keys from j0 on; sinks: some of them may be.
   template <int SUB>
   __device__ __forceinline__ void tile(const char* kt, const char* vt, int j0, const Frag<T>* q,
-                                       float c2, bool inside, const Keys& ks, int lane) {
-    const int r = lane & 31, h = lane >> 5;
+                                       float c2, bool inside, bool sinks, const Keys& ks, int h,
+                                       const typename Tile<T, HD>::Reader& rd) {
     f32x16 s[SUB];
 #pragma unroll
     for (int b = 0; b < SUB; ++b) {
-      zero(s[b]);
-#pragma unroll
-      for (int kk = 0; kk < HD / 16; ++kk) {
-        Frag<T> a;
-        Tile<T, HD>::operand(kt, b * 32 + r, kk, h, a);
-        s[b] = mma(a, q[kk], s[b]);
+      Frag<T> a;
+      rd.operand(kt, b * 32, 0, a);
+      if (inside) {
+        zero(s[b]);
+        s[b] = mma(a, q[0], s[b]);
+      } else {
+        s[b] = mma(a, q[0], hidden(j0 + b * 32 + 4 * h, ks, sinks));
       }
     }
-    if (!inside) {
-      const unsigned len = (unsigned)max(ks.hi - ks.lo + 1, 0);
 #pragma unroll
-      for (int b = 0; b < SUB; ++b)
+    for (int b = 0; b < SUB; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int j = j0 + b * 32 + 8 * (i >> 2) + 4 * h + (i & 3);
-          const bool sees = j <= ks.hs || (unsigned)(j - ks.lo) < len;
-          s[b][i] = sees ? s[b][i] : -INFINITY;
-        }
-    }
+      for (int kk = 1; kk < HD / 16; ++kk) {
+        Frag<T> a;
+        rd.operand(kt, b * 32, kk, a);
+        s[b] = mma(a, q[kk], s[b]);
+      }
     float t = s[0][0];
 #pragma unroll
     for (int b = 0; b < SUB; ++b)
@@ -126,7 +129,7 @@ struct State {
 #pragma unroll
         for (int n = 0; n < HD / 32; ++n) {
           Frag<T> a;
-          Tile<T, HD>::transposed(vt, b * 32 + u * 16, n, lane, a);
+          rd.transposed(vt, b * 32 + u * 16, n, a);
           o[n] = mma(a, pf, o[n]);
         }
       }
@@ -176,16 +179,14 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   // Keys past the last one arrive as zeros: they are masked, and what the
   // memory holds there is not read.
   using Ld = typename Tl::template Loads<S::kKeys, KEYS ? 1 : kWaves>;
-  Ld lk, lv;
   const int lw = KEYS ? 0 : wave;
-  lk.set(lw, lane, [&](int r) { return (uint32_t)r * (uint32_t)p.k.st; });
-  lv.set(lw, lane, [&](int r) { return (uint32_t)r * (uint32_t)p.v.st; });
   auto stage = [&](int n, char* dst) {
     const int j0 = key0(n);
-    lk.issue(dst, lw, kp + j0 * p.k.st, (kl - 1 - j0) * p.k.st + Tl::kRow);
-    lv.issue(dst + S::kTile, lw, vp + j0 * p.v.st, (kl - 1 - j0) * p.v.st + Tl::kRow);
+    Ld::issue(dst, lw, lane, kp + j0 * p.k.st, (kl - 1 - j0) * p.k.st + Tl::kRow, (uint32_t)p.k.st);
+    Ld::issue(dst + S::kTile, lw, lane, vp + j0 * p.v.st, (kl - 1 - j0) * p.v.st + Tl::kRow, (uint32_t)p.v.st);
   };
 
+  const typename Tl::Reader rd(lane);
   State<T, HD> st;
   st.clear();
   Frag<T> q[HD / 16];
@@ -195,35 +196,39 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
 
   auto compute = [&](int n, const char* buf) {
     const int j0 = key0(n), j1 = j0 + S::kKeys - 1;
-    // Nothing of the tile is seen by this wave's rows.
-    if (idle || (j0 > w1.hs && (j1 < w0.lo || j0 > w1.hi))) return;
-    const bool inside = j0 >= w1.lo && j1 <= w0.hi;
-    st.template tile<S::kSub>(buf, buf + S::kTile, j0, q, p.c2, inside, mine, lane);
+    st.hold();
+    // Unless this wave's rows see nothing of the tile.
+    if (!idle && (j0 <= w1.hs || (j1 >= w0.lo && j0 <= w1.hi)))
+      st.template tile<S::kSub>(buf, buf + S::kTile, j0, q, p.c2, j0 >= w1.lo && j1 <= w0.hi,
+                                j0 <= w1.hs, mine, h, rd);
+    st.hold();
   };
   constexpr int kLoads = 2 * Ld::kLoads;
   char* mem = smem + (KEYS ? wave * S::kBuffers * 2 * S::kTile : 0);
   const int step = KEYS ? kWaves : 1;
   int n = zs + (KEYS ? wave : 0);
   if constexpr (S::kBuffers == 2) {
-    if (n < ze) stage(n, mem);
-    int cur = 0;
-    for (; n < ze; n += step) {
-      char* buf = mem + cur * 2 * S::kTile;
+    // cur and next never overlap: without that word the compiler waits for the
+    // next tile's loads before it reads this one.
+    auto body = [&](char* __restrict__ cur, char* __restrict__ next) __attribute__((always_inline)) {
       const bool more = n + step < ze;
-      if (more) stage(n + step, mem + (cur ^ 1) * 2 * S::kTile);
+      if (more) stage(n + step, next);
       asm volatile("" ::: "memory");
       if (more) wait_vm_lds<kLoads>();
       else wait_vm_lds<0>();
       if (!KEYS) __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      compute(n, buf);
+      compute(n, cur);
       // Every read of this tile is done before the next but one overwrites it.
       asm volatile("" ::: "memory");
       wait_lds();
       if (!KEYS) __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      cur ^= 1;
-    }
+    };
+    if (n < ze) stage(n, mem);
+    settle();
+    for (int cur = 0; n < ze; n += step, cur ^= 1)
+      body(mem + cur * 2 * S::kTile, mem + (cur ^ 1) * 2 * S::kTile);
   } else {
     for (; n < ze; n += step) {
       stage(n, mem);

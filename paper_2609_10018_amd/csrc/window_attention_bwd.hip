@@ -40,6 +40,7 @@ struct BwdP {
   Mask mask;
   float scale, c2;
   int64_t blocks;
+  unsigned div_mul, div_shift;  // r / group = umulhi(8 r, div_mul) >> div_shift, r < 2^29
   int row_blocks;          // row kernel
   int key_tiles, parts;    // key kernel: tiles of keys, parts of the first tile's rows
   float2* stat;            // [batch * kv_heads][row]: lse in base 2, D
@@ -50,7 +51,7 @@ template <typename T, int HD>
 struct Shape {
   static constexpr int kSub = sizeof(T) == 2 ? 2 : 1;
   static constexpr int kRows = 32 * kSub;                    // of a staged tile
-  static constexpr int kTile = kRows * Tile<T, HD>::kRow;
+  static constexpr int kTile = Tile<T, HD>::template bytes<kRows>();
   static constexpr int kStat = 64 * 8 * 2;                   // a tile's lse and D, and a spare
   static constexpr int kLdsRow = 2 * 2 * kTile;
   static constexpr int kLdsKey = 2 * (2 * kTile + kStat);
@@ -88,14 +89,12 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   const char* kp = p.k.p + b * p.k.sb + hk * p.k.sh;
   const char* vp = p.v.p + b * p.v.sb + hk * p.v.sh;
   using Ld = typename Tl::template Loads<S::kRows, kWaves>;
-  Ld lk, lv;
-  lk.set(wave, lane, [&](int r) { return (uint32_t)r * (uint32_t)p.k.st; });
-  lv.set(wave, lane, [&](int r) { return (uint32_t)r * (uint32_t)p.v.st; });
   auto stage = [&](int n, char* dst) {
     const int j0 = key0(n);
-    lk.issue(dst, wave, kp + j0 * p.k.st, (kl - 1 - j0) * p.k.st + Tl::kRow);
-    lv.issue(dst + S::kTile, wave, vp + j0 * p.v.st, (kl - 1 - j0) * p.v.st + Tl::kRow);
+    Ld::issue(dst, wave, lane, kp + j0 * p.k.st, (kl - 1 - j0) * p.k.st + Tl::kRow, (uint32_t)p.k.st);
+    Ld::issue(dst + S::kTile, wave, lane, vp + j0 * p.v.st, (kl - 1 - j0) * p.v.st + Tl::kRow, (uint32_t)p.v.st);
   };
+  const typename Tl::Reader rd(lane);
 
   Frag<T> q[HD / 16], d[HD / 16];
   const char* qrow = p.q.p + b * p.q.sb + (int64_t)i * p.q.st + (int64_t)head * p.q.sh;
@@ -115,45 +114,47 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   if (l2 == -INFINITY) l2 = 0.0f;  // a row that sees nothing: every term is masked
   if (h == 0 && row < rows) p.stat[bk * ((int64_t)p.q_tokens * G) + row] = make_float2(l2, D);
 
+  constexpr bool kStay = sizeof(T) == 2 || HD == 64;
   f32x16 dq[HD / 32];
 #pragma unroll
   for (int n = 0; n < HD / 32; ++n) zero(dq[n]);
   constexpr int kLoads = 2 * Ld::kLoads;
-  if (tiles > 0) stage(0, smem);
-  for (int n = 0; n < tiles; ++n) {
-    const char* kt = smem + (n & 1) * 2 * S::kTile;
+  // cur and next never overlap: without that word the compiler waits for the
+  // next tile's loads before it reads this one.
+  auto body = [&](int n, const char* __restrict__ kt, char* __restrict__ next) __attribute__((always_inline)) {
     const char* vt = kt + S::kTile;
     if (n + 1 < tiles) {
-      stage(n + 1, smem + ((n + 1) & 1) * 2 * S::kTile);
+      stage(n + 1, next);
       wait_and_meet<kLoads>();
     } else {
       wait_and_meet<0>();
     }
     const int j0 = key0(n), j1 = j0 + S::kRows - 1;
-    const bool skip = idle || (j0 > w1.hs && (j1 < w0.lo || j0 > w1.hi));
-    if (!skip) {
+#pragma unroll
+    for (int f = 0; f < HD / 32; ++f) stay<kStay>(dq[f]);
+    // Unless this wave's rows see nothing of the tile.
+    if (!idle && (j0 <= w1.hs || (j1 >= w0.lo && j0 <= w1.hi))) {
       const bool inside = j0 >= w1.lo && j1 <= w0.hi;
-      const unsigned len = (unsigned)max(mine.hi - mine.lo + 1, 0);
 #pragma unroll
       for (int s = 0; s < S::kSub; ++s) {
         f32x16 sc, dp;
-        zero(sc);
+        Frag<T> a;
+        rd.operand(kt, s * 32, 0, a);
+        if (inside) {
+          zero(sc);
+          sc = mma(a, q[0], sc);
+        } else {
+          sc = mma(a, q[0], hidden(j0 + s * 32 + 4 * h, mine, j0 <= w1.hs));
+        }
         zero(dp);
 #pragma unroll
         for (int kk = 0; kk < HD / 16; ++kk) {
-          Frag<T> a;
-          Tl::operand(kt, s * 32 + l32, kk, h, a);
-          sc = mma(a, q[kk], sc);
-          Tl::operand(vt, s * 32 + l32, kk, h, a);
-          dp = mma(a, d[kk], dp);
-        }
-        if (!inside) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int j = j0 + s * 32 + 8 * (e >> 2) + 4 * h + (e & 3);
-            const bool sees = j <= mine.hs || (unsigned)(j - mine.lo) < len;
-            sc[e] = sees ? sc[e] : -INFINITY;
+          if (kk > 0) {
+            rd.operand(kt, s * 32, kk, a);
+            sc = mma(a, q[kk], sc);
           }
+          rd.operand(vt, s * 32, kk, a);
+          dp = mma(a, d[kk], dp);
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e)
@@ -165,17 +166,22 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
 #pragma unroll
           for (int f = 0; f < HD / 32; ++f) {
             Frag<T> a;
-            Tl::transposed(kt, s * 32 + u * 16, f, lane, a);
+            rd.transposed(kt, s * 32 + u * 16, f, a);
             dq[f] = mma(a, df, dq[f]);
           }
         }
       }
     }
+#pragma unroll
+    for (int f = 0; f < HD / 32; ++f) stay<kStay>(dq[f]);
     asm volatile("" ::: "memory");
     wait_lds();  // every read of this tile is done before the next but one overwrites it
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-  }
+  };
+  if (tiles > 0) stage(0, smem);
+  settle();
+  for (int n = 0; n < tiles; ++n) body(n, smem + (n & 1) * 2 * S::kTile, smem + ((n + 1) & 1) * 2 * S::kTile);
   if (row >= rows) return;
   T* out = reinterpret_cast<T*>(p.dq.p + b * p.dq.sb + (int64_t)i * p.dq.st + (int64_t)head * p.dq.sh);
 #pragma unroll
@@ -235,12 +241,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   // key's window (a sink's rows go on, those of the keys after it do not).
   const int ilo = w1.lo, ihi = rows_of(p.mask, wfirst, shift, rows, G, false).hi;
   const bool whole = wfirst + 31 < kl;
-  // A tile holds whole queries, so that a row's place in it is the same in every
-  // tile: the most of them whose rows it can take (groups larger than a tile:
-  // rows as they come, placed row by row).
-  const bool whole_queries = G <= S::kRows;
-  const int step = whole_queries ? S::kRows / G * G : S::kRows;
-  const int t_lo = lo / step, t_all = hi >= lo ? hi / step + 1 - t_lo : 0;
+  const int t_lo = lo / S::kRows, t_all = hi >= lo ? hi / S::kRows + 1 - t_lo : 0;
   const bool split = p.parts > 1 && tile == 0;
   const int ts = split ? (int)((int64_t)t_all * part / p.parts) : 0;
   const int te = split ? (int)((int64_t)t_all * (part + 1) / p.parts) : t_all;
@@ -249,30 +250,34 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   const char* dp_ = p.dout.p + b * p.dout.sb + (int64_t)hk * G * p.dout.sh;
   const float2* stat = p.stat + bk * ((int64_t)p.q_tokens * G);
   using Ld = typename Tl::template Loads<S::kRows, kWaves>;
-  Ld lq, ld;
-  // Offsets from the tile's first query i0; rows past the last are that one again.
-  auto set = [&](Ld& l, const View& t, int r0, int i0, int last) {
-    l.set(wave, lane, [&](int r) {
-      const int rr = min(r0 + r, last), i = rr / G;
-      return (uint32_t)(i - i0) * (uint32_t)t.st + (uint32_t)(rr - i * G) * (uint32_t)t.sh;
-    });
-  };
-  set(lq, p.q, 0, 0, step - 1);
-  set(ld, p.dout, 0, 0, step - 1);
-  auto stage = [&](int n, char* dst) {
-    const int r0 = (t_lo + n) * step, i0 = r0 / G;
-    const char* qb = qp + i0 * p.q.st;
-    const char* db = dp_ + i0 * p.dout.st;
-    if (whole_queries && r0 + step <= rows) {
-      lq.issue(dst, wave, qb, 0xffffffffll);
-      ld.issue(dst + S::kTile, wave, db, 0xffffffffll);
+  const typename Tl::Reader rd(lane);
+  // Rows st and sh apart by query and head.  Where the rows of two loads are
+  // whole queries apart, one offset serves all loads of every tile.
+  const bool regular = 4 * Tl::kBlockRows % G == 0;
+  auto load = [&](char* dst, const char* base, const View& t, int r0) {
+    const int i0 = r0 / G;
+    const char* from = base + i0 * t.st;
+    const uint32_t st = (uint32_t)t.st, sh = (uint32_t)t.sh;
+    if (regular && r0 + S::kRows <= rows) {
+      const int r = Ld::row(0, wave, lane), i = r / G;
+      const uint32_t first = (uint32_t)i * st + (uint32_t)(r - i * G) * sh;
+      const uint32_t next = (uint32_t)(4 * Tl::kBlockRows / G) * st;
+      Ld::issue(dst, wave, lane, from, 0xffffffffll, [&](int l) { return first + (uint32_t)l * next; });
     } else {
-      Ld l;
-      set(l, p.q, r0, i0, rows - 1);
-      l.issue(dst, wave, qb, 0xffffffffll);
-      set(l, p.dout, r0, i0, rows - 1);
-      l.issue(dst + S::kTile, wave, db, 0xffffffffll);
+      int ln = lane;  // nothing of this branch is to be kept in registers over the loop
+      asm volatile("" : "+v"(ln));
+      // Rows past the last are that one again.
+      Ld::issue(dst, wave, lane, from, 0xffffffffll, [&](int l) {
+        const unsigned r = (unsigned)min(r0 + Ld::row(l, wave, ln), rows - 1);
+        const unsigned i = __umulhi(r << 3, p.div_mul) >> p.div_shift;
+        return (i - (uint32_t)i0) * st + (r - i * (unsigned)G) * sh;
+      });
     }
+  };
+  auto stage = [&](int n, char* dst) {
+    const int r0 = (t_lo + n) * S::kRows;
+    load(dst, qp, p.q, r0);
+    load(dst + S::kTile, dp_, p.dout, r0);
     // 64 rows' lse and D, 4 bytes a lane: two loads for the 512 bytes; every
     // wave issues one, so that all count the same (waves 2 and 3 to the spare).
     const int r = (wave & 1) * 32 + (lane >> 1);
@@ -289,6 +294,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
     load_operand(krow, kk, h, k[kk]);
     load_operand(vrow, kk, h, v[kk]);
   }
+  constexpr bool kStay = sizeof(T) == 2 || HD == 64;
   f32x16 dk[HD / 32], dv[HD / 32];
 #pragma unroll
   for (int n = 0; n < HD / 32; ++n) {
@@ -297,40 +303,41 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   }
   constexpr int kLoads = 2 * Ld::kLoads + 1;
   constexpr int kBuf = 2 * S::kTile + S::kStat;
-  if (ts < te) stage(ts, smem);
-  for (int n = ts; n < te; ++n) {
-    const char* qt = smem + ((n - ts) & 1) * kBuf;
+  auto body = [&](int n, const char* __restrict__ qt, char* __restrict__ next) __attribute__((always_inline)) {
     const char* dt = qt + S::kTile;
     const f32x4* st = reinterpret_cast<const f32x4*>(qt + 2 * S::kTile);  // two rows each
     if (n + 1 < te) {
-      stage(n + 1, smem + ((n + 1 - ts) & 1) * kBuf);
+      stage(n + 1, next);
       wait_and_meet<kLoads>();
     } else {
       wait_and_meet<0>();
     }
-    const int r0 = (t_lo + n) * step, r1 = r0 + step - 1;
+    const int r0 = (t_lo + n) * S::kRows, r1 = r0 + S::kRows - 1;
+#pragma unroll
+    for (int f = 0; f < HD / 32; ++f) stay<kStay>(dk[f]), stay<kStay>(dv[f]);
     if (!idle && r1 >= wlo && r0 <= whi) {
-      const bool inside = whole && step == S::kRows && r0 >= ilo && r1 <= ihi;
-      const unsigned len = (unsigned)max(min(mine.hi, r1) - mine.lo + 1, 0);
+      const bool inside = whole && r0 >= ilo && r1 <= ihi;
+      const unsigned len = (unsigned)max(mine.hi - mine.lo + 1, 0);
 #pragma unroll 1
       for (int s = 0; s < S::kSub; ++s) {
         f32x16 sc, dp;
-        zero(sc);
+        Frag<T> a;
+        rd.operand(qt, s * 32, 0, a);
+        if (inside) {
+          zero(sc);
+          sc = mma(a, k[0], sc);
+        } else {
+          sc = mma(a, k[0], hidden(r0 + s * 32 + 4 * h - mine.lo, len));
+        }
         zero(dp);
 #pragma unroll
         for (int kk = 0; kk < HD / 16; ++kk) {
-          Frag<T> a;
-          Tl::operand(qt, s * 32 + l32, kk, h, a);
-          sc = mma(a, k[kk], sc);
-          Tl::operand(dt, s * 32 + l32, kk, h, a);
-          dp = mma(a, v[kk], dp);
-        }
-        if (!inside) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int r = r0 + s * 32 + 8 * (e >> 2) + 4 * h + (e & 3);
-            sc[e] = (unsigned)(r - mine.lo) < len ? sc[e] : -INFINITY;
+          if (kk > 0) {
+            rd.operand(qt, s * 32, kk, a);
+            sc = mma(a, k[kk], sc);
           }
+          rd.operand(dt, s * 32, kk, a);
+          dp = mma(a, v[kk], dp);
         }
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
@@ -348,19 +355,24 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
 #pragma unroll
           for (int f = 0; f < HD / 32; ++f) {
             Frag<T> a;
-            Tl::transposed(dt, s * 32 + u * 16, f, lane, a);
+            rd.transposed(dt, s * 32 + u * 16, f, a);
             dv[f] = mma(a, pf, dv[f]);
-            Tl::transposed(qt, s * 32 + u * 16, f, lane, a);
+            rd.transposed(qt, s * 32 + u * 16, f, a);
             dk[f] = mma(a, df, dk[f]);
           }
         }
       }
     }
+#pragma unroll
+    for (int f = 0; f < HD / 32; ++f) stay<kStay>(dk[f]), stay<kStay>(dv[f]);
     asm volatile("" ::: "memory");
     wait_lds();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-  }
+  };
+  if (ts < te) stage(ts, smem);
+  settle();
+  for (int n = ts; n < te; ++n) body(n, smem + ((n - ts) & 1) * kBuf, smem + ((n + 1 - ts) & 1) * kBuf);
   if (split) {
     float* out = p.part + ((bk * p.parts + part) * 2 * kKeys + wave * 32 + l32) * (int64_t)HD;
 #pragma unroll
@@ -459,6 +471,10 @@ hipError_t launch_window_bwd(const elasto_window_t& a, const WindowTensors& t, v
   p.heads = a.heads;
   p.kv_heads = a.kv_heads;
   p.group = a.heads / a.kv_heads;
+  // With 2^(s - 1) < group <= 2^s and m = ceil(2^(29 + s) / group), r m / 2^(29 + s)
+  // exceeds r / group by less than r / 2^29 / group, under 1 / group.
+  while ((1u << p.div_shift) < (unsigned)p.group) ++p.div_shift;
+  p.div_mul = (unsigned)((((uint64_t)1 << (29 + p.div_shift)) + p.group - 1) / p.group);
   p.mask = Mask{a.causal, a.window, a.sinks};
   p.scale = a.scale;
   p.c2 = a.scale * kLog2e;
