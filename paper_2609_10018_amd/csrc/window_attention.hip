@@ -59,7 +59,8 @@ struct Shape {
 template <typename T, int HD>
 struct State {
   f32x16 o[HD / 32];
-  float m, l;  // running maximum (of raw scores), this half-wave's part of the sum
+  static constexpr float kRise = 8.0f;
+  float m, l;  // reference of the exponentials (a raw score), this half-wave's part of the sum
 
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -103,16 +104,19 @@ struct State {
     for (int b = 0; b < SUB; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i) t = fmaxf(t, s[b][i]);
-    t = fmaxf(m, half_max(t));
-    // Rows whose maximum rises bring their sums to the new one.
-    if (__any(t > m)) {
-      const float f = t > m ? __builtin_amdgcn_exp2f((m - t) * c2) : 1.0f;
+    t = half_max(t);
+    // The reference of the exponentials follows the maximum only where that has
+    // risen by more than 2^kRise since: terms of up to 2^kRise are as exact, and
+    // a wave of 32 rows would rescale its sums in most tiles otherwise.
+    if (__any((t - m) * c2 > kRise)) {
+      const float to = fmaxf(m, t);
+      const float f = to > m ? __builtin_amdgcn_exp2f((m - to) * c2) : 1.0f;
       l *= f;
 #pragma unroll
       for (int n = 0; n < HD / 32; ++n)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[n][i] *= f;
-      m = t;
+      m = to;
     }
     const float off = m == -INFINITY ? 0.0f : -m * c2;  // nothing seen so far: all terms are 0
 #pragma unroll

@@ -15,9 +15,11 @@
 // P and dS are rounded to bf16 (bf16 path) as operands of the products that
 // sum them; all sums are fp32.
 //
-// A key among the sinks is seen by every later row, so the first tile of keys
-// has far more rows than the others: its rows are cut into parts of about an
-// ordinary tile's, each a workgroup, whose fp32 sums a third kernel adds up.
+// A key among the sinks is seen by every later row.  The key kernel takes the
+// rows that see the first tile's keys through their windows, as for any tile;
+// the rows behind them, which see the sinks alone, are a kernel of their own,
+// where a workgroup's waves take different rows for the same 32 keys, and whose
+// parts are added up in order.
 #include <algorithm>
 
 #include "layout.h"
@@ -42,9 +44,10 @@ struct BwdP {
   int64_t blocks;
   unsigned div_mul, div_shift;  // r / group = umulhi(8 r, div_mul) >> div_shift, r < 2^29
   int row_blocks;          // row kernel
-  int key_tiles, parts;    // key kernel: tiles of keys, parts of the first tile's rows
+  int key_tiles;           // key kernel
+  int parts, sink_groups;  // sink kernel (parts 0: none): parts of the rows, 32s of sinks
   float2* stat;            // [batch * kv_heads][row]: lse in base 2, D
-  float* part;             // parts > 1: [batch * kv_heads][part][2][kKeys][HD]
+  float* part;             // [batch * kv_heads][key kernel, parts][dk, dv][kMaxSinks][HD]
 };
 
 template <typename T, int HD>
@@ -55,6 +58,16 @@ struct Shape {
   static constexpr int kStat = 64 * 8 * 2;                   // a tile's lse and D, and a spare
   static constexpr int kLdsRow = 2 * 2 * kTile;
   static constexpr int kLdsKey = 2 * (2 * kTile + kStat);
+};
+
+template <typename T, int HD>
+struct SinkShape {
+  static constexpr int kTile = Tile<T, HD>::template bytes<32>();
+  static constexpr int kBuf = 2 * kTile + 256;
+  static constexpr int kBuffers = kWaves * 2 * kBuf <= 144 * 1024 ? 2 : 1;
+  static constexpr int kOs = HD + 4;
+  static constexpr int kLds = std::max(kWaves * kBuffers * kBuf, kWaves * 32 * kOs * 4);
+  static_assert(kLds <= 160 * 1024, "LDS");
 };
 
 template <typename T, int HD>
@@ -206,6 +219,128 @@ __device__ __forceinline__ Rows rows_of(const Mask& m, int j, int shift, int row
   return r;
 }
 
+// 32 keys' side of the products: a lane's key is column l % 32.
+template <typename T, int HD>
+struct KeySide {
+  static constexpr bool kStay = sizeof(T) == 2 || HD == 64;
+  Frag<T> k[HD / 16], v[HD / 16];
+  f32x16 dk[HD / 32], dv[HD / 32];
+
+  __device__ __forceinline__ void load(const char* krow, const char* vrow, int h) {
+#pragma unroll
+    for (int kk = 0; kk < HD / 16; ++kk) {
+      load_operand(krow, kk, h, k[kk]);
+      load_operand(vrow, kk, h, v[kk]);
+    }
+#pragma unroll
+    for (int n = 0; n < HD / 32; ++n) {
+      zero(dk[n]);
+      zero(dv[n]);
+    }
+  }
+  __device__ __forceinline__ void hold() {
+#pragma unroll
+    for (int n = 0; n < HD / 32; ++n) stay<kStay>(dk[n]), stay<kStay>(dv[n]);
+  }
+
+  // SUB * 32 rows of q and dout, and their lse and D (st: two rows each); from
+  // and len: which of them see the lane's key.
+  template <int SUB>
+  __device__ __forceinline__ void rows(const char* qt, const char* dt, const f32x4* st, bool inside,
+                                       int from, unsigned len, float c2, int h,
+                                       const typename Tile<T, HD>::Reader& rd) {
+#pragma unroll 1
+    for (int s = 0; s < SUB; ++s) {
+      f32x16 sc, dp;
+      Frag<T> a;
+      rd.operand(qt, s * 32, 0, a);
+      if (inside) {
+        zero(sc);
+        sc = mma(a, k[0], sc);
+      } else {
+        sc = mma(a, k[0], hidden(from + s * 32 + 4 * h, len));
+      }
+      zero(dp);
+#pragma unroll
+      for (int kk = 0; kk < HD / 16; ++kk) {
+        if (kk > 0) {
+          rd.operand(qt, s * 32, kk, a);
+          sc = mma(a, k[kk], sc);
+        }
+        rd.operand(dt, s * 32, kk, a);
+        dp = mma(a, v[kk], dp);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        const f32x4 x = st[(s * 32 + 8 * (e >> 2) + 4 * h + (e & 3)) >> 1];
+        sc[e] = __builtin_amdgcn_exp2f(fmaf(sc[e], c2, -x[0]));
+        sc[e + 1] = __builtin_amdgcn_exp2f(fmaf(sc[e + 1], c2, -x[2]));
+        dp[e] = sc[e] * (dp[e] - x[1]);
+        dp[e + 1] = sc[e + 1] * (dp[e + 1] - x[3]);
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        Frag<T> pf, df;
+        as_operand(sc, u, pf);
+        as_operand(dp, u, df);
+#pragma unroll
+        for (int f = 0; f < HD / 32; ++f) {
+          rd.transposed(dt, s * 32 + u * 16, f, a);
+          dv[f] = mma(a, pf, dv[f]);
+          rd.transposed(qt, s * 32 + u * 16, f, a);
+          dk[f] = mma(a, df, dk[f]);
+        }
+      }
+    }
+  }
+
+  // fp32 rows of the parts, HD floats a key and then kMaxSinks keys on.
+  __device__ __forceinline__ void store_part(float* ok, float* ov, int h) const {
+#pragma unroll
+    for (int n = 0; n < HD / 32; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int c = n * 32 + 8 * e + 4 * h;
+        store4(ok + c, dk[n][4 * e], dk[n][4 * e + 1], dk[n][4 * e + 2], dk[n][4 * e + 3]);
+        store4(ov + c, dv[n][4 * e], dv[n][4 * e + 1], dv[n][4 * e + 2], dv[n][4 * e + 3]);
+      }
+  }
+};
+
+// Loads of packed rows [r0, r0 + ROWS) of q or dout (base: its first query of
+// the group) to LDS; rows past the last are that one again.
+template <typename T, int HD, int ROWS, int WAVES>
+__device__ __forceinline__ void stage_rows(const BwdP& p, char* dst, const char* base, const View& t,
+                                           int r0, int rows, int wave, int lane) {
+  using Tl = Tile<T, HD>;
+  using Ld = typename Tl::template Loads<ROWS, WAVES>;
+  const int G = p.group, i0 = r0 / G;
+  const char* from = base + i0 * t.st;
+  const uint32_t st = (uint32_t)t.st, sh = (uint32_t)t.sh;
+  // Where the rows of two loads are whole queries apart, one offset serves all
+  // loads of every tile.
+  if (WAVES == 4 && 4 * Tl::kBlockRows % G == 0 && r0 + ROWS <= rows) {
+    const int r = Ld::row(0, wave, lane), i = r / G;
+    const uint32_t first = (uint32_t)i * st + (uint32_t)(r - i * G) * sh;
+    const uint32_t next = (uint32_t)(4 * Tl::kBlockRows / G) * st;
+    Ld::issue(dst, wave, lane, from, 0xffffffffll, [&](int l) { return first + (uint32_t)l * next; });
+  } else {
+    int ln = lane;  // nothing of this branch is to be kept in registers over the loop
+    asm volatile("" : "+v"(ln));
+    Ld::issue(dst, wave, lane, from, 0xffffffffll, [&](int l) {
+      const unsigned r = (unsigned)min(r0 + Ld::row(l, wave, ln), rows - 1);
+      const unsigned i = __umulhi(r << 3, p.div_mul) >> p.div_shift;
+      return (i - (uint32_t)i0) * st + (r - i * (unsigned)G) * sh;
+    });
+  }
+}
+
+// 32 rows' lse and D, 4 bytes a lane.
+__device__ __forceinline__ void stage_stat(char* dst, const float2* stat, int r0, int rows, int lane) {
+  const char* src = reinterpret_cast<const char*>(stat + min(r0 + (lane >> 1), rows - 1)) + (lane & 1) * 4;
+  __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)src, (lds_void*)dst, 4, 0, 0);
+}
+
 template <typename T, int HD>
 __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) void window_dkv_kernel(BwdP p) {
   using S = Shape<T, HD>;
@@ -214,178 +349,78 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t id = xcd_order(blockIdx.x, p.blocks);
-  const int per = p.key_tiles + p.parts - 1;
-  const int64_t bk = id / per;
-  const int item = (int)(id - bk * per);
-  const int tile = max(item - (p.parts - 1), 0), part = min(item, p.parts - 1);
+  const int64_t bk = id / p.key_tiles;
+  const int first = (int)(id - bk * p.key_tiles) * kKeys;
   const int b = (int)(bk / p.kv_heads), hk = (int)(bk - (int64_t)b * p.kv_heads);
   const int ql = clamp_len(p.q_lens, b, p.q_tokens), kl = clamp_len(p.k_lens, b, p.k_tokens);
   const int G = p.group, rows = ql * G, shift = kl - ql;
-  const int first = tile * kKeys;
   if (first >= kl) return;
   const int wfirst = first + 32 * wave, key = wfirst + l32, kc = min(key, kl - 1);
-  // Rows of the workgroup, of this wave, of this lane's key.
+  // Rows that see this lane's key, some key and every key of the wave, some key
+  // of the workgroup.  The earliest row is that of the first key; the last that
+  // of the last key or, with a sink among the keys, the last of all: those
+  // behind every key's window are left to the sink kernel where there is one.
   const int wlast = min(wfirst + 31, kl - 1);
+  const Rows last = rows_of(p.mask, min(first + kKeys, kl) - 1, shift, rows, G, false);
   Rows mine = rows_of(p.mask, kc, shift, rows, G, true);
   if (key >= kl) mine = Rows{0, -1};
-  // The earliest row is that of the first key, the last that of the last key
-  // or, with a sink among the keys, of the first.
   const Rows w0 = rows_of(p.mask, wfirst, shift, rows, G, true);
   const Rows w1 = rows_of(p.mask, wlast, shift, rows, G, true);
   const Rows n0 = rows_of(p.mask, first, shift, rows, G, true);
-  const Rows n1 = rows_of(p.mask, min(first + kKeys, kl) - 1, shift, rows, G, true);
-  int lo = n0.lo, hi = max(n0.hi, n1.hi);
+  const int lo = n0.lo, hi = p.parts ? last.hi : max(n0.hi, last.hi);
   const bool idle = wfirst >= kl;
   const int wlo = w0.lo, whi = max(w0.hi, w1.hi);
-  // Rows that every key of the wave is seen by: up to the last of the first
-  // key's window (a sink's rows go on, those of the keys after it do not).
   const int ilo = w1.lo, ihi = rows_of(p.mask, wfirst, shift, rows, G, false).hi;
   const bool whole = wfirst + 31 < kl;
-  const int t_lo = lo / S::kRows, t_all = hi >= lo ? hi / S::kRows + 1 - t_lo : 0;
-  const bool split = p.parts > 1 && tile == 0;
-  const int ts = split ? (int)((int64_t)t_all * part / p.parts) : 0;
-  const int te = split ? (int)((int64_t)t_all * (part + 1) / p.parts) : t_all;
+  mine.hi = min(mine.hi, hi);
+  const unsigned len = (unsigned)max(mine.hi - mine.lo + 1, 0);
+  const int t_lo = lo / S::kRows, tiles = hi >= lo ? hi / S::kRows + 1 - t_lo : 0;
 
   const char* qp = p.q.p + b * p.q.sb + (int64_t)hk * G * p.q.sh;
-  const char* dp_ = p.dout.p + b * p.dout.sb + (int64_t)hk * G * p.dout.sh;
+  const char* dp = p.dout.p + b * p.dout.sb + (int64_t)hk * G * p.dout.sh;
   const float2* stat = p.stat + bk * ((int64_t)p.q_tokens * G);
-  using Ld = typename Tl::template Loads<S::kRows, kWaves>;
-  const typename Tl::Reader rd(lane);
-  // Rows st and sh apart by query and head.  Where the rows of two loads are
-  // whole queries apart, one offset serves all loads of every tile.
-  const bool regular = 4 * Tl::kBlockRows % G == 0;
-  auto load = [&](char* dst, const char* base, const View& t, int r0) {
-    const int i0 = r0 / G;
-    const char* from = base + i0 * t.st;
-    const uint32_t st = (uint32_t)t.st, sh = (uint32_t)t.sh;
-    if (regular && r0 + S::kRows <= rows) {
-      const int r = Ld::row(0, wave, lane), i = r / G;
-      const uint32_t first = (uint32_t)i * st + (uint32_t)(r - i * G) * sh;
-      const uint32_t next = (uint32_t)(4 * Tl::kBlockRows / G) * st;
-      Ld::issue(dst, wave, lane, from, 0xffffffffll, [&](int l) { return first + (uint32_t)l * next; });
-    } else {
-      int ln = lane;  // nothing of this branch is to be kept in registers over the loop
-      asm volatile("" : "+v"(ln));
-      // Rows past the last are that one again.
-      Ld::issue(dst, wave, lane, from, 0xffffffffll, [&](int l) {
-        const unsigned r = (unsigned)min(r0 + Ld::row(l, wave, ln), rows - 1);
-        const unsigned i = __umulhi(r << 3, p.div_mul) >> p.div_shift;
-        return (i - (uint32_t)i0) * st + (r - i * (unsigned)G) * sh;
-      });
-    }
-  };
+  constexpr int kBuf = 2 * S::kTile + S::kStat;
   auto stage = [&](int n, char* dst) {
     const int r0 = (t_lo + n) * S::kRows;
-    load(dst, qp, p.q, r0);
-    load(dst + S::kTile, dp_, p.dout, r0);
-    // 64 rows' lse and D, 4 bytes a lane: two loads for the 512 bytes; every
-    // wave issues one, so that all count the same (waves 2 and 3 to the spare).
-    const int r = (wave & 1) * 32 + (lane >> 1);
-    const char* src = reinterpret_cast<const char*>(stat + min(r0 + r, rows - 1)) + (lane & 1) * 4;
-    __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)src,
-                                     (lds_void*)(dst + 2 * S::kTile + wave * 256), 4, 0, 0);
+    stage_rows<T, HD, S::kRows, kWaves>(p, dst, qp, p.q, r0, rows, wave, lane);
+    stage_rows<T, HD, S::kRows, kWaves>(p, dst + S::kTile, dp, p.dout, r0, rows, wave, lane);
+    // Every wave issues one, so that all count the same (waves 2 and 3 to the spare).
+    stage_stat(dst + 2 * S::kTile + wave * 256, stat, r0 + (wave & 1) * 32, rows, lane);
   };
+  constexpr int kLoads = 2 * Tl::template Loads<S::kRows, kWaves>::kLoads + 1;
 
-  Frag<T> k[HD / 16], v[HD / 16];
-  const char* krow = p.k.p + b * p.k.sb + (int64_t)kc * p.k.st + hk * p.k.sh;
-  const char* vrow = p.v.p + b * p.v.sb + (int64_t)kc * p.v.st + hk * p.v.sh;
-#pragma unroll
-  for (int kk = 0; kk < HD / 16; ++kk) {
-    load_operand(krow, kk, h, k[kk]);
-    load_operand(vrow, kk, h, v[kk]);
-  }
-  constexpr bool kStay = sizeof(T) == 2 || HD == 64;
-  f32x16 dk[HD / 32], dv[HD / 32];
-#pragma unroll
-  for (int n = 0; n < HD / 32; ++n) {
-    zero(dk[n]);
-    zero(dv[n]);
-  }
-  constexpr int kLoads = 2 * Ld::kLoads + 1;
-  constexpr int kBuf = 2 * S::kTile + S::kStat;
-  auto body = [&](int n, const char* __restrict__ qt, char* __restrict__ next) __attribute__((always_inline)) {
-    const char* dt = qt + S::kTile;
-    const f32x4* st = reinterpret_cast<const f32x4*>(qt + 2 * S::kTile);  // two rows each
-    if (n + 1 < te) {
+  const typename Tl::Reader rd(lane);
+  KeySide<T, HD> ks;
+  ks.load(p.k.p + b * p.k.sb + (int64_t)kc * p.k.st + hk * p.k.sh,
+          p.v.p + b * p.v.sb + (int64_t)kc * p.v.st + hk * p.v.sh, h);
+  // cur and next never overlap (as in window_dq_kernel).
+  auto body = [&](int n, const char* __restrict__ cur, char* __restrict__ next) __attribute__((always_inline)) {
+    if (n + 1 < tiles) {
       stage(n + 1, next);
       wait_and_meet<kLoads>();
     } else {
       wait_and_meet<0>();
     }
     const int r0 = (t_lo + n) * S::kRows, r1 = r0 + S::kRows - 1;
-#pragma unroll
-    for (int f = 0; f < HD / 32; ++f) stay<kStay>(dk[f]), stay<kStay>(dv[f]);
-    if (!idle && r1 >= wlo && r0 <= whi) {
-      const bool inside = whole && r0 >= ilo && r1 <= ihi;
-      const unsigned len = (unsigned)max(mine.hi - mine.lo + 1, 0);
-#pragma unroll 1
-      for (int s = 0; s < S::kSub; ++s) {
-        f32x16 sc, dp;
-        Frag<T> a;
-        rd.operand(qt, s * 32, 0, a);
-        if (inside) {
-          zero(sc);
-          sc = mma(a, k[0], sc);
-        } else {
-          sc = mma(a, k[0], hidden(r0 + s * 32 + 4 * h - mine.lo, len));
-        }
-        zero(dp);
-#pragma unroll
-        for (int kk = 0; kk < HD / 16; ++kk) {
-          if (kk > 0) {
-            rd.operand(qt, s * 32, kk, a);
-            sc = mma(a, k[kk], sc);
-          }
-          rd.operand(dt, s * 32, kk, a);
-          dp = mma(a, v[kk], dp);
-        }
-#pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-          const f32x4 x = st[(s * 32 + 8 * (e >> 2) + 4 * h + (e & 3)) >> 1];
-          sc[e] = __builtin_amdgcn_exp2f(fmaf(sc[e], p.c2, -x[0]));
-          sc[e + 1] = __builtin_amdgcn_exp2f(fmaf(sc[e + 1], p.c2, -x[2]));
-          dp[e] = sc[e] * (dp[e] - x[1]);
-          dp[e + 1] = sc[e + 1] * (dp[e + 1] - x[3]);
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          Frag<T> pf, df;
-          as_operand(sc, u, pf);
-          as_operand(dp, u, df);
-#pragma unroll
-          for (int f = 0; f < HD / 32; ++f) {
-            Frag<T> a;
-            rd.transposed(dt, s * 32 + u * 16, f, a);
-            dv[f] = mma(a, pf, dv[f]);
-            rd.transposed(qt, s * 32 + u * 16, f, a);
-            dk[f] = mma(a, df, dk[f]);
-          }
-        }
-      }
-    }
-#pragma unroll
-    for (int f = 0; f < HD / 32; ++f) stay<kStay>(dk[f]), stay<kStay>(dv[f]);
+    ks.hold();
+    if (!idle && r1 >= wlo && r0 <= whi)
+      ks.template rows<S::kSub>(cur, cur + S::kTile, reinterpret_cast<const f32x4*>(cur + 2 * S::kTile),
+                                whole && r0 >= ilo && r1 <= ihi, r0 - mine.lo, len, p.c2, h, rd);
+    ks.hold();
     asm volatile("" ::: "memory");
     wait_lds();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  if (ts < te) stage(ts, smem);
+  if (tiles > 0) stage(0, smem);
   settle();
-  for (int n = ts; n < te; ++n) body(n, smem + ((n - ts) & 1) * kBuf, smem + ((n + 1 - ts) & 1) * kBuf);
-  if (split) {
-    float* out = p.part + ((bk * p.parts + part) * 2 * kKeys + wave * 32 + l32) * (int64_t)HD;
-#pragma unroll
-    for (int n = 0; n < HD / 32; ++n)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int c = n * 32 + 8 * e + 4 * h;
-        store4(out + c, dk[n][4 * e], dk[n][4 * e + 1], dk[n][4 * e + 2], dk[n][4 * e + 3]);
-        store4(out + kKeys * HD + c, dv[n][4 * e], dv[n][4 * e + 1], dv[n][4 * e + 2], dv[n][4 * e + 3]);
-      }
+  for (int n = 0; n < tiles; ++n) body(n, smem + (n & 1) * kBuf, smem + ((n + 1) & 1) * kBuf);
+  if (key >= kl) return;
+  if (p.parts && key < p.mask.sinks) {
+    float* out = p.part + ((bk * (p.parts + 1)) * 2 * kMaxSinks + key) * (int64_t)HD;
+    ks.store_part(out, out + kMaxSinks * HD, h);
     return;
   }
-  if (key >= kl) return;
   T* ok = reinterpret_cast<T*>(p.dk.p + b * p.dk.sb + (int64_t)key * p.dk.st + hk * p.dk.sh);
   T* ov = reinterpret_cast<T*>(p.dv.p + b * p.dv.sb + (int64_t)key * p.dv.st + hk * p.dv.sh);
 #pragma unroll
@@ -393,27 +428,126 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int c = n * 32 + 8 * e + 4 * h;
-      store4(ok + c, dk[n][4 * e] * p.scale, dk[n][4 * e + 1] * p.scale, dk[n][4 * e + 2] * p.scale,
-             dk[n][4 * e + 3] * p.scale);
-      store4(ov + c, dv[n][4 * e], dv[n][4 * e + 1], dv[n][4 * e + 2], dv[n][4 * e + 3]);
+      store4(ok + c, ks.dk[n][4 * e] * p.scale, ks.dk[n][4 * e + 1] * p.scale,
+             ks.dk[n][4 * e + 2] * p.scale, ks.dk[n][4 * e + 3] * p.scale);
+      store4(ov + c, ks.dv[n][4 * e], ks.dv[n][4 * e + 1], ks.dv[n][4 * e + 2], ks.dv[n][4 * e + 3]);
     }
 }
 
-// The first tile's keys: the parts' sums added up in order, four features a
-// thread, one workgroup a 1024 / HD keys.
+// The sinks' rows behind every window of the first tile of keys: one part of
+// them and 32 of the sinks a workgroup, the rows shared out over its waves (no
+// barrier until they join).
 template <typename T, int HD>
-__global__ __launch_bounds__(kThreads) void window_sink_kernel(BwdP p) {
+__global__ __launch_bounds__(kThreads, 1) void window_sink_kernel(BwdP p) {
+  using S = SinkShape<T, HD>;
+  using Tl = Tile<T, HD>;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t id = xcd_order(blockIdx.x, p.blocks);
+  const int part = (int)(id % p.parts);
+  const int64_t rest = id / p.parts;
+  const int group = (int)(rest % p.sink_groups);
+  const int64_t bk = rest / p.sink_groups;
+  const int b = (int)(bk / p.kv_heads), hk = (int)(bk - (int64_t)b * p.kv_heads);
+  const int ql = clamp_len(p.q_lens, b, p.q_tokens), kl = clamp_len(p.k_lens, b, p.k_tokens);
+  const int G = p.group, rows = ql * G, shift = kl - ql;
+  const int wfirst = 32 * group, key = wfirst + l32, sinks = min(p.mask.sinks, kl);
+  if (wfirst >= sinks) return;
+  const int kc = min(key, kl - 1);
+  // All rows from `from` on see all of the sinks: they stand behind the windows
+  // of keys no earlier.
+  const int from = rows_of(p.mask, min(kKeys, kl) - 1, shift, rows, G, false).hi + 1;
+  const int far = rows - from, all = (far + 31) / 32;
+  const int ts = (int)((int64_t)all * part / p.parts), te = (int)((int64_t)all * (part + 1) / p.parts);
+  const char* qp = p.q.p + b * p.q.sb + (int64_t)hk * G * p.q.sh;
+  const char* dp = p.dout.p + b * p.dout.sb + (int64_t)hk * G * p.dout.sh;
+  const float2* stat = p.stat + bk * ((int64_t)p.q_tokens * G);
+  char* mem = smem + wave * S::kBuffers * S::kBuf;
+  auto stage = [&](int n, char* dst) {
+    const int r0 = from + n * 32;
+    stage_rows<T, HD, 32, 1>(p, dst, qp, p.q, r0, rows, 0, lane);
+    stage_rows<T, HD, 32, 1>(p, dst + S::kTile, dp, p.dout, r0, rows, 0, lane);
+    stage_stat(dst + 2 * S::kTile, stat, r0, rows, lane);
+  };
+  constexpr int kLoads = 2 * Tl::template Loads<32, 1>::kLoads + 1;
+  const typename Tl::Reader rd(lane);
+  KeySide<T, HD> ks;
+  ks.load(p.k.p + b * p.k.sb + (int64_t)kc * p.k.st + hk * p.k.sh,
+          p.v.p + b * p.v.sb + (int64_t)kc * p.v.st + hk * p.v.sh, h);
+  const bool seen = key < sinks;
+  auto compute = [&](int n, const char* cur) {
+    ks.hold();
+    const int left = far - n * 32;
+    ks.template rows<1>(cur, cur + S::kTile, reinterpret_cast<const f32x4*>(cur + 2 * S::kTile),
+                        left >= 32 && wfirst + 32 <= sinks, 0, seen ? (unsigned)min(left, 32) : 0u, p.c2,
+                        h, rd);
+    ks.hold();
+    asm volatile("" ::: "memory");
+    wait_lds();
+    asm volatile("" ::: "memory");
+  };
+  int n = ts + wave;
+  if constexpr (S::kBuffers == 2) {
+    auto body = [&](const char* __restrict__ cur, char* __restrict__ next) __attribute__((always_inline)) {
+      const bool more = n + kWaves < te;
+      if (more) stage(n + kWaves, next);
+      asm volatile("" ::: "memory");
+      if (more) wait_vm_lds<kLoads>();
+      else wait_vm_lds<0>();
+      asm volatile("" ::: "memory");
+      compute(n, cur);
+    };
+    if (n < te) stage(n, mem);
+    settle();
+    for (int cur = 0; n < te; n += kWaves, cur ^= 1) body(mem + cur * S::kBuf, mem + (cur ^ 1) * S::kBuf);
+  } else {
+    for (; n < te; n += kWaves) {
+      stage(n, mem);
+      settle();
+      compute(n, mem);
+    }
+  }
+  // Join the waves, dk and then dv.
+  float* jo = reinterpret_cast<float*>(smem);
+  float* out = p.part + ((bk * (p.parts + 1) + 1 + part) * 2 * kMaxSinks + wfirst) * (int64_t)HD;
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    const f32x16* x = side ? ks.dv : ks.dk;
+    __syncthreads();
+    float* jr = jo + (wave * 32 + l32) * S::kOs;
+#pragma unroll
+    for (int n = 0; n < HD / 32; ++n)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        store4(jr + n * 32 + 8 * e + 4 * h, x[n][4 * e], x[n][4 * e + 1], x[n][4 * e + 2], x[n][4 * e + 3]);
+    __syncthreads();
+    for (int u = threadIdx.x; u < 32 * (HD / 4); u += kThreads) {
+      const int r = u / (HD / 4), c = (u - r * (HD / 4)) * 4;
+      f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) v += *reinterpret_cast<const f32x4*>(jo + (w * 32 + r) * S::kOs + c);
+      *reinterpret_cast<f32x4*>(out + (side * kMaxSinks + r) * (int64_t)HD + c) = v;
+    }
+  }
+}
+
+// The sinks' gradients: the parts' sums added up in order, four features a
+// thread.
+template <typename T, int HD>
+__global__ __launch_bounds__(kThreads) void window_sink_join_kernel(BwdP p) {
   constexpr int kPer = HD / 4, kBlockKeys = kThreads / kPer;
-  const int64_t bk = blockIdx.x / (kKeys / kBlockKeys);
-  const int key = (int)(blockIdx.x % (kKeys / kBlockKeys)) * kBlockKeys + threadIdx.x / kPer;
+  const int64_t bk = blockIdx.x / (kMaxSinks / kBlockKeys);
+  const int key = (int)(blockIdx.x % (kMaxSinks / kBlockKeys)) * kBlockKeys + threadIdx.x / kPer;
   const int c = (threadIdx.x % kPer) * 4;
   const int b = (int)(bk / p.kv_heads), hk = (int)(bk - (int64_t)b * p.kv_heads);
-  if (key >= clamp_len(p.k_lens, b, p.k_tokens)) return;
+  if (key >= min(p.mask.sinks, clamp_len(p.k_lens, b, p.k_tokens))) return;
   f32x4 dk = {0.f, 0.f, 0.f, 0.f}, dv = dk;
-  for (int i = 0; i < p.parts; ++i) {
-    const float* in = p.part + ((bk * p.parts + i) * 2 * kKeys + key) * (int64_t)HD + c;
+  const float* in = p.part + ((bk * (p.parts + 1)) * 2 * kMaxSinks + key) * (int64_t)HD + c;
+#pragma unroll 4
+  for (int i = 0; i <= p.parts; ++i, in += 2 * kMaxSinks * HD) {
     dk += *reinterpret_cast<const f32x4*>(in);
-    dv += *reinterpret_cast<const f32x4*>(in + kKeys * HD);
+    dv += *reinterpret_cast<const f32x4*>(in + kMaxSinks * HD);
   }
   T* ok = reinterpret_cast<T*>(p.dk.p + b * p.dk.sb + (int64_t)key * p.dk.st + hk * p.dk.sh);
   T* ov = reinterpret_cast<T*>(p.dv.p + b * p.dv.sb + (int64_t)key * p.dv.st + hk * p.dv.sh);
@@ -421,13 +555,15 @@ __global__ __launch_bounds__(kThreads) void window_sink_kernel(BwdP p) {
   store4(ov + c, dv[0], dv[1], dv[2], dv[3]);
 }
 
-// Parts of the first tile's rows: an ordinary tile has the rows of its own
-// positions and its window's, the first tile all that follow.
+// Parts of the rows that only the sinks are seen by, for launches in which they
+// are more than a tile of keys has otherwise (0: the first tile's workgroup
+// takes them along): about 256 workgroups, 512 rows or more each.
 int parts_of(const elasto_window_t& a) {
   const int64_t G = a.heads / a.kv_heads, rows = (int64_t)a.q_tokens * G;
-  const int64_t near = (kKeys + (a.causal ? (int64_t)a.window : 2 * (int64_t)a.window)) * G;
-  if (a.sinks == 0) return 1;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(64, rows / std::max<int64_t>(near, 1024)));
+  const int64_t near = (kKeys + (int64_t)a.window) * G;
+  if (a.sinks == 0 || rows - near <= std::max<int64_t>(near / 2, 512)) return 0;
+  const int64_t groups = (int64_t)a.batch * a.kv_heads * ((a.sinks + 31) / 32);
+  return (int)std::max<int64_t>(1, std::min<int64_t>({(rows - near) / 512, 256 / groups, 256}));
 }
 
 int64_t stat_bytes(const elasto_window_t& a) { return (int64_t)a.batch * a.heads * a.q_tokens * 8; }
@@ -442,12 +578,19 @@ hipError_t launch(BwdP p, int64_t pairs, hipStream_t s) {
     e = hipGetLastError();
   }
   if (e != hipSuccess || p.key_tiles == 0) return e;
-  p.blocks = pairs * (p.key_tiles + p.parts - 1);
+  if (p.parts > 0) {
+    p.blocks = pairs * p.sink_groups * p.parts;
+    hipLaunchKernelGGL((window_sink_kernel<T, HD>), dim3((unsigned)p.blocks), dim3(kThreads),
+                       (SinkShape<T, HD>::kLds), s, p);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  p.blocks = pairs * p.key_tiles;
   hipLaunchKernelGGL((window_dkv_kernel<T, HD>), dim3((unsigned)p.blocks), dim3(kThreads),
                      (Shape<T, HD>::kLdsKey), s, p);
   e = hipGetLastError();
-  if (e != hipSuccess || p.parts == 1) return e;
-  hipLaunchKernelGGL((window_sink_kernel<T, HD>), dim3((unsigned)(pairs * (kKeys * HD / 1024))),
+  if (e != hipSuccess || p.parts == 0) return e;
+  hipLaunchKernelGGL((window_sink_join_kernel<T, HD>), dim3((unsigned)(pairs * (kMaxSinks * HD / 1024))),
                      dim3(kThreads), 0, s, p);
   return hipGetLastError();
 }
@@ -457,7 +600,7 @@ hipError_t launch(BwdP p, int64_t pairs, hipStream_t s) {
 int64_t window_bwd_workspace(const elasto_window_t& a) {
   const int parts = parts_of(a);
   return (stat_bytes(a) + 255) / 256 * 256 +
-         (parts > 1 ? (int64_t)a.batch * a.kv_heads * parts * 2 * kKeys * a.head_dim * 4 : 0);
+         (parts > 0 ? (int64_t)a.batch * a.kv_heads * (parts + 1) * 2 * kMaxSinks * a.head_dim * 4 : 0);
 }
 
 hipError_t launch_window_bwd(const elasto_window_t& a, const WindowTensors& t, void* ws, hipStream_t s) {
@@ -484,7 +627,8 @@ hipError_t launch_window_bwd(const elasto_window_t& a, const WindowTensors& t, v
   p.parts = parts_of(a);
   p.stat = static_cast<float2*>(ws);
   p.part = reinterpret_cast<float*>(static_cast<char*>(ws) + (stat_bytes(a) + 255) / 256 * 256);
-  if (pairs * std::max(p.row_blocks, p.key_tiles + p.parts) > 0x7fffffff) return hipErrorInvalidValue;
+  p.sink_groups = (a.sinks + 31) / 32;
+  if (pairs * std::max({(int64_t)p.row_blocks, (int64_t)p.key_tiles, (int64_t)p.sink_groups * p.parts}) > 0x7fffffff) return hipErrorInvalidValue;
   if (a.dtype == ELASTO_BF16)
     return a.head_dim == 64 ? launch<uint16_t, 64>(p, pairs, s) : launch<uint16_t, 128>(p, pairs, s);
   return a.head_dim == 64 ? launch<float, 64>(p, pairs, s) : launch<float, 128>(p, pairs, s);
