@@ -49,8 +49,7 @@ __device__ __forceinline__ Keys keys_of(const Mask& m, int pos, int kl) {
 
 // What a block of scores starts from where the mask hides some of them: 0, or
 // -infinity, so that the branch over it leaves the scores where they are.  x[i]
-// is for key (or row) `from` + 8 * (i / 4) + i % 4 of a range of len; with
-// sinks, for key j + 8 * (i / 4) + i % 4.
+// is for row `from` + 8 * (i / 4) + i % 4 of a range of len.
 __device__ __forceinline__ f32x16 hidden(int from, unsigned len) {
   f32x16 x;
 #pragma unroll
@@ -58,9 +57,21 @@ __device__ __forceinline__ f32x16 hidden(int from, unsigned len) {
     x[i] = (unsigned)(from + 8 * (i >> 2) + (i & 3)) < len ? 0.0f : -INFINITY;
   return x;
 }
-__device__ __forceinline__ f32x16 hidden(int j, const Keys& k, bool sinks) {
-  f32x16 x = hidden(j - k.lo, (unsigned)max(k.hi - k.lo + 1, 0));
-  const int sink = k.hs - j;
+// Keys j + 8 * (i / 4) + i % 4.  low, high: some of the block's keys may lie
+// before a row's window, behind it (one of them: one comparison a score);
+// sinks: some may be sinks.
+__device__ __forceinline__ f32x16 hidden(int j, const Keys& k, bool low, bool high, bool sinks) {
+  f32x16 x;
+  const int first = k.lo - j, last = k.hi - j, sink = k.hs - j;
+  if (low && high) {
+    x = hidden(-first, (unsigned)max(k.hi - k.lo + 1, 0));
+  } else if (high) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = 8 * (i >> 2) + (i & 3) <= last ? 0.0f : -INFINITY;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = 8 * (i >> 2) + (i & 3) >= first ? 0.0f : -INFINITY;
+  }
   if (sinks)
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = sink >= 8 * (i >> 2) + (i & 3) ? 0.0f : x[i];
@@ -101,6 +112,36 @@ __device__ __forceinline__ void zero(f32x16& v) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) v[i] = 0.0f;
 }
+
+// `bytes` bytes at p as a buffer (at most 4 GiB - 1 of them).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const char* p, int64_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), (short)0,
+                                           (int)(uint32_t)(bytes < 0xffffffffll ? bytes : 0xffffffffll),
+                                           kRsrcWord3);
+}
+
+// One head of k or v of one sequence: rows st bytes apart.
+struct KeyRows {
+  const char* p;
+  int64_t st;
+  int last;                    // of the sequence
+  bool near;                   // all of it within 32-bit offsets: one buffer for every tile
+  __amdgpu_buffer_rsrc_t all;
+  __device__ __forceinline__ KeyRows(const char* base, int64_t stride, int kl, int row_bytes)
+      : p(base), st(stride), last(kl - 1) {
+    const int64_t bytes = (int64_t)max(last, 0) * st + row_bytes;
+    near = bytes < ((int64_t)1 << 31);
+    all = buffer_of(p, bytes);
+  }
+  // The tile that starts at row j0, to LDS.
+  template <typename L>
+  __device__ __forceinline__ void issue(char* tile, int wave, int lane, int j0, int row_bytes) const {
+    if (near)
+      L::issue(tile, wave, lane, all, (uint32_t)j0 * (uint32_t)st, (uint32_t)st);
+    else
+      L::issue(tile, wave, lane, buffer_of(p + j0 * st, (last - j0) * st + row_bytes), 0, (uint32_t)st);
+  }
+};
 
 template <typename T>
 struct Frag;
@@ -197,26 +238,23 @@ struct Tile {
     static __device__ __forceinline__ int piece(int i, int wave, int lane) {
       return (lane % kPieces) ^ ((row(i, wave, lane) >> 2) & 3);
     }
-    // offset(i): where the lane's row of load i lies after base; what lies past
-    // `bytes` bytes arrives as zeros.
+    // offset(i): where the lane's row of load i lies in src; what lies past its
+    // end arrives as zeros.
     template <typename F>
-    static __device__ __forceinline__ void issue(char* tile, int wave, int lane, const char* base,
-                                                 int64_t bytes, F&& offset) {
-      const __amdgpu_buffer_rsrc_t src = __builtin_amdgcn_make_buffer_rsrc(
-          const_cast<char*>(base), (short)0, (int)(uint32_t)(bytes < 0xffffffffll ? bytes : 0xffffffffll),
-          kRsrcWord3);
+    static __device__ __forceinline__ void issue(char* tile, int wave, int lane,
+                                                 __amdgpu_buffer_rsrc_t src, F&& offset) {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(tile + (wave + WAVES * i) * kBlock), 16,
                                                  (int)(offset(i) + piece(i, wave, lane) * 16), 0, 0, 0);
     }
-    // Rows st bytes apart.
-    static __device__ __forceinline__ void issue(char* tile, int wave, int lane, const char* base,
-                                                 int64_t bytes, uint32_t st) {
+    // Rows st bytes apart, the first at `at`.
+    static __device__ __forceinline__ void issue(char* tile, int wave, int lane,
+                                                 __amdgpu_buffer_rsrc_t src, uint32_t at, uint32_t st) {
       const uint32_t first = (uint32_t)row(0, wave, lane) * st;
-      issue(tile, wave, lane, base, bytes, [&](int i) {
+      issue(tile, wave, lane, src, [&](int i) {
         // The rows of two loads are the same number apart in every lane.
-        return first + (uint32_t)(row(i, 0, 0) - row(0, 0, 0)) * st;
+        return first + (at + (uint32_t)(row(i, 0, 0) - row(0, 0, 0)) * st);
       });
     }
   };

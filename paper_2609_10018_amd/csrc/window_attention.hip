@@ -74,21 +74,21 @@ struct State {
     for (int n = 0; n < HD / 32; ++n) stay<sizeof(T) == 2 || HD == 64>(o[n]);
   }
 
-  // One tile of SUB * 32 keys from j0 on; sinks: some of them may be.
+  // One tile of SUB * 32 keys from j0 on; low, high, sinks: as for hidden().
   template <int SUB>
   __device__ __forceinline__ void tile(const char* kt, const char* vt, int j0, const Frag<T>* q,
-                                       float c2, bool inside, bool sinks, const Keys& ks, int h,
+                                       float c2, bool low, bool high, bool sinks, const Keys& ks, int h,
                                        const typename Tile<T, HD>::Reader& rd) {
     f32x16 s[SUB];
 #pragma unroll
     for (int b = 0; b < SUB; ++b) {
       Frag<T> a;
       rd.operand(kt, b * 32, 0, a);
-      if (inside) {
+      if (!low && !high) {
         zero(s[b]);
         s[b] = mma(a, q[0], s[b]);
       } else {
-        s[b] = mma(a, q[0], hidden(j0 + b * 32 + 4 * h, ks, sinks));
+        s[b] = mma(a, q[0], hidden(j0 + b * 32 + 4 * h, ks, low, high, sinks));
       }
     }
 #pragma unroll
@@ -178,16 +178,15 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   const int zs = (int)((int64_t)tiles * z / p.splits), ze = (int)((int64_t)tiles * (z + 1) / p.splits);
   auto key0 = [&](int n) { return (n < sink_tiles ? n : t0 + n - sink_tiles) * S::kKeys; };
 
-  const char* kp = p.k.p + b * p.k.sb + hk * p.k.sh;
-  const char* vp = p.v.p + b * p.v.sb + hk * p.v.sh;
+  const KeyRows kr(p.k.p + b * p.k.sb + hk * p.k.sh, p.k.st, kl, Tl::kRow);
+  const KeyRows vr(p.v.p + b * p.v.sb + hk * p.v.sh, p.v.st, kl, Tl::kRow);
   // Keys past the last one arrive as zeros: they are masked, and what the
   // memory holds there is not read.
   using Ld = typename Tl::template Loads<S::kKeys, KEYS ? 1 : kWaves>;
   const int lw = KEYS ? 0 : wave;
   auto stage = [&](int n, char* dst) {
-    const int j0 = key0(n);
-    Ld::issue(dst, lw, lane, kp + j0 * p.k.st, (kl - 1 - j0) * p.k.st + Tl::kRow, (uint32_t)p.k.st);
-    Ld::issue(dst + S::kTile, lw, lane, vp + j0 * p.v.st, (kl - 1 - j0) * p.v.st + Tl::kRow, (uint32_t)p.v.st);
+    kr.template issue<Ld>(dst, lw, lane, key0(n), Tl::kRow);
+    vr.template issue<Ld>(dst + S::kTile, lw, lane, key0(n), Tl::kRow);
   };
 
   const typename Tl::Reader rd(lane);
@@ -203,7 +202,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
     st.hold();
     // Unless this wave's rows see nothing of the tile.
     if (!idle && (j0 <= w1.hs || (j1 >= w0.lo && j0 <= w1.hi)))
-      st.template tile<S::kSub>(buf, buf + S::kTile, j0, q, p.c2, j0 >= w1.lo && j1 <= w0.hi,
+      st.template tile<S::kSub>(buf, buf + S::kTile, j0, q, p.c2, j0 < w1.lo, j1 > w0.hi,
                                 j0 <= w1.hs, mine, h, rd);
     st.hold();
   };

@@ -99,13 +99,12 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   const int t0 = max(a0.lo / S::kRows, sink_tiles);
   const int tiles = sink_tiles + (a1.hi >= a0.lo ? max(a1.hi / S::kRows + 1 - t0, 0) : 0);
   auto key0 = [&](int n) { return (n < sink_tiles ? n : t0 + n - sink_tiles) * S::kRows; };
-  const char* kp = p.k.p + b * p.k.sb + hk * p.k.sh;
-  const char* vp = p.v.p + b * p.v.sb + hk * p.v.sh;
+  const KeyRows kr(p.k.p + b * p.k.sb + hk * p.k.sh, p.k.st, kl, Tl::kRow);
+  const KeyRows vr(p.v.p + b * p.v.sb + hk * p.v.sh, p.v.st, kl, Tl::kRow);
   using Ld = typename Tl::template Loads<S::kRows, kWaves>;
   auto stage = [&](int n, char* dst) {
-    const int j0 = key0(n);
-    Ld::issue(dst, wave, lane, kp + j0 * p.k.st, (kl - 1 - j0) * p.k.st + Tl::kRow, (uint32_t)p.k.st);
-    Ld::issue(dst + S::kTile, wave, lane, vp + j0 * p.v.st, (kl - 1 - j0) * p.v.st + Tl::kRow, (uint32_t)p.v.st);
+    kr.template issue<Ld>(dst, wave, lane, key0(n), Tl::kRow);
+    vr.template issue<Ld>(dst + S::kTile, wave, lane, key0(n), Tl::kRow);
   };
   const typename Tl::Reader rd(lane);
 
@@ -147,17 +146,17 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
     for (int f = 0; f < HD / 32; ++f) stay<kStay>(dq[f]);
     // Unless this wave's rows see nothing of the tile.
     if (!idle && (j0 <= w1.hs || (j1 >= w0.lo && j0 <= w1.hi))) {
-      const bool inside = j0 >= w1.lo && j1 <= w0.hi;
+      const bool low = j0 < w1.lo, high = j1 > w0.hi;
 #pragma unroll
       for (int s = 0; s < S::kSub; ++s) {
         f32x16 sc, dp;
         Frag<T> a;
         rd.operand(kt, s * 32, 0, a);
-        if (inside) {
+        if (!low && !high) {
           zero(sc);
           sc = mma(a, q[0], sc);
         } else {
-          sc = mma(a, q[0], hidden(j0 + s * 32 + 4 * h, mine, j0 <= w1.hs));
+          sc = mma(a, q[0], hidden(j0 + s * 32 + 4 * h, mine, low, high, j0 <= w1.hs));
         }
         zero(dp);
 #pragma unroll
@@ -315,7 +314,7 @@ __device__ __forceinline__ void stage_rows(const BwdP& p, char* dst, const char*
   using Tl = Tile<T, HD>;
   using Ld = typename Tl::template Loads<ROWS, WAVES>;
   const int G = p.group, i0 = r0 / G;
-  const char* from = base + i0 * t.st;
+  const __amdgpu_buffer_rsrc_t from = buffer_of(base + i0 * t.st, 0xffffffffll);
   const uint32_t st = (uint32_t)t.st, sh = (uint32_t)t.sh;
   // Where the rows of two loads are whole queries apart, one offset serves all
   // loads of every tile.
@@ -323,11 +322,11 @@ __device__ __forceinline__ void stage_rows(const BwdP& p, char* dst, const char*
     const int r = Ld::row(0, wave, lane), i = r / G;
     const uint32_t first = (uint32_t)i * st + (uint32_t)(r - i * G) * sh;
     const uint32_t next = (uint32_t)(4 * Tl::kBlockRows / G) * st;
-    Ld::issue(dst, wave, lane, from, 0xffffffffll, [&](int l) { return first + (uint32_t)l * next; });
+    Ld::issue(dst, wave, lane, from, [&](int l) { return first + (uint32_t)l * next; });
   } else {
     int ln = lane;  // nothing of this branch is to be kept in registers over the loop
     asm volatile("" : "+v"(ln));
-    Ld::issue(dst, wave, lane, from, 0xffffffffll, [&](int l) {
+    Ld::issue(dst, wave, lane, from, [&](int l) {
       const unsigned r = (unsigned)min(r0 + Ld::row(l, wave, ln), rows - 1);
       const unsigned i = __umulhi(r << 3, p.div_mul) >> p.div_shift;
       return (i - (uint32_t)i0) * st + (r - i * (unsigned)G) * sh;
