@@ -463,8 +463,9 @@ typedef struct {
  * BF16: q and k in bf16, everything between load and store in fp32, rounded
  * once; FP32: fp32 throughout.
  * Needs head_dim a multiple of 16 in [16, 256], rot_dim a multiple of 16 in
- * [0, head_dim], eps > 0, batch, tokens, q_heads and kv_heads >= 0 with at
- * least one head (a side of no heads takes NULL tensors). */
+ * [0, head_dim], eps > 0 (and not subnormal), batch, tokens, q_heads and
+ * kv_heads >= 0 with at least one head (a side of no heads takes NULL tensors),
+ * batch * tokens below 2^31. */
 typedef struct {
   int32_t dtype, batch, tokens, q_heads, kv_heads, head_dim;
   int32_t rot_dim, interleaved, table_rows;

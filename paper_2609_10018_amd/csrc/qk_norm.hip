@@ -9,13 +9,14 @@
 //   dx = r (g - u mean(g (.) u)),  dgamma = sum over tokens and heads of e (.) u.
 //
 // A group of GW lanes takes a head vector in 16-byte pieces, one a lane, so a
-// vector is read once, straight into registers, and the reductions are xor
-// shuffles inside the group.  A unit of work is kHeads vectors of one token:
-// their loads are all in flight together, and the token's cosines and sines
-// (which depend on neither the head nor q or k) are loaded once for them.  With
-// halves paired, feature i turns with i + rot/2, which another lane of the
-// group holds: its raw piece is exchanged (4 registers) before the norm, since
-// r is the group's and gamma is known to both.
+// vector is read once, straight into registers, and the reductions stay inside
+// the group.  A group walks the heads of a token (or a part of them, where the
+// tokens alone would leave CUs idle), kHeads loads in flight at a time: the
+// token's cosines and sines, which depend on neither the head nor q or k, are
+// loaded once and multiplied with gamma once, and a head then costs a feature
+// about eight instructions.  With halves paired, feature i turns with i + rot/2,
+// which another lane of the group holds: its raw piece is exchanged (4
+// registers), since the norm is the group's and gamma is known to both.
 //
 // Everything between the load and the store is fp32; the result is rounded
 // once.  Bound by memory: 2 (backward 3) passes over q and k.
@@ -28,8 +29,8 @@ namespace elasto {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kHeads = 4;        // head vectors of a unit
-constexpr int kGradBlocks = 1024;  // workgroups of the backward pass (4 a CU)
+constexpr int kHeads = 4;          // head vectors in flight
+constexpr int kGradBlocks = 768;   // workgroups of the backward pass (3 a CU, as its registers allow)
 
 struct Side {  // q or k
   View x;      // the input
@@ -43,8 +44,8 @@ struct QkP {
   Side q, k;
   const float *cos, *sin;
   const int32_t *positions, *lens;
-  int tokens, dim, rot, table_rows, chunks;
-  int64_t units;  // batch * tokens * chunks
+  int tokens, dim, rot, table_rows;
+  int rows, parts, part_heads;  // batch * tokens; parts of the heads, heads of each
   float eps, inv_dim;
   float* part;  // backward: [workgroup][2][dim]
 };
@@ -79,23 +80,43 @@ struct Piece<float> {
   }
 };
 
+// The sum over the group in each of its lanes: in quads, in eights and in rows
+// of 16 by lane moves of the adder itself (each step's operands are the same in
+// all lanes that it pairs up), beyond by exchanging halves.
+template <int CTRL>
+__device__ __forceinline__ float add_moved(float v) {
+  return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(
+                 0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
 template <int GW>
 __device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-  for (int o = GW / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+  v = add_moved<0xB1>(v);                       // lane ^ 1
+  if constexpr (GW >= 4) v = add_moved<0x4E>(v);   // lane ^ 2
+  if constexpr (GW >= 8) v = add_moved<0x141>(v);  // the other quad of eight
+  if constexpr (GW >= 16) v = add_moved<0x140>(v); // the other eight of a row
+  if constexpr (GW >= 32) v += __shfl_xor(v, 16, 64);
+  if constexpr (GW >= 64) v += __shfl_xor(v, 32, 64);
   return v;
 }
 
-// What a lane knows about its features for the whole launch.
+__device__ __forceinline__ u32x4 exchange(const u32x4& w, int lane4) {
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = (uint32_t)__builtin_amdgcn_ds_bpermute(lane4, (int)w[i]);
+  return r;
+}
+
+// What a lane knows about its features: out = r (x (.) own + xp (.) other), with
+// xp the features that x turns with.
 template <typename T, bool PAIRS>
 struct Lane {
   static constexpr int N = Piece<T>::N;
-  int f0;       // first feature of the piece
-  bool on;      // the piece lies inside the head
-  bool turns;   // its features are rotated
-  int partner;  // lane that holds the features these turn with
-  float sign;   // of the sine in this piece's results (halves)
-  float gq[N], gk[N], pq[N], pk[N];  // gamma of the piece, and of the partner's
+  int f0;        // first feature of the piece
+  bool on;       // the piece lies inside the head
+  bool turns;    // its features are rotated
+  int partner4;  // 4 * the lane that holds the features these turn with
+  int pf;        // their first
+  float sign;    // of the sine in this piece's results (halves)
 
   __device__ __forceinline__ Lane(const QkP& p, int li, int lane) {
     f0 = li * N;
@@ -103,23 +124,16 @@ struct Lane {
     turns = f0 < p.rot;
     const int half = p.rot / 2;
     const bool low = f0 < half;
-    const int shift = half / N;
-    partner = PAIRS || !turns ? lane : low ? lane + shift : lane - shift;
+    partner4 = 4 * (PAIRS || !turns ? lane : low ? lane + half / N : lane - half / N);
+    pf = PAIRS || !turns ? f0 : low ? f0 + half : f0 - half;
     sign = low ? -1.0f : 1.0f;
-    const int pf = PAIRS || !turns ? f0 : low ? f0 + half : f0 - half;
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      gq[e] = on && p.q.gamma ? p.q.gamma[f0 + e] : 1.0f;
-      gk[e] = on && p.k.gamma ? p.k.gamma[f0 + e] : 1.0f;
-      pq[e] = on && p.q.gamma ? p.q.gamma[pf + e] : 1.0f;
-      pk[e] = on && p.k.gamma ? p.k.gamma[pf + e] : 1.0f;
-    }
   }
 
-  // Cosines and sines of the piece at token row `row`; NaN where the position
-  // has no row in the tables.
-  __device__ __forceinline__ void angles(const QkP& p, int64_t row, int t, float* c,
-                                         float* s) const {
+  // Cosines and signed sines of the piece at token row `row` (1 and 0 where it
+  // does not turn); NaN where the position has no row in the tables.
+  __device__ __forceinline__ void angles(const QkP& p, int row, int t, float* c, float* s) const {
+#pragma unroll
+    for (int e = 0; e < N; ++e) c[e] = 1.0f, s[e] = 0.0f;
     if (!turns) return;
     const int pos = p.positions ? p.positions[row] : t;
     const bool ok = pos >= 0 && pos < p.table_rows;
@@ -127,107 +141,159 @@ struct Lane {
     const int at = PAIRS ? f0 / 2 : (f0 < half ? f0 : f0 - half);
     const float* cp = p.cos + (int64_t)(ok ? pos : 0) * half + at;
     const float* sp = p.sin + (int64_t)(ok ? pos : 0) * half + at;
-    constexpr int M = PAIRS ? N / 2 : N;
 #pragma unroll
-    for (int e = 0; e < M; ++e) {
-      c[e] = ok ? cp[e] : NAN;
-      s[e] = ok ? sp[e] : NAN;
+    for (int e = 0; e < (PAIRS ? N / 2 : N); ++e) {
+      const float ce = ok ? cp[e] : NAN, se = ok ? sp[e] : NAN;
+      if constexpr (PAIRS) {
+        c[2 * e] = c[2 * e + 1] = ce;
+        s[2 * e] = -se;
+        s[2 * e + 1] = se;
+      } else {
+        c[e] = ce;
+        s[e] = sign * se;
+      }
+    }
+  }
+  __device__ __forceinline__ void weights(const float* gamma, float* g, float* gp) const {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      g[e] = on && gamma ? gamma[f0 + e] : 1.0f;
+      gp[e] = on && gamma ? gamma[PAIRS ? f0 + (e ^ 1) : pf + e] : 1.0f;
+    }
+  }
+  // The features that x turns with, from the group's raw pieces.
+  __device__ __forceinline__ void partners(const u32x4& raw, const float* x, float* xp) const {
+    if constexpr (PAIRS) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) xp[e] = x[e ^ 1];
+    } else {
+      Piece<T>::unpack(exchange(raw, partner4), xp);
     }
   }
 };
 
+// A group's token and its share of the heads.
 struct Unit {
-  int64_t b;
-  int t, h0;
+  int row, b, t, h0, h1;
+  bool live;
 };
-
-__device__ __forceinline__ Unit unit_of(const QkP& p, int64_t u, int64_t* row) {
+__device__ __forceinline__ Unit unit_of(const QkP& p, int64_t u) {
   Unit w;
-  *row = u / p.chunks;
-  w.h0 = (int)(u - *row * p.chunks) * kHeads;
-  w.b = *row / p.tokens;
-  w.t = (int)(*row - w.b * p.tokens);
+  w.live = u < (int64_t)p.rows * p.parts;
+  const unsigned v = w.live ? (unsigned)u : 0u;  // rows * parts < 2^31
+  w.row = (int)(v / (unsigned)p.parts);
+  w.h0 = (int)(v - (unsigned)w.row * p.parts) * p.part_heads;
+  w.h1 = min(w.h0 + p.part_heads, p.q.heads + p.k.heads);
+  w.b = (int)((unsigned)w.row / (unsigned)p.tokens);
+  w.t = w.row - w.b * p.tokens;
+  if (w.live && p.lens) w.live = w.t < p.lens[w.b];
   return w;
 }
 
-// y turned; yp: the partner's y (halves only).
-template <typename T, bool PAIRS>
-__device__ __forceinline__ void turn(const Lane<T, PAIRS>& L, const float* c, const float* s,
-                                     float* y, const float* yp) {
-  constexpr int N = Piece<T>::N;
-  if (!L.turns) return;
-  if constexpr (PAIRS) {
-#pragma unroll
-    for (int e = 0; e < N; e += 2) {
-      const float a = y[e], b = y[e + 1];
-      y[e] = fmaf(a, c[e / 2], -b * s[e / 2]);
-      y[e + 1] = fmaf(b, c[e / 2], a * s[e / 2]);
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < N; ++e) y[e] = fmaf(y[e], c[e], L.sign * yp[e] * s[e]);
-  }
+__device__ __forceinline__ float inv_norm(float ss, const QkP& p) {
+  return __builtin_amdgcn_rsqf(fmaf(ss, p.inv_dim, p.eps));
 }
 
-__device__ __forceinline__ u32x4 from_lane(const u32x4& w, int lane) {
-  u32x4 r;
+template <typename T, int GW, bool PAIRS>
+__device__ __forceinline__ void forward_heads(const QkP& p, const Side& s, const Lane<T, PAIRS>& L,
+                                              const Unit& w, int h0, int h1, const float* c,
+                                              const float* sn) {
+  constexpr int N = Piece<T>::N;
+  float own[N], other[N];
+  L.weights(s.gamma, own, other);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) r[i] = (uint32_t)__shfl((int)w[i], lane, 64);
-  return r;
+  for (int e = 0; e < N; ++e) own[e] *= c[e], other[e] *= sn[e];
+  const bool on = w.live && L.on;
+  const char* x = s.x.p + w.b * s.x.sb + w.t * s.x.st + h0 * s.x.sh + L.f0 * (int)sizeof(T);
+  char* out = s.out.p + w.b * s.out.sb + w.t * s.out.st + h0 * s.out.sh + L.f0 * (int)sizeof(T);
+  for (int h = h0; h < h1; h += kHeads) {
+    u32x4 raw[kHeads];
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i) {
+      raw[i] = u32x4{0u, 0u, 0u, 0u};
+      if (on && h + i < h1) raw[i] = *reinterpret_cast<const u32x4*>(x + i * s.x.sh);
+    }
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i) {
+      float v[N], vp[N];
+      Piece<T>::unpack(raw[i], v);
+      float ss = 0.0f;
+#pragma unroll
+      for (int e = 0; e < N; ++e) ss = fmaf(v[e], v[e], ss);
+      const float r = inv_norm(group_sum<GW>(ss), p);
+      L.partners(raw[i], v, vp);
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = r * fmaf(v[e], own[e], vp[e] * other[e]);
+      if (on && h + i < h1) *reinterpret_cast<u32x4*>(out + i * s.out.sh) = Piece<T>::pack(v);
+    }
+    x += kHeads * s.x.sh;
+    out += kHeads * s.out.sh;
+  }
 }
 
 template <typename T, int GW, bool PAIRS>
 __global__ __launch_bounds__(kThreads) void qk_norm_kernel(QkP p) {
   constexpr int N = Piece<T>::N;
-  const int lane = threadIdx.x & 63, li = lane % GW;
-  const int64_t u = (int64_t)blockIdx.x * (kThreads / GW) + threadIdx.x / GW;
-  const Lane<T, PAIRS> L(p, li, lane);
-  int64_t row = 0;
-  Unit w = {0, 0, 0};
-  bool live = u < p.units;
-  if (live) {
-    w = unit_of(p, u, &row);
-    live = !p.lens || w.t < p.lens[w.b];
-  }
-  const int heads = p.q.heads + p.k.heads;
-  u32x4 raw[kHeads];
-#pragma unroll
-  for (int i = 0; i < kHeads; ++i) {
-    const int h = w.h0 + i;
-    raw[i] = u32x4{0u, 0u, 0u, 0u};
-    if (live && L.on && h < heads) {
-      const Side& s = h < p.q.heads ? p.q : p.k;
-      const int hh = h < p.q.heads ? h : h - p.q.heads;
-      raw[i] = *reinterpret_cast<const u32x4*>(s.x.p + w.b * s.x.sb + w.t * s.x.st + hh * s.x.sh + L.f0 * (int)sizeof(T));
-    }
-  }
+  const int lane = threadIdx.x & 63;
+  const Lane<T, PAIRS> L(p, lane % GW, lane);
+  const Unit w = unit_of(p, (int64_t)blockIdx.x * (kThreads / GW) + threadIdx.x / GW);
   float c[N], sn[N];
+  L.angles(p, w.row, w.t, c, sn);
+  // Every group of a wave takes as many rounds: those of the longest share.
+  const int q1 = min(w.h1, p.q.heads);
+  if (__any(w.h0 < q1)) forward_heads<T, GW, PAIRS>(p, p.q, L, w, w.h0, q1, c, sn);
+  const int k0 = max(w.h0 - p.q.heads, 0), k1 = w.h1 - p.q.heads;
+  if (__any(k0 < k1)) forward_heads<T, GW, PAIRS>(p, p.k, L, w, k0, k1, c, sn);
+}
+
+template <typename T, int GW, bool PAIRS>
+__device__ __forceinline__ void backward_heads(const QkP& p, const Side& s, const Lane<T, PAIRS>& L,
+                                               const Unit& w, int h0, int h1, const float* c,
+                                               const float* sn, const float* gamma, float* dgamma) {
+  constexpr int N = Piece<T>::N;
+  const bool on = w.live && L.on;
+  const int f = L.f0 * (int)sizeof(T);
+  const char* x = s.x.p + w.b * s.x.sb + w.t * s.x.st + h0 * s.x.sh + f;
+  const char* d = s.dout.p + w.b * s.dout.sb + w.t * s.dout.st + h0 * s.dout.sh + f;
+  char* out = s.out.p + w.b * s.out.sb + w.t * s.out.st + h0 * s.out.sh + f;
+  for (int h = h0; h < h1; h += kHeads) {
+    u32x4 raw[kHeads], draw[kHeads];
 #pragma unroll
-  for (int e = 0; e < N; ++e) c[e] = sn[e] = 0.0f;
-  if (live) L.angles(p, row, w.t, c, sn);
-#pragma unroll
-  for (int i = 0; i < kHeads; ++i) {
-    const int h = w.h0 + i;
-    const bool isq = h < p.q.heads;
-    float x[N], xp[N];
-    Piece<T>::unpack(raw[i], x);
-    float ss = 0.0f;
-#pragma unroll
-    for (int e = 0; e < N; ++e) ss = fmaf(x[e], x[e], ss);
-    const float r = 1.0f / sqrtf(fmaf(group_sum<GW>(ss), p.inv_dim, p.eps));
-    if constexpr (!PAIRS) Piece<T>::unpack(from_lane(raw[i], L.partner), xp);
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      x[e] *= r * (isq ? L.gq[e] : L.gk[e]);
-      if constexpr (!PAIRS) xp[e] *= r * (isq ? L.pq[e] : L.pk[e]);
+    for (int i = 0; i < kHeads; ++i) {
+      raw[i] = draw[i] = u32x4{0u, 0u, 0u, 0u};
+      if (on && h + i < h1) {
+        raw[i] = *reinterpret_cast<const u32x4*>(x + i * s.x.sh);
+        draw[i] = *reinterpret_cast<const u32x4*>(d + i * s.dout.sh);
+      }
     }
-    turn<T, PAIRS>(L, c, sn, x, xp);
-    if (live && L.on && h < heads) {
-      const Side& s = isq ? p.q : p.k;
-      const int hh = isq ? h : h - p.q.heads;
-      *reinterpret_cast<u32x4*>(s.out.p + w.b * s.out.sb + w.t * s.out.st + hh * s.out.sh + L.f0 * (int)sizeof(T)) =
-          Piece<T>::pack(x);
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i) {
+      float u[N], e[N], ep[N];
+      Piece<T>::unpack(raw[i], u);
+      float ss = 0.0f;
+#pragma unroll
+      for (int j = 0; j < N; ++j) ss = fmaf(u[j], u[j], ss);
+      const float r = inv_norm(group_sum<GW>(ss), p);
+      Piece<T>::unpack(draw[i], e);
+      L.partners(draw[i], e, ep);
+      float gu = 0.0f;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        // The transposed rotation turns the other way.
+        e[j] = fmaf(e[j], c[j], -ep[j] * sn[j]);
+        u[j] *= r;
+        const float a = e[j] * u[j];
+        dgamma[j] += a;  // heads and lanes that are not there hold zeros
+        gu = fmaf(gamma[j], a, gu);
+      }
+      gu = group_sum<GW>(gu) * p.inv_dim;
+#pragma unroll
+      for (int j = 0; j < N; ++j) e[j] = r * fmaf(gamma[j], e[j], -u[j] * gu);
+      if (on && h + i < h1) *reinterpret_cast<u32x4*>(out + i * s.out.sh) = Piece<T>::pack(e);
     }
+    x += kHeads * s.x.sh;
+    d += kHeads * s.dout.sh;
+    out += kHeads * s.out.sh;
   }
 }
 
@@ -235,80 +301,30 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(QkP p) {
 // part of dgamma in registers; the workgroup's groups are summed in LDS and its
 // row goes to part, which qk_gamma_kernel sums in a fixed order.
 template <typename T, int GW, bool PAIRS>
-__global__ __launch_bounds__(kThreads) void qk_norm_bwd_kernel(QkP p) {
+__global__ __launch_bounds__(kThreads, 3) void qk_norm_bwd_kernel(QkP p) {
   constexpr int N = Piece<T>::N, G = kThreads / GW;
   __shared__ float red[2][G][GW * N];
   const int lane = threadIdx.x & 63, li = lane % GW, grp = threadIdx.x / GW;
   const Lane<T, PAIRS> L(p, li, lane);
-  const int heads = p.q.heads + p.k.heads;
-  float dgq[N], dgk[N];
+  float dgq[N], dgk[N], gq[N], gk[N];
 #pragma unroll
-  for (int e = 0; e < N; ++e) dgq[e] = dgk[e] = 0.0f;
-  // Every group of a workgroup takes the same number of rounds: the shuffles
-  // stay uniform.
-  for (int64_t u0 = (int64_t)blockIdx.x * G; u0 < p.units; u0 += (int64_t)gridDim.x * G) {
-    const int64_t u = u0 + grp;
-    int64_t row = 0;
-    Unit w = {0, 0, 0};
-    bool live = u < p.units;
-    if (live) {
-      w = unit_of(p, u, &row);
-      live = !p.lens || w.t < p.lens[w.b];
-    }
-    u32x4 raw[kHeads], draw[kHeads];
-#pragma unroll
-    for (int i = 0; i < kHeads; ++i) {
-      const int h = w.h0 + i;
-      raw[i] = draw[i] = u32x4{0u, 0u, 0u, 0u};
-      if (live && L.on && h < heads) {
-        const Side& s = h < p.q.heads ? p.q : p.k;
-        const int hh = h < p.q.heads ? h : h - p.q.heads;
-        raw[i] = *reinterpret_cast<const u32x4*>(s.x.p + w.b * s.x.sb + w.t * s.x.st + hh * s.x.sh + L.f0 * (int)sizeof(T));
-        draw[i] = *reinterpret_cast<const u32x4*>(s.dout.p + w.b * s.dout.sb + w.t * s.dout.st + hh * s.dout.sh + L.f0 * (int)sizeof(T));
-      }
-    }
+  for (int e = 0; e < N; ++e) {
+    dgq[e] = dgk[e] = 0.0f;
+    gq[e] = L.on && p.q.gamma ? p.q.gamma[L.f0 + e] : 1.0f;
+    gk[e] = L.on && p.k.gamma ? p.k.gamma[L.f0 + e] : 1.0f;
+  }
+  const int64_t units = (int64_t)p.rows * p.parts;
+  for (int64_t u0 = (int64_t)blockIdx.x * G; u0 < units; u0 += (int64_t)gridDim.x * G) {
+    const Unit w = unit_of(p, u0 + grp);
     float c[N], sn[N];
+    L.angles(p, w.row, w.t, c, sn);
+    if (!w.live)  // no position of a token that is not there spoils the sums
 #pragma unroll
-    for (int e = 0; e < N; ++e) c[e] = sn[e] = 0.0f;
-    if (live) {
-      L.angles(p, row, w.t, c, sn);
-      // The transposed rotation turns the other way.
-#pragma unroll
-      for (int e = 0; e < N; ++e) sn[e] = -sn[e];
-    }
-#pragma unroll
-    for (int i = 0; i < kHeads; ++i) {
-      const int h = w.h0 + i;
-      const bool isq = h < p.q.heads, some = live && h < heads;
-      float x[N], d[N], dp[N];
-      Piece<T>::unpack(raw[i], x);
-      Piece<T>::unpack(draw[i], d);
-      if constexpr (!PAIRS) Piece<T>::unpack(from_lane(draw[i], L.partner), dp);
-      turn<T, PAIRS>(L, c, sn, d, dp);
-      float ss = 0.0f;
-#pragma unroll
-      for (int e = 0; e < N; ++e) ss = fmaf(x[e], x[e], ss);
-      const float r = 1.0f / sqrtf(fmaf(group_sum<GW>(ss), p.inv_dim, p.eps));
-      float gu = 0.0f;
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        x[e] *= r;
-        const float a = d[e] * x[e];
-        if (some && isq) dgq[e] += a;
-        if (some && !isq) dgk[e] += a;
-        d[e] *= isq ? L.gq[e] : L.gk[e];
-        gu = fmaf(d[e], x[e], gu);
-      }
-      gu = group_sum<GW>(gu) * p.inv_dim;
-#pragma unroll
-      for (int e = 0; e < N; ++e) d[e] = r * fmaf(-x[e], gu, d[e]);
-      if (some && L.on) {
-        const Side& s = isq ? p.q : p.k;
-        const int hh = isq ? h : h - p.q.heads;
-        *reinterpret_cast<u32x4*>(s.out.p + w.b * s.out.sb + w.t * s.out.st + hh * s.out.sh + L.f0 * (int)sizeof(T)) =
-            Piece<T>::pack(d);
-      }
-    }
+      for (int e = 0; e < N; ++e) c[e] = sn[e] = 0.0f;
+    const int q1 = min(w.h1, p.q.heads);
+    if (__any(w.h0 < q1)) backward_heads<T, GW, PAIRS>(p, p.q, L, w, w.h0, q1, c, sn, gq, dgq);
+    const int k0 = max(w.h0 - p.q.heads, 0), k1 = w.h1 - p.q.heads;
+    if (__any(k0 < k1)) backward_heads<T, GW, PAIRS>(p, p.k, L, w, k0, k1, c, sn, gk, dgk);
   }
   if (!p.part) return;
 #pragma unroll
@@ -325,18 +341,20 @@ __global__ __launch_bounds__(kThreads) void qk_norm_bwd_kernel(QkP p) {
   }
 }
 
-// dgamma: column i of part summed over its rows, 16 columns a workgroup.
-__global__ __launch_bounds__(kThreads) void qk_gamma_kernel(const float* part, int rows, int dim,
-                                                            float* dq, float* dk) {
-  __shared__ float red[16][16];
-  const int col = blockIdx.x * 16 + (threadIdx.x & 15), sl = threadIdx.x >> 4;
+// dgamma: column i of part summed over its rows, 16 columns a workgroup, its
+// 1024 threads 64 slices of the rows.
+__global__ __launch_bounds__(1024) void qk_gamma_kernel(const float* part, int rows, int dim,
+                                                        float* dq, float* dk) {
+  __shared__ float red[64][17];
+  const int c = threadIdx.x & 15, sl = threadIdx.x >> 4, col = blockIdx.x * 16 + c;
   float s = 0.0f;
-  for (int r = sl; r < rows; r += 16) s += part[(int64_t)r * 2 * dim + col];
-  red[sl][threadIdx.x & 15] = s;
+#pragma unroll 16
+  for (int r = sl; r < rows; r += 64) s += part[(int64_t)r * 2 * dim + col];
+  red[sl][c] = s;
   __syncthreads();
   if (threadIdx.x >= 16) return;
   s = 0.0f;
-  for (int i = 0; i < 16; ++i) s += red[i][threadIdx.x];
+  for (int i = 0; i < 64; ++i) s += red[i][threadIdx.x];
   float* out = col < dim ? dq : dk;
   if (out) out[col < dim ? col : col - dim] = s;
 }
@@ -394,8 +412,8 @@ elasto_status_t run(const elasto_qk_norm_t* a, const elasto_heads_t* q, const el
                     const elasto_heads_t* q_res, const elasto_heads_t* k_res, float* dq_gamma,
                     float* dk_gamma, void* ws, int64_t ws_bytes, bool back, void* hip_stream) {
   if (!check_desc(a)) return ELASTO_ERR_INVALID_ARG;
-  if (!(a->eps > 0.0f) || !(a->eps < INFINITY))
-    return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: eps must be positive and finite");
+  if (!(a->eps >= 1.17549435e-38f) || !(a->eps < INFINITY))
+    return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: eps must be a positive normal number");
   if (a->rot_dim < 0 || a->rot_dim > a->head_dim || a->rot_dim % 16)
     return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: rot_dim %d is not a multiple of 16 in [0, head_dim]", a->rot_dim);
   const int64_t rows = (int64_t)a->batch * a->tokens;
@@ -420,14 +438,24 @@ elasto_status_t run(const elasto_qk_norm_t* a, const elasto_heads_t* q, const el
   p.dim = a->head_dim;
   p.rot = a->rot_dim;
   p.table_rows = a->table_rows;
-  p.chunks = (a->q_heads + a->kv_heads + kHeads - 1) / kHeads;
-  p.units = rows * p.chunks;
   p.eps = a->eps;
   p.inv_dim = 1.0f / (float)a->head_dim;
   int gw = 2;
   while (gw * n < a->head_dim) gw *= 2;
   const int groups = kThreads / gw;
-  int64_t grid = (p.units + groups - 1) / groups;
+  // Parts of the heads, whole rounds of kHeads each: as many as it takes for
+  // 1024 workgroups (backward: for two units a group).  Each part loads the
+  // cosines again: 256 x 197 tokens in 1, 2 and 6 parts 66, 79 and 127 us, 64 x
+  // 197 in 1 and 3 33 and 23 us; backward 4 x 6001 tokens in 1, 2, 3 and 6 parts
+  // 140, 134, 143 and 147 us.
+  const int heads = a->q_heads + a->kv_heads, rounds = (heads + kHeads - 1) / kHeads;
+  const int64_t want = (int64_t)(back ? 2 * kGradBlocks : 1024) * groups;
+  const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(rounds, (want + rows - 1) / std::max<int64_t>(rows, 1)));
+  p.part_heads = (rounds + parts - 1) / parts * kHeads;
+  p.parts = (heads + p.part_heads - 1) / p.part_heads;
+  p.rows = (int)rows;
+  if (rows * p.parts >= ((int64_t)1 << 31)) return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: too many head vectors");
+  int64_t grid = (rows * p.parts + groups - 1) / groups;
   const bool weights = back && (dq_gamma || dk_gamma);
   if (back) {
     grid = std::min<int64_t>(grid, kGradBlocks);
@@ -438,8 +466,6 @@ elasto_status_t run(const elasto_qk_norm_t* a, const elasto_heads_t* q, const el
                     (long long)(ws ? ws_bytes : 0), (long long)need);
       p.part = static_cast<float*>(ws);
     }
-  } else if (grid > 0x7fffffff) {
-    return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: too many head vectors");
   }
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   hipError_t e = hipSuccess;
@@ -453,7 +479,7 @@ elasto_status_t run(const elasto_qk_norm_t* a, const elasto_heads_t* q, const el
     e = hipGetLastError();
   }
   if (e == hipSuccess && weights) {
-    hipLaunchKernelGGL(qk_gamma_kernel, dim3((unsigned)(2 * a->head_dim / 16)), dim3(kThreads), 0, s,
+    hipLaunchKernelGGL(qk_gamma_kernel, dim3((unsigned)(2 * a->head_dim / 16)), dim3(1024), 0, s,
                        p.part, (int)grid, a->head_dim, dq_gamma, dk_gamma);
     e = hipGetLastError();
   }

@@ -380,28 +380,45 @@ def op_attention(dtype: int, qkv, qkv_stride: int, o, o_stride: int, batch: int,
                                              _stream_ptr(stream)))
 
 
+# Per-call work of the operators below is kept small: a call on a few tokens
+# takes less time on the GPU than these checks would if they formatted names.
+_torch = None        # the module, its element types and its current-device call, at the first use
+
+
+class _Torch:
+    def __init__(self):
+        import torch
+        self.f32, self.i32, self.u8 = torch.float32, torch.int32, torch.uint8
+        self.types = {torch.bfloat16: BF16, torch.float32: FP32}
+        self.device = torch.cuda.current_device
+
+
+def _tt() -> _Torch:
+    global _torch
+    if _torch is None:
+        _torch = _Torch()
+    return _torch
+
+
 def _same_device(*tensors) -> None:
     """Refuse tensors that do not all lie on the current device: the kernels run there."""
-    import torch
-    d = torch.cuda.current_device()
+    d = _tt().device()
     for t in tensors:
-        if t is not None and t.device.index != d:
+        if t is not None and t.get_device() != d:
             raise ValueError(f"a tensor lies on {t.device}, the current device is cuda:{d}")
 
 
 def _dtype(t) -> int:
-    name = str(t.dtype)
-    if name == "torch.bfloat16":
-        return BF16
-    if name == "torch.float32":
-        return FP32
-    raise ValueError(f"{name} is not supported: bfloat16 or float32")
+    try:
+        return _tt().types[t.dtype]
+    except KeyError:
+        raise ValueError(f"{t.dtype} is not supported: bfloat16 or float32") from None
 
 
-def _typed(want: str, **tensors) -> None:
+def _typed(want, **tensors) -> None:
     """Contiguous device tensors of one element type (None passes)."""
     for name, t in tensors.items():
-        if t is not None and (str(t.dtype) != want or not t.is_contiguous()):
+        if t is not None and (t.dtype != want or not t.is_contiguous()):
             raise ValueError(f"{name} must be contiguous and {want}")
 
 
@@ -409,24 +426,26 @@ def _heads(t, shape, dtype, name: str):
     """A [batch, tokens, heads, head_dim] tensor as the C ABI takes it (None: no heads)."""
     if t is None:
         return None
-    if tuple(t.shape) != shape or t.dtype != dtype:
-        raise ValueError(f"{name} is {tuple(t.shape)} {t.dtype}, not {shape} {dtype}")
-    s = t.stride()
-    if s[3] != 1 and shape[3] > 1:
+    if t.shape != shape or t.dtype != dtype:
+        raise ValueError(f"{name} is {tuple(t.shape)} {t.dtype}, not {tuple(shape)} {dtype}")
+    b, r, h, f = t.stride()
+    nb, nr, nh, n = shape
+    if f != 1 and n > 1:
         raise ValueError(f"the features of {name} must be contiguous")
     # The stride of an axis of one element means nothing; torch may give any.
-    n = shape[3]
-    return Heads(t.data_ptr(), *(s[i] if shape[i] > 1 else n for i in range(3)))
+    return Heads(t.data_ptr(), b if nb > 1 else n, r if nr > 1 else n, h if nh > 1 else n)
 
 
 def _qk_desc(q, k, cos, sin, q_gamma, k_gamma, positions, lens, eps, interleaved):
     x = q if q is not None else k
+    if x.dim() != 4:
+        raise ValueError(f"q and k must be [batch, tokens, heads, head_dim], not {tuple(x.shape)}")
     b, t, _, d = x.shape
     rot = 0 if cos is None else 2 * int(cos.shape[1])
     if (cos is None) != (sin is None) or (cos is not None and cos.shape != sin.shape):
         raise ValueError("cos and sin must be given together, of one shape")
-    _typed("torch.float32", cos=cos, sin=sin, q_gamma=q_gamma, k_gamma=k_gamma)
-    _typed("torch.int32", positions=positions, lens=lens)
+    _typed(_tt().f32, cos=cos, sin=sin, q_gamma=q_gamma, k_gamma=k_gamma)
+    _typed(_tt().i32, positions=positions, lens=lens)
     for name, g in (("q_gamma", q_gamma), ("k_gamma", k_gamma)):
         if g is not None and g.numel() != d:
             raise ValueError(f"{name} has {g.numel()} elements, not {d}")
@@ -472,8 +491,8 @@ def op_qk_norm_rotate_bwd(q, k, dq_out, dk_out, dq, dk, dq_gamma=None, dk_gamma=
     dq_gamma, dk_gamma: fp32 [head_dim] or None.  workspace: a uint8 device tensor of
     qk_norm_rotate_workspace() bytes where a weight gradient is asked for."""
     a = _qk_desc(q, k, cos, sin, q_gamma, k_gamma, positions, lens, eps, interleaved)
-    _typed("torch.float32", dq_gamma=dq_gamma, dk_gamma=dk_gamma)
-    _typed("torch.uint8", workspace=workspace)
+    _typed(_tt().f32, dq_gamma=dq_gamma, dk_gamma=dk_gamma)
+    _typed(_tt().u8, workspace=workspace)
     for name, g in (("dq_gamma", dq_gamma), ("dk_gamma", dk_gamma)):
         if g is not None and g.numel() != a.head_dim:
             raise ValueError(f"{name} has {g.numel()} elements, not {a.head_dim}")
@@ -491,7 +510,7 @@ def _window_desc(q, k, window, sinks, causal, scale, q_lens, k_lens):
     if q.dim() != 4 or k.dim() != 4 or q.shape[0] != k.shape[0] or q.shape[3] != k.shape[3]:
         raise ValueError(f"q {tuple(q.shape)} and k {tuple(k.shape)} do not go together")
     b, tq, h, d = q.shape
-    _typed("torch.int32", q_lens=q_lens, k_lens=k_lens)
+    _typed(_tt().i32, q_lens=q_lens, k_lens=k_lens)
     for name, n in (("q_lens", q_lens), ("k_lens", k_lens)):
         if n is not None and n.numel() != b:
             raise ValueError(f"{name} has {n.numel()} elements, not {b}")
@@ -519,11 +538,11 @@ def op_window_attention(q, k, v, o, window: int, sinks: int = 0, causal: bool = 
     workspace: a uint8 device tensor of window_attention_workspace() bytes."""
     a = _window_desc(q, k, window, sinks, causal, scale, q_lens, k_lens)
     _same_device(q, k, v, o, lse, q_lens, k_lens, workspace)
-    _typed("torch.float32", lse=lse)
-    _typed("torch.uint8", workspace=workspace)
+    _typed(_tt().f32, lse=lse)
+    _typed(_tt().u8, workspace=workspace)
     if lse is not None and lse.numel() != a.batch * a.heads * a.q_tokens:
         raise ValueError(f"lse has {lse.numel()} elements")
-    sq, sk = tuple(q.shape), tuple(k.shape)
+    sq, sk = q.shape, k.shape
     check(load_library().elasto_op_window_attention(
         a, _heads(q, sq, q.dtype, "q"), _heads(k, sk, q.dtype, "k"), _heads(v, sk, q.dtype, "v"),
         _heads(o, sq, q.dtype, "o"), _ptr(lse), _ptr(workspace),
@@ -537,11 +556,11 @@ def op_window_attention_bwd(q, k, v, o, lse, dout, dq, dk, dv, window: int, sink
     o and lse."""
     a = _window_desc(q, k, window, sinks, causal, scale, q_lens, k_lens)
     _same_device(q, k, v, o, lse, dout, dq, dk, dv, q_lens, k_lens, workspace)
-    _typed("torch.float32", lse=lse)
-    _typed("torch.uint8", workspace=workspace)
+    _typed(_tt().f32, lse=lse)
+    _typed(_tt().u8, workspace=workspace)
     if lse.numel() != a.batch * a.heads * a.q_tokens:
         raise ValueError(f"lse has {lse.numel()} elements")
-    sq, sk, dt = tuple(q.shape), tuple(k.shape), q.dtype
+    sq, sk, dt = q.shape, k.shape, q.dtype
     h = {n: _heads(t, s, dt, n) for n, t, s in (
         ("q", q, sq), ("k", k, sk), ("v", v, sk), ("o", o, sq), ("dout", dout, sq), ("dq", dq, sq),
         ("dk", dk, sk), ("dv", dv, sk))}
@@ -562,8 +581,8 @@ def op_top_logits(logits, values, indices, stream=None) -> None:
     """logits: bf16 or fp32 [rows, classes] device tensor (any row stride); values: fp32 and
     indices: int32, [rows, top]."""
     r, c, ld = _rows(logits, "logits")
-    _typed("torch.float32", values=values)
-    _typed("torch.int32", indices=indices)
+    _typed(_tt().f32, values=values)
+    _typed(_tt().i32, indices=indices)
     if values.dim() != 2 or values.shape != indices.shape or values.shape[0] != r:
         raise ValueError(f"values {tuple(values.shape)} and indices {tuple(indices.shape)} must be "
                          f"[{r}, top]")
@@ -581,8 +600,8 @@ def op_distill(logits, teacher_values, teacher_indices, loss, dlogits=None, labe
     or fp32 [rows, classes] or None; labels: int32 [rows] or None; row_weight: fp32 [rows] or
     None."""
     r, c, ld = _rows(logits, "logits")
-    _typed("torch.float32", teacher_values=teacher_values, loss=loss, row_weight=row_weight)
-    _typed("torch.int32", teacher_indices=teacher_indices, labels=labels)
+    _typed(_tt().f32, teacher_values=teacher_values, loss=loss, row_weight=row_weight)
+    _typed(_tt().i32, teacher_indices=teacher_indices, labels=labels)
     top = 0
     if teacher_values is not None:
         if (teacher_indices is None or teacher_values.dim() != 2 or teacher_values.shape[0] != r
@@ -633,8 +652,8 @@ class GrowthContext:
         (int32) are [batch, top] device tensors; labels may be None with alpha 1."""
         if not images.is_contiguous() or (labels is not None and not labels.is_contiguous()):
             raise ValueError("images and labels must be contiguous")
-        _typed("torch.float32", teacher_values=teacher_values)
-        _typed("torch.int32", teacher_indices=teacher_indices, labels=labels)
+        _typed(_tt().f32, teacher_values=teacher_values)
+        _typed(_tt().i32, teacher_indices=teacher_indices, labels=labels)
         n = int(images.shape[0])
         if teacher_values.dim() != 2 or teacher_values.shape != teacher_indices.shape or \
                 teacher_values.shape[0] != n or (labels is not None and labels.numel() != n):

@@ -41,7 +41,7 @@ def qk(lib, q=heads(), k=heads(), q_out=heads(), k_out=heads(), **kw):
 @pytest.mark.parametrize("kw", [
     dict(dtype=2), dict(batch=-1), dict(tokens=-1), dict(q_heads=0, kv_heads=0), dict(q_heads=-1),
     dict(head_dim=72), dict(head_dim=8), dict(head_dim=272), dict(rot_dim=8), dict(rot_dim=80),
-    dict(rot_dim=-16), dict(eps=0.0), dict(eps=math.nan), dict(eps=math.inf), dict(cos=None),
+    dict(rot_dim=-16), dict(eps=0.0), dict(eps=1e-39), dict(eps=math.nan), dict(eps=math.inf), dict(cos=None),
     dict(sin=None), dict(table_rows=0), dict(table_rows=7), dict(cos=P16 + 2),
     dict(positions=P16 + 2), dict(lens=P16 + 1), dict(q_gamma=P16 + 2),
     dict(batch=1 << 20, tokens=1 << 20)])
