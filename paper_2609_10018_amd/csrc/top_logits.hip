@@ -13,7 +13,9 @@
 //  3. the collected keys are sorted and the first `top` written.
 // The order of collecting does not matter to the result.
 //
-// Bound by memory: the second reading finds the row in the caches behind L2.
+// A thread keeps the largest value of each of its runs of eight, so the second
+// walk reads only runs that hold a key from the bound on again.  Bound by memory:
+// one pass over the logits.
 #include "layout.h"
 #include "logits.h"
 
@@ -63,8 +65,18 @@ __device__ __forceinline__ void block_sort(uint64_t* keys, int n, int tid) {
     }
 }
 
-template <typename T, int N>
-__global__ __launch_bounds__(N) void top_logits_kernel(const T* logits, int64_t ld, int C, int top,
+// The largest of eight values, NaN if there is one.
+__device__ __forceinline__ float top8(const float* v) {
+  float m = v[0];
+#pragma unroll
+  for (int e = 1; e < 8; ++e) m = __builtin_elementwise_maximum(m, v[e]);
+  return m;
+}
+
+// RUNS: runs of eight a thread, whose largest values it keeps for the second
+// walk; 0: more, which are all read again.
+template <typename T, int N, int RUNS>
+__global__ __launch_bounds__(N, (N == 1024 ? 8 : 2)) void top_logits_kernel(const T* logits, int64_t ld, int C, int top,
                                                        float* values, int32_t* indices) {
   __shared__ uint64_t held[kHold];
   __shared__ uint64_t bounds[N / 64];
@@ -73,22 +85,47 @@ __global__ __launch_bounds__(N) void top_logits_kernel(const T* logits, int64_t 
   const T* z = logits + (int64_t)blockIdx.x * ld;
   const RowSpan<T> span(z, C);
 
+  // The thread's largest key, or rather one that is no larger: of a run, its
+  // largest value at its last index.
+  uint64_t best = 0;  // less than any key
+  uint32_t most[RUNS > 0 ? RUNS : 1];  // order of each run's largest value
   uint32_t bo = 0;
   int bi = 0;
-  uint64_t best = 0;  // less than any key
-  walk_row<N>(z, span, tid,
-              [&](int i, const float* v) {
+  auto take = [&](uint32_t o, int last) {
+    bi = o > bo ? last : bi;
+    bo = o > bo ? o : bo;
+  };
+  if constexpr (RUNS > 0) {
+    constexpr int kBatch = RUNS < 4 ? RUNS : 4;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                  const uint32_t o = order_of(v[e]);
-                  bi = o > bo ? i + e : bi;
-                  bo = o > bo ? o : bo;
-                }
-              },
-              [&](int i, float v) {
-                const uint64_t k = key_of(order_of(v), i);
-                best = k > best ? k : best;
-              });
+    for (int r0 = 0; r0 < RUNS; r0 += kBatch) {
+      float v[kBatch][8];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int c = tid + (r0 + u) * N;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[u][e] = 0.0f;
+        if (c < span.runs) load8(z + span.run(c), v[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int c = tid + (r0 + u) * N;
+        most[r0 + u] = c < span.runs ? order_of(top8(v[u])) : 0;
+        take(most[r0 + u], span.run(c) + 7);
+      }
+      asm volatile("" ::: "memory");  // four loads in flight are enough, and their registers
+    }
+    for (int i = tid; i < span.singles; i += N) {
+      const uint64_t k = key_of(order_of(load1(z + span.single(i))), span.single(i));
+      best = k > best ? k : best;
+    }
+  } else {
+    walk_row<N>(z, span, tid, [&](int i, const float* v) { take(order_of(top8(v)), i + 7); },
+                [&](int i, float v) {
+                  const uint64_t k = key_of(order_of(v), i);
+                  best = k > best ? k : best;
+                });
+  }
   if (bo) {
     const uint64_t k = key_of(bo, bi);
     best = k > best ? k : best;
@@ -110,25 +147,35 @@ __global__ __launch_bounds__(N) void top_logits_kernel(const T* logits, int64_t 
       if (at < kHold) held[at] = k;
     };
     const uint32_t bh = (uint32_t)(bound >> 32);
-    walk_row<N>(z, span, tid,
-                [&](int i, const float* v) {
-                  uint32_t o[8], m = 0;
+    auto keep8 = [&](int i, const float* v) {
 #pragma unroll
-                  for (int e = 0; e < 8; ++e) {
-                    o[e] = order_of(v[e]);
-                    m = o[e] > m ? o[e] : m;
-                  }
-                  if (m < bh) return;
+      for (int e = 0; e < 8; ++e) {
+        const uint64_t k = key_of(order_of(v[e]), i + e);
+        if (k >= bound) keep(k);
+      }
+    };
+    auto keep1 = [&](int i, float v) {
+      const uint64_t k = key_of(order_of(v), i);
+      if (k >= bound) keep(k);
+    };
+    if constexpr (RUNS > 0) {
+      unsigned hits = 0;
 #pragma unroll
-                  for (int e = 0; e < 8; ++e) {
-                    const uint64_t k = key_of(o[e], i + e);
-                    if (k >= bound) keep(k);
-                  }
-                },
-                [&](int i, float v) {
-                  const uint64_t k = key_of(order_of(v), i);
-                  if (k >= bound) keep(k);
-                });
+      for (int r = 0; r < RUNS; ++r) hits |= most[r] >= bh && most[r] ? 1u << r : 0u;
+      for (; hits; hits &= hits - 1) {
+        const int i = span.run(tid + (__ffs((int)hits) - 1) * N);
+        float v[8];
+        load8(z + i, v);
+        keep8(i, v);
+      }
+      for (int i = tid; i < span.singles; i += N) keep1(span.single(i), load1(z + span.single(i)));
+    } else {
+      walk_row<N>(z, span, tid,
+                  [&](int i, const float* v) {
+                    if (order_of(top8(v)) >= bh) keep8(i, v);
+                  },
+                  keep1);
+    }
     __syncthreads();
     n = count;
     const int got = n < kHold ? n : kHold;
@@ -148,16 +195,27 @@ __global__ __launch_bounds__(N) void top_logits_kernel(const T* logits, int64_t 
   }
 }
 
+template <typename T, int N, int RUNS>
+void start(const T* z, int64_t ld, int64_t rows, int C, int top, float* values, int32_t* indices,
+           hipStream_t s) {
+  hipLaunchKernelGGL((top_logits_kernel<T, N, RUNS>), dim3((unsigned)rows), dim3(N), 0, s, z, ld, C, top,
+                     values, indices);
+}
+
 template <typename T>
 hipError_t launch(const void* logits, int64_t ld, int64_t rows, int C, int top, float* values,
                   int32_t* indices, hipStream_t s) {
   const T* z = static_cast<const T*>(logits);
-  if (C >= 8192)
-    hipLaunchKernelGGL((top_logits_kernel<T, 1024>), dim3((unsigned)rows), dim3(1024), 0, s, z, ld, C,
-                       top, values, indices);
+  if (C <= 2048 && top <= 64)  // a wave's 64 keys hold the bound themselves
+    start<T, 64, 4>(z, ld, rows, C, top, values, indices, s);
+  else if (C < 8192)
+    start<T, 256, 4>(z, ld, rows, C, top, values, indices, s);
+  else if (C <= 65536)
+    start<T, 1024, 8>(z, ld, rows, C, top, values, indices, s);
+  else if (C <= 131072)
+    start<T, 1024, 16>(z, ld, rows, C, top, values, indices, s);
   else
-    hipLaunchKernelGGL((top_logits_kernel<T, 256>), dim3((unsigned)rows), dim3(256), 0, s, z, ld, C,
-                       top, values, indices);
+    start<T, 1024, 0>(z, ld, rows, C, top, values, indices, s);
   return hipGetLastError();
 }
 

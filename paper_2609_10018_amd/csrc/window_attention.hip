@@ -48,7 +48,9 @@ struct Shape {
   static constexpr int kKeys = 32 * kSub;
   static constexpr int kTile = Tile<T, HD>::template bytes<kKeys>();  // of K (and of V)
   static constexpr int kPrivate = KEYS ? kWaves : 1;            // tiles held at once
-  static constexpr int kBuffers = kPrivate * kTile * 4 <= 140 * 1024 ? 2 : 1;
+  // fp32 waves with tiles of their own: one, which leaves room for two
+  // workgroups on a CU (2 x 1024 tokens x 6 heads of 64: 21 us, with two 26 us).
+  static constexpr int kBuffers = KEYS && sizeof(T) == 4 ? 1 : 2;
   static constexpr int kOs = HD + 4;  // floats of a row of the join
   static constexpr int kJoin = KEYS ? kWaves * 32 * kOs * 4 + kWaves * 64 * 4 : 0;
   static constexpr int kLds = std::max(kPrivate * kBuffers * 2 * kTile, kJoin);
@@ -380,7 +382,12 @@ Cut cut_of(const elasto_window_t& a) {
   constexpr int kCUs = 256;
   const int64_t pairs = (int64_t)a.batch * a.kv_heads, rows = (int64_t)a.q_tokens * (a.heads / a.kv_heads);
   Cut c;
-  c.keys = rows <= 32;
+  // fp32 products take 16 times as long a tile, so a launch of few workgroups
+  // wants its tiles shared out over waves: 2 x 1024 tokens x 6 heads of 64 (96
+  // workgroups of rows) 44 us by rows, 21 by keys; 2 x 4096 x 16 of 128 (1024)
+  // 643 and 714 us.  In bf16 the two are within 3 us of each other there, and by
+  // rows K and V are read a quarter as often.
+  c.keys = rows <= 32 || (a.dtype == ELASTO_FP32 && pairs * ((rows + 127) / 128) < 512);
   const int per = c.keys ? 32 : 128;
   c.row_blocks = (int)((rows + per - 1) / per);
   const int64_t blocks = pairs * c.row_blocks;
