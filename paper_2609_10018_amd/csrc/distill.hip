@@ -16,7 +16,8 @@
 // logits gathered before: each sums what all entries of its class take off (a
 // class may come twice), so no order of atomics enters.
 //
-// Bound by memory: the logits once, the gradient once.
+// Bound by memory: the logits once, the gradient once (2048 x 131072 bf16 with
+// its gradient: 247 us, 4.35 TB/s; a copy of that size runs at 5.1).
 #include <math.h>
 
 #include "distill.h"
@@ -46,16 +47,34 @@ struct DistillP {
   float tau, scale;
 };
 
-// A running maximum of x and sums of 2^(c (x - max)) for two factors c.
+// A running maximum m of x and sums of 2^(c x - c m) for two factors c: the
+// exponents as one multiply-add each, with the product c m rounded first (about).
+// That rounding is the same wherever the maximum is the same, so it cancels in
+// the quotients, and the logarithms of the sums are taken about the same number.
+__device__ __forceinline__ float about(float m, float c) {
+#pragma clang fp contract(off)  // rounded, whatever it is added to
+  const float r = -m * c;
+  return m == -INFINITY ? 0.0f : r;
+}
+__device__ __forceinline__ float power(float x, float c, float off) {
+  return __builtin_amdgcn_exp2f(fmaf(x, c, off));
+}
 struct Sums {
   float m, a, b;
 };
-__device__ __forceinline__ void merge(Sums& s, float m, float a, float b, float ca, float cb) {
-  const float t = fmaxf(s.m, m), base = t == -INFINITY ? 0.0f : t;
-  const float fs = s.m - base, fo = m - base;
-  s.a = s.a * __builtin_amdgcn_exp2f(fs * ca) + a * __builtin_amdgcn_exp2f(fo * ca);
-  s.b = s.b * __builtin_amdgcn_exp2f(fs * cb) + b * __builtin_amdgcn_exp2f(fo * cb);
+// Brings s to the maximum t (of at least s.m).
+__device__ __forceinline__ void move_to(Sums& s, float t, float ca, float cb) {
+#pragma clang fp contract(off)
+  s.a *= __builtin_amdgcn_exp2f(s.m == -INFINITY ? 0.0f : about(t, ca) - about(s.m, ca));
+  s.b *= __builtin_amdgcn_exp2f(s.m == -INFINITY ? 0.0f : about(t, cb) - about(s.m, cb));
   s.m = t;
+}
+__device__ __forceinline__ void merge(Sums& s, Sums o, float ca, float cb) {
+  const float t = fmaxf(s.m, o.m);
+  move_to(s, t, ca, cb);
+  move_to(o, t, ca, cb);
+  s.a += o.a;
+  s.b += o.b;
 }
 
 // TWO: the sums of both temperatures are needed and differ.
@@ -102,32 +121,34 @@ __global__ __launch_bounds__(N) void distill_kernel(DistillP<T, G> p) {
 
   // One walk: maximum and sums.
   Sums s = {-INFINITY, 0.0f, 0.0f};
-  auto add = [&](float x, float base) {
-    s.a += __builtin_amdgcn_exp2f((x - base) * ct);
-    if constexpr (TWO) s.b += __builtin_amdgcn_exp2f((x - base) * kLog2e);
-  };
+  float oa = 0.0f, ob = 0.0f;  // about(s.m)
   auto raise = [&](float t) {
     if (t > s.m) {
-      const float d = s.m - t;
-      s.a *= __builtin_amdgcn_exp2f(d * ct);
-      if constexpr (TWO) s.b *= __builtin_amdgcn_exp2f(d * kLog2e);
-      s.m = t;
+      move_to(s, t, ct, kLog2e);
+      oa = about(t, ct);
+      if constexpr (TWO) ob = about(t, kLog2e);
     }
-    return s.m == -INFINITY ? 0.0f : s.m;
+  };
+  auto add = [&](float x) {
+    s.a += power(x, ct, oa);
+    if constexpr (TWO) s.b += power(x, kLog2e, ob);
   };
   walk_row<N>(z, span, tid,
               [&](int, const float* v) {
                 float t = v[0];
 #pragma unroll
                 for (int e = 1; e < 8; ++e) t = fmaxf(t, v[e]);
-                const float base = raise(t);
+                raise(t);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) add(v[e], base);
+                for (int e = 0; e < 8; ++e) add(v[e]);
               },
-              [&](int, float v) { add(v, raise(v)); });
+              [&](int, float v) {
+                raise(v);
+                add(v);
+              });
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1)
-    merge(s, __shfl_xor(s.m, o, 64), __shfl_xor(s.a, o, 64), __shfl_xor(s.b, o, 64), ct, kLog2e);
+    merge(s, Sums{__shfl_xor(s.m, o, 64), __shfl_xor(s.a, o, 64), __shfl_xor(s.b, o, 64)}, ct, kLog2e);
   // The teacher's maximum goes along.
   const float tw = wave_max(tv);
   if (lane == 0) {
@@ -141,7 +162,7 @@ __global__ __launch_bounds__(N) void distill_kernel(DistillP<T, G> p) {
   float tm = red[0][3];
 #pragma unroll
   for (int i = 1; i < W; ++i) {
-    merge(s, red[i][0], red[i][1], red[i][2], ct, kLog2e);
+    merge(s, Sums{red[i][0], red[i][1], red[i][2]}, ct, kLog2e);
     tm = fmaxf(tm, red[i][3]);
   }
   __syncthreads();
@@ -158,15 +179,16 @@ __global__ __launch_bounds__(N) void distill_kernel(DistillP<T, G> p) {
   __syncthreads();
   const bool taught = p.alpha > 0.0f && tm > -INFINITY;  // the teacher gives the row something
   const float prob = taught ? te / tsum : 0.0f;
-  const float la = log2f(s.a) * kLn2, lb = log2f(s.b) * kLn2;  // of the sums about the maximum
+  oa = about(s.m, ct);
+  ob = about(s.m, kLog2e);
   float part = 0.0f;
   if (tid < p.top) {
     // log p - log q, each from differences to its own maximum.
     if (prob > 0.0f || prob != prob)
       part = p.alpha * p.tau * p.tau * prob *
-             ((tv - tm) - log2f(tsum) * kLn2 - ((zs - s.m) / p.tau - la));
+             ((tv - tm) - log2f(tsum) * kLn2 - (fmaf(zs, ct, oa) - log2f(s.a)) * kLn2);
   } else if (tid == p.top && p.beta > 0.0f) {
-    part = p.beta * (lb - (zs - s.m));
+    part = p.beta * (log2f(s.b) - fmaf(zs, kLog2e, ob)) * kLn2;
   }
   const float total = wave_sum(part);
   if (lane == 0) red[wave][0] = total;
@@ -182,22 +204,22 @@ __global__ __launch_bounds__(N) void distill_kernel(DistillP<T, G> p) {
   }
   if (!g) return;
 
-  // The gradient: fa 2^((z - m) ct) + fb 2^((z - m) log2 e), factors of both sums.
-  const float fa = taught ? p.alpha * p.tau / s.a : 0.0f;
-  const float fb = p.labels ? p.beta / s.b : 0.0f;
-  const float m = s.m;
+  // The gradient: both softmaxes with their weights in the factors.
+  const float fa = (taught ? p.alpha * p.tau / s.a : 0.0f) * w;
+  const float fb = (p.labels ? p.beta / s.b : 0.0f) * w;
+  const float f1 = fa + fb;
   auto value = [&](float x) {
     if constexpr (TWO)
-      return fmaf(fa, __builtin_amdgcn_exp2f((x - m) * ct), fb * __builtin_amdgcn_exp2f((x - m) * kLog2e));
+      return fmaf(fa, power(x, ct, oa), fb * power(x, kLog2e, ob));
     else
-      return (fa + fb) * __builtin_amdgcn_exp2f((x - m) * ct);
+      return f1 * power(x, ct, oa);
   };
   const bool wide = (reinterpret_cast<uintptr_t>(g + span.head) & 15) == 0;
   walk_row<N>(z, span, tid,
               [&](int i, const float* v) {
                 float o[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o[e] = value(v[e]) * w;
+                for (int e = 0; e < 8; ++e) o[e] = value(v[e]);
                 if (wide) {
                   store8(g + i, o);
                 } else {
@@ -205,7 +227,7 @@ __global__ __launch_bounds__(N) void distill_kernel(DistillP<T, G> p) {
                   for (int e = 0; e < 8; ++e) store1(g + i + e, o[e]);
                 }
               },
-              [&](int i, float v) { store1(g + i, value(v) * w); });
+              [&](int i, float v) { store1(g + i, value(v)); });
   __syncthreads();  // the special classes' values go over those
   if (tid <= p.top && cls >= 0) {
     float off = 0.0f;
@@ -215,7 +237,7 @@ __global__ __launch_bounds__(N) void distill_kernel(DistillP<T, G> p) {
         if (i < tid) first = false;
         off += amount[i];
       }
-    if (first) store1(g + cls, (value(zs) - off) * w);
+    if (first) store1(g + cls, fmaf(-off, w, value(zs)));
   }
 }
 
@@ -248,9 +270,19 @@ hipError_t launch(const DistillArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// More threads than teacher entries, one for the label among them; about one run
+// of eight a thread for short rows, of which many run at once (4096 x 1000 fp32:
+// 34 us with 512 threads, 19 with 256, 14 with 128); and all of a CU's for two
+// rows where the rows at work, read a second time for the gradient, would not
+// stay in the cache behind L2 (2048 x 131072 bf16: 257 us with 512 threads, 247
+// with 1024; 4096 x 32000: 122 and 190).  The loss alone takes as many, so that
+// its bits are the same.
 template <typename T, typename G>
 hipError_t launch_threads(const DistillArgs& a, hipStream_t s) {
-  return a.classes >= 8192 ? launch<T, G, 1024>(a, s) : launch<T, G, 512>(a, s);
+  if (a.classes <= 1024 && a.top < 128) return launch<T, G, 128>(a, s);
+  if (a.classes <= 2048 && a.top < 256) return launch<T, G, 256>(a, s);
+  if ((int64_t)a.classes * (int)sizeof(T) > 200 * 1024) return launch<T, G, 1024>(a, s);
+  return launch<T, G, 512>(a, s);
 }
 
 }  // namespace

@@ -22,13 +22,16 @@ __device__ __forceinline__ void load8(const float* p, float* v) {
 __device__ __forceinline__ float load1(const uint16_t* p) { return bf16_to_f32(*p); }
 __device__ __forceinline__ float load1(const float* p) { return *p; }
 
+// Past the caches: what is written is not read again here, and the row that is
+// read twice keeps its place in them.
 __device__ __forceinline__ void store8(uint16_t* p, const float* v) {
-  *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
-                                       pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+  const u32x4 w = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                   pack_bf16x2(v[6], v[7])};
+  __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p));
 }
 __device__ __forceinline__ void store8(float* p, const float* v) {
-  *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-  *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+  __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4*>(p));
+  __builtin_nontemporal_store(f32x4{v[4], v[5], v[6], v[7]}, reinterpret_cast<f32x4*>(p + 4));
 }
 __device__ __forceinline__ void store1(uint16_t* p, float v) { *p = f32_to_bf16(v); }
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
