@@ -374,13 +374,21 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   mine.hi = min(mine.hi, hi);
   const unsigned len = (unsigned)max(mine.hi - mine.lo + 1, 0);
   const int t_lo = lo / S::kRows, tiles = hi >= lo ? hi / S::kRows + 1 - t_lo : 0;
+  // The tiles are taken from the one whose number is a multiple of how many there
+  // are, and round: workgroups of neighbouring keys, whose rows are mostly the
+  // same, then read the same tile at the same time, out of the L2 that they share.
+  const int t_first = tiles > 0 ? (tiles - t_lo % tiles) % tiles : 0;
+  auto row0 = [&](int n) {
+    const int t = t_first + n;
+    return (t_lo + (t < tiles ? t : t - tiles)) * S::kRows;
+  };
 
   const char* qp = p.q.p + b * p.q.sb + (int64_t)hk * G * p.q.sh;
   const char* dp = p.dout.p + b * p.dout.sb + (int64_t)hk * G * p.dout.sh;
   const float2* stat = p.stat + bk * ((int64_t)p.q_tokens * G);
   constexpr int kBuf = 2 * S::kTile + S::kStat;
   auto stage = [&](int n, char* dst) {
-    const int r0 = (t_lo + n) * S::kRows;
+    const int r0 = row0(n);
     stage_rows<T, HD, S::kRows, kWaves>(p, dst, qp, p.q, r0, rows, wave, lane);
     stage_rows<T, HD, S::kRows, kWaves>(p, dst + S::kTile, dp, p.dout, r0, rows, wave, lane);
     // Every wave issues one, so that all count the same (waves 2 and 3 to the spare).
@@ -400,7 +408,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
     } else {
       wait_and_meet<0>();
     }
-    const int r0 = (t_lo + n) * S::kRows, r1 = r0 + S::kRows - 1;
+    const int r0 = row0(n), r1 = r0 + S::kRows - 1;
     ks.hold();
     if (!idle && r1 >= wlo && r0 <= whi)
       ks.template rows<S::kSub>(cur, cur + S::kTile, reinterpret_cast<const f32x4*>(cur + 2 * S::kTile),
