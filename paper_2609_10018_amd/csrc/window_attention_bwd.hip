@@ -48,6 +48,8 @@ struct BwdP {
   int parts, sink_groups;  // sink kernel (parts 0: none): parts of the rows, 32s of sinks
   float2* stat;            // [batch * kv_heads][row]: lse in base 2, D
   float* part;             // [batch * kv_heads][key kernel, parts][dk, dv][kMaxSinks][HD]
+  int row_parts;           // key kernel: parts of a tile's rows; more than one: their sums go to
+  float* row_part;         // [batch * kv_heads][row part][dk, dv][k_tokens][HD]
 };
 
 template <typename T, int HD>
@@ -318,17 +320,17 @@ __device__ __forceinline__ void stage_rows(const BwdP& p, char* dst, const char*
   const uint32_t st = (uint32_t)t.st, sh = (uint32_t)t.sh;
   // Where the rows of two loads are whole queries apart, one offset serves all
   // loads of every tile.
+  int ln = lane;  // nothing of this is to be kept in registers over the loop
+  asm volatile("" : "+v"(ln));
+  auto query = [&](unsigned r) { return __umulhi(r << 3, p.div_mul) >> p.div_shift; };
   if (WAVES == 4 && 4 * Tl::kBlockRows % G == 0 && r0 + ROWS <= rows) {
-    const int r = Ld::row(0, wave, lane), i = r / G;
-    const uint32_t first = (uint32_t)i * st + (uint32_t)(r - i * G) * sh;
-    const uint32_t next = (uint32_t)(4 * Tl::kBlockRows / G) * st;
-    Ld::issue(dst, wave, lane, from, [&](int l) { return first + (uint32_t)l * next; });
+    const unsigned r = (unsigned)Ld::row(0, wave, ln), i = query(r);
+    const uint32_t first = i * st + (r - i * (unsigned)G) * sh;
+    const uint32_t next = query(4 * Tl::kBlockRows) * st;
+    Ld::issue(dst, wave, ln, from, [&](int l) { return first + (uint32_t)l * next; });
   } else {
-    int ln = lane;  // nothing of this branch is to be kept in registers over the loop
-    asm volatile("" : "+v"(ln));
-    Ld::issue(dst, wave, lane, from, [&](int l) {
-      const unsigned r = (unsigned)min(r0 + Ld::row(l, wave, ln), rows - 1);
-      const unsigned i = __umulhi(r << 3, p.div_mul) >> p.div_shift;
+    Ld::issue(dst, wave, ln, from, [&](int l) {
+      const unsigned r = (unsigned)min(r0 + Ld::row(l, wave, ln), rows - 1), i = query(r);
       return (i - (uint32_t)i0) * st + (r - i * (unsigned)G) * sh;
     });
   }
@@ -348,8 +350,9 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t id = xcd_order(blockIdx.x, p.blocks);
-  const int64_t bk = id / p.key_tiles;
-  const int first = (int)(id - bk * p.key_tiles) * kKeys;
+  const int z = (int)(id % p.row_parts);
+  const int64_t rest = id / p.row_parts, bk = rest / p.key_tiles;
+  const int first = (int)(rest - bk * p.key_tiles) * kKeys;
   const int b = (int)(bk / p.kv_heads), hk = (int)(bk - (int64_t)b * p.kv_heads);
   const int ql = clamp_len(p.q_lens, b, p.q_tokens), kl = clamp_len(p.k_lens, b, p.k_tokens);
   const int G = p.group, rows = ql * G, shift = kl - ql;
@@ -401,8 +404,9 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   ks.load(p.k.p + b * p.k.sb + (int64_t)kc * p.k.st + hk * p.k.sh,
           p.v.p + b * p.v.sb + (int64_t)kc * p.v.st + hk * p.v.sh, h);
   // cur and next never overlap (as in window_dq_kernel).
+  const int zs = (int)((int64_t)tiles * z / p.row_parts), ze = (int)((int64_t)tiles * (z + 1) / p.row_parts);
   auto body = [&](int n, const char* __restrict__ cur, char* __restrict__ next) __attribute__((always_inline)) {
-    if (n + 1 < tiles) {
+    if (n + 1 < ze) {
       stage(n + 1, next);
       wait_and_meet<kLoads>();
     } else {
@@ -419,11 +423,16 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  if (tiles > 0) stage(0, smem);
+  if (zs < ze) stage(zs, smem);
   settle();
-  for (int n = 0; n < tiles; ++n) body(n, smem + (n & 1) * kBuf, smem + ((n + 1) & 1) * kBuf);
+  for (int n = zs; n < ze; ++n) body(n, smem + ((n - zs) & 1) * kBuf, smem + ((n + 1 - zs) & 1) * kBuf);
   if (key >= kl) return;
-  if (p.parts && key < p.mask.sinks) {
+  if (p.row_parts > 1) {
+    float* out = p.row_part + ((bk * p.row_parts + z) * 2 * p.k_tokens + key) * (int64_t)HD;
+    ks.store_part(out, out + (int64_t)p.k_tokens * HD, h);
+    return;
+  }
+  if (p.parts && key < p.mask.sinks) {  // the sink kernel's sums come to these
     float* out = p.part + ((bk * (p.parts + 1)) * 2 * kMaxSinks + key) * (int64_t)HD;
     ks.store_part(out, out + kMaxSinks * HD, h);
     return;
@@ -539,22 +548,31 @@ __global__ __launch_bounds__(kThreads, 1) void window_sink_kernel(BwdP p) {
   }
 }
 
-// The sinks' gradients: the parts' sums added up in order, four features a
+// The gradients of keys whose sums are in parts (all keys, or with a single
+// part of the rows the sinks): the parts added up in order, four features a
 // thread.
 template <typename T, int HD>
-__global__ __launch_bounds__(kThreads) void window_sink_join_kernel(BwdP p) {
+__global__ __launch_bounds__(kThreads) void window_key_join_kernel(BwdP p, int keys) {
   constexpr int kPer = HD / 4, kBlockKeys = kThreads / kPer;
-  const int64_t bk = blockIdx.x / (kMaxSinks / kBlockKeys);
-  const int key = (int)(blockIdx.x % (kMaxSinks / kBlockKeys)) * kBlockKeys + threadIdx.x / kPer;
+  const int blocks = (keys + kBlockKeys - 1) / kBlockKeys;
+  const int64_t bk = blockIdx.x / blocks;
+  const int key = (int)(blockIdx.x - bk * blocks) * kBlockKeys + threadIdx.x / kPer;
   const int c = (threadIdx.x % kPer) * 4;
   const int b = (int)(bk / p.kv_heads), hk = (int)(bk - (int64_t)b * p.kv_heads);
-  if (key >= min(p.mask.sinks, clamp_len(p.k_lens, b, p.k_tokens))) return;
+  if (key >= min(keys, clamp_len(p.k_lens, b, p.k_tokens))) return;
   f32x4 dk = {0.f, 0.f, 0.f, 0.f}, dv = dk;
-  const float* in = p.part + ((bk * (p.parts + 1)) * 2 * kMaxSinks + key) * (int64_t)HD + c;
+  auto add = [&](const float* in, int n, int64_t side) {
 #pragma unroll 4
-  for (int i = 0; i <= p.parts; ++i, in += 2 * kMaxSinks * HD) {
-    dk += *reinterpret_cast<const f32x4*>(in);
-    dv += *reinterpret_cast<const f32x4*>(in + kMaxSinks * HD);
+    for (int i = 0; i < n; ++i, in += 2 * side) {
+      dk += *reinterpret_cast<const f32x4*>(in);
+      dv += *reinterpret_cast<const f32x4*>(in + side);
+    }
+  };
+  const int64_t all = (int64_t)p.k_tokens * HD, few = (int64_t)kMaxSinks * HD, at = (int64_t)key * HD + c;
+  if (p.row_parts > 1) add(p.row_part + bk * p.row_parts * 2 * all + at, p.row_parts, all);
+  if (p.parts > 0 && key < p.mask.sinks) {
+    const int skip = p.row_parts > 1;  // the key kernel's own sums are then among the row parts
+    add(p.part + (bk * (p.parts + 1) + skip) * 2 * few + at, p.parts + 1 - skip, few);
   }
   T* ok = reinterpret_cast<T*>(p.dk.p + b * p.dk.sb + (int64_t)key * p.dk.st + hk * p.dk.sh);
   T* ov = reinterpret_cast<T*>(p.dv.p + b * p.dv.sb + (int64_t)key * p.dv.st + hk * p.dv.sh);
@@ -562,16 +580,39 @@ __global__ __launch_bounds__(kThreads) void window_sink_join_kernel(BwdP p) {
   store4(ov + c, dv[0], dv[1], dv[2], dv[3]);
 }
 
+// Rows that see some key of a tile through its window, at most.
+int64_t near_rows(const elasto_window_t& a) {
+  const int64_t G = a.heads / a.kv_heads, reach = a.causal ? (int64_t)a.window : 2 * (int64_t)a.window;
+  return std::min<int64_t>((int64_t)a.q_tokens * G, (kKeys + reach) * G);
+}
+
 // Parts of the rows that only the sinks are seen by, for launches in which they
 // are more than a tile of keys has otherwise (0: the first tile's workgroup
-// takes them along): about 256 workgroups, 512 rows or more each.
+// takes them along): about 256 workgroups, 128 rows or more each.
 int parts_of(const elasto_window_t& a) {
   const int64_t G = a.heads / a.kv_heads, rows = (int64_t)a.q_tokens * G;
   const int64_t near = (kKeys + (int64_t)a.window) * G;
   if (a.sinks == 0 || rows - near <= std::max<int64_t>(near / 2, 512)) return 0;
   const int64_t groups = (int64_t)a.batch * a.kv_heads * ((a.sinks + 31) / 32);
-  return (int)std::max<int64_t>(1, std::min<int64_t>({(rows - near) / 512, 256 / groups, 256}));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({(rows - near) / 128, 256 / groups, 256}));
 }
+
+// Parts of a tile's rows, where the tiles of keys would leave CUs idle (few
+// key heads): 512 workgroups (2 a CU), four tiles of rows or more each.
+int row_parts_of(const elasto_window_t& a) {
+  const int64_t blocks = (int64_t)a.batch * a.kv_heads * ((a.k_tokens + kKeys - 1) / kKeys);
+  const int64_t want = (512 + blocks - 1) / std::max<int64_t>(blocks, 1);
+  return (int)std::max<int64_t>(1, std::min<int64_t>({want, near_rows(a) / 256, 16}));
+}
+int64_t row_part_bytes(const elasto_window_t& a) {
+  const int n = row_parts_of(a);
+  return n > 1 ? (int64_t)a.batch * a.kv_heads * n * 2 * a.k_tokens * a.head_dim * 4 : 0;
+}
+int64_t part_bytes(const elasto_window_t& a) {
+  const int n = parts_of(a);
+  return n > 0 ? (int64_t)a.batch * a.kv_heads * (n + 1) * 2 * kMaxSinks * a.head_dim * 4 : 0;
+}
+int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 
 int64_t stat_bytes(const elasto_window_t& a) { return (int64_t)a.batch * a.heads * a.q_tokens * 8; }
 
@@ -592,22 +633,21 @@ hipError_t launch(BwdP p, int64_t pairs, hipStream_t s) {
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  p.blocks = pairs * p.key_tiles;
+  p.blocks = pairs * p.key_tiles * p.row_parts;
   hipLaunchKernelGGL((window_dkv_kernel<T, HD>), dim3((unsigned)p.blocks), dim3(kThreads),
                      (Shape<T, HD>::kLdsKey), s, p);
   e = hipGetLastError();
-  if (e != hipSuccess || p.parts == 0) return e;
-  hipLaunchKernelGGL((window_sink_join_kernel<T, HD>), dim3((unsigned)(pairs * (kMaxSinks * HD / 1024))),
-                     dim3(kThreads), 0, s, p);
+  if (e != hipSuccess || (p.parts == 0 && p.row_parts == 1)) return e;
+  const int keys = p.row_parts > 1 ? p.k_tokens : p.mask.sinks, per = 1024 / HD;
+  hipLaunchKernelGGL((window_key_join_kernel<T, HD>), dim3((unsigned)(pairs * ((keys + per - 1) / per))),
+                     dim3(kThreads), 0, s, p, keys);
   return hipGetLastError();
 }
 
 }  // namespace
 
 int64_t window_bwd_workspace(const elasto_window_t& a) {
-  const int parts = parts_of(a);
-  return (stat_bytes(a) + 255) / 256 * 256 +
-         (parts > 0 ? (int64_t)a.batch * a.kv_heads * (parts + 1) * 2 * kMaxSinks * a.head_dim * 4 : 0);
+  return up256(stat_bytes(a)) + up256(part_bytes(a)) + row_part_bytes(a);
 }
 
 hipError_t launch_window_bwd(const elasto_window_t& a, const WindowTensors& t, void* ws, hipStream_t s) {
@@ -633,9 +673,12 @@ hipError_t launch_window_bwd(const elasto_window_t& a, const WindowTensors& t, v
   p.key_tiles = (a.k_tokens + kKeys - 1) / kKeys;
   p.parts = parts_of(a);
   p.stat = static_cast<float2*>(ws);
-  p.part = reinterpret_cast<float*>(static_cast<char*>(ws) + (stat_bytes(a) + 255) / 256 * 256);
+  p.part = reinterpret_cast<float*>(static_cast<char*>(ws) + up256(stat_bytes(a)));
+  p.row_parts = row_parts_of(a);
+  p.row_part = reinterpret_cast<float*>(static_cast<char*>(ws) + up256(stat_bytes(a)) + up256(part_bytes(a)));
   p.sink_groups = (a.sinks + 31) / 32;
-  if (pairs * std::max({(int64_t)p.row_blocks, (int64_t)p.key_tiles, (int64_t)p.sink_groups * p.parts}) > 0x7fffffff) return hipErrorInvalidValue;
+  if (pairs * std::max({(int64_t)p.row_blocks, (int64_t)p.key_tiles * std::max(p.row_parts, kKeys * a.head_dim / 1024),
+                        (int64_t)p.sink_groups * p.parts}) > 0x7fffffff) return hipErrorInvalidValue;
   if (a.dtype == ELASTO_BF16)
     return a.head_dim == 64 ? launch<uint16_t, 64>(p, pairs, s) : launch<uint16_t, 128>(p, pairs, s);
   return a.head_dim == 64 ? launch<float, 64>(p, pairs, s) : launch<float, 128>(p, pairs, s);

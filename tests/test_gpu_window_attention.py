@@ -199,6 +199,9 @@ CASES = [
     dict(tq=65, b=3, k_lens=[65, 0, 32], d=128, window=10),
     dict(tq=1100, b=1, h=2, kv=2, window=90, sinks=4),          # sinks' rows in several parts
     dict(tq=1300, b=1, h=2, kv=1, window=33, sinks=7, causal=False),
+    dict(tq=700, b=1, h=8, kv=1, window=600, sinks=5, d=128),   # few key heads: rows in parts
+    dict(tq=1500, b=1, h=4, kv=1, window=100, sinks=40, d=128, k_lens=[1400], dtype=F32),
+    dict(tq=600, b=2, h=6, kv=1, causal=False, window=300, q_lens=[600, 77], k_lens=[500, 90]),
     dict(tq=1200, b=2, h=1, kv=1, window=50, sinks=64, dtype=F32, q_lens=[1200, 700],
          k_lens=[1200, 700]),
 ]
