@@ -153,8 +153,9 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   const int64_t id = xcd_order(blockIdx.x, p.blocks);
   const int z = (int)(id % p.splits);
   const int64_t rest = id / p.splits;
-  const int rb = (int)(rest % p.row_blocks);
   const int64_t bk = rest / p.row_blocks;
+  const int turn = (int)(rest - bk * p.row_blocks);
+  const int rb = p.mask.causal ? p.row_blocks - 1 - turn : turn;  // late rows, which have the most keys, first
   const int b = (int)(bk / p.kv_heads), hk = (int)(bk - (int64_t)b * p.kv_heads);
   const int ql = clamp_len(p.q_lens, b, p.q_tokens), kl = clamp_len(p.k_lens, b, p.k_tokens);
   const int G = p.group, rows = ql * G;

@@ -80,8 +80,9 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   const int lane = threadIdx.x & 63, h = lane >> 5, l32 = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t id = xcd_order(blockIdx.x, p.blocks);
-  const int rb = (int)(id % p.row_blocks);
   const int64_t bk = id / p.row_blocks;
+  const int turn = (int)(id - bk * p.row_blocks);
+  const int rb = p.mask.causal ? p.row_blocks - 1 - turn : turn;  // late rows, which have the most keys, first
   const int b = (int)(bk / p.kv_heads), hk = (int)(bk - (int64_t)b * p.kv_heads);
   const int ql = clamp_len(p.q_lens, b, p.q_tokens), kl = clamp_len(p.k_lens, b, p.k_tokens);
   const int G = p.group, rows = ql * G, shift = kl - ql;
@@ -352,7 +353,10 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   const int64_t id = xcd_order(blockIdx.x, p.blocks);
   const int z = (int)(id % p.row_parts);
   const int64_t rest = id / p.row_parts, bk = rest / p.key_tiles;
-  const int first = (int)(rest - bk * p.key_tiles) * kKeys;
+  // Causal: early keys have the most rows.  Every other sequence the other way
+  // round, so that a CU's two workgroups are not both of early ones.
+  const int turn = (int)(rest - bk * p.key_tiles);
+  const int first = ((bk & 1) ? p.key_tiles - 1 - turn : turn) * kKeys;
   const int b = (int)(bk / p.kv_heads), hk = (int)(bk - (int64_t)b * p.kv_heads);
   const int ql = clamp_len(p.q_lens, b, p.q_tokens), kl = clamp_len(p.k_lens, b, p.k_tokens);
   const int G = p.group, rows = ql * G, shift = kl - ql;
