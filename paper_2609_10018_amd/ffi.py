@@ -415,18 +415,22 @@ def _dtype(t) -> int:
         raise ValueError(f"{t.dtype} is not supported: bfloat16 or float32") from None
 
 
-def _typed(want, **tensors) -> None:
-    """Contiguous device tensors of one element type (None passes)."""
-    for name, t in tensors.items():
-        if t is not None and (t.dtype != want or not t.is_contiguous()):
-            raise ValueError(f"{name} must be contiguous and {want}")
+def _plain(t, want, name: str, numel: int = -1):
+    """The address of a contiguous device tensor of one element type (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not want or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous and {want}, not {t.dtype}")
+    if numel >= 0 and t.numel() != numel:
+        raise ValueError(f"{name} has {t.numel()} elements, not {numel}")
+    return t.data_ptr()
 
 
 def _heads(t, shape, dtype, name: str):
     """A [batch, tokens, heads, head_dim] tensor as the C ABI takes it (None: no heads)."""
     if t is None:
         return None
-    if t.shape != shape or t.dtype != dtype:
+    if t.shape != shape or t.dtype is not dtype:
         raise ValueError(f"{name} is {tuple(t.shape)} {t.dtype}, not {tuple(shape)} {dtype}")
     b, r, h, f = t.stride()
     nb, nr, nh, n = shape
@@ -436,35 +440,44 @@ def _heads(t, shape, dtype, name: str):
     return Heads(t.data_ptr(), b if nb > 1 else n, r if nr > 1 else n, h if nh > 1 else n)
 
 
+def _space(workspace):
+    """Address and bytes of a workspace (None: none)."""
+    if workspace is None:
+        return None, 0
+    return _plain(workspace, _tt().u8, "workspace"), workspace.numel()
+
+
 def _qk_desc(q, k, cos, sin, q_gamma, k_gamma, positions, lens, eps, interleaved):
+    """The description, and the shapes of q and of k."""
     x = q if q is not None else k
     if x.dim() != 4:
         raise ValueError(f"q and k must be [batch, tokens, heads, head_dim], not {tuple(x.shape)}")
-    b, t, _, d = x.shape
-    rot = 0 if cos is None else 2 * int(cos.shape[1])
+    tt = _tt()
+    shape = x.shape
+    b, t, n, d = shape
+    other = 0 if q is None or k is None else k.shape[2]
+    nq, nk = (0, n) if q is None else (n, other)
+    rot = rows = 0
+    if cos is not None:
+        rows, rot = cos.shape
+        rot *= 2
     if (cos is None) != (sin is None) or (cos is not None and cos.shape != sin.shape):
         raise ValueError("cos and sin must be given together, of one shape")
-    _typed(_tt().f32, cos=cos, sin=sin, q_gamma=q_gamma, k_gamma=k_gamma)
-    _typed(_tt().i32, positions=positions, lens=lens)
-    for name, g in (("q_gamma", q_gamma), ("k_gamma", k_gamma)):
-        if g is not None and g.numel() != d:
-            raise ValueError(f"{name} has {g.numel()} elements, not {d}")
-    if positions is not None and tuple(positions.shape) != (b, t):
+    if positions is not None and positions.shape != (b, t):
         raise ValueError(f"positions is {tuple(positions.shape)}, not {(b, t)}")
-    if lens is not None and lens.numel() != b:
-        raise ValueError(f"lens has {lens.numel()} elements, not {b}")
-    _same_device(q, k, cos, sin, q_gamma, k_gamma, positions, lens)
-    return QkNorm(_dtype(x), b, t, 0 if q is None else int(q.shape[2]),
-                  0 if k is None else int(k.shape[2]), d, rot, int(bool(interleaved)),
-                  0 if cos is None else int(cos.shape[0]), eps, _ptr(positions), _ptr(lens),
-                  _ptr(cos), _ptr(sin), _ptr(q_gamma), _ptr(k_gamma))
+    f32, i32 = tt.f32, tt.i32
+    a = QkNorm(_dtype(x), b, t, nq, nk, d, rot, 1 if interleaved else 0, rows, eps,
+               _plain(positions, i32, "positions"), _plain(lens, i32, "lens", b),
+               _plain(cos, f32, "cos"), _plain(sin, f32, "sin"),
+               _plain(q_gamma, f32, "q_gamma", d), _plain(k_gamma, f32, "k_gamma", d))
+    return a, (b, t, nq, d), (b, t, nk, d), x.dtype
 
 
 def qk_norm_rotate_workspace(q, k) -> int:
     """Workspace bytes of op_qk_norm_rotate_bwd for these q and k."""
     n = c_i64()
-    a = _qk_desc(q, k, None, None, None, None, None, None, 1.0, False)
-    check(load_library().elasto_qk_norm_rotate_workspace(ctypes.byref(a), ctypes.byref(n)))
+    a = _qk_desc(q, k, None, None, None, None, None, None, 1.0, False)[0]
+    check(load_library().elasto_qk_norm_rotate_workspace(a, ctypes.byref(n)))
     return n.value
 
 
@@ -475,12 +488,11 @@ def op_qk_norm_rotate(q, k, q_out, k_out, cos=None, sin=None, q_gamma=None, k_ga
     contiguous); k, k_out likewise with their own heads; either pair may be None.  cos, sin: fp32
     [rows, rot_dim / 2] (None: no rotation).  positions: int32 [batch, tokens]; lens: int32
     [batch]."""
-    a = _qk_desc(q, k, cos, sin, q_gamma, k_gamma, positions, lens, eps, interleaved)
-    _same_device(q_out, k_out)
-    h = [_heads(t, (a.batch, a.tokens, n, a.head_dim), (q if q is not None else k).dtype, name)
-         for t, n, name in ((q, a.q_heads, "q"), (k, a.kv_heads, "k"), (q_out, a.q_heads, "q_out"),
-                            (k_out, a.kv_heads, "k_out"))]
-    check(load_library().elasto_op_qk_norm_rotate(a, *h, _stream_ptr(stream)))
+    _same_device(q, k, q_out, k_out, cos, sin, q_gamma, k_gamma, positions, lens)
+    a, sq, sk, dt = _qk_desc(q, k, cos, sin, q_gamma, k_gamma, positions, lens, eps, interleaved)
+    check(load_library().elasto_op_qk_norm_rotate(
+        a, _heads(q, sq, dt, "q"), _heads(k, sk, dt, "k"), _heads(q_out, sq, dt, "q_out"),
+        _heads(k_out, sk, dt, "k_out"), _stream_ptr(stream)))
 
 
 def op_qk_norm_rotate_bwd(q, k, dq_out, dk_out, dq, dk, dq_gamma=None, dk_gamma=None,
@@ -490,33 +502,30 @@ def op_qk_norm_rotate_bwd(q, k, dq_out, dk_out, dq, dk, dq_gamma=None, dk_gamma=
     """dq_out, dk_out: the gradients of op_qk_norm_rotate's results; dq, dk: those of q and k;
     dq_gamma, dk_gamma: fp32 [head_dim] or None.  workspace: a uint8 device tensor of
     qk_norm_rotate_workspace() bytes where a weight gradient is asked for."""
-    a = _qk_desc(q, k, cos, sin, q_gamma, k_gamma, positions, lens, eps, interleaved)
-    _typed(_tt().f32, dq_gamma=dq_gamma, dk_gamma=dk_gamma)
-    _typed(_tt().u8, workspace=workspace)
-    for name, g in (("dq_gamma", dq_gamma), ("dk_gamma", dk_gamma)):
-        if g is not None and g.numel() != a.head_dim:
-            raise ValueError(f"{name} has {g.numel()} elements, not {a.head_dim}")
-    _same_device(dq_out, dk_out, dq, dk, dq_gamma, dk_gamma, workspace)
-    h = [_heads(t, (a.batch, a.tokens, n, a.head_dim), (q if q is not None else k).dtype, name)
-         for t, n, name in ((q, a.q_heads, "q"), (k, a.kv_heads, "k"),
-                            (dq_out, a.q_heads, "dq_out"), (dk_out, a.kv_heads, "dk_out"),
-                            (dq, a.q_heads, "dq"), (dk, a.kv_heads, "dk"))]
+    _same_device(q, k, dq_out, dk_out, dq, dk, dq_gamma, dk_gamma, workspace, cos, sin, q_gamma,
+                 k_gamma, positions, lens)
+    a, sq, sk, dt = _qk_desc(q, k, cos, sin, q_gamma, k_gamma, positions, lens, eps, interleaved)
+    f32 = _tt().f32
     check(load_library().elasto_op_qk_norm_rotate_bwd(
-        a, *h, _ptr(dq_gamma), _ptr(dk_gamma), _ptr(workspace),
-        0 if workspace is None else workspace.numel(), _stream_ptr(stream)))
+        a, _heads(q, sq, dt, "q"), _heads(k, sk, dt, "k"), _heads(dq_out, sq, dt, "dq_out"),
+        _heads(dk_out, sk, dt, "dk_out"), _heads(dq, sq, dt, "dq"), _heads(dk, sk, dt, "dk"),
+        _plain(dq_gamma, f32, "dq_gamma", sq[3]), _plain(dk_gamma, f32, "dk_gamma", sq[3]),
+        *_space(workspace), _stream_ptr(stream)))
 
 
 def _window_desc(q, k, window, sinks, causal, scale, q_lens, k_lens):
-    if q.dim() != 4 or k.dim() != 4 or q.shape[0] != k.shape[0] or q.shape[3] != k.shape[3]:
-        raise ValueError(f"q {tuple(q.shape)} and k {tuple(k.shape)} do not go together")
-    b, tq, h, d = q.shape
-    _typed(_tt().i32, q_lens=q_lens, k_lens=k_lens)
-    for name, n in (("q_lens", q_lens), ("k_lens", k_lens)):
-        if n is not None and n.numel() != b:
-            raise ValueError(f"{name} has {n.numel()} elements, not {b}")
-    return Window(_dtype(q), b, tq, int(k.shape[1]), h, int(k.shape[2]), d, int(bool(causal)),
-                  min(int(window), 2 ** 31 - 1), int(sinks),
-                  1.0 / math.sqrt(d) if scale is None else scale, _ptr(q_lens), _ptr(k_lens))
+    """The description, and the shapes of q and of k."""
+    sq, sk = q.shape, k.shape
+    if len(sq) != 4 or len(sk) != 4 or sq[0] != sk[0] or sq[3] != sk[3]:
+        raise ValueError(f"q {tuple(sq)} and k {tuple(sk)} do not go together")
+    b, tq, h, d = sq
+    i32 = _tt().i32
+    if scale is None:
+        scale = 1.0 / math.sqrt(d or 1)
+    a = Window(_dtype(q), b, tq, sk[1], h, sk[2], d, 1 if causal else 0,
+               min(int(window), 2 ** 31 - 1), int(sinks), scale,
+               _plain(q_lens, i32, "q_lens", b), _plain(k_lens, i32, "k_lens", b))
+    return a, sq, sk, q.dtype
 
 
 def window_attention_workspace(q, k, window: int, sinks: int = 0, causal: bool = True,
@@ -524,7 +533,7 @@ def window_attention_workspace(q, k, window: int, sinks: int = 0, causal: bool =
     """Workspace bytes of op_window_attention (backward: op_window_attention_bwd) for tensors of
     these shapes."""
     n = c_i64()
-    a = _window_desc(q, k, window, sinks, causal, None, None, None)
+    a = _window_desc(q, k, window, sinks, causal, None, None, None)[0]
     check(load_library().elasto_window_attention_workspace(a, int(bool(backward)), ctypes.byref(n)))
     return n.value
 
@@ -536,17 +545,12 @@ def op_window_attention(q, k, v, o, window: int, sinks: int = 0, causal: bool = 
     contiguous); k, v: [batch, k_tokens, kv_heads, head_dim].  lse: fp32 [batch, heads, q_tokens]
     or None.  q_lens, k_lens: int32 [batch] or None.  scale: None for 1 / sqrt(head_dim).
     workspace: a uint8 device tensor of window_attention_workspace() bytes."""
-    a = _window_desc(q, k, window, sinks, causal, scale, q_lens, k_lens)
     _same_device(q, k, v, o, lse, q_lens, k_lens, workspace)
-    _typed(_tt().f32, lse=lse)
-    _typed(_tt().u8, workspace=workspace)
-    if lse is not None and lse.numel() != a.batch * a.heads * a.q_tokens:
-        raise ValueError(f"lse has {lse.numel()} elements")
-    sq, sk = q.shape, k.shape
+    a, sq, sk, dt = _window_desc(q, k, window, sinks, causal, scale, q_lens, k_lens)
     check(load_library().elasto_op_window_attention(
-        a, _heads(q, sq, q.dtype, "q"), _heads(k, sk, q.dtype, "k"), _heads(v, sk, q.dtype, "v"),
-        _heads(o, sq, q.dtype, "o"), _ptr(lse), _ptr(workspace),
-        0 if workspace is None else workspace.numel(), _stream_ptr(stream)))
+        a, _heads(q, sq, dt, "q"), _heads(k, sk, dt, "k"), _heads(v, sk, dt, "v"),
+        _heads(o, sq, dt, "o"), _plain(lse, _tt().f32, "lse", sq[0] * sq[1] * sq[2]),
+        *_space(workspace), _stream_ptr(stream)))
 
 
 def op_window_attention_bwd(q, k, v, o, lse, dout, dq, dk, dv, window: int, sinks: int = 0,
@@ -554,42 +558,36 @@ def op_window_attention_bwd(q, k, v, o, lse, dout, dq, dk, dv, window: int, sink
                             k_lens=None, workspace=None, stream=None) -> None:
     """The gradients dq, dk, dv (shaped like q, k, v) from dout (like o), with op_window_attention's
     o and lse."""
-    a = _window_desc(q, k, window, sinks, causal, scale, q_lens, k_lens)
     _same_device(q, k, v, o, lse, dout, dq, dk, dv, q_lens, k_lens, workspace)
-    _typed(_tt().f32, lse=lse)
-    _typed(_tt().u8, workspace=workspace)
-    if lse.numel() != a.batch * a.heads * a.q_tokens:
-        raise ValueError(f"lse has {lse.numel()} elements")
-    sq, sk, dt = q.shape, k.shape, q.dtype
-    h = {n: _heads(t, s, dt, n) for n, t, s in (
-        ("q", q, sq), ("k", k, sk), ("v", v, sk), ("o", o, sq), ("dout", dout, sq), ("dq", dq, sq),
-        ("dk", dk, sk), ("dv", dv, sk))}
+    a, sq, sk, dt = _window_desc(q, k, window, sinks, causal, scale, q_lens, k_lens)
     check(load_library().elasto_op_window_attention_bwd(
-        a, h["q"], h["k"], h["v"], h["o"], _ptr(lse), h["dout"], h["dq"], h["dk"], h["dv"],
-        _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream_ptr(stream)))
+        a, _heads(q, sq, dt, "q"), _heads(k, sk, dt, "k"), _heads(v, sk, dt, "v"),
+        _heads(o, sq, dt, "o"), _plain(lse, _tt().f32, "lse", sq[0] * sq[1] * sq[2]),
+        _heads(dout, sq, dt, "dout"), _heads(dq, sq, dt, "dq"), _heads(dk, sk, dt, "dk"),
+        _heads(dv, sk, dt, "dv"), *_space(workspace), _stream_ptr(stream)))
 
 
 def _rows(t, name: str):
     """A [rows, classes] tensor with contiguous rows: (rows, classes, row stride)."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
         raise ValueError(f"{name} must be [rows, classes] with contiguous rows")
-    r, c = t.shape
-    return r, c, t.stride(0) if r > 1 else c
+    r, c = shape
+    return r, c, stride[0] if r > 1 else c
 
 
 def op_top_logits(logits, values, indices, stream=None) -> None:
     """logits: bf16 or fp32 [rows, classes] device tensor (any row stride); values: fp32 and
     indices: int32, [rows, top]."""
-    r, c, ld = _rows(logits, "logits")
-    _typed(_tt().f32, values=values)
-    _typed(_tt().i32, indices=indices)
-    if values.dim() != 2 or values.shape != indices.shape or values.shape[0] != r:
-        raise ValueError(f"values {tuple(values.shape)} and indices {tuple(indices.shape)} must be "
-                         f"[{r}, top]")
     _same_device(logits, values, indices)
-    check(load_library().elasto_op_top_logits(_dtype(logits), logits.data_ptr(), ld, r, c,
-                                              int(values.shape[1]), values.data_ptr(),
-                                              indices.data_ptr(), _stream_ptr(stream)))
+    r, c, ld = _rows(logits, "logits")
+    shape = values.shape
+    if len(shape) != 2 or shape != indices.shape or shape[0] != r:
+        raise ValueError(f"values {tuple(shape)} and indices {tuple(indices.shape)} must be "
+                         f"[{r}, top]")
+    check(load_library().elasto_op_top_logits(
+        _dtype(logits), logits.data_ptr(), ld, r, c, shape[1], _plain(values, _tt().f32, "values"),
+        _plain(indices, _tt().i32, "indices"), _stream_ptr(stream)))
 
 
 def op_distill(logits, teacher_values, teacher_indices, loss, dlogits=None, labels=None,
@@ -599,29 +597,28 @@ def op_distill(logits, teacher_values, teacher_indices, loss, dlogits=None, labe
     and teacher_indices: int32, [rows, top] (None with alpha 0); loss: fp32 [rows]; dlogits: bf16
     or fp32 [rows, classes] or None; labels: int32 [rows] or None; row_weight: fp32 [rows] or
     None."""
+    _same_device(logits, teacher_values, teacher_indices, loss, dlogits, labels, row_weight)
     r, c, ld = _rows(logits, "logits")
-    _typed(_tt().f32, teacher_values=teacher_values, loss=loss, row_weight=row_weight)
-    _typed(_tt().i32, teacher_indices=teacher_indices, labels=labels)
     top = 0
     if teacher_values is not None:
-        if (teacher_indices is None or teacher_values.dim() != 2 or teacher_values.shape[0] != r
-                or teacher_values.shape != teacher_indices.shape):
+        shape = teacher_values.shape
+        if (teacher_indices is None or len(shape) != 2 or shape[0] != r
+                or shape != teacher_indices.shape):
             raise ValueError(f"teacher values and indices must both be [{r}, top]")
-        top = int(teacher_values.shape[1])
-    for name, t in (("loss", loss), ("labels", labels), ("row_weight", row_weight)):
-        if t is not None and t.numel() != r:
-            raise ValueError(f"{name} has {t.numel()} elements, not {r}")
-    gd, ldg = _dtype(logits), ld
+        top = shape[1]
+    dt = gd = _dtype(logits)
+    ldg, grad = ld, None
     if dlogits is not None:
         rg, cg, ldg = _rows(dlogits, "dlogits")
         if (rg, cg) != (r, c):
             raise ValueError(f"dlogits is {(rg, cg)}, not {(r, c)}")
-        gd = _dtype(dlogits)
-    _same_device(logits, teacher_values, teacher_indices, loss, dlogits, labels, row_weight)
+        gd, grad = _dtype(dlogits), dlogits.data_ptr()
+    f32, i32 = _tt().f32, _tt().i32
     check(load_library().elasto_op_distill(
-        _dtype(logits), logits.data_ptr(), ld, r, c, _ptr(teacher_values), _ptr(teacher_indices),
-        top, _ptr(labels), _ptr(row_weight), float(temperature), float(alpha), float(scale),
-        loss.data_ptr(), gd, _ptr(dlogits), ldg, _stream_ptr(stream)))
+        dt, logits.data_ptr(), ld, r, c, _plain(teacher_values, f32, "teacher_values"),
+        _plain(teacher_indices, i32, "teacher_indices"), top, _plain(labels, i32, "labels", r),
+        _plain(row_weight, f32, "row_weight", r), temperature, alpha, scale,
+        _plain(loss, f32, "loss", r), gd, grad, ldg, _stream_ptr(stream)))
 
 
 class GrowthContext:
@@ -652,16 +649,17 @@ class GrowthContext:
         (int32) are [batch, top] device tensors; labels may be None with alpha 1."""
         if not images.is_contiguous() or (labels is not None and not labels.is_contiguous()):
             raise ValueError("images and labels must be contiguous")
-        _typed(_tt().f32, teacher_values=teacher_values)
-        _typed(_tt().i32, teacher_indices=teacher_indices, labels=labels)
         n = int(images.shape[0])
         if teacher_values.dim() != 2 or teacher_values.shape != teacher_indices.shape or \
-                teacher_values.shape[0] != n or (labels is not None and labels.numel() != n):
-            raise ValueError(f"teacher values and indices must be [{n}, top], labels [{n}]")
+                teacher_values.shape[0] != n:
+            raise ValueError(f"teacher values and indices must be [{n}, top]")
+        _same_device(images, labels, teacher_values, teacher_indices, stats)
         check(self.lib.elasto_growth_step_distill(
-            self.g, int(mode), images.data_ptr(), _ptr(labels), teacher_values.data_ptr(),
-            teacher_indices.data_ptr(), int(teacher_values.shape[1]), float(temperature),
-            float(alpha), n, float(lr), float(clip), _ptr(stats), _stream_ptr(stream)))
+            self.g, int(mode), images.data_ptr(), _plain(labels, _tt().i32, "labels", n),
+            _plain(teacher_values, _tt().f32, "teacher_values"),
+            _plain(teacher_indices, _tt().i32, "teacher_indices"), int(teacher_values.shape[1]),
+            float(temperature), float(alpha), n, float(lr), float(clip), _ptr(stats),
+            _stream_ptr(stream)))
 
     def read(self, which: int) -> np.ndarray:
         """which 0: packed weights (uint8); 1: fp32 masters (float32, one per bf16 element)."""
