@@ -506,17 +506,20 @@ elasto_status_t elasto_qk_norm_rotate_workspace(const elasto_qk_norm_t* desc, in
  *   o_i = sum_j softmax_j(scale q_i . k_j) v_j,
  *   lse_i = log sum_j exp(scale q_i . k_j)   (fp32 [batch][heads][q_tokens]).
  * A query that sees no key gets o = 0 and lse = -infinity.  Query head h reads
- * key head h / (heads / kv_heads).  What lies behind a sequence's lengths is
- * neither used (it may be anything, NaN included) nor written.
+ * key head h / (heads / kv_heads).  What lies behind a sequence's lengths, and
+ * keys and values that none of its queries sees (before the window of the first
+ * one, say), are not used: they may be anything, NaN included.  Nothing is
+ * written behind the lengths, and such keys get zero gradients.  (An infinity or NaN in a row
+ * that some see may also reach others of its sequence that do not.)
  * BF16: products of bf16 with fp32 sums, softmax statistics in fp32, the
  * probabilities (backward: also the gradients of the scores) rounded to bf16
  * for the products that sum them.  FP32: fp32 throughout.  Results are the
  * same bits every time.
  * Needs head_dim 64 or 128, heads a multiple of kv_heads, window >= 1,
- * 0 <= sinks <= 64, scale > 0; k_tokens, q_tokens * heads / kv_heads and
+ * 0 <= sinks <= 64, scale in [1e-30, 1e30]; k_tokens, q_tokens * heads / kv_heads and
  * batch * heads at most 2^29; 64 tokens of a head of k and of v (backward: of
  * the heads / kv_heads heads of q and of dout that share a key head) within
- * 4 GiB. */
+ * 4 GiB less 4 KB. */
 typedef struct {
   int32_t dtype, batch, q_tokens, k_tokens, heads, kv_heads, head_dim;
   int32_t causal, window, sinks;

@@ -113,33 +113,50 @@ __device__ __forceinline__ void zero(f32x16& v) {
   for (int i = 0; i < 16; ++i) v[i] = 0.0f;
 }
 
-// `bytes` bytes at p as a buffer (at most 4 GiB - 1 of them).
+// Keys that some of the rows between two positions see (their keys_of: a0, a1):
+// [0, last] without [gap0, gap1).
+struct SeenKeys {
+  int last, gap0, gap1;
+  __device__ __forceinline__ SeenKeys(const Keys& a0, const Keys& a1)
+      : last(max(a1.hs, a1.hi)), gap0(max(a1.hs + 1, 0)), gap1(a0.lo) {}
+};
+
+// `bytes` bytes at p as a buffer (at most kReach of them; an offset of kReach
+// lies outside, as do the row's bytes that follow it).
+constexpr uint32_t kReach = 0xfffff000u;
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const char* p, int64_t bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), (short)0,
-                                           (int)(uint32_t)(bytes < 0xffffffffll ? bytes : 0xffffffffll),
+                                           (int)(bytes < (int64_t)kReach ? (uint32_t)bytes : kReach),
                                            kRsrcWord3);
 }
 
-// One head of k or v of one sequence: rows st bytes apart.
+// One head of k or v of one sequence: rows st bytes apart.  Keys that none of
+// the workgroup's rows sees arrive as zeros: what their memory holds (pages that
+// a cache has given up, say) never meets a product.
 struct KeyRows {
   const char* p;
   int64_t st;
-  int last;                    // of the sequence
+  SeenKeys seen;
   bool near;                   // all of it within 32-bit offsets: one buffer for every tile
   __amdgpu_buffer_rsrc_t all;
-  __device__ __forceinline__ KeyRows(const char* base, int64_t stride, int kl, int row_bytes)
-      : p(base), st(stride), last(kl - 1) {
-    const int64_t bytes = (int64_t)max(last, 0) * st + row_bytes;
+  __device__ __forceinline__ KeyRows(const char* base, int64_t stride, const SeenKeys& keys, int row_bytes)
+      : p(base), st(stride), seen(keys) {
+    const int64_t bytes = (int64_t)max(seen.last, 0) * st + row_bytes;
     near = bytes < ((int64_t)1 << 31);
     all = buffer_of(p, bytes);
   }
   // The tile that starts at row j0, to LDS.
   template <typename L>
   __device__ __forceinline__ void issue(char* tile, int wave, int lane, int j0, int row_bytes) const {
-    if (near)
+    if (j0 < seen.gap1 && j0 + L::kTileRows > seen.gap0)
+      L::issue(tile, wave, lane, buffer_of(p + j0 * st, (seen.last - j0) * st + row_bytes), [&](int i) {
+        const int r = L::row(i, wave, lane), key = j0 + r;
+        return key >= seen.gap0 && key < seen.gap1 ? kReach : (uint32_t)r * (uint32_t)st;
+      });
+    else if (near)
       L::issue(tile, wave, lane, all, (uint32_t)j0 * (uint32_t)st, (uint32_t)st);
     else
-      L::issue(tile, wave, lane, buffer_of(p + j0 * st, (last - j0) * st + row_bytes), 0, (uint32_t)st);
+      L::issue(tile, wave, lane, buffer_of(p + j0 * st, (seen.last - j0) * st + row_bytes), 0, (uint32_t)st);
   }
 };
 
@@ -228,6 +245,7 @@ struct Tile {
   // Loads of ROWS rows straight to LDS, the blocks shared out over WAVES waves.
   template <int ROWS, int WAVES>
   struct Loads {
+    static constexpr int kTileRows = ROWS;
     static constexpr int kLoads = ROWS / kBlockRows / WAVES;
     static_assert(ROWS % (kBlockRows * WAVES) == 0 && (WAVES == 1 || WAVES == 4), "whole blocks a wave");
     // Row of the tile that a lane loads from at load i, and its piece there.

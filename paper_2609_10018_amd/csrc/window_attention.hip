@@ -181,10 +181,9 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   const int zs = (int)((int64_t)tiles * z / p.splits), ze = (int)((int64_t)tiles * (z + 1) / p.splits);
   auto key0 = [&](int n) { return (n < sink_tiles ? n : t0 + n - sink_tiles) * S::kKeys; };
 
-  const KeyRows kr(p.k.p + b * p.k.sb + hk * p.k.sh, p.k.st, kl, Tl::kRow);
-  const KeyRows vr(p.v.p + b * p.v.sb + hk * p.v.sh, p.v.st, kl, Tl::kRow);
-  // Keys past the last one arrive as zeros: they are masked, and what the
-  // memory holds there is not read.
+  const SeenKeys seen(a0, a1);
+  const KeyRows kr(p.k.p + b * p.k.sb + hk * p.k.sh, p.k.st, seen, Tl::kRow);
+  const KeyRows vr(p.v.p + b * p.v.sb + hk * p.v.sh, p.v.st, seen, Tl::kRow);
   using Ld = typename Tl::template Loads<S::kKeys, KEYS ? 1 : kWaves>;
   const int lw = KEYS ? 0 : wave;
   auto stage = [&](int n, char* dst) {

@@ -102,8 +102,9 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   const int t0 = max(a0.lo / S::kRows, sink_tiles);
   const int tiles = sink_tiles + (a1.hi >= a0.lo ? max(a1.hi / S::kRows + 1 - t0, 0) : 0);
   auto key0 = [&](int n) { return (n < sink_tiles ? n : t0 + n - sink_tiles) * S::kRows; };
-  const KeyRows kr(p.k.p + b * p.k.sb + hk * p.k.sh, p.k.st, kl, Tl::kRow);
-  const KeyRows vr(p.v.p + b * p.v.sb + hk * p.v.sh, p.v.st, kl, Tl::kRow);
+  const SeenKeys seen(a0, a1);
+  const KeyRows kr(p.k.p + b * p.k.sb + hk * p.k.sh, p.k.st, seen, Tl::kRow);
+  const KeyRows vr(p.v.p + b * p.v.sb + hk * p.v.sh, p.v.st, seen, Tl::kRow);
   using Ld = typename Tl::template Loads<S::kRows, kWaves>;
   auto stage = [&](int n, char* dst) {
     kr.template issue<Ld>(dst, wave, lane, key0(n), Tl::kRow);
@@ -228,11 +229,17 @@ struct KeySide {
   Frag<T> k[HD / 16], v[HD / 16];
   f32x16 dk[HD / 32], dv[HD / 32];
 
-  __device__ __forceinline__ void load(const char* krow, const char* vrow, int h) {
+  // seen: by any row (what the memory of another key holds meets no product).
+  __device__ __forceinline__ void load(const char* krow, const char* vrow, int h, bool seen) {
 #pragma unroll
     for (int kk = 0; kk < HD / 16; ++kk) {
-      load_operand(krow, kk, h, k[kk]);
-      load_operand(vrow, kk, h, v[kk]);
+      if (seen) {
+        load_operand(krow, kk, h, k[kk]);
+        load_operand(vrow, kk, h, v[kk]);
+      } else {
+        k[kk] = Frag<T>{};
+        v[kk] = Frag<T>{};
+      }
     }
 #pragma unroll
     for (int n = 0; n < HD / 32; ++n) {
@@ -406,7 +413,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   const typename Tl::Reader rd(lane);
   KeySide<T, HD> ks;
   ks.load(p.k.p + b * p.k.sb + (int64_t)kc * p.k.st + hk * p.k.sh,
-          p.v.p + b * p.v.sb + (int64_t)kc * p.v.st + hk * p.v.sh, h);
+          p.v.p + b * p.v.sb + (int64_t)kc * p.v.st + hk * p.v.sh, h, len > 0);
   // cur and next never overlap (as in window_dq_kernel).
   const int zs = (int)((int64_t)tiles * z / p.row_parts), ze = (int)((int64_t)tiles * (z + 1) / p.row_parts);
   auto body = [&](int n, const char* __restrict__ cur, char* __restrict__ next) __attribute__((always_inline)) {
@@ -492,10 +499,10 @@ __global__ __launch_bounds__(kThreads, 1) void window_sink_kernel(BwdP p) {
   };
   constexpr int kLoads = 2 * Tl::template Loads<32, 1>::kLoads + 1;
   const typename Tl::Reader rd(lane);
+  const bool seen = key < sinks;
   KeySide<T, HD> ks;
   ks.load(p.k.p + b * p.k.sb + (int64_t)kc * p.k.st + hk * p.k.sh,
-          p.v.p + b * p.v.sb + (int64_t)kc * p.v.st + hk * p.v.sh, h);
-  const bool seen = key < sinks;
+          p.v.p + b * p.v.sb + (int64_t)kc * p.v.st + hk * p.v.sh, h, seen);
   auto compute = [&](int n, const char* cur) {
     ks.hold();
     const int left = far - n * 32;

@@ -24,8 +24,8 @@ bool check_desc(const elasto_window_t* d, elasto_window_t* a) {
   if (a->window < 1) return fail(ELASTO_ERR_INVALID_ARG, "window %d is below 1", a->window), false;
   if (a->sinks < 0 || a->sinks > kMaxSinks)
     return fail(ELASTO_ERR_INVALID_ARG, "sinks %d outside [0, %d]", a->sinks, kMaxSinks), false;
-  if (!(a->scale > 0.0f) || !(a->scale < INFINITY))
-    return fail(ELASTO_ERR_INVALID_ARG, "window attention: scale must be positive and finite"), false;
+  if (!(a->scale >= 1e-30f) || !(a->scale <= 1e30f))
+    return fail(ELASTO_ERR_INVALID_ARG, "window attention: scale must be positive, within [1e-30, 1e30]"), false;
   if (!aligned(a->q_lens, 4) || !aligned(a->k_lens, 4))
     return fail(ELASTO_ERR_INVALID_ARG, "window attention: misaligned lengths"), false;
   // No distance between a query and a key of one sequence reaches 2^30.
@@ -43,9 +43,9 @@ bool set_view(const char* name, const elasto_window_t& a, const elasto_heads_t* 
 // Tiles of up to 64 tokens (of `heads` heads together) are loaded at 32-bit
 // offsets from their first row.
 bool check_reach(const char* name, const View& v, int heads) {
-  const int64_t limit = (int64_t)1 << 32;
+  const int64_t limit = kReach;
   if (v.st > limit || v.sh > limit || 64 * v.st + (heads - 1) * v.sh + 512 >= limit)
-    return fail(ELASTO_ERR_INVALID_ARG, "window attention: 64 tokens of %s span 4 GiB or more", name), false;
+    return fail(ELASTO_ERR_INVALID_ARG, "window attention: 64 tokens of %s span nearly 4 GiB or more", name), false;
   return true;
 }
 

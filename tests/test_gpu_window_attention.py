@@ -407,3 +407,36 @@ def test_gradients_of_large_and_odd_groups():
         o, lse = c.exact_forward()
         c.check_backward(o, *c.backward(o, lse))
         c.check_forward(*c.forward())
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("tq,tk,window,sinks,causal,k_lens", [
+    (1, 700, 100, 4, True, [700, 333]),     # one new token: a window and sinks in a cache
+    (1, 700, 64, 0, True, [700, 50]),
+    (37, 900, 70, 40, True, [900, 411]),    # the window of the first query starts inside a tile
+    (37, 900, 70, 33, False, [850, 200]),
+    (5, 40, 3, 1, False, [40, 7]),
+    (260, 1000, 130, 64, True, [1000, 300]),
+])
+def test_keys_that_no_query_sees(dtype, d, tq, tk, window, sinks, causal, k_lens):
+    """NaN in keys and values that no query of the sequence sees changes no bit."""
+    c = Case(dtype=dtype, tq=tq, tk=tk, h=6, kv=2, d=d, window=window, sinks=sinks, causal=causal,
+             k_lens=k_lens, layout="heads")
+    hidden = [torch.ones(tk, dtype=torch.bool) for _ in range(2)]
+    for b in range(2):
+        hidden[b][:c.kl[b]] = ~c.mask(b).any(0)
+        assert hidden[b].any() and not hidden[b].all()
+    results = []
+    for value in (0.0, math.nan, math.inf):
+        for b in range(2):
+            at = torch.nonzero(hidden[b])[:, 0].cuda()
+            c.k[b, at], c.v[b, at] = value, value
+        o, lse = c.forward()
+        results.append((o, lse, *c.backward(o, lse)))
+    for got in results[1:]:
+        for x, y in zip(results[0], got):
+            assert torch.equal(x, y)
+    assert all(bool(torch.isfinite(x).all()) for x in results[0])
+    for b in range(2):
+        at = torch.nonzero(hidden[b][:c.kl[b]])[:, 0].cuda()
+        assert not results[0][3][b, at].any() and not results[0][4][b, at].any()

@@ -116,7 +116,7 @@ def attn_bwd(lib, lse=P16, ws=P16, size=BIG, desc=None, **kw):
     dict(dtype=7), dict(head_dim=32), dict(head_dim=96), dict(batch=-1), dict(q_tokens=-1),
     dict(k_tokens=-1), dict(heads=0), dict(kv_heads=0), dict(kv_heads=5), dict(window=0),
     dict(window=-3), dict(sinks=-1), dict(sinks=65), dict(scale=0.0), dict(scale=-1.0),
-    dict(scale=math.nan), dict(scale=math.inf), dict(q_lens=P16 + 2), dict(k_lens=P16 + 1),
+    dict(scale=math.nan), dict(scale=math.inf), dict(scale=1e-31), dict(scale=1e31), dict(q_lens=P16 + 2), dict(k_lens=P16 + 1),
     dict(k_tokens=(1 << 29) + 1), dict(q_tokens=1 << 29), dict(batch=1 << 28), dict(lse=P16 + 2)])
 def test_window_attention_refuses_bad_descriptions(lib, kw):
     assert attn(lib, **kw) == INVALID
