@@ -464,8 +464,8 @@ typedef struct {
  * once; FP32: fp32 throughout.
  * Needs head_dim a multiple of 16 in [16, 256], rot_dim a multiple of 16 in
  * [0, head_dim], eps > 0 (and not subnormal), batch, tokens, q_heads and
- * kv_heads >= 0 with at least one head (a side of no heads takes NULL tensors),
- * batch * tokens below 2^31. */
+ * kv_heads >= 0 with at least one head and at most 65536 (a side of no heads
+ * takes NULL tensors), batch * tokens at most 2^25. */
 typedef struct {
   int32_t dtype, batch, tokens, q_heads, kv_heads, head_dim;
   int32_t rot_dim, interleaved, table_rows;
@@ -576,7 +576,7 @@ elasto_status_t elasto_op_top_logits(int32_t dtype, const void* logits, int64_t 
  * labels may be NULL with alpha = 1; with alpha = 0 top may be 0 and the call
  * is the cross-entropy.  dlogits may be logits itself (same type and stride).
  * fp32 between load and store, sums in fp32 in a fixed order.  Needs top <=
- * 256, temperature > 0, alpha in [0, 1], scale finite, classes <= 2^30. */
+ * 256, temperature in [1e-6, 1e6], alpha in [0, 1], scale finite, classes <= 2^30. */
 elasto_status_t elasto_op_distill(int32_t dtype, const void* logits, int64_t ld, int64_t rows,
                                   int32_t classes, const float* teacher_values,
                                   const int32_t* teacher_indices, int32_t top,

@@ -20,6 +20,8 @@
 // its gradient: 247 us, 4.35 TB/s; a copy of that size runs at 5.1).
 #include <math.h>
 
+#include <algorithm>
+
 #include "distill.h"
 #include "growth_step.h"
 #include "heads.h"
@@ -41,32 +43,49 @@ struct DistillP {
   const float* weight;
   float* loss;
   G* grad;  // NULL: the loss alone
-  int64_t ldg;
+  int64_t ldg, row0;
   int C, top;
   float alpha, beta;  // of the teacher's and of the labels' part
   float tau, scale;
 };
 
 // A running maximum m of x and sums of 2^(c x - c m) for two factors c: the
-// exponents as one multiply-add each, with the product c m rounded first (about).
-// That rounding is the same wherever the maximum is the same, so it cancels in
-// the quotients, and the logarithms of the sums are taken about the same number.
-__device__ __forceinline__ float about(float m, float c) {
-#pragma clang fp contract(off)  // rounded, whatever it is added to
-  const float r = -m * c;
-  return m == -INFINITY ? 0.0f : r;
-}
-__device__ __forceinline__ float power(float x, float c, float off) {
-  return __builtin_amdgcn_exp2f(fmaf(x, c, off));
-}
+// exponents as one multiply-add each, with the product c m rounded first.  That
+// rounding is the same wherever the maximum is the same, so it cancels in the
+// quotients, and what it leaves in the sums' logarithms is known (left).
+//
+// Beyond |c m| = 2^30 (maxima of rows that a mask of the lowest finite value
+// fills, say) that rounding would leave the exponents' range.  Numbers that far
+// out are 64 or more apart in c x, so only those equal to m count: a smaller
+// factor, which brings c m to 2^30, leaves the others nothing either.
+constexpr float kFar = 1073741824.0f;
+__device__ __forceinline__ bool far_out(float m, float c) { return fabsf(m * c) > kFar; }
+struct Power {
+  float c, off;
+  __device__ __forceinline__ Power(float m, float factor) {
+#pragma clang fp contract(off)  // the product rounded, whatever it is added to
+    c = m != -INFINITY && far_out(m, factor) ? kFar / fabsf(m) : factor;
+    const float r = -m * c;
+    off = m == -INFINITY ? 0.0f : r;
+  }
+  __device__ __forceinline__ float operator()(float x) const {
+    return __builtin_amdgcn_exp2f(fmaf(x, c, off));
+  }
+  __device__ __forceinline__ float left(float m) const { return m == -INFINITY ? 0.0f : fmaf(m, c, off); }
+};
 struct Sums {
   float m, a, b;
 };
-// Brings s to the maximum t (of at least s.m).
-__device__ __forceinline__ void move_to(Sums& s, float t, float ca, float cb) {
+// What a sum about m becomes about t, of at least m.
+__device__ __forceinline__ float moved(float m, float t, float c) {
 #pragma clang fp contract(off)
-  s.a *= __builtin_amdgcn_exp2f(s.m == -INFINITY ? 0.0f : about(t, ca) - about(s.m, ca));
-  s.b *= __builtin_amdgcn_exp2f(s.m == -INFINITY ? 0.0f : about(t, cb) - about(s.m, cb));
+  const float r = m * c, q = t * c;
+  return m == t || m == -INFINITY ? 1.0f
+         : far_out(m, c) || far_out(t, c) ? 0.0f : __builtin_amdgcn_exp2f(r - q);
+}
+__device__ __forceinline__ void move_to(Sums& s, float t, float ca, float cb) {
+  s.a *= moved(s.m, t, ca);
+  s.b *= moved(s.m, t, cb);
   s.m = t;
 }
 __device__ __forceinline__ void merge(Sums& s, Sums o, float ca, float cb) {
@@ -85,14 +104,18 @@ __global__ __launch_bounds__(N) void distill_kernel(DistillP<T, G> p) {
   __shared__ float amount[kMaxTop + 1];  // what entry i takes off its class
   __shared__ int where[kMaxTop + 1];     // its class, -1: none
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t r = blockIdx.x;
+  const int64_t r = p.row0 + blockIdx.x;
   const T* z = p.logits + r * p.ld;
   const int C = p.C;
   const float weight = (p.weight ? p.weight[r] : 1.0f);
   G* g = p.grad ? p.grad + r * p.ldg : nullptr;
   if (weight == 0.0f) {  // a row left out: its logits are not read
-    if (g)
-      for (int i = tid; i < C; i += N) store1(g + i, 0.0f);
+    if (g) {
+      const RowSpan<G> gs(g, C);
+      const float none[8] = {};
+      for (int c = tid; c < gs.runs; c += N) store8(g + gs.run(c), none);
+      for (int i = tid; i < gs.singles; i += N) store1(g + gs.single(i), 0.0f);
+    }
     if (tid == 0) p.loss[r] = 0.0f;
     return;
   }
@@ -109,7 +132,7 @@ __global__ __launch_bounds__(N) void distill_kernel(DistillP<T, G> p) {
     bad = c < -1 || c >= C;
     if (c >= 0 && c < C) {
       cls = c;
-      tv = p.teacher[r * p.top + tid] / p.tau;
+      tv = p.teacher[r * p.top + tid];
       bad = tv != tv;
     }
   } else if (tid == p.top && p.labels) {
@@ -121,17 +144,17 @@ __global__ __launch_bounds__(N) void distill_kernel(DistillP<T, G> p) {
 
   // One walk: maximum and sums.
   Sums s = {-INFINITY, 0.0f, 0.0f};
-  float oa = 0.0f, ob = 0.0f;  // about(s.m)
+  Power pa(s.m, ct), pb(s.m, kLog2e);
   auto raise = [&](float t) {
     if (t > s.m) {
       move_to(s, t, ct, kLog2e);
-      oa = about(t, ct);
-      if constexpr (TWO) ob = about(t, kLog2e);
+      pa = Power(t, ct);
+      if constexpr (TWO) pb = Power(t, kLog2e);
     }
   };
   auto add = [&](float x) {
-    s.a += power(x, ct, oa);
-    if constexpr (TWO) s.b += power(x, kLog2e, ob);
+    s.a += pa(x);
+    if constexpr (TWO) s.b += pb(x);
   };
   walk_row<N>(z, span, tid,
               [&](int, const float* v) {
@@ -169,7 +192,8 @@ __global__ __launch_bounds__(N) void distill_kernel(DistillP<T, G> p) {
   if constexpr (!TWO) s.b = s.a;  // tau 1, or one of the two not needed
 
   // Teacher probabilities and the row's loss.
-  const float te = tid < p.top && tm > -INFINITY ? __builtin_amdgcn_exp2f((tv - tm) * kLog2e) : 0.0f;
+  const float tx = (tv - tm) / p.tau;
+  const float te = tid < p.top && tm > -INFINITY ? __builtin_amdgcn_exp2f(tx * kLog2e) : 0.0f;
   const float ts = wave_sum(te);
   if (lane == 0) red[wave][0] = ts;
   __syncthreads();
@@ -179,16 +203,17 @@ __global__ __launch_bounds__(N) void distill_kernel(DistillP<T, G> p) {
   __syncthreads();
   const bool taught = p.alpha > 0.0f && tm > -INFINITY;  // the teacher gives the row something
   const float prob = taught ? te / tsum : 0.0f;
-  oa = about(s.m, ct);
-  ob = about(s.m, kLog2e);
+  pa = Power(s.m, ct);
+  if constexpr (TWO) pb = Power(s.m, kLog2e);
+  const Power& p1 = TWO ? pb : pa;  // of the labels' part
   float part = 0.0f;
   if (tid < p.top) {
     // log p - log q, each from differences to its own maximum.
     if (prob > 0.0f || prob != prob)
       part = p.alpha * p.tau * p.tau * prob *
-             ((tv - tm) - log2f(tsum) * kLn2 - (fmaf(zs, ct, oa) - log2f(s.a)) * kLn2);
+             (tx - log2f(tsum) * kLn2 + ((s.m - zs) / p.tau + (log2f(s.a) - pa.left(s.m)) * kLn2));
   } else if (tid == p.top && p.beta > 0.0f) {
-    part = p.beta * (log2f(s.b) - fmaf(zs, kLog2e, ob)) * kLn2;
+    part = p.beta * ((s.m - zs) + (log2f(s.b) - p1.left(s.m)) * kLn2);
   }
   const float total = wave_sum(part);
   if (lane == 0) red[wave][0] = total;
@@ -210,9 +235,9 @@ __global__ __launch_bounds__(N) void distill_kernel(DistillP<T, G> p) {
   const float f1 = fa + fb;
   auto value = [&](float x) {
     if constexpr (TWO)
-      return fmaf(fa, power(x, ct, oa), fb * power(x, kLog2e, ob));
+      return fmaf(fa, pa(x), fb * pb(x));
     else
-      return f1 * power(x, ct, oa);
+      return f1 * pa(x);
   };
   const bool wide = (reinterpret_cast<uintptr_t>(g + span.head) & 15) == 0;
   walk_row<N>(z, span, tid,
@@ -263,11 +288,16 @@ hipError_t launch(const DistillArgs& a, hipStream_t s) {
   // that is needed.
   if (a.alpha == 0.0f) p.tau = 1.0f;
   const bool two = a.labels && a.alpha > 0.0f && a.alpha < 1.0f && p.tau != 1.0f;
-  if (two)
-    hipLaunchKernelGGL((distill_kernel<T, G, N, true>), dim3((unsigned)a.rows), dim3(N), 0, s, p);
-  else
-    hipLaunchKernelGGL((distill_kernel<T, G, N, false>), dim3((unsigned)a.rows), dim3(N), 0, s, p);
-  return hipGetLastError();
+  hipError_t e = hipSuccess;
+  for (p.row0 = 0; p.row0 < a.rows && e == hipSuccess; p.row0 += kLaunchRows) {
+    const unsigned rows = (unsigned)std::min<int64_t>(a.rows - p.row0, kLaunchRows);
+    if (two)
+      hipLaunchKernelGGL((distill_kernel<T, G, N, true>), dim3(rows), dim3(N), 0, s, p);
+    else
+      hipLaunchKernelGGL((distill_kernel<T, G, N, false>), dim3(rows), dim3(N), 0, s, p);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 // More threads than teacher entries, one for the label among them; about one run
@@ -297,9 +327,9 @@ bool check_distill(const DistillArgs& a) {
     return fail(ELASTO_ERR_INVALID_ARG, "distill: bad rows, classes or row strides"), false;
   if (a.top < 0 || a.top > kMaxTop)
     return fail(ELASTO_ERR_INVALID_ARG, "distill: top %d outside [0, %d]", a.top, kMaxTop), false;
-  if (!(a.temperature > 0.0f) || !(a.temperature < INFINITY) || !(a.alpha >= 0.0f) || !(a.alpha <= 1.0f) ||
+  if (!(a.temperature >= 1e-6f) || !(a.temperature <= 1e6f) || !(a.alpha >= 0.0f) || !(a.alpha <= 1.0f) ||
       !(fabsf(a.scale) < INFINITY))
-    return fail(ELASTO_ERR_INVALID_ARG, "distill: needs temperature > 0, alpha in [0, 1] and a finite scale"), false;
+    return fail(ELASTO_ERR_INVALID_ARG, "distill: needs temperature in [1e-6, 1e6], alpha in [0, 1] and a finite scale"), false;
   if (a.alpha > 0.0f && a.top == 0)
     return fail(ELASTO_ERR_INVALID_ARG, "distill: alpha > 0 needs teacher entries"), false;
   if (a.rows == 0) return true;

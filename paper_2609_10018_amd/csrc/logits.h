@@ -6,6 +6,9 @@
 
 namespace elasto {
 
+// Rows of one launch, a workgroup each: a launch holds fewer than 2^32 threads.
+constexpr int64_t kLaunchRows = 1 << 21;
+
 __device__ __forceinline__ void load8(const uint16_t* p, float* v) {
   const u32x4 w = *reinterpret_cast<const u32x4*>(p);
 #pragma unroll

@@ -31,6 +31,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kHeads = 4;          // head vectors in flight
 constexpr int kGradBlocks = 768;   // workgroups of the backward pass (3 a CU, as its registers allow)
+constexpr int64_t kMaxTokens = 1 << 25;  // of a call, at 64 lanes each: a launch holds fewer than 2^32 threads
 
 struct Side {  // q or k
   View x;      // the input
@@ -385,7 +386,7 @@ bool check_desc(const elasto_qk_norm_t* a) {
     return fail(ELASTO_ERR_INVALID_ARG, "bad dtype %d", a->dtype), false;
   if (a->batch < 0 || a->tokens < 0 || a->q_heads < 0 || a->kv_heads < 0 ||
       (int64_t)a->q_heads + a->kv_heads < 1 || (int64_t)a->q_heads + a->kv_heads > 65536 ||
-      (int64_t)a->batch * a->tokens >= ((int64_t)1 << 31))
+      (int64_t)a->batch * a->tokens > kMaxTokens)
     return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: bad batch, tokens or heads"), false;
   if (a->head_dim < 16 || a->head_dim > 256 || a->head_dim % 16)
     return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: head_dim %d is not a multiple of 16 in [16, 256]", a->head_dim), false;
@@ -454,7 +455,6 @@ elasto_status_t run(const elasto_qk_norm_t* a, const elasto_heads_t* q, const el
   p.part_heads = (rounds + parts - 1) / parts * kHeads;
   p.parts = (heads + p.part_heads - 1) / p.part_heads;
   p.rows = (int)rows;
-  if (rows * p.parts >= ((int64_t)1 << 31)) return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: too many head vectors");
   int64_t grid = (rows * p.parts + groups - 1) / groups;
   const bool weights = back && (dq_gamma || dk_gamma);
   if (back) {

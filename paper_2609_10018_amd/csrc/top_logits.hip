@@ -16,6 +16,8 @@
 // A thread keeps the largest value of each of its runs of eight, so the second
 // walk reads only runs that hold a key from the bound on again.  Bound by memory:
 // one pass over the logits.
+#include <algorithm>
+
 #include "layout.h"
 #include "logits.h"
 
@@ -76,8 +78,8 @@ __device__ __forceinline__ float top8(const float* v) {
 // RUNS: runs of eight a thread, whose largest values it keeps for the second
 // walk; 0: more, which are all read again.
 template <typename T, int N, int RUNS>
-__global__ __launch_bounds__(N, (N == 1024 ? 8 : 2)) void top_logits_kernel(const T* logits, int64_t ld, int C, int top,
-                                                       float* values, int32_t* indices) {
+__global__ __launch_bounds__(N, (N == 1024 ? 8 : 2)) void top_logits_kernel(
+    const T* logits, int64_t ld, int C, int top, float* values, int32_t* indices) {
   __shared__ uint64_t held[kHold];
   __shared__ uint64_t bounds[N / 64];
   __shared__ int count;
@@ -198,8 +200,9 @@ __global__ __launch_bounds__(N, (N == 1024 ? 8 : 2)) void top_logits_kernel(cons
 template <typename T, int N, int RUNS>
 void start(const T* z, int64_t ld, int64_t rows, int C, int top, float* values, int32_t* indices,
            hipStream_t s) {
-  hipLaunchKernelGGL((top_logits_kernel<T, N, RUNS>), dim3((unsigned)rows), dim3(N), 0, s, z, ld, C, top,
-                     values, indices);
+  for (int64_t r = 0; r < rows; r += kLaunchRows)
+    hipLaunchKernelGGL((top_logits_kernel<T, N, RUNS>), dim3((unsigned)std::min(rows - r, kLaunchRows)),
+                       dim3(N), 0, s, z + r * ld, ld, C, top, values + r * top, indices + r * top);
 }
 
 template <typename T>

@@ -21,6 +21,9 @@ int64_t window_bwd_workspace(const elasto_window_t& a);
 hipError_t launch_window_fwd(const elasto_window_t& a, const WindowTensors& t, void* ws, hipStream_t s);
 hipError_t launch_window_bwd(const elasto_window_t& a, const WindowTensors& t, void* ws, hipStream_t s);
 
+// A launch holds fewer than 2^32 threads, 256 a workgroup.
+constexpr int64_t kMaxBlocks = 1 << 24;
+
 // Largest sinks: the keys of the first tile of the backward pass's key kernel
 // must hold them all.
 constexpr int kMaxSinks = 64;

@@ -446,7 +446,7 @@ hipError_t launch_window_fwd(const elasto_window_t& a, const WindowTensors& t, v
   p.blocks = (int64_t)a.batch * a.kv_heads * c.row_blocks * c.splits;
   p.part_o = static_cast<float*>(ws);
   p.part_ml = p.part_o + (int64_t)a.batch * a.heads * a.q_tokens * c.splits * a.head_dim;
-  if (p.blocks > 0x7fffffff) return hipErrorInvalidValue;
+  if (p.blocks >= kMaxBlocks) return hipErrorInvalidConfiguration;
   return a.dtype == ELASTO_BF16 ? launch_dim<uint16_t>(p, a.head_dim, c.keys, s)
                                 : launch_dim<float>(p, a.head_dim, c.keys, s);
 }

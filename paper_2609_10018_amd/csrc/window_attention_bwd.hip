@@ -627,6 +627,9 @@ int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 
 int64_t stat_bytes(const elasto_window_t& a) { return (int64_t)a.batch * a.heads * a.q_tokens * 8; }
 
+// Keys whose gradients are joined from parts.
+int64_t join_keys(const BwdP& p) { return p.row_parts > 1 ? p.k_tokens : p.parts > 0 ? p.mask.sinks : 0; }
+
 template <typename T, int HD>
 hipError_t launch(BwdP p, int64_t pairs, hipStream_t s) {
   hipError_t e = hipSuccess;
@@ -648,8 +651,8 @@ hipError_t launch(BwdP p, int64_t pairs, hipStream_t s) {
   hipLaunchKernelGGL((window_dkv_kernel<T, HD>), dim3((unsigned)p.blocks), dim3(kThreads),
                      (Shape<T, HD>::kLdsKey), s, p);
   e = hipGetLastError();
-  if (e != hipSuccess || (p.parts == 0 && p.row_parts == 1)) return e;
-  const int keys = p.row_parts > 1 ? p.k_tokens : p.mask.sinks, per = 1024 / HD;
+  const int keys = (int)join_keys(p), per = 1024 / HD;
+  if (e != hipSuccess || keys == 0) return e;
   hipLaunchKernelGGL((window_key_join_kernel<T, HD>), dim3((unsigned)(pairs * ((keys + per - 1) / per))),
                      dim3(kThreads), 0, s, p, keys);
   return hipGetLastError();
@@ -688,8 +691,10 @@ hipError_t launch_window_bwd(const elasto_window_t& a, const WindowTensors& t, v
   p.row_parts = row_parts_of(a);
   p.row_part = reinterpret_cast<float*>(static_cast<char*>(ws) + up256(stat_bytes(a)) + up256(part_bytes(a)));
   p.sink_groups = (a.sinks + 31) / 32;
-  if (pairs * std::max({(int64_t)p.row_blocks, (int64_t)p.key_tiles * std::max(p.row_parts, kKeys * a.head_dim / 1024),
-                        (int64_t)p.sink_groups * p.parts}) > 0x7fffffff) return hipErrorInvalidValue;
+  const int64_t join = join_keys(p) * a.head_dim / 1024 + 1;
+  if (pairs * std::max({(int64_t)p.row_blocks, (int64_t)p.key_tiles * p.row_parts,
+                        (int64_t)p.sink_groups * p.parts, join}) >= kMaxBlocks)
+    return hipErrorInvalidConfiguration;
   if (a.dtype == ELASTO_BF16)
     return a.head_dim == 64 ? launch<uint16_t, 64>(p, pairs, s) : launch<uint16_t, 128>(p, pairs, s);
   return a.head_dim == 64 ? launch<float, 64>(p, pairs, s) : launch<float, 128>(p, pairs, s);

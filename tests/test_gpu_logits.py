@@ -300,6 +300,44 @@ def test_distill_infinite_logits():
     assert torch.isnan(loss[2:]).all()
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("classes", [200, 9003])
+@pytest.mark.parametrize("tau", [0.5, 1.0, 3.0])
+def test_distill_masks_of_the_lowest_value(dtype, classes, tau):
+    """Classes masked by the type's lowest finite value have no weight; a row of nothing else is
+    uniform.  Far out, only logits equal to the maximum count."""
+    low = torch.finfo(dtype).min
+    c = Distill(dtype=dtype, grad=F32, rows=5, classes=classes, top=4, tau=tau)
+    c.idx[:], c.y[:] = torch.tensor([1, 3, 5, 7], dtype=torch.int32), 3
+    c.z[0, 8:] = low
+    c.z[1] = low                                       # nothing is left
+    c.z[2], c.z[2, 1:9:2] = 1.0e30, 2.0e30             # the teacher's classes are the largest
+    c.z[3], c.z[3, 1:9:2] = low, -1.0e30
+    c.val[4, :] = torch.finfo(F32).min                 # a teacher without an opinion
+    c.val[0, 1:] = torch.finfo(F32).min
+    loss, grad = c.run()
+    c.check(loss, grad)
+    assert torch.isfinite(loss).all() and (grad[0, 9:] == 0).all()
+
+
+def test_distill_label_on_a_masked_class():
+    """Its loss is the distance, finite as long as that is."""
+    c = Distill(classes=70, top=0, alpha=0.0)
+    c.z[:, 11], c.y[:] = -1.0e38, 11
+    c.check(*c.run())
+
+
+@pytest.mark.parametrize("grad,pad", [(BF, 0), (BF, 3), (F32, 1)])
+def test_distill_rows_left_out_are_filled_with_zeros(grad, pad):
+    """... whole, at any alignment, and nothing beside them is written."""
+    c = Distill(rows=3, classes=1003, weight=[0.0, 0.0, 1.0])
+    buf = torch.full((3, 1003 + 8), FILL, dtype=grad, device="cuda")
+    into = buf[:, pad:pad + 1003]
+    c.run(into=into)
+    assert (into[:2] == 0).all() and (into[2] != FILL).all()
+    assert (buf[:, :pad] == FILL).all() and (buf[:, pad + 1003:] == FILL).all()
+
+
 def test_distill_gradient_against_differences():
     """h = 2^-6: truncation ~ h^2 / 6 of a third derivative near 1, rounding ~ 8 * 2^-24 loss / h."""
     c = Distill(rows=1, classes=30, top=5, gain=1.0, tau=1.5)
