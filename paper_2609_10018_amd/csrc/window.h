@@ -91,11 +91,14 @@ __device__ __forceinline__ int64_t xcd_order(int64_t id, int64_t n) {
 }
 
 // Keeps an accumulator where it is across a branch: without this the compiler
-// moves whole accumulators (16 instructions each) at the join.  Kernels whose
-// accumulators also live in the other register file do without.
-template <bool ON>
+// moves whole accumulators (16 instructions each) at the join.  FEW: the kernel
+// needs no more than 256 registers a lane; otherwise its accumulators lie in the
+// second file (fp32, heads of 128, backward 2 x 2048 tokens x 8 heads: 411 us
+// untied, with spills, 372 tied).
+template <bool FEW>
 __device__ __forceinline__ void stay(f32x16& x) {
-  if constexpr (ON) asm volatile("" : "+v"(x));
+  if constexpr (FEW) asm volatile("" : "+v"(x));
+  else asm volatile("" : "+a"(x));
 }
 
 // The other half-wave's value.
