@@ -18,6 +18,8 @@
 // Where the workgroups are still few, each row block's tiles are split over
 // several, whose unnormalised results a second kernel joins (the running
 // maximum and sum of each part go with it).
+#include <math.h>
+
 #include <algorithm>
 
 #include "layout.h"
@@ -354,8 +356,10 @@ __global__ __launch_bounds__(kThreads) void window_join_kernel(FwdP p) {
   const int64_t total = p.blocks / p.splits / p.row_blocks * rmax;
   if (at >= total || row >= clamp_len(p.q_lens, b, p.q_tokens) * p.group) return;
   float M = -INFINITY, L = 0.0f, v[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
   for (int z = 0; z < p.splits; ++z) M = fmaxf(M, p.part_ml[((bk * p.splits + z) * rmax + row) * 2]);
   const float base = M == -INFINITY ? 0.0f : M;
+#pragma unroll 4
   for (int z = 0; z < p.splits; ++z) {
     const int64_t pr = (bk * p.splits + z) * rmax + row;
     const float f = __builtin_amdgcn_exp2f((p.part_ml[pr * 2] - base) * p.c2);
@@ -394,8 +398,26 @@ Cut cut_of(const elasto_window_t& a) {
   // Keys that a row block can see, in shares of at least 256 a workgroup.
   const int64_t reach = (a.causal ? (int64_t)a.window : 2 * (int64_t)a.window - 1) + per / (a.heads / a.kv_heads);
   const int64_t keys = std::min<int64_t>(a.k_tokens, reach + a.sinks);
-  const int64_t want = (2 * kCUs + blocks - 1) / std::max<int64_t>(blocks, 1);
-  c.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want, keys / 256, 64}));
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>(keys / 256, 128));
+  if (!c.keys) {
+    c.splits = (int)std::min((2 * kCUs + blocks - 1) / std::max<int64_t>(blocks, 1), most);
+    return c;
+  }
+  // By keys, a CU holds one workgroup of heads of 128, two of 64, and what counts
+  // is how many rounds of them there are: rounds times a share's length, with 160
+  // keys' worth (of 64 features twice that) for starting it, and 128 for the join.
+  // 32 x 16/4 heads of 128 on 2048 keys in 2 shares (one round) 28.4 us, in 4
+  // (two) 30.4, in 8 36; 32 x 12 of 64 in 1 share 34.6, in 2 37.6; 40 x 32/8 of
+  // 128 on 4096 in 1 146 (a round and a quarter takes two), in 4 121.
+  const int64_t slots = kCUs * (128 / a.head_dim);
+  const double start = 160.0 * 128 / a.head_dim, join = 128.0 * 128 / a.head_dim;
+  double best = INFINITY;
+  c.splits = 1;
+  for (int64_t n = 1; n <= most && blocks * n <= 4 * slots + blocks; ++n) {
+    const double cost =
+        (double)((blocks * n + slots - 1) / slots) * ((double)keys / n + start) + (n > 1 ? join : 0.0);
+    if (cost < best) best = cost, c.splits = (int)n;
+  }
   return c;
 }
 
