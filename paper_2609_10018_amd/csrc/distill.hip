@@ -49,15 +49,15 @@ struct DistillP {
   float tau, scale;
 };
 
-// A running maximum m of x and sums of 2^(c x - c m) for two factors c: the
+// A reference m near the maximum of x and sums of 2^(c x - c m) for two factors c: the
 // exponents as one multiply-add each, with the product c m rounded first.  That
 // rounding is the same wherever the maximum is the same, so it cancels in the
 // quotients, and what it leaves in the sums' logarithms is known (left).
 //
-// Beyond |c m| = 2^30 (maxima of rows that a mask of the lowest finite value
+// Beyond |c m| = 2^30 (rows that a mask of the lowest finite value
 // fills, say) that rounding would leave the exponents' range.  Numbers that far
-// out are 64 or more apart in c x, so only those equal to m count: a smaller
-// factor, which brings c m to 2^30, leaves the others nothing either.
+// out are 64 or more apart in c x, so only those equal to the maximum count: a
+// smaller factor, which brings c m to 2^30, leaves the others nothing either.
 constexpr float kFar = 1073741824.0f;
 __device__ __forceinline__ bool far_out(float m, float c) { return fabsf(m * c) > kFar; }
 struct Power {
@@ -142,11 +142,16 @@ __global__ __launch_bounds__(N) void distill_kernel(DistillP<T, G> p) {
   }
   if (cls >= 0) zs = load1(z + cls);
 
-  // One walk: maximum and sums.
+  // One walk: reference and sums.
   Sums s = {-INFINITY, 0.0f, 0.0f};
   Power pa(s.m, ct), pb(s.m, kLog2e);
+  // The reference follows the maximum only where that has risen by more than
+  // 2^kRise (in the sharper sum): terms of up to 2^kRise are as exact, and of
+  // a wave's 64 lanes one would raise its own at most runs otherwise.
+  constexpr float kRise = 8.0f;
+  const float sharp = TWO ? fmaxf(ct, kLog2e) : ct;
   auto raise = [&](float t) {
-    if (t > s.m) {
+    if ((t - s.m) * sharp > kRise) {
       move_to(s, t, ct, kLog2e);
       pa = Power(t, ct);
       if constexpr (TWO) pb = Power(t, kLog2e);
