@@ -16,8 +16,10 @@
 // logits gathered before: each sums what all entries of its class take off (a
 // class may come twice), so no order of atomics enters.
 //
-// Bound by memory: the logits once, the gradient once (2048 x 131072 bf16 with
-// its gradient: 247 us, 4.35 TB/s; a copy of that size runs at 5.1).
+// Bound by memory: the logits once, the gradient once.  2048 x 131072 bf16 with its
+// gradient 241 us, 4.45 TB/s (a copy of that size runs at 5.1); the loss alone,
+// 1000 x 50021 fp32, 35-39 us.  Both temperatures together take two exponentials
+// an element and walk: 2048 x 131072 bf16, 302 us, bound by the vector ALU.
 #include <math.h>
 
 #include <algorithm>

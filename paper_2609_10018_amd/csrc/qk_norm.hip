@@ -19,7 +19,9 @@
 // registers), since the norm is the group's and gamma is known to both.
 //
 // Everything between the load and the store is fp32; the result is rounded
-// once.  Bound by memory: 2 (backward 3) passes over q and k.
+// once.  Bound by memory, 2 (backward 3) passes over q and k: 256 x 197 tokens,
+// 24 heads of 64 in bf16, 66 us (4.9 TB/s, a copy runs at 5.1); backward on 4 x
+// 6001 padded tokens, 40 heads of 128, with both weights' gradients, 133 us (4.7).
 #include <algorithm>
 
 #include "common.h"

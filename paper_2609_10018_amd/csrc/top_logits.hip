@@ -14,8 +14,10 @@
 // The order of collecting does not matter to the result.
 //
 // A thread keeps the largest value of each of its runs of eight, so the second
-// walk reads only runs that hold a key from the bound on again.  Bound by memory:
-// one pass over the logits.
+// walk reads only runs that hold a key from the bound on again.  Bound by memory,
+// one pass over the logits: 1024 x 100003 bf16, top 64, 56-60 us (3.4-3.6 TB/s; a
+// read-only sum of 2 GiB runs at 4.0).  64 x 1000 fp32, top 16: 7.4 us, a launch and
+// the chain of one wave.
 #include <algorithm>
 
 #include "layout.h"
