@@ -517,7 +517,8 @@ elasto_status_t elasto_qk_norm_rotate_workspace(const elasto_qk_norm_t* desc, in
  * same bits every time.
  * Needs head_dim 64 or 128, heads a multiple of kv_heads, window >= 1,
  * 0 <= sinks <= 64, scale in [1e-30, 1e30]; k_tokens, q_tokens * heads / kv_heads and
- * batch * heads at most 2^29; 64 tokens of a head of k and of v (backward: of
+ * batch * heads at most 2^29 (and a call below 2^24 workgroups, of 128 rows or
+ * keys, for few rows 32); 64 tokens of a head of k and of v (backward: of
  * the heads / kv_heads heads of q and of dout that share a key head) within
  * 4 GiB less 4 KB. */
 typedef struct {

@@ -58,6 +58,13 @@ bool check_ws(const void* ws, int64_t have, int64_t need) {
   return true;
 }
 
+// The launchers refuse grids that a launch does not hold before they launch any.
+elasto_status_t launch_error(hipError_t e) {
+  if (e == hipErrorInvalidConfiguration)
+    return fail(ELASTO_ERR_INVALID_ARG, "window attention: more than %lld workgroups", (long long)kMaxBlocks - 1);
+  return fail(ELASTO_ERR_HIP, "window attention: %s", hipGetErrorString(e));
+}
+
 }  // namespace
 
 extern "C" {
@@ -89,7 +96,7 @@ elasto_status_t elasto_op_window_attention(const elasto_window_t* desc, const el
   if (!check_ws(workspace, workspace_bytes, window_fwd_workspace(a))) return ELASTO_ERR_INVALID_ARG;
   t.lse = lse;
   const hipError_t e = launch_window_fwd(a, t, workspace, static_cast<hipStream_t>(hip_stream));
-  if (e != hipSuccess) return fail(ELASTO_ERR_HIP, "window attention: %s", hipGetErrorString(e));
+  if (e != hipSuccess) return launch_error(e);
   return ELASTO_OK;
 }
 
@@ -120,7 +127,7 @@ elasto_status_t elasto_op_window_attention_bwd(const elasto_window_t* desc, cons
   if (!check_ws(workspace, workspace_bytes, window_bwd_workspace(a))) return ELASTO_ERR_INVALID_ARG;
   t.lse = const_cast<float*>(lse);
   const hipError_t e = launch_window_bwd(a, t, workspace, static_cast<hipStream_t>(hip_stream));
-  if (e != hipSuccess) return fail(ELASTO_ERR_HIP, "window attention backward: %s", hipGetErrorString(e));
+  if (e != hipSuccess) return launch_error(e);
   return ELASTO_OK;
 }
 

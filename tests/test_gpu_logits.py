@@ -380,3 +380,25 @@ def test_distill_captured_and_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(loss, l2) and torch.equal(grad, g2)
+
+
+def test_more_rows_than_one_launch_holds():
+    """2^21 rows and a few: the largest logits are copies, equal to a sort's; of the loss
+    the last rows are those of a call for them alone, bit for bit."""
+    rows, n = (1 << 21) + 5, 100
+    g = torch.Generator(device="cuda").manual_seed(5)
+    z = torch.randn(rows, 10, device="cuda", generator=g)
+    values = torch.full((rows, 2), FILL, device="cuda")
+    indices = torch.full((rows, 2), -7, dtype=torch.int32, device="cuda")
+    ffi.op_top_logits(z, values, indices)
+    assert torch.equal(values, torch.topk(z, 2, dim=1).values)
+    assert torch.equal(values, z.gather(1, indices.long())) and (indices[:, 0] != indices[:, 1]).all()
+    y = indices[:, 1].contiguous()
+    loss, grad = torch.full((rows,), FILL, device="cuda"), torch.full_like(z, FILL)
+    ffi.op_distill(z, values, indices, loss, dlogits=grad, labels=y, temperature=2.0, alpha=0.5)
+    some, sgrad = torch.empty(n, device="cuda"), torch.empty(n, 10, device="cuda")
+    for at in (0, rows - n):
+        ffi.op_distill(z[at:at + n], values[at:at + n], indices[at:at + n], some, dlogits=sgrad,
+                       labels=y[at:at + n], temperature=2.0, alpha=0.5)
+        assert torch.equal(some, loss[at:at + n]) and torch.equal(sgrad, grad[at:at + n])
+    assert (loss != FILL).all() and torch.isfinite(loss).all()

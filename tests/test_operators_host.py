@@ -116,7 +116,8 @@ def attn_bwd(lib, lse=P16, ws=P16, size=BIG, desc=None, **kw):
     dict(dtype=7), dict(head_dim=32), dict(head_dim=96), dict(batch=-1), dict(q_tokens=-1),
     dict(k_tokens=-1), dict(heads=0), dict(kv_heads=0), dict(kv_heads=5), dict(window=0),
     dict(window=-3), dict(sinks=-1), dict(sinks=65), dict(scale=0.0), dict(scale=-1.0),
-    dict(scale=math.nan), dict(scale=math.inf), dict(scale=1e-31), dict(scale=1e31), dict(q_lens=P16 + 2), dict(k_lens=P16 + 1),
+    dict(scale=math.nan), dict(scale=math.inf), dict(scale=1e-31), dict(scale=1e31),
+    dict(q_lens=P16 + 2), dict(k_lens=P16 + 1),
     dict(k_tokens=(1 << 29) + 1), dict(q_tokens=1 << 29), dict(batch=1 << 28), dict(lse=P16 + 2)])
 def test_window_attention_refuses_bad_descriptions(lib, kw):
     assert attn(lib, **kw) == INVALID
@@ -150,6 +151,16 @@ def test_window_attention_refuses_tiles_wider_than_four_gigabytes(lib):
     for side in ("q", "dout"):
         assert attn_bwd(lib, **{side: far}) == INVALID
         assert attn_bwd(lib, **{side: heads(h=1 << 30)}) == INVALID
+
+
+def test_more_work_than_a_launch_holds_is_refused(lib):
+    many = dict(batch=1 << 20, heads=16, kv_heads=16, q_tokens=1, k_tokens=10)
+    assert attn(lib, **many) == INVALID
+    many["q_tokens"] = 1 << 12
+    assert attn_bwd(lib, desc=win_desc(**many), size=1 << 60) == INVALID
+    many.update(q_tokens=1, k_tokens=1 << 12)
+    assert attn_bwd(lib, desc=win_desc(**many), size=1 << 60) == INVALID
+    assert qk(lib, batch=1 << 13, tokens=(1 << 12) + 1) == INVALID
 
 
 def test_negative_strides_are_refused(lib):
