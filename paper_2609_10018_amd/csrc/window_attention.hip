@@ -30,7 +30,7 @@
 //   8192 keys each: 28 us, 4.7 TB/s (a read-only sum of 2 GiB: 4.0, a copy 5.1);
 // * fp32: matrix instructions of 64 cycles, and at small sizes the latency of a
 //   wave's two or three tiles.  5 x 777 padded tokens, 6 heads of 64, 200 keys:
-//   34 us; 2 x 2048 x 8 heads of 128, 512 keys: 118 us.
+//   25 us; 2 x 2048 x 8 heads of 128, 512 keys: 118 us.
 #include <math.h>
 
 #include <algorithm>
@@ -66,9 +66,16 @@ struct Shape {
   // fp32 waves with tiles of their own: one, which leaves room for two
   // workgroups on a CU (2 x 1024 tokens x 6 heads of 64: 21 us, with two 26 us).
   static constexpr int kBuffers = KEYS && sizeof(T) == 4 ? 1 : 2;
+  // Of 64 features even that one holds K and V in turns, V on its way during the
+  // softmax: three workgroups on a CU (5 x 777 tokens x 6 heads, 200 keys: 29 us
+  // with both at once, 22 in turns; 2 x 2048 x 8, 512 keys, two whole rounds
+  // otherwise: 56 and 60).  Heads of 128 have no registers for more workgroups.
+  static constexpr bool kTurns = KEYS && sizeof(T) == 4 && HD == 64;
+  static constexpr int kStaged = (kTurns ? 1 : 2) * kTile;  // of a tile
+  static constexpr int kPerSimd = kTurns ? 3 : sizeof(T) == 2 || HD == 64 ? 2 : 1;  // waves
   static constexpr int kOs = HD + 4;  // floats of a row of the join
   static constexpr int kJoin = KEYS ? kWaves * 32 * kOs * 4 + kWaves * 64 * 4 : 0;
-  static constexpr int kLds = std::max(kPrivate * kBuffers * 2 * kTile, kJoin);
+  static constexpr int kLds = std::max(kPrivate * kBuffers * kStaged, kJoin);
   static constexpr int kRows = KEYS ? 32 : 32 * kWaves;
 };
 
@@ -92,10 +99,11 @@ struct State {
   }
 
   // One tile of SUB * 32 keys from j0 on; low, high, sinks: as for hidden().
-  template <int SUB>
+  // scored: called when the keys have been read; values: before the values are.
+  template <int SUB, typename F, typename W>
   __device__ __forceinline__ void tile(const char* kt, const char* vt, int j0, const Frag<T>* q,
                                        float c2, bool low, bool high, bool sinks, const Keys& ks, int h,
-                                       const typename Tile<T, HD>::Reader& rd) {
+                                       const typename Tile<T, HD>::Reader& rd, F&& scored, W&& values) {
     f32x16 s[SUB];
 #pragma unroll
     for (int b = 0; b < SUB; ++b) {
@@ -116,6 +124,7 @@ struct State {
         rd.operand(kt, b * 32, kk, a);
         s[b] = mma(a, q[kk], s[b]);
       }
+    scored();
     float t = s[0][0];
 #pragma unroll
     for (int b = 0; b < SUB; ++b)
@@ -143,6 +152,7 @@ struct State {
         s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c2, off));
         l += s[b][i];
       }
+      if (b == 0) values();
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         Frag<T> pf;
@@ -159,7 +169,7 @@ struct State {
 };
 
 template <typename T, int HD, bool KEYS>
-__global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) void window_fwd_kernel(FwdP p) {
+__global__ __launch_bounds__(kThreads, (Shape<T, HD, KEYS>::kPerSimd)) void window_fwd_kernel(FwdP p) {
   using S = Shape<T, HD, KEYS>;
   using Tl = Tile<T, HD>;
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -203,7 +213,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
   const int lw = KEYS ? 0 : wave;
   auto stage = [&](int n, char* dst) {
     kr.template issue<Ld>(dst, lw, lane, key0(n), Tl::kRow);
-    vr.template issue<Ld>(dst + S::kTile, lw, lane, key0(n), Tl::kRow);
+    if constexpr (!S::kTurns) vr.template issue<Ld>(dst + S::kTile, lw, lane, key0(n), Tl::kRow);
   };
 
   const typename Tl::Reader rd(lane);
@@ -214,17 +224,28 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) == 2 || HD == 64 ? 2 : 1)) voi
 #pragma unroll
   for (int kk = 0; kk < HD / 16; ++kk) load_operand(qrow, kk, h, q[kk]);
 
-  auto compute = [&](int n, const char* buf) {
+  auto compute = [&](int n, char* buf) __attribute__((always_inline)) {
     const int j0 = key0(n), j1 = j0 + S::kKeys - 1;
     st.hold();
     // Unless this wave's rows see nothing of the tile.
     if (!idle && (j0 <= w1.hs || (j1 >= w0.lo && j0 <= w1.hi)))
-      st.template tile<S::kSub>(buf, buf + S::kTile, j0, q, p.c2, j0 < w1.lo, j1 > w0.hi,
-                                j0 <= w1.hs, mine, h, rd);
+      st.template tile<S::kSub>(
+          buf, buf + S::kStaged - S::kTile, j0, q, p.c2, j0 < w1.lo, j1 > w0.hi, j0 <= w1.hs, mine, h, rd,
+          [&]() __attribute__((always_inline)) {
+            if constexpr (S::kTurns) {
+              asm volatile("" ::: "memory");
+              wait_lds();
+              vr.template issue<Ld>(buf, lw, lane, j0, Tl::kRow);
+              asm volatile("" ::: "memory");
+            }
+          },
+          [&]() __attribute__((always_inline)) {
+            if constexpr (S::kTurns) settle();
+          });
     st.hold();
   };
-  constexpr int kLoads = 2 * Ld::kLoads;
-  char* mem = smem + (KEYS ? wave * S::kBuffers * 2 * S::kTile : 0);
+  constexpr int kLoads = (S::kTurns ? 1 : 2) * Ld::kLoads;
+  char* mem = smem + (KEYS ? wave * S::kBuffers * S::kStaged : 0);
   const int step = KEYS ? kWaves : 1;
   int n = zs + (KEYS ? wave : 0);
   if constexpr (S::kBuffers == 2) {
@@ -416,13 +437,14 @@ Cut cut_of(const elasto_window_t& a) {
     c.splits = (int)std::min((2 * kCUs + blocks - 1) / std::max<int64_t>(blocks, 1), most);
     return c;
   }
-  // By keys, a CU holds one workgroup of heads of 128, two of 64, and what counts
-  // is how many rounds of them there are: rounds times a share's length, with 160
-  // keys' worth (of 64 features twice that) for starting it, and 128 for the join.
+  // By keys, a CU holds one workgroup of heads of 128, two of 64 (fp32 three), and
+  // what counts is how many rounds of them there are: rounds times a share's length,
+  // with 160 keys' worth (of 64 features twice that) for starting it, and 128 for
+  // the join.
   // 32 x 16/4 heads of 128 on 2048 keys in 2 shares (one round) 28.4 us, in 4
   // (two) 30.4, in 8 36; 32 x 12 of 64 in 1 share 34.6, in 2 37.6; 40 x 32/8 of
   // 128 on 4096 in 1 146 (a round and a quarter takes two), in 4 121.
-  const int64_t slots = kCUs * (128 / a.head_dim);
+  const int64_t slots = kCUs * (a.head_dim == 128 ? 1 : a.dtype == ELASTO_FP32 ? 3 : 2);
   const double start = 160.0 * 128 / a.head_dim, join = 128.0 * 128 / a.head_dim;
   double best = INFINITY;
   c.splits = 1;
