@@ -10,15 +10,17 @@
 //     collected in LDS.  Where they are too many to hold (the largest ones lie
 //     in few threads' shares), the top-th of those held is the next bound: each
 //     round drops all but `top` of what it held, so the rounds end;
-//  3. the collected keys are sorted and the first `top` written.
+//  3. the collected keys are sorted, up to 256 of them by one wave in registers,
+//     and the first `top` written.
 // The order of collecting does not matter to the result.
 //
 // A thread keeps the largest value of each of its runs of eight, so the second
 // walk reads only runs that hold a key from the bound on again.  Bound by memory,
 // one pass over the logits: 1024 x 100003 bf16, top 64, 56-60 us (3.4-3.6 TB/s; a
-// read-only sum of 2 GiB runs at 4.0).  64 x 1000 fp32, top 16: 7.4 us, a launch and
+// read-only sum of 2 GiB runs at 4.0).  64 x 1000 fp32, top 16: 6.5 us, a launch and
 // the chain of one wave.
 #include <algorithm>
+#include <type_traits>
 
 #include "layout.h"
 #include "logits.h"
@@ -38,18 +40,67 @@ __device__ __forceinline__ uint64_t key_of(uint32_t order, int i) {
   return (uint64_t)order << 32 | (uint32_t)~i;
 }
 
-// The wave's 64 keys, largest in lane 0.
-__device__ __forceinline__ uint64_t wave_sort(uint64_t k, int lane) {
+// v of lane ^ STEP, by lane moves rather than through LDS: half the time of a sort
+// is the wait for them.
+template <int STEP>
+__device__ __forceinline__ uint32_t moved(uint32_t v, int lane) {
+  auto dpp = [](uint32_t x, auto ctrl) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, 0xf, 0xf, true);
+  };
+  if constexpr (STEP == 1) return dpp(v, std::integral_constant<int, 0xB1>());
+  else if constexpr (STEP == 2) return dpp(v, std::integral_constant<int, 0x4E>());
+  else if constexpr (STEP == 4)  // ^ 3, then ^ 7
+    return dpp(dpp(v, std::integral_constant<int, 0x1B>()), std::integral_constant<int, 0x141>());
+  else if constexpr (STEP == 8) return dpp(v, std::integral_constant<int, 0x128>());
+  else if constexpr (STEP == 16) {
+    const auto x = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return lane & 16 ? x[0] : x[1];
+  } else {
+    const auto x = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return lane & 32 ? x[0] : x[1];
+  }
+}
+
+// One step of a bitonic sort of the wave's keys: key 64 r + lane in k[r].
+template <int K, int SIZE, int STEP>
+__device__ __forceinline__ void sort_step(uint64_t (&k)[K], int lane) {
+  if constexpr (STEP >= 64) {
 #pragma unroll
-  for (int size = 2; size <= 64; size *= 2)
-#pragma unroll
-    for (int step = size / 2; step >= 1; step /= 2) {
-      const uint64_t o = (uint64_t)(uint32_t)__shfl_xor((int)(k >> 32), step, 64) << 32 |
-                         (uint32_t)__shfl_xor((int)(uint32_t)k, step, 64);
-      const bool down = (lane & size) == 0, low = (lane & step) == 0;
-      k = (low == down) == (k > o) ? k : o;
+    for (int r = 0; r < K; ++r) {
+      constexpr int D = STEP / 64;
+      if (r & D) continue;
+      const bool down = (64 * r & SIZE) == 0;
+      const uint64_t a = k[r], b = k[r | D];
+      if ((a < b) == down) k[r] = b, k[r | D] = a;
     }
-  return k;
+  } else {
+#pragma unroll
+    for (int r = 0; r < K; ++r) {
+      const uint64_t o = (uint64_t)moved<STEP>((uint32_t)(k[r] >> 32), lane) << 32 |
+                         moved<STEP>((uint32_t)k[r], lane);
+      const bool down = ((64 * r + lane) & SIZE) == 0, low = (lane & STEP) == 0;
+      k[r] = (low == down) == (k[r] > o) ? k[r] : o;
+    }
+  }
+  if constexpr (STEP > 1) sort_step<K, SIZE, STEP / 2>(k, lane);
+}
+// The wave's 64 K keys, largest first.
+template <int K, int SIZE = 2>
+__device__ __forceinline__ void wave_sort(uint64_t (&k)[K], int lane) {
+  sort_step<K, SIZE, SIZE / 2>(k, lane);
+  if constexpr (SIZE < 64 * K) wave_sort<K, SIZE * 2>(k, lane);
+}
+
+// The largest `top` of n <= 64 K keys in LDS, by one wave.
+template <int K, typename F>
+__device__ __forceinline__ void write_sorted(const uint64_t* keys, int n, int top, int lane, F&& write) {
+  uint64_t k[K];
+#pragma unroll
+  for (int r = 0; r < K; ++r) k[r] = 64 * r + lane < n ? keys[64 * r + lane] : 0;
+  wave_sort(k, lane);
+#pragma unroll
+  for (int r = 0; r < K; ++r)
+    if (64 * r + lane < top) write(64 * r + lane, k[r]);
 }
 
 // keys[0, n) largest first; n a power of two.
@@ -135,14 +186,19 @@ __global__ __launch_bounds__(N, (N == 1024 ? 8 : 2)) void top_logits_kernel(
     best = k > best ? k : best;
   }
   constexpr int W = N / 64;
-  const uint64_t sorted = wave_sort(best, lane);
-  if (lane == (top + W - 1) / W - 1) bounds[tid >> 6] = sorted;
+  uint64_t sorted[1] = {best};
+  wave_sort(sorted, lane);
+  if (lane == (top + W - 1) / W - 1) bounds[tid >> 6] = sorted[0];
   __syncthreads();
   uint64_t bound = bounds[0];
 #pragma unroll
   for (int w = 1; w < W; ++w) bound = bounds[w] < bound ? bounds[w] : bound;
 
-  int n;
+  auto write = [&](int t, uint64_t k) {
+    const int i = (int)~(uint32_t)k;
+    values[(int64_t)blockIdx.x * top + t] = load1(z + i);
+    indices[(int64_t)blockIdx.x * top + t] = i;
+  };
   while (true) {
     if (tid == 0) count = 0;
     __syncthreads();
@@ -181,7 +237,14 @@ __global__ __launch_bounds__(N, (N == 1024 ? 8 : 2)) void top_logits_kernel(
                   keep1);
     }
     __syncthreads();
-    n = count;
+    const int n = count;
+    if (n <= 256) {  // the rule: few more than top
+      if (tid >= 64) return;
+      if (n <= 64) write_sorted<1>(held, n, top, lane, write);
+      else if (n <= 128) write_sorted<2>(held, n, top, lane, write);
+      else write_sorted<4>(held, n, top, lane, write);
+      return;
+    }
     const int got = n < kHold ? n : kHold;
     int p2 = 1;
     while (p2 < got) p2 *= 2;
@@ -192,11 +255,7 @@ __global__ __launch_bounds__(N, (N == 1024 ? 8 : 2)) void top_logits_kernel(
     bound = held[top - 1];
     __syncthreads();
   }
-  for (int t = tid; t < top; t += N) {
-    const int i = (int)~(uint32_t)held[t];
-    values[(int64_t)blockIdx.x * top + t] = load1(z + i);
-    indices[(int64_t)blockIdx.x * top + t] = i;
-  }
+  for (int t = tid; t < top; t += N) write(t, held[t]);
 }
 
 template <typename T, int N, int RUNS>
