@@ -440,9 +440,9 @@ elasto_status_t elasto_op_conv2d(const void* x, int32_t batch, int32_t H, int32_
  * order (so q, k and v may lie head by head in one buffer, as the q/k/v
  * projection writes them: head_stride 3 * head_dim, token_stride qkv_stride;
  * or in a cache of [batch][kv_heads][capacity][head_dim]).  data and every
- * stride are multiples of 16 bytes, no stride is negative.  Strides of tensors that are written are
- * at least head_dim along axes longer than 1; rows of one tensor must not
- * overlap, nor written tensors others unless stated. */
+ * stride are multiples of 16 bytes, no stride is negative.  Strides of tensors
+ * that are written are at least head_dim along axes longer than 1; rows of one
+ * written tensor must not overlap, nor written tensors others unless stated. */
 typedef struct {
   void* data;
   int64_t batch_stride, token_stride, head_stride;
@@ -509,18 +509,19 @@ elasto_status_t elasto_qk_norm_rotate_workspace(const elasto_qk_norm_t* desc, in
  * key head h / (heads / kv_heads).  What lies behind a sequence's lengths, and
  * keys and values that none of its queries sees (before the window of the first
  * one, say), are not used: they may be anything, NaN included.  Nothing is
- * written behind the lengths, and such keys get zero gradients.  (An infinity or NaN in a row
- * that some see may also reach others of its sequence that do not.)
+ * written behind the lengths; keys within them that no query sees get zero
+ * gradients.  (An infinity or NaN in a row that some see may also reach others
+ * of its sequence that do not.)
  * BF16: products of bf16 with fp32 sums, softmax statistics in fp32, the
  * probabilities (backward: also the gradients of the scores) rounded to bf16
  * for the products that sum them.  FP32: fp32 throughout.  Results are the
  * same bits every time.
  * Needs head_dim 64 or 128, heads a multiple of kv_heads, window >= 1,
- * 0 <= sinks <= 64, scale in [1e-30, 1e30]; k_tokens, q_tokens * heads / kv_heads and
- * batch * heads at most 2^29 (and a call below 2^24 workgroups, of 128 rows or
- * keys, for few rows 32); 64 tokens of a head of k and of v (backward: of
- * the heads / kv_heads heads of q and of dout that share a key head) within
- * 4 GiB less 4 KB. */
+ * 0 <= sinks <= 64, scale in [1e-30, 1e30]; k_tokens, q_tokens * heads /
+ * kv_heads and batch * heads at most 2^29 (and a call below 2^24 workgroups, of
+ * 128 rows or keys, for few rows 32); 64 tokens of a head of k and of v
+ * (backward: of the heads / kv_heads heads of q and of dout that share a key
+ * head) within 4 GiB less 4 KB. */
 typedef struct {
   int32_t dtype, batch, q_tokens, k_tokens, heads, kv_heads, head_dim;
   int32_t causal, window, sinks;
