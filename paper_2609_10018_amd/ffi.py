@@ -243,14 +243,17 @@ def pack_weights(cfg: ModelConfig, w: Dict[str, np.ndarray], table: DNTable) -> 
 _raw_stream = None      # torch's (device index) -> hipStream_t of its current stream
 
 
-def _stream_ptr(stream) -> int:
-    """The hipStream_t of `stream`; None: torch's current stream.
+def _stream_ptr(stream, device: Optional[int] = None) -> int:
+    """The hipStream_t of `stream`; None: torch's current stream (of the current device, which
+    `device` is where the caller has asked for it already).
 
     Asked for as a pointer: building torch's Stream object to read it from took
     3.0 of the 7.8 us of host time of a small call."""
     if stream is not None:
         return int(getattr(stream, "cuda_stream", stream))
     global _raw_stream
+    if device is not None and _raw_stream is not None:
+        return _raw_stream(device)
     import torch
     if _raw_stream is None:
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
@@ -400,12 +403,13 @@ def _tt() -> _Torch:
     return _torch
 
 
-def _same_device(*tensors) -> None:
+def _same_device(*tensors) -> int:
     """Refuse tensors that do not all lie on the current device: the kernels run there."""
     d = _tt().device()
     for t in tensors:
         if t is not None and t.get_device() != d:
             raise ValueError(f"a tensor lies on {t.device}, the current device is cuda:{d}")
+    return d
 
 
 def _dtype(t) -> int:
@@ -432,6 +436,11 @@ def _heads(t, shape, dtype, name: str):
         return None
     if t.shape != shape or t.dtype is not dtype:
         raise ValueError(f"{name} is {tuple(t.shape)} {t.dtype}, not {tuple(shape)} {dtype}")
+    return _strided(t, shape, name)
+
+
+def _strided(t, shape, name: str):
+    """The same of a tensor that the shape was taken from."""
     b, r, h, f = t.stride()
     nb, nr, nh, n = shape
     if f != 1 and n > 1:
@@ -488,11 +497,11 @@ def op_qk_norm_rotate(q, k, q_out, k_out, cos=None, sin=None, q_gamma=None, k_ga
     contiguous); k, k_out likewise with their own heads; either pair may be None.  cos, sin: fp32
     [rows, rot_dim / 2] (None: no rotation).  positions: int32 [batch, tokens]; lens: int32
     [batch]."""
-    _same_device(q, k, q_out, k_out, cos, sin, q_gamma, k_gamma, positions, lens)
+    dev = _same_device(q, k, q_out, k_out, cos, sin, q_gamma, k_gamma, positions, lens)
     a, sq, sk, dt = _qk_desc(q, k, cos, sin, q_gamma, k_gamma, positions, lens, eps, interleaved)
     check(load_library().elasto_op_qk_norm_rotate(
-        a, _heads(q, sq, dt, "q"), _heads(k, sk, dt, "k"), _heads(q_out, sq, dt, "q_out"),
-        _heads(k_out, sk, dt, "k_out"), _stream_ptr(stream)))
+        a, None if q is None else _strided(q, sq, "q"), _heads(k, sk, dt, "k"),
+        _heads(q_out, sq, dt, "q_out"), _heads(k_out, sk, dt, "k_out"), _stream_ptr(stream, dev)))
 
 
 def op_qk_norm_rotate_bwd(q, k, dq_out, dk_out, dq, dk, dq_gamma=None, dk_gamma=None,
@@ -502,15 +511,15 @@ def op_qk_norm_rotate_bwd(q, k, dq_out, dk_out, dq, dk, dq_gamma=None, dk_gamma=
     """dq_out, dk_out: the gradients of op_qk_norm_rotate's results; dq, dk: those of q and k;
     dq_gamma, dk_gamma: fp32 [head_dim] or None.  workspace: a uint8 device tensor of
     qk_norm_rotate_workspace() bytes where a weight gradient is asked for."""
-    _same_device(q, k, dq_out, dk_out, dq, dk, dq_gamma, dk_gamma, workspace, cos, sin, q_gamma,
-                 k_gamma, positions, lens)
+    dev = _same_device(q, k, dq_out, dk_out, dq, dk, dq_gamma, dk_gamma, workspace, cos, sin,
+                       q_gamma, k_gamma, positions, lens)
     a, sq, sk, dt = _qk_desc(q, k, cos, sin, q_gamma, k_gamma, positions, lens, eps, interleaved)
     f32 = _tt().f32
     check(load_library().elasto_op_qk_norm_rotate_bwd(
-        a, _heads(q, sq, dt, "q"), _heads(k, sk, dt, "k"), _heads(dq_out, sq, dt, "dq_out"),
-        _heads(dk_out, sk, dt, "dk_out"), _heads(dq, sq, dt, "dq"), _heads(dk, sk, dt, "dk"),
+        a, None if q is None else _strided(q, sq, "q"), _heads(k, sk, dt, "k"),
+        _heads(dq_out, sq, dt, "dq_out"), _heads(dk_out, sk, dt, "dk_out"), _heads(dq, sq, dt, "dq"), _heads(dk, sk, dt, "dk"),
         _plain(dq_gamma, f32, "dq_gamma", sq[3]), _plain(dk_gamma, f32, "dk_gamma", sq[3]),
-        *_space(workspace), _stream_ptr(stream)))
+        *_space(workspace), _stream_ptr(stream, dev)))
 
 
 def _window_desc(q, k, window, sinks, causal, scale, q_lens, k_lens):
@@ -545,12 +554,12 @@ def op_window_attention(q, k, v, o, window: int, sinks: int = 0, causal: bool = 
     contiguous); k, v: [batch, k_tokens, kv_heads, head_dim].  lse: fp32 [batch, heads, q_tokens]
     or None.  q_lens, k_lens: int32 [batch] or None.  scale: None for 1 / sqrt(head_dim).
     workspace: a uint8 device tensor of window_attention_workspace() bytes."""
-    _same_device(q, k, v, o, lse, q_lens, k_lens, workspace)
+    dev = _same_device(q, k, v, o, lse, q_lens, k_lens, workspace)
     a, sq, sk, dt = _window_desc(q, k, window, sinks, causal, scale, q_lens, k_lens)
     check(load_library().elasto_op_window_attention(
-        a, _heads(q, sq, dt, "q"), _heads(k, sk, dt, "k"), _heads(v, sk, dt, "v"),
+        a, _strided(q, sq, "q"), _heads(k, sk, dt, "k"), _heads(v, sk, dt, "v"),
         _heads(o, sq, dt, "o"), _plain(lse, _tt().f32, "lse", sq[0] * sq[1] * sq[2]),
-        *_space(workspace), _stream_ptr(stream)))
+        *_space(workspace), _stream_ptr(stream, dev)))
 
 
 def op_window_attention_bwd(q, k, v, o, lse, dout, dq, dk, dv, window: int, sinks: int = 0,
@@ -558,13 +567,13 @@ def op_window_attention_bwd(q, k, v, o, lse, dout, dq, dk, dv, window: int, sink
                             k_lens=None, workspace=None, stream=None) -> None:
     """The gradients dq, dk, dv (shaped like q, k, v) from dout (like o), with op_window_attention's
     o and lse."""
-    _same_device(q, k, v, o, lse, dout, dq, dk, dv, q_lens, k_lens, workspace)
+    dev = _same_device(q, k, v, o, lse, dout, dq, dk, dv, q_lens, k_lens, workspace)
     a, sq, sk, dt = _window_desc(q, k, window, sinks, causal, scale, q_lens, k_lens)
     check(load_library().elasto_op_window_attention_bwd(
-        a, _heads(q, sq, dt, "q"), _heads(k, sk, dt, "k"), _heads(v, sk, dt, "v"),
+        a, _strided(q, sq, "q"), _heads(k, sk, dt, "k"), _heads(v, sk, dt, "v"),
         _heads(o, sq, dt, "o"), _plain(lse, _tt().f32, "lse", sq[0] * sq[1] * sq[2]),
         _heads(dout, sq, dt, "dout"), _heads(dq, sq, dt, "dq"), _heads(dk, sk, dt, "dk"),
-        _heads(dv, sk, dt, "dv"), *_space(workspace), _stream_ptr(stream)))
+        _heads(dv, sk, dt, "dv"), *_space(workspace), _stream_ptr(stream, dev)))
 
 
 def _rows(t, name: str):
@@ -579,7 +588,7 @@ def _rows(t, name: str):
 def op_top_logits(logits, values, indices, stream=None) -> None:
     """logits: bf16 or fp32 [rows, classes] device tensor (any row stride); values: fp32 and
     indices: int32, [rows, top]."""
-    _same_device(logits, values, indices)
+    dev = _same_device(logits, values, indices)
     r, c, ld = _rows(logits, "logits")
     shape = values.shape
     if len(shape) != 2 or shape != indices.shape or shape[0] != r:
@@ -587,7 +596,7 @@ def op_top_logits(logits, values, indices, stream=None) -> None:
                          f"[{r}, top]")
     check(load_library().elasto_op_top_logits(
         _dtype(logits), logits.data_ptr(), ld, r, c, shape[1], _plain(values, _tt().f32, "values"),
-        _plain(indices, _tt().i32, "indices"), _stream_ptr(stream)))
+        _plain(indices, _tt().i32, "indices"), _stream_ptr(stream, dev)))
 
 
 def op_distill(logits, teacher_values, teacher_indices, loss, dlogits=None, labels=None,
@@ -597,7 +606,7 @@ def op_distill(logits, teacher_values, teacher_indices, loss, dlogits=None, labe
     and teacher_indices: int32, [rows, top] (None with alpha 0); loss: fp32 [rows]; dlogits: bf16
     or fp32 [rows, classes] or None; labels: int32 [rows] or None; row_weight: fp32 [rows] or
     None."""
-    _same_device(logits, teacher_values, teacher_indices, loss, dlogits, labels, row_weight)
+    dev = _same_device(logits, teacher_values, teacher_indices, loss, dlogits, labels, row_weight)
     r, c, ld = _rows(logits, "logits")
     top = 0
     if teacher_values is not None:
@@ -618,7 +627,7 @@ def op_distill(logits, teacher_values, teacher_indices, loss, dlogits=None, labe
         dt, logits.data_ptr(), ld, r, c, _plain(teacher_values, f32, "teacher_values"),
         _plain(teacher_indices, i32, "teacher_indices"), top, _plain(labels, i32, "labels", r),
         _plain(row_weight, f32, "row_weight", r), temperature, alpha, scale,
-        _plain(loss, f32, "loss", r), gd, grad, ldg, _stream_ptr(stream)))
+        _plain(loss, f32, "loss", r), gd, grad, ldg, _stream_ptr(stream, dev)))
 
 
 class GrowthContext:
