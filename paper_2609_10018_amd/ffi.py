@@ -517,7 +517,8 @@ def op_qk_norm_rotate_bwd(q, k, dq_out, dk_out, dq, dk, dq_gamma=None, dk_gamma=
     f32 = _tt().f32
     check(load_library().elasto_op_qk_norm_rotate_bwd(
         a, None if q is None else _strided(q, sq, "q"), _heads(k, sk, dt, "k"),
-        _heads(dq_out, sq, dt, "dq_out"), _heads(dk_out, sk, dt, "dk_out"), _heads(dq, sq, dt, "dq"), _heads(dk, sk, dt, "dk"),
+        _heads(dq_out, sq, dt, "dq_out"), _heads(dk_out, sk, dt, "dk_out"),
+        _heads(dq, sq, dt, "dq"), _heads(dk, sk, dt, "dk"),
         _plain(dq_gamma, f32, "dq_gamma", sq[3]), _plain(dk_gamma, f32, "dk_gamma", sq[3]),
         *_space(workspace), _stream_ptr(stream, dev)))
 
