@@ -10,14 +10,14 @@
 //     collected in LDS.  Where they are too many to hold (the largest ones lie
 //     in few threads' shares), the top-th of those held is the next bound: each
 //     round drops all but `top` of what it held, so the rounds end;
-//  3. the collected keys are sorted, up to 256 of them by one wave in registers,
+//  3. the collected keys are sorted, up to 512 of them by one wave in registers,
 //     and the first `top` written.
 // The order of collecting does not matter to the result.
 //
 // A thread keeps the largest value of each of its runs of eight, so the second
 // walk reads only runs that hold a key from the bound on again.  Bound by memory,
-// one pass over the logits: 1024 x 100003 bf16, top 64, 56-60 us (3.4-3.6 TB/s; a
-// read-only sum of 2 GiB runs at 4.0).  64 x 1000 fp32, top 16: 6.5 us, a launch and
+// one pass over the logits: 1024 x 100003 bf16, top 64, 52-57 us (3.6-3.9 TB/s; a
+// read-only sum of 2 GiB runs at 4.0).  64 x 1000 fp32, top 16: 6 us, a launch and
 // the chain of one wave.
 #include <algorithm>
 #include <type_traits>
@@ -138,7 +138,22 @@ __global__ __launch_bounds__(N, (N == 1024 ? 8 : 2)) void top_logits_kernel(
   __shared__ int count;
   const int tid = threadIdx.x, lane = tid & 63;
   const T* z = logits + (int64_t)blockIdx.x * ld;
-  const RowSpan<T> span(z, C);
+  RowSpan<T> span(z, C);
+  // Few classes: one by one, so that all threads have some and the bound is close
+  // (422 bf16, top 54: with runs for 52 lanes alone every key is collected, 25 us).
+  if (C <= 8 * N) span.head = span.singles = C, span.runs = 0;
+  // f(index, value) over the thread's single values, eight loads in flight.
+  auto each_single = [&](auto&& f) __attribute__((always_inline)) {
+    for (int i0 = tid; i0 < span.singles; i0 += 8 * N) {
+      float v[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        v[u] = i0 + u * N < span.singles ? load1(z + span.single(i0 + u * N)) : 0.0f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (i0 + u * N < span.singles) f(span.single(i0 + u * N), v[u]);
+    }
+  };
 
   // The thread's largest key, or rather one that is no larger: of a run, its
   // largest value at its last index.
@@ -170,10 +185,10 @@ __global__ __launch_bounds__(N, (N == 1024 ? 8 : 2)) void top_logits_kernel(
       }
       asm volatile("" ::: "memory");  // four loads in flight are enough, and their registers
     }
-    for (int i = tid; i < span.singles; i += N) {
-      const uint64_t k = key_of(order_of(load1(z + span.single(i))), span.single(i));
+    each_single([&](int i, float v) {
+      const uint64_t k = key_of(order_of(v), i);
       best = k > best ? k : best;
-    }
+    });
   } else {
     walk_row<N>(z, span, tid, [&](int i, const float* v) { take(order_of(top8(v)), i + 7); },
                 [&](int i, float v) {
@@ -228,7 +243,7 @@ __global__ __launch_bounds__(N, (N == 1024 ? 8 : 2)) void top_logits_kernel(
         load8(z + i, v);
         keep8(i, v);
       }
-      for (int i = tid; i < span.singles; i += N) keep1(span.single(i), load1(z + span.single(i)));
+      each_single(keep1);
     } else {
       walk_row<N>(z, span, tid,
                   [&](int i, const float* v) {
@@ -238,11 +253,15 @@ __global__ __launch_bounds__(N, (N == 1024 ? 8 : 2)) void top_logits_kernel(
     }
     __syncthreads();
     const int n = count;
-    if (n <= 256) {  // the rule: few more than top
+    // The rule: few more than top.  (512 keys take 16 registers more than 1024
+    // threads, two rows to a CU, have.)
+    constexpr int kInWave = N < 1024 ? 512 : 256;
+    if (n <= kInWave) {
       if (tid >= 64) return;
       if (n <= 64) write_sorted<1>(held, n, top, lane, write);
       else if (n <= 128) write_sorted<2>(held, n, top, lane, write);
-      else write_sorted<4>(held, n, top, lane, write);
+      else if (N == 1024 || n <= 256) write_sorted<4>(held, n, top, lane, write);
+      else write_sorted<8>(held, n, top, lane, write);
       return;
     }
     const int got = n < kHold ? n : kHold;
@@ -270,10 +289,16 @@ template <typename T>
 hipError_t launch(const void* logits, int64_t ld, int64_t rows, int C, int top, float* values,
                   int32_t* indices, hipStream_t s) {
   const T* z = static_cast<const T*>(logits);
-  if (C <= 2048 && top <= 64)  // a wave's 64 keys hold the bound themselves
+  // The bound is each wave's ceil(top / W)-th of 64, and loose where that is one of
+  // its last: most keys are then collected and sorted.  One wave a row, four: 4096
+  // x 1000, top 16 11 and 18 us, top 56 18 and 20, top 64 75 and 20.  Four waves,
+  // eight: top 128 25 and 46, top 250 84 and 56.
+  if (C <= 2048 && top <= 56)
     start<T, 64, 4>(z, ld, rows, C, top, values, indices, s);
-  else if (C < 8192)
+  else if (C < 8192 && top <= 224)
     start<T, 256, 4>(z, ld, rows, C, top, values, indices, s);
+  else if (C < 8192)
+    start<T, 512, 2>(z, ld, rows, C, top, values, indices, s);
   else if (C <= 65536)
     start<T, 1024, 8>(z, ld, rows, C, top, values, indices, s);
   else if (C <= 131072)

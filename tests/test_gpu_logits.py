@@ -66,6 +66,15 @@ def test_top_logits(dtype, rows, classes, top):
     check_top((torch.randn(rows, classes, generator=g) * 3).to(dtype).cuda(), top)
 
 
+@pytest.mark.parametrize("classes", [64, 65, 422, 512, 513, 2048, 2049, 4096, 4097, 8191])
+@pytest.mark.parametrize("top", [1, 54, 56, 57, 64, 129, 224, 225, 256])
+def test_top_logits_of_few_classes(classes, top):
+    """bf16 values, many of them equal: where one wave, four or eight take a row, read one by one
+    or in runs, and the last keys fit a wave or do not."""
+    g = torch.Generator().manual_seed(classes * 257 + top)
+    check_top(torch.randn(9, classes, generator=g).to(BF).cuda(), min(top, classes))
+
+
 @pytest.mark.parametrize("classes", [300, 9001, 70000])
 @pytest.mark.parametrize("kind", ["equal", "two", "rising", "falling", "one share", "infinite",
                                   "nan", "zeros"])
