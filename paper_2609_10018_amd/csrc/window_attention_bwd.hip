@@ -21,7 +21,7 @@
 // keys ~265, sinks 25, join 5); counted as five products 627 TFLOP/s, as the seven
 // that run 880, the key kernel by itself 1.1 PFLOP/s.  Without its exponentials
 // and masks the row kernel ran at 1.24, a library product of 8192^3 runs at 1.4.
-// fp32, 2 x 2048 x 8 heads of 128, 512 keys: 372 us.
+// fp32, 2 x 2048 x 8 heads of 128, 512 keys: 350 us.
 //
 // A key among the sinks is seen by every later row.  The key kernel takes the
 // rows that see the first tile's keys through their windows, as for any tile;
@@ -617,11 +617,15 @@ int parts_of(const elasto_window_t& a) {
 }
 
 // Parts of a tile's rows, where the tiles of keys would leave CUs idle (few
-// key heads): 512 workgroups (2 a CU), four tiles of rows or more each.
+// key heads): as many workgroups as run at once (2 a CU, fp32 of 128 features 1) or
+// fewer, four tiles of rows or more each (fp32, of tiles half as long that take 8
+// times as long: 3 x 481 tokens x 6 heads of 128, 54 keys, in 1 part 198 us, in 2
+// 140; bf16 62 x 256 x 3, 184 keys, in 1 part 52 us, in 2 80).
 int row_parts_of(const elasto_window_t& a) {
   const int64_t blocks = (int64_t)a.batch * a.kv_heads * ((a.k_tokens + kKeys - 1) / kKeys);
-  const int64_t want = (512 + blocks - 1) / std::max<int64_t>(blocks, 1);
-  return (int)std::max<int64_t>(1, std::min<int64_t>({want, near_rows(a) / 256, 16}));
+  const int64_t near = near_rows(a), most = a.dtype == ELASTO_FP32 ? (near + 127) / 128 : near / 256;
+  const int64_t places = a.dtype == ELASTO_FP32 && a.head_dim == 128 ? 256 : 512;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({places / std::max<int64_t>(blocks, 1), most, 16}));
 }
 int64_t row_part_bytes(const elasto_window_t& a) {
   const int n = row_parts_of(a);
