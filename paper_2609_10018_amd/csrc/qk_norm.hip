@@ -20,8 +20,9 @@
 //
 // Everything between the load and the store is fp32; the result is rounded
 // once.  Bound by memory, 2 (backward 3) passes over q and k: 256 x 197 tokens,
-// 24 heads of 64 in bf16, 66 us (4.9 TB/s, a copy runs at 5.1); backward on 4 x
-// 6001 padded tokens, 40 heads of 128, with both weights' gradients, 133 us (4.7).
+// 24 heads of 64 in bf16, 68 us (4.8 TB/s, a copy runs at 5.1; 56 us called again on
+// the same tensors, part of which the caches keep); backward on 4 x 6001 padded
+// tokens, 40 heads of 128, with both weights' gradients, 133 us (4.7).
 #include <algorithm>
 
 #include "common.h"
@@ -49,6 +50,7 @@ struct QkP {
   const int32_t *positions, *lens;
   int tokens, dim, rot, table_rows;
   int rows, parts, part_heads;  // batch * tokens; parts of the heads, heads of each
+  bool wide;  // the tables allow 16-byte loads
   float eps, inv_dim;
   float* part;  // backward: [workgroup][2][dim]
 };
@@ -82,6 +84,25 @@ struct Piece<float> {
                  __float_as_uint(v[3])};
   }
 };
+
+// K values of a table.  wide: all tables start at multiples of 16 bytes, and with
+// them every lane's piece (11 x 1322 tokens, 6 heads of 128: 34 us with single loads,
+// which were most of what a group did, 11 with 16-byte ones).
+template <int K>
+__device__ __forceinline__ void load_table(const float* p, bool wide, float* v) {
+  typedef float piece __attribute__((ext_vector_type(K < 4 ? K : 4)));
+  if (wide) {
+#pragma unroll
+    for (int i = 0; i < K; i += 4) {
+      const piece x = *reinterpret_cast<const piece*>(p + i);
+#pragma unroll
+      for (int e = 0; e < (K < 4 ? K : 4); ++e) v[i + e] = x[e];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < K; ++i) v[i] = p[i];
+  }
+}
 
 // The sum over the group in each of its lanes: in quads, in eights and in rows
 // of 16 by lane moves of the adder itself (each step's operands are the same in
@@ -144,9 +165,13 @@ struct Lane {
     const int at = PAIRS ? f0 / 2 : (f0 < half ? f0 : f0 - half);
     const float* cp = p.cos + (int64_t)(ok ? pos : 0) * half + at;
     const float* sp = p.sin + (int64_t)(ok ? pos : 0) * half + at;
+    constexpr int K = PAIRS ? N / 2 : N;
+    float cv[K], sv[K];
+    load_table<K>(cp, p.wide, cv);
+    load_table<K>(sp, p.wide, sv);
 #pragma unroll
-    for (int e = 0; e < (PAIRS ? N / 2 : N); ++e) {
-      const float ce = ok ? cp[e] : NAN, se = ok ? sp[e] : NAN;
+    for (int e = 0; e < K; ++e) {
+      const float ce = ok ? cv[e] : NAN, se = ok ? sv[e] : NAN;
       if constexpr (PAIRS) {
         c[2 * e] = c[2 * e + 1] = ce;
         s[2 * e] = -se;
@@ -157,12 +182,18 @@ struct Lane {
       }
     }
   }
-  __device__ __forceinline__ void weights(const float* gamma, float* g, float* gp) const {
+  // gamma of the lane's features, and of those that they turn with.
+  __device__ __forceinline__ void weights(const float* gamma, bool wide, float* g) const {
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      g[e] = on && gamma ? gamma[f0 + e] : 1.0f;
-      gp[e] = on && gamma ? gamma[PAIRS ? f0 + (e ^ 1) : pf + e] : 1.0f;
-    }
+    for (int e = 0; e < N; ++e) g[e] = 1.0f;
+    if (on && gamma) load_table<N>(gamma + f0, wide, g);
+  }
+  __device__ __forceinline__ void weights(const float* gamma, bool wide, float* g, float* gp) const {
+    weights(gamma, wide, g);
+#pragma unroll
+    for (int e = 0; e < N; ++e) gp[e] = PAIRS ? g[e ^ 1] : 1.0f;
+    if constexpr (!PAIRS)
+      if (on && gamma) load_table<N>(gamma + pf, wide, gp);
   }
   // The features that x turns with, from the group's raw pieces.
   __device__ __forceinline__ void partners(const u32x4& raw, const float* x, float* xp) const {
@@ -203,7 +234,7 @@ __device__ __forceinline__ void forward_heads(const QkP& p, const Side& s, const
                                               const float* sn) {
   constexpr int N = Piece<T>::N;
   float own[N], other[N];
-  L.weights(s.gamma, own, other);
+  L.weights(s.gamma, p.wide, own, other);
 #pragma unroll
   for (int e = 0; e < N; ++e) own[e] *= c[e], other[e] *= sn[e];
   const bool on = w.live && L.on;
@@ -313,9 +344,9 @@ __global__ __launch_bounds__(kThreads, 3) void qk_norm_bwd_kernel(QkP p) {
 #pragma unroll
   for (int e = 0; e < N; ++e) {
     dgq[e] = dgk[e] = 0.0f;
-    gq[e] = L.on && p.q.gamma ? p.q.gamma[L.f0 + e] : 1.0f;
-    gk[e] = L.on && p.k.gamma ? p.k.gamma[L.f0 + e] : 1.0f;
   }
+  L.weights(p.q.gamma, p.wide, gq);
+  L.weights(p.k.gamma, p.wide, gk);
   const int64_t units = (int64_t)p.rows * p.parts;
   for (int64_t u0 = (int64_t)blockIdx.x * G; u0 < units; u0 += (int64_t)gridDim.x * G) {
     const Unit w = unit_of(p, u0 + grp);
@@ -435,6 +466,7 @@ elasto_status_t run(const elasto_qk_norm_t* a, const elasto_heads_t* q, const el
     return ELASTO_ERR_INVALID_ARG;
   p.cos = a->cos;
   p.sin = a->sin;
+  p.wide = aligned(a->cos, 16) && aligned(a->sin, 16) && aligned(a->q_gamma, 16) && aligned(a->k_gamma, 16);
   p.positions = a->positions;
   p.lens = a->lens;
   p.tokens = a->tokens;
@@ -446,14 +478,12 @@ elasto_status_t run(const elasto_qk_norm_t* a, const elasto_heads_t* q, const el
   int gw = 2;
   while (gw * n < a->head_dim) gw *= 2;
   const int groups = kThreads / gw;
-  // Parts of the heads, whole rounds of kHeads each: as many as it takes for
-  // 1024 workgroups (backward: for two units a group).  Each part loads the
-  // cosines again: 256 x 197 tokens in 1, 2 and 6 parts 66, 79 and 127 us, 64 x
-  // 197 in 1 and 3 33 and 23 us; backward 4 x 6001 tokens in 1, 2, 3 and 6 parts
-  // 140, 134, 143 and 147 us.
+  // Parts of the heads, whole rounds of kHeads each, where the tokens leave CUs
+  // idle: as many as 512 workgroups take (backward: the fixed grid).  Each part
+  // loads the cosines again.
   const int heads = a->q_heads + a->kv_heads, rounds = (heads + kHeads - 1) / kHeads;
-  const int64_t want = (int64_t)(back ? 2 * kGradBlocks : 1024) * groups;
-  const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(rounds, (want + rows - 1) / std::max<int64_t>(rows, 1)));
+  const int64_t want = (int64_t)(back ? kGradBlocks : 512) * groups;
+  const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(rounds, want / std::max<int64_t>(rows, 1)));
   p.part_heads = (rounds + parts - 1) / parts * kHeads;
   p.parts = (heads + p.part_heads - 1) / p.part_heads;
   p.rows = (int)rows;

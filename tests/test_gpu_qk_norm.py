@@ -270,6 +270,27 @@ def test_zeros_large_and_tiny_values():
     assert (out["q"][0, 0] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("pairs", [False, True])
+@pytest.mark.parametrize("name", ["cos", "sin", "q_gamma", "k_gamma"])
+def test_tables_at_any_address(dtype, pairs, name):
+    """A table that starts 4 bytes behind a 16-byte boundary gives the same bits."""
+    c = Case(dtype, 2, 21, 3, 2, 96, 80, pairs=pairs)
+    want = {n: c.empty(n) for n in "qk"}
+    ffi.op_qk_norm_rotate(c.x["q"], c.x["k"], want["q"], want["k"], **c.kw)
+    d, dx, dw = backward(c)
+    moved = torch.empty(c.kw[name].numel() + 1, device="cuda")[1:].view(c.kw[name].shape)
+    assert moved.data_ptr() % 16 == 4
+    moved.copy_(c.kw[name])
+    c.kw[name] = moved
+    out = {n: c.empty(n) for n in "qk"}
+    ffi.op_qk_norm_rotate(c.x["q"], c.x["k"], out["q"], out["k"], **c.kw)
+    _, dx2, dw2 = backward(c)
+    for n in "qk":
+        assert torch.equal(out[n], want[n])
+        assert torch.equal(dx[n], dx2[n]) and torch.equal(dw[n], dw2[n])
+
+
 def test_gradient_against_differences():
     c = Case(F32, 1, 3, 2, 1, 32, 32, seed=3)
     d, dx, dw = backward(c)
