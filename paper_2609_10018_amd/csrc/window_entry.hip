@@ -41,10 +41,11 @@ bool set_view(const char* name, const elasto_window_t& a, const elasto_heads_t* 
 }
 
 // Tiles of up to 64 tokens (of `heads` heads together) are loaded at 32-bit
-// offsets from their first row.
+// offsets from their first row; a single head is reached by its address.
 bool check_reach(const char* name, const View& v, int heads) {
   const int64_t limit = kReach;
-  if (v.st > limit || v.sh > limit || 64 * v.st + (heads - 1) * v.sh + 512 >= limit)
+  const int64_t sh = heads > 1 ? v.sh : 0;
+  if (v.st > limit || sh > limit || 64 * v.st + (heads - 1) * sh + 512 >= limit)
     return fail(ELASTO_ERR_INVALID_ARG, "window attention: 64 tokens of %s span nearly 4 GiB or more", name), false;
   return true;
 }

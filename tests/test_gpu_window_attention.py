@@ -400,6 +400,24 @@ def test_cache_offsets_beyond_four_gigabytes():
     assert torch.equal(o, want) and torch.equal(lse, l1)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_heads_four_gigabytes_apart(dtype):
+    """q, k, v and dout of each head in one place, the next head 2^32 bytes on: the same bits as
+    side by side."""
+    t, d = 150, 64
+    c = Case(dtype=dtype, b=1, tq=t, h=2, kv=2, window=40, sinks=3)
+    o, lse = c.forward()
+    want = (o, lse, *c.backward(o, lse))
+    far = (1 << 32) // c.q.element_size()
+    buf = torch.zeros(far + 4 * t * d, dtype=dtype, device="cuda")
+    for i, n in enumerate(("q", "k", "v", "dout")):
+        x = torch.as_strided(buf, (1, t, 2, d), (2 * far, d, far, 1), i * t * d)
+        x.copy_(getattr(c, n))
+        setattr(c, n, x)
+    o2, lse2 = c.forward()
+    assert all(torch.equal(x, y) for x, y in zip(want, (o2, lse2, *c.backward(o2, lse2))))
+
+
 def test_gradients_of_large_and_odd_groups():
     """Groups that do not divide a tile of rows, and one larger than it."""
     for h, kv, dtype in ((7, 1, BF), (33, 1, F32), (40, 1, BF), (71, 1, BF), (130, 2, F32)):

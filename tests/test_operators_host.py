@@ -153,6 +153,22 @@ def test_window_attention_refuses_tiles_wider_than_four_gigabytes(lib):
         assert attn_bwd(lib, **{side: heads(h=1 << 30)}) == INVALID
 
 
+def test_heads_read_one_at_a_time_may_lie_any_distance_apart(lib):
+    """Only the heads of a group are reached at 32-bit offsets from one another.  The calls end at
+    the workspace, which is looked at behind the tensors."""
+    far = heads(t=64, h=1 << 31)                     # bf16: 4 GiB from head to head
+    for side in "kv":
+        assert attn(lib, ws=None, q_tokens=1, k_tokens=8192, window=4096, **{side: far}) == INVALID
+        assert b"the workspace holds" in lib.elasto_last_error()
+        assert attn_bwd(lib, ws=None, **{side: far}) == INVALID
+        assert b"the workspace holds" in lib.elasto_last_error()
+    for side in ("q", "dout"):
+        assert attn_bwd(lib, ws=None, desc=win_desc(heads=4), **{side: far}) == INVALID
+        assert b"the workspace holds" in lib.elasto_last_error()
+        assert attn_bwd(lib, ws=None, **{side: far}) == INVALID
+        assert b"4 GiB" in lib.elasto_last_error()
+
+
 def test_more_work_than_a_launch_holds_is_refused(lib):
     many = dict(batch=1 << 20, heads=16, kv_heads=16, q_tokens=1, k_tokens=10)
     assert attn(lib, **many) == INVALID
