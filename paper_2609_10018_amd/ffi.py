@@ -412,6 +412,20 @@ def _same_device(*tensors) -> int:
     return d
 
 
+_MAX = 2 ** 31 - 1
+
+
+def _fits(*sizes) -> None:
+    """Refuse sizes of more than the C ABI's 32-bit integers, which ctypes would cut off."""
+    if max(sizes) > _MAX:
+        raise ValueError(f"a size of {max(sizes)} does not fit 32 bits")
+
+
+def _int(n) -> int:
+    """n for the C ABI's own checks: one that it refuses where n does not fit 32 bits."""
+    return max(-1, min(int(n), _MAX))
+
+
 def _dtype(t) -> int:
     try:
         return _tt().types[t.dtype]
@@ -472,6 +486,7 @@ def _qk_desc(q, k, cos, sin, q_gamma, k_gamma, positions, lens, eps, interleaved
         rot *= 2
     if (cos is None) != (sin is None) or (cos is not None and cos.shape != sin.shape):
         raise ValueError("cos and sin must be given together, of one shape")
+    _fits(b, t, n, d, other, rows, rot)
     if positions is not None and positions.shape != (b, t):
         raise ValueError(f"positions is {tuple(positions.shape)}, not {(b, t)}")
     f32, i32 = tt.f32, tt.i32
@@ -529,11 +544,12 @@ def _window_desc(q, k, window, sinks, causal, scale, q_lens, k_lens):
     if len(sq) != 4 or len(sk) != 4 or sq[0] != sk[0] or sq[3] != sk[3]:
         raise ValueError(f"q {tuple(sq)} and k {tuple(sk)} do not go together")
     b, tq, h, d = sq
+    _fits(*sq, *sk)
     i32 = _tt().i32
     if scale is None:
         scale = 1.0 / math.sqrt(d or 1)
     a = Window(_dtype(q), b, tq, sk[1], h, sk[2], d, 1 if causal else 0,
-               min(int(window), 2 ** 31 - 1), int(sinks), scale,
+               _int(window), _int(sinks), scale,
                _plain(q_lens, i32, "q_lens", b), _plain(k_lens, i32, "k_lens", b))
     return a, sq, sk, q.dtype
 
@@ -583,6 +599,7 @@ def _rows(t, name: str):
     if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
         raise ValueError(f"{name} must be [rows, classes] with contiguous rows")
     r, c = shape
+    _fits(c)
     return r, c, stride[0] if r > 1 else c
 
 
@@ -595,6 +612,7 @@ def op_top_logits(logits, values, indices, stream=None) -> None:
     if len(shape) != 2 or shape != indices.shape or shape[0] != r:
         raise ValueError(f"values {tuple(shape)} and indices {tuple(indices.shape)} must be "
                          f"[{r}, top]")
+    _fits(shape[1])
     check(load_library().elasto_op_top_logits(
         _dtype(logits), logits.data_ptr(), ld, r, c, shape[1], _plain(values, _tt().f32, "values"),
         _plain(indices, _tt().i32, "indices"), _stream_ptr(stream, dev)))
@@ -616,6 +634,7 @@ def op_distill(logits, teacher_values, teacher_indices, loss, dlogits=None, labe
                 or shape != teacher_indices.shape):
             raise ValueError(f"teacher values and indices must both be [{r}, top]")
         top = shape[1]
+        _fits(top)
     dt = gd = _dtype(logits)
     ldg, grad = ld, None
     if dlogits is not None:
@@ -663,6 +682,7 @@ class GrowthContext:
         if teacher_values.dim() != 2 or teacher_values.shape != teacher_indices.shape or \
                 teacher_values.shape[0] != n:
             raise ValueError(f"teacher values and indices must be [{n}, top]")
+        _fits(n, teacher_values.shape[1])
         _same_device(images, labels, teacher_values, teacher_indices, stats)
         check(self.lib.elasto_growth_step_distill(
             self.g, int(mode), images.data_ptr(), _plain(labels, _tt().i32, "labels", n),

@@ -278,3 +278,41 @@ def test_binding_refuses_shapes_types_and_devices(monkeypatch):
         with pytest.raises(ValueError):
             call()
             raise AssertionError(f"call {i} was accepted")
+
+
+def test_binding_refuses_sizes_beyond_32_bits(lib, monkeypatch):
+    """ctypes cuts integers off at 32 bits: 2^32 + 8 keys would be 8.  (Tensors without that much
+    memory: expanded, or of shapes alone.)"""
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(ffi, "_same_device", lambda *t: None)
+    n = 2 ** 32 + 8
+    q = torch.zeros(1, 8, 2, 64)
+
+    def wide(axis, size=n):
+        shape = [1, 1, 1, 64]
+        shape[axis] = size
+        return torch.zeros(1, 1, 1, 64).expand(shape)
+
+    def meta(*shape, dtype=torch.float32):
+        return torch.empty(shape, dtype=dtype, device="meta")
+
+    i32 = torch.int32
+    for call in (
+            lambda: ffi.window_attention_workspace(q, wide(1), 8),
+            lambda: ffi.window_attention_workspace(wide(1), q[:, :, :1], 8),
+            lambda: ffi.window_attention_workspace(wide(0), wide(0), 8),
+            lambda: ffi.window_attention_workspace(wide(2), wide(2, 1), 8),
+            lambda: ffi.qk_norm_rotate_workspace(wide(0), None),
+            lambda: ffi.qk_norm_rotate_workspace(None, wide(1)),
+            lambda: ffi.qk_norm_rotate_workspace(wide(1, 3), wide(2)),
+            lambda: ffi.op_qk_norm_rotate(q, None, q, None, cos=meta(n, 32), sin=meta(n, 32)),
+            lambda: ffi.op_top_logits(meta(1, n), meta(1, 2), meta(1, 2, dtype=i32)),
+            lambda: ffi.op_top_logits(meta(1, 9), meta(1, n), meta(1, n, dtype=i32)),
+            lambda: ffi.op_distill(meta(1, n), meta(1, 2), meta(1, 2, dtype=i32), meta(1)),
+            lambda: ffi.op_distill(meta(1, 9), meta(1, n), meta(1, n, dtype=i32), meta(1))):
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
+    for kw in (dict(window=8, sinks=n), dict(window=8, sinks=8 - 2 ** 32), dict(window=8 - 2 ** 32)):
+        with pytest.raises(ffi.ElastoError):
+            ffi.window_attention_workspace(q, q, **kw)
+    assert ffi.window_attention_workspace(q, q, n) == ffi.window_attention_workspace(q, q, 8)
