@@ -385,7 +385,7 @@ def op_attention(dtype: int, qkv, qkv_stride: int, o, o_stride: int, batch: int,
 
 # Per-call work of the operators below is kept small: a call on a few tokens
 # takes less time on the GPU than these checks would if they formatted names.
-_torch = None        # the module, its element types and its current-device call, at the first use
+_torch = None        # torch's element types and its cuda module, at the first use
 
 
 class _Torch:
@@ -393,7 +393,7 @@ class _Torch:
         import torch
         self.f32, self.i32, self.u8 = torch.float32, torch.int32, torch.uint8
         self.types = {torch.bfloat16: BF16, torch.float32: FP32}
-        self.device = torch.cuda.current_device
+        self.cuda = torch.cuda
 
 
 def _tt() -> _Torch:
@@ -405,7 +405,7 @@ def _tt() -> _Torch:
 
 def _same_device(*tensors) -> int:
     """Refuse tensors that do not all lie on the current device: the kernels run there."""
-    d = _tt().device()
+    d = _tt().cuda.current_device()
     for t in tensors:
         if t is not None and t.get_device() != d:
             raise ValueError(f"a tensor lies on {t.device}, the current device is cuda:{d}")

@@ -316,3 +316,12 @@ def test_binding_refuses_sizes_beyond_32_bits(lib, monkeypatch):
         with pytest.raises(ffi.ElastoError):
             ffi.window_attention_workspace(q, q, **kw)
     assert ffi.window_attention_workspace(q, q, n) == ffi.window_attention_workspace(q, q, 8)
+
+
+def test_binding_asks_torch_for_the_current_device_at_each_call(monkeypatch):
+    torch = pytest.importorskip("torch")
+    monkeypatch.setattr(ffi, "_torch", None)
+    for device in (3, 5):
+        with monkeypatch.context() as m:
+            m.setattr(torch.cuda, "current_device", lambda d=device: d)
+            assert ffi._same_device() == device
