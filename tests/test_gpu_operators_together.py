@@ -217,6 +217,42 @@ def test_distilling_step_without_a_teacher_part_is_the_labels_step():
     assert abs(s0[1] - s1[1]) <= 2.0 ** -8 * s0[1]
 
 
+@pytest.mark.parametrize("k,tau", [(0, 1.0), (1, 3.0)])
+def test_distilling_step_without_a_teacher_part_updates_the_labels_weights(k, tau):
+    """alpha 0: every tensor's update, of this step and of elasto_growth_step, against the same
+    oracle under the bar of the step with labels (the loss and the norm alone would not tell a
+    gradient of the wrong sign or in the wrong tensor)."""
+    import test_gpu_growth as tg
+    cfg, batch = CONFIGS["vit_ti"], 2
+    w, t = inputs.make_weights(cfg), inputs.make_dn_table(cfg)
+    x, y = inputs.make_images(cfg, batch), np.array([3, 900])
+    xd = torch.from_numpy(x).to(torch.bfloat16).cuda()
+    yd = torch.from_numpy(y.astype(np.int32)).cuda()
+    ref = og.growth_step(inputs.stored_weights(cfg, w), cfg, t, k, inputs.stored_images(cfg, x), y,
+                         lr=1.0, clip=1e30)
+    for distill in (False, True):
+        vit = ffi.ElasticViT(cfg, w, t, batch)
+        gc = ffi.GrowthContext(vit, batch)
+        packed0 = gc.read(0).copy()
+        stats = torch.zeros(3, device="cuda")
+        if distill:
+            none = torch.full((batch, 1), -1, dtype=torch.int32).cuda()
+            gc.step_distill(k, xd, yd, torch.zeros(batch, 1, device="cuda"), none, 1.0, 1e30,
+                            temperature=tau, alpha=0.0, stats=stats)
+        else:
+            gc.step(k, xd, yd, 1.0, 1e30, stats)
+        r = dict(cfg=cfg, t=t, ref=ref, packed0=packed0, packed1=gc.read(0), master1=gc.read(1),
+                 stats=stats.cpu().numpy(), k=k)
+        assert abs(r["stats"][0] - ref["loss"]) <= tg.LOSS_TOL * abs(ref["loss"])
+        pairs = tg._applied_grads(r, 1.0)
+        gmax = max(np.max(np.abs(e)) for _, _, _, e in pairs)
+        for l, tensor, got, exp in pairs:
+            err = np.max(np.abs(got - exp)) / max(np.max(np.abs(exp)), 1e-3 * gmax)
+            assert err < tg.GRAD_TOL, (distill, l, tensor, err)
+        gc.close()
+        vit.close()
+
+
 def test_distilling_step_refuses_bad_calls():
     cfg = CONFIGS["vit_ti"]
     vit = ffi.ElasticViT(cfg, inputs.make_weights(cfg), inputs.make_dn_table(cfg), 2)
