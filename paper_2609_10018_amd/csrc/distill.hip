@@ -19,7 +19,8 @@
 // Bound by memory: the logits once, the gradient once.  2048 x 131072 bf16 with its
 // gradient 241 us, 4.45 TB/s (a copy of that size runs at 5.1); the loss alone,
 // 1000 x 50021 fp32, 35-39 us.  Both temperatures together take two exponentials
-// an element and walk: 2048 x 131072 bf16, 302 us, bound by the vector ALU.
+// an element and walk, which the memory's time still covers: 2048 x 131072 bf16
+// 263 us (with labels and one temperature 255).
 #include <math.h>
 
 #include <algorithm>
@@ -273,6 +274,12 @@ __global__ __launch_bounds__(N) void distill_kernel(DistillP<T, G> p) {
   }
 }
 
+// Whether the sums of both temperatures are needed and differ.  With no labels, or
+// none of the teacher, one sum does: at the temperature that is needed.
+bool two_sums(const DistillArgs& a) {
+  return a.labels && a.alpha > 0.0f && a.alpha < 1.0f && a.temperature != 1.0f;
+}
+
 template <typename T, typename G, int N>
 hipError_t launch(const DistillArgs& a, hipStream_t s) {
   DistillP<T, G> p;
@@ -289,12 +296,9 @@ hipError_t launch(const DistillArgs& a, hipStream_t s) {
   p.top = a.top;
   p.alpha = a.alpha;
   p.beta = a.labels ? 1.0f - a.alpha : 0.0f;
-  p.tau = a.temperature;
+  p.tau = a.alpha == 0.0f ? 1.0f : a.temperature;
   p.scale = a.scale;
-  // With no labels, or none of the teacher, one sum does: at the temperature
-  // that is needed.
-  if (a.alpha == 0.0f) p.tau = 1.0f;
-  const bool two = a.labels && a.alpha > 0.0f && a.alpha < 1.0f && p.tau != 1.0f;
+  const bool two = two_sums(a);
   hipError_t e = hipSuccess;
   for (p.row0 = 0; p.row0 < a.rows && e == hipSuccess; p.row0 += kLaunchRows) {
     const unsigned rows = (unsigned)std::min<int64_t>(a.rows - p.row0, kLaunchRows);
@@ -307,18 +311,22 @@ hipError_t launch(const DistillArgs& a, hipStream_t s) {
   return e;
 }
 
-// More threads than teacher entries, one for the label among them; about one run
+// More threads than teacher entries, one for the label among them; and about one run
 // of eight a thread for short rows, of which many run at once (4096 x 1000 fp32:
-// 34 us with 512 threads, 19 with 256, 14 with 128); and all of a CU's for two
-// rows where the rows at work, read a second time for the gradient, would not
-// stay in the cache behind L2 (2048 x 131072 bf16: 257 us with 512 threads, 247
-// with 1024; 4096 x 32000: 122 and 190).  The loss alone takes as many, so that
-// its bits are the same.
+// 34 us with 512 threads, 19 with 256, 14 with 128).  Long rows take 1024, which
+// hold two rows on a CU where 512 hold four: the rows at work, read a second time for
+// the gradient, would not stay in the cache behind L2 (2048 x 131072 bf16: 257 us
+// with 512 threads, 247 with 1024; 4096 x 32000: 122 and 190).  At two temperatures
+// 1024 threads take 87 registers, for the sums of 16 waves, and a CU holds one row of
+// them: they pay for longer rows only (2048 x 131072 bf16: 263 us with 512 threads,
+// 310 with 1024; 1600 x 160000: 292 and 302; 1300 x 200003: 332 and 302; 1024 x
+// 65536 fp32: 138 and 158; 400 x 200003: 208 and 200).  The loss alone takes as
+// many, so that its bits are the same.
 template <typename T, typename G>
 hipError_t launch_threads(const DistillArgs& a, hipStream_t s) {
   if (a.classes <= 1024 && a.top < 128) return launch<T, G, 128>(a, s);
   if (a.classes <= 2048 && a.top < 256) return launch<T, G, 256>(a, s);
-  if ((int64_t)a.classes * (int)sizeof(T) > 200 * 1024) return launch<T, G, 1024>(a, s);
+  if ((int64_t)a.classes * (int)sizeof(T) > (two_sums(a) ? 350 : 200) * 1024) return launch<T, G, 1024>(a, s);
   return launch<T, G, 512>(a, s);
 }
 

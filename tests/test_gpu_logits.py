@@ -241,6 +241,17 @@ def test_distill(kw):
     assert torch.equal(alone, loss)
 
 
+@pytest.mark.parametrize("dtype,classes", [(BF, 110000), (BF, 179200), (BF, 179203), (F32, 60001),
+                                           (F32, 89600), (F32, 89603)])
+@pytest.mark.parametrize("tau", [1.0, 2.0])
+def test_distill_long_rows_at_one_and_two_temperatures(dtype, classes, tau):
+    """To either side of the lengths from which a workgroup has more threads."""
+    c = Distill(dtype=dtype, grad=dtype, rows=2, classes=classes, top=40, tau=tau)
+    loss, grad = c.run()
+    c.check(loss, grad)
+    assert torch.equal(c.run(grad=False)[0], loss)
+
+
 @pytest.mark.parametrize("dtype,classes", [(F32, 300), (BF, 9001)])
 def test_distill_over_its_own_logits(dtype, classes):
     c = Distill(dtype=dtype, grad=dtype, classes=classes)
