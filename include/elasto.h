@@ -510,8 +510,10 @@ elasto_status_t elasto_qk_norm_rotate_workspace(const elasto_qk_norm_t* desc, in
  * keys and values that none of its queries sees (before the window of the first
  * one, say), are not used: they may be anything, NaN included.  Nothing is
  * written behind the lengths; keys within them that no query sees get zero
- * gradients.  (An infinity or NaN in a row that some see may also reach others
- * of its sequence that do not.)
+ * gradients.  (An infinity or NaN in a key or value that some queries see may
+ * also reach others of its sequence that do not; one in a query within the
+ * lengths, its o, lse or dout reaches its own results and may reach the
+ * gradients of keys that it does not see.)
  * BF16: products of bf16 with fp32 sums, softmax statistics in fp32, the
  * probabilities (backward: also the gradients of the scores) rounded to bf16
  * for the products that sum them.  FP32: fp32 throughout.  Results are the
@@ -569,8 +571,8 @@ elasto_status_t elasto_op_top_logits(int32_t dtype, const void* logits, int64_t 
  *               - log softmax(z / temperature)[index_i])
  *             + (1 - alpha) * (log sum exp(z) - z[label]),
  * and, where dlogits is given, its gradient with respect to z times
- * scale * row_weight[r] (row_weight NULL: 1) in dlogits row r, row stride ldg,
- * of type grad_dtype.  An index of -1 is an entry that is not there; a class
+ * scale * row_weight[r] (row_weight NULL: 1; neither factor is in loss[r]) in
+ * dlogits row r, row stride ldg, of type grad_dtype.  An index of -1 is an entry that is not there; a class
  * may come more than once.  A row without entries (or whose values are all
  * -infinity) has no teacher part.  Another index outside [0, classes), or such
  * a label, makes the row's loss NaN (it adds nothing to the gradient).  A row

@@ -18,9 +18,9 @@
 //
 // Bound by memory: the logits once, the gradient once.  2048 x 131072 bf16 with its
 // gradient 241 us, 4.45 TB/s (a copy of that size runs at 5.1); the loss alone,
-// 1000 x 50021 fp32, 35-39 us.  Both temperatures together take two exponentials
-// an element and walk, which the memory's time still covers: 2048 x 131072 bf16
-// 263 us (with labels and one temperature 255).
+// 1000 x 50021 fp32, 39 us, 5.1.  Both temperatures together take two exponentials
+// an element and walk (vector ALU 67% of the cycles), which the memory's time nearly
+// covers: 2048 x 131072 bf16 266 us (with labels and one temperature 255).
 #include <math.h>
 
 #include <algorithm>
@@ -247,6 +247,9 @@ __global__ __launch_bounds__(N) void distill_kernel(DistillP<T, G> p) {
     else
       return f1 * pa(x);
   };
+  // Single stores where the two rows reach 16 bytes at different columns (fp32 logits
+  // and a bf16 gradient: half of the rows unless classes are a multiple of 8; 1000 x
+  // 50021 89 us, 1000 x 50024 82).
   const bool wide = (reinterpret_cast<uintptr_t>(g + span.head) & 15) == 0;
   walk_row<N>(z, span, tid,
               [&](int i, const float* v) {
@@ -318,7 +321,7 @@ hipError_t launch(const DistillArgs& a, hipStream_t s) {
 // the gradient, would not stay in the cache behind L2 (2048 x 131072 bf16: 257 us
 // with 512 threads, 247 with 1024; 4096 x 32000: 122 and 190).  At two temperatures
 // 1024 threads take 87 registers, for the sums of 16 waves, and a CU holds one row of
-// them: they pay for longer rows only (2048 x 131072 bf16: 263 us with 512 threads,
+// them: they pay for longer rows only (2048 x 131072 bf16: 266 us with 512 threads,
 // 310 with 1024; 1600 x 160000: 292 and 302; 1300 x 200003: 332 and 302; 1024 x
 // 65536 fp32: 138 and 158; 400 x 200003: 208 and 200).  The loss alone takes as
 // many, so that its bits are the same.

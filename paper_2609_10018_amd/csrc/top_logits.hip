@@ -15,10 +15,12 @@
 // The order of collecting does not matter to the result.
 //
 // A thread keeps the largest value of each of its runs of eight, so the second
-// walk reads only runs that hold a key from the bound on again.  Bound by memory,
-// one pass over the logits: 1024 x 100003 bf16, top 64, 52-57 us (3.6-3.9 TB/s; a
-// read-only sum of 2 GiB runs at 4.0).  64 x 1000 fp32, top 16: 6 us, a launch and
-// the chain of one wave.
+// walk reads only runs that hold a key from the bound on again: one pass over the
+// logits.  1024 x 100003 bf16, top 64: 55-59 us by the card, 3.5-3.7 TB/s.  Kernels that
+// only read reach 5.1 on as many bytes; here two rows on a CU read, sort, collect and
+// sort one after the other, and their waves wait 70% of the time.  64 x 1000 fp32, top
+// 16: 6 us, a launch and the chain of one wave; 4096 x 1000 12 us (1.4 TB/s): 16 KB of
+// LDS a row leave a SIMD two or three waves.
 #include <algorithm>
 #include <type_traits>
 

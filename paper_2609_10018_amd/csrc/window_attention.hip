@@ -7,9 +7,11 @@
 //
 // Scores are taken transposed, S^T = K Q^T: a lane holds one row's scores, so
 // the softmax needs one exchange between the half-waves a tile, and the
-// probabilities (rounded to bf16 on the bf16 path; their sum is taken before, in
-// fp32, since lse is an fp32 result) are the operand of O^T = V^T P^T without
-// moving.
+// probabilities are the operand of O^T = V^T P^T without moving.  On the bf16
+// path they are rounded to bf16 for it, since an fp32 product runs at a ninth of
+// the rate (155 and 1400 TFLOP/s): against 64 bits o is off by 0.0023 of itself, root
+// mean square, of which rounding o alone makes 0.0017.  Their sum is taken before, in
+// fp32, since lse is an fp32 result.
 //
 // Two shapes of a workgroup of four waves:
 // * rows: 128 rows, 32 a wave, which share each tile of keys;
@@ -20,17 +22,23 @@
 // maximum and sum of each part go with it).
 //
 // Every product takes one operand from LDS (1 KB an instruction, at the full rate
-// all of the LDS's 128 bytes a cycle) and one from registers, where q, the
-// probabilities and the sums stay.  What bounds it, and measured times:
-// * heads of 64: the vector ALU (64 keys x 32 rows: 16 matrix instructions of 32
-//   cycles, ~155 vector ones, 32 of them exponentials; it is busy 73% of the
-//   cycles, the matrix cores 31%).  8 x 4097 tokens, 12 heads, 511 keys to either
-//   side: 150 us, 645 TFLOP/s;
+// half of what the LDS gives: 16-byte reads alone ran at 229 bytes a cycle of 2.4 GHz
+// and CU) and one from registers, where q, the probabilities and the sums stay.
+// What bounds it, and measured times (of several cards):
+// * heads of 64: the vector ALU most (64 keys x 32 rows: 16 matrix instructions of 32
+//   cycles, ~155 vector ones, 32 of them exponentials): it is busy 60% of the
+//   launch's cycles, the matrix cores 31%, the LDS 16%, and a SIMD holds three waves on
+//   average.  8 x 4097 tokens, 12 heads, 511 keys to either side: 150-155 us, 640
+//   TFLOP/s;
+// * heads of 128: no unit alone, with two waves a SIMD, as 204 registers allow (vector
+//   ALU 41%, matrix cores 37%).  Causal, 16/4 heads: 2 x 8192 tokens, 1024 keys: 176-188
+//   us, 690-730 TFLOP/s; 2 x 4096, all keys: 158, 870;
 // * single tokens: the cache's bytes.  32 sequences, 16/4 heads of 128, 2048 of
-//   8192 keys each: 28 us, 4.7 TB/s (a read-only sum of 2 GiB: 4.0, a copy 5.1);
+//   8192 keys each: 32 us with other tensors at each call, 4.2 TB/s (a copy: 5.1),
+//   28 with two sets of them in turn; fp32 70 us, 3.9 TB/s;
 // * fp32: matrix instructions of 64 cycles, and at small sizes the latency of a
 //   wave's two or three tiles.  5 x 777 padded tokens, 6 heads of 64, 200 keys:
-//   25 us; 2 x 2048 x 8 heads of 128, 512 keys: 118 us.
+//   25 us; 2 x 2048 x 8 heads of 128, 512 keys: 117-120 us.
 #include <math.h>
 
 #include <algorithm>
@@ -68,8 +76,8 @@ struct Shape {
   static constexpr int kBuffers = KEYS && sizeof(T) == 4 ? 1 : 2;
   // Of 64 features even that one holds K and V in turns, V on its way during the
   // softmax: three workgroups on a CU (5 x 777 tokens x 6 heads, 200 keys: 29 us
-  // with both at once, 22 in turns; 2 x 2048 x 8, 512 keys, two whole rounds
-  // otherwise: 56 and 60).  Heads of 128 have no registers for more workgroups.
+  // with both at once, 22 in turns, though 4 of its registers are spilled; 2 x 2048
+  // x 8, 512 keys, two whole rounds otherwise: 56 and 60).  Heads of 128 have no registers for more workgroups.
   static constexpr bool kTurns = KEYS && sizeof(T) == 4 && HD == 64;
   static constexpr int kStaged = (kTurns ? 1 : 2) * kTile;  // of a tile
   static constexpr int kPerSimd = kTurns ? 3 : sizeof(T) == 2 || HD == 64 ? 2 : 1;  // waves
@@ -434,9 +442,9 @@ Cut cut_of(const elasto_window_t& a) {
   const int64_t keys = std::min<int64_t>(a.k_tokens, reach + a.sinks);
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>(keys / 256, 128));
   if (!c.keys) {
-    // Two workgroups a CU, if whole shares make them: 5 x 1023 tokens x 12 heads of
-    // 64 (480 of them) in 1 share 33 us, in 2 42; 2 x 2048 x 8, causal (256), in 1
-    // 41, in 2 37.
+    // Two workgroups a CU, if whole shares make them (a CU holds two of heads of 128,
+    // four of 64 in bf16, but two keep it busy): 5 x 1023 tokens x 12 heads of 64 (480 of
+    // them) in 1 share 33 us, in 2 42; 2 x 2048 x 8, causal (256), in 1 41, in 2 37.
     c.splits = (int)std::max<int64_t>(1, std::min(2 * kCUs / std::max<int64_t>(blocks, 1), most));
     return c;
   }

@@ -13,15 +13,19 @@
 // cost is less than adding dq up in memory would.
 //
 // P and dS are rounded to bf16 (bf16 path) as operands of the products that
-// sum them; all sums are fp32.
+// sum them, for the same reason and price as in the forward pass (root mean square
+// 0.0024 of the gradients against 64 bits, 0.0017 for rounding the results alone);
+// all sums are fp32.
 //
-// Bound by the matrix cores and what feeds them: each product takes an operand
-// from LDS, 1 KB an instruction, which at the full rate is all that the LDS gives.
-// 2 x 8192 tokens, 16/4 heads of 128, 1024 keys and 4 sinks: 516 us (rows ~215,
-// keys ~265, sinks 25, join 5); counted as five products 627 TFLOP/s, as the seven
-// that run 880, the key kernel by itself 1.1 PFLOP/s.  Without its exponentials
-// and masks the row kernel ran at 1.24, a library product of 8192^3 runs at 1.4.
-// fp32, 2 x 2048 x 8 heads of 128, 512 keys: 350 us.
+// Bound by no unit alone: of the launches' cycles the matrix cores are busy 43%
+// (rows) and 40% (keys), the vector ALU 33% and 27%, the LDS 22% and 25%.  Registers
+// allow two waves a SIMD, each of which takes a sub-block's products, exponentials
+// and products in turn, with two barriers a tile.  2 x 8192 tokens, 16/4 heads of
+// 128, 1024 keys and 4 sinks: 514-529 us by the card (rows ~220, keys ~280, sinks 25,
+// join 6 under a profiler); counted as five products 610-630 TFLOP/s, as the seven
+// that run 850-880.  Without its exponentials and masks the row kernel ran at 1.24
+// PFLOP/s, a library product of 8192^3 runs at 1.4.  fp32, 2 x 2048 x 8 heads of 128,
+// 512 keys: 350 us.
 //
 // A key among the sinks is seen by every later row.  The key kernel takes the
 // rows that see the first tile's keys through their windows, as for any tile;
