@@ -589,6 +589,52 @@ elasto_status_t elasto_op_distill(int32_t dtype, const void* logits, int64_t ld,
                                   int32_t grad_dtype, void* dlogits, int64_t ldg,
                                   void* hip_stream);
 
+/* Softmax cross-entropy of a linear layer over many classes, z = x W^T + b,
+ * without the logits z in memory: for each of `rows` rows
+ *   lse[r] = log sum_c exp(z[r][c]),  loss[r] = lse[r] - z[r][labels[r]],
+ * and the gradients, with dz[r][c] = row_weight[r] (softmax(z[r])[c]
+ * - [c = labels[r]]) (row_weight NULL: 1; it is not in loss[r]),
+ *   dx = scale dz W,  dweight = scale dz^T x,  dbias = scale sum_r dz[r].
+ * x is [rows][dim] with row stride ldx (elements), weight [classes][dim] with
+ * ldw, bias (or NULL) fp32 [classes].  A row of weight 0 is not used, whatever
+ * it holds: its loss, lse and gradients are 0.  A label outside [0, classes)
+ * makes the row's loss NaN, and the row adds nothing to the gradients.  An
+ * entry of bias of -infinity leaves its class out.
+ * BF16: products of bf16 with fp32 sums, softmax in fp32; dz is rounded to bf16
+ * for the products that sum it (not for dbias); dx and dweight are bf16, rounded
+ * once.  FP32: fp32 throughout.  Results are the same bits every time.
+ * Needs dim a multiple of 8 (FP32: 4), x, weight and their strides multiples
+ * of 16 bytes, dim and strides at most 2^20, rows at most 2^24, classes at most
+ * 2^30, and a product of any two of rows, classes and dim below 2^37. */
+typedef struct {
+  int32_t dtype, dim, classes;
+  int64_t rows;
+  const void* x;
+  int64_t ldx;
+  const void* weight;
+  int64_t ldw;
+  const float* bias;       /* device [classes] or NULL */
+  const int32_t* labels;   /* device [rows]            */
+  const float* row_weight; /* device [rows] or NULL    */
+} elasto_linear_ce_t;
+
+/* loss fp32 [rows]; lse fp32 [rows] or NULL.  The workspace
+ * (elasto_linear_ce_workspace, 256-byte aligned) is free again when the call's
+ * work is done: calls that may overlap need one each. */
+elasto_status_t elasto_op_linear_ce(const elasto_linear_ce_t* desc, float* loss, float* lse,
+                                    void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* The gradients, from the forward's lse; dx [rows][dim] and dweight
+ * [classes][dim] in the type of x, dbias fp32 [classes], each or NULL.  With no
+ * rows dweight and dbias become 0. */
+elasto_status_t elasto_op_linear_ce_bwd(const elasto_linear_ce_t* desc, const float* lse,
+                                        float scale, void* dx, int64_t lddx, void* dweight,
+                                        int64_t lddw, float* dbias, void* workspace,
+                                        int64_t workspace_bytes, void* hip_stream);
+/* Bytes of workspace of either call: of dtype, rows, classes and dim alone. */
+elasto_status_t elasto_linear_ce_workspace(const elasto_linear_ce_t* desc, int32_t backward,
+                                           int64_t* bytes);
+
 /* ================================================ growth step (Section 4.2) */
 /* Growing DN mode k re-introduces the weights mode k holds and the next
  * smaller mode k + 1 (the previous level) lacks; mode k + 1's weights are

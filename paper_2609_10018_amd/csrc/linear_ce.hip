@@ -1,0 +1,654 @@
+// Softmax cross-entropy of a linear layer, z = x W^T + b, without keeping z:
+//   lse_r = log sum_c exp(z_rc),  loss_r = lse_r - z_r,label,
+// and with dz = w_r (softmax(z)_rc - [c = label]), w the row's weight,
+//   dx = s dz W,  dW = s dz^T x,  db = s sum_r dz.
+//
+// Forward: each tile of z stays in the accumulators of its workgroup; what leaves it is,
+// for each row, the largest logit of the tile and the sum of exponentials about it.  A
+// second kernel joins the tiles of a row.
+// Backward: z is formed again, in pieces of the classes.  A piece's dz goes to the
+// workspace, rounded to the operands' type (bf16: the two products that sum it would run
+// at a ninth of the rate in fp32), and is the left operand of dx (straight) and of dW
+// (turned).  dx is summed over the pieces, and over parts of a piece where its tiles leave
+// CUs idle, in fp32; everything in a fixed order.
+#include <math.h>
+
+#include <algorithm>
+
+#include "heads.h"
+#include "tile_product.h"
+
+namespace elasto {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct CeP {
+  Matrix x, w, dz;  // dz: the piece's gradient of the logits, [rows][piece]
+  int64_t rows, dim;
+  int64_t c0;  // first class of the piece
+  int64_t classes;  // of the piece (forward: all)
+  const float* bias;
+  const int32_t* labels;
+  const float* weight;
+  const float* lse;
+  float2* part;   // forward: [tiles of classes][rows]
+  float* picked;  // forward: the label's logit
+  const uint32_t* live;
+  float* db_part;  // [tiles of rows][piece]
+  int tiles_m, tiles_n, group;
+  int label_classes;  // all classes
+};
+
+// The tile of workgroup v: each XCD (workgroup v runs on XCD v % 8) takes a run of tiles, in
+// groups of `group` row tiles that share the other operand's panels in its L2.
+__device__ __forceinline__ void tile_of(int v, int tiles_m, int tiles_n, int group, int& tm, int& tn) {
+  const int total = tiles_m * tiles_n, q = total >> 3, r8 = total & 7, xcd = v & 7, idx = v >> 3;
+  const int logical = xcd < r8 ? xcd * (q + 1) + idx : r8 * (q + 1) + (xcd - r8) * q + idx;
+  const int gsz = group * tiles_n, g = logical / gsz, in_group = logical - g * gsz;
+  const int gm = min(group, tiles_m - g * group);
+  tn = in_group / gm;
+  tm = g * group + (in_group - tn * gm);
+}
+
+// Logits of a tile: the accumulators start from the bias, -infinity behind the last class.
+template <typename S>
+__device__ __forceinline__ void logits(char* smem, const CeP& p, int64_t m0, int64_t n0,
+                                       f32x16 (&acc)[S::TM][S::TN]) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c0 = (int)n0 + wave % S::WN * S::WTN + 4 * (lane >> 5);
+#pragma unroll
+  for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int c = c0 + j * 32 + 8 * (e >> 2) + (e & 3);
+      const float b = c < p.classes ? (p.bias ? p.bias[p.c0 + c] : 0.0f) : -INFINITY;
+#pragma unroll
+      for (int i = 0; i < S::TM; ++i) acc[i][j][e] = b;
+    }
+  const Matrix w = {p.w.p + p.c0 * p.w.ld, p.w.ld};
+  tile_product<S, false, false, false>(smem, p.x, w, p.rows, p.classes, m0, n0, 0, p.dim, nullptr, acc);
+}
+
+// A reference for the exponentials of values up to m.
+__device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.0f : m; }
+
+template <typename S>
+__global__ __launch_bounds__(S::kThreads) void ce_forward_kernel(CeP p) {
+  __shared__ __attribute__((aligned(1024))) char smem[2 * S::kStage];
+  int tm, tn;
+  tile_of(blockIdx.x, p.tiles_m, p.tiles_n, p.group, tm, tn);
+  const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
+  f32x16 acc[S::TM][S::TN];
+  logits<S>(smem, p, m0, n0, acc);
+  __syncthreads();
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / S::WN, wn = wave % S::WN, lr = lane & 31, lg = lane >> 5;
+  float2* red = reinterpret_cast<float2*>(smem);  // [WN][BM]
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i) {
+    float m = acc[i][0][0];
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) m = fmaxf(m, acc[i][j][e]);
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    const float ref = reference(m);
+    float s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f((acc[i][j][e] - ref) * kLog2e);
+    s += __shfl_xor(s, 32, 64);
+    const int r = wm * S::WTM + i * 32 + lr;
+    if (lg == 0) red[wn * S::BM + r] = make_float2(m, s);
+    // The label's logit, by the one lane that holds it.
+    const int64_t row = m0 + r;
+    const int first = (int)n0 + wn * S::WTN;
+    const int y = row < p.rows ? p.labels[row] : -1;
+    if (y >= first && y < first + S::WTN && y < p.classes)
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (y == first + j * 32 + 8 * (e >> 2) + 4 * lg + (e & 3)) p.picked[row] = acc[i][j][e];
+  }
+  __syncthreads();
+  for (int r = tid; r < S::BM && m0 + r < p.rows; r += S::kThreads) {
+    float2 t = red[r];
+    float m = t.x;
+#pragma unroll
+    for (int k = 1; k < S::WN; ++k) m = fmaxf(m, red[k * S::BM + r].x);
+    const float ref = reference(m);
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < S::WN; ++k) {
+      const float2 o = red[k * S::BM + r];
+      s += o.y * __builtin_amdgcn_exp2f((o.x - ref) * kLog2e);
+    }
+    p.part[(int64_t)tn * p.rows + m0 + r] = make_float2(m, s);
+  }
+}
+
+// Joins the tiles of 64 rows: 16 waves take the tiles in turn.
+struct JoinP {
+  const float2* part;
+  const float *picked, *weight;
+  const int32_t* labels;
+  float *loss, *lse;
+  int64_t rows;
+  int tiles, classes;
+};
+__global__ __launch_bounds__(1024) void ce_join_kernel(JoinP p) {
+  __shared__ float2 red[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = (int64_t)blockIdx.x * 64 + lane;
+  const bool there = row < p.rows;
+  float m = -INFINITY, s = 0.0f;
+  if (there)
+#pragma unroll 4
+    for (int t = wave; t < p.tiles; t += 16) {
+      const float2 o = p.part[(int64_t)t * p.rows + row];
+      const float n = fmaxf(m, o.x), ref = reference(n);
+      s = s * __builtin_amdgcn_exp2f((m - ref) * kLog2e) + o.y * __builtin_amdgcn_exp2f((o.x - ref) * kLog2e);
+      m = n;
+    }
+  red[wave][lane] = make_float2(m, s);
+  __syncthreads();
+  if (wave != 0 || !there) return;
+  float top = m;
+  for (int k = 1; k < 16; ++k) top = fmaxf(top, red[k][lane].x);
+  const float ref = reference(top);
+  s = 0.0f;
+  for (int k = 0; k < 16; ++k) s += red[k][lane].y * __builtin_amdgcn_exp2f((red[k][lane].x - ref) * kLog2e);
+  const float above = log2f(s) * kLn2;
+  const bool out = p.weight && p.weight[row] == 0.0f;
+  const int y = p.labels[row];
+  const bool ok = y >= 0 && y < p.classes;
+  p.loss[row] = out ? 0.0f : ok ? above + (ref - p.picked[row]) : NAN;
+  if (p.lse) p.lse[row] = out ? 0.0f : above + ref;
+}
+
+// One bit a row: whether it gives the gradients anything.
+__global__ __launch_bounds__(256) void ce_live_kernel(const float* weight, const int32_t* labels, int64_t rows,
+                                                      int classes, uint32_t* live) {
+  const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  bool on = false;
+  if (r < rows) {
+    const int y = labels[r];
+    on = y >= 0 && y < classes && !(weight && weight[r] == 0.0f);
+  }
+  const uint64_t b = __ballot(on);
+  if ((threadIdx.x & 31) == 0) live[r >> 5] = (uint32_t)(b >> (threadIdx.x & 32));
+}
+
+__device__ __forceinline__ void store4(float* p, const float* v) {
+  *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+}
+__device__ __forceinline__ void store4(uint16_t* p, const float* v) {
+  *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+}
+
+// dz of one tile of the piece.
+template <typename S>
+__global__ __launch_bounds__(S::kThreads) void ce_dz_kernel(CeP p) {
+  typedef typename S::T T;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * S::kStage];
+  int tm, tn;
+  tile_of(blockIdx.x, p.tiles_m, p.tiles_n, p.group, tm, tn);
+  const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
+  f32x16 acc[S::TM][S::TN];
+  logits<S>(smem, p, m0, n0, acc);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave / S::WN, wn = wave % S::WN, lr = lane & 31, lg = lane >> 5;
+  const int first = (int)n0 + wn * S::WTN;  // of the wave's classes in the piece
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i) {
+    const int64_t row = m0 + wm * S::WTM + i * 32 + lr;
+    float w = 0.0f, lse = 0.0f;
+    int y = -1;
+    if (row < p.rows) {
+      y = p.labels[row];
+      w = y >= 0 && y < p.label_classes ? (p.weight ? p.weight[row] : 1.0f) : 0.0f;
+      lse = p.lse[row];
+    }
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float v = __builtin_amdgcn_exp2f((acc[i][j][e] - lse) * kLog2e);
+        acc[i][j][e] = w != 0.0f ? w * v : 0.0f;
+      }
+    const int64_t at = y - p.c0 - first;
+    if (w != 0.0f && at >= 0 && at < S::WTN)
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (at == j * 32 + 8 * (e >> 2) + 4 * lg + (e & 3)) acc[i][j][e] -= w;
+    if (row < p.rows) {
+      T* out = reinterpret_cast<T*>(const_cast<char*>(p.dz.p) + row * p.dz.ld) + first + 4 * lg;
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float v[4] = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+          store4(out + j * 32 + 8 * g, v);
+        }
+    }
+  }
+  if (!p.db_part) return;
+  // Sums over the tile's rows: over the wave's blocks, its lanes, then the waves.
+  __syncthreads();
+  float* red = reinterpret_cast<float*>(smem);  // [WM][BN]
+#pragma unroll
+  for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      float s = acc[0][j][e];
+#pragma unroll
+      for (int i = 1; i < S::TM; ++i) s += acc[i][j][e];
+#pragma unroll
+      for (int o = 16; o >= 1; o >>= 1) s += __shfl_xor(s, o, 64);
+      if (lr == 0) red[wm * S::BN + wn * S::WTN + j * 32 + 8 * (e >> 2) + 4 * lg + (e & 3)] = s;
+    }
+  __syncthreads();
+  for (int c = tid; c < S::BN; c += S::kThreads) {
+    float s = red[c];
+#pragma unroll
+    for (int k = 1; k < S::WM; ++k) s += red[k * S::BN + c];
+    p.db_part[(int64_t)tm * p.tiles_n * S::BN + n0 + c] = s;
+  }
+}
+
+__global__ __launch_bounds__(256) void ce_db_kernel(const float* part, int tiles, int64_t ld, int64_t n, float scale,
+                                                    float* db) {
+  for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < n; c += (int64_t)gridDim.x * 256) {
+    float s = 0.0f;
+#pragma unroll 8
+    for (int t = 0; t < tiles; ++t) s += part[t * ld + c];
+    db[c] = s * scale;
+  }
+}
+
+// C = s A B^T of one tile: dx (A = dz, B = W turned) and dW (A = dz turned, B = x turned).
+struct ProductP {
+  Matrix a, b;
+  int64_t M, N, K;
+  char* out;        // the result, of T
+  int64_t ldo;      // bytes
+  float* sum;       // or fp32 sums [split][M][N], N's stride ld_sum
+  int64_t ld_sum;
+  bool add;         // to what sum holds
+  float scale;
+  const uint32_t* live;
+  int tiles_m, tiles_n, group, split;
+  int64_t chunk;    // of K
+};
+template <typename S, bool TA, bool LIVE>
+__global__ __launch_bounds__(S::kThreads) void ce_product_kernel(ProductP p) {
+  typedef typename S::T T;
+  __shared__ __attribute__((aligned(1024))) char smem[2 * S::kStage];
+  const int tiles = p.tiles_m * p.tiles_n, part = blockIdx.x / tiles;
+  int tm, tn;
+  tile_of(blockIdx.x - part * tiles, p.tiles_m, p.tiles_n, p.group, tm, tn);
+  const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
+  const int64_t k0 = part * p.chunk, k1 = min(p.K, k0 + p.chunk);
+  f32x16 acc[S::TM][S::TN];
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+  tile_product<S, TA, true, LIVE>(smem, p.a, p.b, p.M, p.N, m0, n0, k0, k1, p.live, acc);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t r0 = m0 + wave / S::WN * S::WTM + (lane & 31);
+  const int64_t c0 = n0 + wave % S::WN * S::WTN + 4 * (lane >> 5);
+#pragma unroll
+  for (int i = 0; i < S::TM; ++i) {
+    const int64_t r = r0 + i * 32;
+    if (r >= p.M) continue;
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int64_t c = c0 + j * 32 + 8 * g;
+        if (c >= p.N) continue;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * g + e];
+        if (p.sum) {
+          float* at = p.sum + (part * p.M + r) * p.ld_sum + c;
+          if (p.add) {
+            const f32x4 o = *reinterpret_cast<const f32x4*>(at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += o[e];
+          }
+          store4(at, v);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] *= p.scale;
+          store4(reinterpret_cast<T*>(p.out + r * p.ldo) + c, v);
+        }
+      }
+  }
+}
+
+// dx = s times the sum of the parts.
+template <typename T>
+__global__ __launch_bounds__(256) void ce_sum_kernel(const float* sum, int split, int64_t M, int64_t N, float scale,
+                                                     char* out, int64_t ldo) {
+  const int64_t quads = N / 4;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < M * quads; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / quads, c = (i - r * quads) * 4;
+    float v[4] = {};
+    for (int s = 0; s < split; ++s) {
+      const f32x4 o = *reinterpret_cast<const f32x4*>(sum + (s * M + r) * N + c);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += o[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] *= scale;
+    store4(reinterpret_cast<T*>(out + r * ldo) + c, v);
+  }
+}
+
+// The gradients of a batch of no rows.
+template <typename T>
+__global__ __launch_bounds__(256) void ce_zero_kernel(char* out, int64_t ldo, int64_t M, int64_t N) {
+  const int64_t quads = N / 4;
+  const float v[4] = {};
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < M * quads; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / quads;
+    store4(reinterpret_cast<T*>(out + r * ldo) + (i - r * quads) * 4, v);
+  }
+}
+__global__ __launch_bounds__(256) void ce_zero_db_kernel(float* db, int64_t n) {
+  for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < n; c += (int64_t)gridDim.x * 256) db[c] = 0.0f;
+}
+
+// ---------------------------------------------------------------- host
+
+constexpr int64_t kTile = 128;
+constexpr int64_t kMaxRows = 1 << 24, kMaxClasses = 1 << 30, kMaxDim = 1 << 20;
+constexpr int64_t kMaxTiles = 1 << 23;  // of a launch, of up to 512 threads each: below 2^32 threads
+
+struct Args {
+  elasto_linear_ce_t d;
+  Matrix x, w;
+  int es = 0;
+};
+
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+int64_t tiles(int64_t n) { return (n + kTile - 1) / kTile; }
+
+// Classes of a piece of the backward pass: a piece's dz takes about 256 MB (the cache
+// behind L2), but at least 2048 classes.
+int64_t piece_of(const elasto_linear_ce_t& d, int es) {
+  const int64_t fit = ((int64_t)256 << 20) / (std::max<int64_t>(1, d.rows) * es) / 256 * 256;
+  return std::min(up(d.classes, 256), std::max<int64_t>(2048, fit));
+}
+// Parts of a piece that dx is summed in: two workgroups a CU, of at least eight steps.
+int parts_of(const elasto_linear_ce_t& d, int es, int64_t piece) {
+  const int64_t t = tiles(d.rows) * tiles(d.dim), steps = piece * es / 128;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(1, t), steps / 8, 64}));
+}
+
+struct BackLayout {
+  int64_t live = 0, dz = 0, db = 0, sum = 0, total = 0;
+  int64_t piece = 0;
+  int parts = 0;
+  bool summed = false;  // dx goes through fp32 sums
+};
+BackLayout backward_layout(const elasto_linear_ce_t& d) {
+  const int es = d.dtype == ELASTO_BF16 ? 2 : 4;
+  BackLayout l;
+  if (d.rows == 0) return l;
+  l.piece = piece_of(d, es);
+  l.parts = parts_of(d, es, l.piece);
+  l.summed = l.parts > 1 || l.piece < d.classes;
+  auto take = [&](int64_t bytes) {
+    const int64_t at = l.total;
+    l.total += up(bytes, 256);
+    return at;
+  };
+  l.live = take(up(d.rows, 256) / 8);
+  l.dz = take(d.rows * l.piece * es);
+  l.db = take(tiles(d.rows) * l.piece * 4);
+  l.sum = take(l.summed ? (int64_t)l.parts * d.rows * d.dim * 4 : 0);
+  return l;
+}
+int64_t forward_bytes(const elasto_linear_ce_t& d) {
+  return up(tiles(d.classes) * d.rows * 8, 256) + up(d.rows * 4, 256);
+}
+
+bool check_desc(const elasto_linear_ce_t* d) {
+  if (!d) return fail(ELASTO_ERR_INVALID_ARG, "linear_ce: NULL description"), false;
+  if (d->dtype != ELASTO_BF16 && d->dtype != ELASTO_FP32)
+    return fail(ELASTO_ERR_INVALID_ARG, "bad dtype %d", d->dtype), false;
+  const int n = d->dtype == ELASTO_BF16 ? 8 : 4;
+  if (d->rows < 0 || d->rows > kMaxRows || d->classes < 1 || d->classes > kMaxClasses || d->dim < n ||
+      d->dim > kMaxDim || d->dim % n)
+    return fail(ELASTO_ERR_INVALID_ARG, "linear_ce: bad rows or classes, or dim %d is not a multiple of %d", d->dim, n),
+           false;
+  const int64_t tr = tiles(d->rows), tc = tiles(d->classes), td = tiles(d->dim);
+  if (tr * tc >= kMaxTiles || tr * td >= kMaxTiles || tc * td >= kMaxTiles)
+    return fail(ELASTO_ERR_INVALID_ARG, "linear_ce: too many tiles for a launch"), false;
+  return true;
+}
+
+bool check_matrix(const char* name, const void* p, int64_t ld, int dim, int es) {
+  if (!p) return fail(ELASTO_ERR_INVALID_ARG, "linear_ce: %s is NULL", name), false;
+  if (!aligned(p, 16) || ld * es % 16 || ld < dim || ld > kMaxDim)
+    return fail(ELASTO_ERR_INVALID_ARG, "linear_ce: %s and its row stride must be multiples of 16 bytes, the stride in [dim, 2^20]", name),
+           false;
+  return true;
+}
+
+bool check_common(const elasto_linear_ce_t* d, Args* a) {
+  if (!check_desc(d)) return false;
+  a->d = *d;
+  a->es = d->dtype == ELASTO_BF16 ? 2 : 4;
+  if (d->rows > 0 && !check_matrix("x", d->x, d->ldx, d->dim, a->es)) return false;
+  if (!check_matrix("weight", d->weight, d->ldw, d->dim, a->es)) return false;
+  if (d->rows > 0 && !d->labels) return fail(ELASTO_ERR_INVALID_ARG, "linear_ce: labels is NULL"), false;
+  if (!aligned(d->labels, 4) || !aligned(d->bias, 4) || !aligned(d->row_weight, 4))
+    return fail(ELASTO_ERR_INVALID_ARG, "linear_ce: misaligned pointer"), false;
+  a->x = Matrix{static_cast<const char*>(d->x), d->ldx * a->es};
+  a->w = Matrix{static_cast<const char*>(d->weight), d->ldw * a->es};
+  return true;
+}
+
+bool check_workspace(const void* ws, int64_t have, int64_t need) {
+  if (need > 0 && (!ws || !aligned(ws, 256) || have < need))
+    return fail(ELASTO_ERR_INVALID_ARG, "linear_ce: the workspace holds %lld of %lld bytes (256-byte aligned)",
+                (long long)(ws ? have : 0), (long long)need),
+           false;
+  return true;
+}
+
+CeP params(const Args& a) {
+  CeP p = {};
+  p.x = a.x;
+  p.w = a.w;
+  p.rows = a.d.rows;
+  p.dim = a.d.dim;
+  p.bias = a.d.bias;
+  p.labels = a.d.labels;
+  p.weight = a.d.row_weight;
+  p.classes = a.d.classes;
+  p.label_classes = a.d.classes;
+  p.tiles_m = (int)tiles(a.d.rows);
+  p.tiles_n = (int)tiles(a.d.classes);
+  p.group = 8;
+  return p;
+}
+
+template <typename T>
+using Tile = Shape<T, 128, 128, 2, 2>;
+
+template <typename T>
+hipError_t forward(const Args& a, float* loss, float* lse, char* ws, hipStream_t s) {
+  typedef Tile<T> S;
+  CeP p = params(a);
+  p.part = reinterpret_cast<float2*>(ws);
+  p.picked = reinterpret_cast<float*>(ws + up(tiles(a.d.classes) * a.d.rows * 8, 256));
+  hipLaunchKernelGGL((ce_forward_kernel<S>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(S::kThreads), 0, s, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const JoinP j = {p.part, p.picked, a.d.row_weight, a.d.labels, loss, lse, a.d.rows, p.tiles_n, a.d.classes};
+  hipLaunchKernelGGL(ce_join_kernel, dim3((unsigned)((a.d.rows + 63) / 64)), dim3(1024), 0, s, j);
+  return hipGetLastError();
+}
+
+struct Grads {
+  const float* lse;
+  char* dx;
+  int64_t lddx;
+  char* dw;
+  int64_t lddw;
+  float* db;
+  float scale;
+};
+
+unsigned blocks(int64_t n) { return (unsigned)std::min<int64_t>((n + 255) / 256, 1 << 16); }
+
+template <typename T>
+hipError_t backward(const Args& a, const Grads& g, char* ws, hipStream_t s) {
+  typedef Tile<T> S;
+  const elasto_linear_ce_t& d = a.d;
+  const int es = a.es;
+  if (d.rows == 0) {
+    if (g.dw)
+      hipLaunchKernelGGL((ce_zero_kernel<T>), dim3(blocks((int64_t)d.classes * d.dim / 4)), dim3(256), 0, s, g.dw,
+                         g.lddw * es, d.classes, d.dim);
+    if (g.db) hipLaunchKernelGGL(ce_zero_db_kernel, dim3(blocks(d.classes)), dim3(256), 0, s, g.db, d.classes);
+    return hipGetLastError();
+  }
+  const BackLayout l = backward_layout(d);
+  uint32_t* live = reinterpret_cast<uint32_t*>(ws + l.live);
+  hipLaunchKernelGGL(ce_live_kernel, dim3(blocks(d.rows)), dim3(256), 0, s, d.row_weight, d.labels, d.rows, d.classes,
+                     live);
+  hipError_t e = hipGetLastError();
+  for (int64_t c0 = 0; c0 < d.classes && e == hipSuccess; c0 += l.piece) {
+    const int64_t n = std::min<int64_t>(l.piece, d.classes - c0);
+    CeP p = params(a);
+    p.c0 = c0;
+    p.classes = n;
+    p.tiles_n = (int)tiles(n);
+    p.lse = g.lse;
+    const int64_t ld = (int64_t)p.tiles_n * kTile;  // of dz: whole tiles
+    p.dz = Matrix{ws + l.dz, ld * es};
+    p.db_part = g.db ? reinterpret_cast<float*>(ws + l.db) : nullptr;
+    hipLaunchKernelGGL((ce_dz_kernel<S>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(S::kThreads), 0, s, p);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (g.db) {
+      hipLaunchKernelGGL(ce_db_kernel, dim3(blocks(n)), dim3(256), 0, s, p.db_part, p.tiles_m, ld, n, g.scale,
+                         g.db + c0);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    ProductP q = {};
+    q.scale = g.scale;
+    q.group = 8;
+    q.tiles_n = (int)tiles(d.dim);
+    q.N = d.dim;
+    if (g.dx) {
+      q.a = p.dz;
+      q.b = Matrix{a.w.p + c0 * a.w.ld, a.w.ld};
+      q.M = d.rows;
+      q.K = n;
+      q.tiles_m = p.tiles_m;
+      q.out = g.dx;
+      q.ldo = g.lddx * es;
+      if (l.summed) {
+        q.sum = reinterpret_cast<float*>(ws + l.sum);
+        q.ld_sum = d.dim;
+        q.add = c0 > 0;
+      }
+      // Parts of whole steps; those behind a short last piece's end have no steps.
+      q.split = l.parts;
+      q.chunk = up((n + l.parts - 1) / l.parts, Step<T>::K);
+      hipLaunchKernelGGL((ce_product_kernel<S, false, false>), dim3((unsigned)(q.tiles_m * q.tiles_n * q.split)),
+                         dim3(S::kThreads), 0, s, q);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    if (g.dw) {
+      q.a = p.dz;
+      q.b = a.x;
+      q.M = n;
+      q.K = d.rows;
+      q.tiles_m = p.tiles_n;
+      q.out = g.dw + c0 * g.lddw * es;
+      q.ldo = g.lddw * es;
+      q.sum = nullptr;
+      q.add = false;
+      q.split = 1;
+      q.chunk = up(d.rows, Step<T>::K);
+      q.live = live;
+      hipLaunchKernelGGL((ce_product_kernel<S, true, true>), dim3((unsigned)(q.tiles_m * q.tiles_n)),
+                         dim3(S::kThreads), 0, s, q);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+  }
+  if (g.dx && l.summed) {
+    hipLaunchKernelGGL((ce_sum_kernel<T>), dim3(blocks(d.rows * (int64_t)d.dim / 4)), dim3(256), 0, s,
+                       reinterpret_cast<const float*>(ws + l.sum), l.parts, d.rows, d.dim, g.scale, g.dx,
+                       g.lddx * es);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace
+}  // namespace elasto
+
+using namespace elasto;
+
+extern "C" {
+
+elasto_status_t elasto_op_linear_ce(const elasto_linear_ce_t* desc, float* loss, float* lse, void* workspace,
+                                    int64_t workspace_bytes, void* hip_stream) {
+  Args a;
+  if (!check_common(desc, &a)) return ELASTO_ERR_INVALID_ARG;
+  if (a.d.rows == 0) return ELASTO_OK;
+  if (!loss) return fail(ELASTO_ERR_INVALID_ARG, "linear_ce: loss is NULL");
+  if (!aligned(loss, 4) || !aligned(lse, 4)) return fail(ELASTO_ERR_INVALID_ARG, "linear_ce: misaligned pointer");
+  if (!check_workspace(workspace, workspace_bytes, forward_bytes(a.d))) return ELASTO_ERR_INVALID_ARG;
+  char* ws = static_cast<char*>(workspace);
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const hipError_t e = a.d.dtype == ELASTO_BF16 ? forward<uint16_t>(a, loss, lse, ws, s)
+                                                : forward<float>(a, loss, lse, ws, s);
+  if (e != hipSuccess) return fail(ELASTO_ERR_HIP, "linear_ce: %s", hipGetErrorString(e));
+  return ELASTO_OK;
+}
+
+elasto_status_t elasto_op_linear_ce_bwd(const elasto_linear_ce_t* desc, const float* lse, float scale, void* dx,
+                                        int64_t lddx, void* dweight, int64_t lddw, float* dbias, void* workspace,
+                                        int64_t workspace_bytes, void* hip_stream) {
+  Args a;
+  if (!check_common(desc, &a)) return ELASTO_ERR_INVALID_ARG;
+  if (!(fabsf(scale) < INFINITY)) return fail(ELASTO_ERR_INVALID_ARG, "linear_ce: scale must be finite");
+  if (a.d.rows > 0 && !lse) return fail(ELASTO_ERR_INVALID_ARG, "linear_ce: lse is NULL");
+  if (!aligned(lse, 4) || !aligned(dbias, 4)) return fail(ELASTO_ERR_INVALID_ARG, "linear_ce: misaligned pointer");
+  if ((dx && a.d.rows > 0 && !check_matrix("dx", dx, lddx, a.d.dim, a.es)) ||
+      (dweight && !check_matrix("dweight", dweight, lddw, a.d.dim, a.es)))
+    return ELASTO_ERR_INVALID_ARG;
+  if (!check_workspace(workspace, workspace_bytes, backward_layout(a.d).total)) return ELASTO_ERR_INVALID_ARG;
+  const Grads g = {lse, static_cast<char*>(dx), lddx, static_cast<char*>(dweight), lddw, dbias, scale};
+  char* ws = static_cast<char*>(workspace);
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const hipError_t e = a.d.dtype == ELASTO_BF16 ? backward<uint16_t>(a, g, ws, s) : backward<float>(a, g, ws, s);
+  if (e != hipSuccess) return fail(ELASTO_ERR_HIP, "linear_ce: %s", hipGetErrorString(e));
+  return ELASTO_OK;
+}
+
+elasto_status_t elasto_linear_ce_workspace(const elasto_linear_ce_t* desc, int32_t backward, int64_t* bytes) {
+  if (!bytes) return fail(ELASTO_ERR_INVALID_ARG, "NULL argument");
+  if (!check_desc(desc)) return ELASTO_ERR_INVALID_ARG;
+  *bytes = backward ? backward_layout(*desc).total : forward_bytes(*desc);
+  return ELASTO_OK;
+}
+
+}  // extern "C"

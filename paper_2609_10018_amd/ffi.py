@@ -99,6 +99,12 @@ class Window(ctypes.Structure):
                [("scale", c_f32), ("q_lens", c_vp), ("k_lens", c_vp)]
 
 
+class LinearCE(ctypes.Structure):
+    _fields_ = [("dtype", c_i32), ("dim", c_i32), ("classes", c_i32), ("rows", c_i64),
+                ("x", c_vp), ("ldx", c_i64), ("weight", c_vp), ("ldw", c_i64), ("bias", c_vp),
+                ("labels", c_vp), ("row_weight", c_vp)]
+
+
 _lib: Optional[ctypes.CDLL] = None
 
 
@@ -147,6 +153,10 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "elasto_op_top_logits": [c_i32, c_vp, c_i64, c_i64, c_i32, c_i32, c_vp, c_vp, c_vp],
         "elasto_op_distill": [c_i32, c_vp, c_i64, c_i64, c_i32, c_vp, c_vp, c_i32, c_vp, c_vp, c_f32,
                               c_f32, c_f32, c_vp, c_i32, c_vp, c_i64, c_vp],
+        "elasto_op_linear_ce": [P(LinearCE), c_vp, c_vp, c_vp, c_i64, c_vp],
+        "elasto_op_linear_ce_bwd": [P(LinearCE), c_vp, c_f32, c_vp, c_i64, c_vp, c_i64, c_vp, c_vp,
+                                    c_i64, c_vp],
+        "elasto_linear_ce_workspace": [P(LinearCE), c_i32, P(c_i64)],
         "elasto_select_mode": [P(DNLut), c_f64, c_f64, c_f64, c_f64, P(c_i32)],
         "elasto_growth_create": [c_vp, c_i32, P(c_vp)],
         "elasto_growth_destroy": [c_vp],
@@ -650,6 +660,66 @@ def op_distill(logits, teacher_values, teacher_indices, loss, dlogits=None, labe
         _plain(loss, f32, "loss", r), gd, grad, ldg, _stream_ptr(stream, dev)))
 
 
+def _ce_desc(x, weight, labels, bias, row_weight):
+    """The description; labels None: of the shapes alone."""
+    r, d, ldx = _rows(x, "x")
+    c, dw, ldw = _rows(weight, "weight")
+    if dw != d or weight.dtype is not x.dtype:
+        raise ValueError(f"x {tuple(x.shape)} {x.dtype} and weight {tuple(weight.shape)} "
+                         f"{weight.dtype} do not go together")
+    _fits(c)
+    f32, i32 = _tt().f32, _tt().i32
+    return LinearCE(_dtype(x), d, c, r, x.data_ptr(), ldx, weight.data_ptr(), ldw,
+                    _plain(bias, f32, "bias", c), _plain(labels, i32, "labels", r),
+                    _plain(row_weight, f32, "row_weight", r))
+
+
+def linear_cross_entropy_workspace(x, weight, backward: bool = False) -> int:
+    """Workspace bytes of op_linear_cross_entropy (backward: op_linear_cross_entropy_bwd) for
+    tensors of these shapes."""
+    n = c_i64()
+    a = _ce_desc(x, weight, None, None, None)
+    check(load_library().elasto_linear_ce_workspace(a, int(bool(backward)), ctypes.byref(n)))
+    return n.value
+
+
+def op_linear_cross_entropy(x, weight, labels, loss, bias=None, row_weight=None, lse=None,
+                            workspace=None, stream=None) -> None:
+    """The cross-entropy of x @ weight.T + bias with labels, row by row, without those logits in
+    memory.  x: bf16 or fp32 [rows, dim], weight: [classes, dim] device tensors (any row stride);
+    labels: int32 [rows]; bias: fp32 [classes], row_weight: fp32 [rows], lse: fp32 [rows], or None;
+    loss: fp32 [rows].  workspace: a uint8 device tensor of linear_cross_entropy_workspace()
+    bytes."""
+    dev = _same_device(x, weight, labels, loss, bias, row_weight, lse, workspace)
+    a = _ce_desc(x, weight, labels, bias, row_weight)
+    f32 = _tt().f32
+    check(load_library().elasto_op_linear_ce(a, _plain(loss, f32, "loss", a.rows),
+                                             _plain(lse, f32, "lse", a.rows), *_space(workspace),
+                                             _stream_ptr(stream, dev)))
+
+
+def op_linear_cross_entropy_bwd(x, weight, labels, lse, dx=None, dweight=None, dbias=None, bias=None,
+                                row_weight=None, scale: float = 1.0, workspace=None,
+                                stream=None) -> None:
+    """The gradients of scale * sum(row_weight * loss), with op_linear_cross_entropy's lse: dx and
+    dweight like x and weight (any row stride), dbias fp32 [classes], each or None."""
+    dev = _same_device(x, weight, labels, lse, dx, dweight, dbias, bias, row_weight, workspace)
+    a = _ce_desc(x, weight, labels, bias, row_weight)
+    out = []
+    for t, like, name in ((dx, x, "dx"), (dweight, weight, "dweight")):
+        if t is None:
+            out += [None, 0]
+            continue
+        if t.shape != like.shape or t.dtype is not like.dtype:
+            raise ValueError(f"{name} is {tuple(t.shape)} {t.dtype}, not {tuple(like.shape)} "
+                             f"{like.dtype}")
+        out += [t.data_ptr(), _rows(t, name)[2]]
+    f32 = _tt().f32
+    check(load_library().elasto_op_linear_ce_bwd(
+        a, _plain(lse, f32, "lse", a.rows), scale, *out, _plain(dbias, f32, "dbias", a.classes),
+        *_space(workspace), _stream_ptr(stream, dev)))
+
+
 class GrowthContext:
     """Growth-step state of a bf16 ElasticViT handle (fp32 masters, saved
     activations, gradients) for batches of up to max_batch images."""
@@ -819,4 +889,5 @@ __all__ = ["ElasticViT", "ElasticResNet", "cnn_validate", "select_mode", "Elasto
            "op_qk_norm_rotate", "op_qk_norm_rotate_bwd", "qk_norm_rotate_workspace",
            "op_window_attention", "op_window_attention_bwd", "window_attention_workspace",
            "op_top_logits", "op_distill",
+           "op_linear_cross_entropy", "op_linear_cross_entropy_bwd", "linear_cross_entropy_workspace",
            "KERNELS", "FP32", "BF16"]
