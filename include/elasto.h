@@ -495,6 +495,31 @@ elasto_status_t elasto_op_qk_norm_rotate_bwd(const elasto_qk_norm_t* desc, const
                                              int64_t workspace_bytes, void* hip_stream);
 elasto_status_t elasto_qk_norm_rotate_workspace(const elasto_qk_norm_t* desc, int64_t* bytes);
 
+/* The same for tokens with a position on each of `axes` axes (time, height and
+ * width of a video's patches, say).  Each pair of features belongs to an axis:
+ * sections[a] pairs to axis a (sum: rot_dim / 2), the axes' sections one
+ * after another or, in_turn, dealt out one pair an axis in turn, leaving out axes
+ * that have theirs.  Pair f of a token turns by row positions[axis of f] and
+ * column f of cos and sin.  base.positions is [batch][tokens][axes] and needed;
+ * an axis' position outside [0, table_rows) makes that axis' features NaN.
+ * norm = 0: the rotation alone (no weights; eps is not used), whose backward pass
+ * needs no q and k (both may be NULL).  1 <= axes <= 4; everything else as above,
+ * the workspace too. */
+typedef struct {
+  elasto_qk_norm_t base;
+  int32_t axes, in_turn, norm;
+  int32_t sections[4];
+} elasto_qk_axes_t;
+
+elasto_status_t elasto_op_qk_norm_rotate_axes(const elasto_qk_axes_t* desc, const elasto_heads_t* q,
+                                              const elasto_heads_t* k, const elasto_heads_t* q_out,
+                                              const elasto_heads_t* k_out, void* hip_stream);
+elasto_status_t elasto_op_qk_norm_rotate_axes_bwd(
+    const elasto_qk_axes_t* desc, const elasto_heads_t* q, const elasto_heads_t* k,
+    const elasto_heads_t* dq_out, const elasto_heads_t* dk_out, const elasto_heads_t* dq,
+    const elasto_heads_t* dk, float* dq_gamma, float* dk_gamma, void* workspace,
+    int64_t workspace_bytes, void* hip_stream);
+
 /* Attention in a sliding window, with a few first tokens (sinks) that stay
  * visible, for sequences of any length.  Sequence b has k_lens[b] keys and
  * q_lens[b] queries (NULL: k_tokens and q_tokens; lengths are clamped to
@@ -634,6 +659,39 @@ elasto_status_t elasto_op_linear_ce_bwd(const elasto_linear_ce_t* desc, const fl
 /* Bytes of workspace of either call: of dtype, rows, classes and dim alone. */
 elasto_status_t elasto_linear_ce_workspace(const elasto_linear_ce_t* desc, int32_t backward,
                                            int64_t* bytes);
+
+/* A gradient (or any tensor) of `count` contiguous elements of type dtype in
+ * device memory, aligned to its elements. */
+typedef struct {
+  void* data;
+  int64_t count;
+  int32_t dtype;
+} elasto_grad_t;
+
+/* The global L2 norm of n tensors, of both types mixed: norm[0] (device, fp32) =
+ * sqrt(sum of the squares of all their elements), summed in 64 bits in a fixed
+ * order.  grads is a HOST array, read during the call and not kept; the
+ * tensors' addresses are fixed in a captured graph.  A tensor that is listed
+ * twice counts twice.  Needs n at most 2^20, 2^40 elements in all.  The
+ * workspace (elasto_grad_norm_workspace, 16-byte aligned) is free again when the
+ * call's work is done: calls that may overlap need one each. */
+elasto_status_t elasto_op_grad_norm(const elasto_grad_t* grads, int32_t n, float* norm,
+                                    void* workspace, int64_t workspace_bytes, void* hip_stream);
+
+/* Clipping by the global norm: out[i] = grads[i] * factor, factor = min(1,
+ * max_norm / norm) (the growth step's selective clipping has the same), rounded
+ * once; stats (device float[2]) = norm, factor.  A norm that is not a finite
+ * fp32 number scales nothing: factor is 0, for the step that follows to leave
+ * out, and out[i] = grads[i].  out is a HOST array like grads, of the same
+ * counts and types; out[i].data may be grads[i].data (then nothing is written where
+ * nothing changes), but otherwise no result may overlap another or a gradient.
+ * max_norm > 0 (INFINITY: no clipping).  Everything else as for
+ * elasto_op_grad_norm, the workspace too. */
+elasto_status_t elasto_op_clip_gradients(const elasto_grad_t* grads, const elasto_grad_t* out,
+                                         int32_t n, float max_norm, float* stats, void* workspace,
+                                         int64_t workspace_bytes, void* hip_stream);
+/* Bytes of workspace of either call: of the counts and types alone. */
+elasto_status_t elasto_grad_norm_workspace(const elasto_grad_t* grads, int32_t n, int64_t* bytes);
 
 /* ================================================ growth step (Section 4.2) */
 /* Growing DN mode k re-introduces the weights mode k holds and the next

@@ -19,7 +19,15 @@
 // registers), since the norm is the group's and gamma is known to both.
 //
 // Everything between the load and the store is fp32; the result is rounded
-// once.  Bound by memory, 2 (backward 3) passes over q and k: 256 x 197 tokens,
+// once.
+//
+// AXES: a token has a position on each of up to four axes (time, height, width), and
+// pair f turns by that of its axis: row position[axis of f] of the tables, column f.  A
+// lane's pairs lie on one axis as a rule where the axes' sections follow one another, and
+// are then loaded like those of one position.  Without the norm r = 1, and the backward
+// pass is the forward one by the opposite angles.
+//
+// Bound by memory, 2 (backward 3) passes over q and k: 256 x 197 tokens,
 // 24 heads of 64 in bf16, 68 us (4.8 TB/s, a copy runs at 5.1; 56 us called again on
 // the same tensors, part of which the caches keep); backward on 4 x 6001 padded
 // tokens, 40 heads of 128, with both weights' gradients, 133 us (4.7).
@@ -53,6 +61,12 @@ struct QkP {
   bool wide;  // the tables allow 16-byte loads
   float eps, inv_dim;
   float* part;  // backward: [workgroup][2][dim]
+  // AXES: positions of a token; what the sine is multiplied with; whether pairs of one axis
+  // follow one another; whether there is a norm; the axis of each pair.
+  int axes;
+  float sense;
+  bool blocks, norm;
+  uint8_t axis_of[128];
 };
 
 template <typename T>
@@ -132,7 +146,7 @@ __device__ __forceinline__ u32x4 exchange(const u32x4& w, int lane4) {
 
 // What a lane knows about its features: out = r (x (.) own + xp (.) other), with
 // xp the features that x turns with.
-template <typename T, bool PAIRS>
+template <typename T, bool PAIRS, bool AXES>
 struct Lane {
   static constexpr int N = Piece<T>::N;
   int f0;        // first feature of the piece
@@ -159,6 +173,7 @@ struct Lane {
 #pragma unroll
     for (int e = 0; e < N; ++e) c[e] = 1.0f, s[e] = 0.0f;
     if (!turns) return;
+    if constexpr (AXES) return angles_on_axes(p, row, c, s);
     const int pos = p.positions ? p.positions[row] : t;
     const bool ok = pos >= 0 && pos < p.table_rows;
     const int half = p.rot / 2;
@@ -178,6 +193,46 @@ struct Lane {
         s[2 * e + 1] = se;
       } else {
         c[e] = ce;
+        s[e] = sign * se;
+      }
+    }
+  }
+  // The same where each pair has an axis; pairs whose position has no row become NaN.
+  __device__ __forceinline__ void angles_on_axes(const QkP& p, int row, float* c, float* s) const {
+    const int half = p.rot / 2;
+    const int at = PAIRS ? f0 / 2 : (f0 < half ? f0 : f0 - half);
+    const int32_t* pos = p.positions + (int64_t)row * p.axes;
+    constexpr int K = PAIRS ? N / 2 : N;
+    float cv[K], sv[K];
+    const int a0 = p.axis_of[at];
+    if (p.blocks && a0 == p.axis_of[at + K - 1]) {
+      const int ps = pos[a0];
+      const bool ok = ps >= 0 && ps < p.table_rows;
+      const int64_t from = (int64_t)(ok ? ps : 0) * half + at;
+      load_table<K>(p.cos + from, p.wide, cv);
+      load_table<K>(p.sin + from, p.wide, sv);
+      if (!ok)
+#pragma unroll
+        for (int e = 0; e < K; ++e) cv[e] = sv[e] = NAN;
+    } else {
+#pragma unroll
+      for (int e = 0; e < K; ++e) {
+        const int ps = pos[p.axis_of[at + e]];
+        const bool ok = ps >= 0 && ps < p.table_rows;
+        const int64_t from = (int64_t)(ok ? ps : 0) * half + at + e;
+        cv[e] = ok ? p.cos[from] : NAN;
+        sv[e] = ok ? p.sin[from] : NAN;
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < K; ++e) {
+      const float se = sv[e] * p.sense;
+      if constexpr (PAIRS) {
+        c[2 * e] = c[2 * e + 1] = cv[e];
+        s[2 * e] = -se;
+        s[2 * e + 1] = se;
+      } else {
+        c[e] = cv[e];
         s[e] = sign * se;
       }
     }
@@ -224,12 +279,15 @@ __device__ __forceinline__ Unit unit_of(const QkP& p, int64_t u) {
   return w;
 }
 
+template <bool AXES>
 __device__ __forceinline__ float inv_norm(float ss, const QkP& p) {
+  if constexpr (AXES)
+    if (!p.norm) return 1.0f;
   return __builtin_amdgcn_rsqf(fmaf(ss, p.inv_dim, p.eps));
 }
 
-template <typename T, int GW, bool PAIRS>
-__device__ __forceinline__ void forward_heads(const QkP& p, const Side& s, const Lane<T, PAIRS>& L,
+template <typename T, int GW, bool PAIRS, bool AXES>
+__device__ __forceinline__ void forward_heads(const QkP& p, const Side& s, const Lane<T, PAIRS, AXES>& L,
                                               const Unit& w, int h0, int h1, const float* c,
                                               const float* sn) {
   constexpr int N = Piece<T>::N;
@@ -254,7 +312,7 @@ __device__ __forceinline__ void forward_heads(const QkP& p, const Side& s, const
       float ss = 0.0f;
 #pragma unroll
       for (int e = 0; e < N; ++e) ss = fmaf(v[e], v[e], ss);
-      const float r = inv_norm(group_sum<GW>(ss), p);
+      const float r = inv_norm<AXES>(group_sum<GW>(ss), p);
       L.partners(raw[i], v, vp);
 #pragma unroll
       for (int e = 0; e < N; ++e) v[e] = r * fmaf(v[e], own[e], vp[e] * other[e]);
@@ -265,23 +323,23 @@ __device__ __forceinline__ void forward_heads(const QkP& p, const Side& s, const
   }
 }
 
-template <typename T, int GW, bool PAIRS>
+template <typename T, int GW, bool PAIRS, bool AXES>
 __global__ __launch_bounds__(kThreads) void qk_norm_kernel(QkP p) {
   constexpr int N = Piece<T>::N;
   const int lane = threadIdx.x & 63;
-  const Lane<T, PAIRS> L(p, lane % GW, lane);
+  const Lane<T, PAIRS, AXES> L(p, lane % GW, lane);
   const Unit w = unit_of(p, (int64_t)blockIdx.x * (kThreads / GW) + threadIdx.x / GW);
   float c[N], sn[N];
   L.angles(p, w.row, w.t, c, sn);
   // Every group of a wave takes as many rounds: those of the longest share.
   const int q1 = min(w.h1, p.q.heads);
-  if (__any(w.h0 < q1)) forward_heads<T, GW, PAIRS>(p, p.q, L, w, w.h0, q1, c, sn);
+  if (__any(w.h0 < q1)) forward_heads<T, GW, PAIRS, AXES>(p, p.q, L, w, w.h0, q1, c, sn);
   const int k0 = max(w.h0 - p.q.heads, 0), k1 = w.h1 - p.q.heads;
-  if (__any(k0 < k1)) forward_heads<T, GW, PAIRS>(p, p.k, L, w, k0, k1, c, sn);
+  if (__any(k0 < k1)) forward_heads<T, GW, PAIRS, AXES>(p, p.k, L, w, k0, k1, c, sn);
 }
 
-template <typename T, int GW, bool PAIRS>
-__device__ __forceinline__ void backward_heads(const QkP& p, const Side& s, const Lane<T, PAIRS>& L,
+template <typename T, int GW, bool PAIRS, bool AXES>
+__device__ __forceinline__ void backward_heads(const QkP& p, const Side& s, const Lane<T, PAIRS, AXES>& L,
                                                const Unit& w, int h0, int h1, const float* c,
                                                const float* sn, const float* gamma, float* dgamma) {
   constexpr int N = Piece<T>::N;
@@ -307,7 +365,7 @@ __device__ __forceinline__ void backward_heads(const QkP& p, const Side& s, cons
       float ss = 0.0f;
 #pragma unroll
       for (int j = 0; j < N; ++j) ss = fmaf(u[j], u[j], ss);
-      const float r = inv_norm(group_sum<GW>(ss), p);
+      const float r = inv_norm<AXES>(group_sum<GW>(ss), p);
       Piece<T>::unpack(draw[i], e);
       L.partners(draw[i], e, ep);
       float gu = 0.0f;
@@ -334,12 +392,12 @@ __device__ __forceinline__ void backward_heads(const QkP& p, const Side& s, cons
 // Backward: a fixed grid walks the units, so that a lane sums its features'
 // part of dgamma in registers; the workgroup's groups are summed in LDS and its
 // row goes to part, which qk_gamma_kernel sums in a fixed order.
-template <typename T, int GW, bool PAIRS>
+template <typename T, int GW, bool PAIRS, bool AXES>
 __global__ __launch_bounds__(kThreads, 3) void qk_norm_bwd_kernel(QkP p) {
   constexpr int N = Piece<T>::N, G = kThreads / GW;
   __shared__ float red[2][G][GW * N];
   const int lane = threadIdx.x & 63, li = lane % GW, grp = threadIdx.x / GW;
-  const Lane<T, PAIRS> L(p, li, lane);
+  const Lane<T, PAIRS, AXES> L(p, li, lane);
   float dgq[N], dgk[N], gq[N], gk[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) {
@@ -356,9 +414,9 @@ __global__ __launch_bounds__(kThreads, 3) void qk_norm_bwd_kernel(QkP p) {
 #pragma unroll
       for (int e = 0; e < N; ++e) c[e] = sn[e] = 0.0f;
     const int q1 = min(w.h1, p.q.heads);
-    if (__any(w.h0 < q1)) backward_heads<T, GW, PAIRS>(p, p.q, L, w, w.h0, q1, c, sn, gq, dgq);
+    if (__any(w.h0 < q1)) backward_heads<T, GW, PAIRS, AXES>(p, p.q, L, w, w.h0, q1, c, sn, gq, dgq);
     const int k0 = max(w.h0 - p.q.heads, 0), k1 = w.h1 - p.q.heads;
-    if (__any(k0 < k1)) backward_heads<T, GW, PAIRS>(p, p.k, L, w, k0, k1, c, sn, gk, dgk);
+    if (__any(k0 < k1)) backward_heads<T, GW, PAIRS, AXES>(p, p.k, L, w, k0, k1, c, sn, gk, dgk);
   }
   if (!p.part) return;
 #pragma unroll
@@ -393,23 +451,23 @@ __global__ __launch_bounds__(1024) void qk_gamma_kernel(const float* part, int r
   if (out) out[col < dim ? col : col - dim] = s;
 }
 
-template <typename T, int GW, bool PAIRS>
+template <typename T, int GW, bool PAIRS, bool AXES>
 void launch(const QkP& p, bool back, int grid, hipStream_t s) {
   if (back)
-    hipLaunchKernelGGL((qk_norm_bwd_kernel<T, GW, PAIRS>), dim3((unsigned)grid), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((qk_norm_bwd_kernel<T, GW, PAIRS, AXES>), dim3((unsigned)grid), dim3(kThreads), 0, s, p);
   else
-    hipLaunchKernelGGL((qk_norm_kernel<T, GW, PAIRS>), dim3((unsigned)grid), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((qk_norm_kernel<T, GW, PAIRS, AXES>), dim3((unsigned)grid), dim3(kThreads), 0, s, p);
 }
 
-template <typename T, bool PAIRS>
+template <typename T, bool PAIRS, bool AXES>
 void launch_width(const QkP& p, int gw, bool back, int grid, hipStream_t s) {
   switch (gw) {
-    case 2: return launch<T, 2, PAIRS>(p, back, grid, s);
-    case 4: return launch<T, 4, PAIRS>(p, back, grid, s);
-    case 8: return launch<T, 8, PAIRS>(p, back, grid, s);
-    case 16: return launch<T, 16, PAIRS>(p, back, grid, s);
-    case 32: return launch<T, 32, PAIRS>(p, back, grid, s);
-    default: return launch<T, 64, PAIRS>(p, back, grid, s);
+    case 2: return launch<T, 2, PAIRS, AXES>(p, back, grid, s);
+    case 4: return launch<T, 4, PAIRS, AXES>(p, back, grid, s);
+    case 8: return launch<T, 8, PAIRS, AXES>(p, back, grid, s);
+    case 16: return launch<T, 16, PAIRS, AXES>(p, back, grid, s);
+    case 32: return launch<T, 32, PAIRS, AXES>(p, back, grid, s);
+    default: return launch<T, 64, PAIRS, AXES>(p, back, grid, s);
   }
 }
 
@@ -441,12 +499,51 @@ bool set_side(Side* s, const elasto_qk_norm_t& a, const char* name, int heads, c
   return take(x, false, &s->x) && (!back || take(dout, false, &s->dout)) && take(out, true, &s->out);
 }
 
-elasto_status_t run(const elasto_qk_norm_t* a, const elasto_heads_t* q, const elasto_heads_t* k,
+// The axis of each pair: the axes' sections one after another, or dealt out in turn.
+bool set_axes(const elasto_qk_axes_t& x, QkP* p) {
+  if (x.axes < 1 || x.axes > 4) return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: %d axes, not 1 to 4", x.axes), false;
+  int left[4] = {}, sum = 0;
+  for (int a = 0; a < x.axes; ++a) {
+    if (x.sections[a] < 0 || x.sections[a] > 128)
+      return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: section %d of %d pairs", a, x.sections[a]), false;
+    sum += left[a] = x.sections[a];
+  }
+  if (2 * sum != x.base.rot_dim)
+    return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: the sections hold %d pairs, rot_dim %d", sum, x.base.rot_dim), false;
+  for (int f = 0, a = 0; f < sum;) {
+    if (left[a] > 0) {
+      p->axis_of[f++] = (uint8_t)a;
+      --left[a];
+      if (!x.in_turn) continue;
+    }
+    a = (a + 1) % x.axes;
+  }
+  p->axes = x.axes;
+  p->blocks = !x.in_turn;
+  p->norm = x.norm != 0;
+  p->sense = 1.0f;
+  if (!p->norm && (x.base.q_gamma || x.base.k_gamma))
+    return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: weights without the norm"), false;
+  if (!x.base.positions && x.base.rot_dim > 0 && (int64_t)x.base.batch * x.base.tokens > 0)
+    return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: positions is NULL"), false;
+  return true;
+}
+
+template <bool AXES>
+void launch_types(const QkP& p, bool bf16, bool pairs, int gw, bool back, int grid, hipStream_t s) {
+  if (bf16)
+    pairs ? launch_width<uint16_t, true, AXES>(p, gw, back, grid, s) : launch_width<uint16_t, false, AXES>(p, gw, back, grid, s);
+  else
+    pairs ? launch_width<float, true, AXES>(p, gw, back, grid, s) : launch_width<float, false, AXES>(p, gw, back, grid, s);
+}
+
+// axes: NULL where tokens have one position.
+elasto_status_t run(const elasto_qk_norm_t* a, const elasto_qk_axes_t* axes, const elasto_heads_t* q, const elasto_heads_t* k,
                     const elasto_heads_t* dq_out, const elasto_heads_t* dk_out,
                     const elasto_heads_t* q_res, const elasto_heads_t* k_res, float* dq_gamma,
                     float* dk_gamma, void* ws, int64_t ws_bytes, bool back, void* hip_stream) {
   if (!check_desc(a)) return ELASTO_ERR_INVALID_ARG;
-  if (!(a->eps >= 1.17549435e-38f) || !(a->eps < INFINITY))
+  if ((!axes || axes->norm) && (!(a->eps >= 1.17549435e-38f) || !(a->eps < INFINITY)))
     return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: eps must be a positive normal number");
   if (a->rot_dim < 0 || a->rot_dim > a->head_dim || a->rot_dim % 16)
     return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: rot_dim %d is not a multiple of 16 in [0, head_dim]", a->rot_dim);
@@ -454,13 +551,21 @@ elasto_status_t run(const elasto_qk_norm_t* a, const elasto_heads_t* q, const el
   if (a->rot_dim > 0 && rows > 0) {
     if (!a->cos || !a->sin || !aligned(a->cos, 4) || !aligned(a->sin, 4) || a->table_rows < 1)
       return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: a rotation needs cos, sin and table_rows >= 1");
-    if (!a->positions && a->table_rows < a->tokens)
+    if (!axes && !a->positions && a->table_rows < a->tokens)
       return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: the tables hold %d rows for %d tokens", a->table_rows, a->tokens);
   }
   if (!aligned(a->positions, 4) || !aligned(a->lens, 4) || !aligned(dq_gamma, 4) || !aligned(dk_gamma, 4))
     return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: misaligned pointer");
   const int es = a->dtype == ELASTO_BF16 ? 2 : 4, n = 16 / es;
   QkP p = {};
+  if (axes && !set_axes(*axes, &p)) return ELASTO_ERR_INVALID_ARG;
+  if (back && axes && !p.norm) {
+    if (dq_gamma || dk_gamma) return fail(ELASTO_ERR_INVALID_ARG, "qk_norm: weights without the norm");
+    back = false;
+    p.sense = -1.0f;
+    q = dq_out;
+    k = dk_out;
+  }
   if (!set_side(&p.q, *a, "q, its result or a gradient", a->q_heads, q, dq_out, q_res, a->q_gamma, back) ||
       !set_side(&p.k, *a, "k, its result or a gradient", a->kv_heads, k, dk_out, k_res, a->k_gamma, back))
     return ELASTO_ERR_INVALID_ARG;
@@ -502,12 +607,10 @@ elasto_status_t run(const elasto_qk_norm_t* a, const elasto_heads_t* q, const el
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   hipError_t e = hipSuccess;
   if (grid > 0) {
-    if (a->dtype == ELASTO_BF16)
-      a->interleaved ? launch_width<uint16_t, true>(p, gw, back, (int)grid, s)
-                     : launch_width<uint16_t, false>(p, gw, back, (int)grid, s);
+    if (axes)
+      launch_types<true>(p, a->dtype == ELASTO_BF16, a->interleaved, gw, back, (int)grid, s);
     else
-      a->interleaved ? launch_width<float, true>(p, gw, back, (int)grid, s)
-                     : launch_width<float, false>(p, gw, back, (int)grid, s);
+      launch_types<false>(p, a->dtype == ELASTO_BF16, a->interleaved, gw, back, (int)grid, s);
     e = hipGetLastError();
   }
   if (e == hipSuccess && weights) {
@@ -529,7 +632,7 @@ extern "C" {
 elasto_status_t elasto_op_qk_norm_rotate(const elasto_qk_norm_t* desc, const elasto_heads_t* q,
                                   const elasto_heads_t* k, const elasto_heads_t* q_out,
                                   const elasto_heads_t* k_out, void* hip_stream) {
-  return run(desc, q, k, nullptr, nullptr, q_out, k_out, nullptr, nullptr, nullptr, 0, false,
+  return run(desc, nullptr, q, k, nullptr, nullptr, q_out, k_out, nullptr, nullptr, nullptr, 0, false,
              hip_stream);
 }
 
@@ -538,8 +641,25 @@ elasto_status_t elasto_op_qk_norm_rotate_bwd(const elasto_qk_norm_t* desc, const
                                       const elasto_heads_t* dk_out, const elasto_heads_t* dq,
                                       const elasto_heads_t* dk, float* dq_gamma, float* dk_gamma,
                                       void* workspace, int64_t workspace_bytes, void* hip_stream) {
-  return run(desc, q, k, dq_out, dk_out, dq, dk, dq_gamma, dk_gamma, workspace, workspace_bytes,
+  return run(desc, nullptr, q, k, dq_out, dk_out, dq, dk, dq_gamma, dk_gamma, workspace, workspace_bytes,
              true, hip_stream);
+}
+
+elasto_status_t elasto_op_qk_norm_rotate_axes(const elasto_qk_axes_t* desc, const elasto_heads_t* q,
+                                              const elasto_heads_t* k, const elasto_heads_t* q_out,
+                                              const elasto_heads_t* k_out, void* hip_stream) {
+  return run(desc ? &desc->base : nullptr, desc, q, k, nullptr, nullptr, q_out, k_out, nullptr, nullptr,
+             nullptr, 0, false, hip_stream);
+}
+
+elasto_status_t elasto_op_qk_norm_rotate_axes_bwd(const elasto_qk_axes_t* desc, const elasto_heads_t* q,
+                                                  const elasto_heads_t* k, const elasto_heads_t* dq_out,
+                                                  const elasto_heads_t* dk_out, const elasto_heads_t* dq,
+                                                  const elasto_heads_t* dk, float* dq_gamma,
+                                                  float* dk_gamma, void* workspace,
+                                                  int64_t workspace_bytes, void* hip_stream) {
+  return run(desc ? &desc->base : nullptr, desc, q, k, dq_out, dk_out, dq, dk, dq_gamma, dk_gamma, workspace,
+             workspace_bytes, true, hip_stream);
 }
 
 elasto_status_t elasto_qk_norm_rotate_workspace(const elasto_qk_norm_t* desc, int64_t* bytes) {

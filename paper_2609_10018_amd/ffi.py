@@ -93,6 +93,11 @@ class QkNorm(ctypes.Structure):
                [(n, c_vp) for n in ("positions", "lens", "cos", "sin", "q_gamma", "k_gamma")]
 
 
+class QkAxes(ctypes.Structure):
+    _fields_ = [("base", QkNorm), ("axes", c_i32), ("in_turn", c_i32), ("norm", c_i32),
+                ("sections", c_i32 * 4)]
+
+
 class Window(ctypes.Structure):
     _fields_ = [(n, c_i32) for n in ("dtype", "batch", "q_tokens", "k_tokens", "heads", "kv_heads",
                                      "head_dim", "causal", "window", "sinks")] + \
@@ -103,6 +108,10 @@ class LinearCE(ctypes.Structure):
     _fields_ = [("dtype", c_i32), ("dim", c_i32), ("classes", c_i32), ("rows", c_i64),
                 ("x", c_vp), ("ldx", c_i64), ("weight", c_vp), ("ldw", c_i64), ("bias", c_vp),
                 ("labels", c_vp), ("row_weight", c_vp)]
+
+
+class Grad(ctypes.Structure):
+    _fields_ = [("data", c_vp), ("count", c_i64), ("dtype", c_i32)]
 
 
 _lib: Optional[ctypes.CDLL] = None
@@ -153,10 +162,16 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "elasto_op_top_logits": [c_i32, c_vp, c_i64, c_i64, c_i32, c_i32, c_vp, c_vp, c_vp],
         "elasto_op_distill": [c_i32, c_vp, c_i64, c_i64, c_i32, c_vp, c_vp, c_i32, c_vp, c_vp, c_f32,
                               c_f32, c_f32, c_vp, c_i32, c_vp, c_i64, c_vp],
+        "elasto_op_qk_norm_rotate_axes": [P(QkAxes)] + [P(Heads)] * 4 + [c_vp],
+        "elasto_op_qk_norm_rotate_axes_bwd": [P(QkAxes)] + [P(Heads)] * 6 + [c_vp, c_vp, c_vp, c_i64,
+                                                                            c_vp],
         "elasto_op_linear_ce": [P(LinearCE), c_vp, c_vp, c_vp, c_i64, c_vp],
         "elasto_op_linear_ce_bwd": [P(LinearCE), c_vp, c_f32, c_vp, c_i64, c_vp, c_i64, c_vp, c_vp,
                                     c_i64, c_vp],
         "elasto_linear_ce_workspace": [P(LinearCE), c_i32, P(c_i64)],
+        "elasto_op_grad_norm": [P(Grad), c_i32, c_vp, c_vp, c_i64, c_vp],
+        "elasto_op_clip_gradients": [P(Grad), P(Grad), c_i32, c_f32, c_vp, c_vp, c_i64, c_vp],
+        "elasto_grad_norm_workspace": [P(Grad), c_i32, P(c_i64)],
         "elasto_select_mode": [P(DNLut), c_f64, c_f64, c_f64, c_f64, P(c_i32)],
         "elasto_growth_create": [c_vp, c_i32, P(c_vp)],
         "elasto_growth_destroy": [c_vp],
@@ -480,8 +495,8 @@ def _space(workspace):
     return _plain(workspace, _tt().u8, "workspace"), workspace.numel()
 
 
-def _qk_desc(q, k, cos, sin, q_gamma, k_gamma, positions, lens, eps, interleaved):
-    """The description, and the shapes of q and of k."""
+def _qk_desc(q, k, cos, sin, q_gamma, k_gamma, positions, lens, eps, interleaved, axes=None):
+    """The description, and the shapes of q and of k.  axes: positions of a token, None for one."""
     x = q if q is not None else k
     if x.dim() != 4:
         raise ValueError(f"q and k must be [batch, tokens, heads, head_dim], not {tuple(x.shape)}")
@@ -497,8 +512,9 @@ def _qk_desc(q, k, cos, sin, q_gamma, k_gamma, positions, lens, eps, interleaved
     if (cos is None) != (sin is None) or (cos is not None and cos.shape != sin.shape):
         raise ValueError("cos and sin must be given together, of one shape")
     _fits(b, t, n, d, other, rows, rot)
-    if positions is not None and positions.shape != (b, t):
-        raise ValueError(f"positions is {tuple(positions.shape)}, not {(b, t)}")
+    want = (b, t) if axes is None else (b, t, axes)
+    if positions is not None and positions.shape != want:
+        raise ValueError(f"positions is {tuple(positions.shape)}, not {want}")
     f32, i32 = tt.f32, tt.i32
     a = QkNorm(_dtype(x), b, t, nq, nk, d, rot, 1 if interleaved else 0, rows, eps,
                _plain(positions, i32, "positions"), _plain(lens, i32, "lens", b),
@@ -546,6 +562,51 @@ def op_qk_norm_rotate_bwd(q, k, dq_out, dk_out, dq, dk, dq_gamma=None, dk_gamma=
         _heads(dq, sq, dt, "dq"), _heads(dk, sk, dt, "dk"),
         _plain(dq_gamma, f32, "dq_gamma", sq[3]), _plain(dk_gamma, f32, "dk_gamma", sq[3]),
         *_space(workspace), _stream_ptr(stream, dev)))
+
+
+def _axes_desc(q, k, cos, sin, positions, sections, in_turn, norm, q_gamma, k_gamma, lens, eps,
+               interleaved):
+    sections = [_int(n) for n in sections]
+    if not 1 <= len(sections) <= 4:
+        raise ValueError(f"{len(sections)} axes, not 1 to 4")
+    a, sq, sk, dt = _qk_desc(q, k, cos, sin, q_gamma, k_gamma, positions, lens, eps, interleaved,
+                             len(sections))
+    return QkAxes(a, len(sections), 1 if in_turn else 0, 1 if norm else 0,
+                  (c_i32 * 4)(*sections)), sq, sk, dt
+
+
+def op_qk_norm_rotate_axes(q, k, q_out, k_out, cos, sin, positions, sections, in_turn: bool = False,
+                           norm: bool = True, q_gamma=None, k_gamma=None, lens=None,
+                           eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
+    """op_qk_norm_rotate for tokens with a position on each of several axes: positions is int32
+    [batch, tokens, axes], sections the pairs of features of each axis (one after another, or
+    in_turn), and pair f turns by row positions[axis of f], column f of cos and sin.  norm False: the
+    rotation alone."""
+    dev = _same_device(q, k, q_out, k_out, cos, sin, q_gamma, k_gamma, positions, lens)
+    a, sq, sk, dt = _axes_desc(q, k, cos, sin, positions, sections, in_turn, norm, q_gamma, k_gamma,
+                               lens, eps, interleaved)
+    check(load_library().elasto_op_qk_norm_rotate_axes(
+        a, None if q is None else _strided(q, sq, "q"), _heads(k, sk, dt, "k"),
+        _heads(q_out, sq, dt, "q_out"), _heads(k_out, sk, dt, "k_out"), _stream_ptr(stream, dev)))
+
+
+def op_qk_norm_rotate_axes_bwd(q, k, dq_out, dk_out, dq, dk, cos, sin, positions, sections,
+                               in_turn: bool = False, norm: bool = True, dq_gamma=None, dk_gamma=None,
+                               workspace=None, q_gamma=None, k_gamma=None, lens=None,
+                               eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
+    """The gradients, as op_qk_norm_rotate_bwd has them (the workspace too).  With norm False q and k
+    are not used and may be None."""
+    dev = _same_device(q, k, dq_out, dk_out, dq, dk, dq_gamma, dk_gamma, workspace, cos, sin,
+                       q_gamma, k_gamma, positions, lens)
+    # Shapes as the results have them: q and k may be missing.
+    a, sq, sk, dt = _axes_desc(dq, dk, cos, sin, positions, sections, in_turn, norm, q_gamma, k_gamma,
+                               lens, eps, interleaved)
+    f32 = _tt().f32
+    check(load_library().elasto_op_qk_norm_rotate_axes_bwd(
+        a, _heads(q, sq, dt, "q"), _heads(k, sk, dt, "k"), _heads(dq_out, sq, dt, "dq_out"),
+        _heads(dk_out, sk, dt, "dk_out"), None if dq is None else _strided(dq, sq, "dq"),
+        _heads(dk, sk, dt, "dk"), _plain(dq_gamma, f32, "dq_gamma", sq[3]),
+        _plain(dk_gamma, f32, "dk_gamma", sq[3]), *_space(workspace), _stream_ptr(stream, dev)))
 
 
 def _window_desc(q, k, window, sinks, causal, scale, q_lens, k_lens):
@@ -720,6 +781,93 @@ def op_linear_cross_entropy_bwd(x, weight, labels, lse, dx=None, dweight=None, d
         *_space(workspace), _stream_ptr(stream, dev)))
 
 
+def _dense(t) -> bool:
+    """Whether t's elements fill one run of memory, in any order of its axes."""
+    if t.is_contiguous():
+        return True
+    size = 1
+    for st, n in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n != 1):
+        if st != size:
+            return False
+        size *= n
+    return True
+
+
+class GradList:
+    """Tensors for op_grad_norm and op_clip_gradients, laid out for the C ABI once: bf16 and fp32
+    device tensors of any shape whose elements fill one run of memory (in any order of the axes).
+    Holds the tensors; where a tensor's memory has moved, the next call takes the new place.
+    Gradients that are new tensors need a new list."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self.array = (Grad * max(1, len(self.tensors)))()
+        self._seen = [None] * len(self.tensors)
+        self.entries()
+
+    def __len__(self) -> int:
+        return len(self.tensors)
+
+    def entries(self):
+        """The C array, up to date."""
+        seen = self._seen
+        for i, t in enumerate(self.tensors):
+            now = t.data_ptr(), t.numel()
+            if now != seen[i]:
+                if not _dense(t):
+                    raise ValueError(f"tensor {i} {tuple(t.shape)} with strides {t.stride()} is not "
+                                     f"one run of memory")
+                if i and t.device != self.tensors[0].device:
+                    raise ValueError(f"tensor {i} lies on {t.device}, the first on "
+                                     f"{self.tensors[0].device}")
+                self.array[i] = Grad(now[0], now[1], _dtype(t))
+                seen[i] = now
+        return self.array
+
+
+def _grad_list(tensors) -> GradList:
+    return tensors if isinstance(tensors, GradList) else GradList(tensors)
+
+
+def _list_device(grads: GradList, *tensors) -> int:
+    return _same_device(*grads.tensors[:1], *tensors)
+
+
+def grad_norm_workspace(grads) -> int:
+    """Workspace bytes of op_grad_norm and op_clip_gradients for these tensors."""
+    g = _grad_list(grads)
+    n = c_i64()
+    check(load_library().elasto_grad_norm_workspace(g.entries(), len(g), ctypes.byref(n)))
+    return n.value
+
+
+def op_grad_norm(grads, norm, workspace=None, stream=None) -> None:
+    """norm (fp32, one element): the L2 norm over all elements of grads, a GradList or a sequence of
+    tensors that makes one.  workspace: a uint8 device tensor of grad_norm_workspace() bytes."""
+    g = _grad_list(grads)
+    dev = _list_device(g, norm, workspace)
+    check(load_library().elasto_op_grad_norm(g.entries(), len(g), _plain(norm, _tt().f32, "norm", 1),
+                                             *_space(workspace), _stream_ptr(stream, dev)))
+
+
+def op_clip_gradients(grads, max_norm: float, stats, out=None, workspace=None, stream=None) -> None:
+    """grads times min(1, max_norm / their norm), into out (None: grads themselves); stats: fp32 with
+    2 elements, norm and factor.  A norm that is not finite scales nothing and gives the factor 0.
+    grads, out: GradLists or sequences of tensors that make one."""
+    g = _grad_list(grads)
+    o = g if out is None else _grad_list(out)
+    if len(o) != len(g):
+        raise ValueError(f"{len(o)} results for {len(g)} gradients")
+    dev = _list_device(g, *o.tensors[:1], stats, workspace)
+    if o is not g:
+        for i, (a, b) in enumerate(zip(g.tensors, o.tensors)):
+            if a is not b and a.stride() != b.stride() and not (a.is_contiguous() and b.is_contiguous()):
+                raise ValueError(f"result {i} has its elements in another order than its gradient")
+    check(load_library().elasto_op_clip_gradients(
+        g.entries(), o.entries(), len(g), max_norm, _plain(stats, _tt().f32, "stats", 2),
+        *_space(workspace), _stream_ptr(stream, dev)))
+
+
 class GrowthContext:
     """Growth-step state of a bf16 ElasticViT handle (fp32 masters, saved
     activations, gradients) for batches of up to max_batch images."""
@@ -887,7 +1035,9 @@ def select_mode(flops, latency_ms, memory_bytes, accuracy=None, power_w=None,
 __all__ = ["ElasticViT", "ElasticResNet", "cnn_validate", "select_mode", "ElastoError", "load_library", "validate", "packed_bytes",
            "packed_layout", "pack_weights", "op_layernorm", "op_linear", "op_linear_ln", "op_attention",
            "op_qk_norm_rotate", "op_qk_norm_rotate_bwd", "qk_norm_rotate_workspace",
+           "op_qk_norm_rotate_axes", "op_qk_norm_rotate_axes_bwd",
            "op_window_attention", "op_window_attention_bwd", "window_attention_workspace",
            "op_top_logits", "op_distill",
            "op_linear_cross_entropy", "op_linear_cross_entropy_bwd", "linear_cross_entropy_workspace",
+           "GradList", "op_grad_norm", "op_clip_gradients", "grad_norm_workspace",
            "KERNELS", "FP32", "BF16"]

@@ -1,0 +1,211 @@
+"""Norms of q and k with positions on several axes, forward and backward, against the
+formulas in 64 bits.  The tolerances are those of one position for a token
+(test_gpu_qk_norm.py): the same kernels' arithmetic, with a cosine and a sine of another
+row.  Without the norm a result is a c - b s of the inputs themselves: three fp32
+roundings before the one to the result's type.
+"""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2609_10018_amd import ffi  # noqa: E402
+from test_gpu_qk_norm import BF, F32, FILL, Case, check_backward, turn  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    ffi.load_library()
+
+
+def axis_of_pair(sections, in_turn):
+    if not in_turn:
+        return [a for a, n in enumerate(sections) for _ in range(n)]
+    out, left = [], list(sections)
+    while sum(left):
+        for a in range(len(left)):
+            if left[a] > 0:
+                out.append(a)
+                left[a] -= 1
+    return out
+
+
+class Axes(Case):
+    def __init__(self, dtype, b, t, h, kv, dim, sections, pairs=False, in_turn=False, norm=True, lens=None,
+                 layout="plain", seed=0):
+        super().__init__(dtype, b, t, h, kv, dim, 2 * sum(sections), pairs, layout, lens, gamma=norm, seed=seed)
+        g = torch.Generator().manual_seed(seed + 1)
+        self.sections, self.in_turn, self.with_norm = sections, in_turn, norm
+        self.positions = torch.randint(0, t + 40, (b, t, len(sections)), generator=g, dtype=torch.int32).cuda()
+        if not self.rot:
+            self.cos = self.sin = torch.zeros(t + 40, 0, device="cuda")
+        self.kw = dict(cos=self.cos, sin=self.sin, q_gamma=self.gamma["q"], k_gamma=self.gamma["k"],
+                       positions=self.positions, lens=self.lens, eps=self.eps, interleaved=pairs,
+                       sections=sections, in_turn=in_turn, norm=norm)
+
+    def tables(self):
+        if not self.rot:
+            return None, None
+        axis = torch.tensor(axis_of_pair(self.sections, self.in_turn), device="cuda")
+        pos = self.positions.long()[:, :, axis]
+        f = torch.arange(self.rot // 2, device="cuda")
+        return self.cos.double()[pos, f][:, :, None], self.sin.double()[pos, f][:, :, None]
+
+    def norm(self, n):
+        if self.with_norm:
+            return super().norm(n)
+        x = self.x[n].double()
+        return x, torch.ones_like(x[..., :1]), torch.ones_like(x[0, 0, 0])
+
+    def forward(self):
+        out = {n: self.empty(n) for n in "qk"}
+        ffi.op_qk_norm_rotate_axes(self.x["q"], self.x["k"], out["q"], out["k"], **self.kw)
+        return out
+
+    def backward(self, seed=5, inputs=True):
+        g = torch.Generator().manual_seed(seed)
+        d = {n: torch.randn(self.b, self.t, self.heads[n], self.dim, generator=g).to(self.dtype).cuda() for n in "qk"}
+        dx = {n: self.empty(n) for n in "qk"}
+        dw, ws = {"q": None, "k": None}, None
+        if self.with_norm:
+            dw = {n: torch.full((self.dim,), FILL, device="cuda") for n in "qk"}
+            ws = torch.empty(ffi.qk_norm_rotate_workspace(self.x["q"], self.x["k"]), dtype=torch.uint8, device="cuda")
+        q, k = (self.x["q"], self.x["k"]) if inputs else (None, None)
+        ffi.op_qk_norm_rotate_axes_bwd(q, k, d["q"], d["k"], dx["q"], dx["k"], dq_gamma=dw["q"], dk_gamma=dw["k"],
+                                       workspace=ws, **self.kw)
+        return d, dx, dw
+
+    def check_backward(self, d, dx, dw):
+        if self.with_norm:
+            return check_backward(self, d, dx, dw)
+        c, s = self.tables()
+        m = self.inside()
+        u = torch.finfo(self.dtype).eps / 2
+        for n in "qk":
+            ref, size = turn(d[n].double(), c, -s if s is not None else None, self.rot, self.pairs)
+            got = dx[n].double()
+            assert ((got - ref).abs() <= u * ref.abs() + 4 * 2.0 ** -24 * size)[m].all()
+            assert (got[~m] == FILL).all()
+
+
+CASES = [
+    # dtype, batch, tokens, q heads, k heads, dim, sections
+    (BF, 2, 7, 3, 3, 64, (12, 10, 10)),
+    (BF, 1, 1, 12, 4, 128, (16, 24, 24)),
+    (BF, 3, 197, 6, 2, 128, (32, 32)),
+    (BF, 2, 33, 5, 1, 80, (1, 0, 22, 1)),
+    (BF, 2, 9, 4, 4, 96, (24,)),
+    (BF, 1, 70, 8, 2, 256, (100, 14, 14)),
+    (BF, 2, 5, 1, 1, 16, (3, 5)),
+    (BF, 2, 5, 3, 2, 32, (0, 0)),
+    (F32, 2, 7, 3, 3, 64, (12, 10, 10)),
+    (F32, 1, 61, 5, 1, 80, (5, 5, 6)),
+    (F32, 2, 19, 4, 2, 128, (16, 24, 24)),
+    (F32, 1, 3, 2, 1, 256, (64, 64)),
+    (F32, 4, 1, 1, 1, 16, (2, 2, 2, 2)),
+]
+
+
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("pairs,in_turn", [(False, False), (False, True), (True, False), (True, True)])
+@pytest.mark.parametrize("args", CASES, ids=str)
+def test_forward_and_backward(args, pairs, in_turn, norm):
+    c = Axes(*args, pairs=pairs, in_turn=in_turn, norm=norm)
+    c.check_forward(c.forward())
+    c.check_backward(*c.backward(inputs=norm))
+
+
+def test_one_axis_is_the_operator_of_one_position():
+    """The same bits, forward and backward."""
+    for dtype in (BF, F32):
+        c = Axes(dtype, 2, 50, 6, 2, 64, (32,))
+        kw = {n: c.kw[n] for n in ("cos", "sin", "q_gamma", "k_gamma", "lens", "eps", "interleaved")}
+        kw["positions"] = c.positions[:, :, 0].contiguous()
+        out, ref = c.forward(), {n: c.empty(n) for n in "qk"}
+        ffi.op_qk_norm_rotate(c.x["q"], c.x["k"], ref["q"], ref["k"], **kw)
+        assert all(torch.equal(out[n], ref[n]) for n in "qk")
+        d, dx, dw = c.backward()
+        rx = {n: c.empty(n) for n in "qk"}
+        rw = {n: torch.empty(64, device="cuda") for n in "qk"}
+        ws = torch.empty(ffi.qk_norm_rotate_workspace(c.x["q"], c.x["k"]), dtype=torch.uint8, device="cuda")
+        ffi.op_qk_norm_rotate_bwd(c.x["q"], c.x["k"], d["q"], d["k"], rx["q"], rx["k"], rw["q"], rw["k"], ws, **kw)
+        assert all(torch.equal(dx[n], rx[n]) and torch.equal(dw[n], rw[n]) for n in "qk")
+
+
+@pytest.mark.parametrize("norm", [True, False])
+@pytest.mark.parametrize("lens", [[0, 5, 11], [11, 0, 1], [-3, 40, 7], [0, 0, 0]])
+def test_padded_batches(lens, norm):
+    c = Axes(BF, 3, 11, 4, 2, 64, (8, 4, 4), lens=lens, norm=norm)
+    pad = ~c.inside()
+    for n in "qk":
+        c.x[n][pad] = math.nan
+    c.positions[pad] = -5
+    c.check_forward(c.forward())
+    c.check_backward(*c.backward())
+
+
+@pytest.mark.parametrize("in_turn", [False, True])
+def test_a_position_without_a_row_spoils_its_axis_alone(in_turn):
+    c = Axes(F32, 1, 3, 2, 1, 64, (16, 8, 8), in_turn=in_turn)
+    c.positions[0, 1, 1] = 3 + 40
+    c.positions[0, 2, 0] = -1
+    out = c.forward()
+    axis = torch.tensor(axis_of_pair(c.sections, in_turn), device="cuda")
+    for n in "qk":
+        for t, a in ((1, 1), (2, 0)):
+            spoiled = torch.cat([axis == a, axis == a])
+            assert (out[n][0, t].isnan() == spoiled).all()
+        assert out[n][0, 0].isfinite().all()
+
+
+def test_in_place_and_misaligned_tables():
+    c = Axes(BF, 2, 40, 4, 2, 128, (24, 20, 20))
+    ref = c.forward()
+    tables = [torch.empty(x.numel() + 1, device="cuda")[1:].view(x.shape).copy_(x) for x in (c.cos, c.sin)]
+    out = {n: c.x[n].clone() for n in "qk"}
+    ffi.op_qk_norm_rotate_axes(out["q"], out["k"], out["q"], out["k"], **{**c.kw, "cos": tables[0], "sin": tables[1]})
+    assert all(torch.equal(out[n], ref[n]) for n in "qk")
+
+
+def test_back_and_forth_is_the_identity():
+    """Without the norm the backward pass undoes the rotation: two rotations of 4 fp32 roundings."""
+    c = Axes(F32, 2, 30, 3, 1, 64, (12, 10, 10), norm=False)
+    out, back = c.forward(), {n: c.empty(n) for n in "qk"}
+    ffi.op_qk_norm_rotate_axes_bwd(None, None, out["q"], out["k"], back["q"], back["k"], **c.kw)
+    for n in "qk":
+        x = c.x[n].double()
+        lo, hi = x[..., :32].abs(), x[..., 32:].abs()
+        size = torch.cat([lo + hi, lo + hi], -1)
+        # cos and sin are rounded to fp32: cos^2 + sin^2 is off by up to 2^-23.
+        assert ((back[n].double() - x).abs() <= 12 * 2.0 ** -24 * size + 2.0 ** -23 * x.abs()).all()
+
+
+def test_captured_and_replayed():
+    c = Axes(BF, 2, 100, 4, 2, 64, (12, 10, 10))
+    out = {n: c.empty(n) for n in "qk"}
+
+    def step():
+        ffi.op_qk_norm_rotate_axes(c.x["q"], c.x["k"], out["q"], out["k"], **c.kw)
+
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        step()
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        step()
+    for i in range(3):
+        c.positions.add_(i)
+        c.positions.remainder_(140)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = {n: out[n].clone() for n in "qk"}
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(got[n], out[n]) for n in "qk")
+        c.check_forward(out)

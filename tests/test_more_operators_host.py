@@ -89,3 +89,125 @@ def test_linear_ce_binding_refuses_tensors_that_do_not_fit():
                          (x.t(), w), (x.half(), w.half())):
         with pytest.raises(ValueError):
             ffi.linear_cross_entropy_workspace(bad_x, bad_w)
+
+
+# ------------------------------------------------------------------------ clipping
+
+def grads(*entries):
+    return (ffi.Grad * max(1, len(entries)))(*[ffi.Grad(*e) for e in entries])
+
+
+def clip(lib, g, o=None, n=None, max_norm=1.0, stats=P256, ws=P256, size=1 << 40):
+    o = g if o is None else o
+    return lib.elasto_op_clip_gradients(g, o, len(g) if n is None else n, max_norm, stats, ws, size, None)
+
+
+GOOD = (P256, 1000, 0), (2 * P256, 77, 1)
+
+
+@pytest.mark.parametrize("bad", [(None, 5, 0), (P256 + 2, 5, 0), (P256 + 1, 5, 1), (P256, -1, 0),
+                                 (P256, 5, 2), (P256, 1 << 40, 0)])
+def test_clip_refuses_bad_tensors(lib, bad):
+    n = ctypes.c_int64()
+    g = grads(GOOD[0], bad)
+    assert lib.elasto_grad_norm_workspace(g, 2, ctypes.byref(n)) == INVALID
+    assert lib.elasto_op_grad_norm(g, 2, P256, P256, 1 << 40, None) == INVALID
+    assert clip(lib, g) == INVALID
+    assert clip(lib, grads(*GOOD), g) == INVALID
+
+
+def test_clip_refuses_bad_arguments(lib):
+    n = ctypes.c_int64()
+    g = grads(*GOOD)
+    assert lib.elasto_grad_norm_workspace(g, 2, None) == INVALID
+    assert lib.elasto_grad_norm_workspace(g, -1, ctypes.byref(n)) == INVALID
+    assert lib.elasto_grad_norm_workspace(None, 1, ctypes.byref(n)) == INVALID
+    assert lib.elasto_grad_norm_workspace(g, (1 << 20) + 1, ctypes.byref(n)) == INVALID
+    assert lib.elasto_grad_norm_workspace(g, 2, ctypes.byref(n)) == 0 and n.value > 0
+    for norm, ws, size in ((None, P256, n.value), (P256 + 2, P256, n.value), (P256, None, n.value),
+                           (P256, P256 + 8, n.value), (P256, P256, n.value - 1)):
+        assert lib.elasto_op_grad_norm(g, 2, norm, ws, size, None) == INVALID
+    for kw in (dict(max_norm=0.0), dict(max_norm=-1.0), dict(max_norm=math.nan), dict(stats=None),
+               dict(stats=P256 + 2), dict(ws=None), dict(size=n.value - 1)):
+        assert clip(lib, g, **kw) == INVALID
+
+
+@pytest.mark.parametrize("out", [
+    (GOOD[0], (2 * P256, 76, 1)), (GOOD[0], (2 * P256, 77, 0)),          # other sizes, other types
+    ((P256 + 4, 1000, 0), GOOD[1]),                                      # over its own gradient, shifted
+    ((2 * P256 + 64, 1000, 0), GOOD[1]),                                 # over the other result
+    ((4 * P256, 1000, 0), (P256 + 400, 77, 1)),                          # over the other gradient
+    ((4 * P256, 1000, 0), (4 * P256 + 3998, 77, 1))])
+def test_clip_refuses_results_that_overlap(lib, out):
+    assert clip(lib, grads(*GOOD), grads(*out)) == INVALID
+
+
+def test_clip_refuses_the_same_tensor_twice(lib):
+    assert clip(lib, grads(GOOD[0], GOOD[0])) == INVALID
+
+
+def test_grad_lists_refuse_what_is_not_one_run():
+    torch = pytest.importorskip("torch")
+    t = torch.zeros(6, 8)
+    for bad in (t[:, :4], t[::2], t.half(), torch.zeros(1).expand(5)):
+        with pytest.raises(ValueError):
+            ffi.GradList([bad])
+    assert len(ffi.GradList([t.t(), t[2:4], torch.zeros(3, 0), torch.zeros(())])) == 4
+
+
+# --------------------------------------------------- queries and keys on several axes
+
+def heads(data=P256, b=1 << 16, t=768, h=64):
+    return ffi.Heads(data, b, t, h)
+
+
+def axes_desc(axes=3, in_turn=0, norm=1, sections=(12, 10, 10, 0), **kw):
+    d = dict(dtype=1, batch=2, tokens=8, q_heads=12, kv_heads=4, head_dim=64, rot_dim=64, interleaved=0,
+             table_rows=8, eps=1e-6, positions=P256, lens=None, cos=P256, sin=P256, q_gamma=P256, k_gamma=P256)
+    d.update(kw)
+    base = ffi.QkNorm(*[d[n] for n, _ in ffi.QkNorm._fields_])
+    return ffi.QkAxes(base, axes, in_turn, norm, (ctypes.c_int32 * 4)(*sections))
+
+
+NO_GAMMA = dict(q_gamma=None, k_gamma=None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(axes=0), dict(axes=5), dict(axes=-1), dict(axes=2), dict(sections=(12, 10, 9, 1)),
+    dict(sections=(42, -10, 0, 0)), dict(sections=(1 << 30, 1 << 30, 1 << 30, 0)), dict(positions=None),
+    dict(positions=P256 + 2), dict(norm=0), dict(cos=None), dict(sin=P256 + 1), dict(table_rows=0), dict(eps=0.0),
+    dict(head_dim=72), dict(rot_dim=8, sections=(4, 0, 0, 0)), dict(dtype=5), dict(tokens=-1)])
+def test_axes_refuses_bad_descriptions(lib, kw):
+    h = heads()
+    assert lib.elasto_op_qk_norm_rotate_axes(axes_desc(**kw), h, h, h, h, None) == INVALID
+    assert lib.elasto_op_qk_norm_rotate_axes_bwd(axes_desc(**kw), h, h, h, h, h, h, None, None, None, 0,
+                                                 None) == INVALID
+    assert lib.elasto_last_error()
+
+
+def test_axes_refuses_bad_tensors(lib):
+    h = heads()
+    for i in range(4):
+        for bad in (None, heads(None), heads(P256 + 8), heads(b=4), heads(t=772)):
+            args = [h] * 4
+            args[i] = bad
+            assert lib.elasto_op_qk_norm_rotate_axes(axes_desc(), *args, None) == INVALID
+    for norm in (0, 1):
+        d = axes_desc(norm=norm, **({} if norm else NO_GAMMA))
+        for i in range(6):
+            if not norm and i < 2:       # q and k are not used
+                continue
+            args = [h] * 6
+            args[i] = None
+            assert lib.elasto_op_qk_norm_rotate_axes_bwd(d, *args, None, None, None, 0, None) == INVALID
+    assert lib.elasto_op_qk_norm_rotate_axes(None, h, h, h, h, None) == INVALID
+    # Gradients of weights that are not there, and a workspace that is too short for those that are.
+    assert lib.elasto_op_qk_norm_rotate_axes_bwd(axes_desc(norm=0, **NO_GAMMA), h, h, h, h, h, h, P256, None, P256,
+                                                 1 << 30, None) == INVALID
+    assert lib.elasto_op_qk_norm_rotate_axes_bwd(axes_desc(), h, h, h, h, h, h, P256, None, P256, 16, None) == INVALID
+
+
+def test_axes_of_no_tokens_is_no_error(lib):
+    for kw in (dict(batch=0), dict(tokens=0)):
+        d = axes_desc(**kw, positions=None, cos=None, sin=None)
+        assert lib.elasto_op_qk_norm_rotate_axes(d, None, None, None, None, None) == 0
