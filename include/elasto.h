@@ -614,6 +614,66 @@ elasto_status_t elasto_op_distill(int32_t dtype, const void* logits, int64_t ld,
                                   int32_t grad_dtype, void* dlogits, int64_t ldg,
                                   void* hip_stream);
 
+/* A [batch][tokens][dim] tensor in device memory: the features of a token are
+ * contiguous, the other axes have strides in elements, none negative; strides of
+ * tensors that are written are at least dim along axes longer than 1. */
+typedef struct {
+  void* data;
+  int64_t batch_stride, token_stride;
+} elasto_rows_t;
+
+typedef enum { ELASTO_NORM_RMS = 0, ELASTO_NORM_LAYER = 1 } elasto_norm_t;
+
+/* What lies between two blocks of a transformer, in one pass: the norm behind a
+ * block (post_norm), its gate, the residual addition, and the norm ahead of the
+ * next block.  For each token's stream x and block output y
+ *   n = N(y; post_gamma, post_beta)  (post_norm 0: n = y),
+ *   x_out = residual_scale x + gate (.) n,   u = N(x_out; pre_gamma, pre_beta),
+ *   N(v) = (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) (.) gamma + beta,
+ * with mean(v) taken as 0, and no beta, for ELASTO_NORM_RMS.  NULL weights: gamma
+ * 1, beta 0; gate NULL: 1.  gate is fp32 [dim], or [batch][dim] where
+ * gate_per_sequence is set.  lens (or NULL): tokens t >= lens[b] are neither read
+ * nor written and add nothing to the gradients.
+ * x, x_out and their gradients are of stream_dtype, y, u and theirs of dtype
+ * (stream_dtype FP32 with either, BF16 with BF16).  Everything between load and
+ * store is fp32, rounded once; u is taken from x_out before its rounding.
+ * Needs 1 <= dim <= 16384, eps > 0 (and not subnormal), residual_scale
+ * finite, batch * tokens at most 2^25; any alignment of the types (fastest where
+ * dim is a multiple of 8 and all is aligned to 16 bytes). */
+typedef struct {
+  int32_t dtype, stream_dtype, kind, batch, tokens, dim;
+  int32_t post_norm, gate_per_sequence;
+  float residual_scale, eps;
+  const float *pre_gamma, *pre_beta;   /* device [dim] or NULL                */
+  const float *post_gamma, *post_beta; /* device [dim] or NULL                */
+  const float* gate;                   /* device [dim] or [batch][dim] or NULL */
+  const int32_t* lens;                 /* device [batch] or NULL              */
+} elasto_block_norm_t;
+
+/* y may be NULL (no post_norm, no gate): x_out = residual_scale x.  x_out or u
+ * may be NULL where it is not wanted.  x_out may be x itself, and u y (same
+ * pointer and strides, and type). */
+elasto_status_t elasto_op_block_norm(const elasto_block_norm_t* desc, const elasto_rows_t* x,
+                                     const elasto_rows_t* y, const elasto_rows_t* x_out,
+                                     const elasto_rows_t* u, void* hip_stream);
+
+/* The gradients: dx and dy (each or NULL) of x and y, and, where the pointers are
+ * given, the weights' (fp32 [dim], the gate's like the gate; summed over tokens in
+ * a fixed order), from dx_out and du, those of x_out and u (one of them may be
+ * NULL: none), with the forward's x_out (needed with du) and y.  dx may be dx_out
+ * or x_out itself, dy du or y.  The workspace (elasto_block_norm_workspace, 16-byte
+ * aligned) is needed where a weight's gradient is asked for; it is free again
+ * when the call's work is done.  With no tokens the weights' gradients become 0. */
+elasto_status_t elasto_op_block_norm_bwd(const elasto_block_norm_t* desc, const elasto_rows_t* x_out,
+                                         const elasto_rows_t* y, const elasto_rows_t* dx_out,
+                                         const elasto_rows_t* du, const elasto_rows_t* dx,
+                                         const elasto_rows_t* dy, float* d_pre_gamma,
+                                         float* d_pre_beta, float* d_post_gamma,
+                                         float* d_post_beta, float* d_gate, void* workspace,
+                                         int64_t workspace_bytes, void* hip_stream);
+/* Of batch, tokens, dim and the types alone. */
+elasto_status_t elasto_block_norm_workspace(const elasto_block_norm_t* desc, int64_t* bytes);
+
 /* Softmax cross-entropy of a linear layer over many classes, z = x W^T + b,
  * without the logits z in memory: for each of `rows` rows
  *   lse[r] = log sum_c exp(z[r][c]),  loss[r] = lse[r] - z[r][labels[r]],

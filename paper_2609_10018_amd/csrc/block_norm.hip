@@ -1,0 +1,635 @@
+// What lies between two blocks of a transformer, in one pass over the tokens: the norm behind a
+// block, its gate, the residual addition and the norm ahead of the next block.
+//   n = N_post(y)  (or y),  x' = a x + g (.) n,  u = N_pre(x'),
+//   N(v) = (v - mean) r (.) gamma + beta,  r = 1 / sqrt(mean((v - mean)^2) + eps)
+// (RMS: mean = 0).  Backward, with v^ = (v - mean) r and N'(d) = r (d gamma - v^ mean(d gamma v^)
+// - mean(d gamma)) (RMS: without the last term):
+//   dX = dx' + N_pre'(du),  dx = a dX,  dn = g (.) dX,  dy = N_post'(dn)  (or dn),
+//   dgamma = sum d v^ and dbeta = sum d over the tokens, dg = sum dX (.) n over a gate's tokens.
+//
+// A row is held in the registers of one to sixteen waves and read once; its statistics are taken in
+// the registers, about the row's mean (each wave about its own, joined by the pairwise update of
+// Chan, Golub and LeVeque), so a large mean costs no digits.  Everything between the load and the
+// store is fp32; u is taken from x' before x' is rounded.  Backward, a workgroup walks the rows of
+// one gate (or a part of them) and sums the weights' gradients of its columns in registers; the
+// parts are summed by a second kernel in a fixed order.
+//
+// Bound by memory: forward four passes over the tokens, backward six.
+#include <math.h>
+
+#include <algorithm>
+
+#include "common.h"
+#include "heads.h"
+
+namespace elasto {
+namespace {
+
+constexpr int kMaxDim = 16384;
+constexpr int kGradBlocks = 1024;  // workgroups of the backward pass
+constexpr int kSums = 5;           // pre gamma, pre beta, post gamma, post beta, gate
+
+struct Rows {  // strides in bytes
+  char* p;
+  int64_t sb, st;
+};
+
+struct BlockP {
+  Rows x, y, x_out, u;     // backward: x_out and y are inputs,
+  Rows dx_out, du, dx, dy;
+  const float *pre_gamma, *pre_beta, *post_gamma, *post_beta, *gate;
+  int64_t gate_ld;         // 0: one for all sequences
+  const int32_t* lens;
+  int batch, tokens, dim;
+  bool layer, post, has_y;
+  float a, eps, inv_dim;
+  // Backward.
+  float* part;             // [workgroup][kSums][dim]
+  float* dgate;            // [batch][dim] where a workgroup has all rows of a gate, else NULL
+  int slices;              // workgroups of a sequence
+  int wanted;              // bits: the sums that are asked for
+};
+
+// Values of a row in the registers of a thread: E of them, in runs of 8 where WIDE.
+template <int W, int CH, bool WIDE>
+struct Place {
+  static constexpr int E = 8 * CH, T = 64 * W;
+  // Column of value e of thread t of the row's.
+  static __device__ __forceinline__ int column(int e, int t) {
+    return WIDE ? ((e >> 3) * T + t) * 8 + (e & 7) : e * T + t;
+  }
+};
+
+__device__ __forceinline__ void load_run(const uint16_t* p, float* v) {
+  const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void load_run(const float* p, float* v) {
+  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+}
+__device__ __forceinline__ void store_run(uint16_t* p, const float* v) {
+  *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                                       pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+}
+__device__ __forceinline__ void store_run(float* p, const float* v) {
+  *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+  *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+}
+__device__ __forceinline__ float load_value(const uint16_t* p) { return bf16_to_f32(*p); }
+__device__ __forceinline__ float load_value(const float* p) { return *p; }
+__device__ __forceinline__ void store_value(uint16_t* p, float v) { *p = f32_to_bf16(v); }
+__device__ __forceinline__ void store_value(float* p, float v) { *p = v; }
+
+template <typename L, bool WIDE, typename T>
+__device__ __forceinline__ void load_row(const T* p, int dim, int t, float (&v)[L::E], float none = 0.0f) {
+  if constexpr (WIDE) {
+#pragma unroll
+    for (int e = 0; e < L::E; e += 8) {
+      const int c = L::column(e, t);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[e + i] = none;
+      if (c < dim) load_run(p + c, v + e);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < L::E; ++e) {
+      const int c = L::column(e, t);
+      v[e] = c < dim ? load_value(p + c) : none;
+    }
+  }
+}
+template <typename L, bool WIDE, typename T>
+__device__ __forceinline__ void store_row(T* p, int dim, int t, const float (&v)[L::E]) {
+#pragma unroll
+  for (int e = 0; e < L::E; e += WIDE ? 8 : 1) {
+    const int c = L::column(e, t);
+    if (c >= dim) continue;
+    if constexpr (WIDE)
+      store_run(p + c, v + e);
+    else
+      store_value(p + c, v[e]);
+  }
+}
+
+// Sums over a row's W waves: each wave's value by lane exchanges, the waves' through LDS.
+template <int W, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float* red, int t) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
+  if constexpr (W > 1) {
+    __syncthreads();  // the last sums have been read
+    if ((t & 63) == 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i) red[(t >> 6) * N + i] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = red[i];
+      for (int k = 1; k < W; ++k) v[i] += red[k * N + i];
+    }
+  }
+}
+
+// Mean (RMS: 0) and factor r of a row.
+template <typename L, int W>
+__device__ __forceinline__ float2 statistics(const float (&v)[L::E], const BlockP& p, float* red, int t) {
+  float mean = 0.0f;
+  if (p.layer) {
+    float s[1] = {0.0f};
+#pragma unroll
+    for (int e = 0; e < L::E; ++e) s[0] += v[e];  // columns that are not there hold zeros
+    row_sums<W>(s, red, t);
+    mean = s[0] * p.inv_dim;
+  }
+  float q[1] = {0.0f};
+#pragma unroll
+  for (int e = 0; e < L::E; ++e) {
+    const float d = v[e] - mean;
+    q[0] += L::column(e, t) < p.dim ? d * d : 0.0f;
+  }
+  row_sums<W>(q, red, t);
+  return make_float2(mean, 1.0f / sqrtf(q[0] * p.inv_dim + p.eps));
+}
+
+template <typename T>
+__device__ __forceinline__ T* at(const Rows& r, int b, int t) {
+  return reinterpret_cast<T*>(r.p + b * r.sb + t * r.st);
+}
+
+template <typename L, bool WIDE>
+__device__ __forceinline__ void load_weight(const float* w, float none, int dim, int t, float (&v)[L::E]) {
+  if (w)
+    load_row<L, WIDE>(w, dim, t, v, none);
+  else
+#pragma unroll
+    for (int e = 0; e < L::E; ++e) v[e] = none;
+}
+
+// T: of y and u.  S: of the stream.  W waves a row; a workgroup of 256 threads holds 4 / W rows.
+template <typename T, typename S, int W, int CH, bool WIDE>
+__global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_kernel(BlockP p) {
+  typedef Place<W, CH, WIDE> L;
+  constexpr int E = L::E, R = W > 4 ? 1 : 4 / W;
+  __shared__ float red[W > 4 ? W : 4];
+  const int t = threadIdx.x % L::T;
+  float* mine = red + threadIdx.x / L::T * W;
+  const int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / L::T;
+  const int64_t rows = (int64_t)p.batch * p.tokens;
+  const int b = (int)(min(row, rows - 1) / p.tokens), tok = (int)(min(row, rows - 1) - (int64_t)b * p.tokens);
+  bool live = row < rows;
+  if (live && p.lens) live = tok < p.lens[b];
+  // Waves that share a row go on or leave together; with W > 1 all rows of a workgroup meet at its
+  // barriers.
+  if (W == 1 && !live) return;
+  float v[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = 0.0f;
+  float x[E], g[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = 0.0f;
+  if (live) {
+    load_row<L, WIDE>(at<const S>(p.x, b, tok), p.dim, t, x);
+    if (p.has_y) load_row<L, WIDE>(at<const T>(p.y, b, tok), p.dim, t, v);
+  }
+  if (p.has_y) {
+    if (p.post) {
+      const float2 st = statistics<L, W>(v, p, mine, t);
+      float w[E], c[E];
+      load_weight<L, WIDE>(p.post_gamma, 1.0f, p.dim, t, w);
+      load_weight<L, WIDE>(p.post_beta, 0.0f, p.dim, t, c);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = fmaf((v[e] - st.x) * st.y, w[e], c[e]);
+    }
+    load_weight<L, WIDE>(p.gate ? p.gate + b * p.gate_ld : nullptr, 1.0f, p.dim, t, g);
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = fmaf(p.a, x[e], L::column(e, t) < p.dim ? g[e] * v[e] : 0.0f);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] *= p.a;
+  }
+  if (live && p.x_out.p) store_row<L, WIDE>(at<S>(p.x_out, b, tok), p.dim, t, x);
+  if (!p.u.p) return;
+  const float2 st = statistics<L, W>(x, p, mine, t);
+  float w[E], c[E];
+  load_weight<L, WIDE>(p.pre_gamma, 1.0f, p.dim, t, w);
+  load_weight<L, WIDE>(p.pre_beta, 0.0f, p.dim, t, c);
+#pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = fmaf((x[e] - st.x) * st.y, w[e], c[e]);
+  if (live) store_row<L, WIDE>(at<T>(p.u, b, tok), p.dim, t, x);
+}
+
+// The gradient through a norm: d, that of its result, becomes that of its input; xn the normed
+// values, r the factor; the weights' gradients are added to dg and db.
+template <typename L, bool WIDE, int W>
+__device__ __forceinline__ void norm_back(const BlockP& p, const float* gamma, float r, const float (&xn)[L::E],
+                                          float (&d)[L::E], float (&dg)[L::E], float (&db)[L::E], float* red, int t) {
+  float w[L::E], s[2] = {0.0f, 0.0f};
+  load_weight<L, WIDE>(gamma, 1.0f, p.dim, t, w);
+#pragma unroll
+  for (int e = 0; e < L::E; ++e) {
+    dg[e] = fmaf(d[e], xn[e], dg[e]);
+    db[e] += d[e];
+    d[e] *= L::column(e, t) < p.dim ? w[e] : 0.0f;
+    s[0] = fmaf(d[e], xn[e], s[0]);
+    s[1] += d[e];
+  }
+  row_sums<W>(s, red, t);
+  const float a = s[0] * p.inv_dim, c = p.layer ? s[1] * p.inv_dim : 0.0f;
+#pragma unroll
+  for (int e = 0; e < L::E; ++e) d[e] = r * (d[e] - fmaf(xn[e], a, c));
+}
+
+template <typename T, typename S, int W, int CH, bool WIDE>
+__global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_bwd_kernel(BlockP p) {
+  typedef Place<W, CH, WIDE> L;
+  constexpr int E = L::E, R = W > 4 ? 1 : 4 / W;
+  __shared__ float red[W > 4 ? 2 * W : 8];
+  __shared__ float sums[R > 1 ? (R - 1) * L::T : 1];
+  const int t = threadIdx.x % L::T, mine = threadIdx.x / L::T;
+  float* rd = red + mine * 2 * W;
+  float pg[E], pb[E], qg[E], qb[E], gg[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) pg[e] = pb[e] = qg[e] = qb[e] = gg[e] = 0.0f;
+  // The workgroup's rows sum into the first one's thread, value by value, which hands them out.
+  auto flush = [&](const float (&v)[E], float* out) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      float s = v[e];
+      if constexpr (R > 1) {
+        __syncthreads();
+        if (mine > 0) sums[(mine - 1) * L::T + t] = s;
+        __syncthreads();
+        if (mine == 0)
+#pragma unroll
+          for (int k = 0; k < R - 1; ++k) s += sums[k * L::T + t];
+      }
+      const int c = L::column(e, t);
+      if (mine == 0 && c < p.dim) out[c] = s;
+    }
+  };
+  const int units = p.batch * p.slices;
+  for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int b = unit / p.slices, slice = unit - b * p.slices;
+    const int n = p.lens ? max(0, min(p.tokens, p.lens[b])) : p.tokens;
+    const int share = (n + p.slices - 1) / p.slices, first = slice * share, last = min(n, first + share);
+    // Every row of a workgroup takes as many rounds: they meet at its barriers.
+    for (int k = first; k < last; k += R) {
+      const int tok = k + mine;
+      const bool live = tok < last;
+      float d[E], xn[E], v[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) d[e] = xn[e] = v[e] = 0.0f;
+      if (live) {
+        if (p.du.p) load_row<L, WIDE>(at<const T>(p.du, b, tok), p.dim, t, d);
+        if (p.du.p) load_row<L, WIDE>(at<const S>(p.x_out, b, tok), p.dim, t, xn);
+        if (p.has_y) load_row<L, WIDE>(at<const T>(p.y, b, tok), p.dim, t, v);
+      }
+      if (p.du.p) {
+        const float2 st = statistics<L, W>(xn, p, rd, t);
+#pragma unroll
+        for (int e = 0; e < E; ++e) xn[e] = L::column(e, t) < p.dim ? (xn[e] - st.x) * st.y : 0.0f;
+        norm_back<L, WIDE, W>(p, p.pre_gamma, st.y, xn, d, pg, pb, rd, t);
+      }
+      if (p.dx_out.p && live) {
+        load_row<L, WIDE>(at<const S>(p.dx_out, b, tok), p.dim, t, xn);
+#pragma unroll
+        for (int e = 0; e < E; ++e) d[e] += xn[e];
+      }
+      if (p.dx.p && live) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) xn[e] = p.a * d[e];
+        store_row<L, WIDE>(at<S>(p.dx, b, tok), p.dim, t, xn);
+      }
+      if (!p.has_y) continue;
+      float2 st = make_float2(0.0f, 1.0f);
+      if (p.post) st = statistics<L, W>(v, p, rd, t);
+      if (!live)
+#pragma unroll
+        for (int e = 0; e < E; ++e) d[e] = 0.0f;
+      float w[E];
+      if (p.post) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = L::column(e, t) < p.dim ? (v[e] - st.x) * st.y : 0.0f;
+      }
+      if (p.gate) {
+        if (p.wanted & 16) {
+          if (p.post) {
+            float c[E];
+            load_weight<L, WIDE>(p.post_gamma, 1.0f, p.dim, t, w);
+            load_weight<L, WIDE>(p.post_beta, 0.0f, p.dim, t, c);
+#pragma unroll
+            for (int e = 0; e < E; ++e) gg[e] = fmaf(d[e], fmaf(v[e], w[e], c[e]), gg[e]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) gg[e] = fmaf(d[e], v[e], gg[e]);
+          }
+        }
+        load_weight<L, WIDE>(p.gate + b * p.gate_ld, 0.0f, p.dim, t, w);
+#pragma unroll
+        for (int e = 0; e < E; ++e) d[e] *= w[e];
+      }
+      if (p.post) norm_back<L, WIDE, W>(p, p.post_gamma, st.y, v, d, qg, qb, rd, t);
+      if (p.dy.p && live) store_row<L, WIDE>(at<T>(p.dy, b, tok), p.dim, t, d);
+    }
+    if (p.dgate) {  // all rows of this gate are here
+      flush(gg, p.dgate + (int64_t)b * p.dim);
+#pragma unroll
+      for (int e = 0; e < E; ++e) gg[e] = 0.0f;
+    }
+  }
+  if (!p.part) return;
+  float* part = p.part + (int64_t)blockIdx.x * kSums * p.dim;
+  if (p.wanted & 1) flush(pg, part);
+  if (p.wanted & 2) flush(pb, part + p.dim);
+  if (p.wanted & 4) flush(qg, part + 2 * p.dim);
+  if (p.wanted & 8) flush(qb, part + 3 * p.dim);
+  if ((p.wanted & 16) && !p.dgate) flush(gg, part + 4 * p.dim);
+}
+
+// out[b][c] = the sum over its parts, 64 columns a workgroup, 16 slices of the parts.
+struct SumP {
+  const float* part;
+  float* out[kSums];
+  int dim, parts;
+  int gates, gate_parts;  // of the gate's gradient
+};
+__global__ __launch_bounds__(1024) void block_sum_kernel(SumP p) {
+  __shared__ float red[16][65];
+  const int which = blockIdx.y;
+  // The gate's gradients are further rows of the grid.
+  const int sum = which < 4 ? which : 4, gate = which < 4 ? 0 : which - 4;
+  float* out = p.out[sum];
+  if (!out) return;
+  const int from = sum == 4 ? gate * p.gate_parts : 0, n = sum == 4 ? p.gate_parts : p.parts;
+  const int lane = threadIdx.x & 63, sl = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+  float s = 0.0f;
+  if (c < p.dim)
+#pragma unroll 8
+    for (int i = sl; i < n; i += 16) s += p.part[((int64_t)(from + i) * kSums + sum) * p.dim + c];
+  red[sl][lane] = s;
+  __syncthreads();
+  if (sl != 0 || c >= p.dim) return;
+  s = 0.0f;
+  for (int i = 0; i < 16; ++i) s += red[i][lane];
+  out[(int64_t)gate * p.dim + c] = s;
+}
+
+// The gradients of a batch of no tokens.
+__global__ __launch_bounds__(256) void block_zero_kernel(float* out, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) out[i] = 0.0f;
+}
+
+// ---------------------------------------------------------------- host
+
+template <typename T, typename S, int W, int CH, bool WIDE>
+void launch(const BlockP& p, bool back, unsigned grid, hipStream_t s) {
+  constexpr int N = W > 4 ? 64 * W : 256;
+  if (back)
+    hipLaunchKernelGGL((block_norm_bwd_kernel<T, S, W, CH, WIDE>), dim3(grid), dim3(N), 0, s, p);
+  else
+    hipLaunchKernelGGL((block_norm_kernel<T, S, W, CH, WIDE>), dim3(grid), dim3(N), 0, s, p);
+}
+
+// Waves of a row and runs of eight a thread, by the width: at most 16 values a thread, so that
+// backward the five sums stay in registers.
+struct Width {
+  int waves, runs;
+};
+Width width_of(int dim) {
+  if (dim <= 512) return {1, 1};
+  if (dim <= 1024) return {1, 2};
+  if (dim <= 2048) return {2, 2};
+  if (dim <= 4096) return {4, 2};
+  if (dim <= 8192) return {8, 2};
+  return {16, 2};
+}
+int rows_of(int dim) {
+  const int w = width_of(dim).waves;
+  return w > 4 ? 1 : 4 / w;
+}
+
+template <typename T, typename S, bool WIDE>
+void launch_width(const BlockP& p, bool back, unsigned grid, hipStream_t s) {
+  const Width w = width_of(p.dim);
+  if (w.waves == 1) return w.runs == 1 ? launch<T, S, 1, 1, WIDE>(p, back, grid, s) : launch<T, S, 1, 2, WIDE>(p, back, grid, s);
+  if (w.waves == 2) return launch<T, S, 2, 2, WIDE>(p, back, grid, s);
+  if (w.waves == 4) return launch<T, S, 4, 2, WIDE>(p, back, grid, s);
+  if (w.waves == 8) return launch<T, S, 8, 2, WIDE>(p, back, grid, s);
+  launch<T, S, 16, 2, WIDE>(p, back, grid, s);
+}
+
+template <bool WIDE>
+void launch_types(const BlockP& p, bool bf16, bool stream_bf16, bool back, unsigned grid, hipStream_t s) {
+  if (!bf16) return launch_width<float, float, WIDE>(p, back, grid, s);
+  if (stream_bf16) return launch_width<uint16_t, uint16_t, WIDE>(p, back, grid, s);
+  launch_width<uint16_t, float, WIDE>(p, back, grid, s);
+}
+
+bool check_sizes(const elasto_block_norm_t* d) {
+  if (!d) return fail(ELASTO_ERR_INVALID_ARG, "block_norm: NULL description"), false;
+  const bool types = (d->dtype == ELASTO_BF16 && (d->stream_dtype == ELASTO_BF16 || d->stream_dtype == ELASTO_FP32)) ||
+                     (d->dtype == ELASTO_FP32 && d->stream_dtype == ELASTO_FP32);
+  if (!types) return fail(ELASTO_ERR_INVALID_ARG, "block_norm: bad dtypes %d and %d", d->dtype, d->stream_dtype), false;
+  if (d->batch < 0 || d->tokens < 0 || d->dim < 1 || d->dim > kMaxDim || (int64_t)d->batch * d->tokens > (1 << 25))
+    return fail(ELASTO_ERR_INVALID_ARG, "block_norm: bad batch, tokens or dim"), false;
+  return true;
+}
+
+struct Slices {
+  int per;        // workgroups of a sequence
+  int grid;
+};
+Slices slices_of(const elasto_block_norm_t& d) {
+  const int64_t rounds = (d.tokens + rows_of(d.dim) - 1) / std::max(1, rows_of(d.dim));
+  const int64_t per = std::max<int64_t>(1, std::min<int64_t>(rounds, kGradBlocks / std::max(1, d.batch)));
+  return {(int)per, (int)std::min<int64_t>((int64_t)d.batch * per, kGradBlocks)};
+}
+
+bool check_desc(const elasto_block_norm_t* d) {
+  if (!check_sizes(d)) return false;
+  if (d->kind != ELASTO_NORM_RMS && d->kind != ELASTO_NORM_LAYER)
+    return fail(ELASTO_ERR_INVALID_ARG, "block_norm: bad kind %d", d->kind), false;
+  if (!(d->eps >= 1.17549435e-38f) || !(d->eps < INFINITY) || !(fabsf(d->residual_scale) < INFINITY))
+    return fail(ELASTO_ERR_INVALID_ARG, "block_norm: eps must be a positive normal number, residual_scale finite"), false;
+  if (!d->post_norm && (d->post_gamma || d->post_beta))
+    return fail(ELASTO_ERR_INVALID_ARG, "block_norm: weights without their norm"), false;
+  if (d->kind == ELASTO_NORM_RMS && (d->pre_beta || d->post_beta))
+    return fail(ELASTO_ERR_INVALID_ARG, "block_norm: the RMS norm has no beta"), false;
+  for (const void* p : {(const void*)d->pre_gamma, (const void*)d->pre_beta, (const void*)d->post_gamma,
+                        (const void*)d->post_beta, (const void*)d->gate, (const void*)d->lens})
+    if (!aligned(p, 4)) return fail(ELASTO_ERR_INVALID_ARG, "block_norm: misaligned pointer"), false;
+  return true;
+}
+
+// *r from t (NULL or of no data: r->p stays NULL).
+bool take(const char* name, const elasto_rows_t* t, const elasto_block_norm_t& d, int es, bool needed, bool written,
+          Rows* r) {
+  *r = Rows{nullptr, 0, 0};
+  if (!t || !t->data) {
+    if (needed) return fail(ELASTO_ERR_INVALID_ARG, "block_norm: %s is NULL", name), false;
+    return true;
+  }
+  if (!aligned(t->data, es)) return fail(ELASTO_ERR_INVALID_ARG, "block_norm: %s is misaligned", name), false;
+  if (t->batch_stride < 0 || t->token_stride < 0)
+    return fail(ELASTO_ERR_INVALID_ARG, "block_norm: %s has a negative stride", name), false;
+  if (written && ((d.batch > 1 && t->batch_stride < d.dim) || (d.tokens > 1 && t->token_stride < d.dim)))
+    return fail(ELASTO_ERR_INVALID_ARG, "block_norm: rows of %s overlap", name), false;
+  *r = Rows{static_cast<char*>(t->data), t->batch_stride * es, t->token_stride * es};
+  return true;
+}
+
+BlockP params(const elasto_block_norm_t& d) {
+  BlockP p = {};
+  p.pre_gamma = d.pre_gamma;
+  p.pre_beta = d.pre_beta;
+  p.post_gamma = d.post_gamma;
+  p.post_beta = d.post_beta;
+  p.gate = d.gate;
+  p.gate_ld = d.gate_per_sequence ? d.dim : 0;
+  p.lens = d.lens;
+  p.batch = d.batch;
+  p.tokens = d.tokens;
+  p.dim = d.dim;
+  p.layer = d.kind == ELASTO_NORM_LAYER;
+  p.post = d.post_norm != 0;
+  p.a = d.residual_scale;
+  p.eps = d.eps;
+  p.inv_dim = 1.0f / (float)d.dim;
+  return p;
+}
+
+// Whether everything starts at, and goes in steps of, 16 bytes.
+bool wide(const BlockP& p) {
+  auto ok = [](const Rows& r) { return aligned(r.p, 16) && r.sb % 16 == 0 && r.st % 16 == 0; };
+  for (const Rows* r : {&p.x, &p.y, &p.x_out, &p.u, &p.dx_out, &p.du, &p.dx, &p.dy})
+    if (r->p && !ok(*r)) return false;
+  for (const void* w : {(const void*)p.pre_gamma, (const void*)p.pre_beta, (const void*)p.post_gamma,
+                        (const void*)p.post_beta, (const void*)p.gate})
+    if (!aligned(w, 16)) return false;
+  return p.dim % 8 == 0;
+}
+
+}  // namespace
+}  // namespace elasto
+
+using namespace elasto;
+
+extern "C" {
+
+elasto_status_t elasto_op_block_norm(const elasto_block_norm_t* d, const elasto_rows_t* x, const elasto_rows_t* y,
+                                     const elasto_rows_t* x_out, const elasto_rows_t* u, void* hip_stream) {
+  if (!check_desc(d)) return ELASTO_ERR_INVALID_ARG;
+  const int64_t rows = (int64_t)d->batch * d->tokens;
+  if (rows == 0) return ELASTO_OK;
+  const int es = d->dtype == ELASTO_BF16 ? 2 : 4, ss = d->stream_dtype == ELASTO_BF16 ? 2 : 4;
+  BlockP p = params(*d);
+  if (!take("x", x, *d, ss, true, false, &p.x) || !take("y", y, *d, es, false, false, &p.y) ||
+      !take("x_out", x_out, *d, ss, false, true, &p.x_out) || !take("u", u, *d, es, false, true, &p.u))
+    return ELASTO_ERR_INVALID_ARG;
+  p.has_y = p.y.p != nullptr;
+  if (!p.x_out.p && !p.u.p) return fail(ELASTO_ERR_INVALID_ARG, "block_norm: neither x_out nor u is asked for");
+  if (!p.has_y && (p.post || p.gate)) return fail(ELASTO_ERR_INVALID_ARG, "block_norm: a norm or gate of no y");
+  const int per = rows_of(d->dim);
+  const unsigned grid = (unsigned)((rows + per - 1) / per);
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if (wide(p))
+    launch_types<true>(p, es == 2, ss == 2, false, grid, s);
+  else
+    launch_types<false>(p, es == 2, ss == 2, false, grid, s);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(ELASTO_ERR_HIP, "block_norm: %s", hipGetErrorString(e));
+  return ELASTO_OK;
+}
+
+elasto_status_t elasto_op_block_norm_bwd(const elasto_block_norm_t* d, const elasto_rows_t* x_out,
+                                         const elasto_rows_t* y, const elasto_rows_t* dx_out,
+                                         const elasto_rows_t* du, const elasto_rows_t* dx, const elasto_rows_t* dy,
+                                         float* d_pre_gamma, float* d_pre_beta, float* d_post_gamma,
+                                         float* d_post_beta, float* d_gate, void* workspace,
+                                         int64_t workspace_bytes, void* hip_stream) {
+  if (!check_desc(d)) return ELASTO_ERR_INVALID_ARG;
+  const int64_t rows = (int64_t)d->batch * d->tokens;
+  const int es = d->dtype == ELASTO_BF16 ? 2 : 4, ss = d->stream_dtype == ELASTO_BF16 ? 2 : 4;
+  BlockP p = params(*d);
+  if (rows > 0) {
+    if (!take("x_out", x_out, *d, ss, du && du->data, false, &p.x_out) || !take("y", y, *d, es, false, false, &p.y) ||
+        !take("dx_out", dx_out, *d, ss, false, false, &p.dx_out) || !take("du", du, *d, es, false, false, &p.du) ||
+        !take("dx", dx, *d, ss, false, true, &p.dx) || !take("dy", dy, *d, es, false, true, &p.dy))
+      return ELASTO_ERR_INVALID_ARG;
+    p.has_y = p.y.p != nullptr;
+    if (!p.dx_out.p && !p.du.p) return fail(ELASTO_ERR_INVALID_ARG, "block_norm: neither dx_out nor du is given");
+    if (!p.has_y && (p.post || p.gate || p.dy.p))
+      return fail(ELASTO_ERR_INVALID_ARG, "block_norm: a norm, gate or gradient of no y");
+    if (!p.du.p && (d_pre_gamma || d_pre_beta))
+      return fail(ELASTO_ERR_INVALID_ARG, "block_norm: gradients of pre_gamma and pre_beta need du");
+  }
+  if ((d_post_gamma || d_post_beta) && !d->post_norm)
+    return fail(ELASTO_ERR_INVALID_ARG, "block_norm: gradients of weights without their norm");
+  if ((d_pre_beta || d_post_beta) && d->kind == ELASTO_NORM_RMS)
+    return fail(ELASTO_ERR_INVALID_ARG, "block_norm: the RMS norm has no beta");
+  if (d_gate && !d->gate) return fail(ELASTO_ERR_INVALID_ARG, "block_norm: the gradient of no gate");
+  float* const out[kSums] = {d_pre_gamma, d_pre_beta, d_post_gamma, d_post_beta, d_gate};
+  for (int i = 0; i < kSums; ++i) {
+    if (!aligned(out[i], 4)) return fail(ELASTO_ERR_INVALID_ARG, "block_norm: misaligned pointer");
+    if (out[i]) p.wanted |= 1 << i;
+  }
+  const bool per_sequence = d->gate_per_sequence != 0;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  hipError_t e = hipSuccess;
+  if (rows == 0) {
+    for (int i = 0; i < kSums && e == hipSuccess; ++i) {
+      const int64_t n = (i == 4 && per_sequence ? (int64_t)d->batch : 1) * d->dim;
+      if (!out[i] || n == 0) continue;
+      hipLaunchKernelGGL(block_zero_kernel, dim3((unsigned)std::min<int64_t>((n + 255) / 256, 4096)), dim3(256), 0, s,
+                         out[i], n);
+      e = hipGetLastError();
+    }
+    if (e != hipSuccess) return fail(ELASTO_ERR_HIP, "block_norm: %s", hipGetErrorString(e));
+    return ELASTO_OK;
+  }
+  const Slices sl = slices_of(*d);
+  p.slices = sl.per;
+  if (d_gate && per_sequence && sl.per == 1) p.dgate = d_gate;
+  const int sums = p.wanted & ~(p.dgate ? 16 : 0);
+  if (sums) {
+    const int64_t need = (int64_t)sl.grid * kSums * d->dim * 4;
+    if (need > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < need))
+      return fail(ELASTO_ERR_INVALID_ARG, "block_norm: the workspace holds %lld of %lld bytes",
+                  (long long)(workspace ? workspace_bytes : 0), (long long)need);
+    p.part = static_cast<float*>(workspace);
+  }
+  if (wide(p))
+    launch_types<true>(p, es == 2, ss == 2, true, (unsigned)sl.grid, s);
+  else
+    launch_types<false>(p, es == 2, ss == 2, true, (unsigned)sl.grid, s);
+  e = hipGetLastError();
+  if (e == hipSuccess && sums) {
+    SumP q = {};
+    q.part = p.part;
+    for (int i = 0; i < kSums; ++i) q.out[i] = i == 4 && p.dgate ? nullptr : out[i];
+    q.dim = d->dim;
+    q.parts = sl.grid;
+    q.gates = per_sequence ? d->batch : 1;
+    q.gate_parts = per_sequence ? sl.per : sl.grid;
+    const unsigned gates = q.out[4] ? (unsigned)q.gates : 0;
+    hipLaunchKernelGGL(block_sum_kernel, dim3((unsigned)((d->dim + 63) / 64), 4 + gates), dim3(1024), 0, s, q);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess) return fail(ELASTO_ERR_HIP, "block_norm: %s", hipGetErrorString(e));
+  return ELASTO_OK;
+}
+
+elasto_status_t elasto_block_norm_workspace(const elasto_block_norm_t* d, int64_t* bytes) {
+  if (!bytes) return fail(ELASTO_ERR_INVALID_ARG, "NULL argument");
+  if (!check_sizes(d)) return ELASTO_ERR_INVALID_ARG;
+  *bytes = (int64_t)slices_of(*d).grid * kSums * d->dim * 4;
+  return ELASTO_OK;
+}
+
+}  // extern "C"

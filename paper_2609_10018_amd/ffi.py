@@ -104,6 +104,21 @@ class Window(ctypes.Structure):
                [("scale", c_f32), ("q_lens", c_vp), ("k_lens", c_vp)]
 
 
+class Rows(ctypes.Structure):
+    _fields_ = [("data", c_vp), ("batch_stride", c_i64), ("token_stride", c_i64)]
+
+
+class BlockNorm(ctypes.Structure):
+    _fields_ = [(n, c_i32) for n in ("dtype", "stream_dtype", "kind", "batch", "tokens", "dim",
+                                     "post_norm", "gate_per_sequence")] + \
+               [("residual_scale", c_f32), ("eps", c_f32)] + \
+               [(n, c_vp) for n in ("pre_gamma", "pre_beta", "post_gamma", "post_beta", "gate",
+                                    "lens")]
+
+
+NORM_KINDS = {"rms": 0, "layer": 1}   # elasto_norm_t
+
+
 class LinearCE(ctypes.Structure):
     _fields_ = [("dtype", c_i32), ("dim", c_i32), ("classes", c_i32), ("rows", c_i64),
                 ("x", c_vp), ("ldx", c_i64), ("weight", c_vp), ("ldw", c_i64), ("bias", c_vp),
@@ -165,6 +180,9 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
         "elasto_op_qk_norm_rotate_axes": [P(QkAxes)] + [P(Heads)] * 4 + [c_vp],
         "elasto_op_qk_norm_rotate_axes_bwd": [P(QkAxes)] + [P(Heads)] * 6 + [c_vp, c_vp, c_vp, c_i64,
                                                                             c_vp],
+        "elasto_op_block_norm": [P(BlockNorm)] + [P(Rows)] * 4 + [c_vp],
+        "elasto_op_block_norm_bwd": [P(BlockNorm)] + [P(Rows)] * 6 + [c_vp] * 6 + [c_i64, c_vp],
+        "elasto_block_norm_workspace": [P(BlockNorm), P(c_i64)],
         "elasto_op_linear_ce": [P(LinearCE), c_vp, c_vp, c_vp, c_i64, c_vp],
         "elasto_op_linear_ce_bwd": [P(LinearCE), c_vp, c_f32, c_vp, c_i64, c_vp, c_i64, c_vp, c_vp,
                                     c_i64, c_vp],
@@ -721,6 +739,100 @@ def op_distill(logits, teacher_values, teacher_indices, loss, dlogits=None, labe
         _plain(loss, f32, "loss", r), gd, grad, ldg, _stream_ptr(stream, dev)))
 
 
+def _tokens(t, shape, dtype, name: str):
+    """A [batch, tokens, dim] tensor as the C ABI takes it (None: NULL)."""
+    if t is None:
+        return None
+    if t.shape != shape or t.dtype is not dtype:
+        raise ValueError(f"{name} is {tuple(t.shape)} {t.dtype}, not {tuple(shape)} {dtype}")
+    b, r, f = t.stride()
+    nb, nr, n = shape
+    if f != 1 and n > 1:
+        raise ValueError(f"the features of {name} must be contiguous")
+    return Rows(t.data_ptr(), b if nb > 1 else n, r if nr > 1 else n)
+
+
+def _block_desc(stream, y, gate, pre_gamma, pre_beta, post_gamma, post_beta, post_norm, lens,
+                residual_scale, eps, kind):
+    """The description, the tokens' shape and the two types; stream: a tensor of the stream's
+    type, y: one of the blocks' type."""
+    shape = stream.shape
+    if len(shape) != 3:
+        raise ValueError(f"tokens must be [batch, tokens, dim], not {tuple(shape)}")
+    b, t, d = shape
+    _fits(b, t, d)
+    f32 = _tt().f32
+    per = gate is not None and gate.dim() == 2
+    if gate is not None and gate.shape != ((b, d) if per else (d,)):
+        raise ValueError(f"gate is {tuple(gate.shape)}, not {(d,)} or {(b, d)}")
+    if kind not in NORM_KINDS:
+        raise ValueError(f"kind {kind!r} is none of {sorted(NORM_KINDS)}")
+    a = BlockNorm(_dtype(y), _dtype(stream), NORM_KINDS[kind], b, t, d, 1 if post_norm else 0,
+                  1 if per else 0, residual_scale, eps, _plain(pre_gamma, f32, "pre_gamma", d),
+                  _plain(pre_beta, f32, "pre_beta", d), _plain(post_gamma, f32, "post_gamma", d),
+                  _plain(post_beta, f32, "post_beta", d), _plain(gate, f32, "gate"),
+                  _plain(lens, _tt().i32, "lens", b))
+    return a, shape, stream.dtype, y.dtype
+
+
+def _first(*tensors):
+    for t in tensors:
+        if t is not None:
+            return t
+    raise ValueError("no tensor is given")
+
+
+def block_norm_workspace(tokens, gate=None) -> int:
+    """Workspace bytes of op_block_norm_bwd for a [batch, tokens, dim] tensor (and gate)."""
+    n = c_i64()
+    a = _block_desc(tokens, tokens, gate, None, None, None, None, False, None, 1.0, 1.0, "rms")[0]
+    check(load_library().elasto_block_norm_workspace(a, ctypes.byref(n)))
+    return n.value
+
+
+def op_block_norm(x, y=None, x_out=None, u=None, gate=None, pre_gamma=None, pre_beta=None,
+                  post_gamma=None, post_beta=None, post_norm: bool = False, lens=None,
+                  residual_scale: float = 1.0, eps: float = 1e-6, kind: str = "rms",
+                  stream=None) -> None:
+    """Between two blocks: x_out = residual_scale x + gate * norm(y) (post_norm False: * y) and u =
+    norm(x_out), the next block's input.  x, x_out: [batch, tokens, dim] device tensors of the stream's
+    type; y, u: of the blocks' (bf16 or fp32; the stream may be fp32 beside bf16 blocks), any strides of
+    batch and tokens.  y, and x_out or u, may be None.  gate: fp32 [dim] or [batch, dim]; the
+    weights fp32 [dim]; lens int32 [batch]; or None.  kind: "rms" or "layer"."""
+    dev = _same_device(x, y, x_out, u, gate, pre_gamma, pre_beta, post_gamma, post_beta, lens)
+    a, shape, st, dt = _block_desc(x, _first(y, u, x), gate, pre_gamma, pre_beta, post_gamma,
+                                   post_beta, post_norm, lens, residual_scale, eps, kind)
+    check(load_library().elasto_op_block_norm(
+        a, _tokens(x, shape, st, "x"), _tokens(y, shape, dt, "y"),
+        _tokens(x_out, shape, st, "x_out"), _tokens(u, shape, dt, "u"), _stream_ptr(stream, dev)))
+
+
+def op_block_norm_bwd(x_out, y, dx_out, du, dx=None, dy=None, d_pre_gamma=None, d_pre_beta=None,
+                      d_post_gamma=None, d_post_beta=None, d_gate=None, workspace=None, gate=None,
+                      pre_gamma=None, pre_beta=None, post_gamma=None, post_beta=None,
+                      post_norm: bool = False, lens=None, residual_scale: float = 1.0,
+                      eps: float = 1e-6, kind: str = "rms", stream=None) -> None:
+    """The gradients of op_block_norm from dx_out and du (one of them may be None), with its x_out
+    (None without du) and y: dx, dy like x and y, the weights' fp32 and shaped like them, each or
+    None.  workspace: a uint8 device tensor of block_norm_workspace() bytes where a weight's gradient
+    is asked for."""
+    dev = _same_device(x_out, y, dx_out, du, dx, dy, d_pre_gamma, d_pre_beta, d_post_gamma,
+                       d_post_beta, d_gate, workspace, gate, pre_gamma, pre_beta, post_gamma,
+                       post_beta, lens)
+    s = _first(x_out, dx_out, dx)
+    a, shape, st, dt = _block_desc(s, _first(y, du, dy, s), gate, pre_gamma, pre_beta, post_gamma,
+                                   post_beta, post_norm, lens, residual_scale, eps, kind)
+    f32, d = _tt().f32, shape[2]
+    check(load_library().elasto_op_block_norm_bwd(
+        a, _tokens(x_out, shape, st, "x_out"), _tokens(y, shape, dt, "y"),
+        _tokens(dx_out, shape, st, "dx_out"), _tokens(du, shape, dt, "du"),
+        _tokens(dx, shape, st, "dx"), _tokens(dy, shape, dt, "dy"),
+        _plain(d_pre_gamma, f32, "d_pre_gamma", d), _plain(d_pre_beta, f32, "d_pre_beta", d),
+        _plain(d_post_gamma, f32, "d_post_gamma", d), _plain(d_post_beta, f32, "d_post_beta", d),
+        _plain(d_gate, f32, "d_gate", -1 if gate is None else gate.numel()), *_space(workspace),
+        _stream_ptr(stream, dev)))
+
+
 def _ce_desc(x, weight, labels, bias, row_weight):
     """The description; labels None: of the shapes alone."""
     r, d, ldx = _rows(x, "x")
@@ -1039,5 +1151,6 @@ __all__ = ["ElasticViT", "ElasticResNet", "cnn_validate", "select_mode", "Elasto
            "op_window_attention", "op_window_attention_bwd", "window_attention_workspace",
            "op_top_logits", "op_distill",
            "op_linear_cross_entropy", "op_linear_cross_entropy_bwd", "linear_cross_entropy_workspace",
+           "op_block_norm", "op_block_norm_bwd", "block_norm_workspace",
            "GradList", "op_grad_norm", "op_clip_gradients", "grad_norm_workspace",
            "KERNELS", "FP32", "BF16"]

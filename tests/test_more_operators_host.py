@@ -211,3 +211,93 @@ def test_axes_of_no_tokens_is_no_error(lib):
     for kw in (dict(batch=0), dict(tokens=0)):
         d = axes_desc(**kw, positions=None, cos=None, sin=None)
         assert lib.elasto_op_qk_norm_rotate_axes(d, None, None, None, None, None) == 0
+
+
+# ------------------------------------------------------------------- between blocks
+
+def rows(data=P256, b=1 << 16, t=768):
+    return ffi.Rows(data, b, t)
+
+
+def block(**kw):
+    d = dict(dtype=1, stream_dtype=0, kind=1, batch=2, tokens=8, dim=64, post_norm=1, gate_per_sequence=0,
+             residual_scale=1.0, eps=1e-6, pre_gamma=P256, pre_beta=P256, post_gamma=P256, post_beta=P256,
+             gate=P256, lens=None)
+    d.update(kw)
+    return ffi.BlockNorm(*[d[n] for n, _ in ffi.BlockNorm._fields_])
+
+
+def block_fwd(lib, d, x=rows(), y=rows(), x_out=rows(), u=rows()):
+    return lib.elasto_op_block_norm(d, x, y, x_out, u, None)
+
+
+def block_bwd(lib, d, x_out=rows(), y=rows(), dx_out=rows(), du=rows(), dx=rows(), dy=rows(), grads=(P256,) * 5,
+              ws=P256, size=1 << 40):
+    return lib.elasto_op_block_norm_bwd(d, x_out, y, dx_out, du, dx, dy, *grads, ws, size, None)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(dtype=2), dict(stream_dtype=3), dict(dtype=0, stream_dtype=1), dict(kind=2), dict(kind=-1), dict(batch=-1),
+    dict(tokens=-1), dict(dim=0), dict(dim=16385), dict(batch=1 << 13, tokens=1 << 13), dict(eps=0.0),
+    dict(eps=1e-39), dict(eps=math.inf), dict(eps=math.nan), dict(residual_scale=math.inf),
+    dict(residual_scale=math.nan), dict(post_norm=0), dict(kind=0), dict(pre_gamma=P256 + 2),
+    dict(post_beta=P256 + 1), dict(gate=P256 + 2), dict(lens=P256 + 2)])
+def test_block_norm_refuses_bad_descriptions(lib, kw):
+    assert block_fwd(lib, block(**kw)) == INVALID
+    assert block_bwd(lib, block(**kw)) == INVALID
+    assert lib.elasto_last_error()
+
+
+def test_block_norm_refuses_bad_tensors(lib):
+    for bad in (rows(P256 + 1), rows(b=-768), rows(t=-64)):
+        for name in ("x", "y", "x_out", "u"):
+            assert block_fwd(lib, block(), **{name: bad}) == INVALID
+        for name in ("x_out", "y", "dx_out", "du", "dx", "dy"):
+            assert block_bwd(lib, block(), **{name: bad}) == INVALID
+    for bad in (rows(b=63), rows(t=0), rows(t=63)):      # rows that overlap
+        for name in ("x_out", "u"):
+            assert block_fwd(lib, block(), **{name: bad}) == INVALID
+        for name in ("dx", "dy"):
+            assert block_bwd(lib, block(), **{name: bad}) == INVALID
+    assert block_fwd(lib, None) == INVALID and block_bwd(lib, None) == INVALID
+    assert block_fwd(lib, block(), x=None) == INVALID
+    assert block_fwd(lib, block(), x_out=None, u=None) == INVALID
+    assert block_fwd(lib, block(), y=None) == INVALID                       # a norm and a gate of nothing
+    assert block_fwd(lib, block(post_norm=0, post_gamma=None, post_beta=None), y=None) == INVALID
+
+
+def test_block_norm_backward_refuses_what_does_not_go_together(lib):
+    none = (None,) * 5
+    assert block_bwd(lib, block(), x_out=None) == INVALID                   # du needs it
+    assert block_bwd(lib, block(), dx_out=None, du=None, grads=none) == INVALID
+    assert block_bwd(lib, block(), y=None, dy=None, grads=none) == INVALID
+    assert block_bwd(lib, block(), du=None) == INVALID                      # gradients of pre_gamma and pre_beta
+    bare = dict(post_norm=0, post_gamma=None, post_beta=None)
+    assert block_bwd(lib, block(**bare)) == INVALID                         # of weights that are not there
+    assert block_bwd(lib, block(gate=None), grads=(None,) * 4 + (P256,)) == INVALID
+    assert block_bwd(lib, block(kind=0, pre_beta=None, post_beta=None), grads=(None, P256, None, None, None)) == INVALID
+    assert block_bwd(lib, block(**bare, gate=None), y=None, grads=none) == INVALID     # dy of no y
+    for i in range(5):
+        grads = [None] * 5
+        grads[i] = P256 + 2
+        assert block_bwd(lib, block(), grads=grads) == INVALID
+    n = ctypes.c_int64()
+    assert lib.elasto_block_norm_workspace(block(), ctypes.byref(n)) == 0 and n.value > 0
+    assert lib.elasto_block_norm_workspace(block(), None) == INVALID
+    assert lib.elasto_block_norm_workspace(block(dim=0), ctypes.byref(n)) == INVALID
+    for ws, size in ((None, n.value), (P256 + 8, n.value), (P256, n.value - 1)):
+        assert block_bwd(lib, block(), ws=ws, size=size) == INVALID
+
+
+def test_block_norm_binding_refuses_tensors_that_do_not_fit():
+    torch = pytest.importorskip("torch")
+    x = torch.zeros(2, 3, 8)
+    for args in ((x[0], None), (x, torch.zeros(3, 8)), (x, torch.zeros(7))):
+        with pytest.raises(ValueError):
+            ffi.block_norm_workspace(*args)
+
+
+def test_block_norm_of_no_tokens_is_no_error(lib):
+    for kw in (dict(batch=0), dict(tokens=0)):
+        assert block_fwd(lib, block(**kw), None, None, None, None) == 0
+        assert block_bwd(lib, block(**kw), None, None, None, None, None, None, (None,) * 5, None, 0) == 0
