@@ -36,7 +36,8 @@ struct CeP {
   float2* part;   // forward: [tiles of classes][rows]
   float* picked;  // forward: the label's logit
   const uint32_t* live;
-  float* db_part;  // [tiles of rows][piece]
+  float* db_part;  // [tiles of rows][ld_db]
+  int64_t ld_db;
   int tiles_m, tiles_n, group;
   int label_classes;  // all classes
 };
@@ -74,9 +75,25 @@ __device__ __forceinline__ void logits(char* smem, const CeP& p, int64_t m0, int
 // A reference for the exponentials of values up to m.
 __device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.0f : m; }
 
+// exp(z - ref) for many z as one multiply-add and 2^: the product ref log2(e) is rounded once, and what
+// that leaves out is the same factor for all of them (`left`).  Where ref lies so far out that the
+// rounding would leave the exponents' range, only what equals ref counts, and a smaller factor says so.
+struct Power {
+  float c, off, left;
+  __device__ __forceinline__ explicit Power(float ref) {
+#pragma clang fp contract(off)
+    constexpr float kFar = 1073741824.0f;
+    c = fabsf(ref * kLog2e) > kFar ? kFar / fabsf(ref) : kLog2e;
+    const float r = -ref * c;
+    off = r;
+    left = __builtin_amdgcn_exp2f(-fmaf(ref, c, r));
+  }
+  __device__ __forceinline__ float operator()(float z) const { return __builtin_amdgcn_exp2f(fmaf(z, c, off)); }
+};
+
 template <typename S>
-__global__ __launch_bounds__(S::kThreads) void ce_forward_kernel(CeP p) {
-  __shared__ __attribute__((aligned(1024))) char smem[2 * S::kStage];
+__global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_forward_kernel(CeP p) {
+  __shared__ __attribute__((aligned(1024))) char smem[S::STAGES * S::kStage];
   int tm, tn;
   tile_of(blockIdx.x, p.tiles_m, p.tiles_n, p.group, tm, tn);
   const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
@@ -94,13 +111,14 @@ __global__ __launch_bounds__(S::kThreads) void ce_forward_kernel(CeP p) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) m = fmaxf(m, acc[i][j][e]);
     m = fmaxf(m, __shfl_xor(m, 32, 64));
-    const float ref = reference(m);
+    const Power power(reference(m));
     float s = 0.0f;
 #pragma unroll
     for (int j = 0; j < S::TN; ++j)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s += __builtin_amdgcn_exp2f((acc[i][j][e] - ref) * kLog2e);
+      for (int e = 0; e < 16; ++e) s += power(acc[i][j][e]);
     s += __shfl_xor(s, 32, 64);
+    s *= power.left;
     const int r = wm * S::WTM + i * 32 + lr;
     if (lg == 0) red[wn * S::BM + r] = make_float2(m, s);
     // The label's logit, by the one lane that holds it.
@@ -190,11 +208,39 @@ __device__ __forceinline__ void store4(uint16_t* p, const float* v) {
   *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
 }
 
+// A wave's block of 32 rows x S::WTN columns as rows: through the wave's part of LDS, from which each
+// lane takes 16 bytes of a row.  each(row, first column, the 16 bytes) for the block's pieces.
+template <typename S, typename O>
+struct RowsOut {
+  static constexpr int kRow = S::WTN * (int)sizeof(O) + 16;
+  static constexpr int kPieces = S::WTN * (int)sizeof(O) / 16, kPer = 16 / (int)sizeof(O);
+  static constexpr int kWave = 32 * kRow;
+  static_assert(kWave * S::kThreads / 64 <= S::STAGES * S::kStage, "the tiles' LDS holds it");
+  template <typename F>
+  static __device__ __forceinline__ void go(char* mine, const f32x16 (&acc)[S::TN], int lane, F&& each) {
+    O* to = reinterpret_cast<O*>(mine + (lane & 31) * kRow) + 4 * (lane >> 5);
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float v[4] = {acc[j][4 * g], acc[j][4 * g + 1], acc[j][4 * g + 2], acc[j][4 * g + 3]};
+        store4(to + j * 32 + 8 * g, v);
+      }
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < kPieces / 2; ++i) {
+      const int r = (i * 64 + lane) / kPieces, c = (i * 64 + lane) % kPieces;
+      each(r, c * kPer, *reinterpret_cast<const u32x4*>(mine + r * kRow + c * 16));
+    }
+    asm volatile("" ::: "memory");
+  }
+};
+
 // dz of one tile of the piece.
 template <typename S>
-__global__ __launch_bounds__(S::kThreads) void ce_dz_kernel(CeP p) {
+__global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_dz_kernel(CeP p) {
   typedef typename S::T T;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * S::kStage];
+  __shared__ __attribute__((aligned(1024))) char smem[S::STAGES * S::kStage];
   int tm, tn;
   tile_of(blockIdx.x, p.tiles_m, p.tiles_n, p.group, tm, tn);
   const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
@@ -203,9 +249,12 @@ __global__ __launch_bounds__(S::kThreads) void ce_dz_kernel(CeP p) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / S::WN, wn = wave % S::WN, lr = lane & 31, lg = lane >> 5;
   const int first = (int)n0 + wn * S::WTN;  // of the wave's classes in the piece
+  typedef RowsOut<S, T> Out;
+  char* mine = smem + wave * Out::kWave;
+  __syncthreads();  // the tiles have been read
 #pragma unroll
   for (int i = 0; i < S::TM; ++i) {
-    const int64_t row = m0 + wm * S::WTM + i * 32 + lr;
+    const int64_t block = m0 + wm * S::WTM + i * 32, row = block + lr;
     float w = 0.0f, lse = 0.0f;
     int y = -1;
     if (row < p.rows) {
@@ -213,12 +262,14 @@ __global__ __launch_bounds__(S::kThreads) void ce_dz_kernel(CeP p) {
       w = y >= 0 && y < p.label_classes ? (p.weight ? p.weight[row] : 1.0f) : 0.0f;
       lse = p.lse[row];
     }
+    const Power power(lse);
+    const float f = w * power.left;
 #pragma unroll
     for (int j = 0; j < S::TN; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const float v = __builtin_amdgcn_exp2f((acc[i][j][e] - lse) * kLog2e);
-        acc[i][j][e] = w != 0.0f ? w * v : 0.0f;
+        const float v = f * power(acc[i][j][e]);
+        acc[i][j][e] = w != 0.0f ? v : 0.0f;
       }
     const int64_t at = y - p.c0 - first;
     if (w != 0.0f && at >= 0 && at < S::WTN)
@@ -227,16 +278,11 @@ __global__ __launch_bounds__(S::kThreads) void ce_dz_kernel(CeP p) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
           if (at == j * 32 + 8 * (e >> 2) + 4 * lg + (e & 3)) acc[i][j][e] -= w;
-    if (row < p.rows) {
-      T* out = reinterpret_cast<T*>(const_cast<char*>(p.dz.p) + row * p.dz.ld) + first + 4 * lg;
-#pragma unroll
-      for (int j = 0; j < S::TN; ++j)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const float v[4] = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-          store4(out + j * 32 + 8 * g, v);
-        }
-    }
+    Out::go(mine, acc[i], lane, [&](int r, int c, const u32x4& v) {
+      if (block + r < p.rows)
+        *reinterpret_cast<u32x4*>(const_cast<char*>(p.dz.p) + (block + r) * p.dz.ld +
+                                  (int64_t)(first + c) * (int)sizeof(T)) = v;
+    });
   }
   if (!p.db_part) return;
   // Sums over the tile's rows: over the wave's blocks, its lanes, then the waves.
@@ -258,7 +304,7 @@ __global__ __launch_bounds__(S::kThreads) void ce_dz_kernel(CeP p) {
     float s = red[c];
 #pragma unroll
     for (int k = 1; k < S::WM; ++k) s += red[k * S::BN + c];
-    p.db_part[(int64_t)tm * p.tiles_n * S::BN + n0 + c] = s;
+    if (n0 + c < p.ld_db) p.db_part[tm * p.ld_db + n0 + c] = s;
   }
 }
 
@@ -287,9 +333,9 @@ struct ProductP {
   int64_t chunk;    // of K
 };
 template <typename S, bool TA, bool LIVE>
-__global__ __launch_bounds__(S::kThreads) void ce_product_kernel(ProductP p) {
+__global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_product_kernel(ProductP p) {
   typedef typename S::T T;
-  __shared__ __attribute__((aligned(1024))) char smem[2 * S::kStage];
+  __shared__ __attribute__((aligned(1024))) char smem[S::STAGES * S::kStage];
   const int tiles = p.tiles_m * p.tiles_n, part = blockIdx.x / tiles;
   int tm, tn;
   tile_of(blockIdx.x - part * tiles, p.tiles_m, p.tiles_n, p.group, tm, tn);
@@ -304,35 +350,31 @@ __global__ __launch_bounds__(S::kThreads) void ce_product_kernel(ProductP p) {
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
   tile_product<S, TA, true, LIVE>(smem, p.a, p.b, p.M, p.N, m0, n0, k0, k1, p.live, acc);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t r0 = m0 + wave / S::WN * S::WTM + (lane & 31);
-  const int64_t c0 = n0 + wave % S::WN * S::WTN + 4 * (lane >> 5);
+  const int64_t r0 = m0 + wave / S::WN * S::WTM, c0 = n0 + wave % S::WN * S::WTN;
+  __syncthreads();  // the tiles have been read
 #pragma unroll
   for (int i = 0; i < S::TM; ++i) {
-    const int64_t r = r0 + i * 32;
-    if (r >= p.M) continue;
+    const int64_t block = r0 + i * 32;
+    if (p.sum) {
+      typedef RowsOut<S, float> Out;
+      Out::go(smem + wave * Out::kWave, acc[i], lane, [&](int r, int c, const u32x4& v) {
+        if (block + r >= p.M || c0 + c >= p.N) return;
+        f32x4* at = reinterpret_cast<f32x4*>(p.sum + (part * p.M + block + r) * p.ld_sum + c0 + c);
+        f32x4 f = __builtin_bit_cast(f32x4, v);
+        if (p.add) f += *at;
+        *at = f;
+      });
+    } else {
+      typedef RowsOut<S, T> Out;
 #pragma unroll
-    for (int j = 0; j < S::TN; ++j)
+      for (int j = 0; j < S::TN; ++j)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int64_t c = c0 + j * 32 + 8 * g;
-        if (c >= p.N) continue;
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * g + e];
-        if (p.sum) {
-          float* at = p.sum + (part * p.M + r) * p.ld_sum + c;
-          if (p.add) {
-            const f32x4 o = *reinterpret_cast<const f32x4*>(at);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += o[e];
-          }
-          store4(at, v);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] *= p.scale;
-          store4(reinterpret_cast<T*>(p.out + r * p.ldo) + c, v);
-        }
-      }
+        for (int e = 0; e < 16; ++e) acc[i][j][e] *= p.scale;
+      Out::go(smem + wave * Out::kWave, acc[i], lane, [&](int r, int c, const u32x4& v) {
+        if (block + r < p.M && c0 + c < p.N)
+          *reinterpret_cast<u32x4*>(p.out + (block + r) * p.ldo + (c0 + c) * (int)sizeof(T)) = v;
+      });
+    }
   }
 }
 
@@ -371,18 +413,90 @@ __global__ __launch_bounds__(256) void ce_zero_db_kernel(float* db, int64_t n) {
 
 // ---------------------------------------------------------------- host
 
-constexpr int64_t kTile = 128;
 constexpr int64_t kMaxRows = 1 << 24, kMaxClasses = 1 << 30, kMaxDim = 1 << 20;
-constexpr int64_t kMaxTiles = 1 << 23;  // of a launch, of up to 512 threads each: below 2^32 threads
-
-struct Args {
-  elasto_linear_ce_t d;
-  Matrix x, w;
-  int es = 0;
-};
+constexpr int64_t kMaxTiles = 1 << 23;  // of 128 x 128, of 256 threads each: a launch holds fewer than 2^32
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
-int64_t tiles(int64_t n) { return (n + kTile - 1) / kTile; }
+int64_t tiles(int64_t n, int64_t b) { return (n + b - 1) / b; }
+
+// Tile shapes.  Large (bf16): one workgroup of eight waves a CU.  Middle: two workgroups.  Deep: one,
+// with three steps of loads in flight, where there are not two for each CU.  Small: two, for few tiles.
+enum class Kind { Large, Middle, Deep, Small };
+template <typename T, Kind K>
+struct ShapeOf;
+template <typename T>
+struct ShapeOf<T, Kind::Middle> {
+  typedef Shape<T, 128, 128, 2, 2, 128, 2, 2> S;
+};
+template <typename T>
+struct ShapeOf<T, Kind::Deep> {
+  typedef Shape<T, 128, 128, 2, 2, 128, 4, 1> S;
+};
+template <typename T>
+struct ShapeOf<T, Kind::Small> {
+  typedef Shape<T, 64, 64, 2, 2, 128, 4, 2> S;
+};
+template <>
+struct ShapeOf<uint16_t, Kind::Large> {
+  typedef Shape<uint16_t, 256, 256, 2, 4, 128, 2, 1> S;
+};
+template <>
+struct ShapeOf<float, Kind::Large> : ShapeOf<float, Kind::Middle> {};
+
+// f(Shape()) for the shape of kind k.
+template <typename T, typename F>
+void with_shape(Kind k, F&& f) {
+  switch (k) {
+    case Kind::Large: return f(typename ShapeOf<T, Kind::Large>::S());
+    case Kind::Middle: return f(typename ShapeOf<T, Kind::Middle>::S());
+    case Kind::Deep: return f(typename ShapeOf<T, Kind::Deep>::S());
+    default: return f(typename ShapeOf<T, Kind::Small>::S());
+  }
+}
+
+// What a round of workgroups takes, in us: `step` a step of 128 bytes of K where a CU holds all its workgroups,
+// `alone` where it holds one, and `end` for the first loads and the results.  Measured: bf16 4096 x 131072 x
+// 2048 58 us a round of Large tiles, 8192 x 1000 x 4096 67 of Middle ones (Large, which fill half of the
+// CUs: 82), 300 x 10007 x 1024 15 of Middle, alone (Large 28, two rounds of Small 21), 256 x 1000 x 768 7
+// of Small, alone (Middle 12); 128 x 32000 x 4096 54 of Deep (Middle 67); fp32 2048 x 20000 x 1024 131 of
+// Middle (four rounds of Small 160), 256 x 1000 x 768 19 of Small, alone (Middle 56).
+struct Round {
+  Kind kind;
+  int side, groups;  // tile, workgroups of a CU
+  float step, alone, end;
+};
+constexpr Round kRounds[2][4] = {{{Kind::Large, 256, 1, 1.6f, 1.6f, 8.0f},
+                                  {Kind::Middle, 128, 2, 1.0f, 0.75f, 3.5f},
+                                  {Kind::Deep, 128, 1, 0.7f, 0.7f, 4.5f},
+                                  {Kind::Small, 64, 2, 0.45f, 0.35f, 3.0f}},
+                                 {{Kind::Middle, 128, 2, 3.9f, 2.2f, 4.0f},
+                                  {Kind::Deep, 128, 1, 2.1f, 2.1f, 4.5f},
+                                  {Kind::Small, 64, 2, 1.18f, 0.68f, 3.0f},
+                                  {Kind::Small, 64, 2, 1.18f, 0.68f, 3.0f}}};
+
+// How a product of M x N over K runs: in tiles of a kind, and in parts of K that are summed afterwards.
+struct Way {
+  Kind kind;
+  int side, parts;
+};
+Way way_of(int64_t M, int64_t N, int64_t K, int es, bool may_split) {
+  Way best = {Kind::Small, 64, 1};
+  float least = INFINITY;
+  const int64_t steps = (K * es + 127) / 128;
+  for (const Round& r : kRounds[es == 4]) {
+    const int64_t t = tiles(M, r.side) * tiles(N, r.side), slots = 256 * r.groups;
+    // As many parts as fill the GPU once, of at least eight steps.
+    const int64_t parts = may_split ? std::max<int64_t>(1, std::min<int64_t>({slots / t, steps / 8, 64})) : 1;
+    const int64_t rounds = tiles(t * parts, slots), each = tiles(steps, parts);
+    float us = (float)rounds * ((t * parts <= 256 ? r.alone : r.step) * (float)each + r.end);
+    if (parts > 1) us += 3.0f + (float)(parts * M * N) * 8e-6f / 4.5f;
+    if (us < least) {
+      least = us;
+      best = {r.kind, r.side, (int)parts};
+    }
+  }
+  return best;
+}
 
 // Classes of a piece of the backward pass: a piece's dz takes about 256 MB (the cache
 // behind L2), but at least 2048 classes.
@@ -390,25 +504,21 @@ int64_t piece_of(const elasto_linear_ce_t& d, int es) {
   const int64_t fit = ((int64_t)256 << 20) / (std::max<int64_t>(1, d.rows) * es) / 256 * 256;
   return std::min(up(d.classes, 256), std::max<int64_t>(2048, fit));
 }
-// Parts of a piece that dx is summed in: two workgroups a CU, of at least eight steps.
-int parts_of(const elasto_linear_ce_t& d, int es, int64_t piece) {
-  const int64_t t = tiles(d.rows) * tiles(d.dim), steps = piece * es / 128;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(1, t), steps / 8, 64}));
-}
 
 struct BackLayout {
-  int64_t live = 0, dz = 0, db = 0, sum = 0, total = 0;
+  int64_t live = 0, dz = 0, db = 0, sum = 0, wsum = 0, total = 0;
   int64_t piece = 0;
-  int parts = 0;
-  bool summed = false;  // dx goes through fp32 sums
+  Way x = {}, w = {};     // of dx and of dW
+  bool x_summed = false;         // dx goes through fp32 sums
 };
 BackLayout backward_layout(const elasto_linear_ce_t& d) {
   const int es = d.dtype == ELASTO_BF16 ? 2 : 4;
   BackLayout l;
   if (d.rows == 0) return l;
   l.piece = piece_of(d, es);
-  l.parts = parts_of(d, es, l.piece);
-  l.summed = l.parts > 1 || l.piece < d.classes;
+  l.x = way_of(d.rows, d.dim, l.piece, es, true);
+  l.w = way_of(l.piece, d.dim, d.rows, es, true);
+  l.x_summed = l.x.parts > 1 || l.piece < d.classes;
   auto take = [&](int64_t bytes) {
     const int64_t at = l.total;
     l.total += up(bytes, 256);
@@ -416,13 +526,24 @@ BackLayout backward_layout(const elasto_linear_ce_t& d) {
   };
   l.live = take(up(d.rows, 256) / 8);
   l.dz = take(d.rows * l.piece * es);
-  l.db = take(tiles(d.rows) * l.piece * 4);
-  l.sum = take(l.summed ? (int64_t)l.parts * d.rows * d.dim * 4 : 0);
+  l.db = take(tiles(d.rows, 64) * l.piece * 4);
+  // dx's sums live through all pieces, dW's through one.
+  l.sum = take(l.x_summed ? (int64_t)l.x.parts * d.rows * d.dim * 4 : 0);
+  l.wsum = take(l.w.parts > 1 ? (int64_t)l.w.parts * l.piece * d.dim * 4 : 0);
   return l;
 }
-int64_t forward_bytes(const elasto_linear_ce_t& d) {
-  return up(tiles(d.classes) * d.rows * 8, 256) + up(d.rows * 4, 256);
+Way forward_way(const elasto_linear_ce_t& d) {
+  return way_of(d.rows, d.classes, d.dim, d.dtype == ELASTO_BF16 ? 2 : 4, false);
 }
+int64_t forward_bytes(const elasto_linear_ce_t& d) {
+  return up(tiles(d.classes, forward_way(d).side) * d.rows * 8, 256) + up(d.rows * 4, 256);
+}
+
+struct Args {
+  elasto_linear_ce_t d;
+  Matrix x, w;
+  int es = 0;
+};
 
 bool check_desc(const elasto_linear_ce_t* d) {
   if (!d) return fail(ELASTO_ERR_INVALID_ARG, "linear_ce: NULL description"), false;
@@ -433,7 +554,7 @@ bool check_desc(const elasto_linear_ce_t* d) {
       d->dim > kMaxDim || d->dim % n)
     return fail(ELASTO_ERR_INVALID_ARG, "linear_ce: bad rows or classes, or dim %d is not a multiple of %d", d->dim, n),
            false;
-  const int64_t tr = tiles(d->rows), tc = tiles(d->classes), td = tiles(d->dim);
+  const int64_t tr = tiles(d->rows, 128), tc = tiles(d->classes, 128), td = tiles(d->dim, 128);
   if (tr * tc >= kMaxTiles || tr * td >= kMaxTiles || tc * td >= kMaxTiles)
     return fail(ELASTO_ERR_INVALID_ARG, "linear_ce: too many tiles for a launch"), false;
   return true;
@@ -480,22 +601,23 @@ CeP params(const Args& a) {
   p.weight = a.d.row_weight;
   p.classes = a.d.classes;
   p.label_classes = a.d.classes;
-  p.tiles_m = (int)tiles(a.d.rows);
-  p.tiles_n = (int)tiles(a.d.classes);
   p.group = 8;
   return p;
 }
 
 template <typename T>
-using Tile = Shape<T, 128, 128, 2, 2>;
-
-template <typename T>
 hipError_t forward(const Args& a, float* loss, float* lse, char* ws, hipStream_t s) {
-  typedef Tile<T> S;
   CeP p = params(a);
+  const Way way = forward_way(a.d);
+  const int64_t n = tiles(a.d.classes, way.side);
   p.part = reinterpret_cast<float2*>(ws);
-  p.picked = reinterpret_cast<float*>(ws + up(tiles(a.d.classes) * a.d.rows * 8, 256));
-  hipLaunchKernelGGL((ce_forward_kernel<S>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(S::kThreads), 0, s, p);
+  p.picked = reinterpret_cast<float*>(ws + up(n * a.d.rows * 8, 256));
+  with_shape<T>(way.kind, [&](auto shape) {
+    typedef decltype(shape) S;
+    p.tiles_m = (int)tiles(p.rows, S::BM);
+    p.tiles_n = (int)tiles(p.classes, S::BN);
+    hipLaunchKernelGGL((ce_forward_kernel<S>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(S::kThreads), 0, s, p);
+  });
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const JoinP j = {p.part, p.picked, a.d.row_weight, a.d.labels, loss, lse, a.d.rows, p.tiles_n, a.d.classes};
@@ -515,9 +637,31 @@ struct Grads {
 
 unsigned blocks(int64_t n) { return (unsigned)std::min<int64_t>((n + 255) / 256, 1 << 16); }
 
+// q.out = q.scale q.a q.b^T, in `parts` parts of K where sums are given.
+template <typename T, bool TA, bool LIVE>
+hipError_t product(ProductP q, Kind kind, int parts, hipStream_t s) {
+  q.group = 8;
+  q.split = parts;
+  // Parts of whole steps; those behind a short last piece's end have none.
+  q.chunk = up((q.K + parts - 1) / parts, 128 / (int)sizeof(T));
+  with_shape<T>(kind, [&](auto shape) {
+    typedef decltype(shape) S;
+    q.tiles_m = (int)tiles(q.M, S::BM);
+    q.tiles_n = (int)tiles(q.N, S::BN);
+    hipLaunchKernelGGL((ce_product_kernel<S, TA, LIVE>), dim3((unsigned)(q.tiles_m * q.tiles_n * parts)),
+                       dim3(S::kThreads), 0, s, q);
+  });
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t sum_parts(const ProductP& q, int parts, hipStream_t s) {
+  hipLaunchKernelGGL((ce_sum_kernel<T>), dim3(blocks(q.M * q.N / 4)), dim3(256), 0, s, q.sum, parts, q.M, q.N,
+                     q.scale, q.out, q.ldo);
+  return hipGetLastError();
+}
+
 template <typename T>
 hipError_t backward(const Args& a, const Grads& g, char* ws, hipStream_t s) {
-  typedef Tile<T> S;
   const elasto_linear_ce_t& d = a.d;
   const int es = a.es;
   if (d.rows == 0) {
@@ -529,75 +673,63 @@ hipError_t backward(const Args& a, const Grads& g, char* ws, hipStream_t s) {
   }
   const BackLayout l = backward_layout(d);
   uint32_t* live = reinterpret_cast<uint32_t*>(ws + l.live);
-  hipLaunchKernelGGL(ce_live_kernel, dim3(blocks(d.rows)), dim3(256), 0, s, d.row_weight, d.labels, d.rows, d.classes,
-                     live);
+  hipLaunchKernelGGL(ce_live_kernel, dim3((unsigned)((d.rows + 255) / 256)), dim3(256), 0, s, d.row_weight, d.labels,
+                     d.rows, d.classes, live);
   hipError_t e = hipGetLastError();
+  ProductP x = {};
+  x.scale = g.scale;
+  x.M = d.rows;
+  x.N = d.dim;
+  x.out = g.dx;
+  x.ldo = g.lddx * es;
+  x.ld_sum = d.dim;
+  if (l.x_summed) x.sum = reinterpret_cast<float*>(ws + l.sum);
   for (int64_t c0 = 0; c0 < d.classes && e == hipSuccess; c0 += l.piece) {
     const int64_t n = std::min<int64_t>(l.piece, d.classes - c0);
     CeP p = params(a);
     p.c0 = c0;
     p.classes = n;
-    p.tiles_n = (int)tiles(n);
     p.lse = g.lse;
-    const int64_t ld = (int64_t)p.tiles_n * kTile;  // of dz: whole tiles
-    p.dz = Matrix{ws + l.dz, ld * es};
+    p.dz = Matrix{ws + l.dz, l.piece * es};
+    p.ld_db = l.piece;
     p.db_part = g.db ? reinterpret_cast<float*>(ws + l.db) : nullptr;
-    hipLaunchKernelGGL((ce_dz_kernel<S>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(S::kThreads), 0, s, p);
+    with_shape<T>(way_of(d.rows, n, d.dim, es, false).kind, [&](auto shape) {
+      typedef decltype(shape) S;
+      p.tiles_m = (int)tiles(p.rows, S::BM);
+      p.tiles_n = (int)tiles(n, S::BN);
+      hipLaunchKernelGGL((ce_dz_kernel<S>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(S::kThreads), 0, s, p);
+    });
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (g.db) {
-      hipLaunchKernelGGL(ce_db_kernel, dim3(blocks(n)), dim3(256), 0, s, p.db_part, p.tiles_m, ld, n, g.scale,
+      hipLaunchKernelGGL(ce_db_kernel, dim3(blocks(n)), dim3(256), 0, s, p.db_part, p.tiles_m, l.piece, n, g.scale,
                          g.db + c0);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    ProductP q = {};
-    q.scale = g.scale;
-    q.group = 8;
-    q.tiles_n = (int)tiles(d.dim);
-    q.N = d.dim;
     if (g.dx) {
-      q.a = p.dz;
-      q.b = Matrix{a.w.p + c0 * a.w.ld, a.w.ld};
-      q.M = d.rows;
-      q.K = n;
-      q.tiles_m = p.tiles_m;
-      q.out = g.dx;
-      q.ldo = g.lddx * es;
-      if (l.summed) {
-        q.sum = reinterpret_cast<float*>(ws + l.sum);
-        q.ld_sum = d.dim;
-        q.add = c0 > 0;
-      }
-      // Parts of whole steps; those behind a short last piece's end have no steps.
-      q.split = l.parts;
-      q.chunk = up((n + l.parts - 1) / l.parts, Step<T>::K);
-      hipLaunchKernelGGL((ce_product_kernel<S, false, false>), dim3((unsigned)(q.tiles_m * q.tiles_n * q.split)),
-                         dim3(S::kThreads), 0, s, q);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
+      x.a = p.dz;
+      x.b = Matrix{a.w.p + c0 * a.w.ld, a.w.ld};
+      x.K = n;
+      x.add = c0 > 0;
+      if ((e = product<T, false, false>(x, l.x.kind, l.x.parts, s)) != hipSuccess) return e;
     }
     if (g.dw) {
+      ProductP q = {};
+      q.scale = g.scale;
       q.a = p.dz;
       q.b = a.x;
       q.M = n;
+      q.N = d.dim;
       q.K = d.rows;
-      q.tiles_m = p.tiles_n;
       q.out = g.dw + c0 * g.lddw * es;
       q.ldo = g.lddw * es;
-      q.sum = nullptr;
-      q.add = false;
-      q.split = 1;
-      q.chunk = up(d.rows, Step<T>::K);
+      q.ld_sum = d.dim;
+      if (l.w.parts > 1) q.sum = reinterpret_cast<float*>(ws + l.wsum);
       q.live = live;
-      hipLaunchKernelGGL((ce_product_kernel<S, true, true>), dim3((unsigned)(q.tiles_m * q.tiles_n)),
-                         dim3(S::kThreads), 0, s, q);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
+      if ((e = product<T, true, true>(q, l.w.kind, l.w.parts, s)) != hipSuccess) return e;
+      if (l.w.parts > 1 && (e = sum_parts<T>(q, l.w.parts, s)) != hipSuccess) return e;
     }
   }
-  if (g.dx && l.summed) {
-    hipLaunchKernelGGL((ce_sum_kernel<T>), dim3(blocks(d.rows * (int64_t)d.dim / 4)), dim3(256), 0, s,
-                       reinterpret_cast<const float*>(ws + l.sum), l.parts, d.rows, d.dim, g.scale, g.dx,
-                       g.lddx * es);
-    e = hipGetLastError();
-  }
+  if (e == hipSuccess && g.dx && l.x_summed) e = sum_parts<T>(x, l.x.parts, s);
   return e;
 }
 

@@ -2,9 +2,9 @@
 // workgroup's BM x BN tile, with either operand lying straight (rows of K
 // contiguous values) or turned (K rows of contiguous columns), in bf16 or fp32.
 //
-// A step is 128 bytes of K of a straight operand (64 bf16, 32 fp32 values), 64 or
-// 32 rows of a turned one.  Tiles go to LDS by direct 16-byte loads, two stages.
-//  * Straight: 128-byte LDS rows, 16-byte chunk c of row r at c ^ ((r ^ r>>3) & 7).
+// A step is KB = 128 or 64 bytes of K of a straight operand, and as many rows of a turned one as
+// that holds values.  Tiles go to LDS by direct 16-byte loads, in two to four stages.
+//  * Straight: LDS rows of KB bytes, 16-byte chunk c of row r at c ^ (r>>1 & 7) (64: c ^ (r>>2 & 3)).
 //    bf16: a lane's chunk is its operand.  fp32: four values of K a lane and read,
 //    each the operand of one 32x32x2 product (which two values of K meet in a
 //    product is free as long as both operands agree).
@@ -19,6 +19,8 @@
 // What lies outside an operand gets an offset past every buffer and arrives as zeros.
 #pragma once
 
+#include <type_traits>
+
 #include "common.h"
 #include "lds_load.h"
 
@@ -30,22 +32,18 @@ struct Matrix {
   int64_t ld = 0;  // bytes between its rows
 };
 
-template <typename T>
-struct Step {
-  static constexpr int K = 128 / (int)sizeof(T);  // values of K
-};
-
 // TURNED: whether K is the operand's row.  B: the tile's size along the other axis.
-template <typename T, bool TURNED, int B, int THREADS>
+template <typename T, bool TURNED, int B, int THREADS, int KB>
 struct Operand {
-  static constexpr int kBytes = B * 128;
-  static constexpr int kRow = TURNED ? B * (int)sizeof(T) : 128;  // bytes of an LDS row
+  static constexpr int kBytes = B * KB, kK = KB / (int)sizeof(T), kQuarters = KB / 32;
+  static constexpr int kRow = TURNED ? B * (int)sizeof(T) : KB;  // bytes of an LDS row
   static constexpr int kChunks = kRow / 16;
+  static constexpr int kReads = !TURNED ? 1 : sizeof(T) == 2 ? 2 : 4;  // LDS reads of a quarter
   static constexpr int kLoads = kBytes / (16 * THREADS);
   static_assert(kBytes % (16 * THREADS) == 0, "whole loads");
 
   static __device__ __forceinline__ int swizzle(int r) {
-    if constexpr (!TURNED) return (r ^ (r >> 3)) & 7;
+    if constexpr (!TURNED) return KB == 128 ? (r >> 1) & 7 : (r >> 2) & 3;
     if constexpr (sizeof(T) == 4) return ((r >> 2) & 1) * 8;
     if constexpr (B == 64) return ((r >> 1) & 1) * 4;
     return (r & 3) * 4;
@@ -69,58 +67,74 @@ struct Operand {
   // The loads of a step that starts at `from`, of which k values of K are there.  live:
   // one bit for each of the step's K rows (turned operands).
   template <bool LIVE>
-  __device__ __forceinline__ void issue(char* stage, const char* from, int k, const uint32_t* live,
-                                        int tid) const {
+  __device__ __forceinline__ void issue(char* stage, const char* from, int k, uint64_t live, int tid) const {
     const __amdgpu_buffer_rsrc_t src =
         __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(from), (short)0, 0x7fffffff, kRsrcWord3);
-    uint32_t bits[2] = {~0u, ~0u};
-    if constexpr (LIVE) {
-      bits[0] = live[0];
-      if constexpr (Step<T>::K == 64) bits[1] = live[1];
-    }
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    auto load = [&](int i, uint32_t off) {
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void*)(stage + (i * THREADS + wave * 64) * 16), 16,
+                                               (int)off, 0, 0, 0);
+    };
+    if (k == kK && (!LIVE || live == ~0ull)) {  // a whole step
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int r = row(i, tid);
-      bool in = true;
-      if constexpr (TURNED)
-        in = r < k;
-      else
-        in = chunk(i, tid) * (16 / (int)sizeof(T)) < k;
-      if constexpr (LIVE) in = in && ((bits[r >> 5] >> (r & 31)) & 1);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(
-          src, (lds_void*)(stage + (i * THREADS + wave * 64) * 16), 16, (int)(in ? at[i] : kOutOfRange),
-          0, 0, 0);
+      for (int i = 0; i < kLoads; ++i) load(i, at[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int r = row(i, tid);
+        bool in = TURNED ? r < k : chunk(i, tid) * (16 / (int)sizeof(T)) < k;
+        if constexpr (LIVE) in = in && ((live >> r) & 1);
+        load(i, in ? at[i] : kOutOfRange);
+      }
     }
   }
 
-  // The values of quarter kk of a step in the 32 rows (columns) from `first` on.
-  static __device__ __forceinline__ u32x4 read(const char* stage, int first, int kk, int lane) {
-    const int lr = lane & 31, lg = lane >> 5;
-    if constexpr (!TURNED) {
-      const int r = first + lr;
-      return *reinterpret_cast<const u32x4*>(stage + r * 128 + (((2 * kk + lg) ^ swizzle(r)) << 4));
-    } else if constexpr (sizeof(T) == 2) {
-      typedef short i16x4 __attribute__((ext_vector_type(4)));
-      typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-      const int lq = lane & 15, g = lane >> 4;
-      const int r = kk * 16 + 8 * lg + (lq >> 2), c = first + 16 * (g & 1) + 4 * (lq & 3);
-      const char* p = stage + r * kRow + (((c >> 3) ^ swizzle(r)) << 4) + (c & 7) * 2;
-      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p));
-      const u32x2 hi =
-          __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 4 * kRow)));
-      return u32x4{lo[0], lo[1], hi[0], hi[1]};
-    } else {
-      u32x4 v;
-      const int c = first + lr;
+  // A lane's addresses in a stage, for a wave whose rows (columns) start at `first`, a multiple of 32:
+  // straight, one for each quarter, blocks 32 rows apart; turned, one for each block of 32 columns,
+  // quarters a fixed number of rows apart.
+  template <int BLOCKS>
+  struct Reader {
+    int at[TURNED ? BLOCKS : kQuarters];
+    __device__ __forceinline__ Reader(int first, int lane) {
+      const int lr = lane & 31, lg = lane >> 5;
+      if constexpr (!TURNED) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = 8 * kk + 4 * lg + e;
-        v[e] = *reinterpret_cast<const uint32_t*>(stage + r * kRow + (((c >> 2) ^ swizzle(r)) << 4) + (c & 3) * 4);
+        for (int kk = 0; kk < kQuarters; ++kk) at[kk] = (first + lr) * KB + (((2 * kk + lg) ^ swizzle(lr)) << 4);
+      } else {
+#pragma unroll
+        for (int i = 0; i < BLOCKS; ++i) {
+          if constexpr (sizeof(T) == 2) {
+            const int lq = lane & 15, g = lane >> 4;
+            const int r = 8 * lg + (lq >> 2), c = first + 32 * i + 16 * (g & 1) + 4 * (lq & 3);
+            at[i] = r * kRow + (((c >> 3) ^ swizzle(r)) << 4) + (c & 7) * 2;
+          } else {
+            const int r = 4 * lg, c = first + 32 * i + lr;
+            at[i] = r * kRow + (((c >> 2) ^ swizzle(r)) << 4) + (c & 3) * 4;
+          }
+        }
       }
-      return v;
     }
-  }
+    // The values of quarter kk of block i.
+    __device__ __forceinline__ u32x4 read(const char* stage, int i, int kk) const {
+      if constexpr (!TURNED) {
+        return *reinterpret_cast<const u32x4*>(stage + at[kk] + i * 32 * KB);
+      } else if constexpr (sizeof(T) == 2) {
+        typedef short i16x4 __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+        const char* p = stage + at[i] + kk * 16 * kRow;
+        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p));
+        const u32x2 hi =
+            __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 4 * kRow)));
+        return u32x4{lo[0], lo[1], hi[0], hi[1]};
+      } else {
+        u32x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          v[e] = *reinterpret_cast<const uint32_t*>(stage + at[i] + (8 * kk + e) * kRow);
+        return v;
+      }
+    }
+  };
 };
 
 // acc[i][j] += the product of A's 32-row block i and B's block j of this wave.
@@ -145,72 +159,147 @@ __device__ __forceinline__ void multiply(const u32x4 (&a)[TM], const u32x4 (&b)[
   }
 }
 
-template <typename T_, int BM_, int BN_, int WM_, int WN_>
+// GROUPS: workgroups that a CU holds by their registers and LDS.
+template <typename T_, int BM_, int BN_, int WM_, int WN_, int KB_, int STAGES_, int GROUPS_>
 struct Shape {
   typedef T_ T;
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_, KB = KB_;
+  static constexpr int kK = KB / (int)sizeof(T_);  // values of K of a step
   static constexpr int kThreads = 64 * WM * WN;
   static constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 32, TN = WTN / 32;
-  static constexpr int kStage = (BM + BN) * 128;
+  static constexpr int kStage = (BM + BN) * KB;
+  static constexpr int kGroups = GROUPS_, kWaves = kGroups * WM * WN / 4;  // kWaves: on a SIMD
+  static_assert(STAGES * kStage * kGroups <= 160 * 1024, "LDS of a CU");
 };
 
+// The operands' values of one quarter of a step.
+template <typename S>
+struct Quarter {
+  u32x4 a[S::TM], b[S::TN];
+};
+template <typename S, typename OA, typename OB>
+struct Readers {
+  typename OA::template Reader<S::TM> a;
+  typename OB::template Reader<S::TN> b;
+  __device__ __forceinline__ Readers(int wave, int lane)
+      : a(wave / S::WN * S::WTM, lane), b(wave % S::WN * S::WTN, lane) {}
+  __device__ __forceinline__ void read(Quarter<S>& q, const char* st, int kk) const {
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) q.a[i] = a.read(st, i, kk);
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) q.b[j] = b.read(st + OA::kBytes, j, kk);
+  }
+};
+
+template <int G, int NM, int NR>
+struct Interleave {
+  static __device__ __forceinline__ void go() {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    constexpr int n = NR * (G + 1) / NM - NR * G / NM;
+    if constexpr (n > 0) __builtin_amdgcn_sched_group_barrier(0x100, n, 0);
+    if constexpr (G + 1 < NM) Interleave<G + 1, NM, NR>::go();
+  }
+};
+
+// Where a step's operands lie, and how much of it there is.
+struct StepAt {
+  const char *a, *b;
+  int k;
+  uint64_t live;  // one bit for each of its rows of K
+};
 template <bool LIVE, typename OA, typename OB>
-__device__ __forceinline__ void issue_step(const OA& oa, const OB& ob, char* st, const char* pa, const char* pb,
-                                           int k, const uint32_t* bits, int tid) {
-  oa.template issue<false>(st, pa, k, nullptr, tid);
-  ob.template issue<LIVE>(st + OA::kBytes, pb, k, bits, tid);
+__device__ __forceinline__ void issue_step(const OA& oa, const OB& ob, char* st, const StepAt& at, int tid) {
+  oa.template issue<false>(st, at.a, at.k, ~0ull, tid);
+  ob.template issue<LIVE>(st + OA::kBytes, at.b, at.k, at.live, tid);
 }
 
-// One step: the next one's loads into `fill`, the products from `st`.
-template <typename S, bool LIVE, typename OA, typename OB>
-__device__ __forceinline__ void product_step(const OA& oa, const OB& ob, char* __restrict__ fill,
-                                             const char* __restrict__ st, bool more, const char* pa,
-                                             const char* pb, int k, const uint32_t* bits,
-                                             f32x16 (&acc)[S::TM][S::TN]) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave / S::WN, wn = wave % S::WN;
-  if (more) issue_step<LIVE>(oa, ob, fill, pa, pb, k, bits, tid);
+// One step: the loads of a later one into `fill`, the products from `st`.  Each quarter's operands
+// are read while the one before is multiplied; q[1] comes with the last quarter of the step before (not of
+// the first) and leaves with this one's.  `fill` and `st` are different stages: said so that the
+// compiler does not make the reads of one wait for the loads of the other.
+template <typename S, bool LIVE, bool FIRST, typename OA, typename OB>
+__device__ __forceinline__ void product_step(const OA& oa, const OB& ob, const Readers<S, OA, OB>& rd, char* __restrict__ fill,
+                                             const char* __restrict__ st, bool more, const StepAt& at,
+                                             Quarter<S> (&q)[2], f32x16 (&acc)[S::TM][S::TN]) {
+  typedef typename S::T T;
+  const int tid = threadIdx.x;
+  constexpr int NR = OA::kReads * S::TM + OB::kReads * S::TN, NM = (sizeof(T) == 2 ? 1 : 4) * S::TM * S::TN;
+  __builtin_amdgcn_sched_barrier(0);
+  rd.read(q[0], st, 0);
+  if constexpr (!FIRST) {
+    multiply<T>(q[1].a, q[1].b, acc);
+    Interleave<0, NM, NR>::go();
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  if (more) issue_step<LIVE>(oa, ob, fill, at, tid);
+  __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-  for (int kk = 0; kk < 4; ++kk) {
-    u32x4 a[S::TM], b[S::TN];
-#pragma unroll
-    for (int i = 0; i < S::TM; ++i) a[i] = OA::read(st, wm * S::WTM + 32 * i, kk, lane);
-#pragma unroll
-    for (int j = 0; j < S::TN; ++j) b[j] = OB::read(st + OA::kBytes, wn * S::WTN + 32 * j, kk, lane);
-    multiply<typename S::T>(a, b, acc);
+  for (int kk = 1; kk < OA::kQuarters; ++kk) {
+    rd.read(q[kk & 1], st, kk);
+    multiply<T>(q[~kk & 1].a, q[~kk & 1].b, acc);
+    Interleave<0, NM, NR>::go();
+    __builtin_amdgcn_sched_barrier(0);
   }
 }
 
 // The sums of K values [k0, k1) (k0 a whole step) of the tile at (m0, n0), into acc, which
 // holds what they start from.  M, N: the operands' sizes.  LIVE: bits of K's rows, of which
-// the others are not read in B (in A they hold zeros).
+// the others are not read in B (in A they hold zeros).  Ends with all loads and reads done in this wave;
+// others may still read their last quarter.
 template <typename S, bool TA, bool TB, bool LIVE>
 __device__ __forceinline__ void tile_product(char* smem, const Matrix& A, const Matrix& B, int64_t M, int64_t N,
                                              int64_t m0, int64_t n0, int64_t k0, int64_t k1, const uint32_t* live,
                                              f32x16 (&acc)[S::TM][S::TN]) {
   typedef typename S::T T;
-  constexpr int K = Step<T>::K, ES = (int)sizeof(T);
-  typedef Operand<T, TA, S::BM, S::kThreads> OA;
-  typedef Operand<T, TB, S::BN, S::kThreads> OB;
+  constexpr int K = S::kK, ES = (int)sizeof(T);
+  typedef Operand<T, TA, S::BM, S::kThreads, S::KB> OA;
+  typedef Operand<T, TB, S::BN, S::kThreads, S::KB> OB;
+  constexpr int kLoads = OA::kLoads + OB::kLoads, kAhead = S::STAGES - 1;
   const int tid = threadIdx.x;
   const OA oa(A.ld, M - m0, tid);
   const OB ob(B.ld, N - n0, tid);
+  const Readers<S, OA, OB> rd(__builtin_amdgcn_readfirstlane(tid >> 6), tid & 63);
   const char* pa = A.p + (TA ? k0 * A.ld + m0 * ES : m0 * A.ld + k0 * ES);
   const char* pb = B.p + (TB ? k0 * B.ld + n0 * ES : n0 * B.ld + k0 * ES);
-  const int64_t sa = TA ? A.ld * K : 128, sb = TB ? B.ld * K : 128;
+  const int64_t sa = TA ? A.ld * K : S::KB, sb = TB ? B.ld * K : S::KB;
   const int nk = (int)((k1 - k0 + K - 1) / K);
-  const uint32_t* bits = LIVE ? live + k0 / 32 : nullptr;
-  auto left = [&](int kt) { return (int)min((int64_t)K, k1 - k0 - (int64_t)kt * K); };
-  auto stage = [&](int kt) { return smem + (kt & 1) * S::kStage; };
-  auto bits_of = [&](int kt) { return LIVE ? bits + kt * (K / 32) : nullptr; };
-  if (nk > 0) issue_step<LIVE>(oa, ob, stage(0), pa, pb, left(0), bits_of(0), tid);
-  for (int kt = 0; kt < nk; ++kt) {
-    wait_vm_lds<0>();
-    __syncthreads();
-    const bool more = kt + 1 < nk;
-    product_step<S, LIVE>(oa, ob, stage(kt + 1), stage(kt), more, pa + (kt + 1) * sa, pb + (kt + 1) * sb,
-                          more ? left(kt + 1) : 0, more ? bits_of(kt + 1) : nullptr, acc);
-  }
+  if (nk <= 0) return;
+  const uint32_t* words = live + k0 / 32;
+  auto bits_of = [&](int kt) -> uint64_t {
+    if constexpr (!LIVE) return ~0ull;
+    if constexpr (K == 64) return (uint64_t)words[2 * kt] | (uint64_t)words[2 * kt + 1] << 32;
+    return (uint64_t)words[kt] | ~0ull << 32;
+  };
+  // Read a step ahead of their use, so that nothing waits for them.
+  uint64_t bits = bits_of(0);
+  auto step = [&](int kt) {
+    const StepAt at = {pa + kt * sa, pb + kt * sb, (int)min((int64_t)K, k1 - k0 - (int64_t)kt * K), bits};
+    bits = bits_of(min(kt + 1, nk - 1));
+    return at;
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i)
+    if (i < nk) issue_step<LIVE>(oa, ob, smem + i * S::kStage, step(i), tid);
+  Quarter<S> q[2];
+  int use = 0, fill = kAhead;  // stages
+  auto one = [&](int kt, auto first) {
+    // This step's loads are back: all but those of the steps behind it.
+    if (kAhead > 1 && kt + kAhead <= nk)
+      wait_vm_lds<(kAhead - 1) * kLoads>();
+    else
+      wait_vm_lds<0>();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const bool more = kt + kAhead < nk;
+    product_step<S, LIVE, decltype(first)::value>(oa, ob, rd, smem + fill * S::kStage, smem + use * S::kStage, more,
+                                                  step(more ? kt + kAhead : nk - 1), q, acc);
+    use = use + 1 == S::STAGES ? 0 : use + 1;
+    fill = fill + 1 == S::STAGES ? 0 : fill + 1;
+  };
+  one(0, std::true_type());
+  for (int kt = 1; kt < nk; ++kt) one(kt, std::false_type());
+  multiply<T>(q[1].a, q[1].b, acc);
 }
 
 }  // namespace elasto
