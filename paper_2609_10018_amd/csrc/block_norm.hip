@@ -18,6 +18,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "heads.h"
@@ -60,14 +61,6 @@ struct Place {
   }
 };
 
-__device__ __forceinline__ void load_run(const uint16_t* p, float* v) {
-  const u32x4 w = *reinterpret_cast<const u32x4*>(p);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
 __device__ __forceinline__ void load_run(const float* p, float* v) {
   const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
 #pragma unroll
@@ -117,50 +110,87 @@ __device__ __forceinline__ void store_row(T* p, int dim, int t, const float (&v)
   }
 }
 
-// Sums over a row's W waves: each wave's value by lane exchanges, the waves' through LDS.
-template <int W, int N>
-__device__ __forceinline__ void row_sums(float (&v)[N], float* red, int t) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = wave_sum(v[i]);
-  if constexpr (W > 1) {
-    __syncthreads();  // the last sums have been read
-    if ((t & 63) == 0)
-#pragma unroll
-      for (int i = 0; i < N; ++i) red[(t >> 6) * N + i] = v[i];
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      v[i] = red[i];
-      for (int k = 1; k < W; ++k) v[i] += red[k * N + i];
-    }
-  }
+// The sum over a wave, in all lanes: in rows of 16 by lane moves of the adder itself, then the four
+// rows' sums in their order.
+template <int CTRL>
+__device__ __forceinline__ float add_moved(float v) {
+  return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(
+                 0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float sum_of_wave(float v) {
+  v = add_moved<0xB1>(v);   // lane ^ 1
+  v = add_moved<0x4E>(v);   // lane ^ 2
+  v = add_moved<0x141>(v);  // the other quad of eight
+  v = add_moved<0x140>(v);  // the other eight of a row
+  auto row = [&](int r) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 16 * r)); };
+  return (row(0) + row(1)) + (row(2) + row(3));
 }
 
-// Mean (RMS: 0) and factor r of a row.
-template <typename L, int W>
-__device__ __forceinline__ float2 statistics(const float (&v)[L::E], const BlockP& p, float* red, int t) {
-  float mean = 0.0f;
-  if (p.layer) {
-    float s[1] = {0.0f};
+// Sums over a row's W waves, the waves' through LDS: two buffers in turn, so that one barrier does for
+// each exchange (who writes a buffer again has passed the barrier behind which all have read it).
+constexpr int kMost = 3;  // sums of an exchange
+template <int W>
+struct Exchange {
+  float* buf;  // [2][W][kMost]
+  int turn = 0;
+  template <int N>
+  __device__ __forceinline__ void operator()(float (&v)[N], int t) {
+    static_assert(N <= kMost, "room");
 #pragma unroll
-    for (int e = 0; e < L::E; ++e) s[0] += v[e];  // columns that are not there hold zeros
-    row_sums<W>(s, red, t);
-    mean = s[0] * p.inv_dim;
-  }
-  float q[1] = {0.0f};
+    for (int i = 0; i < N; ++i) v[i] = sum_of_wave(v[i]);
+    if constexpr (W > 1) {
+      float* b = buf + turn * W * kMost;
+      turn ^= 1;
+      if ((t & 63) == 0)
 #pragma unroll
-  for (int e = 0; e < L::E; ++e) {
-    const float d = v[e] - mean;
-    q[0] += L::column(e, t) < p.dim ? d * d : 0.0f;
+        for (int i = 0; i < N; ++i) b[(t >> 6) * kMost + i] = v[i];
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        v[i] = b[i];
+#pragma unroll
+        for (int k = 1; k < W; ++k) v[i] += b[k * kMost + i];
+      }
+    }
   }
-  row_sums<W>(q, red, t);
-  return make_float2(mean, 1.0f / sqrtf(q[0] * p.inv_dim + p.eps));
-}
+};
 
 template <typename T>
 __device__ __forceinline__ T* at(const Rows& r, int b, int t) {
   return reinterpret_cast<T*>(r.p + b * r.sb + t * r.st);
 }
+
+// A row as it was loaded.
+template <typename L, bool WIDE, typename T>
+struct Raw {
+  static constexpr bool kPacked = WIDE && sizeof(T) == 2;
+  u32x4 w[kPacked ? L::E / 8 : 1];
+  float f[kPacked ? 1 : L::E];
+  __device__ __forceinline__ void load(const T* p, bool there, int dim, int t) {
+    if constexpr (kPacked) {
+#pragma unroll
+      for (int i = 0; i < L::E / 8; ++i) {
+        const int c = L::column(8 * i, t);
+        w[i] = u32x4{0, 0, 0, 0};
+        if (there && c < dim) w[i] = *reinterpret_cast<const u32x4*>(p + c);
+      }
+    } else if (there) {
+      load_row<L, WIDE>(p, dim, t, f);
+    } else {
+#pragma unroll
+      for (int e = 0; e < L::E; ++e) f[e] = 0.0f;
+    }
+  }
+  __device__ __forceinline__ void get(float (&v)[L::E]) const {
+#pragma unroll
+    for (int e = 0; e < L::E; ++e) {
+      if constexpr (kPacked)
+        v[e] = __uint_as_float((e & 1) ? (w[e >> 3][(e & 7) >> 1] & 0xffff0000u) : (w[e >> 3][(e & 7) >> 1] << 16));
+      else
+        v[e] = f[e];
+    }
+  }
+};
 
 template <typename L, bool WIDE>
 __device__ __forceinline__ void load_weight(const float* w, float none, int dim, int t, float (&v)[L::E]) {
@@ -171,88 +201,128 @@ __device__ __forceinline__ void load_weight(const float* w, float none, int dim,
     for (int e = 0; e < L::E; ++e) v[e] = none;
 }
 
-// T: of y and u.  S: of the stream.  W waves a row; a workgroup of 256 threads holds 4 / W rows.
-template <typename T, typename S, int W, int CH, bool WIDE>
+// v less its mean, 0 in columns that are not there.
+template <typename L>
+__device__ __forceinline__ void centre(float (&v)[L::E], float mean, int dim, int t) {
+#pragma unroll
+  for (int e = 0; e < L::E; ++e) v[e] = L::column(e, t) < dim ? v[e] - mean : 0.0f;
+}
+
+// Whether the weights and the next row's loads stay in registers: not for rows of 16 waves with sixteen
+// values a thread, which have 128 registers.
+template <int W, int CH>
+constexpr bool kKeep = W * CH < 32;
+
+// T: of y and u.  S: of the stream.  W waves a row; a workgroup of 256 threads holds 4 / W rows.  A group of
+// W waves takes rows in strides of the grid's, the next one's loads in flight, the weights in registers.
+template <typename T, typename S, bool LAYER, int W, int CH, bool WIDE>
 __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_kernel(BlockP p) {
   typedef Place<W, CH, WIDE> L;
   constexpr int E = L::E, R = W > 4 ? 1 : 4 / W;
-  __shared__ float red[W > 4 ? W : 4];
-  const int t = threadIdx.x % L::T;
-  float* mine = red + threadIdx.x / L::T * W;
-  const int64_t row = (int64_t)blockIdx.x * R + threadIdx.x / L::T;
-  const int64_t rows = (int64_t)p.batch * p.tokens;
-  const int b = (int)(min(row, rows - 1) / p.tokens), tok = (int)(min(row, rows - 1) - (int64_t)b * p.tokens);
-  bool live = row < rows;
-  if (live && p.lens) live = tok < p.lens[b];
-  // Waves that share a row go on or leave together; with W > 1 all rows of a workgroup meet at its
-  // barriers.
-  if (W == 1 && !live) return;
-  float v[E];
+  constexpr bool KEEP = kKeep<W, CH>;
+  __shared__ float red[R][2 * W * kMost];
+  const int t = threadIdx.x % L::T, mine = threadIdx.x / L::T;
+  Exchange<W> exchange = {red[mine]};
+  const int rows = p.batch * p.tokens, stride = gridDim.x * R;
+  float pg[E], pb[E], qg[E], qb[E], g[E];
+  auto pre = [&] {
+    load_weight<L, WIDE>(p.pre_gamma, 1.0f, p.dim, t, pg);
+    if constexpr (LAYER) load_weight<L, WIDE>(p.pre_beta, 0.0f, p.dim, t, pb);
+  };
+  auto post = [&] {
+    load_weight<L, WIDE>(p.post_gamma, 1.0f, p.dim, t, qg);
+    if constexpr (LAYER) load_weight<L, WIDE>(p.post_beta, 0.0f, p.dim, t, qb);
+  };
+  if (KEEP && p.u.p) pre();
+  if (KEEP && p.post) post();
+  if (KEEP) load_weight<L, WIDE>(p.gate, 1.0f, p.dim, t, g);  // of the first sequence, or of all
+  int gate_of = 0;
+  Raw<L, WIDE, S> rx;
+  Raw<L, WIDE, T> ry;
+  int b = 0, tok = 0;
+  bool live = false;
+  auto fetch = [&](int row) {
+    live = row < rows;
+    const int r = live ? row : 0;
+    b = (int)((unsigned)r / (unsigned)p.tokens);
+    tok = r - b * p.tokens;
+    if (live && p.lens) live = tok < p.lens[b];
+    rx.load(at<const S>(p.x, b, tok), live, p.dim, t);
+    if (p.has_y) ry.load(at<const T>(p.y, b, tok), live, p.dim, t);
+  };
+  // All rows of a workgroup take as many rounds: with W > 1 they meet at its barriers.
+  int row = blockIdx.x * R;
+  if (KEEP) fetch(row + mine);
+  for (; row < rows; row += stride) {
+    if (!KEEP) fetch(row + mine);
+    float x[E], v[E];
+    rx.get(x);
+    const bool now = live;
+    const int nb = b, nt = tok;
+    if (p.has_y) {
+      ry.get(v);
+      if (KEEP && row + stride < rows) fetch(row + stride + mine);
+      if (p.post) {
+        if constexpr (LAYER) {
+          float s[1] = {0.0f};
 #pragma unroll
-  for (int e = 0; e < E; ++e) v[e] = 0.0f;
-  float x[E], g[E];
+          for (int e = 0; e < E; ++e) s[0] += v[e];
+          exchange(s, t);
+          centre<L>(v, s[0] * p.inv_dim, p.dim, t);
+        }
+        float q[1] = {0.0f};
 #pragma unroll
-  for (int e = 0; e < E; ++e) x[e] = 0.0f;
-  if (live) {
-    load_row<L, WIDE>(at<const S>(p.x, b, tok), p.dim, t, x);
-    if (p.has_y) load_row<L, WIDE>(at<const T>(p.y, b, tok), p.dim, t, v);
-  }
-  if (p.has_y) {
-    if (p.post) {
-      const float2 st = statistics<L, W>(v, p, mine, t);
-      float w[E], c[E];
-      load_weight<L, WIDE>(p.post_gamma, 1.0f, p.dim, t, w);
-      load_weight<L, WIDE>(p.post_beta, 0.0f, p.dim, t, c);
+        for (int e = 0; e < E; ++e) q[0] = fmaf(v[e], v[e], q[0]);
+        exchange(q, t);
+        const float r = 1.0f / sqrtf(fmaf(q[0], p.inv_dim, p.eps));
+        if (!KEEP) post();
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = fmaf((v[e] - st.x) * st.y, w[e], c[e]);
+        for (int e = 0; e < E; ++e) v[e] = LAYER ? fmaf(v[e] * r, qg[e], qb[e]) : v[e] * r * qg[e];
+      }
+      if (!KEEP && !p.gate_ld) load_weight<L, WIDE>(p.gate, 1.0f, p.dim, t, g);
+      if (p.gate_ld && (!KEEP || nb != gate_of)) {
+        load_weight<L, WIDE>(p.gate + nb * p.gate_ld, 1.0f, p.dim, t, g);
+        gate_of = nb;
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = fmaf(p.a, x[e], L::column(e, t) < p.dim ? g[e] * v[e] : 0.0f);
+    } else {
+      if (KEEP && row + stride < rows) fetch(row + stride + mine);
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] *= p.a;
     }
-    load_weight<L, WIDE>(p.gate ? p.gate + b * p.gate_ld : nullptr, 1.0f, p.dim, t, g);
+    if (now && p.x_out.p) store_row<L, WIDE>(at<S>(p.x_out, nb, nt), p.dim, t, x);
+    if (!p.u.p) continue;
+    if constexpr (LAYER) {
+      float s[1] = {0.0f};
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = fmaf(p.a, x[e], L::column(e, t) < p.dim ? g[e] * v[e] : 0.0f);
-  } else {
+      for (int e = 0; e < E; ++e) s[0] += x[e];
+      exchange(s, t);
+      centre<L>(x, s[0] * p.inv_dim, p.dim, t);
+    }
+    float q[1] = {0.0f};
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] *= p.a;
+    for (int e = 0; e < E; ++e) q[0] = fmaf(x[e], x[e], q[0]);
+    exchange(q, t);
+    const float r = 1.0f / sqrtf(fmaf(q[0], p.inv_dim, p.eps));
+    if (!KEEP) pre();
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = LAYER ? fmaf(x[e] * r, pg[e], pb[e]) : x[e] * r * pg[e];
+    if (now) store_row<L, WIDE>(at<T>(p.u, nb, nt), p.dim, t, x);
   }
-  if (live && p.x_out.p) store_row<L, WIDE>(at<S>(p.x_out, b, tok), p.dim, t, x);
-  if (!p.u.p) return;
-  const float2 st = statistics<L, W>(x, p, mine, t);
-  float w[E], c[E];
-  load_weight<L, WIDE>(p.pre_gamma, 1.0f, p.dim, t, w);
-  load_weight<L, WIDE>(p.pre_beta, 0.0f, p.dim, t, c);
-#pragma unroll
-  for (int e = 0; e < E; ++e) x[e] = fmaf((x[e] - st.x) * st.y, w[e], c[e]);
-  if (live) store_row<L, WIDE>(at<T>(p.u, b, tok), p.dim, t, x);
 }
 
-// The gradient through a norm: d, that of its result, becomes that of its input; xn the normed
-// values, r the factor; the weights' gradients are added to dg and db.
-template <typename L, bool WIDE, int W>
-__device__ __forceinline__ void norm_back(const BlockP& p, const float* gamma, float r, const float (&xn)[L::E],
-                                          float (&d)[L::E], float (&dg)[L::E], float (&db)[L::E], float* red, int t) {
-  float w[L::E], s[2] = {0.0f, 0.0f};
-  load_weight<L, WIDE>(gamma, 1.0f, p.dim, t, w);
-#pragma unroll
-  for (int e = 0; e < L::E; ++e) {
-    dg[e] = fmaf(d[e], xn[e], dg[e]);
-    db[e] += d[e];
-    d[e] *= L::column(e, t) < p.dim ? w[e] : 0.0f;
-    s[0] = fmaf(d[e], xn[e], s[0]);
-    s[1] += d[e];
-  }
-  row_sums<W>(s, red, t);
-  const float a = s[0] * p.inv_dim, c = p.layer ? s[1] * p.inv_dim : 0.0f;
-#pragma unroll
-  for (int e = 0; e < L::E; ++e) d[e] = r * (d[e] - fmaf(xn[e], a, c));
-}
-
-template <typename T, typename S, int W, int CH, bool WIDE>
+// Three exchanges a row (RMS: two): sums for the means; about them, with what both norms need that the
+// gradient of x' does not wait for; and the norm behind the block's.
+template <typename T, typename S, bool LAYER, int W, int CH, bool WIDE>
 __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_bwd_kernel(BlockP p) {
   typedef Place<W, CH, WIDE> L;
   constexpr int E = L::E, R = W > 4 ? 1 : 4 / W;
-  __shared__ float red[W > 4 ? 2 * W : 8];
+  constexpr bool KEEP = kKeep<W, CH>;
+  __shared__ float red[R][2 * W * kMost];
   __shared__ float sums[R > 1 ? (R - 1) * L::T : 1];
   const int t = threadIdx.x % L::T, mine = threadIdx.x / L::T;
-  float* rd = red + mine * 2 * W;
+  Exchange<W> exchange = {red[mine]};
   float pg[E], pb[E], qg[E], qb[E], gg[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) pg[e] = pb[e] = qg[e] = qb[e] = gg[e] = 0.0f;
@@ -273,68 +343,129 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_bwd_kernel(Bl
       if (mine == 0 && c < p.dim) out[c] = s;
     }
   };
+  float w_pre[E], w_post[E], b_post[E], w_gate[E];
+  auto post = [&] {
+    load_weight<L, WIDE>(p.post_gamma, 1.0f, p.dim, t, w_post);
+    if constexpr (LAYER) load_weight<L, WIDE>(p.post_beta, 0.0f, p.dim, t, b_post);
+  };
+  if (KEEP) {
+    load_weight<L, WIDE>(p.pre_gamma, 1.0f, p.dim, t, w_pre);
+    if (p.post) post();
+    load_weight<L, WIDE>(p.gate, 1.0f, p.dim, t, w_gate);
+  }
   const int units = p.batch * p.slices;
   for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
     const int b = unit / p.slices, slice = unit - b * p.slices;
     const int n = p.lens ? max(0, min(p.tokens, p.lens[b])) : p.tokens;
     const int share = (n + p.slices - 1) / p.slices, first = slice * share, last = min(n, first + share);
+    if (KEEP && p.gate_ld) load_weight<L, WIDE>(p.gate + b * p.gate_ld, 0.0f, p.dim, t, w_gate);
+    Raw<L, WIDE, S> rx, rd;
+    Raw<L, WIDE, T> ru, ry;
+    auto fetch = [&](int tok) {
+      const bool live = tok < last;
+      const int k = live ? tok : 0;
+      if (p.du.p) {
+        ru.load(at<const T>(p.du, b, k), live, p.dim, t);
+        rx.load(at<const S>(p.x_out, b, k), live, p.dim, t);
+      }
+      if (p.has_y) ry.load(at<const T>(p.y, b, k), live, p.dim, t);
+      if (p.dx_out.p) rd.load(at<const S>(p.dx_out, b, k), live, p.dim, t);
+    };
+    if (KEEP && first < last) fetch(first + mine);
     // Every row of a workgroup takes as many rounds: they meet at its barriers.
     for (int k = first; k < last; k += R) {
       const int tok = k + mine;
       const bool live = tok < last;
-      float d[E], xn[E], v[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) d[e] = xn[e] = v[e] = 0.0f;
-      if (live) {
-        if (p.du.p) load_row<L, WIDE>(at<const T>(p.du, b, tok), p.dim, t, d);
-        if (p.du.p) load_row<L, WIDE>(at<const S>(p.x_out, b, tok), p.dim, t, xn);
-        if (p.has_y) load_row<L, WIDE>(at<const T>(p.y, b, tok), p.dim, t, v);
+      if (!KEEP) {
+        fetch(tok);
+        load_weight<L, WIDE>(p.pre_gamma, 1.0f, p.dim, t, w_pre);
       }
+      float d[E], x[E], v[E], s[3] = {0.0f, 0.0f, 0.0f};
       if (p.du.p) {
-        const float2 st = statistics<L, W>(xn, p, rd, t);
+        ru.get(d);
+        rx.get(x);
 #pragma unroll
-        for (int e = 0; e < E; ++e) xn[e] = L::column(e, t) < p.dim ? (xn[e] - st.x) * st.y : 0.0f;
-        norm_back<L, WIDE, W>(p, p.pre_gamma, st.y, xn, d, pg, pb, rd, t);
-      }
-      if (p.dx_out.p && live) {
-        load_row<L, WIDE>(at<const S>(p.dx_out, b, tok), p.dim, t, xn);
+        for (int e = 0; e < E; ++e) pb[e] += d[e];
+      } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e) d[e] += xn[e];
+        for (int e = 0; e < E; ++e) d[e] = x[e] = 0.0f;
       }
+      if (p.has_y)
+        ry.get(v);
+      else
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = 0.0f;
+      float c = 0.0f;
+      if constexpr (LAYER) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          s[0] += x[e];
+          s[1] += v[e];
+          s[2] = fmaf(d[e], L::column(e, t) < p.dim ? w_pre[e] : 0.0f, s[2]);
+        }
+        exchange(s, t);
+        if (p.du.p) centre<L>(x, s[0] * p.inv_dim, p.dim, t);
+        if (p.post) centre<L>(v, s[1] * p.inv_dim, p.dim, t);
+        c = s[2] * p.inv_dim;
+        s[0] = s[1] = s[2] = 0.0f;
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        s[0] = fmaf(x[e], x[e], s[0]);
+        s[1] = fmaf(v[e], v[e], s[1]);
+        s[2] = fmaf(d[e] * (L::column(e, t) < p.dim ? w_pre[e] : 0.0f), x[e], s[2]);
+      }
+      exchange(s, t);
+      const float r = 1.0f / sqrtf(fmaf(s[0], p.inv_dim, p.eps));
+      const float ry1 = p.post ? 1.0f / sqrtf(fmaf(s[1], p.inv_dim, p.eps)) : 1.0f;
+      if (p.du.p) {
+        const float a = r * s[2] * p.inv_dim;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float xn = x[e] * r;
+          pg[e] = fmaf(d[e], xn, pg[e]);
+          d[e] = r * (fmaf(d[e], w_pre[e], -c) - xn * a);
+        }
+      }
+      if (p.dx_out.p) {
+        rd.get(x);
+#pragma unroll
+        for (int e = 0; e < E; ++e) d[e] += x[e];
+      }
+      if (KEEP && k + R < last) fetch(tok + R);
       if (p.dx.p && live) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) xn[e] = p.a * d[e];
-        store_row<L, WIDE>(at<S>(p.dx, b, tok), p.dim, t, xn);
+        for (int e = 0; e < E; ++e) x[e] = p.a * d[e];
+        store_row<L, WIDE>(at<S>(p.dx, b, tok), p.dim, t, x);
       }
       if (!p.has_y) continue;
-      float2 st = make_float2(0.0f, 1.0f);
-      if (p.post) st = statistics<L, W>(v, p, rd, t);
-      if (!live)
-#pragma unroll
-        for (int e = 0; e < E; ++e) d[e] = 0.0f;
-      float w[E];
-      if (p.post) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = L::column(e, t) < p.dim ? (v[e] - st.x) * st.y : 0.0f;
+      if (!KEEP) {
+        if (p.post) post();
+        load_weight<L, WIDE>(p.gate ? p.gate + b * p.gate_ld : nullptr, 1.0f, p.dim, t, w_gate);
       }
-      if (p.gate) {
-        if (p.wanted & 16) {
-          if (p.post) {
-            float c[E];
-            load_weight<L, WIDE>(p.post_gamma, 1.0f, p.dim, t, w);
-            load_weight<L, WIDE>(p.post_beta, 0.0f, p.dim, t, c);
+      float q[2] = {0.0f, 0.0f};
 #pragma unroll
-            for (int e = 0; e < E; ++e) gg[e] = fmaf(d[e], fmaf(v[e], w[e], c[e]), gg[e]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e) gg[e] = fmaf(d[e], v[e], gg[e]);
-          }
+      for (int e = 0; e < E; ++e) {
+        // What is not there stays out of the sums.
+        d[e] = live && L::column(e, t) < p.dim ? d[e] : 0.0f;
+        v[e] *= ry1;
+        const float n = p.post ? (LAYER ? fmaf(v[e], w_post[e], b_post[e]) : v[e] * w_post[e]) : v[e];
+        gg[e] = fmaf(d[e], n, gg[e]);
+        if (p.gate) d[e] *= w_gate[e];
+        if (p.post) {
+          qg[e] = fmaf(d[e], v[e], qg[e]);
+          if constexpr (LAYER) qb[e] += d[e];
+          d[e] *= w_post[e];
+          q[0] = fmaf(d[e], v[e], q[0]);
+          if constexpr (LAYER) q[1] += d[e];
         }
-        load_weight<L, WIDE>(p.gate + b * p.gate_ld, 0.0f, p.dim, t, w);
-#pragma unroll
-        for (int e = 0; e < E; ++e) d[e] *= w[e];
       }
-      if (p.post) norm_back<L, WIDE, W>(p, p.post_gamma, st.y, v, d, qg, qb, rd, t);
+      if (p.post) {
+        exchange(q, t);
+        const float a = q[0] * p.inv_dim, m = LAYER ? q[1] * p.inv_dim : 0.0f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) d[e] = ry1 * (d[e] - fmaf(v[e], a, m));
+      }
       if (p.dy.p && live) store_row<L, WIDE>(at<T>(p.dy, b, tok), p.dim, t, d);
     }
     if (p.dgate) {  // all rows of this gate are here
@@ -387,21 +518,12 @@ __global__ __launch_bounds__(256) void block_zero_kernel(float* out, int64_t n) 
 
 // ---------------------------------------------------------------- host
 
-template <typename T, typename S, int W, int CH, bool WIDE>
-void launch(const BlockP& p, bool back, unsigned grid, hipStream_t s) {
-  constexpr int N = W > 4 ? 64 * W : 256;
-  if (back)
-    hipLaunchKernelGGL((block_norm_bwd_kernel<T, S, W, CH, WIDE>), dim3(grid), dim3(N), 0, s, p);
-  else
-    hipLaunchKernelGGL((block_norm_kernel<T, S, W, CH, WIDE>), dim3(grid), dim3(N), 0, s, p);
-}
-
-// Waves of a row and runs of eight a thread, by the width: at most 16 values a thread, so that
-// backward the five sums stay in registers.
+// Waves of a row and runs of eight a thread.
 struct Width {
   int waves, runs;
 };
-Width width_of(int dim) {
+// Forward: rows of up to 1024 in one wave, which needs no barrier.
+Width forward_width(int dim) {
   if (dim <= 512) return {1, 1};
   if (dim <= 1024) return {1, 2};
   if (dim <= 2048) return {2, 2};
@@ -409,26 +531,62 @@ Width width_of(int dim) {
   if (dim <= 8192) return {8, 2};
   return {16, 2};
 }
-int rows_of(int dim) {
-  const int w = width_of(dim).waves;
-  return w > 4 ? 1 : 4 / w;
+// Backward: eight values a thread, so that the sums, the weights and the next row's loads stay in
+// registers.
+Width backward_width(int dim) {
+  if (dim <= 512) return {1, 1};
+  if (dim <= 1024) return {2, 1};
+  if (dim <= 2048) return {4, 1};
+  if (dim <= 4096) return {8, 1};
+  if (dim <= 8192) return {16, 1};
+  return {16, 2};
+}
+// Workgroups of a forward launch: what the GPU holds, several times over for rows of one wave.
+int forward_blocks(int dim) { return dim <= 4096 ? 256 * 8 : 256 * 4; }
+int rows_of(Width w) { return w.waves > 4 ? 1 : 4 / w.waves; }
+
+template <typename T, typename S, bool LAYER, bool WIDE>
+void launch_forward(const BlockP& p, unsigned grid, hipStream_t s) {
+  auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, s, p); };
+  const Width w = forward_width(p.dim);
+  switch (w.waves * 2 + w.runs) {
+    case 3: return go(block_norm_kernel<T, S, LAYER, 1, 1, WIDE>, 256);
+    case 4: return go(block_norm_kernel<T, S, LAYER, 1, 2, WIDE>, 256);
+    case 6: return go(block_norm_kernel<T, S, LAYER, 2, 2, WIDE>, 256);
+    case 10: return go(block_norm_kernel<T, S, LAYER, 4, 2, WIDE>, 256);
+    case 18: return go(block_norm_kernel<T, S, LAYER, 8, 2, WIDE>, 512);
+    default: return go(block_norm_kernel<T, S, LAYER, 16, 2, WIDE>, 1024);
+  }
+}
+template <typename T, typename S, bool LAYER, bool WIDE>
+void launch_backward(const BlockP& p, unsigned grid, hipStream_t s) {
+  auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, s, p); };
+  const Width w = backward_width(p.dim);
+  switch (w.waves * 2 + w.runs) {
+    case 3: return go(block_norm_bwd_kernel<T, S, LAYER, 1, 1, WIDE>, 256);
+    case 5: return go(block_norm_bwd_kernel<T, S, LAYER, 2, 1, WIDE>, 256);
+    case 9: return go(block_norm_bwd_kernel<T, S, LAYER, 4, 1, WIDE>, 256);
+    case 17: return go(block_norm_bwd_kernel<T, S, LAYER, 8, 1, WIDE>, 512);
+    case 33: return go(block_norm_bwd_kernel<T, S, LAYER, 16, 1, WIDE>, 1024);
+    default: return go(block_norm_bwd_kernel<T, S, LAYER, 16, 2, WIDE>, 1024);
+  }
 }
 
-template <typename T, typename S, bool WIDE>
-void launch_width(const BlockP& p, bool back, unsigned grid, hipStream_t s) {
-  const Width w = width_of(p.dim);
-  if (w.waves == 1) return w.runs == 1 ? launch<T, S, 1, 1, WIDE>(p, back, grid, s) : launch<T, S, 1, 2, WIDE>(p, back, grid, s);
-  if (w.waves == 2) return launch<T, S, 2, 2, WIDE>(p, back, grid, s);
-  if (w.waves == 4) return launch<T, S, 4, 2, WIDE>(p, back, grid, s);
-  if (w.waves == 8) return launch<T, S, 8, 2, WIDE>(p, back, grid, s);
-  launch<T, S, 16, 2, WIDE>(p, back, grid, s);
+template <typename T, typename S>
+void launch_kind(const BlockP& p, bool wide, bool back, unsigned grid, hipStream_t s) {
+  auto kind = [&](auto layer) {
+    constexpr bool LAYER = decltype(layer)::value;
+    if (back)
+      wide ? launch_backward<T, S, LAYER, true>(p, grid, s) : launch_backward<T, S, LAYER, false>(p, grid, s);
+    else
+      wide ? launch_forward<T, S, LAYER, true>(p, grid, s) : launch_forward<T, S, LAYER, false>(p, grid, s);
+  };
+  p.layer ? kind(std::true_type()) : kind(std::false_type());
 }
-
-template <bool WIDE>
-void launch_types(const BlockP& p, bool bf16, bool stream_bf16, bool back, unsigned grid, hipStream_t s) {
-  if (!bf16) return launch_width<float, float, WIDE>(p, back, grid, s);
-  if (stream_bf16) return launch_width<uint16_t, uint16_t, WIDE>(p, back, grid, s);
-  launch_width<uint16_t, float, WIDE>(p, back, grid, s);
+void launch_types(const BlockP& p, bool wide, bool bf16, bool stream_bf16, bool back, unsigned grid, hipStream_t s) {
+  if (!bf16) return launch_kind<float, float>(p, wide, back, grid, s);
+  if (stream_bf16) return launch_kind<uint16_t, uint16_t>(p, wide, back, grid, s);
+  launch_kind<uint16_t, float>(p, wide, back, grid, s);
 }
 
 bool check_sizes(const elasto_block_norm_t* d) {
@@ -446,7 +604,8 @@ struct Slices {
   int grid;
 };
 Slices slices_of(const elasto_block_norm_t& d) {
-  const int64_t rounds = (d.tokens + rows_of(d.dim) - 1) / std::max(1, rows_of(d.dim));
+  const int r = rows_of(backward_width(d.dim));
+  const int64_t rounds = (d.tokens + r - 1) / r;
   const int64_t per = std::max<int64_t>(1, std::min<int64_t>(rounds, kGradBlocks / std::max(1, d.batch)));
   return {(int)per, (int)std::min<int64_t>((int64_t)d.batch * per, kGradBlocks)};
 }
@@ -535,13 +694,10 @@ elasto_status_t elasto_op_block_norm(const elasto_block_norm_t* d, const elasto_
   p.has_y = p.y.p != nullptr;
   if (!p.x_out.p && !p.u.p) return fail(ELASTO_ERR_INVALID_ARG, "block_norm: neither x_out nor u is asked for");
   if (!p.has_y && (p.post || p.gate)) return fail(ELASTO_ERR_INVALID_ARG, "block_norm: a norm or gate of no y");
-  const int per = rows_of(d->dim);
-  const unsigned grid = (unsigned)((rows + per - 1) / per);
+  const int per = rows_of(forward_width(d->dim));
+  const unsigned grid = (unsigned)std::min<int64_t>((rows + per - 1) / per, forward_blocks(d->dim));
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  if (wide(p))
-    launch_types<true>(p, es == 2, ss == 2, false, grid, s);
-  else
-    launch_types<false>(p, es == 2, ss == 2, false, grid, s);
+  launch_types(p, wide(p), es == 2, ss == 2, false, grid, s);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(ELASTO_ERR_HIP, "block_norm: %s", hipGetErrorString(e));
   return ELASTO_OK;
@@ -604,10 +760,7 @@ elasto_status_t elasto_op_block_norm_bwd(const elasto_block_norm_t* d, const ela
                   (long long)(workspace ? workspace_bytes : 0), (long long)need);
     p.part = static_cast<float*>(workspace);
   }
-  if (wide(p))
-    launch_types<true>(p, es == 2, ss == 2, true, (unsigned)sl.grid, s);
-  else
-    launch_types<false>(p, es == 2, ss == 2, true, (unsigned)sl.grid, s);
+  launch_types(p, wide(p), es == 2, ss == 2, true, (unsigned)sl.grid, s);
   e = hipGetLastError();
   if (e == hipSuccess && sums) {
     SumP q = {};

@@ -64,7 +64,8 @@ __device__ __forceinline__ void logits(char* smem, const CeP& p, int64_t m0, int
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const int c = c0 + j * 32 + 8 * (e >> 2) + (e & 3);
-      const float b = c < p.classes ? (p.bias ? p.bias[p.c0 + c] : 0.0f) : -INFINITY;
+      float b = c < p.classes ? (p.bias ? p.bias[p.c0 + c] : 0.0f) : -INFINITY;
+      if (!leads<S>()) b = 0.0f;
 #pragma unroll
       for (int i = 0; i < S::TM; ++i) acc[i][j][e] = b;
     }
@@ -101,7 +102,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_forward_kernel(CeP 
   logits<S>(smem, p, m0, n0, acc);
   __syncthreads();
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave / S::WN, wn = wave % S::WN, lr = lane & 31, lg = lane >> 5;
+  const int wm = wave % S::kTeam / S::WN, wn = wave % S::WN, lr = lane & 31, lg = lane >> 5;
   float2* red = reinterpret_cast<float2*>(smem);  // [WN][BM]
 #pragma unroll
   for (int i = 0; i < S::TM; ++i) {
@@ -247,7 +248,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_dz_kernel(CeP p) {
   f32x16 acc[S::TM][S::TN];
   logits<S>(smem, p, m0, n0, acc);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wm = wave / S::WN, wn = wave % S::WN, lr = lane & 31, lg = lane >> 5;
+  const int wm = wave % S::kTeam / S::WN, wn = wave % S::WN, lr = lane & 31, lg = lane >> 5;
   const int first = (int)n0 + wn * S::WTN;  // of the wave's classes in the piece
   typedef RowsOut<S, T> Out;
   char* mine = smem + wave * Out::kWave;
@@ -279,7 +280,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_dz_kernel(CeP p) {
         for (int e = 0; e < 16; ++e)
           if (at == j * 32 + 8 * (e >> 2) + 4 * lg + (e & 3)) acc[i][j][e] -= w;
     Out::go(mine, acc[i], lane, [&](int r, int c, const u32x4& v) {
-      if (block + r < p.rows)
+      if (block + r < p.rows && leads<S>())
         *reinterpret_cast<u32x4*>(const_cast<char*>(p.dz.p) + (block + r) * p.dz.ld +
                                   (int64_t)(first + c) * (int)sizeof(T)) = v;
     });
@@ -350,7 +351,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_product_kernel(Prod
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
   tile_product<S, TA, true, LIVE>(smem, p.a, p.b, p.M, p.N, m0, n0, k0, k1, p.live, acc);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t r0 = m0 + wave / S::WN * S::WTM, c0 = n0 + wave % S::WN * S::WTN;
+  const int64_t r0 = m0 + wave % S::kTeam / S::WN * S::WTM, c0 = n0 + wave % S::WN * S::WTN;
   __syncthreads();  // the tiles have been read
 #pragma unroll
   for (int i = 0; i < S::TM; ++i) {
@@ -358,7 +359,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_product_kernel(Prod
     if (p.sum) {
       typedef RowsOut<S, float> Out;
       Out::go(smem + wave * Out::kWave, acc[i], lane, [&](int r, int c, const u32x4& v) {
-        if (block + r >= p.M || c0 + c >= p.N) return;
+        if (block + r >= p.M || c0 + c >= p.N || !leads<S>()) return;
         f32x4* at = reinterpret_cast<f32x4*>(p.sum + (part * p.M + block + r) * p.ld_sum + c0 + c);
         f32x4 f = __builtin_bit_cast(f32x4, v);
         if (p.add) f += *at;
@@ -371,7 +372,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_product_kernel(Prod
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][j][e] *= p.scale;
       Out::go(smem + wave * Out::kWave, acc[i], lane, [&](int r, int c, const u32x4& v) {
-        if (block + r < p.M && c0 + c < p.N)
+        if (block + r < p.M && c0 + c < p.N && leads<S>())
           *reinterpret_cast<u32x4*>(p.out + (block + r) * p.ldo + (c0 + c) * (int)sizeof(T)) = v;
       });
     }
@@ -421,7 +422,7 @@ int64_t tiles(int64_t n, int64_t b) { return (n + b - 1) / b; }
 
 // Tile shapes.  Large (bf16): one workgroup of eight waves a CU.  Middle: two workgroups.  Deep: one,
 // with three steps of loads in flight, where there are not two for each CU.  Small: two, for few tiles.
-enum class Kind { Large, Middle, Deep, Small };
+enum class Kind { Large, Middle, Deep, Narrow, Small, Tiny };
 template <typename T, Kind K>
 struct ShapeOf;
 template <typename T>
@@ -435,6 +436,14 @@ struct ShapeOf<T, Kind::Deep> {
 template <typename T>
 struct ShapeOf<T, Kind::Small> {
   typedef Shape<T, 64, 64, 2, 2, 128, 4, 2> S;
+};
+template <typename T>
+struct ShapeOf<T, Kind::Tiny> {
+  typedef Shape<T, 32, 32, 1, 1, 128, 4, 4, 4> S;
+};
+template <typename T>
+struct ShapeOf<T, Kind::Narrow> {
+  typedef Shape<T, 128, 64, 2, 2, 128, 2, 3> S;
 };
 template <>
 struct ShapeOf<uint16_t, Kind::Large> {
@@ -450,7 +459,9 @@ void with_shape(Kind k, F&& f) {
     case Kind::Large: return f(typename ShapeOf<T, Kind::Large>::S());
     case Kind::Middle: return f(typename ShapeOf<T, Kind::Middle>::S());
     case Kind::Deep: return f(typename ShapeOf<T, Kind::Deep>::S());
-    default: return f(typename ShapeOf<T, Kind::Small>::S());
+    case Kind::Narrow: return f(typename ShapeOf<T, Kind::Narrow>::S());
+    case Kind::Small: return f(typename ShapeOf<T, Kind::Small>::S());
+    default: return f(typename ShapeOf<T, Kind::Tiny>::S());
   }
 }
 
@@ -462,37 +473,46 @@ void with_shape(Kind k, F&& f) {
 // Middle (four rounds of Small 160), 256 x 1000 x 768 19 of Small, alone (Middle 56).
 struct Round {
   Kind kind;
-  int side, groups;  // tile, workgroups of a CU
+  int rows, cols, groups;  // tile, workgroups of a CU
   float step, alone, end;
 };
-constexpr Round kRounds[2][4] = {{{Kind::Large, 256, 1, 1.6f, 1.6f, 8.0f},
-                                  {Kind::Middle, 128, 2, 1.0f, 0.75f, 3.5f},
-                                  {Kind::Deep, 128, 1, 0.7f, 0.7f, 4.5f},
-                                  {Kind::Small, 64, 2, 0.45f, 0.35f, 3.0f}},
-                                 {{Kind::Middle, 128, 2, 3.9f, 2.2f, 4.0f},
-                                  {Kind::Deep, 128, 1, 2.1f, 2.1f, 4.5f},
-                                  {Kind::Small, 64, 2, 1.18f, 0.68f, 3.0f},
-                                  {Kind::Small, 64, 2, 1.18f, 0.68f, 3.0f}}};
+constexpr Round kRounds[2][5] = {{{Kind::Large, 256, 256, 1, 1.6f, 1.6f, 8.0f},
+                                  {Kind::Middle, 128, 128, 2, 1.0f, 0.75f, 3.5f},
+                                  {Kind::Deep, 128, 128, 1, 0.7f, 0.7f, 4.5f},
+                                  {Kind::Small, 64, 64, 2, 0.45f, 0.35f, 3.0f},
+                                  {Kind::Tiny, 32, 32, 4, 0.5f, 0.25f, 3.0f}},
+                                 {{Kind::Middle, 128, 128, 2, 3.9f, 2.2f, 4.0f},
+                                  {Kind::Narrow, 128, 64, 3, 2.8f, 1.3f, 3.5f},
+                                  {Kind::Small, 64, 64, 2, 1.18f, 0.68f, 3.0f},
+                                  {Kind::Tiny, 32, 32, 4, 0.6f, 0.3f, 3.0f},
+                                  {Kind::Tiny, 32, 32, 4, 0.6f, 0.3f, 3.0f}}};
 
 // How a product of M x N over K runs: in tiles of a kind, and in parts of K that are summed afterwards.
 struct Way {
   Kind kind;
-  int side, parts;
+  int cols, parts;
 };
 Way way_of(int64_t M, int64_t N, int64_t K, int es, bool may_split) {
   Way best = {Kind::Small, 64, 1};
   float least = INFINITY;
   const int64_t steps = (K * es + 127) / 128;
   for (const Round& r : kRounds[es == 4]) {
-    const int64_t t = tiles(M, r.side) * tiles(N, r.side), slots = 256 * r.groups;
-    // As many parts as fill the GPU once, of at least eight steps.
-    const int64_t parts = may_split ? std::max<int64_t>(1, std::min<int64_t>({slots / t, steps / 8, 64})) : 1;
-    const int64_t rounds = tiles(t * parts, slots), each = tiles(steps, parts);
-    float us = (float)rounds * ((t * parts <= 256 ? r.alone : r.step) * (float)each + r.end);
-    if (parts > 1) us += 3.0f + (float)(parts * M * N) * 8e-6f / 4.5f;
-    if (us < least) {
-      least = us;
-      best = {r.kind, r.side, (int)parts};
+    const int64_t t = tiles(M, r.rows) * tiles(N, r.cols), slots = 256 * r.groups;
+    // As many parts as fill the GPU once, of at least eight steps; or one.
+    const int64_t most = may_split ? std::max<int64_t>(1, std::min<int64_t>({slots / t, steps / 8, 64})) : 1;
+    for (int64_t parts : {most, (int64_t)1}) {
+      const int64_t full = t * parts / slots, left = t * parts - full * slots;
+      const float each = (float)tiles(steps, parts);
+      float us = (float)full * (r.step * each + r.end);
+      if (left > 0) {  // the last round: some CUs hold fewer workgroups than they could
+        const int64_t held = tiles(left, 256);
+        us += (r.groups == 1 ? r.step : r.alone + (r.step - r.alone) * (float)(held - 1) / (float)(r.groups - 1)) * each + r.end;
+      }
+      if (parts > 1) us += 3.0f + (float)(parts * M * N) * 8e-6f / 4.5f;
+      if (us < least) {
+        least = us;
+        best = {r.kind, r.cols, (int)parts};
+      }
     }
   }
   return best;
@@ -526,7 +546,7 @@ BackLayout backward_layout(const elasto_linear_ce_t& d) {
   };
   l.live = take(up(d.rows, 256) / 8);
   l.dz = take(d.rows * l.piece * es);
-  l.db = take(tiles(d.rows, 64) * l.piece * 4);
+  l.db = take(tiles(d.rows, 32) * l.piece * 4);
   // dx's sums live through all pieces, dW's through one.
   l.sum = take(l.x_summed ? (int64_t)l.x.parts * d.rows * d.dim * 4 : 0);
   l.wsum = take(l.w.parts > 1 ? (int64_t)l.w.parts * l.piece * d.dim * 4 : 0);
@@ -536,7 +556,7 @@ Way forward_way(const elasto_linear_ce_t& d) {
   return way_of(d.rows, d.classes, d.dim, d.dtype == ELASTO_BF16 ? 2 : 4, false);
 }
 int64_t forward_bytes(const elasto_linear_ce_t& d) {
-  return up(tiles(d.classes, forward_way(d).side) * d.rows * 8, 256) + up(d.rows * 4, 256);
+  return up(tiles(d.classes, forward_way(d).cols) * d.rows * 8, 256) + up(d.rows * 4, 256);
 }
 
 struct Args {
@@ -609,7 +629,7 @@ template <typename T>
 hipError_t forward(const Args& a, float* loss, float* lse, char* ws, hipStream_t s) {
   CeP p = params(a);
   const Way way = forward_way(a.d);
-  const int64_t n = tiles(a.d.classes, way.side);
+  const int64_t n = tiles(a.d.classes, way.cols);
   p.part = reinterpret_cast<float2*>(ws);
   p.picked = reinterpret_cast<float*>(ws + up(n * a.d.rows * 8, 256));
   with_shape<T>(way.kind, [&](auto shape) {

@@ -44,6 +44,7 @@ struct Operand {
 
   static __device__ __forceinline__ int swizzle(int r) {
     if constexpr (!TURNED) return KB == 128 ? (r >> 1) & 7 : (r >> 2) & 3;
+    if constexpr (B == 32) return 0;  // four rows are 256 bytes (fp32: the half-waves' rows share banks)
     if constexpr (sizeof(T) == 4) return ((r >> 2) & 1) * 8;
     if constexpr (B == 64) return ((r >> 1) & 1) * 4;
     return (r & 3) * 4;
@@ -95,21 +96,22 @@ struct Operand {
   template <int BLOCKS>
   struct Reader {
     int at[TURNED ? BLOCKS : kQuarters];
-    __device__ __forceinline__ Reader(int first, int lane) {
+    // from: the quarter that counts as the first.
+    __device__ __forceinline__ Reader(int first, int lane, int from) {
       const int lr = lane & 31, lg = lane >> 5;
       if constexpr (!TURNED) {
 #pragma unroll
-        for (int kk = 0; kk < kQuarters; ++kk) at[kk] = (first + lr) * KB + (((2 * kk + lg) ^ swizzle(lr)) << 4);
+        for (int kk = 0; kk < kQuarters; ++kk) at[kk] = (first + lr) * KB + (((2 * (kk + from) + lg) ^ swizzle(lr)) << 4);
       } else {
 #pragma unroll
         for (int i = 0; i < BLOCKS; ++i) {
           if constexpr (sizeof(T) == 2) {
             const int lq = lane & 15, g = lane >> 4;
             const int r = 8 * lg + (lq >> 2), c = first + 32 * i + 16 * (g & 1) + 4 * (lq & 3);
-            at[i] = r * kRow + (((c >> 3) ^ swizzle(r)) << 4) + (c & 7) * 2;
+            at[i] = (r + 16 * from) * kRow + (((c >> 3) ^ swizzle(r)) << 4) + (c & 7) * 2;
           } else {
             const int r = 4 * lg, c = first + 32 * i + lr;
-            at[i] = r * kRow + (((c >> 2) ^ swizzle(r)) << 4) + (c & 3) * 4;
+            at[i] = (r + 8 * from) * kRow + (((c >> 2) ^ swizzle(r)) << 4) + (c & 3) * 4;
           }
         }
       }
@@ -159,17 +161,21 @@ __device__ __forceinline__ void multiply(const u32x4 (&a)[TM], const u32x4 (&b)[
   }
 }
 
-// GROUPS: workgroups that a CU holds by their registers and LDS.
-template <typename T_, int BM_, int BN_, int WM_, int WN_, int KB_, int STAGES_, int GROUPS_>
+// GROUPS: workgroups that a CU holds by their registers and LDS.  KS: 4 where each of four groups of WM x
+// WN waves takes one quarter of every step (small launches: a tile's chain of products is a quarter as
+// long); their sums are added at the end, in the groups' order, in all of them.
+template <typename T_, int BM_, int BN_, int WM_, int WN_, int KB_, int STAGES_, int GROUPS_, int KS_ = 1>
 struct Shape {
   typedef T_ T;
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_, KB = KB_;
   static constexpr int kK = KB / (int)sizeof(T_);  // values of K of a step
-  static constexpr int kThreads = 64 * WM * WN;
+  static constexpr int KS = KS_, kTeam = WM * WN, kThreads = 64 * kTeam * KS;
   static constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 32, TN = WTN / 32;
   static constexpr int kStage = (BM + BN) * KB;
-  static constexpr int kGroups = GROUPS_, kWaves = kGroups * WM * WN / 4;  // kWaves: on a SIMD
+  static constexpr bool kFew = TM * TN <= 2;  // few accumulators
+  static constexpr int kGroups = GROUPS_, kWaves = kGroups * kTeam * KS / 4;  // kWaves: on a SIMD
   static_assert(STAGES * kStage * kGroups <= 160 * 1024, "LDS of a CU");
+  static_assert(KS == 1 || (KB_ == 128 && KS == 4 && KS * kTeam * TM * TN * 4096 <= STAGES * kStage), "quarters");
 };
 
 // The operands' values of one quarter of a step.
@@ -182,7 +188,8 @@ struct Readers {
   typename OA::template Reader<S::TM> a;
   typename OB::template Reader<S::TN> b;
   __device__ __forceinline__ Readers(int wave, int lane)
-      : a(wave / S::WN * S::WTM, lane), b(wave % S::WN * S::WTN, lane) {}
+      : a(wave % S::kTeam / S::WN * S::WTM, lane, wave / S::kTeam),
+        b(wave % S::WN * S::WTN, lane, wave / S::kTeam) {}
   __device__ __forceinline__ void read(Quarter<S>& q, const char* st, int kk) const {
 #pragma unroll
     for (int i = 0; i < S::TM; ++i) q.a[i] = a.read(st, i, kk);
@@ -224,6 +231,13 @@ __device__ __forceinline__ void product_step(const OA& oa, const OB& ob, const R
   typedef typename S::T T;
   const int tid = threadIdx.x;
   constexpr int NR = OA::kReads * S::TM + OB::kReads * S::TN, NM = (sizeof(T) == 2 ? 1 : 4) * S::TM * S::TN;
+  if constexpr (S::KS > 1) {  // this group's quarter, multiplied a step later
+    rd.read(q[0], st, 0);
+    if (more) issue_step<LIVE>(oa, ob, fill, at, tid);
+    if constexpr (!FIRST) multiply<T>(q[1].a, q[1].b, acc);
+    q[1] = q[0];
+    return;
+  }
   __builtin_amdgcn_sched_barrier(0);
   rd.read(q[0], st, 0);
   if constexpr (!FIRST) {
@@ -240,6 +254,12 @@ __device__ __forceinline__ void product_step(const OA& oa, const OB& ob, const R
     Interleave<0, NM, NR>::go();
     __builtin_amdgcn_sched_barrier(0);
   }
+}
+
+// Whether this wave's group starts from acc (the others from zeros) and hands the results out.
+template <typename S>
+__device__ __forceinline__ bool leads() {
+  return S::KS == 1 || (int)threadIdx.x < 64 * S::kTeam;
 }
 
 // The sums of K values [k0, k1) (k0 a whole step) of the tile at (m0, n0), into acc, which
@@ -298,8 +318,58 @@ __device__ __forceinline__ void tile_product(char* smem, const Matrix& A, const 
     fill = fill + 1 == S::STAGES ? 0 : fill + 1;
   };
   one(0, std::true_type());
-  for (int kt = 1; kt < nk; ++kt) one(kt, std::false_type());
-  multiply<T>(q[1].a, q[1].b, acc);
+  if constexpr (S::kFew && sizeof(T) == 4) {
+    // fp32 in small tiles: the sums of eight steps (256 values of K) are added up by themselves, so
+    // that an error does not grow with the root of K.
+    f32x16 sum[S::TM][S::TN] = {};
+    for (int kt = 1; kt < nk;) {
+      const int end = min(nk, kt + 8);
+#pragma clang loop unroll(disable)
+      for (; kt < end; ++kt) one(kt, std::false_type());
+#pragma unroll
+      for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) {
+          sum[i][j] += acc[i][j];
+          acc[i][j] = f32x16{};
+        }
+    }
+    multiply<T>(q[1].a, q[1].b, acc);
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j) acc[i][j] += sum[i][j];
+  } else {
+    for (int kt = 1; kt < nk; ++kt) one(kt, std::false_type());
+    multiply<T>(q[1].a, q[1].b, acc);
+  }
+  if constexpr (S::KS > 1) {
+    __syncthreads();
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), team = wave % S::kTeam, lane = tid & 63;
+    auto slot = [&](int ks, int i, int j, int g) {
+      return reinterpret_cast<f32x4*>(smem) + ((((ks * S::kTeam + team) * S::TM + i) * S::TN + j) * 4 + g) * 64 + lane;
+    };
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *slot(wave / S::kTeam, i, j, g) = f32x4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          f32x4 s = *slot(0, i, j, g);
+#pragma unroll
+          for (int ks = 1; ks < S::KS; ++ks) s += *slot(ks, i, j, g);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][4 * g + e] = s[e];
+        }
+  }
 }
 
 }  // namespace elasto
