@@ -27,8 +27,7 @@ namespace elasto {
 namespace {
 
 constexpr int kMaxDim = 16384;
-constexpr int kGradBlocks = 1024;  // workgroups of the backward pass
-constexpr int kSums = 5;           // pre gamma, pre beta, post gamma, post beta, gate
+constexpr int kSums = 5;                   // pre gamma, pre beta, post gamma, post beta, gate
 
 struct Rows {  // strides in bytes
   char* p;
@@ -45,9 +44,10 @@ struct BlockP {
   bool layer, post, has_y;
   float a, eps, inv_dim;
   // Backward.
-  float* part;             // [workgroup][kSums][dim]
-  float* dgate;            // [batch][dim] where a workgroup has all rows of a gate, else NULL
-  int slices;              // workgroups of a sequence
+  float* part;             // [workgroup][4][dim]
+  float* gate_part;        // [unit or workgroup][dim]
+  bool gate_unit;          // a gate's sums end with the unit
+  int slices;              // units of a sequence: runs of its rows
   int wanted;              // bits: the sums that are asked for
 };
 
@@ -201,17 +201,33 @@ __device__ __forceinline__ void load_weight(const float* w, float none, int dim,
     for (int e = 0; e < L::E; ++e) v[e] = none;
 }
 
-// v less its mean, 0 in columns that are not there.
-template <typename L>
-__device__ __forceinline__ void centre(float (&v)[L::E], float mean, int dim, int t) {
+// 1 where a thread's column is there, 0 where it is not (a run of eight is there or not: dim is a multiple
+// of 8 where rows are read in runs).  What is loaded from columns that are not there is 0, so only what is
+// added to a whole row needs it.
+template <typename L, bool WIDE>
+struct There {
+  float m[WIDE ? L::E / 8 : L::E];
+  __device__ __forceinline__ There(int dim, int t) {
 #pragma unroll
-  for (int e = 0; e < L::E; ++e) v[e] = L::column(e, t) < dim ? v[e] - mean : 0.0f;
-}
+    for (int i = 0; i < (WIDE ? L::E / 8 : L::E); ++i) m[i] = L::column(WIDE ? 8 * i : i, t) < dim ? 1.0f : 0.0f;
+  }
+  // less[e] where the column is there: computed once a run.
+  __device__ __forceinline__ void from(float (&v)[L::E], float less) const {
+#pragma unroll
+    for (int i = 0; i < (WIDE ? L::E / 8 : L::E); ++i) {
+      const float k = less * m[i];
+#pragma unroll
+      for (int e = 0; e < (WIDE ? 8 : 1); ++e) v[(WIDE ? 8 : 1) * i + e] -= k;
+    }
+  }
+};
 
-// Whether the weights and the next row's loads stay in registers: not for rows of 16 waves with sixteen
-// values a thread, which have 128 registers.
-template <int W, int CH>
-constexpr bool kKeep = W * CH < 32;
+// Whether the weights and the next row's loads stay in registers: not forward for rows of 16 waves (which
+// have 128 registers), nor backward.
+template <int W>
+constexpr bool kKeepForward = W < 16;
+template <int CH>
+constexpr bool kKeepBackward = CH == 1;
 
 // T: of y and u.  S: of the stream.  W waves a row; a workgroup of 256 threads holds 4 / W rows.  A group of
 // W waves takes rows in strides of the grid's, the next one's loads in flight, the weights in registers.
@@ -219,10 +235,11 @@ template <typename T, typename S, bool LAYER, int W, int CH, bool WIDE>
 __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_kernel(BlockP p) {
   typedef Place<W, CH, WIDE> L;
   constexpr int E = L::E, R = W > 4 ? 1 : 4 / W;
-  constexpr bool KEEP = kKeep<W, CH>;
+  constexpr bool KEEP = kKeepForward<W>;
   __shared__ float red[R][2 * W * kMost];
-  const int t = threadIdx.x % L::T, mine = threadIdx.x / L::T;
+  const int t = threadIdx.x % L::T, mine = __builtin_amdgcn_readfirstlane(threadIdx.x / L::T);
   Exchange<W> exchange = {red[mine]};
+  const There<L, WIDE> there(p.dim, t);
   const int rows = p.batch * p.tokens, stride = gridDim.x * R;
   float pg[E], pb[E], qg[E], qb[E], g[E];
   auto pre = [&] {
@@ -268,7 +285,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_kernel(BlockP
 #pragma unroll
           for (int e = 0; e < E; ++e) s[0] += v[e];
           exchange(s, t);
-          centre<L>(v, s[0] * p.inv_dim, p.dim, t);
+          there.from(v, s[0] * p.inv_dim);
         }
         float q[1] = {0.0f};
 #pragma unroll
@@ -285,7 +302,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_kernel(BlockP
         gate_of = nb;
       }
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = fmaf(p.a, x[e], L::column(e, t) < p.dim ? g[e] * v[e] : 0.0f);
+      for (int e = 0; e < E; ++e) x[e] = fmaf(p.a, x[e], g[e] * v[e]);
     } else {
       if (KEEP && row + stride < rows) fetch(row + stride + mine);
 #pragma unroll
@@ -298,7 +315,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_kernel(BlockP
 #pragma unroll
       for (int e = 0; e < E; ++e) s[0] += x[e];
       exchange(s, t);
-      centre<L>(x, s[0] * p.inv_dim, p.dim, t);
+      there.from(x, s[0] * p.inv_dim);
     }
     float q[1] = {0.0f};
 #pragma unroll
@@ -315,14 +332,15 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_kernel(BlockP
 // Three exchanges a row (RMS: two): sums for the means; about them, with what both norms need that the
 // gradient of x' does not wait for; and the norm behind the block's.
 template <typename T, typename S, bool LAYER, int W, int CH, bool WIDE>
-__global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_bwd_kernel(BlockP p) {
+__global__ __launch_bounds__(W > 4 ? 64 * W : 256, W > 4 ? 1 : 3) void block_norm_bwd_kernel(BlockP p) {
   typedef Place<W, CH, WIDE> L;
   constexpr int E = L::E, R = W > 4 ? 1 : 4 / W;
-  constexpr bool KEEP = kKeep<W, CH>;
+  constexpr bool KEEP = kKeepBackward<CH>;
   __shared__ float red[R][2 * W * kMost];
   __shared__ float sums[R > 1 ? (R - 1) * L::T : 1];
-  const int t = threadIdx.x % L::T, mine = threadIdx.x / L::T;
+  const int t = threadIdx.x % L::T, mine = __builtin_amdgcn_readfirstlane(threadIdx.x / L::T);
   Exchange<W> exchange = {red[mine]};
+  const There<L, WIDE> there(p.dim, t);
   float pg[E], pb[E], qg[E], qb[E], gg[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) pg[e] = pb[e] = qg[e] = qb[e] = gg[e] = 0.0f;
@@ -384,8 +402,9 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_bwd_kernel(Bl
       if (p.du.p) {
         ru.get(d);
         rx.get(x);
+        if constexpr (LAYER)
 #pragma unroll
-        for (int e = 0; e < E; ++e) pb[e] += d[e];
+          for (int e = 0; e < E; ++e) pb[e] += d[e];
       } else {
 #pragma unroll
         for (int e = 0; e < E; ++e) d[e] = x[e] = 0.0f;
@@ -401,11 +420,11 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_bwd_kernel(Bl
         for (int e = 0; e < E; ++e) {
           s[0] += x[e];
           s[1] += v[e];
-          s[2] = fmaf(d[e], L::column(e, t) < p.dim ? w_pre[e] : 0.0f, s[2]);
+          s[2] = fmaf(d[e], w_pre[e], s[2]);
         }
         exchange(s, t);
-        if (p.du.p) centre<L>(x, s[0] * p.inv_dim, p.dim, t);
-        if (p.post) centre<L>(v, s[1] * p.inv_dim, p.dim, t);
+        if (p.du.p) there.from(x, s[0] * p.inv_dim);
+        if (p.post) there.from(v, s[1] * p.inv_dim);
         c = s[2] * p.inv_dim;
         s[0] = s[1] = s[2] = 0.0f;
       }
@@ -413,7 +432,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_bwd_kernel(Bl
       for (int e = 0; e < E; ++e) {
         s[0] = fmaf(x[e], x[e], s[0]);
         s[1] = fmaf(v[e], v[e], s[1]);
-        s[2] = fmaf(d[e] * (L::column(e, t) < p.dim ? w_pre[e] : 0.0f), x[e], s[2]);
+        s[2] = fmaf(d[e] * w_pre[e], x[e], s[2]);
       }
       exchange(s, t);
       const float r = 1.0f / sqrtf(fmaf(s[0], p.inv_dim, p.eps));
@@ -424,8 +443,9 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_bwd_kernel(Bl
         for (int e = 0; e < E; ++e) {
           const float xn = x[e] * r;
           pg[e] = fmaf(d[e], xn, pg[e]);
-          d[e] = r * (fmaf(d[e], w_pre[e], -c) - xn * a);
+          d[e] = r * fmaf(d[e], w_pre[e], -xn * a);
         }
+        if constexpr (LAYER) there.from(d, r * c);
       }
       if (p.dx_out.p) {
         rd.get(x);
@@ -446,8 +466,6 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_bwd_kernel(Bl
       float q[2] = {0.0f, 0.0f};
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        // What is not there stays out of the sums.
-        d[e] = live && L::column(e, t) < p.dim ? d[e] : 0.0f;
         v[e] *= ry1;
         const float n = p.post ? (LAYER ? fmaf(v[e], w_post[e], b_post[e]) : v[e] * w_post[e]) : v[e];
         gg[e] = fmaf(d[e], n, gg[e]);
@@ -468,41 +486,42 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_bwd_kernel(Bl
       }
       if (p.dy.p && live) store_row<L, WIDE>(at<T>(p.dy, b, tok), p.dim, t, d);
     }
-    if (p.dgate) {  // all rows of this gate are here
-      flush(gg, p.dgate + (int64_t)b * p.dim);
+    if (p.gate_unit) {
+      flush(gg, p.gate_part + (int64_t)unit * p.dim);
 #pragma unroll
       for (int e = 0; e < E; ++e) gg[e] = 0.0f;
     }
   }
   if (!p.part) return;
-  float* part = p.part + (int64_t)blockIdx.x * kSums * p.dim;
+  float* part = p.part + (int64_t)blockIdx.x * 4 * p.dim;
   if (p.wanted & 1) flush(pg, part);
   if (p.wanted & 2) flush(pb, part + p.dim);
   if (p.wanted & 4) flush(qg, part + 2 * p.dim);
   if (p.wanted & 8) flush(qb, part + 3 * p.dim);
-  if ((p.wanted & 16) && !p.dgate) flush(gg, part + 4 * p.dim);
+  if ((p.wanted & 16) && !p.gate_unit) flush(gg, p.gate_part + (int64_t)blockIdx.x * p.dim);
 }
 
-// out[b][c] = the sum over its parts, 64 columns a workgroup, 16 slices of the parts.
+// Column sums of the parts, 64 columns a workgroup, 16 slices of the parts.
 struct SumP {
-  const float* part;
+  const float *part, *gate_part;
   float* out[kSums];
   int dim, parts;
-  int gates, gate_parts;  // of the gate's gradient
+  int gate_parts;  // of each gate
 };
 __global__ __launch_bounds__(1024) void block_sum_kernel(SumP p) {
   __shared__ float red[16][65];
-  const int which = blockIdx.y;
-  // The gate's gradients are further rows of the grid.
-  const int sum = which < 4 ? which : 4, gate = which < 4 ? 0 : which - 4;
+  // The gates' gradients are further rows of the grid.
+  const int sum = min((int)blockIdx.y, 4), gate = blockIdx.y - sum;
   float* out = p.out[sum];
   if (!out) return;
-  const int from = sum == 4 ? gate * p.gate_parts : 0, n = sum == 4 ? p.gate_parts : p.parts;
+  const int n = sum == 4 ? p.gate_parts : p.parts;
+  const int64_t ld = sum == 4 ? p.dim : 4 * (int64_t)p.dim;
+  const float* from = sum == 4 ? p.gate_part + (int64_t)gate * n * p.dim : p.part + sum * (int64_t)p.dim;
   const int lane = threadIdx.x & 63, sl = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
   float s = 0.0f;
   if (c < p.dim)
 #pragma unroll 8
-    for (int i = sl; i < n; i += 16) s += p.part[((int64_t)(from + i) * kSums + sum) * p.dim + c];
+    for (int i = sl; i < n; i += 16) s += from[i * ld + c];
   red[sl][lane] = s;
   __syncthreads();
   if (sl != 0 || c >= p.dim) return;
@@ -538,11 +557,16 @@ Width backward_width(int dim) {
   if (dim <= 1024) return {2, 1};
   if (dim <= 2048) return {4, 1};
   if (dim <= 4096) return {8, 1};
-  if (dim <= 8192) return {16, 1};
-  return {16, 2};
+  if (dim <= 8192) return {8, 2};
+  return {8, 4};
 }
 // Workgroups of a forward launch: what the GPU holds, several times over for rows of one wave.
 int forward_blocks(int dim) { return dim <= 4096 ? 256 * 8 : 256 * 4; }
+// Backward: the workgroups that the GPU holds, three a CU of rows of up to 2048 (kept to a third of its
+// registers: 243 -> 166 us where they took 190 and two ran; 12608 rows of 768, layer norm, 192 -> 109), and the
+// units that they share out (below; with as many as workgroups 175 us, with four times as many 175).
+int grad_blocks(Width w) { return w.waves <= 4 ? 768 : w.runs == 1 ? 256 : 512; }
+int units_of(Width w) { return w.runs == 1 ? 2 * grad_blocks(w) : grad_blocks(w); }
 int rows_of(Width w) { return w.waves > 4 ? 1 : 4 / w.waves; }
 
 template <typename T, typename S, bool LAYER, bool WIDE>
@@ -567,8 +591,8 @@ void launch_backward(const BlockP& p, unsigned grid, hipStream_t s) {
     case 5: return go(block_norm_bwd_kernel<T, S, LAYER, 2, 1, WIDE>, 256);
     case 9: return go(block_norm_bwd_kernel<T, S, LAYER, 4, 1, WIDE>, 256);
     case 17: return go(block_norm_bwd_kernel<T, S, LAYER, 8, 1, WIDE>, 512);
-    case 33: return go(block_norm_bwd_kernel<T, S, LAYER, 16, 1, WIDE>, 1024);
-    default: return go(block_norm_bwd_kernel<T, S, LAYER, 16, 2, WIDE>, 1024);
+    case 18: return go(block_norm_bwd_kernel<T, S, LAYER, 8, 2, WIDE>, 512);
+    default: return go(block_norm_bwd_kernel<T, S, LAYER, 8, 4, WIDE>, 512);
   }
 }
 
@@ -599,16 +623,26 @@ bool check_sizes(const elasto_block_norm_t* d) {
   return true;
 }
 
+// Every sequence is cut into as many runs of its own rows; a workgroup takes runs a grid apart, so runs
+// of sequences of all lengths.
 struct Slices {
-  int per;        // workgroups of a sequence
+  int per;    // of a sequence
+  int units;  // of all
   int grid;
 };
 Slices slices_of(const elasto_block_norm_t& d) {
-  const int r = rows_of(backward_width(d.dim));
+  const Width w = backward_width(d.dim);
+  const int r = rows_of(w);
+  const int blocks = grad_blocks(w);
   const int64_t rounds = (d.tokens + r - 1) / r;
-  const int64_t per = std::max<int64_t>(1, std::min<int64_t>(rounds, kGradBlocks / std::max(1, d.batch)));
-  return {(int)per, (int)std::min<int64_t>((int64_t)d.batch * per, kGradBlocks)};
+  const int64_t per = std::max<int64_t>(1, std::min<int64_t>(rounds, units_of(w) / std::max(1, d.batch)));
+  const int64_t units = (int64_t)d.batch * per;
+  return {(int)per, (int)units, (int)std::min<int64_t>(units, blocks)};
 }
+// Bytes of the parts: of the weights' sums by workgroups, of the gate's by units or workgroups (a unit that
+// has a whole sequence writes the gate's gradient itself).
+int64_t part_bytes(const Slices& s, int dim) { return (int64_t)s.grid * 4 * dim * 4; }
+int64_t gate_bytes(const Slices& s, int dim) { return s.per > 1 ? (int64_t)s.units * dim * 4 : (int64_t)s.grid * dim * 4; }
 
 bool check_desc(const elasto_block_norm_t* d) {
   if (!check_sizes(d)) return false;
@@ -751,26 +785,29 @@ elasto_status_t elasto_op_block_norm_bwd(const elasto_block_norm_t* d, const ela
   }
   const Slices sl = slices_of(*d);
   p.slices = sl.per;
-  if (d_gate && per_sequence && sl.per == 1) p.dgate = d_gate;
-  const int sums = p.wanted & ~(p.dgate ? 16 : 0);
+  p.gate_unit = d_gate && per_sequence;
+  const bool direct = p.gate_unit && sl.per == 1;
+  const int sums = p.wanted & ~(direct ? 16 : 0);
   if (sums) {
-    const int64_t need = (int64_t)sl.grid * kSums * d->dim * 4;
-    if (need > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < need))
+    const int64_t need = part_bytes(sl, d->dim) + gate_bytes(sl, d->dim);
+    if (!workspace || !aligned(workspace, 16) || workspace_bytes < need)
       return fail(ELASTO_ERR_INVALID_ARG, "block_norm: the workspace holds %lld of %lld bytes",
                   (long long)(workspace ? workspace_bytes : 0), (long long)need);
     p.part = static_cast<float*>(workspace);
+    p.gate_part = p.part + part_bytes(sl, d->dim) / 4;
   }
+  if (direct) p.gate_part = d_gate;
   launch_types(p, wide(p), es == 2, ss == 2, true, (unsigned)sl.grid, s);
   e = hipGetLastError();
   if (e == hipSuccess && sums) {
     SumP q = {};
     q.part = p.part;
-    for (int i = 0; i < kSums; ++i) q.out[i] = i == 4 && p.dgate ? nullptr : out[i];
+    q.gate_part = p.gate_part;
+    for (int i = 0; i < kSums; ++i) q.out[i] = i == 4 && direct ? nullptr : out[i];
     q.dim = d->dim;
     q.parts = sl.grid;
-    q.gates = per_sequence ? d->batch : 1;
     q.gate_parts = per_sequence ? sl.per : sl.grid;
-    const unsigned gates = q.out[4] ? (unsigned)q.gates : 0;
+    const unsigned gates = !q.out[4] ? 0 : per_sequence ? (unsigned)d->batch : 1;
     hipLaunchKernelGGL(block_sum_kernel, dim3((unsigned)((d->dim + 63) / 64), 4 + gates), dim3(1024), 0, s, q);
     e = hipGetLastError();
   }
@@ -781,7 +818,8 @@ elasto_status_t elasto_op_block_norm_bwd(const elasto_block_norm_t* d, const ela
 elasto_status_t elasto_block_norm_workspace(const elasto_block_norm_t* d, int64_t* bytes) {
   if (!bytes) return fail(ELASTO_ERR_INVALID_ARG, "NULL argument");
   if (!check_sizes(d)) return ELASTO_ERR_INVALID_ARG;
-  *bytes = (int64_t)slices_of(*d).grid * kSums * d->dim * 4;
+  const Slices s = slices_of(*d);
+  *bytes = part_bytes(s, d->dim) + gate_bytes(s, d->dim);
   return ELASTO_OK;
 }
 

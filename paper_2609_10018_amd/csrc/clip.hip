@@ -22,18 +22,16 @@
 namespace elasto {
 namespace {
 
-constexpr int kTensors = 140;          // of a launch: its arguments stay below 4 KB
+constexpr int kTensors = 180;          // of a launch: its arguments stay below 4 KB
 constexpr int kChunk = 16384;          // bytes of a chunk
 constexpr int kMaxBlocks = 2048;       // workgroups of a call's norm, one partial sum each
 constexpr int kThreads = 256;
 
-struct Entry {
-  const char* in;
-  int64_t count;  // elements; the sign holds the type: negative for bf16
-};
+// The tensors of a launch: 14 bytes each, and 8 for a result.
 struct Table {
-  Entry t[kTensors];
+  uintptr_t at[kTensors];        // address; bit 0: bf16
   uint32_t first[kTensors + 1];  // first chunk of each tensor
+  uint16_t last[kTensors];       // elements of the last chunk
   int n;
 };
 struct Results {
@@ -70,6 +68,20 @@ __device__ __forceinline__ int find(const Tab& t, uint32_t c) {
   }
   return lo;
 }
+
+struct Chunk {
+  const char* p;
+  int64_t offset;  // bytes, in its tensor
+  int tensor, n;
+  bool bf16;
+  __device__ __forceinline__ Chunk(const Table& t, uint32_t c) {
+    tensor = find(t, c);
+    offset = (int64_t)(c - t.first[tensor]) * kChunk;
+    bf16 = t.at[tensor] & 1;
+    p = reinterpret_cast<const char*>(t.at[tensor] & ~(uintptr_t)1) + offset;
+    n = c + 1 == t.first[tensor + 1] ? t.last[tensor] : bf16 ? kPer<uint16_t> : kPer<float>;
+  }
+};
 
 // The n elements of a chunk at p: `head` single ones up to a 16-byte boundary, whole pieces of 16
 // bytes, the rest single again.
@@ -132,17 +144,8 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(Table t, double* part) {
   const uint32_t chunks = t.first[t.n];
   double sum = 0.0;
   for (uint32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-    const int i = find(t, c);
-    const int64_t at = (int64_t)(c - t.first[i]), count = t.t[i].count;
-    if (count < 0) {
-      const int64_t first = at * kPer<uint16_t>;
-      sum += squares(reinterpret_cast<const uint16_t*>(t.t[i].in) + first,
-                     (int)min((int64_t)kPer<uint16_t>, -count - first));
-    } else {
-      const int64_t first = at * kPer<float>;
-      sum += squares(reinterpret_cast<const float*>(t.t[i].in) + first,
-                     (int)min((int64_t)kPer<float>, count - first));
-    }
+    const Chunk k(t, c);
+    sum += k.bf16 ? squares(reinterpret_cast<const uint16_t*>(k.p), k.n) : squares(reinterpret_cast<const float*>(k.p), k.n);
   }
   sum = block_sum(sum, red);
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
@@ -221,17 +224,12 @@ __global__ __launch_bounds__(kThreads) void clip_kernel(Table t, Results r, cons
   const uint32_t chunks = t.first[t.n];
   for (uint32_t b = blockIdx.x; b < chunks; b += gridDim.x) {
     const uint32_t c = chunks - 1 - b;
-    const int i = find(t, c);
-    const int64_t at = (int64_t)(c - t.first[i]), count = t.t[i].count;
-    if (count < 0) {
-      const int64_t first = at * kPer<uint16_t>;
-      scale(reinterpret_cast<const uint16_t*>(t.t[i].in) + first, reinterpret_cast<uint16_t*>(r.out[i]) + first,
-            (int)min((int64_t)kPer<uint16_t>, -count - first), f);
-    } else {
-      const int64_t first = at * kPer<float>;
-      scale(reinterpret_cast<const float*>(t.t[i].in) + first, reinterpret_cast<float*>(r.out[i]) + first,
-            (int)min((int64_t)kPer<float>, count - first), f);
-    }
+    const Chunk k(t, c);
+    char* out = r.out[k.tensor] + k.offset;
+    if (k.bf16)
+      scale(reinterpret_cast<const uint16_t*>(k.p), reinterpret_cast<uint16_t*>(out), k.n, f);
+    else
+      scale(reinterpret_cast<const float*>(k.p), reinterpret_cast<float*>(out), k.n, f);
   }
 }
 
@@ -305,7 +303,9 @@ hipError_t each_launch(const elasto_grad_t* g, int n, F&& f) {
         if (t.n == 0) return hipErrorInvalidValue;  // no tensor of a list has as many
         break;
       }
-      t.t[t.n] = {static_cast<const char*>(g[i].data), g[i].dtype == ELASTO_BF16 ? -g[i].count : g[i].count};
+      const int per = g[i].dtype == ELASTO_BF16 ? kChunk / 2 : kChunk / 4;
+      t.at[t.n] = reinterpret_cast<uintptr_t>(g[i].data) | (g[i].dtype == ELASTO_BF16);
+      t.last[t.n] = (uint16_t)(g[i].count - (c - 1) * per);
       at[t.n] = i;
       chunks += c;
       t.first[++t.n] = (uint32_t)chunks;

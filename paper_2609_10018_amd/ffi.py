@@ -436,7 +436,7 @@ class _Torch:
         import torch
         self.f32, self.i32, self.u8 = torch.float32, torch.int32, torch.uint8
         self.types = {torch.bfloat16: BF16, torch.float32: FP32}
-        self.cuda = torch.cuda
+        self.cuda, self.tensor = torch.cuda, torch.Tensor
 
 
 def _tt() -> _Torch:
@@ -914,7 +914,9 @@ class GradList:
     def __init__(self, tensors):
         self.tensors = list(tensors)
         self.array = (Grad * max(1, len(self.tensors)))()
-        self._seen = [None] * len(self.tensors)
+        self._seen = self.paired = None
+        t = _tt().tensor
+        self._places = t.data_ptr, t.numel   # asked of each tensor at each call
         self.entries()
 
     def __len__(self) -> int:
@@ -922,18 +924,17 @@ class GradList:
 
     def entries(self):
         """The C array, up to date."""
-        seen = self._seen
-        for i, t in enumerate(self.tensors):
-            now = t.data_ptr(), t.numel()
-            if now != seen[i]:
+        ts, (place, size) = self.tensors, self._places
+        now = list(map(place, ts)), list(map(size, ts))
+        if now != self._seen:
+            for i, t in enumerate(ts):
                 if not _dense(t):
                     raise ValueError(f"tensor {i} {tuple(t.shape)} with strides {t.stride()} is not "
                                      f"one run of memory")
-                if i and t.device != self.tensors[0].device:
-                    raise ValueError(f"tensor {i} lies on {t.device}, the first on "
-                                     f"{self.tensors[0].device}")
-                self.array[i] = Grad(now[0], now[1], _dtype(t))
-                seen[i] = now
+                if t.device != ts[0].device:
+                    raise ValueError(f"tensor {i} lies on {t.device}, the first on {ts[0].device}")
+                self.array[i] = Grad(now[0][i], now[1][i], _dtype(t))
+            self._seen, self.paired = now, None
         return self.array
 
 
@@ -971,10 +972,13 @@ def op_clip_gradients(grads, max_norm: float, stats, out=None, workspace=None, s
     if len(o) != len(g):
         raise ValueError(f"{len(o)} results for {len(g)} gradients")
     dev = _list_device(g, *o.tensors[:1], stats, workspace)
-    if o is not g:
+    if o is not g and o.array is not g.paired:
         for i, (a, b) in enumerate(zip(g.tensors, o.tensors)):
-            if a is not b and a.stride() != b.stride() and not (a.is_contiguous() and b.is_contiguous()):
-                raise ValueError(f"result {i} has its elements in another order than its gradient")
+            if a.shape != b.shape or a.stride() != b.stride() and not (
+                    a.is_contiguous() and b.is_contiguous()):
+                raise ValueError(f"result {i} {tuple(b.shape)} with strides {b.stride()} does not have its "
+                                 f"elements where its gradient has them")
+        g.paired = o.array   # checked once for the two lists
     check(load_library().elasto_op_clip_gradients(
         g.entries(), o.entries(), len(g), max_norm, _plain(stats, _tt().f32, "stats", 2),
         *_space(workspace), _stream_ptr(stream, dev)))
