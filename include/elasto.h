@@ -710,8 +710,8 @@ elasto_status_t elasto_op_linear_ce(const elasto_linear_ce_t* desc, float* loss,
                                     void* workspace, int64_t workspace_bytes, void* hip_stream);
 
 /* The gradients, from the forward's lse; dx [rows][dim] and dweight
- * [classes][dim] in the type of x, dbias fp32 [classes], each or NULL.  With no
- * rows dweight and dbias become 0. */
+ * [classes][dim] in the type of x, dbias fp32 [classes], each or NULL, in memory
+ * of their own.  With no rows dweight and dbias become 0. */
 elasto_status_t elasto_op_linear_ce_bwd(const elasto_linear_ce_t* desc, const float* lse,
                                         float scale, void* dx, int64_t lddx, void* dweight,
                                         int64_t lddw, float* dbias, void* workspace,

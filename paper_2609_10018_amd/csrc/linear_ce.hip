@@ -35,12 +35,15 @@ struct CeP {
   const float* lse;
   float2* part;   // forward: [tiles of classes][rows]
   float* picked;  // forward: the label's logit
-  const uint32_t* live;
+  const int32_t *count, *index;  // rows that are there and where they come from, or NULL: `rows`
   float* db_part;  // [tiles of rows][ld_db]
   int64_t ld_db;
-  int tiles_m, tiles_n, group;
+  int tiles_n, group;
   int label_classes;  // all classes
 };
+
+// Rows that are there, and a launch's tile of them: false for a workgroup that has none.
+__device__ __forceinline__ int64_t rows_there(const int32_t* count, int64_t rows) { return count ? *count : rows; }
 
 // The tile of workgroup v: each XCD (workgroup v runs on XCD v % 8) takes a run of tiles, in
 // groups of `group` row tiles that share the other operand's panels in its L2.
@@ -53,9 +56,19 @@ __device__ __forceinline__ void tile_of(int v, int tiles_m, int tiles_n, int gro
   tm = g * group + (in_group - tn * gm);
 }
 
+template <typename S>
+__device__ __forceinline__ bool find_tile(const CeP& p, int64_t rows, int64_t& m0, int64_t& n0, int& tm, int& tn) {
+  const int tiles_m = (int)((rows + S::BM - 1) / S::BM);
+  if ((int64_t)blockIdx.x >= (int64_t)tiles_m * p.tiles_n) return false;
+  tile_of(blockIdx.x, tiles_m, p.tiles_n, p.group, tm, tn);
+  m0 = (int64_t)tm * S::BM;
+  n0 = (int64_t)tn * S::BN;
+  return true;
+}
+
 // Logits of a tile: the accumulators start from the bias, -infinity behind the last class.
 template <typename S>
-__device__ __forceinline__ void logits(char* smem, const CeP& p, int64_t m0, int64_t n0,
+__device__ __forceinline__ void logits(char* smem, const CeP& p, int64_t rows, int64_t m0, int64_t n0,
                                        f32x16 (&acc)[S::TM][S::TN]) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c0 = (int)n0 + wave % S::WN * S::WTN + 4 * (lane >> 5);
@@ -70,7 +83,7 @@ __device__ __forceinline__ void logits(char* smem, const CeP& p, int64_t m0, int
       for (int i = 0; i < S::TM; ++i) acc[i][j][e] = b;
     }
   const Matrix w = {p.w.p + p.c0 * p.w.ld, p.w.ld};
-  tile_product<S, false, false, false>(smem, p.x, w, p.rows, p.classes, m0, n0, 0, p.dim, nullptr, acc);
+  tile_product<S, false, false, false>(smem, p.x, w, rows, p.classes, m0, n0, 0, p.dim, nullptr, acc);
 }
 
 // A reference for the exponentials of values up to m.
@@ -95,11 +108,12 @@ struct Power {
 template <typename S>
 __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_forward_kernel(CeP p) {
   __shared__ __attribute__((aligned(1024))) char smem[S::STAGES * S::kStage];
+  const int64_t rows = rows_there(p.count, p.rows);
+  int64_t m0, n0;
   int tm, tn;
-  tile_of(blockIdx.x, p.tiles_m, p.tiles_n, p.group, tm, tn);
-  const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
+  if (!find_tile<S>(p, rows, m0, n0, tm, tn)) return;
   f32x16 acc[S::TM][S::TN];
-  logits<S>(smem, p, m0, n0, acc);
+  logits<S>(smem, p, rows, m0, n0, acc);
   __syncthreads();
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave % S::kTeam / S::WN, wn = wave % S::WN, lr = lane & 31, lg = lane >> 5;
@@ -125,7 +139,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_forward_kernel(CeP 
     // The label's logit, by the one lane that holds it.
     const int64_t row = m0 + r;
     const int first = (int)n0 + wn * S::WTN;
-    const int y = row < p.rows ? p.labels[row] : -1;
+    const int y = row < rows ? p.labels[row] : -1;
     if (y >= first && y < first + S::WTN && y < p.classes)
 #pragma unroll
       for (int j = 0; j < S::TN; ++j)
@@ -134,7 +148,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_forward_kernel(CeP 
           if (y == first + j * 32 + 8 * (e >> 2) + 4 * lg + (e & 3)) p.picked[row] = acc[i][j][e];
   }
   __syncthreads();
-  for (int r = tid; r < S::BM && m0 + r < p.rows; r += S::kThreads) {
+  for (int r = tid; r < S::BM && m0 + r < rows; r += S::kThreads) {
     float2 t = red[r];
     float m = t.x;
 #pragma unroll
@@ -156,6 +170,7 @@ struct JoinP {
   const float *picked, *weight;
   const int32_t* labels;
   float *loss, *lse;
+  const int32_t *count, *index;  // rows that are there and where their results go, or NULL
   int64_t rows;
   int tiles, classes;
 };
@@ -163,7 +178,7 @@ __global__ __launch_bounds__(1024) void ce_join_kernel(JoinP p) {
   __shared__ float2 red[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t row = (int64_t)blockIdx.x * 64 + lane;
-  const bool there = row < p.rows;
+  const bool there = row < rows_there(p.count, p.rows);
   float m = -INFINITY, s = 0.0f;
   if (there)
 #pragma unroll 4
@@ -185,8 +200,9 @@ __global__ __launch_bounds__(1024) void ce_join_kernel(JoinP p) {
   const bool out = p.weight && p.weight[row] == 0.0f;
   const int y = p.labels[row];
   const bool ok = y >= 0 && y < p.classes;
-  p.loss[row] = out ? 0.0f : ok ? above + (ref - p.picked[row]) : NAN;
-  if (p.lse) p.lse[row] = out ? 0.0f : above + ref;
+  const int64_t to = p.index ? p.index[row] : row;
+  p.loss[to] = out ? 0.0f : ok ? above + (ref - p.picked[row]) : NAN;
+  if (p.lse) p.lse[to] = out ? 0.0f : above + ref;
 }
 
 // One bit a row: whether it gives the gradients anything.
@@ -200,6 +216,100 @@ __global__ __launch_bounds__(256) void ce_live_kernel(const float* weight, const
   }
   const uint64_t b = __ballot(on);
   if ((threadIdx.x & 31) == 0) live[r >> 5] = (uint32_t)(b >> (threadIdx.x & 32));
+}
+
+// Rows that count, one after another: what rows of weight 0 would cost is not spent.  A backward pass
+// leaves out rows with bad labels too.
+struct GatherP {
+  Matrix x;
+  const float *weight, *lse;
+  const int32_t* labels;
+  int64_t rows;
+  int bytes, classes;    // of a row
+  bool back;
+  int32_t *count, *first;  // first[b]: place of the first row of rows 64 b ..
+  int32_t* index;        // rows that count, in order; then what they hold:
+  char* xs;
+  int32_t* ys;
+  float *ws, *ls;
+  char* dx;              // (or NULL) zeros where a row does not count
+  int64_t lddx;
+  float *loss, *lse_out;  // forward: zeros likewise
+};
+__device__ __forceinline__ bool counts(const GatherP& p, int64_t r) {
+  if (r >= p.rows || p.weight[r] == 0.0f) return false;
+  return !p.back || (p.labels[r] >= 0 && p.labels[r] < p.classes);
+}
+constexpr int kGatherRows = 1 << 18;
+// One workgroup: a wave counts 64 rows at a time, then all counts are added up.
+__global__ __launch_bounds__(1024) void ce_count_kernel(GatherP p) {
+  constexpr int kBlocks = kGatherRows / 64, kEach = kBlocks / 1024;
+  __shared__ int32_t n[kBlocks];
+  __shared__ int32_t sums[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, blocks = (int)((p.rows + 63) / 64);
+  for (int b = wave; b < blocks; b += 64) {
+    bool on[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) on[i] = counts(p, (int64_t)(b + 16 * i) * 64 + lane);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint64_t m = __ballot(on[i]);
+      if (lane == 0 && b + 16 * i < blocks) n[b + 16 * i] = __popcll(m);
+    }
+  }
+  __syncthreads();
+  int32_t mine = 0;
+  for (int i = 0; i < kEach; ++i)
+    if (tid * kEach + i < blocks) mine += n[tid * kEach + i];
+  int32_t upto = mine;  // of this wave's threads up to this one
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int32_t v = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += v;
+  }
+  if (lane == 63) sums[wave] = upto;
+  __syncthreads();
+  int32_t at = upto - mine;
+  for (int w = 0; w < wave; ++w) at += sums[w];
+  for (int i = 0; i < kEach; ++i)
+    if (tid * kEach + i < blocks) {
+      p.first[tid * kEach + i] = at;
+      at += n[tid * kEach + i];
+    }
+  if (tid == 1023) *p.count = at;
+}
+// 16 rows a workgroup, four a wave.
+__global__ __launch_bounds__(256) void ce_gather_kernel(GatherP p) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t block = blockIdx.x >> 2;
+  const uint64_t m = __ballot(counts(p, block * 64 + lane));
+  const int first = p.first[block];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int in = (blockIdx.x & 3) * 16 + wave * 4 + i;
+    const int64_t r = block * 64 + in;
+    if (r >= p.rows) return;
+    if ((m >> in) & 1) {
+      const int64_t to = first + __popcll(m & ((1ull << in) - 1));
+      if (lane == 0) {
+        p.index[to] = (int32_t)r;
+        p.ys[to] = p.labels[r];
+        p.ws[to] = p.weight[r];
+        if (p.back) p.ls[to] = p.lse[r];
+      }
+      const char* from = p.x.p + r * p.x.ld;
+      for (int c = lane * 16; c < p.bytes; c += 1024)
+        *reinterpret_cast<u32x4*>(p.xs + to * p.bytes + c) = *reinterpret_cast<const u32x4*>(from + c);
+    } else {
+      if (p.dx)
+        for (int c = lane * 16; c < p.bytes; c += 1024)
+          *reinterpret_cast<u32x4*>(p.dx + r * p.lddx + c) = u32x4{0, 0, 0, 0};
+      if (!p.back && lane == 0) {
+        p.loss[r] = 0.0f;
+        if (p.lse_out) p.lse_out[r] = 0.0f;
+      }
+    }
+  }
 }
 
 __device__ __forceinline__ void store4(float* p, const float* v) {
@@ -242,11 +352,12 @@ template <typename S>
 __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_dz_kernel(CeP p) {
   typedef typename S::T T;
   __shared__ __attribute__((aligned(1024))) char smem[S::STAGES * S::kStage];
+  const int64_t rows = rows_there(p.count, p.rows);
+  int64_t m0, n0;
   int tm, tn;
-  tile_of(blockIdx.x, p.tiles_m, p.tiles_n, p.group, tm, tn);
-  const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
+  if (!find_tile<S>(p, rows, m0, n0, tm, tn)) return;
   f32x16 acc[S::TM][S::TN];
-  logits<S>(smem, p, m0, n0, acc);
+  logits<S>(smem, p, rows, m0, n0, acc);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave % S::kTeam / S::WN, wn = wave % S::WN, lr = lane & 31, lg = lane >> 5;
   const int first = (int)n0 + wn * S::WTN;  // of the wave's classes in the piece
@@ -258,7 +369,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_dz_kernel(CeP p) {
     const int64_t block = m0 + wm * S::WTM + i * 32, row = block + lr;
     float w = 0.0f, lse = 0.0f;
     int y = -1;
-    if (row < p.rows) {
+    if (row < rows) {
       y = p.labels[row];
       w = y >= 0 && y < p.label_classes ? (p.weight ? p.weight[row] : 1.0f) : 0.0f;
       lse = p.lse[row];
@@ -280,7 +391,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_dz_kernel(CeP p) {
         for (int e = 0; e < 16; ++e)
           if (at == j * 32 + 8 * (e >> 2) + 4 * lg + (e & 3)) acc[i][j][e] -= w;
     Out::go(mine, acc[i], lane, [&](int r, int c, const u32x4& v) {
-      if (block + r < p.rows && leads<S>())
+      if (block + r < rows && leads<S>())
         *reinterpret_cast<u32x4*>(const_cast<char*>(p.dz.p) + (block + r) * p.dz.ld +
                                   (int64_t)(first + c) * (int)sizeof(T)) = v;
     });
@@ -309,8 +420,9 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_dz_kernel(CeP p) {
   }
 }
 
-__global__ __launch_bounds__(256) void ce_db_kernel(const float* part, int tiles, int64_t ld, int64_t n, float scale,
-                                                    float* db) {
+__global__ __launch_bounds__(256) void ce_db_kernel(const float* part, const int32_t* count, int64_t rows, int side,
+                                                    int64_t ld, int64_t n, float scale, float* db) {
+  const int tiles = (int)((rows_there(count, rows) + side - 1) / side);
   for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < n; c += (int64_t)gridDim.x * 256) {
     float s = 0.0f;
 #pragma unroll 8
@@ -330,18 +442,24 @@ struct ProductP {
   bool add;         // to what sum holds
   float scale;
   const uint32_t* live;
-  int tiles_m, tiles_n, group, split;
-  int64_t chunk;    // of K
+  const int32_t *count, *index;  // rows that are there and where their results go, or NULL
+  bool rows_of_k;   // which are rows of K (else of the result)
+  int tiles_n, group, split;
 };
 template <typename S, bool TA, bool LIVE>
 __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_product_kernel(ProductP p) {
   typedef typename S::T T;
   __shared__ __attribute__((aligned(1024))) char smem[S::STAGES * S::kStage];
-  const int tiles = p.tiles_m * p.tiles_n, part = blockIdx.x / tiles;
+  const int64_t M = p.rows_of_k ? p.M : rows_there(p.count, p.M), K = p.rows_of_k ? rows_there(p.count, p.K) : p.K;
+  const int tiles_m = (int)((M + S::BM - 1) / S::BM), tiles = tiles_m * p.tiles_n;
+  if ((int64_t)blockIdx.x >= (int64_t)tiles * p.split) return;
+  const int part = blockIdx.x / tiles;
   int tm, tn;
-  tile_of(blockIdx.x - part * tiles, p.tiles_m, p.tiles_n, p.group, tm, tn);
+  tile_of(blockIdx.x - part * tiles, tiles_m, p.tiles_n, p.group, tm, tn);
   const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
-  const int64_t k0 = part * p.chunk, k1 = min(p.K, k0 + p.chunk);
+  // Parts of whole steps; the last ones may have fewer, or none.
+  const int64_t chunk = (K + (int64_t)p.split * S::kK - 1) / ((int64_t)p.split * S::kK) * S::kK;
+  const int64_t k0 = part * chunk, k1 = min(K, k0 + chunk);
   f32x16 acc[S::TM][S::TN];
 #pragma unroll
   for (int i = 0; i < S::TM; ++i)
@@ -349,7 +467,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_product_kernel(Prod
     for (int j = 0; j < S::TN; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
-  tile_product<S, TA, true, LIVE>(smem, p.a, p.b, p.M, p.N, m0, n0, k0, k1, p.live, acc);
+  tile_product<S, TA, true, LIVE>(smem, p.a, p.b, M, p.N, m0, n0, k0, k1, p.live, acc);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t r0 = m0 + wave % S::kTeam / S::WN * S::WTM, c0 = n0 + wave % S::WN * S::WTN;
   __syncthreads();  // the tiles have been read
@@ -359,7 +477,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_product_kernel(Prod
     if (p.sum) {
       typedef RowsOut<S, float> Out;
       Out::go(smem + wave * Out::kWave, acc[i], lane, [&](int r, int c, const u32x4& v) {
-        if (block + r >= p.M || c0 + c >= p.N || !leads<S>()) return;
+        if (block + r >= M || c0 + c >= p.N || !leads<S>()) return;
         f32x4* at = reinterpret_cast<f32x4*>(p.sum + (part * p.M + block + r) * p.ld_sum + c0 + c);
         f32x4 f = __builtin_bit_cast(f32x4, v);
         if (p.add) f += *at;
@@ -372,8 +490,9 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_product_kernel(Prod
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[i][j][e] *= p.scale;
       Out::go(smem + wave * Out::kWave, acc[i], lane, [&](int r, int c, const u32x4& v) {
-        if (block + r < p.M && c0 + c < p.N && leads<S>())
-          *reinterpret_cast<u32x4*>(p.out + (block + r) * p.ldo + (c0 + c) * (int)sizeof(T)) = v;
+        if (block + r >= M || c0 + c >= p.N || !leads<S>()) return;
+        const int64_t to = p.index ? p.index[block + r] : block + r;
+        *reinterpret_cast<u32x4*>(p.out + to * p.ldo + (c0 + c) * (int)sizeof(T)) = v;
       });
     }
   }
@@ -382,9 +501,10 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_product_kernel(Prod
 // dx = s times the sum of the parts.
 template <typename T>
 __global__ __launch_bounds__(256) void ce_sum_kernel(const float* sum, int split, int64_t M, int64_t N, float scale,
-                                                     char* out, int64_t ldo) {
-  const int64_t quads = N / 4;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < M * quads; i += (int64_t)gridDim.x * 256) {
+                                                     char* out, int64_t ldo, const int32_t* count,
+                                                     const int32_t* index) {
+  const int64_t quads = N / 4, rows = rows_there(count, M);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * quads; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / quads, c = (i - r * quads) * 4;
     float v[4] = {};
     for (int s = 0; s < split; ++s) {
@@ -394,7 +514,7 @@ __global__ __launch_bounds__(256) void ce_sum_kernel(const float* sum, int split
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] *= scale;
-    store4(reinterpret_cast<T*>(out + r * ldo) + c, v);
+    store4(reinterpret_cast<T*>(out + (index ? index[r] : r) * ldo) + c, v);
   }
 }
 
@@ -525,8 +645,36 @@ int64_t piece_of(const elasto_linear_ce_t& d, int es) {
   return std::min(up(d.classes, 256), std::max<int64_t>(2048, fit));
 }
 
+// Rows that count are taken together where that costs little against what it may save (two launches and a
+// copy of x: 11 us for 4096 x 2048, against 5.8 ms of gradients at 131072 classes, of which a fifth of
+// the rows left out now saves a fifth).  Below some 40 us of products the launches alone cost as much.
+bool gathers(const elasto_linear_ce_t& d) {
+  const double flops = 2.0 * (double)d.rows * d.dim * d.classes * (d.dtype == ELASTO_BF16 ? 1.0 : 8.0);
+  return d.rows >= 64 && d.rows <= kGatherRows && flops > 4e10;
+}
+struct GatherLayout {
+  int64_t count, first, index, ys, ws, ls, xs, bytes;
+};
+GatherLayout gather_layout(const elasto_linear_ce_t& d) {
+  GatherLayout l = {};
+  if (!gathers(d)) return l;
+  auto take = [&](int64_t bytes) {
+    const int64_t at = l.bytes;
+    l.bytes += up(bytes, 256);
+    return at;
+  };
+  l.count = take(4);
+  l.first = take((d.rows + 63) / 64 * 4);
+  l.index = take(d.rows * 4);
+  l.ys = take(d.rows * 4);
+  l.ws = take(d.rows * 4);
+  l.ls = take(d.rows * 4);
+  l.xs = take(d.rows * d.dim * (d.dtype == ELASTO_BF16 ? 2 : 4));
+  return l;
+}
+
 struct BackLayout {
-  int64_t live = 0, dz = 0, db = 0, sum = 0, wsum = 0, total = 0;
+  int64_t gather = 0, live = 0, dz = 0, db = 0, sum = 0, wsum = 0, total = 0;
   int64_t piece = 0;
   Way x = {}, w = {};     // of dx and of dW
   bool x_summed = false;         // dx goes through fp32 sums
@@ -544,6 +692,7 @@ BackLayout backward_layout(const elasto_linear_ce_t& d) {
     l.total += up(bytes, 256);
     return at;
   };
+  l.gather = take(gather_layout(d).bytes);
   l.live = take(up(d.rows, 256) / 8);
   l.dz = take(d.rows * l.piece * es);
   l.db = take(tiles(d.rows, 32) * l.piece * 4);
@@ -556,7 +705,7 @@ Way forward_way(const elasto_linear_ce_t& d) {
   return way_of(d.rows, d.classes, d.dim, d.dtype == ELASTO_BF16 ? 2 : 4, false);
 }
 int64_t forward_bytes(const elasto_linear_ce_t& d) {
-  return up(tiles(d.classes, forward_way(d).cols) * d.rows * 8, 256) + up(d.rows * 4, 256);
+  return up(tiles(d.classes, forward_way(d).cols) * d.rows * 8, 256) + up(d.rows * 4, 256) + gather_layout(d).bytes;
 }
 
 struct Args {
@@ -625,22 +774,54 @@ CeP params(const Args& a) {
   return p;
 }
 
+// Takes the rows that count together in ws; p then stands for them.  False: the call's own rows are used.
+bool gather(const Args& a, CeP* p, GatherP g, char* ws, hipStream_t s) {
+  if (!a.d.row_weight || !gathers(a.d)) return false;
+  const GatherLayout l = gather_layout(a.d);
+  g.x = a.x;
+  g.weight = a.d.row_weight;
+  g.labels = a.d.labels;
+  g.rows = a.d.rows;
+  g.bytes = a.d.dim * a.es;
+  g.classes = a.d.classes;
+  g.count = reinterpret_cast<int32_t*>(ws + l.count);
+  g.first = reinterpret_cast<int32_t*>(ws + l.first);
+  g.index = reinterpret_cast<int32_t*>(ws + l.index);
+  g.ys = reinterpret_cast<int32_t*>(ws + l.ys);
+  g.ws = reinterpret_cast<float*>(ws + l.ws);
+  g.ls = reinterpret_cast<float*>(ws + l.ls);
+  g.xs = ws + l.xs;
+  hipLaunchKernelGGL(ce_count_kernel, dim3(1), dim3(1024), 0, s, g);
+  hipLaunchKernelGGL(ce_gather_kernel, dim3((unsigned)((g.rows + 63) / 64 * 4)), dim3(256), 0, s, g);
+  p->x = Matrix{g.xs, g.bytes};
+  p->labels = g.ys;
+  p->weight = g.ws;
+  p->lse = g.ls;
+  p->count = g.count;
+  p->index = g.index;
+  return true;
+}
+
 template <typename T>
 hipError_t forward(const Args& a, float* loss, float* lse, char* ws, hipStream_t s) {
   CeP p = params(a);
   const Way way = forward_way(a.d);
-  const int64_t n = tiles(a.d.classes, way.cols);
+  p.tiles_n = (int)tiles(a.d.classes, way.cols);
+  const int64_t parts = up((int64_t)p.tiles_n * a.d.rows * 8, 256);
   p.part = reinterpret_cast<float2*>(ws);
-  p.picked = reinterpret_cast<float*>(ws + up(n * a.d.rows * 8, 256));
+  p.picked = reinterpret_cast<float*>(ws + parts);
+  GatherP g = {};
+  g.loss = loss;
+  g.lse_out = lse;
+  (void)gather(a, &p, g, ws + parts + up(a.d.rows * 4, 256), s);
   with_shape<T>(way.kind, [&](auto shape) {
     typedef decltype(shape) S;
-    p.tiles_m = (int)tiles(p.rows, S::BM);
-    p.tiles_n = (int)tiles(p.classes, S::BN);
-    hipLaunchKernelGGL((ce_forward_kernel<S>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(S::kThreads), 0, s, p);
+    hipLaunchKernelGGL((ce_forward_kernel<S>), dim3((unsigned)(tiles(p.rows, S::BM) * p.tiles_n)), dim3(S::kThreads),
+                       0, s, p);
   });
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const JoinP j = {p.part, p.picked, a.d.row_weight, a.d.labels, loss, lse, a.d.rows, p.tiles_n, a.d.classes};
+  const JoinP j = {p.part, p.picked, p.weight, p.labels, loss, lse, p.count, p.index, a.d.rows, p.tiles_n, a.d.classes};
   hipLaunchKernelGGL(ce_join_kernel, dim3((unsigned)((a.d.rows + 63) / 64)), dim3(1024), 0, s, j);
   return hipGetLastError();
 }
@@ -662,13 +843,10 @@ template <typename T, bool TA, bool LIVE>
 hipError_t product(ProductP q, Kind kind, int parts, hipStream_t s) {
   q.group = 8;
   q.split = parts;
-  // Parts of whole steps; those behind a short last piece's end have none.
-  q.chunk = up((q.K + parts - 1) / parts, 128 / (int)sizeof(T));
   with_shape<T>(kind, [&](auto shape) {
     typedef decltype(shape) S;
-    q.tiles_m = (int)tiles(q.M, S::BM);
     q.tiles_n = (int)tiles(q.N, S::BN);
-    hipLaunchKernelGGL((ce_product_kernel<S, TA, LIVE>), dim3((unsigned)(q.tiles_m * q.tiles_n * parts)),
+    hipLaunchKernelGGL((ce_product_kernel<S, TA, LIVE>), dim3((unsigned)(tiles(q.M, S::BM) * q.tiles_n * parts)),
                        dim3(S::kThreads), 0, s, q);
   });
   return hipGetLastError();
@@ -676,7 +854,7 @@ hipError_t product(ProductP q, Kind kind, int parts, hipStream_t s) {
 template <typename T>
 hipError_t sum_parts(const ProductP& q, int parts, hipStream_t s) {
   hipLaunchKernelGGL((ce_sum_kernel<T>), dim3(blocks(q.M * q.N / 4)), dim3(256), 0, s, q.sum, parts, q.M, q.N,
-                     q.scale, q.out, q.ldo);
+                     q.scale, q.out, q.ldo, q.rows_of_k ? nullptr : q.count, q.index);
   return hipGetLastError();
 }
 
@@ -693,8 +871,17 @@ hipError_t backward(const Args& a, const Grads& g, char* ws, hipStream_t s) {
   }
   const BackLayout l = backward_layout(d);
   uint32_t* live = reinterpret_cast<uint32_t*>(ws + l.live);
-  hipLaunchKernelGGL(ce_live_kernel, dim3((unsigned)((d.rows + 255) / 256)), dim3(256), 0, s, d.row_weight, d.labels,
-                     d.rows, d.classes, live);
+  CeP p = params(a);
+  p.lse = g.lse;
+  GatherP take = {};
+  take.back = true;
+  take.lse = g.lse;
+  take.dx = g.dx;
+  take.lddx = g.lddx * es;
+  const bool gathered = gather(a, &p, take, ws + l.gather, s);
+  if (!gathered && g.dw)
+    hipLaunchKernelGGL(ce_live_kernel, dim3((unsigned)((d.rows + 255) / 256)), dim3(256), 0, s, d.row_weight,
+                       d.labels, d.rows, d.classes, live);
   hipError_t e = hipGetLastError();
   ProductP x = {};
   x.scale = g.scale;
@@ -703,26 +890,28 @@ hipError_t backward(const Args& a, const Grads& g, char* ws, hipStream_t s) {
   x.out = g.dx;
   x.ldo = g.lddx * es;
   x.ld_sum = d.dim;
+  x.count = p.count;
+  x.index = p.index;
   if (l.x_summed) x.sum = reinterpret_cast<float*>(ws + l.sum);
   for (int64_t c0 = 0; c0 < d.classes && e == hipSuccess; c0 += l.piece) {
     const int64_t n = std::min<int64_t>(l.piece, d.classes - c0);
-    CeP p = params(a);
     p.c0 = c0;
     p.classes = n;
-    p.lse = g.lse;
     p.dz = Matrix{ws + l.dz, l.piece * es};
     p.ld_db = l.piece;
     p.db_part = g.db ? reinterpret_cast<float*>(ws + l.db) : nullptr;
+    int side = 0;
     with_shape<T>(way_of(d.rows, n, d.dim, es, false).kind, [&](auto shape) {
       typedef decltype(shape) S;
-      p.tiles_m = (int)tiles(p.rows, S::BM);
+      side = S::BM;
       p.tiles_n = (int)tiles(n, S::BN);
-      hipLaunchKernelGGL((ce_dz_kernel<S>), dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(S::kThreads), 0, s, p);
+      hipLaunchKernelGGL((ce_dz_kernel<S>), dim3((unsigned)(tiles(p.rows, S::BM) * p.tiles_n)), dim3(S::kThreads), 0,
+                         s, p);
     });
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (g.db) {
-      hipLaunchKernelGGL(ce_db_kernel, dim3(blocks(n)), dim3(256), 0, s, p.db_part, p.tiles_m, l.piece, n, g.scale,
-                         g.db + c0);
+      hipLaunchKernelGGL(ce_db_kernel, dim3(blocks(n)), dim3(256), 0, s, p.db_part, p.count, d.rows, side, l.piece, n,
+                         g.scale, g.db + c0);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     if (g.dx) {
@@ -736,7 +925,7 @@ hipError_t backward(const Args& a, const Grads& g, char* ws, hipStream_t s) {
       ProductP q = {};
       q.scale = g.scale;
       q.a = p.dz;
-      q.b = a.x;
+      q.b = p.x;
       q.M = n;
       q.N = d.dim;
       q.K = d.rows;
@@ -745,7 +934,10 @@ hipError_t backward(const Args& a, const Grads& g, char* ws, hipStream_t s) {
       q.ld_sum = d.dim;
       if (l.w.parts > 1) q.sum = reinterpret_cast<float*>(ws + l.wsum);
       q.live = live;
-      if ((e = product<T, true, true>(q, l.w.kind, l.w.parts, s)) != hipSuccess) return e;
+      q.count = p.count;
+      q.rows_of_k = true;
+      e = gathered ? product<T, true, false>(q, l.w.kind, l.w.parts, s) : product<T, true, true>(q, l.w.kind, l.w.parts, s);
+      if (e != hipSuccess) return e;
       if (l.w.parts > 1 && (e = sum_parts<T>(q, l.w.parts, s)) != hipSuccess) return e;
     }
   }

@@ -172,6 +172,73 @@ def test_rows_left_out_may_hold_anything(dtype):
     assert (case.backward(lse)["dx"][case.rw == 0] == 0).all()
 
 
+# Sizes at which rows of weight 0 are set aside before the products (over 4e10 operations, fp32 ones
+# counted eight times); 300000 rows are too many for it.
+GATHERED = [(BF, 1000, 512, 41003), (F32, 1000, 256, 10007), (BF, 70000, 16, 20000), (F32, 20000, 16, 8200),
+            (BF, 300000, 32, 2100)]
+
+
+@pytest.mark.parametrize("dtype,rows,dim,classes", GATHERED)
+def test_rows_are_set_aside(dtype, rows, dim, classes):
+    case = Case(dtype, rows, dim, classes, weights=True, bias=True, pad=16)
+    case.y[::7] = -1
+    ref = case.reference()
+    case.x[case.rw == 0] = math.nan
+    loss, lse = case.forward()
+    holds("loss", loss, ref["loss"])
+    holds("lse", lse, ref["lse"])
+    got = case.backward(lse)
+    for n, t in got.items():
+        holds(n, t, ref[n])
+    assert (got["dx"][(case.rw == 0) | (case.y < 0)] == 0).all()
+    again = case.backward(lse)
+    assert all(torch.equal(got[n], again[n]) for n in got)
+
+
+@pytest.mark.parametrize("share", [0.0, 0.002, 1.0])
+def test_all_or_hardly_any_rows_count(share):
+    case = Case(BF, 1000, 512, 41003, bias=True)
+    g = torch.Generator().manual_seed(3)
+    case.rw = (torch.rand(1000, generator=g) < share).float().cuda()
+    ref = case.reference()
+    loss, lse = case.forward()
+    holds("loss", loss, ref["loss"])
+    for n, t in case.backward(lse).items():
+        holds(n, t, ref[n])
+        assert share > 0 or (t == 0).all()
+    only = case.backward(lse, dx=False, dw=False)
+    assert torch.equal(only["dbias"], case.backward(lse)["dbias"])
+
+
+def test_setting_rows_aside_is_captured():
+    case = Case(BF, 1000, 512, 41003, weights=True)
+    loss, lse = torch.empty(1000, device="cuda"), torch.empty(1000, device="cuda")
+    dx, dw = torch.empty_like(case.x), torch.empty_like(case.w)
+    wf, wb = case.space(False), case.space(True)
+
+    def step():
+        ffi.op_linear_cross_entropy(case.x, case.w, case.y, loss, row_weight=case.rw, lse=lse, workspace=wf)
+        ffi.op_linear_cross_entropy_bwd(case.x, case.w, case.y, lse, dx=dx, dweight=dw, row_weight=case.rw,
+                                        workspace=wb)
+
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        step()
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        step()
+    for i in range(3):   # other rows count at each replay
+        case.rw.copy_(torch.randint(0, 2, (1000,), generator=torch.Generator().manual_seed(i)).float())
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (loss, lse, dx, dw)]
+        step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (loss, lse, dx, dw)))
+        assert int((loss == 0).sum()) >= int((case.rw == 0).sum()) > 300
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_bad_labels_make_their_loss_nan_and_nothing_else(dtype):
     case = Case(dtype, 50, 32, 70)
