@@ -446,16 +446,16 @@ struct ProductP {
   bool rows_of_k;   // which are rows of K (else of the result)
   int tiles_n, group, split;
 };
+// Workgroup `block` of the product.
 template <typename S, bool TA, bool LIVE>
-__global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_product_kernel(ProductP p) {
+__device__ __forceinline__ void product_tile(const ProductP& p, int block, char* smem) {
   typedef typename S::T T;
-  __shared__ __attribute__((aligned(1024))) char smem[S::STAGES * S::kStage];
   const int64_t M = p.rows_of_k ? p.M : rows_there(p.count, p.M), K = p.rows_of_k ? rows_there(p.count, p.K) : p.K;
   const int tiles_m = (int)((M + S::BM - 1) / S::BM), tiles = tiles_m * p.tiles_n;
-  if ((int64_t)blockIdx.x >= (int64_t)tiles * p.split) return;
-  const int part = blockIdx.x / tiles;
+  if ((int64_t)block >= (int64_t)tiles * p.split) return;
+  const int part = block / tiles;
   int tm, tn;
-  tile_of(blockIdx.x - part * tiles, tiles_m, p.tiles_n, p.group, tm, tn);
+  tile_of(block - part * tiles, tiles_m, p.tiles_n, p.group, tm, tn);
   const int64_t m0 = (int64_t)tm * S::BM, n0 = (int64_t)tn * S::BN;
   // Parts of whole steps; the last ones may have fewer, or none.
   const int64_t chunk = (K + (int64_t)p.split * S::kK - 1) / ((int64_t)p.split * S::kK) * S::kK;
@@ -498,6 +498,22 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_product_kernel(Prod
   }
 }
 
+template <typename S, bool TA, bool LIVE>
+__global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_product_kernel(ProductP p) {
+  __shared__ __attribute__((aligned(1024))) char smem[S::STAGES * S::kStage];
+  product_tile<S, TA, LIVE>(p, blockIdx.x, smem);
+}
+// dx and dW of a piece in one launch: where dx has not a whole round of workgroups, dW's take the CUs
+// that are left.  dx has the first x_blocks, a multiple of 8 (each XCD keeps its run of tiles).
+template <typename S, bool LIVE>
+__global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_products_kernel(ProductP x, ProductP w, int x_blocks) {
+  __shared__ __attribute__((aligned(1024))) char smem[S::STAGES * S::kStage];
+  if ((int)blockIdx.x < x_blocks)
+    product_tile<S, false, false>(x, blockIdx.x, smem);
+  else
+    product_tile<S, true, LIVE>(w, blockIdx.x - x_blocks, smem);
+}
+
 // dx = s times the sum of the parts.
 template <typename T>
 __global__ __launch_bounds__(256) void ce_sum_kernel(const float* sum, int split, int64_t M, int64_t N, float scale,
@@ -535,7 +551,7 @@ __global__ __launch_bounds__(256) void ce_zero_db_kernel(float* db, int64_t n) {
 // ---------------------------------------------------------------- host
 
 constexpr int64_t kMaxRows = 1 << 24, kMaxClasses = 1 << 30, kMaxDim = 1 << 20;
-constexpr int64_t kMaxTiles = 1 << 23;  // of 128 x 128, of 256 threads each: a launch holds fewer than 2^32
+constexpr int64_t kMaxTiles = 1 << 22;  // of 128 x 128: two products of 256 threads a tile; a launch holds fewer than 2^32
 
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 int64_t tiles(int64_t n, int64_t b) { return (n + b - 1) / b; }
@@ -838,22 +854,46 @@ struct Grads {
 
 unsigned blocks(int64_t n) { return (unsigned)std::min<int64_t>((n + 255) / 256, 1 << 16); }
 
-// q.out = q.scale q.a q.b^T, in `parts` parts of K where sums are given.
+// q.out = q.scale q.a q.b^T, in `split` parts of K where sums are given.
 template <typename T, bool TA, bool LIVE>
-hipError_t product(ProductP q, Kind kind, int parts, hipStream_t s) {
-  q.group = 8;
-  q.split = parts;
+hipError_t product(ProductP q, Kind kind, hipStream_t s) {
   with_shape<T>(kind, [&](auto shape) {
     typedef decltype(shape) S;
     q.tiles_n = (int)tiles(q.N, S::BN);
-    hipLaunchKernelGGL((ce_product_kernel<S, TA, LIVE>), dim3((unsigned)(tiles(q.M, S::BM) * q.tiles_n * parts)),
+    hipLaunchKernelGGL((ce_product_kernel<S, TA, LIVE>), dim3((unsigned)(tiles(q.M, S::BM) * q.tiles_n * q.split)),
                        dim3(S::kThreads), 0, s, q);
   });
   return hipGetLastError();
 }
+// dx and dW (or one of them) of a piece.  In one launch where both run in large tiles (3277 rows, 131072
+// classes of 2048: 5051 us in two, 4945) or in the smallest, whose launches count; fp32 in tiles of 128x64
+// loses by it (1000 rows, 10007 classes of 384: 220 us in two, 235).
+template <typename T, bool LIVE>
+hipError_t products(const ProductP* px, Kind kx, const ProductP* pw, Kind kw, hipStream_t s) {
+  const bool large = kx == Kind::Large && sizeof(T) == 2;
+  if (px && pw && kx == kw && (large || kx == Kind::Tiny)) {
+    ProductP x = *px, w = *pw;
+    auto go = [&](auto shape) {
+      typedef decltype(shape) S;
+      x.tiles_n = (int)tiles(x.N, S::BN);
+      w.tiles_n = (int)tiles(w.N, S::BN);
+      const int64_t nx = up(tiles(x.M, S::BM) * x.tiles_n * x.split, 8);
+      hipLaunchKernelGGL((ce_products_kernel<S, LIVE>), dim3((unsigned)(nx + tiles(w.M, S::BM) * w.tiles_n * w.split)),
+                         dim3(S::kThreads), 0, s, x, w, (int)nx);
+    };
+    if constexpr (sizeof(T) == 2)
+      if (large) go(typename ShapeOf<T, Kind::Large>::S());
+    if (!large) go(typename ShapeOf<T, Kind::Tiny>::S());
+    return hipGetLastError();
+  }
+  hipError_t e = hipSuccess;
+  if (px) e = product<T, false, false>(*px, kx, s);
+  if (pw && e == hipSuccess) e = product<T, true, LIVE>(*pw, kw, s);
+  return e;
+}
 template <typename T>
-hipError_t sum_parts(const ProductP& q, int parts, hipStream_t s) {
-  hipLaunchKernelGGL((ce_sum_kernel<T>), dim3(blocks(q.M * q.N / 4)), dim3(256), 0, s, q.sum, parts, q.M, q.N,
+hipError_t sum_parts(const ProductP& q, hipStream_t s) {
+  hipLaunchKernelGGL((ce_sum_kernel<T>), dim3(blocks(q.M * q.N / 4)), dim3(256), 0, s, q.sum, q.split, q.M, q.N,
                      q.scale, q.out, q.ldo, q.rows_of_k ? nullptr : q.count, q.index);
   return hipGetLastError();
 }
@@ -892,7 +932,21 @@ hipError_t backward(const Args& a, const Grads& g, char* ws, hipStream_t s) {
   x.ld_sum = d.dim;
   x.count = p.count;
   x.index = p.index;
+  x.group = 8;
+  x.split = l.x.parts;
   if (l.x_summed) x.sum = reinterpret_cast<float*>(ws + l.sum);
+  ProductP w = {};
+  w.scale = g.scale;
+  w.N = d.dim;
+  w.K = d.rows;
+  w.ldo = g.lddw * es;
+  w.ld_sum = d.dim;
+  w.group = 8;
+  w.split = l.w.parts;
+  if (l.w.parts > 1) w.sum = reinterpret_cast<float*>(ws + l.wsum);
+  w.live = live;
+  w.count = p.count;
+  w.rows_of_k = true;
   for (int64_t c0 = 0; c0 < d.classes && e == hipSuccess; c0 += l.piece) {
     const int64_t n = std::min<int64_t>(l.piece, d.classes - c0);
     p.c0 = c0;
@@ -914,34 +968,20 @@ hipError_t backward(const Args& a, const Grads& g, char* ws, hipStream_t s) {
                          g.scale, g.db + c0);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
-    if (g.dx) {
-      x.a = p.dz;
-      x.b = Matrix{a.w.p + c0 * a.w.ld, a.w.ld};
-      x.K = n;
-      x.add = c0 > 0;
-      if ((e = product<T, false, false>(x, l.x.kind, l.x.parts, s)) != hipSuccess) return e;
-    }
-    if (g.dw) {
-      ProductP q = {};
-      q.scale = g.scale;
-      q.a = p.dz;
-      q.b = p.x;
-      q.M = n;
-      q.N = d.dim;
-      q.K = d.rows;
-      q.out = g.dw + c0 * g.lddw * es;
-      q.ldo = g.lddw * es;
-      q.ld_sum = d.dim;
-      if (l.w.parts > 1) q.sum = reinterpret_cast<float*>(ws + l.wsum);
-      q.live = live;
-      q.count = p.count;
-      q.rows_of_k = true;
-      e = gathered ? product<T, true, false>(q, l.w.kind, l.w.parts, s) : product<T, true, true>(q, l.w.kind, l.w.parts, s);
-      if (e != hipSuccess) return e;
-      if (l.w.parts > 1 && (e = sum_parts<T>(q, l.w.parts, s)) != hipSuccess) return e;
-    }
+    x.a = p.dz;
+    x.b = Matrix{a.w.p + c0 * a.w.ld, a.w.ld};
+    x.K = n;
+    x.add = c0 > 0;
+    w.a = p.dz;
+    w.b = p.x;
+    w.M = n;
+    w.out = g.dw + c0 * g.lddw * es;
+    const ProductP *px = g.dx ? &x : nullptr, *pw = g.dw ? &w : nullptr;
+    e = gathered ? products<T, false>(px, l.x.kind, pw, l.w.kind, s) : products<T, true>(px, l.x.kind, pw, l.w.kind, s);
+    if (e != hipSuccess) return e;
+    if (g.dw && l.w.parts > 1) e = sum_parts<T>(w, s);
   }
-  if (e == hipSuccess && g.dx && l.x_summed) e = sum_parts<T>(x, l.x.parts, s);
+  if (e == hipSuccess && g.dx && l.x_summed) e = sum_parts<T>(x, s);
   return e;
 }
 
