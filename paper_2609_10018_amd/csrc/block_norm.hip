@@ -7,14 +7,19 @@
 //   dX = dx' + N_pre'(du),  dx = a dX,  dn = g (.) dX,  dy = N_post'(dn)  (or dn),
 //   dgamma = sum d v^ and dbeta = sum d over the tokens, dg = sum dX (.) n over a gate's tokens.
 //
-// A row is held in the registers of one to sixteen waves and read once; its statistics are taken in
-// the registers, about the row's mean (each wave about its own, joined by the pairwise update of
-// Chan, Golub and LeVeque), so a large mean costs no digits.  Everything between the load and the
-// store is fp32; u is taken from x' before x' is rounded.  Backward, a workgroup walks the rows of
-// one gate (or a part of them) and sums the weights' gradients of its columns in registers; the
-// parts are summed by a second kernel in a fixed order.
+// A row is held in the registers of 16 lanes to sixteen waves, eight or sixteen values a thread, and read
+// once; its statistics are taken there, of a layer norm first the mean and then what is about it, so a large
+// mean costs no digits.  Everything between the load and the store is fp32; u is taken from x' before x' is
+// rounded.  Backward, a workgroup walks the rows of one gate (or a part of them) and sums the weights'
+// gradients of its columns in registers; the parts are summed by a second kernel in a fixed order.  Rows of
+// more than 8192 leave no registers for the sums: a kernel of its own takes them, column by column, from the
+// rows and six numbers that the first one has written of each (568 rows of 8735: 558 us with the sums spilled,
+// 50; 6000 rows of 12288, fp32 beside bf16: 477, for ten passes over the rows instead of six).
 //
-// Bound by memory: forward four passes over the tokens, backward six.
+// Bound by memory: forward four passes over the tokens, backward six.  Measured on a card whose copies reach
+// 4.75 TB/s: forward, 50432 rows of 768, bf16, layer norm and gate, 62 us (5.0 TB/s); backward, 18700 rows of
+// 2048, fp32 beside bf16, norms on both sides and every weight's gradient, 161 us (4.6 TB/s).  Rows of bf16
+// under a layer norm of 2048 to 8192 columns wait for their exchanges: 1.5 to 1.9 times the floor.
 #include <math.h>
 
 #include <algorithm>
@@ -28,6 +33,7 @@ namespace {
 
 constexpr int kMaxDim = 16384;
 constexpr int kSums = 5;                   // pre gamma, pre beta, post gamma, post beta, gate
+constexpr int kStats = 6;                  // mean, r, mean(d gamma v^) r and mean(d gamma) r of x', mean and r of y
 
 struct Rows {  // strides in bytes
   char* p;
@@ -49,95 +55,181 @@ struct BlockP {
   bool gate_unit;          // a gate's sums end with the unit
   int slices;              // units of a sequence: runs of its rows
   int wanted;              // bits: the sums that are asked for
+  float* stats;            // [row][kStats] of rows whose sums a kernel of their own takes
 };
 
-// Values of a row in the registers of a thread: E of them, in runs of 8 where WIDE.
-template <int W, int CH, bool WIDE>
+// A row is held by T threads, CH runs of 8 columns each: run i of thread t begins at column (i T + t) 8.
+// Runs are loaded and stored whole, at whatever address they lie.  Where dim is no multiple of 8, the last
+// run is moved back to end with the row, and its first `skip` values, which are the run's before it, count
+// as 0 and are not stored (CUT; the other dims have kernels without it: 50432 rows of 768, 69 -> 59 us).
+template <int T, int CH, bool CUT>
 struct Place {
-  static constexpr int E = 8 * CH, T = 64 * W;
-  // Column of value e of thread t of the row's.
-  static __device__ __forceinline__ int column(int e, int t) {
-    return WIDE ? ((e >> 3) * T + t) * 8 + (e & 7) : e * T + t;
+  static constexpr int E = 8 * CH;
+  static constexpr bool kCut = CUT, kShort = CUT && T == 16;   // kShort: rows of fewer than 8
+  int dim, t, skip, cut;    // cut: the run that was moved, of the thread that has it; others: -1
+  float m[CH];              // 1 where a run is there, 0 where it is not
+  __device__ __forceinline__ Place(int dim_, int t_) : dim(dim_), t(t_), skip(-dim_ & 7), cut(-1) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      m[i] = there(i) ? 1.0f : 0.0f;
+      if (CUT && there(i) && column(i) + 8 > dim) cut = i;
+    }
+  }
+  __device__ __forceinline__ int column(int i) const { return (i * T + t) * 8; }
+  __device__ __forceinline__ int begin(int i) const { return CUT ? min(column(i), dim - 8) : column(i); }
+  __device__ __forceinline__ bool there(int i) const { return column(i) < dim; }
+  // Whether value e is one of the row's.
+  __device__ __forceinline__ bool holds(int e) const {
+    return there(e >> 3) && !(CUT && cut == (e >> 3) && (e & 7) < skip);
+  }
+  __device__ __forceinline__ void clean_run(float (&v)[E], int i) const {
+    if (CUT && cut == i)
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (e < skip) v[8 * i + e] = 0.0f;
+  }
+  // v less `less` in the columns that are there; in the others it stays 0.
+  __device__ __forceinline__ void subtract_run(float (&v)[E], float less, int i) const {
+    const float k = less * m[i];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[8 * i + e] -= k;
+    clean_run(v, i);
+  }
+  __device__ __forceinline__ void subtract(float (&v)[E], float less) const {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) subtract_run(v, less, i);
   }
 };
 
-__device__ __forceinline__ void load_run(const float* p, float* v) {
-  const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
-}
-__device__ __forceinline__ void store_run(uint16_t* p, const float* v) {
-  *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
-                                       pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
-}
-__device__ __forceinline__ void store_run(float* p, const float* v) {
-  *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-  *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
-}
-__device__ __forceinline__ float load_value(const uint16_t* p) { return bf16_to_f32(*p); }
-__device__ __forceinline__ float load_value(const float* p) { return *p; }
+typedef u32x4 __attribute__((aligned(2))) bf16_run;    // eight bf16 at any bf16's address
+typedef f32x4 __attribute__((aligned(4))) f32_run;
+
 __device__ __forceinline__ void store_value(uint16_t* p, float v) { *p = f32_to_bf16(v); }
 __device__ __forceinline__ void store_value(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_run(uint16_t* p, const float* v) {
+  *reinterpret_cast<bf16_run*>(p) = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+                                          pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+}
+__device__ __forceinline__ void store_run(float* p, const float* v) {
+  *reinterpret_cast<f32_run*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+  *reinterpret_cast<f32_run*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+}
 
-template <typename L, bool WIDE, typename T>
-__device__ __forceinline__ void load_row(const T* p, int dim, int t, float (&v)[L::E], float none = 0.0f) {
-  if constexpr (WIDE) {
+template <typename L, typename T>
+__device__ __forceinline__ void store_run(T* p, const L& l, const float (&v)[L::E], int i) {
+  if (!l.there(i)) return;
+  T* to = p + l.begin(i);
+  if (!L::kCut || l.cut != i)
+    store_run(to, v + 8 * i);
+  else
 #pragma unroll
-    for (int e = 0; e < L::E; e += 8) {
-      const int c = L::column(e, t);
+    for (int e = 1; e < 8; ++e)
+      if (e >= l.skip) store_value(to + e, v[8 * i + e]);
+}
+template <typename L, typename T>
+__device__ __forceinline__ void store_row(T* p, const L& l, const float (&v)[L::E]) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[e + i] = none;
-      if (c < dim) load_run(p + c, v + e);
+  for (int i = 0; i < L::E / 8; ++i) store_run(p, l, v, i);
+}
+
+// A row as it was loaded.  A row shorter than a run has it before its begin: it is loaded by values.
+template <typename L, typename T>
+struct Raw {
+  static constexpr bool kPacked = sizeof(T) == 2;
+  u32x4 w[kPacked ? L::E / 8 : L::E / 4];
+  __device__ __forceinline__ void load_run(const T* p, bool there, const L& l, int i) {
+    u32x4* o = w + (kPacked ? i : 2 * i);
+    o[0] = u32x4{0, 0, 0, 0};
+    if (!kPacked) o[1] = u32x4{0, 0, 0, 0};
+    if (!there || !l.there(i)) return;
+    const T* from = p + l.begin(i);
+    if (L::kShort && l.dim < 8) {
+#pragma unroll
+      for (int e = 1; e < 8; ++e)
+        if (e >= l.skip) {
+          if constexpr (kPacked)
+            o[0][e >> 1] |= (uint32_t)from[e] << (16 * (e & 1));
+          else
+            o[e >> 2][e & 3] = __float_as_uint(from[e]);
+        }
+    } else if constexpr (kPacked) {
+      o[0] = *reinterpret_cast<const bf16_run*>(from);
+    } else {
+      const f32x4 a = *reinterpret_cast<const f32_run*>(from), b = *reinterpret_cast<const f32_run*>(from + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[0][e] = __float_as_uint(a[e]), o[1][e] = __float_as_uint(b[e]);
     }
+  }
+  __device__ __forceinline__ void load(const T* p, bool there, const L& l) {
+#pragma unroll
+    for (int i = 0; i < L::E / 8; ++i) load_run(p, there, l, i);
+  }
+  __device__ __forceinline__ void get_run(float (&v)[L::E], const L& l, int i) const {
+#pragma unroll
+    for (int e = 8 * i; e < 8 * i + 8; ++e) {
+      if constexpr (kPacked)
+        v[e] = __uint_as_float((e & 1) ? (w[e >> 3][(e & 7) >> 1] & 0xffff0000u) : (w[e >> 3][(e & 7) >> 1] << 16));
+      else
+        v[e] = __uint_as_float(w[e >> 2][e & 3]);
+    }
+    l.clean_run(v, i);
+  }
+  __device__ __forceinline__ void get(float (&v)[L::E], const L& l) const {
+#pragma unroll
+    for (int i = 0; i < L::E / 8; ++i) get_run(v, l, i);
+  }
+};
+
+template <typename L>
+__device__ __forceinline__ void load_weight_run(const float* w, float none, const L& l, int i, float (&v)[L::E]) {
+  if (w) {
+    Raw<L, float> r;
+    r.load_run(w, true, l, i);
+    r.get_run(v, l, i);
   } else {
 #pragma unroll
-    for (int e = 0; e < L::E; ++e) {
-      const int c = L::column(e, t);
-      v[e] = c < dim ? load_value(p + c) : none;
-    }
+    for (int e = 0; e < 8; ++e) v[8 * i + e] = none;
   }
 }
-template <typename L, bool WIDE, typename T>
-__device__ __forceinline__ void store_row(T* p, int dim, int t, const float (&v)[L::E]) {
+template <typename L>
+__device__ __forceinline__ void load_weight(const float* w, float none, const L& l, float (&v)[L::E]) {
 #pragma unroll
-  for (int e = 0; e < L::E; e += WIDE ? 8 : 1) {
-    const int c = L::column(e, t);
-    if (c >= dim) continue;
-    if constexpr (WIDE)
-      store_run(p + c, v + e);
-    else
-      store_value(p + c, v[e]);
-  }
+  for (int i = 0; i < L::E / 8; ++i) load_weight_run(w, none, l, i, v);
 }
 
-// The sum over a wave, in all lanes: in rows of 16 by lane moves of the adder itself, then the four
+// The sum over groups of 2 to 64 lanes, in all of them: in rows of 16 by lane moves of the adder itself, then the
 // rows' sums in their order.
 template <int CTRL>
 __device__ __forceinline__ float add_moved(float v) {
   return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(
                  0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
 }
-__device__ __forceinline__ float sum_of_wave(float v) {
-  v = add_moved<0xB1>(v);   // lane ^ 1
-  v = add_moved<0x4E>(v);   // lane ^ 2
-  v = add_moved<0x141>(v);  // the other quad of eight
-  v = add_moved<0x140>(v);  // the other eight of a row
+template <int LANES>
+__device__ __forceinline__ float sum_of_lanes(float v) {
+  v = add_moved<0xB1>(v);                               // lane ^ 1
+  if constexpr (LANES > 2) v = add_moved<0x4E>(v);      // lane ^ 2
+  if constexpr (LANES > 4) v = add_moved<0x141>(v);     // the other quad of eight
+  if constexpr (LANES > 8) v = add_moved<0x140>(v);     // the other eight of a row
+  if constexpr (LANES <= 16) return v;
+  if constexpr (LANES == 32) return v + __shfl_xor(v, 16);
   auto row = [&](int r) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 16 * r)); };
   return (row(0) + row(1)) + (row(2) + row(3));
 }
 
-// Sums over a row's W waves, the waves' through LDS: two buffers in turn, so that one barrier does for
-// each exchange (who writes a buffer again has passed the barrier behind which all have read it).
+// Sums over a row's T threads, where they are several waves through LDS: two buffers in turn, so that one
+// barrier does for each exchange (who writes a buffer again has passed the barrier behind which all have read
+// it).
 constexpr int kMost = 3;  // sums of an exchange
-template <int W>
+template <int T>
 struct Exchange {
+  static constexpr int W = (T + 63) / 64;
   float* buf;  // [2][W][kMost]
   int turn = 0;
   template <int N>
   __device__ __forceinline__ void operator()(float (&v)[N], int t) {
     static_assert(N <= kMost, "room");
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = sum_of_wave(v[i]);
+    for (int i = 0; i < N; ++i) v[i] = sum_of_lanes<T < 64 ? T : 64>(v[i]);
     if constexpr (W > 1) {
       float* b = buf + turn * W * kMost;
       turn ^= 1;
@@ -146,11 +238,7 @@ struct Exchange {
         for (int i = 0; i < N; ++i) b[(t >> 6) * kMost + i] = v[i];
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        v[i] = b[i];
-#pragma unroll
-        for (int k = 1; k < W; ++k) v[i] += b[k * kMost + i];
-      }
+      for (int i = 0; i < N; ++i) v[i] = sum_of_lanes<W>(b[(t & (W - 1)) * kMost + i]);
     }
   }
 };
@@ -160,102 +248,42 @@ __device__ __forceinline__ T* at(const Rows& r, int b, int t) {
   return reinterpret_cast<T*>(r.p + b * r.sb + t * r.st);
 }
 
-// A row as it was loaded.
-template <typename L, bool WIDE, typename T>
-struct Raw {
-  static constexpr bool kPacked = WIDE && sizeof(T) == 2;
-  u32x4 w[kPacked ? L::E / 8 : 1];
-  float f[kPacked ? 1 : L::E];
-  __device__ __forceinline__ void load(const T* p, bool there, int dim, int t) {
-    if constexpr (kPacked) {
-#pragma unroll
-      for (int i = 0; i < L::E / 8; ++i) {
-        const int c = L::column(8 * i, t);
-        w[i] = u32x4{0, 0, 0, 0};
-        if (there && c < dim) w[i] = *reinterpret_cast<const u32x4*>(p + c);
-      }
-    } else if (there) {
-      load_row<L, WIDE>(p, dim, t, f);
-    } else {
-#pragma unroll
-      for (int e = 0; e < L::E; ++e) f[e] = 0.0f;
-    }
-  }
-  __device__ __forceinline__ void get(float (&v)[L::E]) const {
-#pragma unroll
-    for (int e = 0; e < L::E; ++e) {
-      if constexpr (kPacked)
-        v[e] = __uint_as_float((e & 1) ? (w[e >> 3][(e & 7) >> 1] & 0xffff0000u) : (w[e >> 3][(e & 7) >> 1] << 16));
-      else
-        v[e] = f[e];
-    }
-  }
-};
+// Whether the weights and the next row's loads stay in registers: not for rows of 1024 threads, which have
+// 128 registers.  Backward these still hold the next row's where they can.
+template <int T>
+constexpr bool kKeep = T < 1024;
+template <bool LAYER, int T, int CH>
+constexpr bool kAhead = CH == 1 && (T < 1024 || !LAYER);
+constexpr int workgroup(int T) { return T > 256 ? T : 256; }
 
-template <typename L, bool WIDE>
-__device__ __forceinline__ void load_weight(const float* w, float none, int dim, int t, float (&v)[L::E]) {
-  if (w)
-    load_row<L, WIDE>(w, dim, t, v, none);
-  else
-#pragma unroll
-    for (int e = 0; e < L::E; ++e) v[e] = none;
-}
-
-// 1 where a thread's column is there, 0 where it is not (a run of eight is there or not: dim is a multiple
-// of 8 where rows are read in runs).  What is loaded from columns that are not there is 0, so only what is
-// added to a whole row needs it.
-template <typename L, bool WIDE>
-struct There {
-  float m[WIDE ? L::E / 8 : L::E];
-  __device__ __forceinline__ There(int dim, int t) {
-#pragma unroll
-    for (int i = 0; i < (WIDE ? L::E / 8 : L::E); ++i) m[i] = L::column(WIDE ? 8 * i : i, t) < dim ? 1.0f : 0.0f;
-  }
-  // less[e] where the column is there: computed once a run.
-  __device__ __forceinline__ void from(float (&v)[L::E], float less) const {
-#pragma unroll
-    for (int i = 0; i < (WIDE ? L::E / 8 : L::E); ++i) {
-      const float k = less * m[i];
-#pragma unroll
-      for (int e = 0; e < (WIDE ? 8 : 1); ++e) v[(WIDE ? 8 : 1) * i + e] -= k;
-    }
-  }
-};
-
-// Whether the weights and the next row's loads stay in registers: not forward for rows of 16 waves (which
-// have 128 registers), nor backward.
-template <int W>
-constexpr bool kKeepForward = W < 16;
-template <int CH>
-constexpr bool kKeepBackward = CH == 1;
-
-// T: of y and u.  S: of the stream.  W waves a row; a workgroup of 256 threads holds 4 / W rows.  A group of
-// W waves takes rows in strides of the grid's, the next one's loads in flight, the weights in registers.
-template <typename T, typename S, bool LAYER, int W, int CH, bool WIDE>
-__global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_kernel(BlockP p) {
-  typedef Place<W, CH, WIDE> L;
-  constexpr int E = L::E, R = W > 4 ? 1 : 4 / W;
-  constexpr bool KEEP = kKeepForward<W>;
-  __shared__ float red[R][2 * W * kMost];
-  const int t = threadIdx.x % L::T, mine = __builtin_amdgcn_readfirstlane(threadIdx.x / L::T);
-  Exchange<W> exchange = {red[mine]};
-  const There<L, WIDE> there(p.dim, t);
+// T: of y and u.  S: of the stream.  TR threads a row; a workgroup of 256 threads holds 256 / TR rows.  Rows
+// are taken in strides of the grid's, the next one's loads in flight, the weights in registers.
+template <typename T, typename S, bool LAYER, bool CUT, int TR, int CH>
+__global__ __launch_bounds__(workgroup(TR)) void block_norm_kernel(BlockP p) {
+  typedef Place<TR, CH, CUT> L;
+  constexpr int E = L::E, R = workgroup(TR) / TR;
+  constexpr bool KEEP = kKeep<TR>;
+  __shared__ float red[R][2 * Exchange<TR>::W * kMost];
+  const int mine = TR < 64 ? threadIdx.x / TR : __builtin_amdgcn_readfirstlane(threadIdx.x / TR);
+  const L l(p.dim, threadIdx.x % TR);
+  const int t = l.t;
+  Exchange<TR> exchange = {red[mine]};
   const int rows = p.batch * p.tokens, stride = gridDim.x * R;
   float pg[E], pb[E], qg[E], qb[E], g[E];
   auto pre = [&] {
-    load_weight<L, WIDE>(p.pre_gamma, 1.0f, p.dim, t, pg);
-    if constexpr (LAYER) load_weight<L, WIDE>(p.pre_beta, 0.0f, p.dim, t, pb);
+    load_weight(p.pre_gamma, 1.0f, l, pg);
+    if constexpr (LAYER) load_weight(p.pre_beta, 0.0f, l, pb);
   };
   auto post = [&] {
-    load_weight<L, WIDE>(p.post_gamma, 1.0f, p.dim, t, qg);
-    if constexpr (LAYER) load_weight<L, WIDE>(p.post_beta, 0.0f, p.dim, t, qb);
+    load_weight(p.post_gamma, 1.0f, l, qg);
+    if constexpr (LAYER) load_weight(p.post_beta, 0.0f, l, qb);
   };
   if (KEEP && p.u.p) pre();
   if (KEEP && p.post) post();
-  if (KEEP) load_weight<L, WIDE>(p.gate, 1.0f, p.dim, t, g);  // of the first sequence, or of all
+  if (KEEP) load_weight(p.gate, 1.0f, l, g);  // of the first sequence, or of all
   int gate_of = 0;
-  Raw<L, WIDE, S> rx;
-  Raw<L, WIDE, T> ry;
+  Raw<L, S> rx;
+  Raw<L, T> ry;
   int b = 0, tok = 0;
   bool live = false;
   auto fetch = [&](int row) {
@@ -264,8 +292,8 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_kernel(BlockP
     b = (int)((unsigned)r / (unsigned)p.tokens);
     tok = r - b * p.tokens;
     if (live && p.lens) live = tok < p.lens[b];
-    rx.load(at<const S>(p.x, b, tok), live, p.dim, t);
-    if (p.has_y) ry.load(at<const T>(p.y, b, tok), live, p.dim, t);
+    rx.load(at<const S>(p.x, b, tok), live, l);
+    if (p.has_y) ry.load(at<const T>(p.y, b, tok), live, l);
   };
   // All rows of a workgroup take as many rounds: with W > 1 they meet at its barriers.
   int row = blockIdx.x * R;
@@ -273,11 +301,11 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_kernel(BlockP
   for (; row < rows; row += stride) {
     if (!KEEP) fetch(row + mine);
     float x[E], v[E];
-    rx.get(x);
+    rx.get(x, l);
     const bool now = live;
     const int nb = b, nt = tok;
     if (p.has_y) {
-      ry.get(v);
+      ry.get(v, l);
       if (KEEP && row + stride < rows) fetch(row + stride + mine);
       if (p.post) {
         if constexpr (LAYER) {
@@ -285,7 +313,7 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_kernel(BlockP
 #pragma unroll
           for (int e = 0; e < E; ++e) s[0] += v[e];
           exchange(s, t);
-          there.from(v, s[0] * p.inv_dim);
+          l.subtract(v, s[0] * p.inv_dim);
         }
         float q[1] = {0.0f};
 #pragma unroll
@@ -296,9 +324,9 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_kernel(BlockP
 #pragma unroll
         for (int e = 0; e < E; ++e) v[e] = LAYER ? fmaf(v[e] * r, qg[e], qb[e]) : v[e] * r * qg[e];
       }
-      if (!KEEP && !p.gate_ld) load_weight<L, WIDE>(p.gate, 1.0f, p.dim, t, g);
+      if (!KEEP && !p.gate_ld) load_weight(p.gate, 1.0f, l, g);
       if (p.gate_ld && (!KEEP || nb != gate_of)) {
-        load_weight<L, WIDE>(p.gate + nb * p.gate_ld, 1.0f, p.dim, t, g);
+        load_weight(p.gate + nb * p.gate_ld, 1.0f, l, g);
         gate_of = nb;
       }
 #pragma unroll
@@ -308,14 +336,14 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_kernel(BlockP
 #pragma unroll
       for (int e = 0; e < E; ++e) x[e] *= p.a;
     }
-    if (now && p.x_out.p) store_row<L, WIDE>(at<S>(p.x_out, nb, nt), p.dim, t, x);
+    if (now && p.x_out.p) store_row(at<S>(p.x_out, nb, nt), l, x);
     if (!p.u.p) continue;
     if constexpr (LAYER) {
       float s[1] = {0.0f};
 #pragma unroll
       for (int e = 0; e < E; ++e) s[0] += x[e];
       exchange(s, t);
-      there.from(x, s[0] * p.inv_dim);
+      l.subtract(x, s[0] * p.inv_dim);
     }
     float q[1] = {0.0f};
 #pragma unroll
@@ -325,22 +353,23 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256) void block_norm_kernel(BlockP
     if (!KEEP) pre();
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = LAYER ? fmaf(x[e] * r, pg[e], pb[e]) : x[e] * r * pg[e];
-    if (now) store_row<L, WIDE>(at<T>(p.u, nb, nt), p.dim, t, x);
+    if (now) store_row(at<T>(p.u, nb, nt), l, x);
   }
 }
 
 // Three exchanges a row (RMS: two): sums for the means; about them, with what both norms need that the
 // gradient of x' does not wait for; and the norm behind the block's.
-template <typename T, typename S, bool LAYER, int W, int CH, bool WIDE>
-__global__ __launch_bounds__(W > 4 ? 64 * W : 256, W > 4 ? 1 : 3) void block_norm_bwd_kernel(BlockP p) {
-  typedef Place<W, CH, WIDE> L;
-  constexpr int E = L::E, R = W > 4 ? 1 : 4 / W;
-  constexpr bool KEEP = kKeepBackward<CH>;
-  __shared__ float red[R][2 * W * kMost];
-  __shared__ float sums[R > 1 ? (R - 1) * L::T : 1];
-  const int t = threadIdx.x % L::T, mine = __builtin_amdgcn_readfirstlane(threadIdx.x / L::T);
-  Exchange<W> exchange = {red[mine]};
-  const There<L, WIDE> there(p.dim, t);
+template <typename T, typename S, bool LAYER, bool CUT, int TR, int CH>
+__global__ __launch_bounds__(workgroup(TR), TR > 256 ? 1 : 3) void block_norm_bwd_kernel(BlockP p) {
+  typedef Place<TR, CH, CUT> L;
+  constexpr int E = L::E, R = workgroup(TR) / TR;
+  constexpr bool KEEP = kKeep<TR>, AHEAD = kAhead<LAYER, TR, CH>, SUMS = CH == 1;
+  __shared__ float red[R][2 * Exchange<TR>::W * kMost];
+  __shared__ float sums[R > 1 ? (R - 1) * TR : 1];
+  const int mine = TR < 64 ? threadIdx.x / TR : __builtin_amdgcn_readfirstlane(threadIdx.x / TR);
+  const L l(p.dim, threadIdx.x % TR);
+  const int t = l.t;
+  Exchange<TR> exchange = {red[mine]};
   float pg[E], pb[E], qg[E], qb[E], gg[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) pg[e] = pb[e] = qg[e] = qb[e] = gg[e] = 0.0f;
@@ -351,154 +380,274 @@ __global__ __launch_bounds__(W > 4 ? 64 * W : 256, W > 4 ? 1 : 3) void block_nor
       float s = v[e];
       if constexpr (R > 1) {
         __syncthreads();
-        if (mine > 0) sums[(mine - 1) * L::T + t] = s;
+        if (mine > 0) sums[(mine - 1) * TR + t] = s;
         __syncthreads();
         if (mine == 0)
 #pragma unroll
-          for (int k = 0; k < R - 1; ++k) s += sums[k * L::T + t];
+          for (int k = 0; k < R - 1; ++k) s += sums[k * TR + t];
       }
-      const int c = L::column(e, t);
-      if (mine == 0 && c < p.dim) out[c] = s;
+      if (mine == 0 && l.holds(e)) out[l.begin(e >> 3) + (e & 7)] = s;
     }
   };
   float w_pre[E], w_post[E], b_post[E], w_gate[E];
-  auto post = [&] {
-    load_weight<L, WIDE>(p.post_gamma, 1.0f, p.dim, t, w_post);
-    if constexpr (LAYER) load_weight<L, WIDE>(p.post_beta, 0.0f, p.dim, t, b_post);
-  };
   if (KEEP) {
-    load_weight<L, WIDE>(p.pre_gamma, 1.0f, p.dim, t, w_pre);
-    if (p.post) post();
-    load_weight<L, WIDE>(p.gate, 1.0f, p.dim, t, w_gate);
+    load_weight(p.pre_gamma, 1.0f, l, w_pre);
+    if (p.post) load_weight(p.post_gamma, 1.0f, l, w_post);
+    if (LAYER && p.post) load_weight(p.post_beta, 0.0f, l, b_post);
+    load_weight(p.gate, 1.0f, l, w_gate);
   }
+  // Run by run.  Where registers are short, what is loaded behind a mark is not loaded ahead of it.
+  auto hold_order = [] {
+    if constexpr (!KEEP) __builtin_amdgcn_sched_barrier(0);
+  };
+  auto by_runs = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      f(i);
+      hold_order();
+    }
+  };
   const int units = p.batch * p.slices;
   for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
     const int b = unit / p.slices, slice = unit - b * p.slices;
     const int n = p.lens ? max(0, min(p.tokens, p.lens[b])) : p.tokens;
     const int share = (n + p.slices - 1) / p.slices, first = slice * share, last = min(n, first + share);
-    if (KEEP && p.gate_ld) load_weight<L, WIDE>(p.gate + b * p.gate_ld, 0.0f, p.dim, t, w_gate);
-    Raw<L, WIDE, S> rx, rd;
-    Raw<L, WIDE, T> ru, ry;
-    auto fetch = [&](int tok) {
-      const bool live = tok < last;
+    if (KEEP && p.gate_ld) load_weight(p.gate + b * p.gate_ld, 1.0f, l, w_gate);
+    const float* gate = p.gate ? p.gate + b * p.gate_ld : nullptr;
+    Raw<L, S> rx, rd;
+    Raw<L, T> ru, ry;
+    auto load_run = [&](int tok, bool live, int i) {
       const int k = live ? tok : 0;
       if (p.du.p) {
-        ru.load(at<const T>(p.du, b, k), live, p.dim, t);
-        rx.load(at<const S>(p.x_out, b, k), live, p.dim, t);
+        ru.load_run(at<const T>(p.du, b, k), live, l, i);
+        rx.load_run(at<const S>(p.x_out, b, k), live, l, i);
       }
-      if (p.has_y) ry.load(at<const T>(p.y, b, k), live, p.dim, t);
-      if (p.dx_out.p) rd.load(at<const S>(p.dx_out, b, k), live, p.dim, t);
+      if (p.has_y) ry.load_run(at<const T>(p.y, b, k), live, l, i);
+      if (AHEAD && p.dx_out.p) rd.load_run(at<const S>(p.dx_out, b, k), live, l, i);
     };
-    if (KEEP && first < last) fetch(first + mine);
+    auto load = [&](int tok) {
+#pragma unroll
+      for (int i = 0; i < CH; ++i) load_run(tok, tok < last, i);
+    };
+    if (AHEAD && first < last) load(first + mine);
     // Every row of a workgroup takes as many rounds: they meet at its barriers.
     for (int k = first; k < last; k += R) {
       const int tok = k + mine;
       const bool live = tok < last;
-      if (!KEEP) {
-        fetch(tok);
-        load_weight<L, WIDE>(p.pre_gamma, 1.0f, p.dim, t, w_pre);
-      }
+      if (!AHEAD) load(tok);
       float d[E], x[E], v[E], s[3] = {0.0f, 0.0f, 0.0f};
-      if (p.du.p) {
-        ru.get(d);
-        rx.get(x);
-        if constexpr (LAYER)
+      auto get = [&](int i) {
 #pragma unroll
-          for (int e = 0; e < E; ++e) pb[e] += d[e];
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) d[e] = x[e] = 0.0f;
-      }
-      if (p.has_y)
-        ry.get(v);
-      else
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = 0.0f;
-      float c = 0.0f;
-      if constexpr (LAYER) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          s[0] += x[e];
-          s[1] += v[e];
-          s[2] = fmaf(d[e], w_pre[e], s[2]);
+        for (int e = 8 * i; e < 8 * i + 8; ++e) d[e] = x[e] = v[e] = 0.0f;
+        if (p.du.p) {
+          ru.get_run(d, l, i);
+          rx.get_run(x, l, i);
         }
+        if (p.has_y) ry.get_run(v, l, i);
+      };
+      float mean_x = 0.0f, mean_y = 0.0f, c = 0.0f;
+      auto center = [&](int i) {
+        if constexpr (LAYER) {
+          if (p.du.p) l.subtract_run(x, mean_x, i);
+          if (p.post) l.subtract_run(v, mean_y, i);
+        }
+      };
+      if constexpr (LAYER) {
+        by_runs([&](int i) {
+          get(i);
+          hold_order();
+          if (!KEEP) load_weight_run(p.pre_gamma, 1.0f, l, i, w_pre);
+#pragma unroll
+          for (int e = 8 * i; e < 8 * i + 8; ++e) {
+            s[0] += x[e];
+            s[1] += v[e];
+            s[2] = fmaf(d[e], w_pre[e], s[2]);
+          }
+        });
         exchange(s, t);
-        if (p.du.p) there.from(x, s[0] * p.inv_dim);
-        if (p.post) there.from(v, s[1] * p.inv_dim);
+        mean_x = s[0] * p.inv_dim;
+        mean_y = s[1] * p.inv_dim;
         c = s[2] * p.inv_dim;
         s[0] = s[1] = s[2] = 0.0f;
       }
+      by_runs([&](int i) {
+        if constexpr (!LAYER) get(i);
+        if (!KEEP) load_weight_run(p.pre_gamma, 1.0f, l, i, w_pre);
+        center(i);
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        s[0] = fmaf(x[e], x[e], s[0]);
-        s[1] = fmaf(v[e], v[e], s[1]);
-        s[2] = fmaf(d[e] * w_pre[e], x[e], s[2]);
-      }
-      exchange(s, t);
-      const float r = 1.0f / sqrtf(fmaf(s[0], p.inv_dim, p.eps));
-      const float ry1 = p.post ? 1.0f / sqrtf(fmaf(s[1], p.inv_dim, p.eps)) : 1.0f;
-      if (p.du.p) {
-        const float a = r * s[2] * p.inv_dim;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float xn = x[e] * r;
-          pg[e] = fmaf(d[e], xn, pg[e]);
-          d[e] = r * fmaf(d[e], w_pre[e], -xn * a);
+        for (int e = 8 * i; e < 8 * i + 8; ++e) {
+          s[0] = fmaf(x[e], x[e], s[0]);
+          s[1] = fmaf(v[e], v[e], s[1]);
+          s[2] = fmaf(d[e] * w_pre[e], x[e], s[2]);
         }
-        if constexpr (LAYER) there.from(d, r * c);
-      }
-      if (p.dx_out.p) {
-        rd.get(x);
-#pragma unroll
-        for (int e = 0; e < E; ++e) d[e] += x[e];
-      }
-      if (KEEP && k + R < last) fetch(tok + R);
-      if (p.dx.p && live) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = p.a * d[e];
-        store_row<L, WIDE>(at<S>(p.dx, b, tok), p.dim, t, x);
-      }
-      if (!p.has_y) continue;
-      if (!KEEP) {
-        if (p.post) post();
-        load_weight<L, WIDE>(p.gate ? p.gate + b * p.gate_ld : nullptr, 1.0f, p.dim, t, w_gate);
-      }
+      });
+      exchange(s, t);
+      const float r = 1.0f / sqrtf(fmaf(s[0], p.inv_dim, p.eps)), a = r * s[2] * p.inv_dim;
+      const float r_post = p.post ? 1.0f / sqrtf(fmaf(s[1], p.inv_dim, p.eps)) : 1.0f;
+      if constexpr (!SUMS)
+        if (p.stats && t == 0) {
+          float* o = p.stats + ((int64_t)b * p.tokens + tok) * kStats;
+          o[0] = mean_x, o[1] = r, o[2] = a, o[3] = r * c, o[4] = mean_y, o[5] = r_post;
+        }
       float q[2] = {0.0f, 0.0f};
+      by_runs([&](int i) {
+        if (!KEEP) load_weight_run(p.pre_gamma, 1.0f, l, i, w_pre);   // again: not held over the exchange
+        if (p.du.p) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        v[e] *= ry1;
-        const float n = p.post ? (LAYER ? fmaf(v[e], w_post[e], b_post[e]) : v[e] * w_post[e]) : v[e];
-        gg[e] = fmaf(d[e], n, gg[e]);
-        if (p.gate) d[e] *= w_gate[e];
-        if (p.post) {
-          qg[e] = fmaf(d[e], v[e], qg[e]);
-          if constexpr (LAYER) qb[e] += d[e];
+          for (int e = 8 * i; e < 8 * i + 8; ++e) {
+            const float xn = x[e] * r;
+            if constexpr (SUMS && LAYER) pb[e] += d[e];
+            if constexpr (SUMS) pg[e] = fmaf(d[e], xn, pg[e]);
+            d[e] = r * fmaf(d[e], w_pre[e], -xn * a);
+          }
+          if constexpr (LAYER) l.subtract_run(d, r * c, i);
+        }
+        if (p.dx_out.p) {
+          if (!AHEAD) rd.load_run(at<const S>(p.dx_out, b, live ? tok : 0), live, l, i);
+          rd.get_run(x, l, i);
+#pragma unroll
+          for (int e = 8 * i; e < 8 * i + 8; ++e) d[e] += x[e];
+        }
+        if (AHEAD && k + R < last) load(tok + R);
+        if (p.dx.p && live) {
+#pragma unroll
+          for (int e = 8 * i; e < 8 * i + 8; ++e) x[e] = p.a * d[e];
+          store_run(at<S>(p.dx, b, tok), l, x, i);
+        }
+        if (!p.has_y) return;
+        hold_order();
+        if (!KEEP) load_weight_run(gate, 1.0f, l, i, w_gate);
+        if (!p.post) {
+#pragma unroll
+          for (int e = 8 * i; e < 8 * i + 8; ++e) {
+            if constexpr (SUMS) gg[e] = fmaf(d[e], v[e], gg[e]);
+            d[e] *= w_gate[e];
+          }
+          return;
+        }
+        hold_order();
+        if (!KEEP) load_weight_run(p.post_gamma, 1.0f, l, i, w_post);
+        if (!KEEP && LAYER && SUMS) load_weight_run(p.post_beta, 0.0f, l, i, b_post);
+#pragma unroll
+        for (int e = 8 * i; e < 8 * i + 8; ++e) {
+          v[e] *= r_post;
+          if constexpr (SUMS) gg[e] = fmaf(d[e], LAYER ? fmaf(v[e], w_post[e], b_post[e]) : v[e] * w_post[e], gg[e]);
+          d[e] *= w_gate[e];
+          if constexpr (SUMS) qg[e] = fmaf(d[e], v[e], qg[e]);
+          if constexpr (SUMS && LAYER) qb[e] += d[e];
           d[e] *= w_post[e];
           q[0] = fmaf(d[e], v[e], q[0]);
           if constexpr (LAYER) q[1] += d[e];
         }
-      }
+      });
+      if (!p.has_y) continue;
+      float am = 0.0f, m = 0.0f;
       if (p.post) {
         exchange(q, t);
-        const float a = q[0] * p.inv_dim, m = LAYER ? q[1] * p.inv_dim : 0.0f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) d[e] = ry1 * (d[e] - fmaf(v[e], a, m));
+        am = q[0] * p.inv_dim;
+        m = LAYER ? q[1] * p.inv_dim : 0.0f;
       }
-      if (p.dy.p && live) store_row<L, WIDE>(at<T>(p.dy, b, tok), p.dim, t, d);
+      by_runs([&](int i) {
+        if (p.post) {
+#pragma unroll
+          for (int e = 8 * i; e < 8 * i + 8; ++e) d[e] = r_post * (d[e] - fmaf(v[e], am, m));
+        }
+        if (p.dy.p && live) store_run(at<T>(p.dy, b, tok), l, d, i);
+      });
     }
-    if (p.gate_unit) {
+    if (SUMS && p.gate_unit) {
       flush(gg, p.gate_part + (int64_t)unit * p.dim);
 #pragma unroll
       for (int e = 0; e < E; ++e) gg[e] = 0.0f;
     }
   }
-  if (!p.part) return;
+  if (!SUMS || !p.part) return;
   float* part = p.part + (int64_t)blockIdx.x * 4 * p.dim;
   if (p.wanted & 1) flush(pg, part);
   if (p.wanted & 2) flush(pb, part + p.dim);
   if (p.wanted & 4) flush(qg, part + 2 * p.dim);
   if (p.wanted & 8) flush(qb, part + 3 * p.dim);
   if ((p.wanted & 16) && !p.gate_unit) flush(gg, p.gate_part + (int64_t)blockIdx.x * p.dim);
+}
+
+// The sums of the weights' gradients of rows too long to have them in registers beside the row, from the rows
+// and what the kernel above wrote of each: a thread has eight columns, a wave the rows of its units.
+template <typename T, typename S, bool LAYER, bool CUT>
+__global__ __launch_bounds__(64) void block_columns_kernel(BlockP p) {
+  typedef Place<64, 1, CUT> L;
+  const L l(p.dim, blockIdx.y * 64 + threadIdx.x);
+  float pg[8], pb[8], qg[8], qb[8], gg[8], w_pre[8], w_post[8], b_post[8], w_gate[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) pg[e] = pb[e] = qg[e] = qb[e] = gg[e] = 0.0f;
+  load_weight(p.pre_gamma, 1.0f, l, w_pre);
+  load_weight(p.post_gamma, 1.0f, l, w_post);
+  load_weight(p.post_beta, 0.0f, l, b_post);
+  load_weight(p.gate, 1.0f, l, w_gate);
+  auto put = [&](const float (&v)[8], float* out) {
+    if (l.there(0)) store_run(out, l, v, 0);
+  };
+  const bool rest = p.has_y && (p.wanted & 28);   // sums that need y and the gradient of x'
+  const int units = p.batch * p.slices;
+  for (int unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int b = unit / p.slices, slice = unit - b * p.slices;
+    const int n = p.lens ? max(0, min(p.tokens, p.lens[b])) : p.tokens;
+    const int share = (n + p.slices - 1) / p.slices, first = slice * share, last = min(n, first + share);
+    if (p.gate_ld) load_weight(p.gate + b * p.gate_ld, 1.0f, l, w_gate);
+#pragma unroll 2
+    for (int tok = first; tok < last; ++tok) {
+      const float* o = p.stats + ((int64_t)b * p.tokens + tok) * kStats;
+      float d[8] = {}, x[8];
+      if (p.du.p) {
+        Raw<L, T> ru;
+        Raw<L, S> rx;
+        ru.load(at<const T>(p.du, b, tok), true, l);
+        rx.load(at<const S>(p.x_out, b, tok), true, l);
+        ru.get(d, l);
+        rx.get(x, l);
+        if constexpr (LAYER) l.subtract(x, o[0]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float xn = x[e] * o[1];
+          if constexpr (LAYER) pb[e] += d[e];
+          pg[e] = fmaf(d[e], xn, pg[e]);
+          d[e] = o[1] * fmaf(d[e], w_pre[e], -xn * o[2]);
+        }
+        if constexpr (LAYER) l.subtract(d, o[3]);
+      }
+      if (!rest) continue;
+      float v[8];
+      Raw<L, T> ry;
+      ry.load(at<const T>(p.y, b, tok), true, l);
+      if (p.dx_out.p) {
+        Raw<L, S> rd;
+        rd.load(at<const S>(p.dx_out, b, tok), true, l);
+        rd.get(x, l);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[e] += x[e];
+      }
+      ry.get(v, l);
+      if (LAYER && p.post) l.subtract(v, o[4]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[e] *= o[5];
+        gg[e] = fmaf(d[e], fmaf(v[e], w_post[e], b_post[e]), gg[e]);
+        d[e] *= w_gate[e];
+        qg[e] = fmaf(d[e], v[e], qg[e]);
+        if constexpr (LAYER) qb[e] += d[e];
+      }
+    }
+    if (p.gate_unit) {
+      put(gg, p.gate_part + (int64_t)unit * p.dim);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) gg[e] = 0.0f;
+    }
+  }
+  float* part = p.part + (int64_t)blockIdx.x * 4 * p.dim;
+  if (p.wanted & 1) put(pg, part);
+  if (p.wanted & 2) put(pb, part + p.dim);
+  if (p.wanted & 4) put(qg, part + 2 * p.dim);
+  if (p.wanted & 8) put(qb, part + 3 * p.dim);
+  if ((p.wanted & 16) && !p.gate_unit) put(gg, p.gate_part + (int64_t)blockIdx.x * p.dim);
 }
 
 // Column sums of the parts, 64 columns a workgroup, 16 slices of the parts.
@@ -537,80 +686,91 @@ __global__ __launch_bounds__(256) void block_zero_kernel(float* out, int64_t n) 
 
 // ---------------------------------------------------------------- host
 
-// Waves of a row and runs of eight a thread.
+// Threads of a row and runs of eight a thread: as few as hold the row, so that short rows share a wave (281536
+// rows of 40: a wave each 119 us, four a wave 32).
 struct Width {
-  int waves, runs;
+  int threads, runs;
 };
 // Forward: rows of up to 1024 in one wave, which needs no barrier.
 Width forward_width(int dim) {
-  if (dim <= 512) return {1, 1};
-  if (dim <= 1024) return {1, 2};
-  if (dim <= 2048) return {2, 2};
-  if (dim <= 4096) return {4, 2};
-  if (dim <= 8192) return {8, 2};
-  return {16, 2};
+  if (dim <= 128) return {16, 1};
+  if (dim <= 256) return {32, 1};
+  if (dim <= 512) return {64, 1};
+  if (dim <= 1024) return {64, 2};
+  if (dim <= 2048) return {128, 2};
+  if (dim <= 4096) return {256, 2};
+  if (dim <= 8192) return {512, 2};
+  return {1024, 2};
 }
 // Backward: eight values a thread, so that the sums, the weights and the next row's loads stay in
 // registers.
 Width backward_width(int dim) {
-  if (dim <= 512) return {1, 1};
-  if (dim <= 1024) return {2, 1};
-  if (dim <= 2048) return {4, 1};
-  if (dim <= 4096) return {8, 1};
-  if (dim <= 8192) return {8, 2};
-  return {8, 4};
+  if (dim <= 128) return {16, 1};
+  if (dim <= 256) return {32, 1};
+  if (dim <= 512) return {64, 1};
+  if (dim <= 1024) return {128, 1};
+  if (dim <= 2048) return {256, 1};
+  if (dim <= 4096) return {512, 1};
+  if (dim <= 8192) return {1024, 1};
+  return {1024, 2};
 }
 // Workgroups of a forward launch: what the GPU holds, several times over for rows of one wave.
 int forward_blocks(int dim) { return dim <= 4096 ? 256 * 8 : 256 * 4; }
 // Backward: the workgroups that the GPU holds, three a CU of rows of up to 2048 (kept to a third of its
-// registers: 243 -> 166 us where they took 190 and two ran; 12608 rows of 768, layer norm, 192 -> 109), and the
+// registers: 243 -> 166 us where they took 190 and two ran; 50432 rows of 768, layer norm, 192 -> 109), and the
 // units that they share out (below; with as many as workgroups 175 us, with four times as many 175).
-int grad_blocks(Width w) { return w.waves <= 4 ? 768 : w.runs == 1 ? 256 : 512; }
-int units_of(Width w) { return w.runs == 1 ? 2 * grad_blocks(w) : grad_blocks(w); }
-int rows_of(Width w) { return w.waves > 4 ? 1 : 4 / w.waves; }
+int grad_blocks(Width w) { return w.threads <= 256 ? 768 : w.runs > 1 ? 128 : 256; }
+int units_of(Width w) { return 2 * grad_blocks(w); }
+int rows_of(Width w) { return workgroup(w.threads) / w.threads; }
 
-template <typename T, typename S, bool LAYER, bool WIDE>
+template <typename T, typename S, bool LAYER, bool CUT>
 void launch_forward(const BlockP& p, unsigned grid, hipStream_t s) {
-  auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, s, p); };
   const Width w = forward_width(p.dim);
-  switch (w.waves * 2 + w.runs) {
-    case 3: return go(block_norm_kernel<T, S, LAYER, 1, 1, WIDE>, 256);
-    case 4: return go(block_norm_kernel<T, S, LAYER, 1, 2, WIDE>, 256);
-    case 6: return go(block_norm_kernel<T, S, LAYER, 2, 2, WIDE>, 256);
-    case 10: return go(block_norm_kernel<T, S, LAYER, 4, 2, WIDE>, 256);
-    case 18: return go(block_norm_kernel<T, S, LAYER, 8, 2, WIDE>, 512);
-    default: return go(block_norm_kernel<T, S, LAYER, 16, 2, WIDE>, 1024);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(workgroup(w.threads)), 0, s, p); };
+  switch (w.threads * 2 + w.runs) {
+    case 33: return go(block_norm_kernel<T, S, LAYER, CUT, 16, 1>);
+    case 65: return go(block_norm_kernel<T, S, LAYER, CUT, 32, 1>);
+    case 129: return go(block_norm_kernel<T, S, LAYER, CUT, 64, 1>);
+    case 130: return go(block_norm_kernel<T, S, LAYER, CUT, 64, 2>);
+    case 258: return go(block_norm_kernel<T, S, LAYER, CUT, 128, 2>);
+    case 514: return go(block_norm_kernel<T, S, LAYER, CUT, 256, 2>);
+    case 1026: return go(block_norm_kernel<T, S, LAYER, CUT, 512, 2>);
+    default: return go(block_norm_kernel<T, S, LAYER, CUT, 1024, 2>);
   }
 }
-template <typename T, typename S, bool LAYER, bool WIDE>
+template <typename T, typename S, bool LAYER, bool CUT>
 void launch_backward(const BlockP& p, unsigned grid, hipStream_t s) {
-  auto go = [&](auto kernel, int threads) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, s, p); };
   const Width w = backward_width(p.dim);
-  switch (w.waves * 2 + w.runs) {
-    case 3: return go(block_norm_bwd_kernel<T, S, LAYER, 1, 1, WIDE>, 256);
-    case 5: return go(block_norm_bwd_kernel<T, S, LAYER, 2, 1, WIDE>, 256);
-    case 9: return go(block_norm_bwd_kernel<T, S, LAYER, 4, 1, WIDE>, 256);
-    case 17: return go(block_norm_bwd_kernel<T, S, LAYER, 8, 1, WIDE>, 512);
-    case 18: return go(block_norm_bwd_kernel<T, S, LAYER, 8, 2, WIDE>, 512);
-    default: return go(block_norm_bwd_kernel<T, S, LAYER, 8, 4, WIDE>, 512);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(workgroup(w.threads)), 0, s, p); };
+  switch (w.threads * 2 + w.runs) {
+    case 33: return go(block_norm_bwd_kernel<T, S, LAYER, CUT, 16, 1>);
+    case 65: return go(block_norm_bwd_kernel<T, S, LAYER, CUT, 32, 1>);
+    case 129: return go(block_norm_bwd_kernel<T, S, LAYER, CUT, 64, 1>);
+    case 257: return go(block_norm_bwd_kernel<T, S, LAYER, CUT, 128, 1>);
+    case 513: return go(block_norm_bwd_kernel<T, S, LAYER, CUT, 256, 1>);
+    case 1025: return go(block_norm_bwd_kernel<T, S, LAYER, CUT, 512, 1>);
+    case 2049: return go(block_norm_bwd_kernel<T, S, LAYER, CUT, 1024, 1>);
+    default: return go(block_norm_bwd_kernel<T, S, LAYER, CUT, 1024, 2>);
   }
 }
 
+enum class Pass { kForward, kBackward, kColumns };
 template <typename T, typename S>
-void launch_kind(const BlockP& p, bool wide, bool back, unsigned grid, hipStream_t s) {
-  auto kind = [&](auto layer) {
-    constexpr bool LAYER = decltype(layer)::value;
-    if (back)
-      wide ? launch_backward<T, S, LAYER, true>(p, grid, s) : launch_backward<T, S, LAYER, false>(p, grid, s);
-    else
-      wide ? launch_forward<T, S, LAYER, true>(p, grid, s) : launch_forward<T, S, LAYER, false>(p, grid, s);
+void launch_kind(const BlockP& p, Pass pass, unsigned grid, hipStream_t s) {
+  auto kind = [&](auto layer, auto cut) {
+    constexpr bool LAYER = decltype(layer)::value, CUT = decltype(cut)::value;
+    if (pass == Pass::kForward) return launch_forward<T, S, LAYER, CUT>(p, grid, s);
+    if (pass == Pass::kBackward) return launch_backward<T, S, LAYER, CUT>(p, grid, s);
+    hipLaunchKernelGGL((block_columns_kernel<T, S, LAYER, CUT>), dim3(grid, (unsigned)((p.dim + 511) / 512)), dim3(64),
+                       0, s, p);
   };
-  p.layer ? kind(std::true_type()) : kind(std::false_type());
+  auto dims = [&](auto layer) { p.dim % 8 ? kind(layer, std::true_type()) : kind(layer, std::false_type()); };
+  p.layer ? dims(std::true_type()) : dims(std::false_type());
 }
-void launch_types(const BlockP& p, bool wide, bool bf16, bool stream_bf16, bool back, unsigned grid, hipStream_t s) {
-  if (!bf16) return launch_kind<float, float>(p, wide, back, grid, s);
-  if (stream_bf16) return launch_kind<uint16_t, uint16_t>(p, wide, back, grid, s);
-  launch_kind<uint16_t, float>(p, wide, back, grid, s);
+void launch_types(const BlockP& p, bool bf16, bool stream_bf16, Pass pass, unsigned grid, hipStream_t s) {
+  if (!bf16) return launch_kind<float, float>(p, pass, grid, s);
+  if (stream_bf16) return launch_kind<uint16_t, uint16_t>(p, pass, grid, s);
+  launch_kind<uint16_t, float>(p, pass, grid, s);
 }
 
 bool check_sizes(const elasto_block_norm_t* d) {
@@ -642,6 +802,9 @@ Slices slices_of(const elasto_block_norm_t& d) {
 // Bytes of the parts: of the weights' sums by workgroups, of the gate's by units or workgroups (a unit that
 // has a whole sequence writes the gate's gradient itself).
 int64_t part_bytes(const Slices& s, int dim) { return (int64_t)s.grid * 4 * dim * 4; }
+int64_t stats_bytes(const elasto_block_norm_t& d) {
+  return backward_width(d.dim).runs > 1 ? (int64_t)d.batch * d.tokens * kStats * 4 : 0;
+}
 int64_t gate_bytes(const Slices& s, int dim) { return s.per > 1 ? (int64_t)s.units * dim * 4 : (int64_t)s.grid * dim * 4; }
 
 bool check_desc(const elasto_block_norm_t* d) {
@@ -697,17 +860,6 @@ BlockP params(const elasto_block_norm_t& d) {
   return p;
 }
 
-// Whether everything starts at, and goes in steps of, 16 bytes.
-bool wide(const BlockP& p) {
-  auto ok = [](const Rows& r) { return aligned(r.p, 16) && r.sb % 16 == 0 && r.st % 16 == 0; };
-  for (const Rows* r : {&p.x, &p.y, &p.x_out, &p.u, &p.dx_out, &p.du, &p.dx, &p.dy})
-    if (r->p && !ok(*r)) return false;
-  for (const void* w : {(const void*)p.pre_gamma, (const void*)p.pre_beta, (const void*)p.post_gamma,
-                        (const void*)p.post_beta, (const void*)p.gate})
-    if (!aligned(w, 16)) return false;
-  return p.dim % 8 == 0;
-}
-
 }  // namespace
 }  // namespace elasto
 
@@ -731,7 +883,7 @@ elasto_status_t elasto_op_block_norm(const elasto_block_norm_t* d, const elasto_
   const int per = rows_of(forward_width(d->dim));
   const unsigned grid = (unsigned)std::min<int64_t>((rows + per - 1) / per, forward_blocks(d->dim));
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  launch_types(p, wide(p), es == 2, ss == 2, false, grid, s);
+  launch_types(p, es == 2, ss == 2, Pass::kForward, grid, s);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail(ELASTO_ERR_HIP, "block_norm: %s", hipGetErrorString(e));
   return ELASTO_OK;
@@ -788,16 +940,32 @@ elasto_status_t elasto_op_block_norm_bwd(const elasto_block_norm_t* d, const ela
   p.gate_unit = d_gate && per_sequence;
   const bool direct = p.gate_unit && sl.per == 1;
   const int sums = p.wanted & ~(direct ? 16 : 0);
-  if (sums) {
-    const int64_t need = part_bytes(sl, d->dim) + gate_bytes(sl, d->dim);
+  const bool columns = p.wanted && backward_width(d->dim).runs > 1;
+  if (sums || columns) {
+    const int64_t need = part_bytes(sl, d->dim) + gate_bytes(sl, d->dim) + stats_bytes(*d);
     if (!workspace || !aligned(workspace, 16) || workspace_bytes < need)
       return fail(ELASTO_ERR_INVALID_ARG, "block_norm: the workspace holds %lld of %lld bytes",
                   (long long)(workspace ? workspace_bytes : 0), (long long)need);
     p.part = static_cast<float*>(workspace);
     p.gate_part = p.part + part_bytes(sl, d->dim) / 4;
+    if (columns) p.stats = p.gate_part + gate_bytes(sl, d->dim) / 4;
   }
   if (direct) p.gate_part = d_gate;
-  launch_types(p, wide(p), es == 2, ss == 2, true, (unsigned)sl.grid, s);
+  if (columns) {
+    // The columns are summed from the rows as they were: where the gradients take their place, a pass that
+    // writes none comes first.
+    BlockP first = p;
+    const bool over = (p.dx.p && (p.dx.p == p.x_out.p || p.dx.p == p.dx_out.p)) ||
+                      (p.dy.p && (p.dy.p == p.du.p || p.dy.p == p.y.p));
+    if (over) first.dx.p = first.dy.p = nullptr;
+    const unsigned grid = (unsigned)std::min(sl.units, 256);
+    launch_types(first, es == 2, ss == 2, Pass::kBackward, grid, s);
+    launch_types(p, es == 2, ss == 2, Pass::kColumns, (unsigned)sl.grid, s);
+    p.stats = nullptr;
+    if (over) launch_types(p, es == 2, ss == 2, Pass::kBackward, grid, s);
+  } else {
+    launch_types(p, es == 2, ss == 2, Pass::kBackward, (unsigned)sl.grid, s);
+  }
   e = hipGetLastError();
   if (e == hipSuccess && sums) {
     SumP q = {};
@@ -819,7 +987,7 @@ elasto_status_t elasto_block_norm_workspace(const elasto_block_norm_t* d, int64_
   if (!bytes) return fail(ELASTO_ERR_INVALID_ARG, "NULL argument");
   if (!check_sizes(d)) return ELASTO_ERR_INVALID_ARG;
   const Slices s = slices_of(*d);
-  *bytes = part_bytes(s, d->dim) + gate_bytes(s, d->dim);
+  *bytes = part_bytes(s, d->dim) + gate_bytes(s, d->dim) + stats_bytes(*d);
   return ELASTO_OK;
 }
 

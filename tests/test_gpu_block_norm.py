@@ -389,3 +389,37 @@ def test_captured_and_replayed():
         step()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, (x_out, u, dx, dy, *out.values())))
+
+
+@pytest.mark.parametrize("dtype,stream", TYPES)
+@pytest.mark.parametrize("d", [3, 100, 128, 129, 200, 256, 257, 4097, 8191, 8193, 12002])
+def test_rows_that_share_a_wave_and_rows_of_columns_apart(dtype, stream, d):
+    """Rows of 16 and of 32 lanes, ends of rows inside a run, rows whose weights' sums are taken apart:
+    padded batches, unaligned rows, gates of either kind."""
+    for kind, gate, strided in (("rms", "shared", True), ("layer", "sequence", False), ("layer", "shared", True)):
+        c = Case(dtype, stream, 3, 37, d, kind=kind, gate=gate, lens=[37, 0, 19], strided=strided, offset=1)
+        pad = ~c.inside()
+        for v in (c.x, c.y, c.dx_out, c.du):
+            v[pad] = math.nan
+        c.check_forward(*c.forward())
+        c.check_backward(c.backward())
+        c.check_backward(c.backward(dx_out=False), dx_out=False)
+        c.check_backward(c.backward(du=False), du=False)
+
+
+@pytest.mark.parametrize("dtype,stream", [(BF, BF), (F32, F32)])
+@pytest.mark.parametrize("d", [90, 250, 6001, 9000])
+def test_in_place_with_the_weights_gradients(dtype, stream, d):
+    c = Case(dtype, stream, 2, 30, d, kind="layer", gate="sequence")
+    x_out, u = c.forward()
+    x, y = c.x.clone(), c.y.clone()
+    ffi.op_block_norm(x, y, x, y, **c.kw)
+    assert torch.equal(x, x_out) and torch.equal(y, u)
+    ref = c.backward()
+    ws = torch.empty(ffi.block_norm_workspace(c.y, c.w["gate"]), dtype=torch.uint8, device="cuda")
+    for dx_is, dy_is in ((0, 1), (2, 3), (0, 3)):
+        t = [v.clone() for v in (c.dx_out, c.du, c.x, c.y)]
+        out = {"d_" + n: torch.full_like(c.w[n], math.nan) for n in c.w}
+        ffi.op_block_norm_bwd(t[2], t[3], t[0], t[1], t[dx_is], t[dy_is], workspace=ws, **c.kw, **out)
+        assert torch.equal(t[dx_is], ref["dx"]) and torch.equal(t[dy_is], ref["dy"])
+        assert all(torch.equal(out[n], ref[n]) for n in out)
