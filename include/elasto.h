@@ -690,7 +690,8 @@ elasto_status_t elasto_block_norm_workspace(const elasto_block_norm_t* desc, int
  * once.  FP32: fp32 throughout.  Results are the same bits every time.
  * Needs dim a multiple of 8 (FP32: 4), x, weight and their strides multiples
  * of 16 bytes, dim and strides at most 2^20, rows at most 2^24, classes at most
- * 2^30, and a product of any two of rows, classes and dim below 2^36. */
+ * 2^30, and a product of any two of rows, classes and dim, each rounded up to a
+ * multiple of 128, below 2^36. */
 typedef struct {
   int32_t dtype, dim, classes;
   int64_t rows;
