@@ -2,9 +2,9 @@
 // workgroup's BM x BN tile, with either operand lying straight (rows of K
 // contiguous values) or turned (K rows of contiguous columns), in bf16 or fp32.
 //
-// A step is KB = 128 or 64 bytes of K of a straight operand, and as many rows of a turned one as
-// that holds values.  Tiles go to LDS by direct 16-byte loads, in two to four stages.
-//  * Straight: LDS rows of KB bytes, 16-byte chunk c of row r at c ^ (r>>1 & 7) (64: c ^ (r>>2 & 3)).
+// A step is KB = 128 bytes of K of a straight operand, and as many rows of a turned one as that
+// holds values.  Tiles go to LDS by direct 16-byte loads, in two to four stages.
+//  * Straight: LDS rows of KB bytes, 16-byte chunk c of row r at c ^ (r>>1 & 7).
 //    bf16: a lane's chunk is its operand.  fp32: four values of K a lane and read,
 //    each the operand of one 32x32x2 product (which two values of K meet in a
 //    product is free as long as both operands agree).
@@ -32,8 +32,10 @@ struct Matrix {
   int64_t ld = 0;  // bytes between its rows
 };
 
+constexpr int KB = 128;
+
 // TURNED: whether K is the operand's row.  B: the tile's size along the other axis.
-template <typename T, bool TURNED, int B, int THREADS, int KB>
+template <typename T, bool TURNED, int B, int THREADS>
 struct Operand {
   static constexpr int kBytes = B * KB, kK = KB / (int)sizeof(T), kQuarters = KB / 32;
   static constexpr int kRow = TURNED ? B * (int)sizeof(T) : KB;  // bytes of an LDS row
@@ -43,7 +45,7 @@ struct Operand {
   static_assert(kBytes % (16 * THREADS) == 0, "whole loads");
 
   static __device__ __forceinline__ int swizzle(int r) {
-    if constexpr (!TURNED) return KB == 128 ? (r >> 1) & 7 : (r >> 2) & 3;
+    if constexpr (!TURNED) return (r >> 1) & 7;
     if constexpr (B == 32) return 0;  // four rows are 256 bytes (fp32: the half-waves' rows share banks)
     if constexpr (sizeof(T) == 4) return ((r >> 2) & 1) * 8;
     if constexpr (B == 64) return ((r >> 1) & 1) * 4;
@@ -164,10 +166,10 @@ __device__ __forceinline__ void multiply(const u32x4 (&a)[TM], const u32x4 (&b)[
 // GROUPS: workgroups that a CU holds by their registers and LDS.  KS: 4 where each of four groups of WM x
 // WN waves takes one quarter of every step (small launches: a tile's chain of products is a quarter as
 // long); their sums are added at the end, in the groups' order, in all of them.
-template <typename T_, int BM_, int BN_, int WM_, int WN_, int KB_, int STAGES_, int GROUPS_, int KS_ = 1>
+template <typename T_, int BM_, int BN_, int WM_, int WN_, int STAGES_, int GROUPS_, int KS_ = 1>
 struct Shape {
   typedef T_ T;
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_, KB = KB_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, STAGES = STAGES_;
   static constexpr int kK = KB / (int)sizeof(T_);  // values of K of a step
   static constexpr int KS = KS_, kTeam = WM * WN, kThreads = 64 * kTeam * KS;
   static constexpr int WTM = BM / WM, WTN = BN / WN, TM = WTM / 32, TN = WTN / 32;
@@ -175,7 +177,7 @@ struct Shape {
   static constexpr bool kFew = TM * TN <= 2;  // few accumulators
   static constexpr int kGroups = GROUPS_, kWaves = kGroups * kTeam * KS / 4;  // kWaves: on a SIMD
   static_assert(STAGES * kStage * kGroups <= 160 * 1024, "LDS of a CU");
-  static_assert(KS == 1 || (KB_ == 128 && KS == 4 && KS * kTeam * TM * TN * 4096 <= STAGES * kStage), "quarters");
+  static_assert(KS == 1 || (KS == 4 && KS * kTeam * TM * TN * 4096 <= STAGES * kStage), "quarters");
 };
 
 // The operands' values of one quarter of a step.
@@ -272,8 +274,8 @@ __device__ __forceinline__ void tile_product(char* smem, const Matrix& A, const 
                                              f32x16 (&acc)[S::TM][S::TN]) {
   typedef typename S::T T;
   constexpr int K = S::kK, ES = (int)sizeof(T);
-  typedef Operand<T, TA, S::BM, S::kThreads, S::KB> OA;
-  typedef Operand<T, TB, S::BN, S::kThreads, S::KB> OB;
+  typedef Operand<T, TA, S::BM, S::kThreads> OA;
+  typedef Operand<T, TB, S::BN, S::kThreads> OB;
   constexpr int kLoads = OA::kLoads + OB::kLoads, kAhead = S::STAGES - 1;
   const int tid = threadIdx.x;
   const OA oa(A.ld, M - m0, tid);
@@ -281,7 +283,7 @@ __device__ __forceinline__ void tile_product(char* smem, const Matrix& A, const 
   const Readers<S, OA, OB> rd(__builtin_amdgcn_readfirstlane(tid >> 6), tid & 63);
   const char* pa = A.p + (TA ? k0 * A.ld + m0 * ES : m0 * A.ld + k0 * ES);
   const char* pb = B.p + (TB ? k0 * B.ld + n0 * ES : n0 * B.ld + k0 * ES);
-  const int64_t sa = TA ? A.ld * K : S::KB, sb = TB ? B.ld * K : S::KB;
+  const int64_t sa = TA ? A.ld * K : KB, sb = TB ? B.ld * K : KB;
   const int nk = (int)((k1 - k0 + K - 1) / K);
   if (nk <= 0) return;
   const uint32_t* words = live + k0 / 32;
