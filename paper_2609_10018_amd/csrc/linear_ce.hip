@@ -14,7 +14,7 @@
 //
 // Bound by the matrix cores, where rows are few by reading W: forward, 4096 rows of 2048 and 50021 classes
 // 744 us (1.13 PFLOP/s, where a large product reaches 1.28), 16 rows of 4096 and 100003 classes 158 us (5.2
-// TB/s); gradients, 3277 rows of 2048 that count and 131072 classes 4.95 ms (1.07 PFLOP/s); fp32, 1000 rows of
+// TB/s); gradients, 3277 rows of 2048 that count and 131072 classes 4.72 ms (1.12 PFLOP/s); fp32, 1000 rows of
 // 384 and 10007 classes 226 us (102 TFLOP/s of 154).
 #include <math.h>
 
@@ -566,6 +566,10 @@ __global__ __launch_bounds__(256) void ce_zero_db_kernel(float* db, int64_t n) {
 constexpr int64_t kMaxRows = 1 << 24, kMaxClasses = 1 << 30, kMaxDim = 1 << 20;
 constexpr int64_t kMaxTiles = 1 << 22;  // of 128 x 128: two products of 256 threads a tile; a launch holds fewer than 2^32
 
+// Row tiles that an XCD walks together: 13 by 128 of dW's and 13 by 8 of dx's tiles, 4.72 ms of gradients with 4 (2:
+// 4.71), 4.96 with 8; 16 row tiles and other shapes lie within 1% of each other.
+constexpr int kGroup = 4;
+
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 int64_t tiles(int64_t n, int64_t b) { return (n + b - 1) / b; }
 
@@ -798,7 +802,7 @@ CeP params(const Args& a) {
   p.weight = a.d.row_weight;
   p.classes = a.d.classes;
   p.label_classes = a.d.classes;
-  p.group = 8;
+  p.group = kGroup;
   return p;
 }
 
@@ -947,7 +951,7 @@ hipError_t backward(const Args& a, const Grads& g, char* ws, hipStream_t s) {
   x.ld_sum = d.dim;
   x.count = p.count;
   x.index = p.index;
-  x.group = 8;
+  x.group = kGroup;
   x.split = l.x.parts;
   if (l.x_summed) x.sum = reinterpret_cast<float*>(ws + l.sum);
   ProductP w = {};
@@ -956,7 +960,7 @@ hipError_t backward(const Args& a, const Grads& g, char* ws, hipStream_t s) {
   w.K = d.rows;
   w.ldo = g.lddw * es;
   w.ld_sum = d.dim;
-  w.group = 8;
+  w.group = kGroup;
   w.split = l.w.parts;
   if (l.w.parts > 1) w.sum = reinterpret_cast<float*>(ws + l.wsum);
   w.live = live;
