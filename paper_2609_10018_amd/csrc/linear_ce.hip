@@ -41,7 +41,10 @@ struct CeP {
   float2* part;   // forward: [tiles of classes][rows]
   float* picked;  // forward: the label's logit
   const int32_t *count, *index;  // rows that are there and where they come from, or NULL: `rows`
-  float* db_part;  // [tiles of rows][ld_db]
+  float* db_part;  // [tiles of rows][ld_db], or NULL
+  float* db;       // of the piece, where one tile has all rows (then no db_part), or NULL
+  float scale;     // of db
+  uint32_t* live;  // one bit a row: whether it gives the gradients anything; or NULL
   int64_t ld_db;
   int tiles_n, group;
   int label_classes;  // all classes
@@ -218,19 +221,6 @@ __global__ __launch_bounds__(1024) void ce_join_kernel(JoinP p) {
   if (p.lse) p.lse[to] = out ? 0.0f : above + ref;
 }
 
-// One bit a row: whether it gives the gradients anything.
-__global__ __launch_bounds__(256) void ce_live_kernel(const float* weight, const int32_t* labels, int64_t rows,
-                                                      int classes, uint32_t* live) {
-  const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  bool on = false;
-  if (r < rows) {
-    const int y = labels[r];
-    on = y >= 0 && y < classes && !(weight && weight[r] == 0.0f);
-  }
-  const uint64_t b = __ballot(on);
-  if ((threadIdx.x & 31) == 0) live[r >> 5] = (uint32_t)(b >> (threadIdx.x & 32));
-}
-
 // Rows that count, one after another: what rows of weight 0 would cost is not spent.  A backward pass
 // leaves out rows with bad labels too.
 struct GatherP {
@@ -360,7 +350,9 @@ struct RowsOut {
   }
 };
 
-// dz of one tile of the piece.
+// dz of one tile of the piece.  The first column of tiles also says which rows count, and a tile of all rows
+// sums dbias itself: launches that small calls would wait for (8 rows of 768,
+// 1000 classes: 24.7 -> 20.2 us).
 template <typename S>
 __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_dz_kernel(CeP p) {
   typedef typename S::T T;
@@ -387,6 +379,8 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_dz_kernel(CeP p) {
       w = y >= 0 && y < p.label_classes ? (p.weight ? p.weight[row] : 1.0f) : 0.0f;
       lse = p.lse[row];
     }
+    const uint32_t on = (uint32_t)__ballot(w != 0.0f);  // lanes 32 on have the same rows
+    if (p.live && tn == 0 && wn == 0 && lane == 0 && leads<S>()) p.live[block / 32] = on;
     const Power power(lse);
     const float f = w * power.left;
 #pragma unroll
@@ -409,7 +403,7 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_dz_kernel(CeP p) {
                                   (int64_t)(first + c) * (int)sizeof(T)) = v;
     });
   }
-  if (!p.db_part) return;
+  if (!p.db_part && !p.db) return;
   // Sums over the tile's rows: over the wave's blocks, its lanes, then the waves.
   __syncthreads();
   float* red = reinterpret_cast<float*>(smem);  // [WM][BN]
@@ -429,7 +423,11 @@ __global__ __launch_bounds__(S::kThreads, S::kWaves) void ce_dz_kernel(CeP p) {
     float s = red[c];
 #pragma unroll
     for (int k = 1; k < S::WM; ++k) s += red[k * S::BN + c];
-    if (n0 + c < p.ld_db) p.db_part[tm * p.ld_db + n0 + c] = s;
+    if (p.db) {
+      if (n0 + c < p.classes) p.db[n0 + c] = s * p.scale;
+    } else if (n0 + c < p.ld_db) {
+      p.db_part[tm * p.ld_db + n0 + c] = s;
+    }
   }
 }
 
@@ -932,15 +930,13 @@ hipError_t backward(const Args& a, const Grads& g, char* ws, hipStream_t s) {
   uint32_t* live = reinterpret_cast<uint32_t*>(ws + l.live);
   CeP p = params(a);
   p.lse = g.lse;
+  p.scale = g.scale;
   GatherP take = {};
   take.back = true;
   take.lse = g.lse;
   take.dx = g.dx;
   take.lddx = g.lddx * es;
   const bool gathered = gather(a, &p, take, ws + l.gather, s);
-  if (!gathered && g.dw)
-    hipLaunchKernelGGL(ce_live_kernel, dim3((unsigned)((d.rows + 255) / 256)), dim3(256), 0, s, d.row_weight,
-                       d.labels, d.rows, d.classes, live);
   hipError_t e = hipGetLastError();
   ProductP x = {};
   x.scale = g.scale;
@@ -972,17 +968,20 @@ hipError_t backward(const Args& a, const Grads& g, char* ws, hipStream_t s) {
     p.classes = n;
     p.dz = Matrix{ws + l.dz, l.piece * es};
     p.ld_db = l.piece;
-    p.db_part = g.db ? reinterpret_cast<float*>(ws + l.db) : nullptr;
+    p.live = !gathered && g.dw && c0 == 0 ? live : nullptr;
     int side = 0;
     with_shape<T>(way_of(d.rows, n, d.dim, es, false).kind, [&](auto shape) {
       typedef decltype(shape) S;
       side = S::BM;
       p.tiles_n = (int)tiles(n, S::BN);
+      const bool direct = !gathered && p.rows <= side;
+      p.db = g.db && direct ? g.db + c0 : nullptr;
+      p.db_part = g.db && !direct ? reinterpret_cast<float*>(ws + l.db) : nullptr;
       hipLaunchKernelGGL((ce_dz_kernel<S>), dim3((unsigned)(tiles(p.rows, S::BM) * p.tiles_n)), dim3(S::kThreads), 0,
                          s, p);
     });
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (g.db) {
+    if (p.db_part) {
       hipLaunchKernelGGL(ce_db_kernel, dim3(blocks(n)), dim3(256), 0, s, p.db_part, p.count, d.rows, side, l.piece, n,
                          g.scale, g.db + c0);
       if ((e = hipGetLastError()) != hipSuccess) return e;
