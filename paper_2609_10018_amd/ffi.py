@@ -915,6 +915,7 @@ class GradList:
         self.tensors = list(tensors)
         self.array = (Grad * max(1, len(self.tensors)))()
         self._seen = self.paired = None
+        self.changes = 0
         t = _tt().tensor
         self._places = t.data_ptr, t.numel   # asked of each tensor at each call
         self.entries()
@@ -935,6 +936,7 @@ class GradList:
                     raise ValueError(f"tensor {i} lies on {t.device}, the first on {ts[0].device}")
                 self.array[i] = Grad(now[0][i], now[1][i], _dtype(t))
             self._seen, self.paired = now, None
+            self.changes += 1
         return self.array
 
 
@@ -972,16 +974,18 @@ def op_clip_gradients(grads, max_norm: float, stats, out=None, workspace=None, s
     if len(o) != len(g):
         raise ValueError(f"{len(o)} results for {len(g)} gradients")
     dev = _list_device(g, *o.tensors[:1], stats, workspace)
-    if o is not g and o.array is not g.paired:
+    grads = g.entries()
+    results = grads if o is g else o.entries()
+    if o is not g and g.paired != (o, o.changes):
         for i, (a, b) in enumerate(zip(g.tensors, o.tensors)):
             if a.shape != b.shape or a.stride() != b.stride() and not (
                     a.is_contiguous() and b.is_contiguous()):
                 raise ValueError(f"result {i} {tuple(b.shape)} with strides {b.stride()} does not have its "
                                  f"elements where its gradient has them")
-        g.paired = o.array   # checked once for the two lists
+        g.paired = o, o.changes   # checked once for the two lists as they are
     check(load_library().elasto_op_clip_gradients(
-        g.entries(), o.entries(), len(g), max_norm, _plain(stats, _tt().f32, "stats", 2),
-        *_space(workspace), _stream_ptr(stream, dev)))
+        grads, results, len(g), max_norm, _plain(stats, _tt().f32, "stats", 2), *_space(workspace),
+        _stream_ptr(stream, dev)))
 
 
 class GrowthContext:

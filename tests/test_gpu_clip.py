@@ -173,3 +173,22 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         assert torch.equal(st, stats) and all(torch.equal(a, b) for a, b in zip(got, out))
         check(out, ts, 0.1, stats)
+
+
+def test_lists_that_have_changed_are_looked_at_again():
+    """Results whose elements come to lie in another order than their gradients' are refused, whichever
+    of two lists that were used together has changed."""
+    for which in (0, 1):
+        ts, out = ([torch.randn(6, 10, device="cuda"), torch.randn(7, device="cuda")] for _ in range(2))
+        g, o = ffi.GradList(ts), ffi.GradList(out)
+        ws, stats = space(g), torch.empty(2, device="cuda")
+        for _ in range(2):
+            ffi.op_clip_gradients(g, 1.0, stats, out=o, workspace=ws)
+        (ts, out)[which][0].data = torch.randn(10, 6, device="cuda").t()
+        for _ in range(2):
+            with pytest.raises(ValueError, match="result 0"):
+                ffi.op_clip_gradients(g, 1.0, stats, out=o, workspace=ws)
+        # Both in the same order again, though another one than before.
+        (ts, out)[1 - which][0].data = torch.randn(10, 6, device="cuda").t()
+        ffi.op_clip_gradients(g, 1.0, stats, out=o, workspace=ws)
+        check(out, ts, 1.0, stats)
