@@ -58,39 +58,41 @@ struct BlockP {
   float* stats;            // [row][kStats] of rows whose sums a kernel of their own takes
 };
 
-// A row is held by T threads, CH runs of 8 columns each: run i of thread t begins at column (i T + t) 8.
-// Runs are loaded and stored whole, at whatever address they lie.  Where dim is no multiple of 8, the last
-// run is moved back to end with the row, and its first `skip` values, which are the run's before it, count
-// as 0 and are not stored (CUT; the other dims have kernels without it: 50432 rows of 768, 69 -> 59 us).
+// A row is held by T threads, CH runs of 8 columns each: run i of thread t begins at column (i T + t) 8.  Rows
+// reach into the last of the CH (forward_width, backward_width), so the others are there in every thread.
+// Runs are loaded and stored whole, at whatever address they lie.  Where dim is no multiple of 8, the row's
+// last run is moved back to end with it, and its first `skip` values, which are the run's before it, count
+// as 0 and are not stored (CUT; the other dims have kernels without it: 50432 rows of 768, 69 -> 54 us).
 template <int T, int CH, bool CUT>
 struct Place {
-  static constexpr int E = 8 * CH;
+  static constexpr int E = 8 * CH, kLast = CH - 1;
   static constexpr bool kCut = CUT, kShort = CUT && T == 16;   // kShort: rows of fewer than 8
-  int dim, t, skip, cut;    // cut: the run that was moved, of the thread that has it; others: -1
-  float m[CH];              // 1 where a run is there, 0 where it is not
-  __device__ __forceinline__ Place(int dim_, int t_) : dim(dim_), t(t_), skip(-dim_ & 7), cut(-1) {
+  int dim, t, skip;
+  bool cut;       // this thread's last run is the one that was moved
+  bool drop[7];   // its values that are not the thread's
+  float m;        // 1 where the last run is there, 0 where it is not
+  __device__ __forceinline__ Place(int dim_, int t_) : dim(dim_), t(t_), skip(-dim_ & 7) {
+    m = there(kLast) ? 1.0f : 0.0f;
+    cut = CUT && there(kLast) && column(kLast) + 8 > dim;
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      m[i] = there(i) ? 1.0f : 0.0f;
-      if (CUT && there(i) && column(i) + 8 > dim) cut = i;
-    }
+    for (int e = 0; e < 7; ++e) drop[e] = cut && e < skip;
   }
   __device__ __forceinline__ int column(int i) const { return (i * T + t) * 8; }
-  __device__ __forceinline__ int begin(int i) const { return CUT ? min(column(i), dim - 8) : column(i); }
-  __device__ __forceinline__ bool there(int i) const { return column(i) < dim; }
+  __device__ __forceinline__ int begin(int i) const { return CUT && i == kLast ? min(column(i), dim - 8) : column(i); }
+  __device__ __forceinline__ bool there(int i) const { return i < kLast || column(i) < dim; }
   // Whether value e is one of the row's.
   __device__ __forceinline__ bool holds(int e) const {
-    return there(e >> 3) && !(CUT && cut == (e >> 3) && (e & 7) < skip);
+    return there(e >> 3) && !(CUT && (e >> 3) == kLast && (e & 7) < 7 && drop[e & 7]);
   }
   __device__ __forceinline__ void clean_run(float (&v)[E], int i) const {
-    if (CUT && cut == i)
+    if (CUT && i == kLast)
 #pragma unroll
-      for (int e = 0; e < 7; ++e)
-        if (e < skip) v[8 * i + e] = 0.0f;
+      for (int e = 0; e < 7; ++e) v[8 * i + e] = drop[e] ? 0.0f : v[8 * i + e];
   }
+
   // v less `less` in the columns that are there; in the others it stays 0.
   __device__ __forceinline__ void subtract_run(float (&v)[E], float less, int i) const {
-    const float k = less * m[i];
+    const float k = i == kLast ? less * m : less;
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[8 * i + e] -= k;
     clean_run(v, i);
@@ -119,7 +121,7 @@ template <typename L, typename T>
 __device__ __forceinline__ void store_run(T* p, const L& l, const float (&v)[L::E], int i) {
   if (!l.there(i)) return;
   T* to = p + l.begin(i);
-  if (!L::kCut || l.cut != i)
+  if (!L::kCut || i != L::kLast || !l.cut)
     store_run(to, v + 8 * i);
   else
 #pragma unroll
@@ -749,7 +751,9 @@ void launch_backward(const BlockP& p, unsigned grid, hipStream_t s) {
     case 257: return go(block_norm_bwd_kernel<T, S, LAYER, CUT, 128, 1>);
     case 513: return go(block_norm_bwd_kernel<T, S, LAYER, CUT, 256, 1>);
     case 1025: return go(block_norm_bwd_kernel<T, S, LAYER, CUT, 512, 1>);
-    case 2049: return go(block_norm_bwd_kernel<T, S, LAYER, CUT, 1024, 1>);
+    // A layer norm in fp32 runs with CUT in any case, which spills 10 registers instead of 43 (6000 rows of
+    // 6144: 363 -> 277 us; bf16, where it spills none instead of 19, 176 -> 206).
+    case 2049: return go(block_norm_bwd_kernel<T, S, LAYER, CUT || (LAYER && sizeof(T) == 4), 1024, 1>);
     default: return go(block_norm_bwd_kernel<T, S, LAYER, CUT, 1024, 2>);
   }
 }
