@@ -631,8 +631,8 @@ typedef enum { ELASTO_NORM_RMS = 0, ELASTO_NORM_LAYER = 1 } elasto_norm_t;
  *   x_out = residual_scale x + gate (.) n,   u = N(x_out; pre_gamma, pre_beta),
  *   N(v) = (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) (.) gamma + beta,
  * with mean(v) taken as 0, and no beta, for ELASTO_NORM_RMS.  NULL weights: gamma
- * 1, beta 0; gate NULL: 1.  gate is fp32 [dim], or [batch][dim] where
- * gate_per_sequence is set.  lens (or NULL): tokens t >= lens[b] are neither read
+ * 1, beta 0; gate NULL: 1, whatever gate_per_sequence says.  gate is fp32 [dim],
+ * or [batch][dim] where gate_per_sequence is set.  lens (or NULL): tokens t >= lens[b] are neither read
  * nor written and add nothing to the gradients.
  * x, x_out and their gradients are of stream_dtype, y, u and theirs of dtype
  * (stream_dtype FP32 with either, BF16 with BF16).  Everything between load and

@@ -851,7 +851,7 @@ BlockP params(const elasto_block_norm_t& d) {
   p.post_gamma = d.post_gamma;
   p.post_beta = d.post_beta;
   p.gate = d.gate;
-  p.gate_ld = d.gate_per_sequence ? d.dim : 0;
+  p.gate_ld = d.gate && d.gate_per_sequence ? d.dim : 0;  // no gate: no sequence's place behind NULL
   p.lens = d.lens;
   p.batch = d.batch;
   p.tokens = d.tokens;

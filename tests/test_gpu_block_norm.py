@@ -423,3 +423,35 @@ def test_in_place_with_the_weights_gradients(dtype, stream, d):
         ffi.op_block_norm_bwd(t[2], t[3], t[0], t[1], t[dx_is], t[dy_is], workspace=ws, **c.kw, **out)
         assert torch.equal(t[dx_is], ref["dx"]) and torch.equal(t[dy_is], ref["dy"])
         assert all(torch.equal(out[n], ref[n]) for n in out)
+
+
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("d", [40, 768, 3000, 9001, 12000])
+def test_no_gate_where_each_sequence_would_have_one(kind, d):
+    """A description that says gate_per_sequence and holds no gate, for several sequences: the bits of
+    one that does not say it."""
+    c = Case(BF, F32, 5, 7, d, kind=kind, gate="none")
+    got = []
+    for per in (0, 1):
+        for y in (c.y, None):
+            post = y is not None
+            w = {n: t if post or not n.startswith("post") else None for n, t in c.w.items()}
+            desc, shape, st, dt = ffi._block_desc(c.x, c.du, w["gate"], w["pre_gamma"], w["pre_beta"], w["post_gamma"],
+                                                  w["post_beta"], post, None, c.scale, c.eps, kind)
+            desc.gate_per_sequence = per
+            rows = lambda t, of: ffi._tokens(t, shape, of, "rows")  # noqa: E731, B023
+            x_out, u, dx = c.empty(F32), c.empty(BF), c.empty(F32)
+            dy = c.empty(BF) if post else None
+            lib, stream = ffi.load_library(), torch.cuda.current_stream().cuda_stream
+            assert lib.elasto_op_block_norm(desc, rows(c.x, st), rows(y, dt), rows(x_out, st), rows(u, dt), stream) == 0
+            sums = {n: torch.full((d,), math.nan, device="cuda") for n in w if w[n] is not None}
+            ws = torch.full((ffi.block_norm_workspace(c.x),), 0xff, dtype=torch.uint8, device="cuda")
+            place = [sums[n].data_ptr() if n in sums else None
+                     for n in ("pre_gamma", "pre_beta", "post_gamma", "post_beta")]
+            assert lib.elasto_op_block_norm_bwd(desc, rows(c.x, st), rows(y, dt), rows(c.dx_out, st), rows(c.du, dt),
+                                                rows(dx, st), rows(dy, dt), *place, None, ws.data_ptr(), ws.numel(),
+                                                stream) == 0
+            got.append([x_out, u, dx] + ([dy] if post else []) + list(sums.values()))
+    for a, b in zip(got[:2], got[2:]):
+        assert len(a) == len(b) and all(torch.equal(x, y) and x.isfinite().all() for x, y in zip(a, b))
+    c.check_forward(*got[2][:2])
