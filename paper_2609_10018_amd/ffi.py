@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import operator
 import os
 from typing import Dict, Optional
 
@@ -908,34 +909,47 @@ def _dense(t) -> bool:
 class GradList:
     """Tensors for op_grad_norm and op_clip_gradients, laid out for the C ABI once: bf16 and fp32
     device tensors of any shape whose elements fill one run of memory (in any order of the axes).
-    Holds the tensors; where a tensor's memory has moved, the next call takes the new place.
-    Gradients that are new tensors need a new list."""
+    Holds the tensors and looks at each one at each call: where its memory, type or strides are others,
+    the next call takes it as it is now.  Gradients that are new tensors need a new list."""
 
     def __init__(self, tensors):
         self.tensors = list(tensors)
         self.array = (Grad * max(1, len(self.tensors)))()
         self._seen = self.paired = None
+        self._ordered = []     # those whose elements have another order than their axes
         self.changes = 0
         t = _tt().tensor
-        self._places = t.data_ptr, t.numel   # asked of each tensor at each call
+        self._asked = t.data_ptr, t.numel, operator.attrgetter("dtype"), t.is_contiguous
         self.entries()
 
     def __len__(self) -> int:
         return len(self.tensors)
 
+    def _look(self):
+        """All that the array and the pairing rest on, asked of each tensor at each call, since t_(),
+        as_strided_() or .data = can change each by itself.  Contiguous tensors are one run whatever
+        their shape, so it is not asked for (146 tensors: 25 us instead of 29)."""
+        ts = self.tensors
+        return [list(map(f, ts)) for f in self._asked] + [self._orders()]
+
+    def _orders(self):
+        return [(t.shape, t.stride()) for t in self._ordered]
+
     def entries(self):
         """The C array, up to date."""
-        ts, (place, size) = self.tensors, self._places
-        now = list(map(place, ts)), list(map(size, ts))
+        now = self._look()
         if now != self._seen:
-            for i, t in enumerate(ts):
-                if not _dense(t):
+            self._seen = None   # until all are found to be good
+            ts, array = self.tensors, self.array
+            for i, (t, place, size, _, contiguous) in enumerate(zip(ts, *now[:4])):
+                if not contiguous and not _dense(t):
                     raise ValueError(f"tensor {i} {tuple(t.shape)} with strides {t.stride()} is not "
                                      f"one run of memory")
                 if t.device != ts[0].device:
                     raise ValueError(f"tensor {i} lies on {t.device}, the first on {ts[0].device}")
-                self.array[i] = Grad(now[0][i], now[1][i], _dtype(t))
-            self._seen, self.paired = now, None
+                array[i] = Grad(place, size, _dtype(t))
+            self._ordered = [t for t, contiguous in zip(ts, now[3]) if not contiguous]
+            self._seen, self.paired = now[:4] + [self._orders()], None
             self.changes += 1
         return self.array
 

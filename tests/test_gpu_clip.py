@@ -192,3 +192,35 @@ def test_lists_that_have_changed_are_looked_at_again():
         (ts, out)[1 - which][0].data = torch.randn(10, 6, device="cuda").t()
         ffi.op_clip_gradients(g, 1.0, stats, out=o, workspace=ws)
         check(out, ts, 1.0, stats)
+
+
+def test_lists_that_have_changed_in_place_are_looked_at_again():
+    """The address and the number of elements as they were: another order is refused beside results of
+    the first one, another type is read as what it is."""
+    ts, out = ([torch.randn(6, 10, device="cuda"), torch.randn(7, device="cuda")] for _ in range(2))
+    g, o = ffi.GradList(ts), ffi.GradList(out)
+    ws, stats = space(g), torch.empty(2, device="cuda")
+    for _ in range(2):
+        ffi.op_clip_gradients(g, 1.0, stats, out=o, workspace=ws)
+    for which in (ts, out):
+        which[0].t_()
+        for _ in range(2):
+            with pytest.raises(ValueError, match="result 0"):
+                ffi.op_clip_gradients(g, 1.0, stats, out=o, workspace=ws)
+        which[0].t_()
+        ffi.op_clip_gradients(g, 1.0, stats, out=o, workspace=ws)
+        check(out, ts, 1.0, stats)
+    buf = torch.randn(300, device="cuda")
+    t = buf[:100]
+    g = ffi.GradList([t])
+    ws = space(g)
+    ffi.op_clip_gradients(g, 1.0, stats, workspace=ws)
+    buf.view(BF)[:100] = torch.randn(100, device="cuda").to(BF)
+    t.data = buf.view(BF)[:100]
+    before, rest = t.clone(), buf[50:].clone()
+    ffi.op_clip_gradients(g, 0.5 * norm_of([before]), stats, workspace=ws)
+    check([t], [before], 0.5 * norm_of([before]), stats)
+    assert torch.equal(buf[50:], rest)
+    t.data = buf[::2][:100]
+    with pytest.raises(ValueError, match="one run"):
+        ffi.op_clip_gradients(g, 1.0, stats, workspace=ws)

@@ -155,6 +155,50 @@ def test_grad_lists_refuse_what_is_not_one_run():
     assert len(ffi.GradList([t.t(), t[2:4], torch.zeros(3, 0), torch.zeros(())])) == 4
 
 
+def test_grad_lists_follow_types_and_strides_at_the_same_place():
+    """Another type, order or extent at the address and of the size that the list has seen."""
+    torch = pytest.importorskip("torch")
+    buf = torch.zeros(128)
+    t, other = buf[:60].view(6, 10), torch.zeros(5)
+    g = ffi.GradList([other, t])
+
+    def entry():
+        e = g.entries()[1]
+        return e.data, e.count, e.dtype
+
+    place = buf.data_ptr()
+    assert entry() == (place, 60, ffi.FP32) and g.changes == 1
+    g.entries()
+    assert g.changes == 1
+    g.paired = "a list"
+    t.t_()                                             # the elements in another order
+    assert entry() == (place, 60, ffi.FP32) and g.changes == 2 and g.paired is None
+    t.data = buf[:60].view(10, 6)                      # (that order's shape, another order)
+    g.entries()
+    assert g.changes == 3
+    t.data = buf.view(torch.bfloat16)[:60].view(10, 6)   # half of the bytes
+    assert entry() == (place, 60, ffi.BF16) and g.changes == 4
+    for bad in (buf.as_strided((10, 6), (7, 1)),       # beyond its elements
+                buf.as_strided((12, 5), (6, 1)),       # (strides as they were)
+                buf[:1].expand(60), buf.view(torch.int32)[:60].view(10, 6),
+                buf.view(torch.float16)[:60].view(10, 6)):
+        before = t.data
+        t.data = bad
+        for _ in range(2):
+            with pytest.raises(ValueError):
+                g.entries()
+        t.data = before
+        assert entry() == (place, 60, ffi.BF16)
+    # A list that was refused half way is laid out again when its tensors are back.
+    was = other.data
+    other.data, t.data = torch.zeros(9), buf.as_strided((10, 6), (7, 1))
+    with pytest.raises(ValueError):
+        g.entries()
+    other.data, t.data = was, before
+    assert (g.entries()[0].data, g.entries()[0].count) == (was.data_ptr(), 5)
+    assert entry() == (place, 60, ffi.BF16)
+
+
 # --------------------------------------------------- queries and keys on several axes
 
 def heads(data=P256, b=1 << 16, t=768, h=64):
