@@ -502,8 +502,9 @@ elasto_status_t elasto_qk_norm_rotate_workspace(const elasto_qk_norm_t* desc, in
  * that have theirs.  Pair f of a token turns by row positions[axis of f] and
  * column f of cos and sin.  base.positions is [batch][tokens][axes] and needed;
  * an axis' position outside [0, table_rows) makes that axis' features NaN.
- * norm = 0: the rotation alone (no weights; eps is not used), whose backward pass
- * needs no q and k (both may be NULL).  1 <= axes <= 4; everything else as above,
+ * norm = 0: the rotation alone (no weights; eps is not used), which leaves features
+ * from rot_dim on as they are, and whose backward pass needs no q and k (both may be
+ * NULL).  1 <= axes <= 4; everything else as above,
  * the workspace too. */
 typedef struct {
   elasto_qk_norm_t base;

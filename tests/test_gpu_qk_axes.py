@@ -209,3 +209,26 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         assert all(torch.equal(got[n], out[n]) for n in "qk")
         c.check_forward(out)
+
+
+@pytest.mark.parametrize("pairs,in_turn", [(False, False), (False, True), (True, False), (True, True)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("dim,sections", [(64, (12, 4, 8)), (80, (8, 0)), (256, (60, 60)), (32, (0, 0))])
+def test_the_rotation_alone_passes_on_what_it_does_not_turn(dtype, dim, sections, pairs, in_turn):
+    """Bit for bit, infinities, NaN and zeros of either sign among them, which spoil no neighbour."""
+    c = Axes(dtype, 2, 21, 3, 2, dim, sections, pairs=pairs, in_turn=in_turn, norm=False)
+    ref = c.forward()
+    d, dx, _ = c.backward(inputs=False)
+    back = {n: c.empty(n) for n in "qk"}
+    for n in "qk":
+        for t in (c.x[n], d[n]):
+            tail = t[..., c.rot:]
+            for at, v in ((0, math.inf), (3, -math.inf), (5, -0.0), (6, math.nan), (9, 0.0)):
+                tail[:, at::4, :, at] = v
+    got = c.forward()
+    ffi.op_qk_norm_rotate_axes_bwd(None, None, d["q"], d["k"], back["q"], back["k"], **c.kw)
+    bits = {BF: torch.int16, F32: torch.int32}[dtype]
+    for n in "qk":
+        for res, src, before in ((got[n], c.x[n], ref[n]), (back[n], d[n], dx[n])):
+            assert torch.equal(res[..., c.rot:].contiguous().view(bits), src[..., c.rot:].contiguous().view(bits))
+            assert torch.equal(res[..., :c.rot].contiguous().view(bits), before[..., :c.rot].contiguous().view(bits))
