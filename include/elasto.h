@@ -744,7 +744,8 @@ elasto_status_t elasto_op_grad_norm(const elasto_grad_t* grads, int32_t n, float
  * max_norm / norm) (the growth step's selective clipping has the same), rounded
  * once; stats (device float[2]) = norm, factor.  A norm that is not a finite
  * fp32 number scales nothing: factor is 0, for the step that follows to leave
- * out, and out[i] = grads[i].  out is a HOST array like grads, of the same
+ * out, and out[i] = grads[i].  With a finite norm factor is never 0: one below
+ * fp32's range scales by what it is, and is told as 2^-149.  out is a HOST array like grads, of the same
  * counts and types; out[i].data may be grads[i].data (then nothing is written where
  * nothing changes), but otherwise no result may overlap another or a gradient.
  * max_norm > 0 (INFINITY: no clipping).  Everything else as for

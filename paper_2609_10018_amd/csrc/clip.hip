@@ -158,13 +158,27 @@ __device__ __forceinline__ double total_of(const double* part, int parts, double
   return block_sum(s, red);
 }
 
-// norm and factor.  A norm that is no finite number scales nothing: the factor is 0, for the
-// caller's step to leave out.
-__device__ __forceinline__ float2 norm_and_factor(double sum, float max_norm) {
-  const float norm = (float)sqrt(sum);
-  const float factor = !(norm < INFINITY) ? 0.0f : norm > max_norm ? (float)((double)max_norm / sqrt(sum)) : 1.0f;
-  return make_float2(norm, factor);
-}
+// What the norm makes of the gradients: g becomes g a b.  A norm that is no finite number scales nothing:
+// the factor that is told is 0, for the caller's step to leave out.  A factor below fp32's normal range
+// (gradients of 1e30 clipped to 1e-20, say) is taken in two, since the results lie well inside the range,
+// and is told as no less than the smallest number above 0.
+struct Scale {
+  float norm, factor, a, b;
+  __device__ __forceinline__ Scale(double sum, float max_norm) : factor(1.0f), a(1.0f), b(1.0f) {
+    const double root = sqrt(sum);
+    norm = (float)root;
+    if (!(norm < INFINITY)) {
+      factor = 0.0f;
+    } else if (norm > max_norm) {
+      const double f = (double)max_norm / root;
+      const bool far = f < 0x1p-126;
+      a = (float)(far ? f * 0x1p125 : f);
+      b = far ? 0x1p-125f : 1.0f;
+      factor = fmaxf((float)f, 0x1p-149f);
+    }
+  }
+  __device__ __forceinline__ bool nothing() const { return a == 1.0f && b == 1.0f; }
+};
 
 __global__ __launch_bounds__(kThreads) void norm_out_kernel(const double* part, int parts, float* norm) {
   __shared__ double red[kThreads / 64];
@@ -174,7 +188,7 @@ __global__ __launch_bounds__(kThreads) void norm_out_kernel(const double* part, 
 
 // PAST: past the caches, where the gradients do not fit them.
 template <bool PAST, typename T>
-__device__ __forceinline__ void scale(const T* p, T* out, int n, float f) {
+__device__ __forceinline__ void scale(const T* p, T* out, int n, float a, float b) {
   constexpr int E = 16 / (int)sizeof(T);
   const int tid = threadIdx.x;
   const Span<T> s(p, n);
@@ -197,10 +211,10 @@ __device__ __forceinline__ void scale(const T* p, T* out, int n, float f) {
       u32x4 r;
       if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] = pack_bf16x2(v[2 * e] * f, v[2 * e + 1] * f);
+        for (int e = 0; e < 4; ++e) r[e] = pack_bf16x2(v[2 * e] * a * b, v[2 * e + 1] * a * b);
       } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] = __float_as_uint(v[e] * f);
+        for (int e = 0; e < 4; ++e) r[e] = __float_as_uint(v[e] * a * b);
       }
       if constexpr (PAST)
         __builtin_nontemporal_store(r, reinterpret_cast<u32x4*>(o));
@@ -208,34 +222,33 @@ __device__ __forceinline__ void scale(const T* p, T* out, int n, float f) {
         *reinterpret_cast<u32x4*>(o) = r;
     } else {
 #pragma unroll
-      for (int e = 0; e < E; ++e) put(o + e, v[e] * f);
+      for (int e = 0; e < E; ++e) put(o + e, v[e] * a * b);
     }
   }
-  if (tid < s.singles()) put(out + s.single(tid), head * f);
+  if (tid < s.singles()) put(out + s.single(tid), head * a * b);
 }
 
-// stats: where the call's first launch leaves norm and factor.  in_place: a factor of 1, or of 0
-// (a norm that is no finite number), leaves everything as it is.
+// stats: where the call's first launch leaves norm and factor.  in_place: where nothing is scaled everything
+// is left as it is.
 template <bool PAST>
 __global__ __launch_bounds__(kThreads) void clip_kernel(Table t, Results r, const double* part, int parts,
                                                         float max_norm, float* stats, bool in_place) {
   __shared__ double red[kThreads / 64];
-  const float2 nf = norm_and_factor(total_of(part, parts, red), max_norm);
+  const Scale by(total_of(part, parts, red), max_norm);
   if (stats && blockIdx.x == 0 && threadIdx.x == 0) {
-    stats[0] = nf.x;
-    stats[1] = nf.y;
+    stats[0] = by.norm;
+    stats[1] = by.factor;
   }
-  if (in_place && (nf.y == 1.0f || nf.y == 0.0f)) return;
-  const float f = nf.y == 0.0f ? 1.0f : nf.y;
+  if (in_place && by.nothing()) return;
   const uint32_t chunks = t.first[t.n];
   for (uint32_t b = blockIdx.x; b < chunks; b += gridDim.x) {
     const uint32_t c = chunks - 1 - b;
     const Chunk k(t, c);
     char* out = r.out[k.tensor] + k.offset;
     if (k.bf16)
-      scale<PAST>(reinterpret_cast<const uint16_t*>(k.p), reinterpret_cast<uint16_t*>(out), k.n, f);
+      scale<PAST>(reinterpret_cast<const uint16_t*>(k.p), reinterpret_cast<uint16_t*>(out), k.n, by.a, by.b);
     else
-      scale<PAST>(reinterpret_cast<const float*>(k.p), reinterpret_cast<float*>(out), k.n, f);
+      scale<PAST>(reinterpret_cast<const float*>(k.p), reinterpret_cast<float*>(out), k.n, by.a, by.b);
   }
 }
 

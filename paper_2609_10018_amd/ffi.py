@@ -981,7 +981,8 @@ def op_grad_norm(grads, norm, workspace=None, stream=None) -> None:
 
 def op_clip_gradients(grads, max_norm: float, stats, out=None, workspace=None, stream=None) -> None:
     """grads times min(1, max_norm / their norm), into out (None: grads themselves); stats: fp32 with
-    2 elements, norm and factor.  A norm that is not finite scales nothing and gives the factor 0.
+    2 elements, norm and factor.  A norm that is not finite scales nothing and gives the factor 0,
+    which no finite norm does.
     grads, out: GradLists or sequences of tensors that make one."""
     g = _grad_list(grads)
     o = g if out is None else _grad_list(out)

@@ -6,6 +6,7 @@ is rounded to fp32 once: the norm is off by at most 2^-23 relative.  The factor:
 roundings in 64 bits and one to fp32.  A result is the gradient times that factor in fp32,
 rounded to its type: finfo(type).eps / 2 + 3 * 2^-24 relative (and half of the type's smallest step).
 """
+import ctypes
 import math
 
 import pytest
@@ -224,3 +225,27 @@ def test_lists_that_have_changed_in_place_are_looked_at_again():
     t.data = buf[::2][:100]
     with pytest.raises(ValueError, match="one run"):
         ffi.op_clip_gradients(g, 1.0, stats, workspace=ws)
+
+
+@pytest.mark.parametrize("size,limit", [(1e30, 1e-20), (1e30, 1e-9), (1e36, 1.0), (1e36, 1e-30), (1e30, 1e-42)])
+def test_factors_below_the_range_of_fp32(size, limit):
+    """limit / norm is subnormal or 0 in fp32; the results are not.  The factor in two parts: one rounding
+    more in fp32 than a factor in range.  (Numbers below the smallest normal one are off by half of the smallest
+    step, twice where they are rounded to bf16 after that.)"""
+    sizes = [(4097, F32), (501, BF), (3, F32)]
+    ts = tensors(sizes, offset=1, scale=size)
+    ref, stats = norm_of(ts), torch.empty(2, device="cuda")
+    out = tensors(sizes, seed=2, offset=2)
+    ffi.op_clip_gradients(ts, limit, stats, out=out, workspace=space(ts))
+    before = [t.clone() for t in ts]
+    places = stats.tolist()
+    ffi.op_clip_gradients(ts, limit, stats, workspace=space(ts))
+    assert places == stats.tolist() and abs(places[0] - ref) <= 2.0 ** -23 * ref
+    want = ctypes.c_float(limit).value / ref
+    assert 0 < places[1] and abs(places[1] - want) <= 2.0 ** -149
+    for t, o, was in zip(ts, out, before):
+        assert torch.equal(t, o)
+        w = was.double() * want
+        step = torch.finfo(t.dtype).smallest_normal * torch.finfo(t.dtype).eps
+        assert ((o.double() - w).abs() <= (torch.finfo(t.dtype).eps / 2 + 4 * 2.0 ** -24) * w.abs() + step).all()
+        assert limit < 1e-37 or (o != 0).any()
