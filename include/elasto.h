@@ -685,7 +685,8 @@ elasto_status_t elasto_block_norm_workspace(const elasto_block_norm_t* desc, int
  * ldw, bias (or NULL) fp32 [classes].  A row of weight 0 is not used, whatever
  * it holds: its loss, lse and gradients are 0.  A label outside [0, classes)
  * makes the row's loss NaN, and the row adds nothing to the gradients.  An
- * entry of bias of -infinity leaves its class out.
+ * entry of bias of -infinity leaves its class out (its row of weight still has to hold
+ * finite numbers).
  * BF16: products of bf16 with fp32 sums, softmax in fp32; dz is rounded to bf16
  * for the products that sum it (not for dbias); dx and dweight are bf16, rounded
  * once.  FP32: fp32 throughout.  Results are the same bits every time.

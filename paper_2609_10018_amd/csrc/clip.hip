@@ -11,7 +11,8 @@
 // behind L2.
 //
 // Bound by memory: the gradients read (twice where they do not fit the cache) and written.  290 tensors of 2.5
-// GB 1375 us (5.6 TB/s over the three passes), 146 of 75 MB 44 (3.4 over two).
+// GB 1375 us (5.6 TB/s over the three passes); 146 of 75 MB 44 in the kernels (3.4 over two), 63 the call, whose
+// host side is longer.
 #include <math.h>
 
 #include <algorithm>
@@ -345,7 +346,7 @@ Plan plan_of(const elasto_grad_t* g, int n) {
   for (int i = 0; i < n; ++i) all += g[i].count > 0 ? chunks_of(g[i]) : 0;
   Plan p;
   // Gradients of more than the cache behind L2 go past the caches (5.1 GB read and written, 1454 -> 1373
-  // us with the norm; 77 MB 44 -> 46).
+  // us with the norm; 77 MB 44 -> 46 in the kernels).
   p.past = all * kChunk > ((int64_t)256 << 20);
   (void)each_launch(g, n, [&](const Table&, const int*, uint32_t chunks) {
     const int64_t share = ((int64_t)chunks * kMaxBlocks + all - 1) / all;
